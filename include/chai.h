@@ -60,7 +60,8 @@ typedef enum {
     CHAI_ERR_BAD_MEMBERSHIP = 4, /* device status word only: inconsistent membership / reps */
     CHAI_ERR_TIMEOUT = 5,        /* device status word only: a bounded device-side wait expired */
     CHAI_ERR_CUDA = 6,           /* a CUDA call failed; text in chai_last_error() */
-    CHAI_ERR_CACHE_FULL = 7      /* device status word only: chai_append_kv found seq_lens[b] outside [0, T_cap) */
+    CHAI_ERR_CACHE_FULL = 7,     /* device status word only: chai_append_kv found seq_lens[b] outside [0, T_cap) */
+    CHAI_ERR_BAD_PAGE = 8        /* device status word only: a block-table entry outside [0, n_pages) */
 } chai_status_t;
 
 typedef enum { CHAI_F32 = 0, CHAI_BF16 = 1, CHAI_FP8_E4M3 = 2 /* caches of chai_decode_attention_fp8 only */ } chai_dtype_t;
@@ -357,6 +358,94 @@ int chai_decode_attention_fp8(const void* q, const void* k_rep, const void* v, c
                               const int32_t* membership, const int32_t* reps, const int32_t* seq_lens, void* out, int B,
                               int H, int k, int T, int T_cap, int D, size_t k_batch_stride, float scale, void* workspace,
                               size_t workspace_bytes, void* stream);
+
+/*
+ * Paged caches.  Section 4.3 measures what a request's cache costs; a serving loop does not know how long a request
+ * will get, so it keeps the cache in pages from one pool and a list of page numbers per request.  A page holds
+ * page_size consecutive positions of one request, the representatives' keys (Section 3.5) and every head's values:
+ *   k_pages [n_pages,k,page_size,D], v_pages [n_pages,H,page_size,D]
+ *                        k_page_stride / v_page_stride: elements between two pages, 0 for dense (k*page_size*D and
+ *                        H*page_size*D); a larger one lets both lie side by side in one pool
+ *   block_table [B,max_pages] int32, device: position t of request b is row t % page_size of page
+ *                        block_table[b][t / page_size].  Only the entries that a call needs are read
+ *   seq_lens [B] int32, device
+ * page_size is a multiple of 8 (up to 65536), D 64 or 128.  Pages are CHAI_F32 or CHAI_BF16, or e4m3 bytes (format as
+ * for chai_quantize_cache_fp8) with one fp32 scale per ROW: k_scales [n_pages,k,page_size], v_scales
+ * [n_pages,H,page_size].  A plane's scale, as chai_quantize_cache_fp8 chooses it, needs every row of the plane at
+ * once; a row's scale is known when the row is written, so such a cache grows a token at a time.
+ * Requests may share pages that are only read.  A block-table entry outside [0, n_pages) is never turned into an
+ * address: it is reported as CHAI_ERR_BAD_PAGE in the status word of the workspace.
+ */
+
+/*
+ * Cache append, N tokens per request (one for a decode step, a prompt's worth after membership is fixed: the
+ * compaction of the key cache happens on the way in).
+ *   k_new, v_new [B,H,N,D]   the tokens' keys / values of all heads; only representatives' keys are read
+ *   new_lens [B] int32       device, or NULL (N everywhere): tokens of each request, clamped to [0, N]
+ *   For t in [0, new_lens[b]), at position p = seq_lens[b] + t:
+ *     k_pages[block_table[b][p / page_size]][c][p % page_size] = k_new[b][reps[b][c]][t]   (nothing where reps is -1)
+ *     v_pages[block_table[b][p / page_size]][h][p % page_size] = v_new[b][h][t]
+ *   Every other row stays as it was.  The pages written must belong to one request and one place of its list.
+ *   advance                  non-zero: seq_lens[b] grows by the request's tokens afterwards
+ *   workspace                NULL, or >= 256 bytes for the status word: CHAI_OK; CHAI_ERR_CACHE_FULL if some request
+ *                            had seq_lens[b] < 0 or needed positions at or beyond max_pages*page_size (that request is
+ *                            skipped); CHAI_ERR_BAD_PAGE (rows on such pages are skipped, and the request's length
+ *                            does not advance)
+ * _fp8: k_new / v_new of type dtype become e4m3 rows: scale = 2^e with the smallest e >= -126 for which the row's
+ *   largest finite magnitude is at most 448 * 2^e (1 if that magnitude is 0), byte = x / scale rounded to the nearest
+ *   e4m3 value, ties to even; an infinity saturates to +-448, a NaN stays one.  Since the scale is a power of two the
+ *   division is exact, and so is reading back to bf16: writing what was read back gives the same numbers again.
+ * k*N and H*N (rows of one request) must stay below 2^30 each, B below 65536, H at most 1024.
+ */
+int chai_append_kv_paged(const void* k_new, const void* v_new, void* k_pages, void* v_pages, const int32_t* reps,
+                         const int32_t* block_table, int32_t* seq_lens, const int32_t* new_lens, int B, int H, int k, int N,
+                         int n_pages, int page_size, int max_pages, int D, size_t k_page_stride, size_t v_page_stride,
+                         int dtype, int advance, void* workspace, void* stream);
+int chai_append_kv_paged_fp8(const void* k_new, const void* v_new, void* k_pages, void* v_pages, float* k_scales,
+                             float* v_scales, const int32_t* reps, const int32_t* block_table, int32_t* seq_lens,
+                             const int32_t* new_lens, int B, int H, int k, int N, int n_pages, int page_size, int max_pages,
+                             int D, size_t k_page_stride, size_t v_page_stride, int dtype, int advance, void* workspace,
+                             void* stream);
+
+/*
+ * Reading a paged cache back into dense arrays, as chai_prefill_attention and chai_decode_attention_ragged take them
+ * and as a request's cache is moved out of the pool: for t < min(seq_lens[b], T_out)
+ *   k_out[b][c][t] = row t of plane c, v_out[b][h][t] = row t of plane h      (k_out [B,k,T_out,D], v_out [B,H,T_out,D])
+ * Rows behind that are left as they were.  seq_lens[b] is clamped to [0, max_pages*page_size].  k_out or v_out (and
+ * then its pages and scales) may be NULL.  Rows whose page is bad are zero, with CHAI_ERR_BAD_PAGE in the workspace's
+ * status word (NULL or >= 256 bytes).  _fp8: a row is its e4m3 numbers times its scale, rounded once to dtype.
+ */
+int chai_read_kv_paged(const void* k_pages, const void* v_pages, const int32_t* block_table, const int32_t* seq_lens,
+                       void* k_out, void* v_out, int B, int H, int k, int T_out, int n_pages, int page_size, int max_pages,
+                       int D, size_t k_page_stride, size_t v_page_stride, int dtype, void* workspace, void* stream);
+int chai_read_kv_paged_fp8(const void* k_pages, const void* v_pages, const float* k_scales, const float* v_scales,
+                           const int32_t* block_table, const int32_t* seq_lens, void* k_out, void* v_out, int B, int H,
+                           int k, int T_out, int n_pages, int page_size, int max_pages, int D, size_t k_page_stride,
+                           size_t v_page_stride, int dtype, void* workspace, void* stream);
+
+/*
+ * Clustered decode attention over a paged cache, one new token per request: the operator of chai_decode_attention on
+ * the rows t < seq_lens[b] (clamped to [0, max_pages*page_size]; they include the current token).
+ *   q, out [B,H,D] of type dtype, which is the pages' type too; _fp8: CHAI_F32 or CHAI_BF16, e4m3 pages.
+ * A request of length 0 gets zero rows, and so does a request one of whose pages is bad (CHAI_ERR_BAD_PAGE) and a head
+ * whose membership cannot be resolved (CHAI_ERR_BAD_MEMBERSHIP).  Rows at or beyond a request's length are never used,
+ * whatever they hold.  Sums and softmax statistics are fp32, taken in an order that depends on the lengths alone:
+ * results are bitwise repeatable.  The workspace (chai_decode_paged_workspace_bytes: 64 KiB and (160 + B) * H * (D + 8)
+ * 32-bit words, whatever the lengths) needs no clearing; calls that share one must be ordered on one stream.
+ * H is at most 1024 and B below 65536.
+ */
+size_t chai_decode_paged_workspace_bytes(int B, int H, int D);
+int chai_decode_attention_paged(const void* q, const void* k_pages, const void* v_pages, const int32_t* membership,
+                                const int32_t* reps, const int32_t* block_table, const int32_t* seq_lens, void* out, int B,
+                                int H, int k, int n_pages, int page_size, int max_pages, int D, size_t k_page_stride,
+                                size_t v_page_stride, float scale, int dtype, void* workspace, size_t workspace_bytes,
+                                void* stream);
+int chai_decode_attention_paged_fp8(const void* q, const void* k_pages, const void* v_pages, const float* k_scales,
+                                    const float* v_scales, const int32_t* membership, const int32_t* reps,
+                                    const int32_t* block_table, const int32_t* seq_lens, void* out, int B, int H, int k,
+                                    int n_pages, int page_size, int max_pages, int D, size_t k_page_stride,
+                                    size_t v_page_stride, float scale, int dtype, void* workspace, size_t workspace_bytes,
+                                    void* stream);
 
 /* Blocking read of the status a decode/prefill call left in `workspace`
  * (synchronises `stream`).  *status_out receives a chai_status_t. */

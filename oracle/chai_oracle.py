@@ -332,3 +332,85 @@ def decode_attention_fp8(q, k8, v8, k_scale, v_scale, membership, reps, seq_lens
     k_rep = vals[np.asarray(k8)] * np.asarray(k_scale, dtype=np.float64)[:, :, None, None]
     v = vals[np.asarray(v8)] * np.asarray(v_scale, dtype=np.float64)[:, :, None, None]
     return decode_attention_ragged(q, k_rep, v, membership, reps, seq_lens, scale)
+
+
+# ---- paged caches: a request's rows lie in pages named by its block table --------------------------------
+
+def row_scales_fp8(x) -> np.ndarray:
+    """The scale of each row x[..., D]: the smallest power of two 2^e, e >= -126, with max|x| <= 448 * 2^e over the
+    row's finite elements; 1 for a row whose finite elements are all zero.  Found by trying exponents."""
+    x = np.asarray(x, dtype=np.float64)
+    top = np.where(np.isfinite(x), np.abs(x), 0.0).max(-1)
+    out = np.ones(top.shape)
+    todo = top > 0
+    for e in range(127, -127, -1):
+        out = np.where(todo & (top <= 448.0 * 2.0 ** e), 2.0 ** e, out)
+    return out
+
+
+def quantize_rows_fp8(x):
+    """x [..., D] -> (bytes uint8 [..., D], scales float64 [...]): x / scale to the nearest e4m3 value, ties to the even
+    mantissa, infinities saturated to +-448, NaN to the NaN code."""
+    x = np.asarray(x, dtype=np.float64)
+    scales = row_scales_fp8(x)
+    y = x / scales[..., None]
+    pos = e4m3_values()[:127]
+    mag = np.minimum(np.where(np.isnan(y), 0.0, np.abs(y)), 448.0)
+    hi = np.minimum(np.searchsorted(pos, mag, side="left"), 126)
+    lo = np.maximum(hi - 1, 0)
+    d_hi, d_lo = pos[hi] - mag, mag - pos[lo]
+    code = np.where((d_lo < d_hi) | ((d_lo == d_hi) & (lo % 2 == 0)), lo, hi)
+    code = np.where(pos[hi] == mag, hi, code) | np.where(np.signbit(y), 0x80, 0)
+    return np.where(np.isnan(y), code | 0x7F, code).astype(np.uint8), scales
+
+
+def paged_rows(pages, table_row, n: int) -> np.ndarray:
+    """Rows 0..n-1 of one request, [planes, n, ...], from pages [n_pages, planes, page_size, ...]."""
+    ps = pages.shape[2]
+    out = np.zeros((pages.shape[1], n) + pages.shape[3:], dtype=pages.dtype)
+    for t in range(n):
+        out[:, t] = pages[int(table_row[t // ps]), :, t % ps]
+    return out
+
+
+def append_kv_paged(k_new, v_new, k_pages, v_pages, reps, block_table, seq_lens, new_lens):
+    """Rows k_new [B,H,N,...] (representatives' only) and v_new to the positions seq_lens[b] .. of each request's pages
+    (k_pages [n_pages,k,page_size,...]); arrays of any dtype, also scales [B,H,N] into [n_pages,k,page_size].
+    A request that does not fit is skipped, rows on a bad page too, and such a request's length does not advance.
+    Returns (k_pages', v_pages', seq_lens') as new arrays."""
+    k_pages, v_pages = np.array(k_pages, copy=True), np.array(v_pages, copy=True)
+    reps = _i32(reps)
+    lens = np.array(seq_lens, dtype=np.int64, copy=True)
+    n_pages, ps = v_pages.shape[0], v_pages.shape[2]
+    for b in range(len(lens)):
+        n = min(max(int(new_lens[b]), 0), k_new.shape[2])
+        if lens[b] < 0 or (n > 0 and lens[b] + n > block_table.shape[1] * ps):
+            continue
+        good = True
+        for t in range(n):
+            pos = int(lens[b]) + t
+            page = int(block_table[b][pos // ps])
+            if not 0 <= page < n_pages:
+                good = False
+                continue
+            v_pages[page, :, pos % ps] = v_new[b, :, t]
+            for c in range(reps.shape[1]):
+                if 0 <= reps[b, c] < v_new.shape[1]:
+                    k_pages[page, c, pos % ps] = k_new[b, reps[b, c], t]
+        if good:
+            lens[b] += n
+    return k_pages, v_pages, lens
+
+
+def decode_attention_paged(q, k_pages, v_pages, membership, reps, block_table, seq_lens, scale: float):
+    """Clustered decode over pages of float64 numbers, request by request with the main definition -> [B,H,D]."""
+    q = _f64(q)
+    membership, reps = _i32(membership), _i32(reps)
+    out = np.zeros(q.shape)
+    for b in range(q.shape[0]):
+        n = min(max(int(seq_lens[b]), 0), block_table.shape[1] * v_pages.shape[2])
+        if n == 0:
+            continue
+        kr, vr = paged_rows(k_pages, block_table[b], n), paged_rows(v_pages, block_table[b], n)
+        out[b] = cha_attention(q[b:b + 1], kr[None], vr[None], membership[b:b + 1], reps[b:b + 1], scale, False)[0]
+    return out

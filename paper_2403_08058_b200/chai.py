@@ -16,7 +16,7 @@ LIB_PATH = os.path.join(_PKG, "libchai.so")
 
 CHAI_OK = 0
 CHAI_ERR_INVALID_ARG, CHAI_ERR_UNSUPPORTED, CHAI_ERR_WORKSPACE = 1, 2, 3
-CHAI_ERR_BAD_MEMBERSHIP, CHAI_ERR_TIMEOUT, CHAI_ERR_CUDA, CHAI_ERR_CACHE_FULL = 4, 5, 6, 7
+CHAI_ERR_BAD_MEMBERSHIP, CHAI_ERR_TIMEOUT, CHAI_ERR_CUDA, CHAI_ERR_CACHE_FULL, CHAI_ERR_BAD_PAGE = 4, 5, 6, 7, 8
 CHAI_F32, CHAI_BF16 = 0, 1
 
 # every symbol include/chai.h declares
@@ -31,6 +31,8 @@ EXPORTS = [
     "chai_prefill_attention_qkv", "chai_broadcast_membership", "chai_select_representatives", "chai_cluster_sweep",
     "chai_quantize_cache_fp8", "chai_decode_fp8_workspace_bytes", "chai_decode_attention_fp8",
     "chai_set_decode_wait_limit_cycles",
+    "chai_append_kv_paged", "chai_append_kv_paged_fp8", "chai_read_kv_paged", "chai_read_kv_paged_fp8",
+    "chai_decode_paged_workspace_bytes", "chai_decode_attention_paged", "chai_decode_attention_paged_fp8",
 ]
 DECODE_STATIC_SCRATCH_BYTES = 8 << 20   # CHAI_DECODE_STATIC_SCRATCH_BYTES
 
@@ -85,6 +87,14 @@ def load() -> ctypes.CDLL:
     lib.chai_device_status.argtypes = [vp, ctypes.POINTER(ci), vp]
     lib.chai_set_decode_wait_limit_cycles.argtypes = [ctypes.c_longlong]
     lib.chai_set_decode_wait_limit_cycles.restype = None
+    lib.chai_append_kv_paged.argtypes = [vp] * 8 + [ci] * 8 + [sz, sz, ci, ci, vp, vp]
+    lib.chai_append_kv_paged_fp8.argtypes = [vp] * 10 + [ci] * 8 + [sz, sz, ci, ci, vp, vp]
+    lib.chai_read_kv_paged.argtypes = [vp] * 6 + [ci] * 8 + [sz, sz, ci, vp, vp]
+    lib.chai_read_kv_paged_fp8.argtypes = [vp] * 8 + [ci] * 8 + [sz, sz, ci, vp, vp]
+    lib.chai_decode_paged_workspace_bytes.argtypes = [ci, ci, ci]
+    lib.chai_decode_paged_workspace_bytes.restype = sz
+    lib.chai_decode_attention_paged.argtypes = [vp] * 8 + [ci] * 7 + [sz, sz, cf, ci, vp, sz, vp]
+    lib.chai_decode_attention_paged_fp8.argtypes = [vp] * 10 + [ci] * 7 + [sz, sz, cf, ci, vp, sz, vp]
     lib.chai_status_string.argtypes = [ci]
     lib.chai_status_string.restype = ctypes.c_char_p
     lib.chai_last_error.restype = ctypes.c_char_p
@@ -456,6 +466,205 @@ def chai_decode_attention_fp8(q, k_rep8, v8, k_scale, v_scale, membership, reps,
                                             _ptr(membership), _ptr(reps), _ptr(seq_lens), _ptr(out), B, H, k, T, T_cap, D,
                                             stride, scale, _ptr(workspace), workspace.numel(), _stream()))
     return out
+
+
+# ---- paged caches -----------------------------------------------------------------------------------------------
+
+_PAGED_IO = {torch.float32: CHAI_F32, torch.bfloat16: CHAI_BF16}
+
+
+def _paged_call(fn, device, *args) -> None:
+    """Calls fn(*args, stream) on the device that the tensors live on, on that device's current stream."""
+    if device.index == torch.cuda.current_device():
+        _check(fn(*args, torch.cuda.current_stream().cuda_stream))
+        return
+    with torch.cuda.device(device):
+        _check(fn(*args, torch.cuda.current_stream().cuda_stream))
+
+
+def _want(t, name, shape, dtype, device) -> None:
+    if t.dtype is not dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.shape != shape:
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    if t.device != device or not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous and on {device}")
+
+
+def _pages(k_pages, v_pages, k_scales, v_scales, block_table, seq_lens):
+    """Checks a pool and its tables; returns (n_pages, k, H, page_size, D, page strides, B, max_pages, device)."""
+    if k_pages.dim() != 4 or v_pages.dim() != 4:
+        raise ValueError("k_pages must be [n_pages,k,page_size,D] and v_pages [n_pages,H,page_size,D]")
+    n, k, ps, D = k_pages.shape
+    H = v_pages.shape[1]
+    device = k_pages.device
+    if v_pages.shape != (n, H, ps, D):
+        raise ValueError("k_pages and v_pages must agree in pages, page size and head dimension")
+    if device.type != "cuda" or v_pages.device != device:
+        raise ValueError("the pages must be CUDA tensors on one device")
+    inner = (ps * D, D, 1)
+    ks, vs = k_pages.stride(), v_pages.stride()
+    if ks[1:] != inner or vs[1:] != inner:
+        if not (k_pages[0].is_contiguous() and v_pages[0].is_contiguous()):   # (strides of planes of size 1 are free)
+            raise ValueError("every page must be contiguous (pages may be any distance apart)")
+    if n > 1 and (ks[0] < k * ps * D or vs[0] < H * ps * D):
+        raise ValueError("pages must not overlap")
+    k_stride, v_stride = (ks[0], vs[0]) if n > 1 else (0, 0)
+    if k_scales is None:
+        if k_pages.dtype not in _PAGED_IO or v_pages.dtype is not k_pages.dtype:
+            raise TypeError("k_pages and v_pages must both be float32 or both bfloat16")
+    else:
+        for t in (k_pages, v_pages):
+            if t.dtype is not torch.uint8 and t.dtype is not torch.float8_e4m3fn:
+                raise TypeError(f"e4m3 pages must be uint8 or float8_e4m3fn, got {t.dtype}")
+        _want(k_scales, "k_scales", (n, k, ps), torch.float32, device)
+        _want(v_scales, "v_scales", (n, H, ps), torch.float32, device)
+    if block_table.dim() != 2:
+        raise ValueError("block_table must be [B,max_pages]")
+    B, max_pages = block_table.shape
+    _want(block_table, "block_table", (B, max_pages), torch.int32, device)
+    _want(seq_lens, "seq_lens", (B,), torch.int32, device)
+    return n, k, H, ps, D, k_stride, v_stride, B, max_pages, device
+
+
+def _paged_workspace(workspace, device):
+    """(pointer, bytes) of a workspace, which may be None."""
+    if workspace is None:
+        return None, 0
+    if workspace.device != device or not workspace.is_contiguous():
+        raise ValueError(f"workspace must be contiguous and on {device}")
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
+def _append_paged(fn_name, k_new, v_new, k_pages, v_pages, k_scales, v_scales, reps, block_table, seq_lens, new_lens,
+                  advance, workspace):
+    n, k, H, ps, D, k_stride, v_stride, B, max_pages, device = _pages(k_pages, v_pages, k_scales, v_scales, block_table,
+                                                                      seq_lens)
+    N = k_new.shape[2] if k_new.dim() == 4 else 1
+    io = _PAGED_IO.get(k_new.dtype)
+    if io is None or (k_scales is None and k_new.dtype is not k_pages.dtype):
+        raise TypeError(f"k_new of type {k_new.dtype} does not go into pages of type {k_pages.dtype}")
+    shape = (B, H, N, D) if k_new.dim() == 4 else (B, H, D)
+    _want(k_new, "k_new", shape, k_new.dtype, device)
+    _want(v_new, "v_new", shape, k_new.dtype, device)
+    _want(reps, "reps", (B, k), torch.int32, device)
+    if new_lens is not None:
+        _want(new_lens, "new_lens", (B,), torch.int32, device)
+    ws, ws_bytes = _paged_workspace(workspace, device)
+    if workspace is not None and ws_bytes < 256:
+        raise ValueError("workspace must hold at least 256 bytes")
+    scales = () if k_scales is None else (k_scales.data_ptr(), v_scales.data_ptr())
+    _paged_call(getattr(load(), fn_name), device, k_new.data_ptr(), v_new.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(),
+                *scales, reps.data_ptr(), block_table.data_ptr(), seq_lens.data_ptr(), _ptr(new_lens), B, H, k, N, n, ps,
+                max_pages, D, k_stride, v_stride, io, 1 if advance else 0, ws)
+
+
+def chai_append_kv_paged(k_new, v_new, k_pages, v_pages, reps, block_table, seq_lens, new_lens=None, advance: bool = True,
+                         workspace=None):
+    """New tokens into a paged cache: k_new, v_new [B,H,N,D] (or [B,H,D] for one token each) go to the positions
+    seq_lens[b] .. of their request's pages, keys of representatives only; new_lens [B] says how many of the N tokens
+    each request has.  seq_lens grows by them when `advance`.  k_pages [n_pages,k,page_size,D] and
+    v_pages [n_pages,H,page_size,D] may lie side by side in one pool (any distance between pages)."""
+    _append_paged("chai_append_kv_paged", k_new, v_new, k_pages, v_pages, None, None, reps, block_table, seq_lens, new_lens,
+                  advance, workspace)
+
+
+def chai_append_kv_paged_fp8(k_new, v_new, k_pages, v_pages, k_scales, v_scales, reps, block_table, seq_lens, new_lens=None,
+                             advance: bool = True, workspace=None):
+    """The same into e4m3 pages (uint8 or float8_e4m3fn) with one fp32 power-of-two scale per row: k_scales
+    [n_pages,k,page_size], v_scales [n_pages,H,page_size]; k_new / v_new float32 or bfloat16."""
+    _append_paged("chai_append_kv_paged_fp8", k_new, v_new, k_pages, v_pages, k_scales, v_scales, reps, block_table,
+                  seq_lens, new_lens, advance, workspace)
+
+
+def _read_paged(fn_name, k_pages, v_pages, k_scales, v_scales, block_table, seq_lens, T_out, dtype, k_out, v_out, workspace):
+    n, k, H, ps, D, k_stride, v_stride, B, max_pages, device = _pages(k_pages, v_pages, k_scales, v_scales, block_table,
+                                                                      seq_lens)
+    given = k_out if k_out is not None else v_out
+    if given is None:
+        if T_out is None:
+            raise ValueError("give T_out, or the arrays to read into")
+        k_out = torch.zeros((B, k, T_out, D), device=device, dtype=dtype)
+        v_out = torch.zeros((B, H, T_out, D), device=device, dtype=dtype)
+        given = k_out
+    if given.dim() != 4:
+        raise ValueError("k_out must be [B,k,T_out,D] and v_out [B,H,T_out,D]")
+    if T_out is not None and given.shape[2] != T_out:
+        raise ValueError("T_out differs from the length of the arrays to read into")
+    T_out = given.shape[2]
+    io = _PAGED_IO.get(given.dtype)
+    if io is None or (k_scales is None and given.dtype is not k_pages.dtype):
+        raise TypeError(f"pages of type {k_pages.dtype} are not read into arrays of type {given.dtype}")
+    if k_out is not None:
+        _want(k_out, "k_out", (B, k, T_out, D), given.dtype, device)
+    if v_out is not None:
+        _want(v_out, "v_out", (B, H, T_out, D), given.dtype, device)
+    ws, ws_bytes = _paged_workspace(workspace, device)
+    if workspace is not None and ws_bytes < 256:
+        raise ValueError("workspace must hold at least 256 bytes")
+    scales = () if k_scales is None else (k_scales.data_ptr(), v_scales.data_ptr())
+    _paged_call(getattr(load(), fn_name), device, k_pages.data_ptr(), v_pages.data_ptr(), *scales, block_table.data_ptr(),
+                seq_lens.data_ptr(), _ptr(k_out), _ptr(v_out), B, H, k, T_out, n, ps, max_pages, D, k_stride, v_stride, io,
+                ws)
+    return k_out, v_out
+
+
+def chai_read_kv_paged(k_pages, v_pages, block_table, seq_lens, T_out: int | None = None, k_out=None, v_out=None,
+                       workspace=None):
+    """Rows [0, min(seq_lens[b], T_out)) of a paged cache -> (k_out [B,k,T_out,D], v_out [B,H,T_out,D]).  Rows behind
+    them are left as they were (zeros in arrays made here).  With only one of k_out / v_out given only that is read."""
+    return _read_paged("chai_read_kv_paged", k_pages, v_pages, None, None, block_table, seq_lens, T_out, k_pages.dtype,
+                       k_out, v_out, workspace)
+
+
+def chai_read_kv_paged_fp8(k_pages, v_pages, k_scales, v_scales, block_table, seq_lens, T_out: int | None = None,
+                           dtype=torch.bfloat16, k_out=None, v_out=None, workspace=None):
+    """The same from e4m3 pages: each row's numbers times its scale, rounded to `dtype` (the type of arrays given)."""
+    return _read_paged("chai_read_kv_paged_fp8", k_pages, v_pages, k_scales, v_scales, block_table, seq_lens, T_out, dtype,
+                       k_out, v_out, workspace)
+
+
+def chai_decode_paged_workspace_bytes(B, H, D) -> int:
+    return int(load().chai_decode_paged_workspace_bytes(B, H, D))
+
+
+def _decode_paged(fn_name, q, k_pages, v_pages, k_scales, v_scales, membership, reps, block_table, seq_lens, scale, out,
+                  workspace):
+    n, k, H, ps, D, k_stride, v_stride, B, max_pages, device = _pages(k_pages, v_pages, k_scales, v_scales, block_table,
+                                                                      seq_lens)
+    io = _PAGED_IO.get(q.dtype)
+    if io is None or (k_scales is None and q.dtype is not k_pages.dtype):
+        raise TypeError(f"queries of type {q.dtype} do not go with pages of type {k_pages.dtype}")
+    _want(q, "q", (B, H, D), q.dtype, device)
+    _want(membership, "membership", (B, H), torch.int32, device)
+    _want(reps, "reps", (B, k), torch.int32, device)
+    if out is None:
+        out = torch.empty_like(q)
+    else:
+        _want(out, "out", (B, H, D), q.dtype, device)
+    if workspace is None:
+        workspace = new_workspace(chai_decode_paged_workspace_bytes(B, H, D), device)
+    ws, ws_bytes = _paged_workspace(workspace, device)
+    scales = () if k_scales is None else (k_scales.data_ptr(), v_scales.data_ptr())
+    _paged_call(getattr(load(), fn_name), device, q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), *scales,
+                membership.data_ptr(), reps.data_ptr(), block_table.data_ptr(), seq_lens.data_ptr(), out.data_ptr(), B, H, k,
+                n, ps, max_pages, D, k_stride, v_stride, scale, io, ws, ws_bytes)
+    return out
+
+
+def chai_decode_attention_paged(q, k_pages, v_pages, membership, reps, block_table, seq_lens, scale: float, out=None,
+                                workspace=None):
+    """Decode over a paged cache: q [B,H,D], k_pages [n_pages,k,page_size,D], v_pages [n_pages,H,page_size,D] of q's
+    type, block_table [B,max_pages] and seq_lens [B] int32 -> out [B,H,D].  A request of length 0 gets zeros."""
+    return _decode_paged("chai_decode_attention_paged", q, k_pages, v_pages, None, None, membership, reps, block_table,
+                         seq_lens, scale, out, workspace)
+
+
+def chai_decode_attention_paged_fp8(q, k_pages, v_pages, k_scales, v_scales, membership, reps, block_table, seq_lens,
+                                    scale: float, out=None, workspace=None):
+    """The same over e4m3 pages with one scale per row, as chai_append_kv_paged_fp8 writes them; q float32 or bfloat16."""
+    return _decode_paged("chai_decode_attention_paged_fp8", q, k_pages, v_pages, k_scales, v_scales, membership, reps,
+                         block_table, seq_lens, scale, out, workspace)
 
 
 def chai_set_decode_wait_limit_cycles(cycles: int) -> None:

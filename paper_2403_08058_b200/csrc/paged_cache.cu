@@ -1,0 +1,448 @@
+// What writes a paged cache and what reads it back (Section 3.5: after clustering only the representatives' keys are
+// cached; Section 4.3: every head keeps its values).
+//
+//   chai_append_kv_paged, _fp8   N new tokens per request -> rows of the request's pages, as they are or as e4m3
+//   chai_read_kv_paged, _fp8     the cached rows of every request -> dense arrays
+//
+// Both are copies, bound by HBM.  The rows (plane, token) of a request are one sequence of 16-byte vectors of the dense
+// side; a thread moves four of them with all loads issued before the first store.  Where a vector goes follows from two
+// divisions by multiplication (FastDiv).
+#include "paged.cuh"
+
+namespace chai {
+namespace {
+
+constexpr int kCopyUnroll = 4;
+constexpr int kCopyThreads = 256;
+
+__global__ void paged_reset_status_kernel(WsHeader* hdr) {
+    dependent_grid_sync();
+    reset_status(hdr);
+}
+
+// ---- row scales of e4m3 caches ----------------------------------------------------------------------------------
+
+// Bits of |x| if x is finite, else 0: positive floats order like their bits, so an integer maximum finds the largest.
+__device__ __forceinline__ unsigned finite_magnitude(float x) {
+    const unsigned a = __float_as_uint(x) & 0x7fffffffu;
+    return a < 0x7f800000u ? a : 0u;
+}
+// The smallest e >= -126 with amax <= 448 * 2^e.  448 = 1.75 * 2^8: with amax = 1.m * 2^x, e is x - 8, and one more if
+// 1.m > 1.75; adding 0x1fffff to the bits carries into the exponent exactly then.
+__device__ __forceinline__ int scale_exponent(unsigned amax_bits) {
+    const int x = (int)((amax_bits + 0x1fffffu) >> 23) - 127;
+    return max(x - 8, -126);
+}
+__device__ __forceinline__ float pow2(int e) { return __uint_as_float((unsigned)(e + 127) << 23); }
+
+template <int N>
+__device__ __forceinline__ void quantize(const float* f, float inv, unsigned* words) {  // N floats -> N bytes
+#pragma unroll
+    for (int i = 0; i < N / 4; ++i) {
+        const unsigned lo = __nv_cvt_float2_to_fp8x2(make_float2(f[4 * i] * inv, f[4 * i + 1] * inv), __NV_SATFINITE, __NV_E4M3);
+        const unsigned hi = __nv_cvt_float2_to_fp8x2(make_float2(f[4 * i + 2] * inv, f[4 * i + 3] * inv), __NV_SATFINITE, __NV_E4M3);
+        words[i] = lo | (hi << 16);
+    }
+}
+
+// ---- append -----------------------------------------------------------------------------------------------------
+
+struct AppendArgs {
+    const void *k_new, *v_new;
+    void *k_pages, *v_pages;
+    float *k_scales, *v_scales;
+    const int32_t* reps;
+    int32_t* seq_lens;
+    const int32_t* new_lens;
+    WsHeader* hdr;
+    PagePool pool;
+    FastDiv by_n;
+    int H, k, N;
+    int advance;
+};
+
+// Tokens of request b and whether they fit; the same in every thread of every block of the request.
+__device__ __forceinline__ bool tokens_fit(const AppendArgs& a, int b, int* pos0, int* n) {
+    *pos0 = a.seq_lens[b];
+    *n = a.new_lens != nullptr ? min(max(a.new_lens[b], 0), a.N) : a.N;
+    return *pos0 >= 0 && (*n == 0 || *pos0 <= a.pool.capacity - *n);
+}
+
+// grid (blocks of a request, B).  FUSED: one block per request, which also advances its length.
+template <typename TS, int D, bool FP8, bool FUSED>
+__global__ void __launch_bounds__(kCopyThreads) append_paged_kernel(const AppendArgs a) {
+    if constexpr (FUSED) dependent_grid_sync();
+    constexpr int LPR = D * (int)sizeof(TS) / 16, EPV = 16 / (int)sizeof(TS);
+    __shared__ int s_bad;
+    const int b = blockIdx.y, tid = threadIdx.x;
+    int pos0, n;
+    const bool fit = tokens_fit(a, b, &pos0, &n);
+    if constexpr (FUSED) {
+        if (tid == 0) s_bad = 0;
+        __syncthreads();  // every thread holds the position before thread 0 may advance it
+    }
+    if (!fit) {
+        if (tid == 0 && blockIdx.x == 0) flag_status(a.hdr, CHAI_ERR_CACHE_FULL, b);
+        return;
+    }
+    const int32_t* table = a.pool.block_table + (size_t)b * a.pool.max_pages;
+    const int32_t* reps = a.reps + (size_t)b * a.k;
+    const TS* k_new = static_cast<const TS*>(a.k_new) + (size_t)b * a.H * a.N * D;
+    const TS* v_new = static_cast<const TS*>(a.v_new) + (size_t)b * a.H * a.N * D;
+    const size_t total = (size_t)(a.k + a.H) * a.N * LPR;
+    const size_t per_block = (size_t)kCopyThreads * kCopyUnroll;
+    bool bad = false;
+    for (size_t base = blockIdx.x * per_block; base < total; base += gridDim.x * per_block) {
+        uint4 raw[kCopyUnroll];
+        int page[kCopyUnroll], plane[kCopyUnroll], row[kCopyUnroll];  // page -1: nothing to store
+#pragma unroll
+        for (int u = 0; u < kCopyUnroll; ++u) {
+            const size_t i = base + (size_t)u * kCopyThreads + tid;
+            const unsigned r = (unsigned)(i / LPR);
+            const int x = (int)(i % LPR);
+            plane[u] = (int)a.by_n.div(r);
+            const int t = (int)(r - (unsigned)plane[u] * (unsigned)a.N);
+            raw[u] = make_uint4(0, 0, 0, 0);
+            page[u] = -1;
+            row[u] = 0;
+            if (i >= total || t >= n) continue;
+            const unsigned pos = (unsigned)(pos0 + t), pi = a.pool.by_page.div(pos);
+            row[u] = (int)(pos - pi * (unsigned)a.pool.page_size);
+            const int pg = table[pi];
+            int head = plane[u] - a.k;
+            if (plane[u] < a.k) {
+                head = reps[plane[u]];
+                if (head < 0 || head >= a.H) continue;  // unused cluster slot
+            }
+            const TS* src = (plane[u] < a.k ? k_new : v_new) + ((size_t)head * a.N + t) * D;
+            raw[u] = ld_stream16(src + x * EPV);
+            if (pg < 0 || pg >= a.pool.n_pages) bad = true;
+            else page[u] = pg;
+        }
+#pragma unroll
+        for (int u = 0; u < kCopyUnroll; ++u) {
+            const int x = (int)((base + (size_t)u * kCopyThreads + tid) % LPR);
+            const bool key = plane[u] < a.k;
+            const int planes = key ? a.k : a.H, pl = key ? plane[u] : plane[u] - a.k;
+            const size_t at = (size_t)page[u] * (key ? a.pool.k_page_stride : a.pool.v_page_stride) +
+                              ((size_t)pl * a.pool.page_size + row[u]) * D + x * EPV;
+            if constexpr (!FP8) {
+                if (page[u] >= 0) *reinterpret_cast<uint4*>(static_cast<TS*>(key ? a.k_pages : a.v_pages) + at) = raw[u];
+            } else {
+                // the LPR lanes of a row are neighbours in one warp and take every branch together up to the store
+                float f[EPV];
+                Vec16<TS>::unpack(raw[u], f);
+                unsigned amax = 0;
+#pragma unroll
+                for (int e = 0; e < EPV; ++e) amax = max(amax, finite_magnitude(f[e]));
+#pragma unroll
+                for (int o = LPR / 2; o > 0; o >>= 1) amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, o));
+                const int e2 = amax == 0 ? 0 : scale_exponent(amax);
+                unsigned w[EPV / 4];
+                quantize<EPV>(f, pow2(-e2), w);
+                if (page[u] >= 0) {
+                    unsigned char* dst = static_cast<unsigned char*>(key ? a.k_pages : a.v_pages) + at;
+                    if constexpr (EPV == 8) *reinterpret_cast<uint2*>(dst) = make_uint2(w[0], w[1]);
+                    else *reinterpret_cast<unsigned*>(dst) = w[0];
+                    if (x == 0)
+                        (key ? a.k_scales : a.v_scales)[((size_t)page[u] * planes + pl) * a.pool.page_size + row[u]] = pow2(e2);
+                }
+            }
+        }
+    }
+    if (bad) flag_status(a.hdr, CHAI_ERR_BAD_PAGE, b);
+    if constexpr (FUSED) {
+        if (bad) s_bad = 1;
+        __syncthreads();
+        if (tid == 0 && a.advance && !s_bad) a.seq_lens[b] = pos0 + n;
+    }
+}
+
+// Advances the lengths behind an append of many blocks: every request whose tokens fit and whose pages are all good.
+__global__ void __launch_bounds__(128) advance_paged_kernel(const AppendArgs a) {
+    dependent_grid_sync();
+    const int b = blockIdx.x;
+    int pos0, n;
+    if (!tokens_fit(a, b, &pos0, &n) || n == 0) return;
+    const int32_t* table = a.pool.block_table + (size_t)b * a.pool.max_pages;
+    const unsigned last = a.pool.by_page.div((unsigned)(pos0 + n - 1));
+    bool bad = false;
+    for (unsigned p = a.pool.by_page.div((unsigned)pos0) + threadIdx.x; p <= last; p += blockDim.x)
+        bad |= table[p] < 0 || table[p] >= a.pool.n_pages;
+    bad = __syncthreads_or(bad);
+    if (threadIdx.x == 0 && !bad) a.seq_lens[b] = pos0 + n;
+}
+
+template <typename TS, int D, bool FP8>
+int launch_append(const AppendArgs& a, int B, cudaStream_t s) {
+    constexpr int LPR = D * (int)sizeof(TS) / 16;
+    const size_t total = (size_t)(a.k + a.H) * a.N * LPR, per_block = (size_t)kCopyThreads * kCopyUnroll;
+    // A decode step's tokens: one block per request moves them in a pass or two and advances the length itself, which
+    // saves a launch; a prompt's rows are spread over the GPU and the lengths follow in a launch of their own.
+    if (total <= 4 * per_block) {
+        CHAI_LAUNCH_DEPENDENT("append_paged_kernel launch", (append_paged_kernel<TS, D, FP8, true>), dim3(1, B),
+                              dim3(kCopyThreads), 0, s, a);
+        return CHAI_OK;
+    }
+    const size_t blocks = (total + per_block - 1) / per_block;
+    append_paged_kernel<TS, D, FP8, false><<<dim3((unsigned)blocks, B), kCopyThreads, 0, s>>>(a);
+    CHAI_LAUNCH_CHECK("append_paged_kernel launch");
+    if (a.advance) CHAI_LAUNCH_DEPENDENT("advance_paged_kernel launch", advance_paged_kernel, dim3(B), dim3(128), 0, s, a);
+    return CHAI_OK;
+}
+
+int append(const char* fn, bool fp8, AppendArgs a, int B, int n_pages, int page_size, int max_pages, int D,
+           const int32_t* block_table, size_t k_page_stride, size_t v_page_stride, int dtype, cudaStream_t s) {
+    CHAI_REQUIRE(a.k_new && a.v_new && a.k_pages && a.v_pages && a.reps && block_table && a.seq_lens, CHAI_ERR_INVALID_ARG,
+                 "%s: null pointer", fn);
+    CHAI_REQUIRE(!fp8 || (a.k_scales && a.v_scales), CHAI_ERR_INVALID_ARG, "%s: null pointer", fn);
+    CHAI_REQUIRE(aligned16(a.k_new) && aligned16(a.v_new) && aligned16(a.k_pages) && aligned16(a.v_pages) &&
+                     aligned16(a.k_scales) && aligned16(a.v_scales) && aligned16(a.hdr),
+                 CHAI_ERR_INVALID_ARG, "%s: pointers must be 16-byte aligned", fn);
+    CHAI_REQUIRE(dtype == CHAI_F32 || dtype == CHAI_BF16, CHAI_ERR_UNSUPPORTED, "%s: unknown dtype %d", fn, dtype);
+    const int rc = make_pool(fn, block_table, B, a.H, a.k, n_pages, page_size, max_pages, D, k_page_stride, v_page_stride,
+                             fp8 ? 1 : elem_size(dtype), &a.pool);
+    if (rc != CHAI_OK) return rc;
+    CHAI_REQUIRE(a.N > 0, CHAI_ERR_INVALID_ARG, "%s: need N > 0", fn);
+    CHAI_REQUIRE((long long)a.H * a.N < (1ll << 30), CHAI_ERR_UNSUPPORTED, "%s: H*N must be below 2^30", fn);
+    a.by_n = FastDiv((unsigned)a.N);
+    CHAI_LOG_CALL("%s: B=%d H=%d k=%d N=%d D=%d dtype=%d page_size=%d", fn, B, a.H, a.k, a.N, D, dtype, page_size);
+    if (a.hdr != nullptr)
+        CHAI_LAUNCH_DEPENDENT("paged append: status reset", paged_reset_status_kernel, dim3(1), dim3(1), 0, s, a.hdr);
+    using bf16 = __nv_bfloat16;
+    if (dtype == CHAI_BF16) {
+        if (D == 128) return fp8 ? launch_append<bf16, 128, true>(a, B, s) : launch_append<bf16, 128, false>(a, B, s);
+        return fp8 ? launch_append<bf16, 64, true>(a, B, s) : launch_append<bf16, 64, false>(a, B, s);
+    }
+    if (D == 128) return fp8 ? launch_append<float, 128, true>(a, B, s) : launch_append<float, 128, false>(a, B, s);
+    return fp8 ? launch_append<float, 64, true>(a, B, s) : launch_append<float, 64, false>(a, B, s);
+}
+
+// ---- read-back --------------------------------------------------------------------------------------------------
+
+struct ReadArgs {
+    const void *k_pages, *v_pages;
+    const float *k_scales, *v_scales;
+    const int32_t* seq_lens;
+    void *k_out, *v_out;
+    WsHeader* hdr;
+    PagePool pool;
+    FastDiv by_t;
+    int H, k, T_out;
+    int nk, nv;  // planes that are wanted
+};
+
+template <typename TO>
+__device__ __forceinline__ uint4 pack16(const float* f);
+template <>
+__device__ __forceinline__ uint4 pack16<float>(const float* f) {
+    return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+}
+template <>
+__device__ __forceinline__ uint4 pack16<__nv_bfloat16>(const float* f) {
+    uint4 r;
+    unsigned* w = &r.x;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const __nv_bfloat162 p = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
+        w[i] = *reinterpret_cast<const unsigned*>(&p);
+    }
+    return r;
+}
+
+// grid (blocks of a request, B): a thread writes four 16-byte vectors of the dense arrays.
+template <typename TO, int D, bool FP8>
+__global__ void __launch_bounds__(kCopyThreads) read_paged_kernel(const ReadArgs a) {
+    constexpr int LPR = D * (int)sizeof(TO) / 16, EPV = 16 / (int)sizeof(TO);
+    const int b = blockIdx.y, tid = threadIdx.x;
+    const int n = min(min(max(a.seq_lens[b], 0), a.pool.capacity), a.T_out);
+    const int32_t* table = a.pool.block_table + (size_t)b * a.pool.max_pages;
+    const size_t total = (size_t)(a.nk + a.nv) * a.T_out * LPR;
+    const size_t base = (size_t)blockIdx.x * kCopyThreads * kCopyUnroll;
+    TO* k_out = static_cast<TO*>(a.k_out) + (size_t)b * a.nk * a.T_out * D;
+    TO* v_out = static_cast<TO*>(a.v_out) + (size_t)b * a.nv * a.T_out * D;
+    uint4 raw[kCopyUnroll];
+    float scale[kCopyUnroll];
+    TO* dst[kCopyUnroll];
+    bool bad = false;
+#pragma unroll
+    for (int u = 0; u < kCopyUnroll; ++u) {
+        const size_t i = base + (size_t)u * kCopyThreads + tid;
+        const unsigned r = (unsigned)(i / LPR);
+        const int x = (int)(i % LPR);
+        const int plane = (int)a.by_t.div(r);
+        const int t = (int)(r - (unsigned)plane * (unsigned)a.T_out);
+        raw[u] = make_uint4(0, 0, 0, 0);
+        scale[u] = 0.f;
+        dst[u] = nullptr;
+        if (i >= total || t >= n) continue;
+        const bool key = plane < a.nk;
+        const int planes = key ? a.k : a.H, pl = key ? plane : plane - a.nk;
+        dst[u] = (key ? k_out : v_out) + ((size_t)pl * a.T_out + t) * D + x * EPV;
+        const unsigned pi = a.pool.by_page.div((unsigned)t);
+        const int row = (int)((unsigned)t - pi * (unsigned)a.pool.page_size), page = table[pi];
+        if (page < 0 || page >= a.pool.n_pages) {
+            bad = true;
+            continue;
+        }
+        const size_t at = (size_t)page * (key ? a.pool.k_page_stride : a.pool.v_page_stride) +
+                          ((size_t)pl * a.pool.page_size + row) * D + x * EPV;
+        const void* pages = key ? a.k_pages : a.v_pages;
+        if constexpr (!FP8) {
+            raw[u] = ld_stream16(static_cast<const TO*>(pages) + at);
+        } else {
+            const unsigned char* src = static_cast<const unsigned char*>(pages) + at;
+            if constexpr (EPV == 8) {
+                const uint2 w = __ldcs(reinterpret_cast<const uint2*>(src));
+                raw[u].x = w.x;
+                raw[u].y = w.y;
+            } else {
+                raw[u].x = __ldcs(reinterpret_cast<const unsigned*>(src));
+            }
+            scale[u] = (key ? a.k_scales : a.v_scales)[((size_t)page * planes + pl) * a.pool.page_size + row];
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < kCopyUnroll; ++u) {
+        if (dst[u] == nullptr) continue;
+        if constexpr (FP8) {
+            float f[EPV];
+            const unsigned w[2] = {raw[u].x, raw[u].y};
+#pragma unroll
+            for (int e = 0; e < EPV / 2; ++e) {
+                const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)((w[e / 2] >> (16 * (e & 1))) & 0xffffu), __NV_E4M3);
+                const float2 p = __half22float2(*reinterpret_cast<const __half2*>(&h));
+                f[2 * e] = p.x * scale[u];
+                f[2 * e + 1] = p.y * scale[u];
+            }
+            raw[u] = pack16<TO>(f);
+        }
+        __stcs(reinterpret_cast<uint4*>(dst[u]), raw[u]);
+    }
+    if (bad) flag_status(a.hdr, CHAI_ERR_BAD_PAGE, b);
+}
+
+template <typename TO, int D, bool FP8>
+int launch_read(const ReadArgs& a, int B, cudaStream_t s) {
+    constexpr int LPR = D * (int)sizeof(TO) / 16;
+    const size_t total = (size_t)(a.nk + a.nv) * a.T_out * LPR, per_block = (size_t)kCopyThreads * kCopyUnroll;
+    read_paged_kernel<TO, D, FP8><<<dim3((unsigned)((total + per_block - 1) / per_block), B), kCopyThreads, 0, s>>>(a);
+    CHAI_LAUNCH_CHECK("read_paged_kernel launch");
+    return CHAI_OK;
+}
+
+int read_back(const char* fn, bool fp8, ReadArgs a, int B, int n_pages, int page_size, int max_pages, int D,
+              const int32_t* block_table, size_t k_page_stride, size_t v_page_stride, int dtype, cudaStream_t s) {
+    CHAI_REQUIRE(block_table && a.seq_lens && (a.k_out || a.v_out), CHAI_ERR_INVALID_ARG, "%s: null pointer", fn);
+    CHAI_REQUIRE((!a.k_out || (a.k_pages && (!fp8 || a.k_scales))) && (!a.v_out || (a.v_pages && (!fp8 || a.v_scales))),
+                 CHAI_ERR_INVALID_ARG, "%s: null pointer to pages or scales of an output that is wanted", fn);
+    CHAI_REQUIRE(aligned16(a.k_pages) && aligned16(a.v_pages) && aligned16(a.k_out) && aligned16(a.v_out) &&
+                     aligned16(a.k_scales) && aligned16(a.v_scales) && aligned16(a.hdr),
+                 CHAI_ERR_INVALID_ARG, "%s: pointers must be 16-byte aligned", fn);
+    CHAI_REQUIRE(dtype == CHAI_F32 || dtype == CHAI_BF16, CHAI_ERR_UNSUPPORTED, "%s: unknown dtype %d", fn, dtype);
+    const int rc = make_pool(fn, block_table, B, a.H, a.k, n_pages, page_size, max_pages, D, k_page_stride, v_page_stride,
+                             fp8 ? 1 : elem_size(dtype), &a.pool);
+    if (rc != CHAI_OK) return rc;
+    CHAI_REQUIRE(a.T_out > 0, CHAI_ERR_INVALID_ARG, "%s: need T_out > 0", fn);
+    CHAI_REQUIRE((long long)a.H * a.T_out < (1ll << 30), CHAI_ERR_UNSUPPORTED, "%s: H*T_out must be below 2^30", fn);
+    a.by_t = FastDiv((unsigned)a.T_out);
+    a.nk = a.k_out != nullptr ? a.k : 0;
+    a.nv = a.v_out != nullptr ? a.H : 0;
+    CHAI_LOG_CALL("%s: B=%d H=%d k=%d T_out=%d D=%d dtype=%d page_size=%d", fn, B, a.H, a.k, a.T_out, D, dtype, page_size);
+    if (a.hdr != nullptr)
+        CHAI_LAUNCH_DEPENDENT("paged read: status reset", paged_reset_status_kernel, dim3(1), dim3(1), 0, s, a.hdr);
+    using bf16 = __nv_bfloat16;
+    if (dtype == CHAI_BF16) {
+        if (D == 128) return fp8 ? launch_read<bf16, 128, true>(a, B, s) : launch_read<bf16, 128, false>(a, B, s);
+        return fp8 ? launch_read<bf16, 64, true>(a, B, s) : launch_read<bf16, 64, false>(a, B, s);
+    }
+    if (D == 128) return fp8 ? launch_read<float, 128, true>(a, B, s) : launch_read<float, 128, false>(a, B, s);
+    return fp8 ? launch_read<float, 64, true>(a, B, s) : launch_read<float, 64, false>(a, B, s);
+}
+
+AppendArgs append_args(const void* k_new, const void* v_new, void* k_pages, void* v_pages, float* k_scales,
+                       float* v_scales, const int32_t* reps, int32_t* seq_lens, const int32_t* new_lens, int H, int k, int N,
+                       int advance, void* workspace) {
+    AppendArgs a = {};
+    a.k_new = k_new;
+    a.v_new = v_new;
+    a.k_pages = k_pages;
+    a.v_pages = v_pages;
+    a.k_scales = k_scales;
+    a.v_scales = v_scales;
+    a.reps = reps;
+    a.seq_lens = seq_lens;
+    a.new_lens = new_lens;
+    a.hdr = static_cast<WsHeader*>(workspace);
+    a.H = H;
+    a.k = k;
+    a.N = N;
+    a.advance = advance;
+    return a;
+}
+
+ReadArgs read_args(const void* k_pages, const void* v_pages, const float* k_scales, const float* v_scales,
+                   const int32_t* seq_lens, void* k_out, void* v_out, int H, int k, int T_out, void* workspace) {
+    ReadArgs a = {};
+    a.k_pages = k_pages;
+    a.v_pages = v_pages;
+    a.k_scales = k_scales;
+    a.v_scales = v_scales;
+    a.seq_lens = seq_lens;
+    a.k_out = k_out;
+    a.v_out = v_out;
+    a.hdr = static_cast<WsHeader*>(workspace);
+    a.H = H;
+    a.k = k;
+    a.T_out = T_out;
+    return a;
+}
+
+}  // namespace
+}  // namespace chai
+
+extern "C" {
+
+int chai_append_kv_paged(const void* k_new, const void* v_new, void* k_pages, void* v_pages, const int32_t* reps,
+                         const int32_t* block_table, int32_t* seq_lens, const int32_t* new_lens, int B, int H, int k, int N,
+                         int n_pages, int page_size, int max_pages, int D, size_t k_page_stride, size_t v_page_stride,
+                         int dtype, int advance, void* workspace, void* stream) {
+    return chai::append("chai_append_kv_paged", false,
+                        chai::append_args(k_new, v_new, k_pages, v_pages, nullptr, nullptr, reps, seq_lens, new_lens, H, k,
+                                          N, advance, workspace),
+                        B, n_pages, page_size, max_pages, D, block_table, k_page_stride, v_page_stride, dtype,
+                        static_cast<cudaStream_t>(stream));
+}
+
+int chai_append_kv_paged_fp8(const void* k_new, const void* v_new, void* k_pages, void* v_pages, float* k_scales,
+                             float* v_scales, const int32_t* reps, const int32_t* block_table, int32_t* seq_lens,
+                             const int32_t* new_lens, int B, int H, int k, int N, int n_pages, int page_size, int max_pages,
+                             int D, size_t k_page_stride, size_t v_page_stride, int dtype, int advance, void* workspace,
+                             void* stream) {
+    return chai::append("chai_append_kv_paged_fp8", true,
+                        chai::append_args(k_new, v_new, k_pages, v_pages, k_scales, v_scales, reps, seq_lens, new_lens, H,
+                                          k, N, advance, workspace),
+                        B, n_pages, page_size, max_pages, D, block_table, k_page_stride, v_page_stride, dtype,
+                        static_cast<cudaStream_t>(stream));
+}
+
+int chai_read_kv_paged(const void* k_pages, const void* v_pages, const int32_t* block_table, const int32_t* seq_lens,
+                       void* k_out, void* v_out, int B, int H, int k, int T_out, int n_pages, int page_size, int max_pages,
+                       int D, size_t k_page_stride, size_t v_page_stride, int dtype, void* workspace, void* stream) {
+    return chai::read_back("chai_read_kv_paged", false,
+                           chai::read_args(k_pages, v_pages, nullptr, nullptr, seq_lens, k_out, v_out, H, k, T_out, workspace),
+                           B, n_pages, page_size, max_pages, D, block_table, k_page_stride, v_page_stride, dtype,
+                           static_cast<cudaStream_t>(stream));
+}
+
+int chai_read_kv_paged_fp8(const void* k_pages, const void* v_pages, const float* k_scales, const float* v_scales,
+                           const int32_t* block_table, const int32_t* seq_lens, void* k_out, void* v_out, int B, int H,
+                           int k, int T_out, int n_pages, int page_size, int max_pages, int D, size_t k_page_stride,
+                           size_t v_page_stride, int dtype, void* workspace, void* stream) {
+    return chai::read_back("chai_read_kv_paged_fp8", true,
+                           chai::read_args(k_pages, v_pages, k_scales, v_scales, seq_lens, k_out, v_out, H, k, T_out, workspace),
+                           B, n_pages, page_size, max_pages, D, block_table, k_page_stride, v_page_stride, dtype,
+                           static_cast<cudaStream_t>(stream));
+}
+
+}  // extern "C"
