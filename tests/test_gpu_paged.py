@@ -508,3 +508,39 @@ def test_a_request_from_prompt_to_answer(cache):
                       [vr[b, :, :n[b]].double().cpu().numpy() for b in range(B)], mem.cpu().numpy(), reps.cpu().numpy(), n,
                       scale, "bf16", fp8, f"step {i}")
         assert chai.chai_device_status(ws) == chai.CHAI_OK
+
+
+# ---- waits that run out (bounded, nothing faults: see test_gpu_failure_paths.py) ---------------------------------
+
+@pytest.mark.parametrize("cache", ["bf16"])
+def test_decode_wait_that_runs_out_is_reported_and_the_next_launch_is_clean(cache, guard):
+    B, H, k, D, page, T = 2, 40, 8, 128, 16, 16000
+    gen = torch.Generator(device=DEV).manual_seed(51)
+    n_pages = B * T // page
+    mem, reps = (torch.from_numpy(x).to(DEV) for x in partition(B, H, k, 51))
+    table = torch.randperm(n_pages, generator=gen, device=DEV).to(torch.int32).view(B, -1).contiguous()
+    seq = torch.tensor([T, T - 1000], dtype=torch.int32, device=DEV)
+    q = torch.randn(B, H, D, generator=gen, device=DEV).to(torch.bfloat16)
+    if cache == "bf16":
+        pages = [torch.randn(n_pages, p, page, D, generator=gen, device=DEV).to(torch.bfloat16) for p in (k, H)]
+        scales, attend = [], chai.chai_decode_attention_paged
+    else:
+        pages = [torch.randint(0, 120, (n_pages, p, page, D), generator=gen, device=DEV, dtype=torch.uint8) for p in (k, H)]
+        scales, attend = [torch.full((n_pages, p, page), 2.0 ** -8, device=DEV) for p in (k, H)], chai.chai_decode_attention_paged_fp8
+    ws = chai.new_workspace(chai.chai_decode_paged_workspace_bytes(B, H, D), DEV)
+    out = guard.empty_like(q)
+    call = lambda: attend(q, *pages, *scales, mem, reps, table, seq, 0.01, out=out, workspace=ws)
+    want = call().clone()
+    assert chai.chai_device_status(ws) == chai.CHAI_OK and torch.isfinite(want).all()
+    # every warp goes through many times what it holds in flight: somebody has to wait for more than a cycle
+    chai.chai_set_decode_wait_limit_cycles(1)
+    try:
+        for _ in range(2):
+            call()
+            assert chai.chai_device_status(ws) == chai.CHAI_ERR_TIMEOUT
+    finally:
+        chai.chai_set_decode_wait_limit_cycles(0)
+    for _ in range(2):
+        out.zero_()
+        call()
+        assert chai.chai_device_status(ws) == chai.CHAI_OK and torch.equal(out, want)

@@ -68,6 +68,8 @@ def test_refusals(lib, name):
                 dict(B=-1), dict(page_size=-8), dict(k_stride=2 * 16 * 128 - 8), dict(v_stride=4 * 16 * 128 - 8),
                 dict(k_stride=2 * 16 * 128 + 4 if "fp8" in name else 2 * 16 * 128 + 4)):
         assert call(lib, name, **bad) == chai.CHAI_ERR_INVALID_ARG, bad
+    if name.startswith("decode"):
+        assert call(lib, name, B=65535, max_pages=1 << 15, page_size=16) == chai.CHAI_ERR_UNSUPPORTED
     for bad in (dict(page_size=4), dict(page_size=20), dict(page_size=65544), dict(D=96), dict(dtype=2), dict(dtype=-1),
                 dict(H=1025), dict(B=65536), dict(max_pages=1 << 26, page_size=16)):
         assert call(lib, name, **bad) == chai.CHAI_ERR_UNSUPPORTED, bad
