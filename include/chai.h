@@ -432,7 +432,7 @@ int chai_read_kv_paged_fp8(const void* k_pages, const void* v_pages, const float
  * whatever they hold.  Sums and softmax statistics are fp32, taken in an order that depends on the lengths alone:
  * results are bitwise repeatable.  The workspace (chai_decode_paged_workspace_bytes: 64 KiB and (160 + B) * H * (D + 8)
  * 32-bit words, whatever the lengths) needs no clearing; calls that share one must be ordered on one stream.
- * H is at most 1024, B below 65536, B * max_pages * page_size below 2^34.
+ * H is at most 1024, B below 65536, B * max_pages * page_size below 2^33.
  */
 size_t chai_decode_paged_workspace_bytes(int B, int H, int D);
 int chai_decode_attention_paged(const void* q, const void* k_pages, const void* v_pages, const int32_t* membership,

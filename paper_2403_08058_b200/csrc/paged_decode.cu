@@ -24,28 +24,33 @@
 namespace chai {
 namespace {
 
-constexpr int kWarps = 8, kThreads = kWarps * 32;
-constexpr int kMaxCtas = 160;       // the workspace bound is stated for this many; a B200 has 148 SMs
-constexpr int kQuantum = 8;         // rows; page sizes are multiples of it
-constexpr int kMaxChunkRows = 512;
-constexpr int kScoreFloats = 4096;  // scores of a chunk: clusters * rows
-constexpr int kGroupHeads = 128;    // heads a CTA handles at most
-constexpr int kJoinThreads = 256;
+constexpr int kMaxCtas = 160;     // the workspace bound is stated for this many; a B200 has 148 SMs
+constexpr int kQuantum = 8;       // rows; page sizes are multiples of it
+constexpr int kJoinThreads = 128;
+constexpr int kJoinBlocks = 37;   // blocks per head, at most
+constexpr int kOverhead = 16;     // rows; see below (a multiple of 16)
+constexpr float kProbScale = 16384.f;  // e4m3: probabilities are kept times 2^14 (see phase V)
 
-template <typename T, int D>
+template <typename T, typename TQ, int D>
 struct Geom {
     static constexpr bool FP8 = std::is_same<T, Fp8E4M3>::value;
+    static constexpr int W = std::is_same<T, __nv_bfloat16>::value ? 14 : 12, THREADS = W * 32;  // warps
     static constexpr int ROW = D * (int)sizeof(T);
-    static constexpr int TR = FP8 ? 64 : 8192 / ROW;       // rows of a tile
-    static constexpr int STAGES = FP8 && D == 64 ? 5 : 3;  // slots of a warp (about 24 KB)
-    static constexpr int LPR = ROW / 16, RPW = 32 / LPR;   // lanes a row, rows a warp-wide load (types of 2 and 4 bytes)
-    static constexpr int IT = TR / RPW;                    // ... and such loads a tile
-    // e4m3: a tile is four runs of 16 rows, each 32 bytes further than dense, so that the four lanes which read rows of
-    // the four runs at once meet different banks
-    static constexpr int RUN = FP8 ? TR / 4 : TR;
-    static constexpr int RUN_STRIDE = RUN * ROW + (FP8 ? 32 : 0);
-    static constexpr int DATA = FP8 ? 4 * RUN_STRIDE : TR * ROW;
-    static constexpr int SLOT = DATA + (FP8 ? TR * 4 : 0);  // e4m3: the rows' scales lie behind them
+    static constexpr int TR = FP8 ? 32 : 4096 / ROW;    // rows of a tile
+    static constexpr int STAGES = FP8 && D == 64 ? 6 : 3;  // slots of a warp
+    static constexpr int DATA = TR * ROW;
+    static constexpr int QUERY = DATA + (FP8 ? TR * 4 : 0);  // e4m3: the rows' scales lie behind them ...
+    static constexpr int QROW = D * (int)sizeof(TQ), SLOT = QUERY + QROW;  // ... and the query of a new cluster's keys
+    static constexpr int HEADS = 112;           // heads a CTA handles at most
+    static constexpr int SCORES = std::is_same<T, __nv_bfloat16>::value ? 4096 : 8192;  // scores of a chunk: clusters * rows
+    static constexpr int CHUNK_ROWS = 512;
+    // types of 2 and 4 bytes: lanes a row, rows a warp-wide load, such loads a tile
+    static constexpr int LPR = ROW / 16, RPW = 32 / LPR, IT = TR / RPW;
+    // e4m3: on the tensor cores a quarter of the lanes reads rows of one quarter of the tile (RUN rows), STEPS times four
+    static constexpr int RUN = 8, STEPS = 2;
+    static_assert(!FP8 || TR == 4 * RUN, "");
+    // ... and a row's 16-byte pieces lie in its 128-byte line (two rows a line for D = 64) at a place that is the piece's
+    // number xor 2 * (row / RUN), for D = 128 also xor 4 * (row % 2): the lanes of a load then meet different banks
     // how a lane holds a row of values: VPL neighbours from column col(lane) on, in the lanes that own(lane)
     static constexpr int VPL = FP8 ? D / 8 : 16 / (int)sizeof(T);
     __device__ static __forceinline__ bool own(int lane) { return FP8 ? (lane & 3) == 0 : lane < LPR; }
@@ -92,32 +97,60 @@ struct DecodeArgs {
 
 // ---- shared memory ----------------------------------------------------------------------------------------------
 
+template <int HEADS>
 struct Segment {  // the rows of one request in this CTA's piece
-    unsigned short head[kGroupHeads];     // heads, ordered by cluster
-    unsigned short cluster[kGroupHeads];  // the head's cluster, counted within this list
-    unsigned short id[kGroupHeads];       // a counted cluster's own number ...
-    unsigned short rep[kGroupHeads];      // ... and representative
+    unsigned short head[HEADS];     // heads, ordered by cluster
+    unsigned short cluster[HEADS];  // the head's cluster: its place among the clusters that have heads
+    unsigned short id[HEADS];       // at place % HEADS: the cluster's own number ...
+    unsigned short rep[HEADS];      // ... and representative
+    int first, last;                      // places of this list's clusters (heads are many to a cluster: never more places than heads)
 };
 struct Chunk {
-    int b, t0, rows, stride;  // stride: floats between two clusters' scores
+    int b, rows, stride;  // stride: floats between two clusters' scores
     int tiles, heads, clusters, run;
     int first, last, single, slot;  // first / last chunk of the segment; single: the segment is the whole request
-    int seg, bad;
+    int seg;
+    int span_end;  // > 0: the request begins here and goes on; where on the line it ends
 };
-template <int SLOT, int STAGES, int D>
+__device__ __forceinline__ int uniform(int x) { return __shfl_sync(0xffffffffu, x, 0); }  // the same in every lane, and known to be
+__device__ __forceinline__ Chunk uniform_copy(const Chunk& s) {
+    Chunk c;
+    c.b = uniform(s.b);
+    c.rows = uniform(s.rows);
+    c.stride = uniform(s.stride);
+    c.tiles = uniform(s.tiles);
+    c.heads = uniform(s.heads);
+    c.clusters = uniform(s.clusters);
+    c.run = uniform(s.run);
+    c.first = uniform(s.first);
+    c.last = uniform(s.last);
+    c.single = uniform(s.single);
+    c.slot = uniform(s.slot);
+    c.seg = uniform(s.seg);
+    c.span_end = uniform(s.span_end);
+    return c;
+}
+struct Rows {  // eight rows of a chunk: where they lie
+    size_t k, v;  // byte offsets of their row in plane 0 of the pages
+    int page, row;
+};
+template <typename G, int D>
 struct Smem {
-    alignas(128) unsigned char slot[kWarps][STAGES][SLOT];
-    alignas(16) float score[kScoreFloats];
+    alignas(128) unsigned char slot[G::W][G::STAGES][G::SLOT];
+    alignas(16) float score[G::SCORES];
     union {
-        alignas(16) float part[kWarps][D];   // phase V: sums of a head's rows that another warp finishes
-        unsigned short cl[kPagedMaxHeads];   // while a segment is prepared: every head's cluster (0xffff: unknown)
+        alignas(16) float part[G::W][D];  // phase V: sums of a head's rows that another warp finishes
+        struct {                          // while a segment is prepared, of every head:
+            alignas(16) unsigned key[kPagedMaxHeads];  // cluster * 2048 + 2 * head, + 1 for a representative
+            unsigned short mem[kPagedMaxHeads], rep[kPagedMaxHeads];
+        } all;
     };
-    float top[kGroupHeads], sum[kGroupHeads], keep[kGroupHeads];  // per cluster: running maximum and sum, rescaling factor
-    Segment seg[2];
+    float top[G::HEADS], sum[G::HEADS], keep[G::HEADS];  // per cluster: running maximum and sum, rescaling factor
+    Segment<G::HEADS> seg[2];
     Chunk chunk[2];
-    int2 at[2][kMaxChunkRows / kQuantum];  // page and row of every eighth row of the chunk
-    alignas(8) unsigned long long full[kWarps][STAGES];
-    int scan[kWarps];
+    Rows at[2][G::CHUNK_ROWS / kQuantum];
+    alignas(8) unsigned long long full[G::W][G::STAGES];
+    int scan[2][G::W];
     int found_b, found_start;
     int err, err_b, any_bad;
 };
@@ -143,11 +176,10 @@ __device__ __forceinline__ bool bar_test(uint32_t bar, uint32_t parity) {
         : "memory");
     return ok != 0;
 }
-// try_wait lets the hardware suspend the warp for a while, which a limit shorter than the default would not notice:
-// such a limit polls instead.
-__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, long long limit) {
+// A wait that does not succeed at once.  try_wait lets the hardware suspend the warp for a while, which a limit shorter
+// than the default would not notice: such a limit polls instead.
+__device__ __noinline__ bool bar_wait(uint32_t bar, uint32_t parity, long long limit) {
     const bool poll = limit < kDefaultWaitLimitCycles;
-    if (poll ? bar_test(bar, parity) : bar_try(bar, parity)) return true;
     const long long t0 = clock64();
     while (clock64() - t0 <= limit)
         if (poll ? bar_test(bar, parity) : bar_try(bar, parity)) return true;
@@ -158,21 +190,17 @@ __device__ __forceinline__ void copy_rows(uint32_t dst, const void* src, uint32_
                  "r"(bytes), "r"(bar)
                  : "memory");
 }
+// 16 bytes, of which `n` come from src and the others are zero
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, int n) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
+}
 __device__ __forceinline__ float exp2_approx(float x) {
     float y;
     asm("ex2.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-__device__ __forceinline__ uint4 lds16(uint32_t a) {
-    uint4 r;
-    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "r"(a));
-    return r;
-}
-__device__ __forceinline__ uint2 lds8(uint32_t a) {
-    uint2 r;
-    asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(r.x), "=r"(r.y) : "r"(a));
-    return r;
-}
+__device__ __forceinline__ uint4 lds16(const unsigned char* p) { return *reinterpret_cast<const uint4*>(p); }
+__device__ __forceinline__ uint2 lds8(const unsigned char* p) { return *reinterpret_cast<const uint2*>(p); }
 __device__ __forceinline__ uint64_t pack2(float x, float y) {
     uint64_t r;
     asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y));
@@ -188,9 +216,11 @@ __device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
     asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
     return d;
 }
-__device__ __forceinline__ uint32_t e4m3_pair(uint32_t two_bytes) {  // two numbers as two fp16 (exact)
-    const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)two_bytes, __NV_E4M3);
-    return (uint32_t)h.x | ((uint32_t)h.y << 16);
+// four e4m3 numbers as two pairs of fp16 (exact): the low two bytes and the high two
+__device__ __forceinline__ void e4m3_halves(uint32_t w, uint32_t* lo, uint32_t* hi) {
+    asm("{\n\t.reg .b16 x, y;\n\tmov.b32 {x, y}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, x;\n\tcvt.rn.f16x2.e4m3x2 %1, y;\n\t}"
+        : "=r"(*lo), "=r"(*hi)
+        : "r"(w));
 }
 __device__ __forceinline__ uint32_t half_pair(float x, float y) {
     const __half2 h = __floats2half2_rn(x, y);
@@ -199,11 +229,13 @@ __device__ __forceinline__ uint32_t half_pair(float x, float y) {
 __device__ __forceinline__ float2 half_floats(uint32_t h) { return __half22float2(*reinterpret_cast<const __half2*>(&h)); }
 // c += a b with a 16 x 16 (row), b 16 x 8 (col), fp16, fp32 sums
 __device__ __forceinline__ void mma16816(float* c, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-    asm volatile(
+    asm(
         "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
+// n / d for 0 <= n < 2^20, 0 < d: (n + 1/2) / d is 1/(2 d) or more away from an integer, its rounding at most n / d * 2^-22.
+__device__ __forceinline__ int small_div(int n, int d) { return (int)__fdividef((float)n + 0.5f, (float)d); }
 // A power of two f with |x| f in [1, 2) and its inverse; 1 where x is 0, tiny, infinite or NaN.
 __device__ __forceinline__ void normaliser(float x, float* f, float* inv) {
     const unsigned e = (__float_as_uint(x) >> 23) & 0xffu;
@@ -215,76 +247,94 @@ __device__ __forceinline__ void normaliser(float x, float* f, float* inv) {
 // ---- the main kernel --------------------------------------------------------------------------------------------
 
 // A warp's way through the tiles of a chunk: its share of the (cluster, tile) pairs, then of the (head, tile) pairs.
+template <int W>
 struct Walk {
     int phase, p, j, left;
+    bool fresh;  // p has changed
     __device__ __forceinline__ void start(int ph, const Chunk& c, int warp) {
         const int n = (ph == 0 ? c.clusters : c.heads) * c.tiles;
-        const int lo = n * warp / kWarps;
+        const int lo = n * warp / W;
         phase = ph;
-        left = n * (warp + 1) / kWarps - lo;
-        p = lo / c.tiles;
+        left = n * (warp + 1) / W - lo;
+        p = small_div(lo, c.tiles);
         j = lo - p * c.tiles;
+        fresh = true;
     }
     __device__ __forceinline__ void step(int tiles) {
         --left;
         if (++j == tiles) {
             j = 0;
             ++p;
+            fresh = true;
         }
     }
 };
 
 template <typename T, typename TQ, int D>
-__global__ void __launch_bounds__(kThreads, 1) paged_decode_kernel(const DecodeArgs a) {
-    using G = Geom<T, D>;
-    using S = Smem<G::SLOT, G::STAGES, D>;
+__global__ void __launch_bounds__(Geom<T, TQ, D>::THREADS, 1) paged_decode_kernel(const DecodeArgs a) {
+    using G = Geom<T, TQ, D>;
+    using S = Smem<G, D>;
+    constexpr int W = G::W, THREADS = G::THREADS;
     extern __shared__ __align__(128) unsigned char smem_raw[];
     S& sm = *reinterpret_cast<S*>(smem_raw);
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int tid = threadIdx.x, lane = tid & 31, warp = uniform(tid >> 5);
     const int ps = a.pool.page_size;
-    dependent_grid_sync();
-
     if (lane == 0) {
+        // types of 2 and 4 bytes: one arrival that announces the bytes of the bulk copies; e4m3: one a lane
         for (int s = 0; s < G::STAGES; ++s)
-            asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(smem_addr(&sm.full[warp][s])) : "memory");
+            asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_addr(&sm.full[warp][s])), "r"(G::FP8 ? 32 : 1) : "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
     if (tid == 0) sm.err = CHAI_OK, sm.err_b = -1;
+    if (tid < 5) {  // warms the address translation while the kernel before this one drains; what is there is read later
+        const void* p = tid == 0 ? (const void*)a.seq_lens : tid == 1 ? (const void*)a.membership : tid == 2 ? (const void*)a.reps
+                        : tid == 3 ? (const void*)a.pool.block_table : a.q;
+        asm volatile("prefetch.global.L2 [%0];" ::"l"(p));
+    }
+    dependent_grid_sync();
 
-    // -- the line of all rows, this CTA's piece [q_lo, q_hi) and the request it starts in
+    // -- the line of all rows, this CTA's piece [q_lo, q_hi) and the request it starts in.  A request counts
+    // kOverhead rows more than it has, in front: what a CTA loses where one request ends and the next begins.
     auto length = [&](int b) { return min(max(a.seq_lens[b], 0), a.pool.capacity); };
-    auto quanta = [](int n) { return (n + kQuantum - 1) / kQuantum; };
-    const int per = (a.B + kThreads - 1) / kThreads;
+    const int per = (a.B + THREADS - 1) / THREADS;
     const int b_lo = min(tid * per, a.B), b_hi = min(b_lo + per, a.B);
-    int mine = 0;
-    for (int b = b_lo; b < b_hi; ++b) mine += quanta(length(b));
-    int upto = mine;
+    int mine8 = 0, mine16 = 0;  // in units of eight and of sixteen rows
+    for (int b = b_lo; b < b_hi; ++b) {
+        const int n = length(b);
+        mine8 += n > 0 ? (n + 7 + kOverhead) / 8 : 0;
+        mine16 += n > 0 ? (n + 15 + kOverhead) / 16 : 0;
+    }
+    int upto8 = mine8, upto16 = mine16;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-        const int x = __shfl_up_sync(0xffffffffu, upto, o);
-        if (lane >= o) upto += x;
+        const int x = __shfl_up_sync(0xffffffffu, upto8, o), y = __shfl_up_sync(0xffffffffu, upto16, o);
+        if (lane >= o) upto8 += x, upto16 += y;
     }
-    if (lane == 31) sm.scan[warp] = upto;
+    if (lane == 31) sm.scan[0][warp] = upto8, sm.scan[1][warp] = upto16;
     __syncthreads();
-    int total = 0;
-    for (int w = 0; w < kWarps; ++w) {
-        if (w < warp) upto += sm.scan[w];
-        total += sm.scan[w];
+    int total8 = 0, total16 = 0;
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+        const int x = sm.scan[0][w], y = sm.scan[1][w];
+        if (w < warp) upto8 += x, upto16 += y;
+        total8 += x;
+        total16 += y;
     }
     // Heads are dealt to several CTAs when a piece would be shorter than 32 rows, down to 4 heads a CTA.
-    int groups = (a.H + kGroupHeads - 1) / kGroupHeads;
-    while ((long long)total * groups < 4ll * gridDim.x && 8 * groups <= a.H && 2 * groups <= (int)gridDim.x) groups *= 2;
-    const int pieces = max(1, min((int)gridDim.x / groups, total));
-    const int piece = blockIdx.x / groups, group = blockIdx.x - piece * groups;
-    const bool by_request = a.n_desc == a.B;  // descriptions are kept per request, or (more requests than CTAs) per piece
-    if (!by_request && (int)blockIdx.x >= pieces && (int)blockIdx.x < a.n_desc && tid == 0) a.ws.desc[blockIdx.x] = make_int4(-1, 0, 0, 0);
-    for (int b = blockIdx.x; b < a.B; b += gridDim.x) {  // requests without rows: zeros
-        if (length(b) > 0) continue;
-        if (by_request && tid == 0) a.ws.desc[b] = make_int4(-1, 0, 0, 0);
-        uint4* o = reinterpret_cast<uint4*>(static_cast<TQ*>(a.out) + (size_t)b * a.H * D);
-        for (int i = tid; i < a.H * D * (int)sizeof(TQ) / 16; i += kThreads) o[i] = make_uint4(0, 0, 0, 0);
-    }
-    auto piece_start = [&](int i) { return (int)((long long)i * total / pieces); };
+    const int n_ctas = gridDim.x;
+    const int base_groups = (a.H + G::HEADS - 1) / G::HEADS;
+    int group_log = 0, most_pieces = base_groups == 1 ? n_ctas : small_div(n_ctas, base_groups);
+    while (total8 < 4 * most_pieces && (8 * base_groups << group_log) <= a.H && most_pieces > 1) ++group_log, most_pieces >>= 1;
+    const int groups = base_groups << group_log;
+    // Pieces are cut in units of sixteen rows where that is fine enough (twelve a piece): copies are longer then.
+    const bool coarse = total16 >= 12 * most_pieces;
+    const int unit_log = coarse ? 4 : 3, total = coarse ? total16 : total8, overhead = kOverhead >> unit_log;
+    const int upto = coarse ? upto16 : upto8, mine = coarse ? mine16 : mine8;
+    auto quanta = [&](int n) { return n > 0 ? (n + (1 << unit_log) - 1 + kOverhead) >> unit_log : 0; };
+    const int pieces = max(1, min(most_pieces, total));
+    const int piece = base_groups == 1 ? (int)blockIdx.x >> group_log : small_div(blockIdx.x, groups), group = blockIdx.x - piece * groups;
+    const int each = total / pieces, rest = total - each * pieces;  // (piece * total / pieces without 64-bit division)
+    auto piece_start = [&](int i) { return i * each + small_div(i * rest, pieces); };  // (i and rest are at most kMaxCtas)
     const bool work = piece < pieces && total > 0;
     const int q_lo = work ? piece_start(piece) : 0, q_hi = work ? piece_start(piece + 1) : 0;
     if (work && mine > 0 && q_lo >= upto - mine && q_lo < upto) {
@@ -297,123 +347,130 @@ __global__ void __launch_bounds__(kThreads, 1) paged_decode_kernel(const DecodeA
 
     // -- state of the division into segments and chunks, the same in every thread
     int q_at = q_lo, b = work ? sm.found_b : 0, b_start = work ? sm.found_start : 0;
-    int seg_t = 0, seg_end = 0, seg_par = 1, seg_rows = 0, seg_heads = 0, seg_clusters = 0, seg_slot = 0;
+    int seg_t = 0, seg_end = 0, seg_par = 1, seg_rows = 0, seg_heads = 0, seg_clusters = 0, seg_slot = 0, span_end = 0;
     bool seg_single = false, seg_first = false;
-    bool opened_span = false;
 
-    // Prepares the next chunk into buffer `par`; false if the piece is done.  Called by all threads together.
+    // Prepares the next chunk into buffer `par`; false if the piece is done.  Called by all threads together, which
+    // meet at a barrier afterwards.
     auto prepare = [&](int par) -> bool {
-        if (seg_t >= seg_end) {
+        bool fresh = false, from_start = false;
+        while (seg_t >= seg_end) {  // the next request that has rows here
             if (q_at >= q_hi) return false;
             int n = length(b);
             while (q_at >= b_start + quanta(n)) {
                 b_start += quanta(n);
                 n = length(++b);
             }
-            const int nq = quanta(n), q_end = min(q_hi, b_start + nq);
-            seg_t = (q_at - b_start) * kQuantum;
-            seg_end = min(n, (q_end - b_start) * kQuantum);
-            seg_single = q_at == b_start && q_end == b_start + nq;
-            seg_first = true;
+            const int stop = b_start + quanta(n), rows_at = b_start + overhead, q_end = min(q_hi, stop);
+            from_start = q_at <= rows_at;
+            seg_t = max(q_at - rows_at, 0) << unit_log;
+            seg_end = q_end > rows_at ? min(n, (q_end - rows_at) << unit_log) : seg_t;
+            seg_single = from_start && q_end == stop;
+            span_end = from_start && !seg_single ? stop : 0;
             seg_slot = piece + b;
-            seg_par ^= 1;
-            Segment& sg = sm.seg[seg_par];
-            const bool opens = q_at == b_start && group == 0;  // this CTA answers for the request's unknown heads
-            if (q_at == b_start && !seg_single) opened_span = true;
-            if (tid == 0 && opens && (by_request || !seg_single)) {
-                const long long last = b_start + nq - 1;
-                const int end = (int)(((last + 1) * pieces - 1) / total);
-                a.ws.desc[by_request ? b : piece] = make_int4(seg_single ? -1 : b, seg_slot, end - piece + 1, 0);
-            }
             q_at = q_end;
+            fresh = true;
+        }
+        // pages of the rows that the chunk may have (how many it has follows from the number of clusters)
+        const int32_t* table = a.pool.block_table + (size_t)b * a.pool.max_pages;
+        const int reach = min(seg_end - seg_t, fresh ? G::CHUNK_ROWS : seg_rows);
+        int page = 0, row = 0;
+        static_assert(G::CHUNK_ROWS / kQuantum <= THREADS, "one thread looks up eight rows");
+        if (tid * kQuantum < reach) {
+            const unsigned pos = (unsigned)(seg_t + tid * kQuantum), pi = a.pool.by_page.div(pos);
+            page = table[pi];
+            row = (int)(pos - pi * (unsigned)ps);
+        }
+        if (fresh) {
+            seg_par ^= 1;
+            seg_first = true;
+            auto& sg = sm.seg[seg_par];
+            const bool opens = from_start && group == 0;  // this CTA answers for the request's unknown heads
             // heads ordered by cluster; unknown ones get zeros and are left out
+            const int32_t* mem = a.membership + (size_t)b * a.H;
             const int32_t* reps = a.reps + (size_t)b * a.k;
-            int known = 0;
-            for (int h0 = 0; h0 < a.H; h0 += kThreads) {
-                const int h = h0 + tid;
-                int c = 0xffff, r;
-                bool ok = false;
-                if (h < a.H) {
-                    ok = resolve_head(a.membership, a.reps, b, h, a.H, a.k, &c, &r);
-                    sm.cl[h] = ok ? (unsigned short)c : 0xffff;
-                    if (!ok && opens) {
-                        atomicCAS(&sm.err, CHAI_OK, CHAI_ERR_BAD_MEMBERSHIP);
-                        sm.err_b = b;
-                        if (!seg_single) a.ws.ml[(size_t)seg_slot * a.H + h] = make_float2(0.f, -1.f);
-                        TQ* o = static_cast<TQ*>(a.out) + ((size_t)b * a.H + h) * D;
-                        for (int d = 0; d < D; ++d) o[d] = from_float<TQ>(0.f);
-                    }
-                }
-                known += __syncthreads_count(ok);
+            const int padded = (a.H + 7) & ~7;
+            for (int h = tid; h < a.H; h += THREADS) {
+                const unsigned c = (unsigned)mem[h], r = h < a.k ? (unsigned)reps[h] : 0u;
+                sm.all.mem[h] = c < (unsigned)a.k ? (unsigned short)c : 0xffff;
+                sm.all.rep[h] = r < (unsigned)a.H ? (unsigned short)r : 0xffff;
             }
-            const int lo = (int)((long long)known * group / groups), hi = (int)((long long)known * (group + 1) / groups);
-            for (int h = tid; h < a.H; h += kThreads) {
-                const unsigned c = sm.cl[h];
-                if (c == 0xffff) continue;
-                int rank = 0;
-                for (int x = 0; x < a.H; ++x) rank += sm.cl[x] < c || (sm.cl[x] == c && x < h);
+            if (tid == 0) sm.any_bad = 0;
+            __syncthreads();
+            int known = 0;
+            for (int h0 = 0; h0 < padded; h0 += THREADS) {
+                const int h = h0 + tid;
+                bool ok = false;
+                unsigned c = 0xffff, r = 0xffff;
+                if (h < a.H) {
+                    c = sm.all.mem[h];
+                    if (c != 0xffff) r = sm.all.rep[c];
+                    ok = r != 0xffff && sm.all.mem[r] == c;
+                }
+                if (h < padded) sm.all.key[h] = ok ? c * 2048 + 2 * h + (r == (unsigned)h) : 0xfffffffeu;
+                known += __syncthreads_count(ok);
+                if (h < a.H && !ok && opens) {
+                    atomicCAS(&sm.err, CHAI_OK, CHAI_ERR_BAD_MEMBERSHIP);
+                    sm.err_b = b;
+                    if (!seg_single) a.ws.ml[(size_t)seg_slot * a.H + h] = make_float2(0.f, -1.f);
+                    TQ* o = static_cast<TQ*>(a.out) + ((size_t)b * a.H + h) * D;
+                    for (int d = 0; d < D; ++d) o[d] = from_float<TQ>(0.f);
+                }
+            }
+            const int lo = groups == 1 ? 0 : small_div(known * group, groups), hi = groups == 1 ? known : small_div(known * (group + 1), groups);
+            for (int h = tid; h < a.H; h += THREADS) {
+                const unsigned own = sm.all.key[h], c = own / 2048;
+                if (own == 0xfffffffeu) continue;
+                int rank = 0, place = 0;  // heads before this one, clusters (their representatives) before its own
+#pragma unroll 2
+                for (int x = 0; x < padded; x += 4) {
+                    const uint4 u = *reinterpret_cast<const uint4*>(&sm.all.key[x]);
+                    rank += (u.x < own) + (u.y < own) + (u.z < own) + (u.w < own);
+                    place += (u.x & (u.x < c * 2048)) + (u.y & (u.y < c * 2048)) + (u.z & (u.z < c * 2048)) + (u.w & (u.w < c * 2048));
+                }
                 if (rank >= lo && rank < hi) {
                     sg.head[rank - lo] = (unsigned short)h;
-                    sg.cluster[rank - lo] = (unsigned short)c;
+                    sg.cluster[rank - lo] = (unsigned short)place;
+                    sg.id[place % G::HEADS] = (unsigned short)c;
+                    sg.rep[place % G::HEADS] = sm.all.rep[c];
+                    if (rank == lo) sg.first = place;
+                    if (rank == hi - 1) sg.last = place;
                 }
             }
             __syncthreads();
             seg_heads = hi - lo;
-            // number the clusters that occur: one warp, 32 heads at a time
-            if (warp == 0) {
-                int before = 0;
-                for (int i0 = 0; i0 < seg_heads; i0 += 32) {
-                    const int i = i0 + lane;
-                    const int c = i < seg_heads ? sg.cluster[i] : -1;
-                    const bool opens_cluster = i < seg_heads && (i == 0 || sm.cl[sg.head[i - 1]] != c);
-                    const unsigned bits = __ballot_sync(0xffffffffu, opens_cluster);
-                    const int idx = before + __popc(bits & (0xffffffffu >> (31 - lane))) - 1;
-                    if (opens_cluster) {
-                        sg.id[idx] = (unsigned short)c;
-                        sg.rep[idx] = (unsigned short)reps[c];
-                    }
-                    __syncwarp();
-                    if (i < seg_heads) sg.cluster[i] = (unsigned short)idx;
-                    before += __popc(bits);
-                }
-                if (lane == 0) sm.scan[0] = before;
-            }
-            if (tid == 0) sm.any_bad = 0;
-            __syncthreads();
-            seg_clusters = sm.scan[0];
-            const int most = min(kMaxChunkRows, kScoreFloats / max(seg_clusters, 1) / kQuantum * kQuantum);
-            const int rows = seg_end - seg_t, chunks = (rows + most - 1) / most;
-            seg_rows = ((rows + chunks - 1) / chunks + kQuantum - 1) / kQuantum * kQuantum;
+            seg_clusters = seg_heads > 0 ? sg.last - sg.first + 1 : 0;
+            seg_rows = min(G::CHUNK_ROWS, small_div(G::SCORES, max(seg_clusters, 1)) / G::TR * G::TR);
         }
         const int rows = min(seg_rows, seg_end - seg_t);
-        const int32_t* table = a.pool.block_table + (size_t)b * a.pool.max_pages;
-        bool bad = false;
-        for (int i = tid; i * kQuantum < rows; i += kThreads) {
-            const unsigned pos = (unsigned)(seg_t + i * kQuantum), pi = a.pool.by_page.div(pos);
-            int page = table[pi];
+        if (tid * kQuantum < reach) {
             if (page < 0 || page >= a.pool.n_pages) {
-                bad = true;
+                sm.any_bad = 1;  // of the segment so far
                 page = 0;
             }
-            sm.at[par][i] = make_int2(page, (int)(pos - pi * (unsigned)ps));
+            Rows r;
+            r.k = ((size_t)page * a.pool.k_page_stride + (size_t)row * D) * sizeof(T);
+            r.v = ((size_t)page * a.pool.v_page_stride + (size_t)row * D) * sizeof(T);
+            r.page = page;
+            r.row = row;
+            sm.at[par][tid] = r;
         }
-        if (bad) sm.any_bad = 1;  // of the segment so far
         if (tid == 0) {
             Chunk& c = sm.chunk[par];
             c.b = b;
-            c.t0 = seg_t;
             c.rows = rows;
-            c.stride = (rows + 7) & ~7;
+            c.stride = (rows + G::TR - 1) / G::TR * G::TR;
             c.tiles = (rows + G::TR - 1) / G::TR;
             c.heads = seg_heads;
             c.clusters = seg_clusters;
             const int align = ps | seg_t;
-            c.run = min(align & -align, G::RUN);
+            c.run = min(align & -align, G::TR);
             c.first = seg_first;
             c.last = seg_t + rows >= seg_end;
             c.single = seg_single;
             c.slot = seg_slot;
             c.seg = seg_par;
+            c.span_end = span_end;
         }
         seg_first = false;
         seg_t += rows;
@@ -423,67 +480,123 @@ __global__ void __launch_bounds__(kThreads, 1) paged_decode_kernel(const DecodeA
     // -- the warp's own slots
     int issued = 0, used = 0, in_slot = 0, out_slot = 0, out_phase = 0;  // tiles started / finished; next slot of each
     bool dead = false;                                                   // a wait ran out: no more copies, no more waits
-    Walk ahead;                                                          // the next tile to start, of chunk number ahead_no
-    int ahead_no = 0, ahead_par = 0, ready_no = 0;                       // chunks up to ready_no are prepared
+    Walk<W> ahead;                                                       // the next tile to start, of chunk number ahead_no
+    int ahead_no = 0, ahead_par = 1, ready_no = 0;                       // chunks up to ready_no are prepared
+    Chunk ahead_chunk = {};                                              // that chunk
+    const char* ahead_plane = nullptr;                                   // the plane of the next tile, in page 0 ...
+    [[maybe_unused]] const float* ahead_scales = nullptr;                // ... its rows' scales ...
+    const char* ahead_query = nullptr;                                   // ... and, of keys, the query
     ahead.left = 0;
     ahead.phase = 1;
+    const size_t plane_bytes = (size_t)ps * D * sizeof(T);
+    const uint32_t slots = smem_addr(sm.slot[warp][0]), bars = smem_addr(&sm.full[warp][0]);
+    // e4m3: a lane's place in a warp-wide copy of 512 bytes, apart from the change by the row's quarter
+    const int copy_at = G::FP8 ? (D == 128 ? (lane >> 3) * 128 + 16 * ((lane & 7) ^ (4 * ((lane >> 3) & 1)))
+                                           : (lane >> 3) * 128 + 16 * (lane & 7))
+                               : 0;
 
-    auto start_tile = [&](const Chunk& c, const Walk& w, int par) {
-        const int row0 = w.j * G::TR, rows = min(G::TR, c.rows - row0);
-        const Segment& sg = sm.seg[c.seg];
-        const int plane = w.phase == 0 ? sg.id[w.p] : sg.head[w.p];
-        const int planes = w.phase == 0 ? a.k : a.H;
-        const uint32_t slot = smem_addr(sm.slot[warp][in_slot]), bar = smem_addr(&sm.full[warp][in_slot]);
-        if (lane == 0) {
-            const uint32_t bytes = rows * G::ROW + (G::FP8 ? ((rows + 3) & ~3) * 4 : 0);
-            asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
-        }
-        __syncwarp();
-        const int r0 = lane * c.run;
-        if (r0 < rows) {
-            const int n = min(c.run, rows - r0);
-            const int2 at = sm.at[par][(row0 + r0) / kQuantum];
-            const size_t stride = w.phase == 0 ? a.pool.k_page_stride : a.pool.v_page_stride;
-            const size_t elem = (size_t)at.x * stride + ((size_t)plane * ps + at.y) * D;
-            const char* src = static_cast<const char*>(w.phase == 0 ? a.k_pages : a.v_pages) + elem * sizeof(T);
-            const uint32_t dst = slot + (G::FP8 ? (r0 / G::RUN) * G::RUN_STRIDE + (r0 % G::RUN) * G::ROW : r0 * G::ROW);
-            copy_rows(dst, src, n * G::ROW, bar);
-            if constexpr (G::FP8) {
-                const float* scales = (w.phase == 0 ? a.k_scales : a.v_scales) + ((size_t)at.x * planes + plane) * ps + at.y;
-                copy_rows(slot + G::DATA + r0 * 4, scales, ((n + 3) & ~3) * 4, bar);
+    // The next tile to start, with its addresses worked out ahead of time: the shared-memory reads that they take pass
+    // behind the arithmetic of the tile before.
+    bool staged = false, next_query = false;
+    int next_rows = 0;
+    [[maybe_unused]] int next_run = 0;
+    constexpr int GROUPS = G::TR / kQuantum;
+    const char* next_src[G::FP8 ? GROUPS : 1] = {};
+    [[maybe_unused]] const float* next_scales = nullptr;
+    auto stage = [&]() __attribute__((always_inline)) {
+        while (ahead.left == 0) {
+            if (ahead.phase == 0) {
+                ahead.start(1, ahead_chunk, warp);
+            } else {
+                if (ahead_no >= ready_no) return;
+                ++ahead_no;
+                ahead_par ^= 1;
+                ahead_chunk = uniform_copy(sm.chunk[ahead_par]);
+                ahead.start(0, ahead_chunk, warp);
             }
         }
-        in_slot = in_slot + 1 == G::STAGES ? 0 : in_slot + 1;
-        ++issued;
+        const bool key = ahead.phase == 0;
+        next_query = key && ahead.fresh;
+        if (ahead.fresh) {
+            ahead.fresh = false;
+            const auto& sg = sm.seg[ahead_chunk.seg];
+            const int plane = key ? sg.id[(sg.first + ahead.p) % G::HEADS] : sg.head[ahead.p];
+            ahead_plane = static_cast<const char*>(key ? a.k_pages : a.v_pages) + plane * plane_bytes;
+            if constexpr (G::FP8) ahead_scales = (key ? a.k_scales : a.v_scales) + plane * (size_t)ps;
+            if (key)
+                ahead_query = static_cast<const char*>(a.q) +
+                              ((size_t)ahead_chunk.b * a.H + sg.rep[(sg.first + ahead.p) % G::HEADS]) * G::QROW;
+        }
+        const int row0 = ahead.j * G::TR;
+        next_rows = min(G::TR, ahead_chunk.rows - row0);
+        const Rows* at = &sm.at[ahead_par][row0 / kQuantum];
+        if constexpr (!G::FP8) {
+            const Rows& r = at[min(lane * ahead_chunk.run, next_rows - 1) / kQuantum];
+            next_src[0] = ahead_plane + (key ? r.k : r.v);
+            next_run = ahead_chunk.run;
+        } else {
+            // (rows that are not there: an address that is not read)
+#pragma unroll
+            for (int g = 0; g < GROUPS; ++g) {
+                const Rows& r = at[min(g * kQuantum, next_rows - 1) / kQuantum];
+                next_src[g] = ahead_plane + lane * 16 + (key ? r.k : r.v);
+            }
+            const Rows& r = at[min(lane * 4, next_rows - 1) / kQuantum];
+            next_scales = ahead_scales + (size_t)r.page * (size_t)((key ? a.k : a.H) * ps) + (r.row + (lane & 1) * 4);
+        }
+        ahead.step(ahead_chunk.tiles);
+        staged = true;
     };
-    auto fill = [&]() {
-        while (!dead && issued - used < G::STAGES) {
-            while (ahead.left == 0) {
-                if (ahead.phase == 0) {
-                    ahead.start(1, sm.chunk[ahead_par], warp);
+    // Starts copies until the warp's slots are in flight or nothing is known to copy.
+    auto fill = [&]() __attribute__((always_inline)) {
+#pragma unroll 1
+        while (!dead) {
+            if (staged) {
+                if (issued - used == G::STAGES) return;
+                const uint32_t slot = slots + in_slot * G::SLOT, bar = bars + in_slot * 8;
+                if constexpr (!G::FP8) {
+                    if (lane == 0)
+                        asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar),
+                                     "r"(next_rows * G::ROW + (next_query ? G::QROW : 0))
+                                     : "memory");
+                    __syncwarp();
+                    const int r0 = lane * next_run;
+                    if (r0 < next_rows) copy_rows(slot + r0 * G::ROW, next_src[0], min(next_run, next_rows - r0) * G::ROW, bar);
+                    if (next_query && lane == 31) copy_rows(slot + G::QUERY, ahead_query, G::QROW, bar);
                 } else {
-                    if (ahead_no >= ready_no) return;
-                    ++ahead_no;
-                    ahead_par ^= 1;
-                    ahead.start(0, sm.chunk[ahead_par], warp);
+                    // 16 bytes a lane, and as many of the scales; behind the last row the tile is filled with zeros
+                    const int left = next_rows - lane / (G::ROW / 16);
+#pragma unroll
+                    for (int g = 0; g < GROUPS; ++g) {
+                        const uint32_t dst = slot + g * (kQuantum * G::ROW) + (copy_at ^ (32 * (g * kQuantum / G::RUN)));
+#pragma unroll
+                        for (int u = 0; u < kQuantum * G::ROW / 512; ++u)
+                            copy16(dst + u * 512, next_src[g] + u * 512, left > g * kQuantum + u * (512 / G::ROW) ? 16 : 0);
+                    }
+                    if (lane < G::TR / 4) copy16(slot + G::DATA + lane * 16, next_scales, min(max(next_rows - lane * 4, 0), 4) * 4);
+                    if (next_query && lane * 16 < G::QROW) copy16(slot + G::QUERY + lane * 16, ahead_query + lane * 16, 16);
+                    asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
                 }
+                in_slot = in_slot + 1 == G::STAGES ? 0 : in_slot + 1;
+                ++issued;
+                staged = false;
             }
-            const Chunk& c = sm.chunk[ahead_par];
-            start_tile(c, ahead, ahead_par);
-            ahead.step(c.tiles);
+            stage();
+            if (!staged) return;
         }
     };
-    // Waits for the warp's next tile; false if the wait ran out, now or earlier.
-    auto take = [&](uint32_t* tile) -> bool {
-        if (dead) return false;
-        if (!bar_wait(smem_addr(&sm.full[warp][out_slot]), out_phase, a.wait_limit)) dead = true;
-        dead = __any_sync(0xffffffffu, dead);
-        if (dead) {
-            if (lane == 0) sm.err = CHAI_ERR_TIMEOUT;
-            return false;
+    // Waits for the warp's next tile; nothing if the wait ran out, now or earlier.
+    auto take = [&]() -> const unsigned char* {
+        if (dead) return nullptr;
+        const uint32_t bar = bars + out_slot * 8;
+        if (!__all_sync(0xffffffffu, bar_test(bar, out_phase))) {
+            dead = __any_sync(0xffffffffu, !bar_wait(bar, out_phase, a.wait_limit));
+            if (dead) {
+                if (lane == 0) sm.err = CHAI_ERR_TIMEOUT;
+                return nullptr;
+            }
         }
-        *tile = smem_addr(sm.slot[warp][out_slot]);
-        return true;
+        return sm.slot[warp][out_slot];
     };
     auto release = [&]() {
         ++used;
@@ -492,40 +605,47 @@ __global__ void __launch_bounds__(kThreads, 1) paged_decode_kernel(const DecodeA
             out_phase ^= 1;
         }
         __syncwarp();  // every lane has read the tile before a copy overwrites it
-        fill();
     };
 
     // -- chunk by chunk
+    const bool by_request = a.n_desc == a.B;  // descriptions are kept per request, or (more requests than CTAs) per piece
+    bool opened_span = false;
     int no = 0, par = 1;
     bool more = prepare(0);
     __syncthreads();
-    if (more) ready_no = 1, ahead_par = 1;
-    fill();
+    if (more) ready_no = 1;
+#pragma unroll 1
     while (more) {
         ++no;
         par ^= 1;
-        const Chunk c = sm.chunk[par];
-        const Segment& sg = sm.seg[c.seg];
+        const Chunk c = uniform_copy(sm.chunk[par]);
+        const auto& sg = sm.seg[c.seg];
+        const int first_place = uniform(sg.first);
 
         // K: scores of the warp's tiles, in powers of two
         {
-            Walk w;
+            Walk<W> w;
             w.start(0, c, warp);
             int have = -1;
             float factor = 1.f;
             constexpr int QN = G::FP8 ? 1 : 16 / (int)sizeof(T);
-            float qf[QN];
-            uint32_t qb[G::FP8 ? D / 8 : 1];  // e4m3: the fp16 fragments, column 0 the leading and column 1 the trailing half
-            (void)qf;
-            (void)qb;
-            for (; w.left > 0; w.step(c.tiles)) {
+            [[maybe_unused]] uint64_t qf[QN / 2 + 1];
+            [[maybe_unused]] uint32_t qb[G::FP8 ? D / 8 : 1];  // e4m3: fp16 fragments, column 0 the leading and column 1 the trailing half
+#pragma unroll 1
+            for (;; w.step(c.tiles)) {
+                fill();
+                if (w.left == 0) break;
+                const int row0 = w.j * G::TR;
+                const unsigned char* tile = take();
+                if (tile == nullptr) break;
                 if (w.p != have) {
                     have = w.p;
-                    const TQ* q = static_cast<const TQ*>(a.q) + ((size_t)c.b * a.H + sg.rep[w.p]) * D;
+                    const TQ* q = reinterpret_cast<const TQ*>(tile + G::QUERY);
                     if constexpr (!G::FP8) {
-                        Vec16<T>::unpack(*reinterpret_cast<const uint4*>(q + (lane % G::LPR) * QN), qf);
+                        float x[QN];
+                        Vec16<T>::unpack(*reinterpret_cast<const uint4*>(q + (lane % G::LPR) * QN), x);
 #pragma unroll
-                        for (int e = 0; e < QN; ++e) qf[e] *= a.scale_log2;
+                        for (int e = 0; e < QN / 2; ++e) qf[e] = pack2(x[2 * e] * a.scale_log2, x[2 * e + 1] * a.scale_log2);
                     } else {
                         // lane (g, t) holds the columns 16 (t + 4 j) ... + 15 of its keys
                         constexpr int J = D / 64, QV = 16 / (int)sizeof(TQ);
@@ -552,22 +672,24 @@ __global__ void __launch_bounds__(kThreads, 1) paged_decode_kernel(const DecodeA
                         }
                     }
                 }
-                const int row0 = w.j * G::TR, rows = min(G::TR, c.rows - row0);
-                uint32_t tile;
-                if (!take(&tile)) break;
                 float* score = sm.score + w.p * c.stride + row0;
                 if constexpr (!G::FP8) {
                     // lanes of a group hold 16 bytes each of rows group * IT + i; a butterfly turns 16 partial sums a
                     // lane into whole sums, halving the rows a lane answers for at every step
-                    const uint32_t base = tile + (lane / G::LPR) * G::IT * G::ROW + (lane % G::LPR) * 16;
+                    const unsigned char* base = tile + (lane / G::LPR) * G::IT * G::ROW + (lane % G::LPR) * 16;
+                    uint4 raw[G::IT];
                     float s[G::IT];
+#pragma unroll
+                    for (int i = 0; i < G::IT; ++i) raw[i] = lds16(base + i * G::ROW);
 #pragma unroll
                     for (int i = 0; i < G::IT; ++i) {
                         float kf[QN];
-                        Vec16<T>::unpack(lds16(base + i * G::ROW), kf);
-                        s[i] = qf[0] * kf[0];
+                        Vec16<T>::unpack(raw[i], kf);
+                        uint64_t sum = 0;
 #pragma unroll
-                        for (int e = 1; e < QN; ++e) s[i] = fmaf(qf[e], kf[e], s[i]);
+                        for (int e = 0; e < QN / 2; ++e) sum = fma2(qf[e], pack2(kf[2 * e], kf[2 * e + 1]), sum);
+                        const float2 x = unpack2(sum);
+                        s[i] = x.x + x.y;
                     }
                     int row = (lane / G::LPR) * G::IT;
 #pragma unroll
@@ -591,37 +713,34 @@ __global__ void __launch_bounds__(kThreads, 1) paged_decode_kernel(const DecodeA
                     constexpr int SAME = G::LPR > G::IT ? G::LPR / G::IT : 1;  // lanes that end with the same row
 #pragma unroll
                     for (int i = 0; i < LEFT; ++i)
-                        if (row + i < rows && lane % SAME == 0) score[row + i] = s[i];
+                        if (lane % SAME == 0) score[row + i] = s[i];  // (rows behind the last get scores that nothing reads)
                 } else {
                     // 16 keys are the rows of A, 16 columns of them a step; B holds the query (leading and trailing half)
                     const int g = lane >> 2, t = lane & 3;
-                    const uint32_t scales = tile + G::DATA;
+                    const float* scales = reinterpret_cast<const float*>(tile + G::DATA) + g;
+                    // rows 16 m + g and 16 m + g + 8, pieces t + 4 j (see Geom; the lane's share taken out)
+                    const int lane_at = D == 128 ? g * 128 + 16 * (t + 4 * (g & 1)) : (g >> 1) * 128 + 16 * ((g & 1) * 4 + t);
 #pragma unroll
-                    for (int m = 0; m < 4; ++m) {
-                        if (16 * m < rows) {
-                            const uint32_t base = tile + m * G::RUN_STRIDE + g * G::ROW + t * 16;
-                            float acc[4] = {0.f, 0.f, 0.f, 0.f};
+                    for (int m = 0; m < G::TR / 16; ++m) {
+                        float acc[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                            for (int j = 0; j < D / 64; ++j) {
-                                const uint4 x = lds16(base + j * 64), y = lds16(base + j * 64 + 8 * G::ROW);
-                                const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+                        for (int j = 0; j < D / 64; ++j) {
+                            const uint4 x = lds16(tile + 16 * m * G::ROW + (lane_at ^ (64 * j) ^ (32 * (16 * m / G::RUN))));
+                            const uint4 y = lds16(tile + (16 * m + 8) * G::ROW + (lane_at ^ (64 * j) ^ (32 * ((16 * m + 8) / G::RUN))));
+                            const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
-                                for (int i = 0; i < 4; ++i)
-                                    mma16816(acc, e4m3_pair(xs[i] & 0xffffu), e4m3_pair(ys[i] & 0xffffu), e4m3_pair(xs[i] >> 16),
-                                             e4m3_pair(ys[i] >> 16), qb[8 * j + 2 * i], qb[8 * j + 2 * i + 1]);
+                            for (int i = 0; i < 4; ++i) {
+                                uint32_t a0, a1, a2, a3;
+                                e4m3_halves(xs[i], &a0, &a2);
+                                e4m3_halves(ys[i], &a1, &a3);
+                                mma16816(acc, a0, a1, a2, a3, qb[8 * j + 2 * i], qb[8 * j + 2 * i + 1]);
                             }
-                            if (t == 0) {
-                                const int r = 16 * m + g;
-                                float ks;
-                                if (r < rows) {
-                                    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(ks) : "r"(scales + 4 * r));
-                                    score[r] = (acc[0] + acc[1]) * (ks * factor);
-                                }
-                                if (r + 8 < rows) {
-                                    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(ks) : "r"(scales + 4 * (r + 8)));
-                                    score[r + 8] = (acc[2] + acc[3]) * (ks * factor);
-                                }
-                            }
+                        }
+                        // (rows behind the last get scores that nothing reads)
+                        const float ks = scales[16 * m], ks8 = scales[16 * m + 8];
+                        if (t == 0) {
+                            score[16 * m + g] = (acc[0] + acc[1]) * (ks * factor);
+                            score[16 * m + g + 8] = (acc[2] + acc[3]) * (ks8 * factor);
                         }
                     }
                 }
@@ -631,19 +750,24 @@ __global__ void __launch_bounds__(kThreads, 1) paged_decode_kernel(const DecodeA
         __syncthreads();
 
         // S: running maximum and sum of every cluster, probabilities relative to the new maximum
-        for (int cl = warp; cl < c.clusters; cl += kWarps) {
+#pragma unroll 1
+        for (int cl = warp; cl < c.clusters; cl += W) {
             float* score = sm.score + cl * c.stride;
             float top = -INFINITY, old = c.first ? -INFINITY : sm.top[cl], sum = 0.f;
+#pragma unroll 4
             for (int r = lane; r < c.rows; r += 32) top = fmaxf(top, score[r]);
 #pragma unroll
             for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
             top = fmaxf(top, old);
             const float ref = top == -INFINITY ? 0.f : top;  // scores of -inf leave their rows out
+#pragma unroll 4
             for (int r = lane; r < c.rows; r += 32) {
                 const float p = exp2_approx(score[r] - ref);
-                score[r] = p;
+                score[r] = G::FP8 ? p * kProbScale : p;
                 sum += p;
             }
+            const int r0 = c.rows + lane;
+            if (r0 < c.stride) score[r0] = 0.f;  // (a tile has 32 rows at most)
 #pragma unroll
             for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
             if (lane == 0) {
@@ -656,18 +780,22 @@ __global__ void __launch_bounds__(kThreads, 1) paged_decode_kernel(const DecodeA
         const int bad_so_far = sm.any_bad;
         __syncthreads();  // (the next chunk may be of another request, whose pages count anew)
         more = prepare(par ^ 1);
-        __syncthreads();
-        if (more) ready_no = no + 1;
-        fill();
+        if (more) {
+            __syncthreads();
+            ready_no = no + 1;
+        }
 
         // V: sums of the warp's share
         float acc[G::VPL];
 #pragma unroll
         for (int e = 0; e < G::VPL; ++e) acc[e] = 0.f;
-        int open = -1;  // a head whose first rows are in acc and whose last rows another warp has
+        // e4m3: sums on the tensor cores, of products that are kProbScale * factor too large
+        constexpr int PARTS = G::FP8 ? D / 16 : 1;
+        [[maybe_unused]] float part[PARTS][4];
+        [[maybe_unused]] float factor = 1.f;
         // Writes the finished sums of a head.
-        auto emit = [&](int p) {
-            const int h = sg.head[p], cl = sg.cluster[p];
+        auto emit = [&](int p) __attribute__((always_inline)) {
+            const int h = sg.head[p], cl = sg.cluster[p] - first_place;
             float* o = a.ws.o + ((size_t)c.slot * a.H + h) * D + G::col(lane);
             if (G::own(lane)) {
                 if (!c.first) {
@@ -694,132 +822,139 @@ __global__ void __launch_bounds__(kThreads, 1) paged_decode_kernel(const DecodeA
             }
             if (c.last && !c.single && lane == 0) a.ws.ml[(size_t)c.slot * a.H + h] = make_float2(sm.top[cl], sm.sum[cl]);
         };
+        int open = -1;  // a head whose first rows are in acc and whose last rows another warp has
         {
-            Walk w;
+            Walk<W> w;
             w.start(1, c, warp);
-            bool from_start = w.j == 0;
-            while (w.left > 0) {
-                const int row0 = w.j * G::TR, rows = min(G::TR, c.rows - row0);
-                uint32_t tile;
-                if (!take(&tile)) break;
-                const float* prob = sm.score + sg.cluster[w.p] * c.stride + row0;
+            bool from_start = w.j == 0, begins = true;  // begins: the sums of a head start with this tile
+#pragma unroll 1
+            for (;;) {
+                fill();
+                if (w.left == 0) break;
+                const int row0 = w.j * G::TR;
+                const float* prob = sm.score + (sg.cluster[w.p] - first_place) * c.stride + row0;
+                const unsigned char* tile = take();
+                if (tile == nullptr) break;
                 if constexpr (!G::FP8) {
-                    const int first = (lane / G::LPR) * G::IT;
-                    const uint32_t base = tile + first * G::ROW + (lane % G::LPR) * 16;
-                    if (rows == G::TR) {
-                        uint64_t sum[G::VPL / 2];
+                    const int first = (lane / G::LPR) * G::IT, rows = c.rows - row0;
+                    if (rows < G::TR) {  // rows behind the last hold anything: zeros instead
+#pragma unroll 1
+                        for (int i = rows * G::LPR + lane; i < G::TR * G::LPR; i += 32)
+                            *reinterpret_cast<uint4*>(sm.slot[warp][out_slot] + i * 16) = make_uint4(0, 0, 0, 0);
+                        __syncwarp();
+                    }
+                    const unsigned char* base = tile + first * G::ROW + (lane % G::LPR) * 16;
+                    uint64_t sum[G::VPL / 2];
 #pragma unroll
-                        for (int e = 0; e < G::VPL / 2; ++e) sum[e] = pack2(acc[2 * e], acc[2 * e + 1]);
+                    for (int e = 0; e < G::VPL / 2; ++e) sum[e] = pack2(acc[2 * e], acc[2 * e + 1]);
+                    uint4 raw[G::IT];
+                    float pr[G::IT];
 #pragma unroll
-                        for (int i = 0; i < G::IT; i += 4) {
-                            const float4 p4 = *reinterpret_cast<const float4*>(prob + first + i);
-                            const float pr[4] = {p4.x, p4.y, p4.z, p4.w};
+                    for (int i = 0; i < G::IT; ++i) raw[i] = lds16(base + i * G::ROW);
 #pragma unroll
-                            for (int u = 0; u < 4; ++u) {
-                                float vf[G::VPL];
-                                Vec16<T>::unpack(lds16(base + (i + u) * G::ROW), vf);
-                                const uint64_t pp = pack2(pr[u], pr[u]);
+                    for (int i = 0; i < G::IT; i += 4) *reinterpret_cast<float4*>(pr + i) = *reinterpret_cast<const float4*>(prob + first + i);
 #pragma unroll
-                                for (int e = 0; e < G::VPL / 2; ++e) sum[e] = fma2(pp, pack2(vf[2 * e], vf[2 * e + 1]), sum[e]);
-                            }
-                        }
+                    for (int i = 0; i < G::IT; ++i) {
+                        float vf[G::VPL];
+                        Vec16<T>::unpack(raw[i], vf);
+                        const uint64_t pp = pack2(pr[i], pr[i]);
 #pragma unroll
-                        for (int e = 0; e < G::VPL / 2; ++e) {
-                            const float2 x = unpack2(sum[e]);
-                            acc[2 * e] = x.x;
-                            acc[2 * e + 1] = x.y;
-                        }
-                    } else {  // rows behind the last are not touched: they may hold anything
-                        const int n = min(G::IT, rows - first);
-                        for (int i = 0; i < n; ++i) {
-                            float vf[G::VPL];
-                            Vec16<T>::unpack(lds16(base + i * G::ROW), vf);
-                            const float p = prob[first + i];
+                        for (int e = 0; e < G::VPL / 2; ++e) sum[e] = fma2(pp, pack2(vf[2 * e], vf[2 * e + 1]), sum[e]);
+                    }
+                    if (rows < G::TR) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // (the slot's next rows come by bulk copies)
 #pragma unroll
-                            for (int e = 0; e < G::VPL; ++e) acc[e] = fmaf(p, vf[e], acc[e]);
-                        }
+                    for (int e = 0; e < G::VPL / 2; ++e) {
+                        const float2 x = unpack2(sum[e]);
+                        acc[2 * e] = x.x;
+                        acc[2 * e + 1] = x.y;
                     }
                 } else {
                     // 16 columns are the rows of A, 16 cache rows a step (four of each run); B holds the probabilities
-                    // times the rows' scales, brought below 2 by a power of two and split into two fp16 numbers
+                    // times the rows' scales, as two fp16 numbers each, the leading and the trailing half.  They are good
+                    // to 2^-25 then: with probabilities kept times 2^14 and the largest scale of a head's first rows
+                    // between 2^-16 and 2 that is at most 2^-22 of the largest product.  Other scales, and larger ones
+                    // later, are brought there by a power of two.
                     const int g = lane >> 2, t = lane & 3;
-                    const uint32_t scales = tile + G::DATA + 64 * t;
-                    const bool whole = rows == G::TR;
-                    float4 vs[4];
-                    float top = 0.f, f, inv;
+                    const float4* scales = reinterpret_cast<const float4*>(tile + G::DATA + 4 * G::RUN * t);
+                    float4 vs[G::STEPS];
+                    float top = 0.f;
 #pragma unroll
-                    for (int s = 0; s < 4; ++s) {
-                        const uint4 x = lds16(scales + 16 * s);
-                        vs[s] = make_float4(__uint_as_float(x.x), __uint_as_float(x.y), __uint_as_float(x.z), __uint_as_float(x.w));
-                        if (!whole) {
-                            const int r = 16 * t + 4 * s;
-                            vs[s].x = r < rows ? vs[s].x : 0.f;
-                            vs[s].y = r + 1 < rows ? vs[s].y : 0.f;
-                            vs[s].z = r + 2 < rows ? vs[s].z : 0.f;
-                            vs[s].w = r + 3 < rows ? vs[s].w : 0.f;
-                        }
+                    for (int s = 0; s < G::STEPS; ++s) {
+                        vs[s] = scales[s];
                         top = fmaxf(top, fmaxf(fmaxf(fabsf(vs[s].x), fabsf(vs[s].y)), fmaxf(fabsf(vs[s].z), fabsf(vs[s].w))));
                     }
-                    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-                    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-                    normaliser(top, &f, &inv);
-                    float part[D / 16][4];
+                    if (begins) {
+                        factor = 1.f;
 #pragma unroll
-                    for (int i = 0; i < D / 16; ++i) part[i][0] = part[i][1] = part[i][2] = part[i][3] = 0.f;
+                        for (int i = 0; i < PARTS; ++i) part[i][0] = part[i][1] = part[i][2] = part[i][3] = 0.f;
+                    }
+                    if (__any_sync(0xffffffffu, top * factor > 2.f) || (begins && __all_sync(0xffffffffu, top < 1.f / 65536))) {
+                        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+                        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+                        const float old = factor;
+                        float inverse;
+                        normaliser(top, &factor, &inverse);
+                        const float change = factor / old;
 #pragma unroll
-                    for (int s = 0; s < 4; ++s) {
-                        const int r = 16 * t + 4 * s;
-                        float4 pr = make_float4(0.f, 0.f, 0.f, 0.f);
-                        if (whole) {
-                            pr = *reinterpret_cast<const float4*>(prob + r);
-                        } else {
-                            if (r < rows) pr.x = prob[r];
-                            if (r + 1 < rows) pr.y = prob[r + 1];
-                            if (r + 2 < rows) pr.z = prob[r + 2];
-                            if (r + 3 < rows) pr.w = prob[r + 3];
-                        }
-                        const float x0 = pr.x * (vs[s].x * f), x1 = pr.y * (vs[s].y * f), x2 = pr.z * (vs[s].z * f), x3 = pr.w * (vs[s].w * f);
+                        for (int i = 0; i < PARTS; ++i)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) part[i][e] *= change;
+                    }
+                    if (__any_sync(0xffffffffu, factor != 1.f)) {
+#pragma unroll
+                        for (int s = 0; s < G::STEPS; ++s) vs[s] = make_float4(vs[s].x * factor, vs[s].y * factor, vs[s].z * factor, vs[s].w * factor);
+                    }
+                    constexpr int WORDS = D / 32;  // 32-bit words a lane holds of a row
+                    const int lane_at = G::RUN * t * G::ROW + (D == 128 ? 16 * (g ^ (2 * t)) : (16 * ((g >> 1) ^ (2 * t)) + 8 * (g & 1)));
+#pragma unroll
+                    for (int s = 0; s < G::STEPS; ++s) {
+                        const float4 pr = *reinterpret_cast<const float4*>(prob + G::RUN * t + 4 * s);
+                        const float x0 = pr.x * vs[s].x, x1 = pr.y * vs[s].y, x2 = pr.z * vs[s].z, x3 = pr.w * vs[s].w;
                         const uint32_t h0 = half_pair(x0, x1), h1 = half_pair(x2, x3);
                         const float2 y0 = half_floats(h0), y1 = half_floats(h1);
                         const uint32_t l0 = half_pair(x0 - y0.x, x1 - y0.y), l1 = half_pair(x2 - y1.x, x3 - y1.y);
                         const uint32_t b0 = g == 0 ? h0 : (g == 1 ? l0 : 0u), b1 = g == 0 ? h1 : (g == 1 ? l1 : 0u);
-                        constexpr int WORDS = D / 32;  // 32-bit words a lane holds of a row
                         uint32_t v[4][WORDS];
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
-                            const uint32_t at = tile + t * G::RUN_STRIDE + (4 * s + i) * G::ROW + g * (4 * WORDS);
-                            const bool there = whole || r + i < rows;
+                            // row RUN * t + 4 s + i (see Geom; the lane's share taken out)
+                            const unsigned char* at = tile + (4 * s + i) / (D == 128 ? 1 : 2) * 128 + (lane_at ^ (64 * (i & 1)));
                             if constexpr (WORDS == 4) {
-                                const uint4 x = there ? lds16(at) : make_uint4(0, 0, 0, 0);
+                                const uint4 x = lds16(at);
                                 v[i][0] = x.x; v[i][1] = x.y; v[i][2] = x.z; v[i][3] = x.w;
                             } else {
-                                const uint2 x = there ? lds8(at) : make_uint2(0, 0);
+                                const uint2 x = lds8(at);
                                 v[i][0] = x.x; v[i][1] = x.y;
                             }
                         }
 #pragma unroll
                         for (int wd = 0; wd < WORDS; ++wd) {
                             // columns 4 wd .. + 3 of two rows each, side by side
-                            const uint32_t lo0 = __byte_perm(v[0][wd], v[1][wd], 0x5140), hi0 = __byte_perm(v[0][wd], v[1][wd], 0x7362);
-                            const uint32_t lo1 = __byte_perm(v[2][wd], v[3][wd], 0x5140), hi1 = __byte_perm(v[2][wd], v[3][wd], 0x7362);
-                            mma16816(part[2 * wd], e4m3_pair(lo0 & 0xffffu), e4m3_pair(lo0 >> 16), e4m3_pair(lo1 & 0xffffu),
-                                     e4m3_pair(lo1 >> 16), b0, b1);
-                            mma16816(part[2 * wd + 1], e4m3_pair(hi0 & 0xffffu), e4m3_pair(hi0 >> 16), e4m3_pair(hi1 & 0xffffu),
-                                     e4m3_pair(hi1 >> 16), b0, b1);
-                        }
-                    }
 #pragma unroll
-                    for (int i = 0; i < D / 16; ++i) {
-                        acc[2 * i] = fmaf(part[i][0] + part[i][1], inv, acc[2 * i]);
-                        acc[2 * i + 1] = fmaf(part[i][2] + part[i][3], inv, acc[2 * i + 1]);
+                            for (int x = 0; x < 2; ++x) {
+                                const unsigned sel = x == 0 ? 0x5140 : 0x7362;
+                                uint32_t a0, a1, a2, a3;
+                                e4m3_halves(__byte_perm(v[0][wd], v[1][wd], sel), &a0, &a1);
+                                e4m3_halves(__byte_perm(v[2][wd], v[3][wd], sel), &a2, &a3);
+                                mma16816(part[2 * wd + x], a0, a1, a2, a3, b0, b1);
+                            }
+                        }
                     }
                 }
                 release();
                 const int p = w.p;
                 const bool ends = w.j + 1 == c.tiles;
                 w.step(c.tiles);
+                begins = ends;
                 if (!ends && w.left > 0) continue;
-                if constexpr (!G::FP8) {
+                if constexpr (G::FP8) {
+                    const float f = (1.f / kProbScale) / factor;
+#pragma unroll
+                    for (int i = 0; i < PARTS; ++i) {
+                        acc[2 * i] = (part[i][0] + part[i][1]) * f;
+                        acc[2 * i + 1] = (part[i][2] + part[i][3]) * f;
+                    }
+                } else {
 #pragma unroll
                     for (int o = G::LPR; o < 32; o <<= 1)
 #pragma unroll
@@ -833,6 +968,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_decode_kernel(const DecodeA
                     emit(p);
                 } else {
                     open = p;
+                    fill();
                     break;
                 }
 #pragma unroll
@@ -843,30 +979,53 @@ __global__ void __launch_bounds__(kThreads, 1) paged_decode_kernel(const DecodeA
         __syncthreads();
         if (open >= 0) {
             const int n = c.heads * c.tiles, stop = (open + 1) * c.tiles;
-            for (int w = warp + 1; w < kWarps; ++w) {
-                const int lo = n * w / kWarps;
+#pragma unroll 1
+            for (int w = warp + 1; w < W; ++w) {
+                const int lo = n * w / W;
                 if (lo >= stop) break;
-                if (lo == n * (w + 1) / kWarps) continue;  // a warp without tiles
+                if (lo == n * (w + 1) / W) continue;  // a warp without tiles
                 if (G::own(lane))
 #pragma unroll
                     for (int e = 0; e < G::VPL; ++e) acc[e] += sm.part[w][G::col(lane) + e];
             }
             emit(open);
         }
+        if (c.span_end > 0) opened_span = true;
         if (c.last && tid == 0) {
             if (!c.single && group == 0) a.ws.slot_bad[c.slot] = bad_so_far;
+            if (group == 0 && (c.span_end > 0 || (by_request && c.single))) {
+                int end = piece;  // the piece that the request ends in
+                if (c.span_end > 0) {
+                    end = max(end, (c.span_end - 1) / (each + 1));  // (a piece has each or each + 1)
+                    while (piece_start(end + 1) < c.span_end) ++end;
+                }
+                a.ws.desc[by_request ? c.b : piece] = make_int4(c.single ? -1 : c.b, c.slot, end - piece + 1, 0);
+            }
             if (bad_so_far && atomicCAS(&sm.err, CHAI_OK, CHAI_ERR_BAD_PAGE) == CHAI_OK) sm.err_b = c.b;
         }
     }
     if (dead)  // copies in flight end before the shared memory goes
         for (int i = used; i < issued; ++i) {
-            bar_wait(smem_addr(&sm.full[warp][out_slot]), out_phase, kDefaultWaitLimitCycles);
+            bar_wait(bars + out_slot * 8, out_phase, kDefaultWaitLimitCycles);
             if (++out_slot == G::STAGES) {
                 out_slot = 0;
                 out_phase ^= 1;
             }
         }
-    if (!by_request && group == 0 && piece < pieces && !opened_span && tid == 0) a.ws.desc[piece] = make_int4(-1, 0, 0, 0);
+
+    // -- the rest: requests without rows get zeros, pieces that open no request that goes on say so
+#pragma unroll 1
+    for (int z = blockIdx.x; z < a.B; z += n_ctas) {
+        if (length(z) > 0) continue;
+        if (by_request && tid == 0) a.ws.desc[z] = make_int4(-1, 0, 0, 0);
+        uint4* o = reinterpret_cast<uint4*>(static_cast<TQ*>(a.out) + (size_t)z * a.H * D);
+#pragma unroll 1
+        for (int i = tid; i < a.H * D * (int)sizeof(TQ) / 16; i += THREADS) o[i] = make_uint4(0, 0, 0, 0);
+    }
+    if (!by_request && tid == 0) {
+        if ((int)blockIdx.x >= pieces && (int)blockIdx.x < a.n_desc) a.ws.desc[blockIdx.x] = make_int4(-1, 0, 0, 0);
+        if (piece < pieces && group == 0 && !opened_span) a.ws.desc[piece] = make_int4(-1, 0, 0, 0);
+    }
     __syncthreads();
     if (tid == 0) {
         a.ws.err[blockIdx.x] = sm.err;
@@ -876,10 +1035,11 @@ __global__ void __launch_bounds__(kThreads, 1) paged_decode_kernel(const DecodeA
 
 // ---- joining the pieces of a request ----------------------------------------------------------------------------
 
-// grid (H, descriptions): out[b][h] from the partial results of consecutive pieces.
+// grid (H, blocks): out[b][h] from the partial results of consecutive pieces.  Bound by the round trips to L2, one for the
+// description and one for everything else: the first rows are on their way before the weights are known.
 template <typename TQ, int D>
 __global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(const DecodeArgs a, int n_ctas) {
-    constexpr int WARPS = kJoinThreads / 32, E = D / 32;
+    constexpr int WARPS = kJoinThreads / 32, E = D / 32, AHEAD = 4;
     __shared__ float s_w[kMaxCtas], s_top[WARPS], s_sum[WARPS], s_o[WARPS][D];
     dependent_grid_sync();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, h = blockIdx.x;
@@ -902,60 +1062,84 @@ __global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(const DecodeAr
             a.hdr->bad_b = at;
         }
     }
-    const int4 d = a.ws.desc[blockIdx.y];
-    if (d.x < 0) return;
-    const int b = d.x, first = d.y, n = d.z;
-    float2 ml = make_float2(-INFINITY, 0.f);
-    bool bad = false;
-    if (tid < n) {
-        ml = a.ws.ml[(size_t)(first + tid) * a.H + h];
-        bad = a.ws.slot_bad[first + tid] != 0;
-    }
-    if (__syncthreads_or(tid == 0 && ml.y == -1.f)) return;  // an unknown head: zeros are written already
-    float top = ml.x;
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-    if (lane == 0) s_top[warp] = top;
-    const bool zero = __syncthreads_or(bad);
-    for (int w = 0; w < WARPS; ++w) top = fmaxf(top, s_top[w]);
-    const float ref = top == -INFINITY ? 0.f : top;
-    const float weight = tid < n ? exp2_approx(ml.x - ref) : 0.f;
-    if (tid < n) s_w[tid] = weight;
-    float sum = tid < n ? weight * ml.y : 0.f;
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    if (lane == 0) s_sum[warp] = sum;
-    __syncthreads();
-    float o[E];
-#pragma unroll
-    for (int e = 0; e < E; ++e) o[e] = 0.f;
-    const float* src = a.ws.o + ((size_t)first * a.H + h) * D + lane * E;
-    const size_t apart = (size_t)a.H * D;
-#pragma unroll 8
-    for (int i = warp; i < n; i += WARPS) {
-        const float w = s_w[i];
+    using Row = typename std::conditional<E == 4, float4, float2>::type;
+    auto add = [&](float* o, float w, const Row& x) {
+        o[0] = fmaf(w, x.x, o[0]);
+        o[1] = fmaf(w, x.y, o[1]);
         if constexpr (E == 4) {
-            const float4 x = *reinterpret_cast<const float4*>(src + i * apart);
-            o[0] = fmaf(w, x.x, o[0]);
-            o[1] = fmaf(w, x.y, o[1]);
             o[2] = fmaf(w, x.z, o[2]);
             o[3] = fmaf(w, x.w, o[3]);
-        } else {
-            const float2 x = *reinterpret_cast<const float2*>(src + i * apart);
-            o[0] = fmaf(w, x.x, o[0]);
-            o[1] = fmaf(w, x.y, o[1]);
         }
-    }
+    };
+#pragma unroll 1
+    for (int di = blockIdx.y; di < a.n_desc; di += gridDim.y) {
+        const int4 d = a.ws.desc[di];
+        if (d.x < 0) continue;
+        const int b = d.x, first = d.y, n = d.z;
+        const float* src = a.ws.o + ((size_t)first * a.H + h) * D + lane * E;
+        const size_t apart = (size_t)a.H * D;
+        Row ahead[AHEAD];
 #pragma unroll
-    for (int e = 0; e < E; ++e) s_o[warp][lane * E + e] = o[e];
-    __syncthreads();
-    if (tid < D) {
-        float l = 0.f, x = 0.f;
-        for (int w = 0; w < WARPS; ++w) {
-            l += s_sum[w];
-            x += s_o[w][tid];
+        for (int u = 0; u < AHEAD; ++u)
+            if (warp + u * WARPS < n) ahead[u] = *reinterpret_cast<const Row*>(src + (warp + u * WARPS) * apart);
+        float2 ml[2];
+        bool bad = false, unknown = false;
+        float top = -INFINITY;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const int i = tid + u * kJoinThreads;
+            ml[u] = make_float2(-INFINITY, 0.f);
+            if (i < n) {
+                ml[u] = a.ws.ml[(size_t)(first + i) * a.H + h];
+                bad |= a.ws.slot_bad[first + i] != 0;
+                unknown |= i == 0 && ml[u].y == -1.f;
+            }
+            top = fmaxf(top, ml[u].x);
         }
-        static_cast<TQ*>(a.out)[((size_t)b * a.H + h) * D + tid] = from_float<TQ>(zero ? 0.f : x / l);
+        static_assert(2 * kJoinThreads >= kMaxCtas, "two slots a thread");
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+        if (lane == 0) s_top[warp] = top;
+        if (__syncthreads_or(unknown)) continue;  // an unknown head: zeros are written already
+        const bool zero = __syncthreads_or(bad);
+#pragma unroll
+        for (int w = 0; w < WARPS; ++w) top = fmaxf(top, s_top[w]);
+        const float ref = top == -INFINITY ? 0.f : top;
+        float sum = 0.f;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const int i = tid + u * kJoinThreads;
+            if (i < n) {
+                const float weight = exp2_approx(ml[u].x - ref);
+                s_w[i] = weight;
+                sum += weight * ml[u].y;
+            }
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        if (lane == 0) s_sum[warp] = sum;
+        __syncthreads();
+        float o[E];
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[e] = 0.f;
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u)
+            if (warp + u * WARPS < n) add(o, s_w[warp + u * WARPS], ahead[u]);
+#pragma unroll 8
+        for (int i = warp + AHEAD * WARPS; i < n; i += WARPS) add(o, s_w[i], *reinterpret_cast<const Row*>(src + i * apart));
+#pragma unroll
+        for (int e = 0; e < E; ++e) s_o[warp][lane * E + e] = o[e];
+        __syncthreads();
+        if (tid < D) {
+            float l = 0.f, x = 0.f;
+#pragma unroll
+            for (int w = 0; w < WARPS; ++w) {
+                l += s_sum[w];
+                x += s_o[w][tid];
+            }
+            static_cast<TQ*>(a.out)[((size_t)b * a.H + h) * D + tid] = from_float<TQ>(zero ? 0.f : x / l);
+        }
+        __syncthreads();  // s_* are free for the next description
     }
 }
 
@@ -963,10 +1147,10 @@ __global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(const DecodeAr
 
 template <typename T, typename TQ, int D>
 int launch_decode(const DecodeArgs& args, cudaStream_t s) {
-    using G = Geom<T, D>;
-    constexpr size_t smem = sizeof(Smem<G::SLOT, G::STAGES, D>);
+    using G = Geom<T, TQ, D>;
+    constexpr size_t smem = sizeof(Smem<G, D>);
     static_assert(smem <= 227 * 1024, "one CTA's shared memory");
-    static_assert(G::DATA % 16 == 0 && G::SLOT % 16 == 0 && (G::FP8 || G::IT == 16), "tile geometry");
+    static_assert(G::SLOT % 16 == 0 && (G::FP8 || G::IT == 8) && G::TR % 8 == 0 && G::TR <= 32, "tile geometry");
     static PerDeviceOnce once;  // (one per instantiation)
     static int sm_count[kMaxDevices];
     int dev = 0;
@@ -982,9 +1166,9 @@ int launch_decode(const DecodeArgs& args, cudaStream_t s) {
     const int n_ctas = sm_count[dev & (kMaxDevices - 1)] < kMaxCtas ? sm_count[dev & (kMaxDevices - 1)] : kMaxCtas;
     DecodeArgs a = args;
     a.n_desc = a.B < n_ctas ? a.B : n_ctas;
-    CHAI_LAUNCH_DEPENDENT("paged_decode_kernel launch", (paged_decode_kernel<T, TQ, D>), dim3(n_ctas), dim3(kThreads), smem, s, a);
-    CHAI_LAUNCH_DEPENDENT("paged_join_kernel launch", (paged_join_kernel<TQ, D>), dim3(a.H, a.n_desc), dim3(kJoinThreads), 0, s,
-                          a, n_ctas);
+    CHAI_LAUNCH_DEPENDENT("paged_decode_kernel launch", (paged_decode_kernel<T, TQ, D>), dim3(n_ctas), dim3(G::THREADS), smem, s, a);
+    CHAI_LAUNCH_DEPENDENT("paged_join_kernel launch", (paged_join_kernel<TQ, D>), dim3(a.H, a.n_desc < kJoinBlocks ? a.n_desc : kJoinBlocks),
+                          dim3(kJoinThreads), 0, s, a, n_ctas);
     return CHAI_OK;
 }
 
@@ -1004,8 +1188,8 @@ int decode(const char* fn, bool fp8, const void* q, const void* k_pages, const v
     const int rc = make_pool(fn, block_table, B, H, k, n_pages, page_size, max_pages, D, k_page_stride, v_page_stride,
                              fp8 ? 1 : elem_size(dtype), &a.pool);
     if (rc != CHAI_OK) return rc;
-    CHAI_REQUIRE((long long)B * a.pool.capacity < (1ll << 34), CHAI_ERR_UNSUPPORTED,
-                 "%s: B * max_pages * page_size must be below 2^34", fn);
+    CHAI_REQUIRE((long long)B * a.pool.capacity < (1ll << 33), CHAI_ERR_UNSUPPORTED,
+                 "%s: B * max_pages * page_size must be below 2^33", fn);
     const size_t need = chai_decode_paged_workspace_bytes(B, H, D);
     CHAI_REQUIRE(workspace_bytes >= need, CHAI_ERR_WORKSPACE, "%s: workspace has %zu bytes, %zu needed", fn, workspace_bytes,
                  need);
