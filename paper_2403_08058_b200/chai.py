@@ -473,88 +473,102 @@ def chai_decode_attention_fp8(q, k_rep8, v8, k_scale, v_scale, membership, reps,
 _PAGED_IO = {torch.float32: CHAI_F32, torch.bfloat16: CHAI_BF16}
 
 
-def _paged_call(fn, device, *args) -> None:
+def _paged_call(fn, dev: int, *args) -> None:
     """Calls fn(*args, stream) on the device that the tensors live on, on that device's current stream."""
-    if device.index == torch.cuda.current_device():
-        _check(fn(*args, torch.cuda.current_stream().cuda_stream))
+    if dev == torch.cuda.current_device():
+        rc = fn(*args, _raw_stream(dev))
+    else:
+        with torch.cuda.device(dev):
+            rc = fn(*args, _raw_stream(dev))
+    if rc:
+        _check(rc)
+
+
+def _raw_stream(dev: int) -> int:
+    # (torch.cuda.current_stream builds a Stream object, which costs as much as a launch)
+    get = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return get(dev) if get is not None else torch.cuda.current_stream(dev).cuda_stream
+
+
+def _want(t, name, shape, dtype, dev) -> None:
+    if t.shape == shape and t.dtype is dtype and t.get_device() == dev and t.is_contiguous():
         return
-    with torch.cuda.device(device):
-        _check(fn(*args, torch.cuda.current_stream().cuda_stream))
-
-
-def _want(t, name, shape, dtype, device) -> None:
     if t.dtype is not dtype:
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
     if t.shape != shape:
         raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
-    if t.device != device or not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous and on {device}")
+    raise ValueError(f"{name} must be contiguous and on cuda:{dev}")
+
+
+_E4M3 = (torch.uint8, torch.float8_e4m3fn)
 
 
 def _pages(k_pages, v_pages, k_scales, v_scales, block_table, seq_lens):
-    """Checks a pool and its tables; returns (n_pages, k, H, page_size, D, page strides, B, max_pages, device)."""
+    """Checks a pool and its tables; returns (n_pages, k, H, page_size, D, page strides, B, max_pages, device index)."""
     if k_pages.dim() != 4 or v_pages.dim() != 4:
         raise ValueError("k_pages must be [n_pages,k,page_size,D] and v_pages [n_pages,H,page_size,D]")
     n, k, ps, D = k_pages.shape
     H = v_pages.shape[1]
-    device = k_pages.device
     if v_pages.shape != (n, H, ps, D):
         raise ValueError("k_pages and v_pages must agree in pages, page size and head dimension")
-    if device.type != "cuda" or v_pages.device != device:
+    dev = k_pages.get_device()
+    if dev < 0 or v_pages.get_device() != dev:
         raise ValueError("the pages must be CUDA tensors on one device")
-    inner = (ps * D, D, 1)
-    ks, vs = k_pages.stride(), v_pages.stride()
-    if ks[1:] != inner or vs[1:] != inner:
-        if not (k_pages[0].is_contiguous() and v_pages[0].is_contiguous()):   # (strides of planes of size 1 are free)
+    k_stride, *k_inner = k_pages.stride()
+    v_stride, *v_inner = v_pages.stride()
+    inner = [ps * D, D, 1]
+    if k_inner != inner or v_inner != inner:
+        if n > 0 and not (k_pages[0].is_contiguous() and v_pages[0].is_contiguous()):   # (of one plane the stride is free)
             raise ValueError("every page must be contiguous (pages may be any distance apart)")
-    if n > 1 and (ks[0] < k * ps * D or vs[0] < H * ps * D):
-        raise ValueError("pages must not overlap")
-    k_stride, v_stride = (ks[0], vs[0]) if n > 1 else (0, 0)
+    if n > 1:
+        if k_stride < k * ps * D or v_stride < H * ps * D:
+            raise ValueError("pages must not overlap")
+    else:
+        k_stride = v_stride = 0
     if k_scales is None:
         if k_pages.dtype not in _PAGED_IO or v_pages.dtype is not k_pages.dtype:
             raise TypeError("k_pages and v_pages must both be float32 or both bfloat16")
     else:
-        for t in (k_pages, v_pages):
-            if t.dtype is not torch.uint8 and t.dtype is not torch.float8_e4m3fn:
-                raise TypeError(f"e4m3 pages must be uint8 or float8_e4m3fn, got {t.dtype}")
-        _want(k_scales, "k_scales", (n, k, ps), torch.float32, device)
-        _want(v_scales, "v_scales", (n, H, ps), torch.float32, device)
+        if k_pages.dtype not in _E4M3 or v_pages.dtype not in _E4M3:
+            raise TypeError(f"e4m3 pages must be uint8 or float8_e4m3fn, got {k_pages.dtype} and {v_pages.dtype}")
+        _want(k_scales, "k_scales", (n, k, ps), torch.float32, dev)
+        _want(v_scales, "v_scales", (n, H, ps), torch.float32, dev)
     if block_table.dim() != 2:
         raise ValueError("block_table must be [B,max_pages]")
     B, max_pages = block_table.shape
-    _want(block_table, "block_table", (B, max_pages), torch.int32, device)
-    _want(seq_lens, "seq_lens", (B,), torch.int32, device)
-    return n, k, H, ps, D, k_stride, v_stride, B, max_pages, device
+    _want(block_table, "block_table", (B, max_pages), torch.int32, dev)
+    _want(seq_lens, "seq_lens", (B,), torch.int32, dev)
+    return n, k, H, ps, D, k_stride, v_stride, B, max_pages, dev
 
 
-def _paged_workspace(workspace, device):
+def _paged_workspace(workspace, dev):
     """(pointer, bytes) of a workspace, which may be None."""
     if workspace is None:
         return None, 0
-    if workspace.device != device or not workspace.is_contiguous():
-        raise ValueError(f"workspace must be contiguous and on {device}")
+    if workspace.get_device() != dev or not workspace.is_contiguous():
+        raise ValueError(f"workspace must be contiguous and on cuda:{dev}")
     return workspace.data_ptr(), workspace.numel() * workspace.element_size()
 
 
 def _append_paged(fn_name, k_new, v_new, k_pages, v_pages, k_scales, v_scales, reps, block_table, seq_lens, new_lens,
                   advance, workspace):
-    n, k, H, ps, D, k_stride, v_stride, B, max_pages, device = _pages(k_pages, v_pages, k_scales, v_scales, block_table,
+    n, k, H, ps, D, k_stride, v_stride, B, max_pages, dev = _pages(k_pages, v_pages, k_scales, v_scales, block_table,
                                                                       seq_lens)
     N = k_new.shape[2] if k_new.dim() == 4 else 1
     io = _PAGED_IO.get(k_new.dtype)
     if io is None or (k_scales is None and k_new.dtype is not k_pages.dtype):
         raise TypeError(f"k_new of type {k_new.dtype} does not go into pages of type {k_pages.dtype}")
     shape = (B, H, N, D) if k_new.dim() == 4 else (B, H, D)
-    _want(k_new, "k_new", shape, k_new.dtype, device)
-    _want(v_new, "v_new", shape, k_new.dtype, device)
-    _want(reps, "reps", (B, k), torch.int32, device)
+    _want(k_new, "k_new", shape, k_new.dtype, dev)
+    _want(v_new, "v_new", shape, k_new.dtype, dev)
+    _want(reps, "reps", (B, k), torch.int32, dev)
     if new_lens is not None:
-        _want(new_lens, "new_lens", (B,), torch.int32, device)
-    ws, ws_bytes = _paged_workspace(workspace, device)
+        _want(new_lens, "new_lens", (B,), torch.int32, dev)
+    ws, ws_bytes = _paged_workspace(workspace, dev)
     if workspace is not None and ws_bytes < 256:
         raise ValueError("workspace must hold at least 256 bytes")
     scales = () if k_scales is None else (k_scales.data_ptr(), v_scales.data_ptr())
-    _paged_call(getattr(load(), fn_name), device, k_new.data_ptr(), v_new.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(),
+    _paged_call(getattr(load(), fn_name), dev, k_new.data_ptr(), v_new.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(),
                 *scales, reps.data_ptr(), block_table.data_ptr(), seq_lens.data_ptr(), _ptr(new_lens), B, H, k, N, n, ps,
                 max_pages, D, k_stride, v_stride, io, 1 if advance else 0, ws)
 
@@ -578,14 +592,14 @@ def chai_append_kv_paged_fp8(k_new, v_new, k_pages, v_pages, k_scales, v_scales,
 
 
 def _read_paged(fn_name, k_pages, v_pages, k_scales, v_scales, block_table, seq_lens, T_out, dtype, k_out, v_out, workspace):
-    n, k, H, ps, D, k_stride, v_stride, B, max_pages, device = _pages(k_pages, v_pages, k_scales, v_scales, block_table,
+    n, k, H, ps, D, k_stride, v_stride, B, max_pages, dev = _pages(k_pages, v_pages, k_scales, v_scales, block_table,
                                                                       seq_lens)
     given = k_out if k_out is not None else v_out
     if given is None:
         if T_out is None:
             raise ValueError("give T_out, or the arrays to read into")
-        k_out = torch.zeros((B, k, T_out, D), device=device, dtype=dtype)
-        v_out = torch.zeros((B, H, T_out, D), device=device, dtype=dtype)
+        k_out = torch.zeros((B, k, T_out, D), device=k_pages.device, dtype=dtype)
+        v_out = torch.zeros((B, H, T_out, D), device=k_pages.device, dtype=dtype)
         given = k_out
     if given.dim() != 4:
         raise ValueError("k_out must be [B,k,T_out,D] and v_out [B,H,T_out,D]")
@@ -596,14 +610,14 @@ def _read_paged(fn_name, k_pages, v_pages, k_scales, v_scales, block_table, seq_
     if io is None or (k_scales is None and given.dtype is not k_pages.dtype):
         raise TypeError(f"pages of type {k_pages.dtype} are not read into arrays of type {given.dtype}")
     if k_out is not None:
-        _want(k_out, "k_out", (B, k, T_out, D), given.dtype, device)
+        _want(k_out, "k_out", (B, k, T_out, D), given.dtype, dev)
     if v_out is not None:
-        _want(v_out, "v_out", (B, H, T_out, D), given.dtype, device)
-    ws, ws_bytes = _paged_workspace(workspace, device)
+        _want(v_out, "v_out", (B, H, T_out, D), given.dtype, dev)
+    ws, ws_bytes = _paged_workspace(workspace, dev)
     if workspace is not None and ws_bytes < 256:
         raise ValueError("workspace must hold at least 256 bytes")
     scales = () if k_scales is None else (k_scales.data_ptr(), v_scales.data_ptr())
-    _paged_call(getattr(load(), fn_name), device, k_pages.data_ptr(), v_pages.data_ptr(), *scales, block_table.data_ptr(),
+    _paged_call(getattr(load(), fn_name), dev, k_pages.data_ptr(), v_pages.data_ptr(), *scales, block_table.data_ptr(),
                 seq_lens.data_ptr(), _ptr(k_out), _ptr(v_out), B, H, k, T_out, n, ps, max_pages, D, k_stride, v_stride, io,
                 ws)
     return k_out, v_out
@@ -630,23 +644,23 @@ def chai_decode_paged_workspace_bytes(B, H, D) -> int:
 
 def _decode_paged(fn_name, q, k_pages, v_pages, k_scales, v_scales, membership, reps, block_table, seq_lens, scale, out,
                   workspace):
-    n, k, H, ps, D, k_stride, v_stride, B, max_pages, device = _pages(k_pages, v_pages, k_scales, v_scales, block_table,
+    n, k, H, ps, D, k_stride, v_stride, B, max_pages, dev = _pages(k_pages, v_pages, k_scales, v_scales, block_table,
                                                                       seq_lens)
     io = _PAGED_IO.get(q.dtype)
     if io is None or (k_scales is None and q.dtype is not k_pages.dtype):
         raise TypeError(f"queries of type {q.dtype} do not go with pages of type {k_pages.dtype}")
-    _want(q, "q", (B, H, D), q.dtype, device)
-    _want(membership, "membership", (B, H), torch.int32, device)
-    _want(reps, "reps", (B, k), torch.int32, device)
+    _want(q, "q", (B, H, D), q.dtype, dev)
+    _want(membership, "membership", (B, H), torch.int32, dev)
+    _want(reps, "reps", (B, k), torch.int32, dev)
     if out is None:
         out = torch.empty_like(q)
     else:
-        _want(out, "out", (B, H, D), q.dtype, device)
+        _want(out, "out", (B, H, D), q.dtype, dev)
     if workspace is None:
-        workspace = new_workspace(chai_decode_paged_workspace_bytes(B, H, D), device)
-    ws, ws_bytes = _paged_workspace(workspace, device)
+        workspace = new_workspace(chai_decode_paged_workspace_bytes(B, H, D), q.device)
+    ws, ws_bytes = _paged_workspace(workspace, dev)
     scales = () if k_scales is None else (k_scales.data_ptr(), v_scales.data_ptr())
-    _paged_call(getattr(load(), fn_name), device, q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), *scales,
+    _paged_call(getattr(load(), fn_name), dev, q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), *scales,
                 membership.data_ptr(), reps.data_ptr(), block_table.data_ptr(), seq_lens.data_ptr(), out.data_ptr(), B, H, k,
                 n, ps, max_pages, D, k_stride, v_stride, scale, io, ws, ws_bytes)
     return out

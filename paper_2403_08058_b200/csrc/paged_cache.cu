@@ -4,16 +4,22 @@
 //   chai_append_kv_paged, _fp8   N new tokens per request -> rows of the request's pages, as they are or as e4m3
 //   chai_read_kv_paged, _fp8     the cached rows of every request -> dense arrays
 //
-// Both are copies, bound by HBM.  The rows (plane, token) of a request are one sequence of 16-byte vectors of the dense
-// side; a thread moves four of them with all loads issued before the first store.  Where a vector goes follows from two
-// divisions by multiplication (FastDiv).
+// Both are copies, bound by HBM.  A block takes a run of tokens of one plane; a thread moves several 16-byte vectors of
+// the dense side, all loads issued before the first store.  (One sequence of vectors over planes and tokens alike, with
+// a division to find the plane of each, was bound by its instructions instead: append to e4m3 65 us where this takes
+// APPENDF8, read-back from e4m3 69 us and READF8.)  A decode step's few rows go to one block per request that also advances
+// the request's length.
+#include <type_traits>
+
 #include "paged.cuh"
 
 namespace chai {
 namespace {
 
-constexpr int kCopyUnroll = 4;
 constexpr int kCopyThreads = 256;
+constexpr int kStepUnroll = 4;       // vectors a thread has in flight: a decode step's append ...
+constexpr int kAppendUnroll = 4;     // ... a prompt's ...
+constexpr int kReadUnroll = 4;       // ... and read-back (twice as many from e4m3, whose loads are half as long)
 
 __global__ void paged_reset_status_kernel(WsHeader* hdr) {
     dependent_grid_sync();
@@ -68,38 +74,61 @@ __device__ __forceinline__ bool tokens_fit(const AppendArgs& a, int b, int* pos0
     return *pos0 >= 0 && (*n == 0 || *pos0 <= a.pool.capacity - *n);
 }
 
-// grid (blocks of a request, B).  FUSED: one block per request, which also advances its length.
-template <typename TS, int D, bool FP8, bool FUSED>
-__global__ void __launch_bounds__(kCopyThreads) append_paged_kernel(const AppendArgs a) {
-    if constexpr (FUSED) dependent_grid_sync();
+// Stores the vector x of a row at `row` of plane `pl` (of the keys or the values) of a page; page -1: nothing.  The LPR
+// lanes of a row are neighbours in one warp and call this together.
+template <typename TS, int D, bool FP8>
+__device__ __forceinline__ void store_vector(const AppendArgs& a, bool key, int pl, int page, int row, int x, const uint4& raw) {
     constexpr int LPR = D * (int)sizeof(TS) / 16, EPV = 16 / (int)sizeof(TS);
-    __shared__ int s_bad;
+    const size_t at = (size_t)page * (key ? a.pool.k_page_stride : a.pool.v_page_stride) +
+                      ((size_t)pl * a.pool.page_size + row) * D + x * EPV;
+    if constexpr (!FP8) {
+        if (page >= 0) *reinterpret_cast<uint4*>(static_cast<TS*>(key ? a.k_pages : a.v_pages) + at) = raw;
+    } else {
+        float f[EPV];
+        Vec16<TS>::unpack(raw, f);
+        unsigned amax = 0;
+#pragma unroll
+        for (int e = 0; e < EPV; ++e) amax = max(amax, finite_magnitude(f[e]));
+#pragma unroll
+        for (int o = LPR / 2; o > 0; o >>= 1) amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, o));
+        const int e2 = amax == 0 ? 0 : scale_exponent(amax);
+        unsigned w[EPV / 4];
+        quantize<EPV>(f, pow2(-e2), w);
+        if (page >= 0) {
+            unsigned char* dst = static_cast<unsigned char*>(key ? a.k_pages : a.v_pages) + at;
+            if constexpr (EPV == 8) *reinterpret_cast<uint2*>(dst) = make_uint2(w[0], w[1]);
+            else *reinterpret_cast<unsigned*>(dst) = w[0];
+            if (x == 0)
+                (key ? a.k_scales : a.v_scales)[((size_t)page * (key ? a.k : a.H) + pl) * a.pool.page_size + row] = pow2(e2);
+        }
+    }
+}
+
+// A decode step's tokens: grid (1, B), one block moves all rows of a request and advances its length.
+template <typename TS, int D, bool FP8>
+__global__ void __launch_bounds__(kCopyThreads) append_step_kernel(const AppendArgs a) {
+    dependent_grid_sync();
+    constexpr int LPR = D * (int)sizeof(TS) / 16, EPV = 16 / (int)sizeof(TS);
     const int b = blockIdx.y, tid = threadIdx.x;
     int pos0, n;
     const bool fit = tokens_fit(a, b, &pos0, &n);
-    if constexpr (FUSED) {
-        if (tid == 0) s_bad = 0;
-        __syncthreads();  // every thread holds the position before thread 0 may advance it
-    }
+    __syncthreads();  // every thread holds the position before thread 0 may advance it
     if (!fit) {
-        if (tid == 0 && blockIdx.x == 0) flag_status(a.hdr, CHAI_ERR_CACHE_FULL, b);
+        if (tid == 0) flag_status(a.hdr, CHAI_ERR_CACHE_FULL, b);
         return;
     }
     const int32_t* table = a.pool.block_table + (size_t)b * a.pool.max_pages;
     const int32_t* reps = a.reps + (size_t)b * a.k;
     const TS* k_new = static_cast<const TS*>(a.k_new) + (size_t)b * a.H * a.N * D;
     const TS* v_new = static_cast<const TS*>(a.v_new) + (size_t)b * a.H * a.N * D;
-    const size_t total = (size_t)(a.k + a.H) * a.N * LPR;
-    const size_t per_block = (size_t)kCopyThreads * kCopyUnroll;
+    const unsigned total = (unsigned)(a.k + a.H) * a.N * LPR;
     bool bad = false;
-    for (size_t base = blockIdx.x * per_block; base < total; base += gridDim.x * per_block) {
-        uint4 raw[kCopyUnroll];
-        int page[kCopyUnroll], plane[kCopyUnroll], row[kCopyUnroll];  // page -1: nothing to store
+    for (unsigned base = 0; base < total; base += kCopyThreads * kStepUnroll) {
+        uint4 raw[kStepUnroll];
+        int page[kStepUnroll], plane[kStepUnroll], row[kStepUnroll];  // page -1: nothing to store
 #pragma unroll
-        for (int u = 0; u < kCopyUnroll; ++u) {
-            const size_t i = base + (size_t)u * kCopyThreads + tid;
-            const unsigned r = (unsigned)(i / LPR);
-            const int x = (int)(i % LPR);
+        for (int u = 0; u < kStepUnroll; ++u) {
+            const unsigned i = base + u * kCopyThreads + tid, r = i / LPR;
             plane[u] = (int)a.by_n.div(r);
             const int t = (int)(r - (unsigned)plane[u] * (unsigned)a.N);
             raw[u] = make_uint4(0, 0, 0, 0);
@@ -109,53 +138,73 @@ __global__ void __launch_bounds__(kCopyThreads) append_paged_kernel(const Append
             const unsigned pos = (unsigned)(pos0 + t), pi = a.pool.by_page.div(pos);
             row[u] = (int)(pos - pi * (unsigned)a.pool.page_size);
             const int pg = table[pi];
+            const bool known = pg >= 0 && pg < a.pool.n_pages;
+            bad |= !known;
             int head = plane[u] - a.k;
             if (plane[u] < a.k) {
                 head = reps[plane[u]];
                 if (head < 0 || head >= a.H) continue;  // unused cluster slot
             }
-            const TS* src = (plane[u] < a.k ? k_new : v_new) + ((size_t)head * a.N + t) * D;
-            raw[u] = ld_stream16(src + x * EPV);
-            if (pg < 0 || pg >= a.pool.n_pages) bad = true;
-            else page[u] = pg;
+            raw[u] = ld_stream16((plane[u] < a.k ? k_new : v_new) + ((size_t)head * a.N + t) * D + (int)(i % LPR) * EPV);
+            page[u] = known ? pg : -1;
         }
 #pragma unroll
-        for (int u = 0; u < kCopyUnroll; ++u) {
-            const int x = (int)((base + (size_t)u * kCopyThreads + tid) % LPR);
+        for (int u = 0; u < kStepUnroll; ++u) {
             const bool key = plane[u] < a.k;
-            const int planes = key ? a.k : a.H, pl = key ? plane[u] : plane[u] - a.k;
-            const size_t at = (size_t)page[u] * (key ? a.pool.k_page_stride : a.pool.v_page_stride) +
-                              ((size_t)pl * a.pool.page_size + row[u]) * D + x * EPV;
-            if constexpr (!FP8) {
-                if (page[u] >= 0) *reinterpret_cast<uint4*>(static_cast<TS*>(key ? a.k_pages : a.v_pages) + at) = raw[u];
-            } else {
-                // the LPR lanes of a row are neighbours in one warp and take every branch together up to the store
-                float f[EPV];
-                Vec16<TS>::unpack(raw[u], f);
-                unsigned amax = 0;
-#pragma unroll
-                for (int e = 0; e < EPV; ++e) amax = max(amax, finite_magnitude(f[e]));
-#pragma unroll
-                for (int o = LPR / 2; o > 0; o >>= 1) amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, o));
-                const int e2 = amax == 0 ? 0 : scale_exponent(amax);
-                unsigned w[EPV / 4];
-                quantize<EPV>(f, pow2(-e2), w);
-                if (page[u] >= 0) {
-                    unsigned char* dst = static_cast<unsigned char*>(key ? a.k_pages : a.v_pages) + at;
-                    if constexpr (EPV == 8) *reinterpret_cast<uint2*>(dst) = make_uint2(w[0], w[1]);
-                    else *reinterpret_cast<unsigned*>(dst) = w[0];
-                    if (x == 0)
-                        (key ? a.k_scales : a.v_scales)[((size_t)page[u] * planes + pl) * a.pool.page_size + row[u]] = pow2(e2);
-                }
-            }
+            store_vector<TS, D, FP8>(a, key, key ? plane[u] : plane[u] - a.k, page[u], row[u], tid % LPR, raw[u]);
         }
     }
     if (bad) flag_status(a.hdr, CHAI_ERR_BAD_PAGE, b);
-    if constexpr (FUSED) {
-        if (bad) s_bad = 1;
-        __syncthreads();
-        if (tid == 0 && a.advance && !s_bad) a.seq_lens[b] = pos0 + n;
+    bad = __syncthreads_or(bad);
+    if (tid == 0 && a.advance && !bad) a.seq_lens[b] = pos0 + n;
+}
+
+// A prompt's tokens: grid (runs of tokens, planes, B).
+template <typename TS, int D, bool FP8>
+__global__ void __launch_bounds__(kCopyThreads) append_rows_kernel(const AppendArgs a) {
+    constexpr int LPR = D * (int)sizeof(TS) / 16, EPV = 16 / (int)sizeof(TS), ROWS = kCopyThreads / LPR;
+    const int plane = blockIdx.y, b = blockIdx.z, x = threadIdx.x % LPR;
+    const int t0 = blockIdx.x * (ROWS * kAppendUnroll) + threadIdx.x / LPR;
+    int pos0, n;
+    if (!tokens_fit(a, b, &pos0, &n)) {
+        if (threadIdx.x == 0 && blockIdx.x == 0 && plane == 0) flag_status(a.hdr, CHAI_ERR_CACHE_FULL, b);
+        return;
     }
+    if ((int)(blockIdx.x * (ROWS * kAppendUnroll)) >= n) return;
+    const bool key = plane < a.k;
+    int head = plane - a.k;
+    const int pl = key ? plane : head;
+    if (key) {
+        head = a.reps[(size_t)b * a.k + plane];
+        if (head < 0 || head >= a.H) return;  // unused cluster slot
+    }
+    const int32_t* table = a.pool.block_table + (size_t)b * a.pool.max_pages;
+    const TS* src = static_cast<const TS*>(key ? a.k_new : a.v_new) + (((size_t)b * a.H + head) * a.N + t0) * D + x * EPV;
+    uint4 raw[kAppendUnroll];
+    int page[kAppendUnroll], row[kAppendUnroll];  // page -1: nothing to store
+    bool bad = false;
+#pragma unroll
+    for (int u = 0; u < kAppendUnroll; ++u) {
+        const int t = t0 + u * ROWS;
+        raw[u] = make_uint4(0, 0, 0, 0);
+        page[u] = -1;
+        row[u] = 0;
+        if (t < n) {
+            raw[u] = ld_stream16(src + (size_t)u * ROWS * D);
+            const unsigned pos = (unsigned)(pos0 + t), pi = a.pool.by_page.div(pos);
+            row[u] = (int)(pos - pi * (unsigned)a.pool.page_size);
+            page[u] = table[pi];
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < kAppendUnroll; ++u) {
+        if (page[u] < 0 || page[u] >= a.pool.n_pages) {
+            bad |= t0 + u * ROWS < n;
+            page[u] = -1;
+        }
+        store_vector<TS, D, FP8>(a, key, pl, page[u], row[u], x, raw[u]);
+    }
+    if (bad) flag_status(a.hdr, CHAI_ERR_BAD_PAGE, b);
 }
 
 // Advances the lengths behind an append of many blocks: every request whose tokens fit and whose pages are all good.
@@ -175,18 +224,14 @@ __global__ void __launch_bounds__(128) advance_paged_kernel(const AppendArgs a) 
 
 template <typename TS, int D, bool FP8>
 int launch_append(const AppendArgs& a, int B, cudaStream_t s) {
-    constexpr int LPR = D * (int)sizeof(TS) / 16;
-    const size_t total = (size_t)(a.k + a.H) * a.N * LPR, per_block = (size_t)kCopyThreads * kCopyUnroll;
-    // A decode step's tokens: one block per request moves them in a pass or two and advances the length itself, which
-    // saves a launch; a prompt's rows are spread over the GPU and the lengths follow in a launch of their own.
-    if (total <= 4 * per_block) {
-        CHAI_LAUNCH_DEPENDENT("append_paged_kernel launch", (append_paged_kernel<TS, D, FP8, true>), dim3(1, B),
-                              dim3(kCopyThreads), 0, s, a);
+    constexpr int LPR = D * (int)sizeof(TS) / 16, TOKENS = kCopyThreads / LPR * kAppendUnroll;
+    // One block per request saves the launch that advances the lengths, as long as it has a few passes to make.
+    if ((size_t)(a.k + a.H) * a.N * LPR <= 4 * kCopyThreads * kStepUnroll) {
+        CHAI_LAUNCH_DEPENDENT("append_step_kernel launch", (append_step_kernel<TS, D, FP8>), dim3(1, B), dim3(kCopyThreads), 0, s, a);
         return CHAI_OK;
     }
-    const size_t blocks = (total + per_block - 1) / per_block;
-    append_paged_kernel<TS, D, FP8, false><<<dim3((unsigned)blocks, B), kCopyThreads, 0, s>>>(a);
-    CHAI_LAUNCH_CHECK("append_paged_kernel launch");
+    append_rows_kernel<TS, D, FP8><<<dim3((a.N + TOKENS - 1) / TOKENS, a.k + a.H, B), kCopyThreads, 0, s>>>(a);
+    CHAI_LAUNCH_CHECK("append_rows_kernel launch");
     if (a.advance) CHAI_LAUNCH_DEPENDENT("advance_paged_kernel launch", advance_paged_kernel, dim3(B), dim3(128), 0, s, a);
     return CHAI_OK;
 }
@@ -227,7 +272,6 @@ struct ReadArgs {
     void *k_out, *v_out;
     WsHeader* hdr;
     PagePool pool;
-    FastDiv by_t;
     int H, k, T_out;
     int nk, nv;  // planes that are wanted
 };
@@ -250,64 +294,55 @@ __device__ __forceinline__ uint4 pack16<__nv_bfloat16>(const float* f) {
     return r;
 }
 
-// grid (blocks of a request, B): a thread writes four 16-byte vectors of the dense arrays.
+// grid (runs of tokens, planes that are wanted, B).
 template <typename TO, int D, bool FP8>
 __global__ void __launch_bounds__(kCopyThreads) read_paged_kernel(const ReadArgs a) {
-    constexpr int LPR = D * (int)sizeof(TO) / 16, EPV = 16 / (int)sizeof(TO);
-    const int b = blockIdx.y, tid = threadIdx.x;
+    constexpr int LPR = D * (int)sizeof(TO) / 16, EPV = 16 / (int)sizeof(TO), ROWS = kCopyThreads / LPR;
+    constexpr int UNROLL = FP8 ? 2 * kReadUnroll : kReadUnroll;
+    const int plane = blockIdx.y, b = blockIdx.z, x = threadIdx.x % LPR;
+    const int t0 = blockIdx.x * (ROWS * UNROLL) + threadIdx.x / LPR;
     const int n = min(min(max(a.seq_lens[b], 0), a.pool.capacity), a.T_out);
+    if ((int)(blockIdx.x * (ROWS * UNROLL)) >= n) return;
+    const bool key = plane < a.nk;
+    const int pl = key ? plane : plane - a.nk;
     const int32_t* table = a.pool.block_table + (size_t)b * a.pool.max_pages;
-    const size_t total = (size_t)(a.nk + a.nv) * a.T_out * LPR;
-    const size_t base = (size_t)blockIdx.x * kCopyThreads * kCopyUnroll;
-    TO* k_out = static_cast<TO*>(a.k_out) + (size_t)b * a.nk * a.T_out * D;
-    TO* v_out = static_cast<TO*>(a.v_out) + (size_t)b * a.nv * a.T_out * D;
-    uint4 raw[kCopyUnroll];
-    float scale[kCopyUnroll];
-    TO* dst[kCopyUnroll];
+    using Raw = typename std::conditional<FP8, typename std::conditional<EPV == 8, uint2, unsigned>::type, uint4>::type;
+    Raw raw[UNROLL];
+    [[maybe_unused]] float scale[UNROLL];
+    int page[UNROLL], row[UNROLL];
     bool bad = false;
 #pragma unroll
-    for (int u = 0; u < kCopyUnroll; ++u) {
-        const size_t i = base + (size_t)u * kCopyThreads + tid;
-        const unsigned r = (unsigned)(i / LPR);
-        const int x = (int)(i % LPR);
-        const int plane = (int)a.by_t.div(r);
-        const int t = (int)(r - (unsigned)plane * (unsigned)a.T_out);
-        raw[u] = make_uint4(0, 0, 0, 0);
+    for (int u = 0; u < UNROLL; ++u) {
+        const int t = t0 + u * ROWS;
+        const unsigned pos = (unsigned)min(t, n - 1), pi = a.pool.by_page.div(pos);
+        row[u] = (int)(pos - pi * (unsigned)a.pool.page_size);
+        page[u] = table[pi];
+    }
+    const char* pages = static_cast<const char*>(key ? a.k_pages : a.v_pages);
+    const size_t stride = key ? a.pool.k_page_stride : a.pool.v_page_stride;
+#pragma unroll
+    for (int u = 0; u < UNROLL; ++u) {
+        raw[u] = Raw{};
         scale[u] = 0.f;
-        dst[u] = nullptr;
-        if (i >= total || t >= n) continue;
-        const bool key = plane < a.nk;
-        const int planes = key ? a.k : a.H, pl = key ? plane : plane - a.nk;
-        dst[u] = (key ? k_out : v_out) + ((size_t)pl * a.T_out + t) * D + x * EPV;
-        const unsigned pi = a.pool.by_page.div((unsigned)t);
-        const int row = (int)((unsigned)t - pi * (unsigned)a.pool.page_size), page = table[pi];
-        if (page < 0 || page >= a.pool.n_pages) {
-            bad = true;
-            continue;
-        }
-        const size_t at = (size_t)page * (key ? a.pool.k_page_stride : a.pool.v_page_stride) +
-                          ((size_t)pl * a.pool.page_size + row) * D + x * EPV;
-        const void* pages = key ? a.k_pages : a.v_pages;
-        if constexpr (!FP8) {
-            raw[u] = ld_stream16(static_cast<const TO*>(pages) + at);
-        } else {
-            const unsigned char* src = static_cast<const unsigned char*>(pages) + at;
-            if constexpr (EPV == 8) {
-                const uint2 w = __ldcs(reinterpret_cast<const uint2*>(src));
-                raw[u].x = w.x;
-                raw[u].y = w.y;
-            } else {
-                raw[u].x = __ldcs(reinterpret_cast<const unsigned*>(src));
-            }
-            scale[u] = (key ? a.k_scales : a.v_scales)[((size_t)page * planes + pl) * a.pool.page_size + row];
+        if (page[u] < 0 || page[u] >= a.pool.n_pages) {
+            bad = true;  // the row is zero
+        } else if (t0 + u * ROWS < n) {
+            const size_t at = (size_t)page[u] * stride + ((size_t)pl * a.pool.page_size + row[u]) * D + x * EPV;
+            raw[u] = __ldcs(reinterpret_cast<const Raw*>(pages + at * (FP8 ? 1 : sizeof(TO))));
+            if constexpr (FP8)
+                scale[u] = __ldg((key ? a.k_scales : a.v_scales) + ((size_t)page[u] * (key ? a.k : a.H) + pl) * a.pool.page_size + row[u]);
         }
     }
+    TO* dst = static_cast<TO*>(key ? a.k_out : a.v_out) + (((size_t)b * (key ? a.nk : a.nv) + pl) * a.T_out + t0) * D + x * EPV;
 #pragma unroll
-    for (int u = 0; u < kCopyUnroll; ++u) {
-        if (dst[u] == nullptr) continue;
+    for (int u = 0; u < UNROLL; ++u) {
+        if (t0 + u * ROWS >= n) break;
+        uint4 v;
         if constexpr (FP8) {
+            unsigned w[2] = {0, 0};
+            if constexpr (EPV == 8) w[0] = raw[u].x, w[1] = raw[u].y;
+            else w[0] = raw[u];
             float f[EPV];
-            const unsigned w[2] = {raw[u].x, raw[u].y};
 #pragma unroll
             for (int e = 0; e < EPV / 2; ++e) {
                 const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)((w[e / 2] >> (16 * (e & 1))) & 0xffffu), __NV_E4M3);
@@ -315,18 +350,19 @@ __global__ void __launch_bounds__(kCopyThreads) read_paged_kernel(const ReadArgs
                 f[2 * e] = p.x * scale[u];
                 f[2 * e + 1] = p.y * scale[u];
             }
-            raw[u] = pack16<TO>(f);
+            v = pack16<TO>(f);
+        } else {
+            v = raw[u];
         }
-        __stcs(reinterpret_cast<uint4*>(dst[u]), raw[u]);
+        __stcs(reinterpret_cast<uint4*>(dst + (size_t)u * ROWS * D), v);
     }
     if (bad) flag_status(a.hdr, CHAI_ERR_BAD_PAGE, b);
 }
 
 template <typename TO, int D, bool FP8>
 int launch_read(const ReadArgs& a, int B, cudaStream_t s) {
-    constexpr int LPR = D * (int)sizeof(TO) / 16;
-    const size_t total = (size_t)(a.nk + a.nv) * a.T_out * LPR, per_block = (size_t)kCopyThreads * kCopyUnroll;
-    read_paged_kernel<TO, D, FP8><<<dim3((unsigned)((total + per_block - 1) / per_block), B), kCopyThreads, 0, s>>>(a);
+    constexpr int LPR = D * (int)sizeof(TO) / 16, TOKENS = kCopyThreads / LPR * (FP8 ? 2 * kReadUnroll : kReadUnroll);
+    read_paged_kernel<TO, D, FP8><<<dim3((a.T_out + TOKENS - 1) / TOKENS, a.nk + a.nv, B), kCopyThreads, 0, s>>>(a);
     CHAI_LAUNCH_CHECK("read_paged_kernel launch");
     return CHAI_OK;
 }
@@ -345,7 +381,6 @@ int read_back(const char* fn, bool fp8, ReadArgs a, int B, int n_pages, int page
     if (rc != CHAI_OK) return rc;
     CHAI_REQUIRE(a.T_out > 0, CHAI_ERR_INVALID_ARG, "%s: need T_out > 0", fn);
     CHAI_REQUIRE((long long)a.H * a.T_out < (1ll << 30), CHAI_ERR_UNSUPPORTED, "%s: H*T_out must be below 2^30", fn);
-    a.by_t = FastDiv((unsigned)a.T_out);
     a.nk = a.k_out != nullptr ? a.k : 0;
     a.nv = a.v_out != nullptr ? a.H : 0;
     CHAI_LOG_CALL("%s: B=%d H=%d k=%d T_out=%d D=%d dtype=%d page_size=%d", fn, B, a.H, a.k, a.T_out, D, dtype, page_size);
