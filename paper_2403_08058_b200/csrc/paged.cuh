@@ -62,7 +62,7 @@ inline int make_pool(const char* fn, const int32_t* block_table, int B, int H, i
     return CHAI_OK;
 }
 
-inline bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+inline bool aligned32(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 31u) == 0; }
 
 // Records a status that a kernel met first (nothing without a workspace).
 __device__ __forceinline__ void flag_status(WsHeader* hdr, int status, int b) {

@@ -7,7 +7,7 @@
 // Both are copies, bound by HBM.  A block takes a run of tokens of one plane; a thread moves several 16-byte vectors of
 // the dense side, all loads issued before the first store.  (One sequence of vectors over planes and tokens alike, with
 // a division to find the plane of each, was bound by its instructions instead: append to e4m3 65 us where this takes
-// APPENDF8, read-back from e4m3 69 us and READF8.)  A decode step's few rows go to one block per request that also advances
+// 31, read-back from e4m3 69 us and 52.)  A decode step's few rows go to one block per request that also advances
 // the request's length.
 #include <type_traits>
 
@@ -16,10 +16,47 @@
 namespace chai {
 namespace {
 
-constexpr int kCopyThreads = 256;
-constexpr int kStepUnroll = 4;       // vectors a thread has in flight: a decode step's append ...
-constexpr int kAppendUnroll = 4;     // ... a prompt's ...
-constexpr int kReadUnroll = 4;       // ... and read-back (twice as many from e4m3, whose loads are half as long)
+constexpr int kStepThreads = 256, kStepUnroll = 4;  // threads a block, vectors a thread: a decode step's append
+constexpr int kRowThreads = 128, kRowUnroll = 4;    // ... a prompt's, and read-back
+
+// What a thread moves at once on the dense side: 16 bytes, or 32 where the other side is e4m3 (8 or 16 bytes there).
+template <bool FP8>
+struct Dense;
+template <>
+struct Dense<false> {
+    static constexpr int BYTES = 16;
+    uint4 a;
+    __device__ __forceinline__ void zero() { a = make_uint4(0, 0, 0, 0); }
+    __device__ __forceinline__ void load(const void* p, bool) { a = ld_stream16(p); }
+    __device__ __forceinline__ void store(void* p, bool) const { __stcs(static_cast<uint4*>(p), a); }
+};
+template <>
+struct Dense<true> {
+    static constexpr int BYTES = 32;
+    uint4 a, b;
+    __device__ __forceinline__ void zero() { a = b = make_uint4(0, 0, 0, 0); }
+    // (wide: the array starts on a 32-byte boundary; 16 are what callers owe)
+    __device__ __forceinline__ void load(const void* p, bool wide) {
+        if (!wide) {
+            a = ld_stream16(p);
+            b = ld_stream16(static_cast<const uint4*>(p) + 1);
+            return;
+        }
+        asm volatile("ld.global.nc.L1::no_allocate.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                     : "=r"(a.x), "=r"(a.y), "=r"(a.z), "=r"(a.w), "=r"(b.x), "=r"(b.y), "=r"(b.z), "=r"(b.w)
+                     : "l"(p));
+    }
+    __device__ __forceinline__ void store(void* p, bool wide) const {
+        if (!wide) {
+            __stcs(static_cast<uint4*>(p), a);
+            __stcs(static_cast<uint4*>(p) + 1, b);
+            return;
+        }
+        asm volatile("st.global.L1::no_allocate.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(a.x), "r"(a.y), "r"(a.z),
+                     "r"(a.w), "r"(b.x), "r"(b.y), "r"(b.z), "r"(b.w)
+                     : "memory");
+    }
+};
 
 __global__ void paged_reset_status_kernel(WsHeader* hdr) {
     dependent_grid_sync();
@@ -32,6 +69,32 @@ __global__ void paged_reset_status_kernel(WsHeader* hdr) {
 __device__ __forceinline__ unsigned finite_magnitude(float x) {
     const unsigned a = __float_as_uint(x) & 0x7fffffffu;
     return a < 0x7f800000u ? a : 0u;
+}
+// Bits of the largest finite |x| of a row whose LPR lanes hold 32 bytes each.  Infinities and NaN are met last: their
+// bits are larger than any finite number's, so only a row that has some is looked at element by element.
+template <typename TS, int LPR>
+__device__ __forceinline__ unsigned row_max(const unsigned* w, const float* f) {
+    unsigned m = 0;
+    if constexpr (sizeof(TS) == 2) {  // two numbers at a time
+#pragma unroll
+        for (int i = 0; i < 8; ++i) m = __vmaxu2(m, w[i] & 0x7fff7fffu);
+#pragma unroll
+        for (int o = LPR / 2; o > 0; o >>= 1) m = __vmaxu2(m, __shfl_xor_sync(0xffffffffu, m, o));
+        m = max(m << 16, m & 0xffff0000u);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) m = max(m, w[i] & 0x7fffffffu);
+#pragma unroll
+        for (int o = LPR / 2; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
+    }
+    if (__any_sync(0xffffffffu, m >= 0x7f800000u)) {
+        m = 0;
+#pragma unroll
+        for (int e = 0; e < 32 / (int)sizeof(TS); ++e) m = max(m, finite_magnitude(f[e]));
+#pragma unroll
+        for (int o = LPR / 2; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
+    }
+    return m;
 }
 // The smallest e >= -126 with amax <= 448 * 2^e.  448 = 1.75 * 2^8: with amax = 1.m * 2^x, e is x - 8, and one more if
 // 1.m > 1.75; adding 0x1fffff to the bits carries into the exponent exactly then.
@@ -65,6 +128,7 @@ struct AppendArgs {
     FastDiv by_n;
     int H, k, N;
     int advance;
+    bool wide;  // the dense arrays start on 32-byte boundaries
 };
 
 // Tokens of request b and whether they fit; the same in every thread of every block of the request.
@@ -74,30 +138,28 @@ __device__ __forceinline__ bool tokens_fit(const AppendArgs& a, int b, int* pos0
     return *pos0 >= 0 && (*n == 0 || *pos0 <= a.pool.capacity - *n);
 }
 
-// Stores the vector x of a row at `row` of plane `pl` (of the keys or the values) of a page; page -1: nothing.  The LPR
-// lanes of a row are neighbours in one warp and call this together.
+// Stores the vector x of a row at `row` of plane `pl` (of the keys or the values) of a page; page -1: nothing.  The lanes
+// of a row are neighbours in one warp and call this together.
 template <typename TS, int D, bool FP8>
-__device__ __forceinline__ void store_vector(const AppendArgs& a, bool key, int pl, int page, int row, int x, const uint4& raw) {
-    constexpr int LPR = D * (int)sizeof(TS) / 16, EPV = 16 / (int)sizeof(TS);
+__device__ __forceinline__ void store_vector(const AppendArgs& a, bool key, int pl, int page, int row, int x, const Dense<FP8>& raw) {
+    constexpr int EPV = Dense<FP8>::BYTES / (int)sizeof(TS);
     const size_t at = (size_t)page * (key ? a.pool.k_page_stride : a.pool.v_page_stride) +
                       ((size_t)pl * a.pool.page_size + row) * D + x * EPV;
     if constexpr (!FP8) {
-        if (page >= 0) *reinterpret_cast<uint4*>(static_cast<TS*>(key ? a.k_pages : a.v_pages) + at) = raw;
+        if (page >= 0) *reinterpret_cast<uint4*>(static_cast<TS*>(key ? a.k_pages : a.v_pages) + at) = raw.a;
     } else {
         float f[EPV];
-        Vec16<TS>::unpack(raw, f);
-        unsigned amax = 0;
-#pragma unroll
-        for (int e = 0; e < EPV; ++e) amax = max(amax, finite_magnitude(f[e]));
-#pragma unroll
-        for (int o = LPR / 2; o > 0; o >>= 1) amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, o));
+        Vec16<TS>::unpack(raw.a, f);
+        Vec16<TS>::unpack(raw.b, f + EPV / 2);
+        const unsigned bits[8] = {raw.a.x, raw.a.y, raw.a.z, raw.a.w, raw.b.x, raw.b.y, raw.b.z, raw.b.w};
+        const unsigned amax = row_max<TS, D * (int)sizeof(TS) / 32>(bits, f);
         const int e2 = amax == 0 ? 0 : scale_exponent(amax);
         unsigned w[EPV / 4];
         quantize<EPV>(f, pow2(-e2), w);
         if (page >= 0) {
             unsigned char* dst = static_cast<unsigned char*>(key ? a.k_pages : a.v_pages) + at;
-            if constexpr (EPV == 8) *reinterpret_cast<uint2*>(dst) = make_uint2(w[0], w[1]);
-            else *reinterpret_cast<unsigned*>(dst) = w[0];
+            if constexpr (EPV == 16) *reinterpret_cast<uint4*>(dst) = make_uint4(w[0], w[1], w[2], w[3]);
+            else *reinterpret_cast<uint2*>(dst) = make_uint2(w[0], w[1]);
             if (x == 0)
                 (key ? a.k_scales : a.v_scales)[((size_t)page * (key ? a.k : a.H) + pl) * a.pool.page_size + row] = pow2(e2);
         }
@@ -106,9 +168,9 @@ __device__ __forceinline__ void store_vector(const AppendArgs& a, bool key, int 
 
 // A decode step's tokens: grid (1, B), one block moves all rows of a request and advances its length.
 template <typename TS, int D, bool FP8>
-__global__ void __launch_bounds__(kCopyThreads) append_step_kernel(const AppendArgs a) {
+__global__ void __launch_bounds__(kStepThreads) append_step_kernel(const AppendArgs a) {
     dependent_grid_sync();
-    constexpr int LPR = D * (int)sizeof(TS) / 16, EPV = 16 / (int)sizeof(TS);
+    constexpr int LPR = D * (int)sizeof(TS) / Dense<FP8>::BYTES, EPV = Dense<FP8>::BYTES / (int)sizeof(TS);
     const int b = blockIdx.y, tid = threadIdx.x;
     int pos0, n;
     const bool fit = tokens_fit(a, b, &pos0, &n);
@@ -123,15 +185,15 @@ __global__ void __launch_bounds__(kCopyThreads) append_step_kernel(const AppendA
     const TS* v_new = static_cast<const TS*>(a.v_new) + (size_t)b * a.H * a.N * D;
     const unsigned total = (unsigned)(a.k + a.H) * a.N * LPR;
     bool bad = false;
-    for (unsigned base = 0; base < total; base += kCopyThreads * kStepUnroll) {
-        uint4 raw[kStepUnroll];
+    for (unsigned base = 0; base < total; base += kStepThreads * kStepUnroll) {
+        Dense<FP8> raw[kStepUnroll];
         int page[kStepUnroll], plane[kStepUnroll], row[kStepUnroll];  // page -1: nothing to store
 #pragma unroll
         for (int u = 0; u < kStepUnroll; ++u) {
-            const unsigned i = base + u * kCopyThreads + tid, r = i / LPR;
+            const unsigned i = base + u * kStepThreads + tid, r = i / LPR;
             plane[u] = (int)a.by_n.div(r);
             const int t = (int)(r - (unsigned)plane[u] * (unsigned)a.N);
-            raw[u] = make_uint4(0, 0, 0, 0);
+            raw[u].zero();
             page[u] = -1;
             row[u] = 0;
             if (i >= total || t >= n) continue;
@@ -145,7 +207,7 @@ __global__ void __launch_bounds__(kCopyThreads) append_step_kernel(const AppendA
                 head = reps[plane[u]];
                 if (head < 0 || head >= a.H) continue;  // unused cluster slot
             }
-            raw[u] = ld_stream16((plane[u] < a.k ? k_new : v_new) + ((size_t)head * a.N + t) * D + (int)(i % LPR) * EPV);
+            raw[u].load((plane[u] < a.k ? k_new : v_new) + ((size_t)head * a.N + t) * D + (int)(i % LPR) * EPV, a.wide);
             page[u] = known ? pg : -1;
         }
 #pragma unroll
@@ -161,16 +223,16 @@ __global__ void __launch_bounds__(kCopyThreads) append_step_kernel(const AppendA
 
 // A prompt's tokens: grid (runs of tokens, planes, B).
 template <typename TS, int D, bool FP8>
-__global__ void __launch_bounds__(kCopyThreads) append_rows_kernel(const AppendArgs a) {
-    constexpr int LPR = D * (int)sizeof(TS) / 16, EPV = 16 / (int)sizeof(TS), ROWS = kCopyThreads / LPR;
+__global__ void __launch_bounds__(kRowThreads) append_rows_kernel(const AppendArgs a) {
+    constexpr int LPR = D * (int)sizeof(TS) / Dense<FP8>::BYTES, EPV = Dense<FP8>::BYTES / (int)sizeof(TS), ROWS = kRowThreads / LPR;
     const int plane = blockIdx.y, b = blockIdx.z, x = threadIdx.x % LPR;
-    const int t0 = blockIdx.x * (ROWS * kAppendUnroll) + threadIdx.x / LPR;
+    const int t0 = blockIdx.x * (ROWS * kRowUnroll) + threadIdx.x / LPR;
     int pos0, n;
     if (!tokens_fit(a, b, &pos0, &n)) {
         if (threadIdx.x == 0 && blockIdx.x == 0 && plane == 0) flag_status(a.hdr, CHAI_ERR_CACHE_FULL, b);
         return;
     }
-    if ((int)(blockIdx.x * (ROWS * kAppendUnroll)) >= n) return;
+    if ((int)(blockIdx.x * (ROWS * kRowUnroll)) >= n) return;
     const bool key = plane < a.k;
     int head = plane - a.k;
     const int pl = key ? plane : head;
@@ -180,24 +242,24 @@ __global__ void __launch_bounds__(kCopyThreads) append_rows_kernel(const AppendA
     }
     const int32_t* table = a.pool.block_table + (size_t)b * a.pool.max_pages;
     const TS* src = static_cast<const TS*>(key ? a.k_new : a.v_new) + (((size_t)b * a.H + head) * a.N + t0) * D + x * EPV;
-    uint4 raw[kAppendUnroll];
-    int page[kAppendUnroll], row[kAppendUnroll];  // page -1: nothing to store
+    Dense<FP8> raw[kRowUnroll];
+    int page[kRowUnroll], row[kRowUnroll];  // page -1: nothing to store
     bool bad = false;
 #pragma unroll
-    for (int u = 0; u < kAppendUnroll; ++u) {
+    for (int u = 0; u < kRowUnroll; ++u) {
         const int t = t0 + u * ROWS;
-        raw[u] = make_uint4(0, 0, 0, 0);
+        raw[u].zero();
         page[u] = -1;
         row[u] = 0;
         if (t < n) {
-            raw[u] = ld_stream16(src + (size_t)u * ROWS * D);
+            raw[u].load(src + (size_t)u * ROWS * D, a.wide);
             const unsigned pos = (unsigned)(pos0 + t), pi = a.pool.by_page.div(pos);
             row[u] = (int)(pos - pi * (unsigned)a.pool.page_size);
             page[u] = table[pi];
         }
     }
 #pragma unroll
-    for (int u = 0; u < kAppendUnroll; ++u) {
+    for (int u = 0; u < kRowUnroll; ++u) {
         if (page[u] < 0 || page[u] >= a.pool.n_pages) {
             bad |= t0 + u * ROWS < n;
             page[u] = -1;
@@ -224,13 +286,13 @@ __global__ void __launch_bounds__(128) advance_paged_kernel(const AppendArgs a) 
 
 template <typename TS, int D, bool FP8>
 int launch_append(const AppendArgs& a, int B, cudaStream_t s) {
-    constexpr int LPR = D * (int)sizeof(TS) / 16, TOKENS = kCopyThreads / LPR * kAppendUnroll;
+    constexpr int LPR = D * (int)sizeof(TS) / Dense<FP8>::BYTES, TOKENS = kRowThreads / LPR * kRowUnroll;
     // One block per request saves the launch that advances the lengths, as long as it has a few passes to make.
-    if ((size_t)(a.k + a.H) * a.N * LPR <= 4 * kCopyThreads * kStepUnroll) {
-        CHAI_LAUNCH_DEPENDENT("append_step_kernel launch", (append_step_kernel<TS, D, FP8>), dim3(1, B), dim3(kCopyThreads), 0, s, a);
+    if ((size_t)(a.k + a.H) * a.N * LPR <= 4 * kStepThreads * kStepUnroll) {
+        CHAI_LAUNCH_DEPENDENT("append_step_kernel launch", (append_step_kernel<TS, D, FP8>), dim3(1, B), dim3(kStepThreads), 0, s, a);
         return CHAI_OK;
     }
-    append_rows_kernel<TS, D, FP8><<<dim3((a.N + TOKENS - 1) / TOKENS, a.k + a.H, B), kCopyThreads, 0, s>>>(a);
+    append_rows_kernel<TS, D, FP8><<<dim3((a.N + TOKENS - 1) / TOKENS, a.k + a.H, B), kRowThreads, 0, s>>>(a);
     CHAI_LAUNCH_CHECK("append_rows_kernel launch");
     if (a.advance) CHAI_LAUNCH_DEPENDENT("advance_paged_kernel launch", advance_paged_kernel, dim3(B), dim3(128), 0, s, a);
     return CHAI_OK;
@@ -251,6 +313,7 @@ int append(const char* fn, bool fp8, AppendArgs a, int B, int n_pages, int page_
     CHAI_REQUIRE(a.N > 0, CHAI_ERR_INVALID_ARG, "%s: need N > 0", fn);
     CHAI_REQUIRE((long long)a.H * a.N < (1ll << 30), CHAI_ERR_UNSUPPORTED, "%s: H*N must be below 2^30", fn);
     a.by_n = FastDiv((unsigned)a.N);
+    a.wide = aligned32(a.k_new) && aligned32(a.v_new);
     CHAI_LOG_CALL("%s: B=%d H=%d k=%d N=%d D=%d dtype=%d page_size=%d", fn, B, a.H, a.k, a.N, D, dtype, page_size);
     if (a.hdr != nullptr)
         CHAI_LAUNCH_DEPENDENT("paged append: status reset", paged_reset_status_kernel, dim3(1), dim3(1), 0, s, a.hdr);
@@ -274,6 +337,7 @@ struct ReadArgs {
     PagePool pool;
     int H, k, T_out;
     int nk, nv;  // planes that are wanted
+    bool wide;   // the dense arrays start on 32-byte boundaries
 };
 
 template <typename TO>
@@ -296,32 +360,30 @@ __device__ __forceinline__ uint4 pack16<__nv_bfloat16>(const float* f) {
 
 // grid (runs of tokens, planes that are wanted, B).
 template <typename TO, int D, bool FP8>
-__global__ void __launch_bounds__(kCopyThreads) read_paged_kernel(const ReadArgs a) {
-    constexpr int LPR = D * (int)sizeof(TO) / 16, EPV = 16 / (int)sizeof(TO), ROWS = kCopyThreads / LPR;
-    constexpr int UNROLL = FP8 ? 2 * kReadUnroll : kReadUnroll;
+__global__ void __launch_bounds__(kRowThreads) read_paged_kernel(const ReadArgs a) {
+    constexpr int LPR = D * (int)sizeof(TO) / Dense<FP8>::BYTES, EPV = Dense<FP8>::BYTES / (int)sizeof(TO), ROWS = kRowThreads / LPR;
     const int plane = blockIdx.y, b = blockIdx.z, x = threadIdx.x % LPR;
-    const int t0 = blockIdx.x * (ROWS * UNROLL) + threadIdx.x / LPR;
+    const int t0 = blockIdx.x * (ROWS * kRowUnroll) + threadIdx.x / LPR;
     const int n = min(min(max(a.seq_lens[b], 0), a.pool.capacity), a.T_out);
-    if ((int)(blockIdx.x * (ROWS * UNROLL)) >= n) return;
+    if ((int)(blockIdx.x * (ROWS * kRowUnroll)) >= n) return;
     const bool key = plane < a.nk;
     const int pl = key ? plane : plane - a.nk;
     const int32_t* table = a.pool.block_table + (size_t)b * a.pool.max_pages;
-    using Raw = typename std::conditional<FP8, typename std::conditional<EPV == 8, uint2, unsigned>::type, uint4>::type;
-    Raw raw[UNROLL];
-    [[maybe_unused]] float scale[UNROLL];
-    int page[UNROLL], row[UNROLL];
+    using Raw = typename std::conditional<FP8, typename std::conditional<EPV == 16, uint4, uint2>::type, uint4>::type;
+    Raw raw[kRowUnroll];
+    [[maybe_unused]] float scale[kRowUnroll];
+    int page[kRowUnroll], row[kRowUnroll];
     bool bad = false;
 #pragma unroll
-    for (int u = 0; u < UNROLL; ++u) {
-        const int t = t0 + u * ROWS;
-        const unsigned pos = (unsigned)min(t, n - 1), pi = a.pool.by_page.div(pos);
+    for (int u = 0; u < kRowUnroll; ++u) {
+        const unsigned pos = (unsigned)min(t0 + u * ROWS, n - 1), pi = a.pool.by_page.div(pos);
         row[u] = (int)(pos - pi * (unsigned)a.pool.page_size);
         page[u] = table[pi];
     }
     const char* pages = static_cast<const char*>(key ? a.k_pages : a.v_pages);
     const size_t stride = key ? a.pool.k_page_stride : a.pool.v_page_stride;
 #pragma unroll
-    for (int u = 0; u < UNROLL; ++u) {
+    for (int u = 0; u < kRowUnroll; ++u) {
         raw[u] = Raw{};
         scale[u] = 0.f;
         if (page[u] < 0 || page[u] >= a.pool.n_pages) {
@@ -335,13 +397,12 @@ __global__ void __launch_bounds__(kCopyThreads) read_paged_kernel(const ReadArgs
     }
     TO* dst = static_cast<TO*>(key ? a.k_out : a.v_out) + (((size_t)b * (key ? a.nk : a.nv) + pl) * a.T_out + t0) * D + x * EPV;
 #pragma unroll
-    for (int u = 0; u < UNROLL; ++u) {
+    for (int u = 0; u < kRowUnroll; ++u) {
         if (t0 + u * ROWS >= n) break;
-        uint4 v;
+        Dense<FP8> v;
         if constexpr (FP8) {
-            unsigned w[2] = {0, 0};
-            if constexpr (EPV == 8) w[0] = raw[u].x, w[1] = raw[u].y;
-            else w[0] = raw[u];
+            unsigned w[4] = {raw[u].x, raw[u].y, 0, 0};
+            if constexpr (EPV == 16) w[2] = raw[u].z, w[3] = raw[u].w;
             float f[EPV];
 #pragma unroll
             for (int e = 0; e < EPV / 2; ++e) {
@@ -350,19 +411,20 @@ __global__ void __launch_bounds__(kCopyThreads) read_paged_kernel(const ReadArgs
                 f[2 * e] = p.x * scale[u];
                 f[2 * e + 1] = p.y * scale[u];
             }
-            v = pack16<TO>(f);
+            v.a = pack16<TO>(f);
+            v.b = pack16<TO>(f + EPV / 2);
         } else {
-            v = raw[u];
+            v.a = raw[u];
         }
-        __stcs(reinterpret_cast<uint4*>(dst + (size_t)u * ROWS * D), v);
+        v.store(dst + (size_t)u * ROWS * D, a.wide);
     }
     if (bad) flag_status(a.hdr, CHAI_ERR_BAD_PAGE, b);
 }
 
 template <typename TO, int D, bool FP8>
 int launch_read(const ReadArgs& a, int B, cudaStream_t s) {
-    constexpr int LPR = D * (int)sizeof(TO) / 16, TOKENS = kCopyThreads / LPR * (FP8 ? 2 * kReadUnroll : kReadUnroll);
-    read_paged_kernel<TO, D, FP8><<<dim3((a.T_out + TOKENS - 1) / TOKENS, a.nk + a.nv, B), kCopyThreads, 0, s>>>(a);
+    constexpr int TOKENS = kRowThreads / (D * (int)sizeof(TO) / Dense<FP8>::BYTES) * kRowUnroll;
+    read_paged_kernel<TO, D, FP8><<<dim3((a.T_out + TOKENS - 1) / TOKENS, a.nk + a.nv, B), kRowThreads, 0, s>>>(a);
     CHAI_LAUNCH_CHECK("read_paged_kernel launch");
     return CHAI_OK;
 }
@@ -381,6 +443,7 @@ int read_back(const char* fn, bool fp8, ReadArgs a, int B, int n_pages, int page
     if (rc != CHAI_OK) return rc;
     CHAI_REQUIRE(a.T_out > 0, CHAI_ERR_INVALID_ARG, "%s: need T_out > 0", fn);
     CHAI_REQUIRE((long long)a.H * a.T_out < (1ll << 30), CHAI_ERR_UNSUPPORTED, "%s: H*T_out must be below 2^30", fn);
+    a.wide = aligned32(a.k_out) && aligned32(a.v_out);
     a.nk = a.k_out != nullptr ? a.k : 0;
     a.nv = a.v_out != nullptr ? a.H : 0;
     CHAI_LOG_CALL("%s: B=%d H=%d k=%d T_out=%d D=%d dtype=%d page_size=%d", fn, B, a.H, a.k, a.T_out, D, dtype, page_size);

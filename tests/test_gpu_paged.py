@@ -429,6 +429,38 @@ def test_read_back(cache, io, D, page, guard):
     assert np.array_equal(v_out[4].double().cpu().numpy(), want) and not v_out[1].any()
 
 
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+def test_arrays_that_start_on_odd_16_byte_boundaries(io):
+    B, H, k, D, page, N = 2, 5, 3, 64, 8, 45
+    g = torch.Generator().manual_seed(61)
+    step = 16 // torch.empty((), dtype=TORCH[io]).element_size()
+    table, n_pages = tables([0, 0], page, 61, room=N)
+    _, reps = partition(B, H, k, 61)
+    reps_t, table_t = torch.from_numpy(reps).to(DEV), torch.from_numpy(table).to(DEV)
+
+    def odd(x):
+        flat = torch.zeros(x.numel() + step, dtype=x.dtype, device=DEV)
+        view = flat[step:].view(x.shape)
+        view.copy_(x)
+        assert view.data_ptr() % 32 == 16
+        return view
+
+    k_new, v_new = (torch.randn(B, H, N, D, generator=g).to(TORCH[io]).to(DEV) for _ in range(2))
+    results = []
+    for at in (lambda x: x, odd):
+        kp, vp = (torch.zeros(n_pages, p, page, D, device=DEV, dtype=torch.uint8) for p in (k, H))
+        ks, vs = (torch.zeros(n_pages, p, page, device=DEV) for p in (k, H))
+        for count in (N, 1):       # a prompt's rows and a decode step's
+            seq = torch.zeros(B, dtype=torch.int32, device=DEV)
+            chai.chai_append_kv_paged_fp8(at(k_new[:, :, :count].contiguous()), at(v_new[:, :, :count].contiguous()), kp, vp, ks,
+                                          vs, reps_t, table_t, seq)
+        seq.fill_(N)
+        k_out, v_out = (at(torch.zeros(B, p, N, D, device=DEV, dtype=TORCH[io])) for p in (k, H))
+        chai.chai_read_kv_paged_fp8(kp, vp, ks, vs, table_t, seq, k_out=k_out, v_out=v_out)
+        results.append((kp, vp, ks, vs, k_out.clone(), v_out.clone()))
+    assert all(torch.equal(x, y) for x, y in zip(*results))
+
+
 def test_writing_what_was_read_back_gives_the_same_numbers():
     B, H, k, D, page, T = 2, 6, 4, 128, 16, 200
     c = make("e4m3", "bf16", B, H, k, D, page, [T, T], seed=41)
