@@ -484,10 +484,8 @@ def _paged_call(fn, dev: int, *args) -> None:
         _check(rc)
 
 
-def _raw_stream(dev: int) -> int:
-    # (torch.cuda.current_stream builds a Stream object, which costs as much as a launch)
-    get = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-    return get(dev) if get is not None else torch.cuda.current_stream(dev).cuda_stream
+# (torch.cuda.current_stream builds a Stream object, which costs as much as a launch)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda dev: torch.cuda.current_stream(dev).cuda_stream)
 
 
 def _want(t, name, shape, dtype, dev) -> None:
@@ -508,25 +506,23 @@ def _pages(k_pages, v_pages, k_scales, v_scales, block_table, seq_lens):
     if k_pages.dim() != 4 or v_pages.dim() != 4:
         raise ValueError("k_pages must be [n_pages,k,page_size,D] and v_pages [n_pages,H,page_size,D]")
     n, k, ps, D = k_pages.shape
-    H = v_pages.shape[1]
-    if v_pages.shape != (n, H, ps, D):
+    n_v, H, ps_v, D_v = v_pages.shape
+    if n_v != n or ps_v != ps or D_v != D:
         raise ValueError("k_pages and v_pages must agree in pages, page size and head dimension")
     dev = k_pages.get_device()
     if dev < 0 or v_pages.get_device() != dev:
         raise ValueError("the pages must be CUDA tensors on one device")
-    k_stride, *k_inner = k_pages.stride()
-    v_stride, *v_inner = v_pages.stride()
-    inner = [ps * D, D, 1]
-    if k_inner != inner or v_inner != inner:
-        if n > 0 and not (k_pages[0].is_contiguous() and v_pages[0].is_contiguous()):   # (of one plane the stride is free)
-            raise ValueError("every page must be contiguous (pages may be any distance apart)")
-    if n > 1:
-        if k_stride < k * ps * D or v_stride < H * ps * D:
-            raise ValueError("pages must not overlap")
-    else:
+    if k_pages.is_contiguous() and v_pages.is_contiguous():
         k_stride = v_stride = 0
+    else:
+        if n > 0 and not (k_pages[0].is_contiguous() and v_pages[0].is_contiguous()):
+            raise ValueError("every page must be contiguous (pages may be any distance apart)")
+        k_stride, v_stride = (k_pages.stride(0), v_pages.stride(0)) if n > 1 else (0, 0)
+        if n > 1 and (k_stride < k * ps * D or v_stride < H * ps * D):
+            raise ValueError("pages must not overlap")
     if k_scales is None:
-        if k_pages.dtype not in _PAGED_IO or v_pages.dtype is not k_pages.dtype:
+        dtype = k_pages.dtype
+        if v_pages.dtype is not dtype or dtype not in _PAGED_IO:
             raise TypeError("k_pages and v_pages must both be float32 or both bfloat16")
     else:
         if k_pages.dtype not in _E4M3 or v_pages.dtype not in _E4M3:

@@ -46,11 +46,10 @@ struct Geom {
     static constexpr int CHUNK_ROWS = 512;
     // types of 2 and 4 bytes: lanes a row, rows a warp-wide load, such loads a tile
     static constexpr int LPR = ROW / 16, RPW = 32 / LPR, IT = TR / RPW;
-    // e4m3: on the tensor cores a quarter of the lanes reads rows of one quarter of the tile (RUN rows), STEPS times four
-    static constexpr int RUN = 8, STEPS = 2;
-    static_assert(!FP8 || TR == 4 * RUN, "");
-    // ... and a row's 16-byte pieces lie in its 128-byte line (two rows a line for D = 64) at a place that is the piece's
-    // number xor 2 * (row / RUN), for D = 128 also xor 4 * (row % 2): the lanes of a load then meet different banks
+    // e4m3: the tensor cores take 16 rows a step; in phase V a quarter of the lanes reads four rows of them.  A row's
+    // 16-byte pieces lie in its 128-byte line (two rows a line for D = 64) at a place that is the piece's number xor
+    // 2 * (row / 4 % 4), for D = 128 also xor 4 * (row % 2): the lanes of a load then meet different banks
+    static constexpr int STEPS = TR / 16;
     // how a lane holds a row of values: VPL neighbours from column col(lane) on, in the lanes that own(lane)
     static constexpr int VPL = FP8 ? D / 8 : 16 / (int)sizeof(T);
     __device__ static __forceinline__ bool own(int lane) { return FP8 ? (lane & 3) == 0 : lane < LPR; }
@@ -113,26 +112,10 @@ struct Chunk {
     int span_end;  // > 0: the request begins here and goes on; where on the line it ends
 };
 __device__ __forceinline__ int uniform(int x) { return __shfl_sync(0xffffffffu, x, 0); }  // the same in every lane, and known to be
-__device__ __forceinline__ Chunk uniform_copy(const Chunk& s) {
-    Chunk c;
-    c.b = uniform(s.b);
-    c.rows = uniform(s.rows);
-    c.stride = uniform(s.stride);
-    c.tiles = uniform(s.tiles);
-    c.heads = uniform(s.heads);
-    c.clusters = uniform(s.clusters);
-    c.run = uniform(s.run);
-    c.first = uniform(s.first);
-    c.last = uniform(s.last);
-    c.single = uniform(s.single);
-    c.slot = uniform(s.slot);
-    c.seg = uniform(s.seg);
-    c.span_end = uniform(s.span_end);
-    return c;
-}
-struct Rows {  // eight rows of a chunk: where they lie
-    size_t k, v;  // byte offsets of their row in plane 0 of the pages
-    int page, row;
+template <int GROUPS>
+struct Rows {  // where each eight rows of a chunk lie: byte offsets in plane 0 of the pages, page and row
+    size_t k[GROUPS], v[GROUPS];
+    int2 at[GROUPS];
 };
 template <typename G, int D>
 struct Smem {
@@ -148,7 +131,7 @@ struct Smem {
     float top[G::HEADS], sum[G::HEADS], keep[G::HEADS];  // per cluster: running maximum and sum, rescaling factor
     Segment<G::HEADS> seg[2];
     Chunk chunk[2];
-    Rows at[2][G::CHUNK_ROWS / kQuantum];
+    alignas(16) Rows<G::CHUNK_ROWS / kQuantum> rows[2];
     alignas(8) unsigned long long full[G::W][G::STAGES];
     int scan[2][G::W];
     int found_b, found_start;
@@ -189,6 +172,9 @@ __device__ __forceinline__ void copy_rows(uint32_t dst, const void* src, uint32_
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src),
                  "r"(bytes), "r"(bar)
                  : "memory");
+}
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
 // 16 bytes, of which `n` come from src and the others are zero
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src, int n) {
@@ -252,12 +238,12 @@ struct Walk {
     int phase, p, j, left;
     bool fresh;  // p has changed
     __device__ __forceinline__ void start(int ph, const Chunk& c, int warp) {
-        const int n = (ph == 0 ? c.clusters : c.heads) * c.tiles;
+        const int tiles = uniform(c.tiles), n = uniform(ph == 0 ? c.clusters : c.heads) * tiles;
         const int lo = n * warp / W;
         phase = ph;
         left = n * (warp + 1) / W - lo;
-        p = small_div(lo, c.tiles);
-        j = lo - p * c.tiles;
+        p = small_div(lo, tiles);
+        j = lo - p * tiles;
         fresh = true;
     }
     __device__ __forceinline__ void step(int tiles) {
@@ -443,17 +429,14 @@ __global__ void __launch_bounds__(Geom<T, TQ, D>::THREADS, 1) paged_decode_kerne
             seg_rows = min(G::CHUNK_ROWS, small_div(G::SCORES, max(seg_clusters, 1)) / G::TR * G::TR);
         }
         const int rows = min(seg_rows, seg_end - seg_t);
-        if (tid * kQuantum < reach) {
+        if (tid * kQuantum < ((reach + 31) & ~31)) {  // (behind the rows: page 0, an address that is never read)
             if (page < 0 || page >= a.pool.n_pages) {
                 sm.any_bad = 1;  // of the segment so far
                 page = 0;
             }
-            Rows r;
-            r.k = ((size_t)page * a.pool.k_page_stride + (size_t)row * D) * sizeof(T);
-            r.v = ((size_t)page * a.pool.v_page_stride + (size_t)row * D) * sizeof(T);
-            r.page = page;
-            r.row = row;
-            sm.at[par][tid] = r;
+            sm.rows[par].k[tid] = ((size_t)page * a.pool.k_page_stride + (size_t)row * D) * sizeof(T);
+            sm.rows[par].v[tid] = ((size_t)page * a.pool.v_page_stride + (size_t)row * D) * sizeof(T);
+            sm.rows[par].at[tid] = make_int2(page, row);
         }
         if (tid == 0) {
             Chunk& c = sm.chunk[par];
@@ -482,7 +465,7 @@ __global__ void __launch_bounds__(Geom<T, TQ, D>::THREADS, 1) paged_decode_kerne
     bool dead = false;                                                   // a wait ran out: no more copies, no more waits
     Walk<W> ahead;                                                       // the next tile to start, of chunk number ahead_no
     int ahead_no = 0, ahead_par = 1, ready_no = 0;                       // chunks up to ready_no are prepared
-    Chunk ahead_chunk = {};                                              // that chunk
+    int ahead_rows = 0, ahead_tiles = 1, ahead_run = 0;                  // of that chunk
     const char* ahead_plane = nullptr;                                   // the plane of the next tile, in page 0 ...
     [[maybe_unused]] const float* ahead_scales = nullptr;                // ... its rows' scales ...
     const char* ahead_query = nullptr;                                   // ... and, of keys, the query
@@ -490,10 +473,15 @@ __global__ void __launch_bounds__(Geom<T, TQ, D>::THREADS, 1) paged_decode_kerne
     ahead.phase = 1;
     const size_t plane_bytes = (size_t)ps * D * sizeof(T);
     const uint32_t slots = smem_addr(sm.slot[warp][0]), bars = smem_addr(&sm.full[warp][0]);
-    // e4m3: a lane's place in a warp-wide copy of 512 bytes, apart from the change by the row's quarter
-    const int copy_at = G::FP8 ? (D == 128 ? (lane >> 3) * 128 + 16 * ((lane & 7) ^ (4 * ((lane >> 3) & 1)))
-                                           : (lane >> 3) * 128 + 16 * (lane & 7))
-                               : 0;
+    // e4m3: a lane's place in a warp-wide copy of 512 bytes (see Geom), by row / 4 % 4 of the lane group's first row: four
+    // rows a copy for D = 128; eight for D = 64, where the lane's own row matters too
+    uint32_t copy_at[4] = {};
+    if constexpr (G::FP8) {
+        const int line = (lane >> 3) * 128;
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+            copy_at[q] = D == 128 ? line + 16 * ((lane & 7) ^ (4 * ((lane >> 3) & 1)) ^ (2 * q)) : line + 16 * ((lane & 7) ^ (2 * ((q + (lane >> 4)) & 3)));
+    }
 
     // The next tile to start, with its addresses worked out ahead of time: the shared-memory reads that they take pass
     // behind the arithmetic of the tile before.
@@ -506,45 +494,49 @@ __global__ void __launch_bounds__(Geom<T, TQ, D>::THREADS, 1) paged_decode_kerne
     auto stage = [&]() __attribute__((always_inline)) {
         while (ahead.left == 0) {
             if (ahead.phase == 0) {
-                ahead.start(1, ahead_chunk, warp);
+                ahead.start(1, sm.chunk[ahead_par], warp);
             } else {
                 if (ahead_no >= ready_no) return;
                 ++ahead_no;
                 ahead_par ^= 1;
-                ahead_chunk = uniform_copy(sm.chunk[ahead_par]);
-                ahead.start(0, ahead_chunk, warp);
+                const Chunk& c = sm.chunk[ahead_par];
+                ahead_rows = uniform(c.rows);
+                ahead_tiles = uniform(c.tiles);
+                ahead_run = uniform(c.run);
+                ahead.start(0, c, warp);
             }
         }
         const bool key = ahead.phase == 0;
         next_query = key && ahead.fresh;
         if (ahead.fresh) {
             ahead.fresh = false;
-            const auto& sg = sm.seg[ahead_chunk.seg];
+            const auto& sg = sm.seg[sm.chunk[ahead_par].seg];
             const int plane = key ? sg.id[(sg.first + ahead.p) % G::HEADS] : sg.head[ahead.p];
             ahead_plane = static_cast<const char*>(key ? a.k_pages : a.v_pages) + plane * plane_bytes;
             if constexpr (G::FP8) ahead_scales = (key ? a.k_scales : a.v_scales) + plane * (size_t)ps;
             if (key)
                 ahead_query = static_cast<const char*>(a.q) +
-                              ((size_t)ahead_chunk.b * a.H + sg.rep[(sg.first + ahead.p) % G::HEADS]) * G::QROW;
+                              ((size_t)sm.chunk[ahead_par].b * a.H + sg.rep[(sg.first + ahead.p) % G::HEADS]) * G::QROW;
         }
         const int row0 = ahead.j * G::TR;
-        next_rows = min(G::TR, ahead_chunk.rows - row0);
-        const Rows* at = &sm.at[ahead_par][row0 / kQuantum];
+        next_rows = min(G::TR, ahead_rows - row0);
+        const auto& rows = sm.rows[ahead_par];
+        const size_t* off = (key ? rows.k : rows.v) + row0 / kQuantum;
         if constexpr (!G::FP8) {
-            const Rows& r = at[min(lane * ahead_chunk.run, next_rows - 1) / kQuantum];
-            next_src[0] = ahead_plane + (key ? r.k : r.v);
-            next_run = ahead_chunk.run;
+            next_src[0] = ahead_plane + off[min(lane * ahead_run, next_rows - 1) / kQuantum];
+            next_run = ahead_run;
         } else {
-            // (rows that are not there: an address that is not read)
-#pragma unroll
-            for (int g = 0; g < GROUPS; ++g) {
-                const Rows& r = at[min(g * kQuantum, next_rows - 1) / kQuantum];
-                next_src[g] = ahead_plane + lane * 16 + (key ? r.k : r.v);
-            }
-            const Rows& r = at[min(lane * 4, next_rows - 1) / kQuantum];
-            next_scales = ahead_scales + (size_t)r.page * (size_t)((key ? a.k : a.H) * ps) + (r.row + (lane & 1) * 4);
+            static_assert(GROUPS == 4, "two loads");
+            const ulonglong2 x = reinterpret_cast<const ulonglong2*>(off)[0], y = reinterpret_cast<const ulonglong2*>(off)[1];
+            const char* mine = ahead_plane + lane * 16;
+            next_src[0] = mine + x.x;
+            next_src[1] = mine + x.y;
+            next_src[2] = mine + y.x;
+            next_src[3] = mine + y.y;
+            const int2 at = rows.at[row0 / kQuantum + (lane & 7) / 2];
+            next_scales = ahead_scales + (size_t)(unsigned)at.x * (unsigned)((key ? a.k : a.H) * ps) + (at.y + (lane & 1) * 4);
         }
-        ahead.step(ahead_chunk.tiles);
+        ahead.step(ahead_tiles);
         staged = true;
     };
     // Starts copies until the warp's slots are in flight or nothing is known to copy.
@@ -564,17 +556,29 @@ __global__ void __launch_bounds__(Geom<T, TQ, D>::THREADS, 1) paged_decode_kerne
                     if (r0 < next_rows) copy_rows(slot + r0 * G::ROW, next_src[0], min(next_run, next_rows - r0) * G::ROW, bar);
                     if (next_query && lane == 31) copy_rows(slot + G::QUERY, ahead_query, G::QROW, bar);
                 } else {
-                    // 16 bytes a lane, and as many of the scales; behind the last row the tile is filled with zeros
-                    const int left = next_rows - lane / (G::ROW / 16);
+                    // 16 bytes a lane, and as many of the scales.  Behind the last row the tile is filled with zeros, up to
+                    // the end of a step
+                    constexpr int UNITS = kQuantum * G::ROW / 512, EACH = 512 / G::ROW;  // warp-wide copies of eight rows, rows of one
+                    if (next_rows == G::TR) {
 #pragma unroll
-                    for (int g = 0; g < GROUPS; ++g) {
-                        const uint32_t dst = slot + g * (kQuantum * G::ROW) + (copy_at ^ (32 * (g * kQuantum / G::RUN)));
+                        for (int g = 0; g < GROUPS; ++g)
 #pragma unroll
-                        for (int u = 0; u < kQuantum * G::ROW / 512; ++u)
-                            copy16(dst + u * 512, next_src[g] + u * 512, left > g * kQuantum + u * (512 / G::ROW) ? 16 : 0);
+                            for (int u = 0; u < UNITS; ++u) copy16(slot + copy_at[(2 * g + u) & (D == 128 ? 3 : 2)] + (g * kQuantum + u * EACH) * G::ROW, next_src[g] + u * 512);
+                        if (lane < 8) copy16(slot + G::DATA + lane * 16, next_scales);
+                    } else {
+                        const int left = next_rows - lane / (G::ROW / 16);
+#pragma unroll 1
+                        for (int s = 0; s * 16 < next_rows; ++s) {
+#pragma unroll
+                            for (int g = 0; g < 2; ++g)
+#pragma unroll
+                                for (int u = 0; u < UNITS; ++u)
+                                    copy16(slot + copy_at[(2 * g + u) & (D == 128 ? 3 : 2)] + (s * 16 + g * kQuantum + u * EACH) * G::ROW,
+                                           (s == 0 ? next_src[g] : next_src[g + 2]) + u * 512, left > s * 16 + g * kQuantum + u * EACH ? 16 : 0);
+                        }
+                        if (lane < 8) copy16(slot + G::DATA + lane * 16, next_scales, min(max(next_rows - lane * 4, 0), 4) * 4);
                     }
-                    if (lane < G::TR / 4) copy16(slot + G::DATA + lane * 16, next_scales, min(max(next_rows - lane * 4, 0), 4) * 4);
-                    if (next_query && lane * 16 < G::QROW) copy16(slot + G::QUERY + lane * 16, ahead_query + lane * 16, 16);
+                    if (next_query && lane * 16 < G::QROW) copy16(slot + G::QUERY + lane * 16, ahead_query + lane * 16);
                     asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
                 }
                 in_slot = in_slot + 1 == G::STAGES ? 0 : in_slot + 1;
@@ -618,9 +622,9 @@ __global__ void __launch_bounds__(Geom<T, TQ, D>::THREADS, 1) paged_decode_kerne
     while (more) {
         ++no;
         par ^= 1;
-        const Chunk c = uniform_copy(sm.chunk[par]);
+        const Chunk& c = sm.chunk[par];
         const auto& sg = sm.seg[c.seg];
-        const int first_place = uniform(sg.first);
+        const int first_place = uniform(sg.first), chunk_rows = uniform(c.rows), chunk_tiles = uniform(c.tiles), stride = uniform(c.stride);
 
         // K: scores of the warp's tiles, in powers of two
         {
@@ -632,7 +636,7 @@ __global__ void __launch_bounds__(Geom<T, TQ, D>::THREADS, 1) paged_decode_kerne
             [[maybe_unused]] uint64_t qf[QN / 2 + 1];
             [[maybe_unused]] uint32_t qb[G::FP8 ? D / 8 : 1];  // e4m3: fp16 fragments, column 0 the leading and column 1 the trailing half
 #pragma unroll 1
-            for (;; w.step(c.tiles)) {
+            for (;; w.step(chunk_tiles)) {
                 fill();
                 if (w.left == 0) break;
                 const int row0 = w.j * G::TR;
@@ -672,7 +676,7 @@ __global__ void __launch_bounds__(Geom<T, TQ, D>::THREADS, 1) paged_decode_kerne
                         }
                     }
                 }
-                float* score = sm.score + w.p * c.stride + row0;
+                float* score = sm.score + w.p * stride + row0;
                 if constexpr (!G::FP8) {
                     // lanes of a group hold 16 bytes each of rows group * IT + i; a butterfly turns 16 partial sums a
                     // lane into whole sums, halving the rows a lane answers for at every step
@@ -719,14 +723,15 @@ __global__ void __launch_bounds__(Geom<T, TQ, D>::THREADS, 1) paged_decode_kerne
                     const int g = lane >> 2, t = lane & 3;
                     const float* scales = reinterpret_cast<const float*>(tile + G::DATA) + g;
                     // rows 16 m + g and 16 m + g + 8, pieces t + 4 j (see Geom; the lane's share taken out)
-                    const int lane_at = D == 128 ? g * 128 + 16 * (t + 4 * (g & 1)) : (g >> 1) * 128 + 16 * ((g & 1) * 4 + t);
+                    const int lane_at = (D == 128 ? g * 128 + 16 * (t + 4 * (g & 1)) : (g >> 1) * 128 + 16 * ((g & 1) * 4 + t)) ^ (32 * (g >> 2));
 #pragma unroll
-                    for (int m = 0; m < G::TR / 16; ++m) {
+                    for (int m = 0; m < G::STEPS; ++m) {
+                        if (16 * m >= chunk_rows - row0) break;
                         float acc[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                         for (int j = 0; j < D / 64; ++j) {
-                            const uint4 x = lds16(tile + 16 * m * G::ROW + (lane_at ^ (64 * j) ^ (32 * (16 * m / G::RUN))));
-                            const uint4 y = lds16(tile + (16 * m + 8) * G::ROW + (lane_at ^ (64 * j) ^ (32 * ((16 * m + 8) / G::RUN))));
+                            const uint4 x = lds16(tile + 16 * m * G::ROW + (lane_at ^ (64 * j)));
+                            const uint4 y = lds16(tile + (16 * m + 8) * G::ROW + (lane_at ^ (64 * j) ^ 64));
                             const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
                             for (int i = 0; i < 4; ++i) {
@@ -752,22 +757,22 @@ __global__ void __launch_bounds__(Geom<T, TQ, D>::THREADS, 1) paged_decode_kerne
         // S: running maximum and sum of every cluster, probabilities relative to the new maximum
 #pragma unroll 1
         for (int cl = warp; cl < c.clusters; cl += W) {
-            float* score = sm.score + cl * c.stride;
+            float* score = sm.score + cl * stride;
             float top = -INFINITY, old = c.first ? -INFINITY : sm.top[cl], sum = 0.f;
 #pragma unroll 4
-            for (int r = lane; r < c.rows; r += 32) top = fmaxf(top, score[r]);
+            for (int r = lane; r < chunk_rows; r += 32) top = fmaxf(top, score[r]);
 #pragma unroll
             for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
             top = fmaxf(top, old);
             const float ref = top == -INFINITY ? 0.f : top;  // scores of -inf leave their rows out
 #pragma unroll 4
-            for (int r = lane; r < c.rows; r += 32) {
+            for (int r = lane; r < chunk_rows; r += 32) {
                 const float p = exp2_approx(score[r] - ref);
                 score[r] = G::FP8 ? p * kProbScale : p;
                 sum += p;
             }
-            const int r0 = c.rows + lane;
-            if (r0 < c.stride) score[r0] = 0.f;  // (a tile has 32 rows at most)
+            const int r0 = chunk_rows + lane;
+            if (r0 < stride) score[r0] = 0.f;  // (a tile has 32 rows at most)
 #pragma unroll
             for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
             if (lane == 0) {
@@ -832,11 +837,11 @@ __global__ void __launch_bounds__(Geom<T, TQ, D>::THREADS, 1) paged_decode_kerne
                 fill();
                 if (w.left == 0) break;
                 const int row0 = w.j * G::TR;
-                const float* prob = sm.score + (sg.cluster[w.p] - first_place) * c.stride + row0;
+                const float* prob = sm.score + (sg.cluster[w.p] - first_place) * stride + row0;
                 const unsigned char* tile = take();
                 if (tile == nullptr) break;
                 if constexpr (!G::FP8) {
-                    const int first = (lane / G::LPR) * G::IT, rows = c.rows - row0;
+                    const int first = (lane / G::LPR) * G::IT, rows = chunk_rows - row0;
                     if (rows < G::TR) {  // rows behind the last hold anything: zeros instead
 #pragma unroll 1
                         for (int i = rows * G::LPR + lane; i < G::TR * G::LPR; i += 32)
@@ -869,18 +874,19 @@ __global__ void __launch_bounds__(Geom<T, TQ, D>::THREADS, 1) paged_decode_kerne
                         acc[2 * e + 1] = x.y;
                     }
                 } else {
-                    // 16 columns are the rows of A, 16 cache rows a step (four of each run); B holds the probabilities
+                    // 16 columns are the rows of A, 16 cache rows a step; B holds the probabilities
                     // times the rows' scales, as two fp16 numbers each, the leading and the trailing half.  They are good
                     // to 2^-25 then: with probabilities kept times 2^14 and the largest scale of a head's first rows
                     // between 2^-16 and 2 that is at most 2^-22 of the largest product.  Other scales, and larger ones
                     // later, are brought there by a power of two.
                     const int g = lane >> 2, t = lane & 3;
-                    const float4* scales = reinterpret_cast<const float4*>(tile + G::DATA + 4 * G::RUN * t);
+                    const float4* scales = reinterpret_cast<const float4*>(tile + G::DATA + 16 * t);
+                    const bool both = chunk_rows - row0 > 16;  // the tile has rows for both steps
                     float4 vs[G::STEPS];
                     float top = 0.f;
 #pragma unroll
                     for (int s = 0; s < G::STEPS; ++s) {
-                        vs[s] = scales[s];
+                        vs[s] = s == 0 || both ? scales[4 * s] : make_float4(0.f, 0.f, 0.f, 0.f);
                         top = fmaxf(top, fmaxf(fmaxf(fabsf(vs[s].x), fabsf(vs[s].y)), fmaxf(fabsf(vs[s].z), fabsf(vs[s].w))));
                     }
                     if (begins) {
@@ -905,10 +911,11 @@ __global__ void __launch_bounds__(Geom<T, TQ, D>::THREADS, 1) paged_decode_kerne
                         for (int s = 0; s < G::STEPS; ++s) vs[s] = make_float4(vs[s].x * factor, vs[s].y * factor, vs[s].z * factor, vs[s].w * factor);
                     }
                     constexpr int WORDS = D / 32;  // 32-bit words a lane holds of a row
-                    const int lane_at = G::RUN * t * G::ROW + (D == 128 ? 16 * (g ^ (2 * t)) : (16 * ((g >> 1) ^ (2 * t)) + 8 * (g & 1)));
+                    const int lane_at = 4 * t * G::ROW + (D == 128 ? 16 * (g ^ (2 * t)) : (16 * ((g >> 1) ^ (2 * t)) + 8 * (g & 1)));
 #pragma unroll
                     for (int s = 0; s < G::STEPS; ++s) {
-                        const float4 pr = *reinterpret_cast<const float4*>(prob + G::RUN * t + 4 * s);
+                        if (s == 1 && !both) break;
+                        const float4 pr = *reinterpret_cast<const float4*>(prob + 16 * s + 4 * t);
                         const float x0 = pr.x * vs[s].x, x1 = pr.y * vs[s].y, x2 = pr.z * vs[s].z, x3 = pr.w * vs[s].w;
                         const uint32_t h0 = half_pair(x0, x1), h1 = half_pair(x2, x3);
                         const float2 y0 = half_floats(h0), y1 = half_floats(h1);
@@ -917,8 +924,8 @@ __global__ void __launch_bounds__(Geom<T, TQ, D>::THREADS, 1) paged_decode_kerne
                         uint32_t v[4][WORDS];
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
-                            // row RUN * t + 4 s + i (see Geom; the lane's share taken out)
-                            const unsigned char* at = tile + (4 * s + i) / (D == 128 ? 1 : 2) * 128 + (lane_at ^ (64 * (i & 1)));
+                            // row 16 s + 4 t + i (see Geom; the lane's share taken out)
+                            const unsigned char* at = tile + 16 * s * G::ROW + i / (D == 128 ? 1 : 2) * 128 + (lane_at ^ (64 * (i & 1)));
                             if constexpr (WORDS == 4) {
                                 const uint4 x = lds16(at);
                                 v[i][0] = x.x; v[i][1] = x.y; v[i][2] = x.z; v[i][3] = x.w;
@@ -943,8 +950,8 @@ __global__ void __launch_bounds__(Geom<T, TQ, D>::THREADS, 1) paged_decode_kerne
                 }
                 release();
                 const int p = w.p;
-                const bool ends = w.j + 1 == c.tiles;
-                w.step(c.tiles);
+                const bool ends = w.j + 1 == chunk_tiles;
+                w.step(chunk_tiles);
                 begins = ends;
                 if (!ends && w.left > 0) continue;
                 if constexpr (G::FP8) {
@@ -978,7 +985,7 @@ __global__ void __launch_bounds__(Geom<T, TQ, D>::THREADS, 1) paged_decode_kerne
         }
         __syncthreads();
         if (open >= 0) {
-            const int n = c.heads * c.tiles, stop = (open + 1) * c.tiles;
+            const int n = c.heads * chunk_tiles, stop = (open + 1) * chunk_tiles;
 #pragma unroll 1
             for (int w = warp + 1; w < W; ++w) {
                 const int lo = n * w / W;
