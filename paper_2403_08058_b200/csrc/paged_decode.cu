@@ -28,13 +28,13 @@ constexpr int kMaxCtas = 160;     // the workspace bound is stated for this many
 constexpr int kQuantum = 8;       // rows; page sizes are multiples of it
 constexpr int kJoinThreads = 128;
 constexpr int kJoinBlocks = 37;   // blocks per head, at most
-constexpr int kOverhead = 16;     // rows; see below (a multiple of 16)
+constexpr int kOverhead = 32;     // rows; see below (a multiple of 16)
 constexpr float kProbScale = 16384.f;  // e4m3: probabilities are kept times 2^14 (see phase V)
 
 template <typename T, typename TQ, int D>
 struct Geom {
     static constexpr bool FP8 = std::is_same<T, Fp8E4M3>::value;
-    static constexpr int W = std::is_same<T, __nv_bfloat16>::value ? 14 : 12, THREADS = W * 32;  // warps
+    static constexpr int W = 12, THREADS = W * 32;  // warps (more would have too few registers)
     static constexpr int ROW = D * (int)sizeof(T);
     static constexpr int TR = FP8 ? 32 : 4096 / ROW;    // rows of a tile
     static constexpr int STAGES = FP8 && D == 64 ? 6 : 3;  // slots of a warp
@@ -42,7 +42,7 @@ struct Geom {
     static constexpr int QUERY = DATA + (FP8 ? TR * 4 : 0);  // e4m3: the rows' scales lie behind them ...
     static constexpr int QROW = D * (int)sizeof(TQ), SLOT = QUERY + QROW;  // ... and the query of a new cluster's keys
     static constexpr int HEADS = 112;           // heads a CTA handles at most
-    static constexpr int SCORES = std::is_same<T, __nv_bfloat16>::value ? 4096 : 8192;  // scores of a chunk: clusters * rows
+    static constexpr int SCORES = 8192;  // scores of a chunk: clusters * rows
     static constexpr int CHUNK_ROWS = 512;
     // types of 2 and 4 bytes: lanes a row, rows a warp-wide load, such loads a tile
     static constexpr int LPR = ROW / 16, RPW = 32 / LPR, IT = TR / RPW;
@@ -109,7 +109,6 @@ struct Chunk {
     int tiles, heads, clusters, run;
     int first, last, single, slot;  // first / last chunk of the segment; single: the segment is the whole request
     int seg;
-    int span_end;  // > 0: the request begins here and goes on; where on the line it ends
 };
 __device__ __forceinline__ int uniform(int x) { return __shfl_sync(0xffffffffu, x, 0); }  // the same in every lane, and known to be
 template <int GROUPS>
@@ -282,9 +281,11 @@ __global__ void __launch_bounds__(Geom<T, TQ, D>::THREADS, 1) paged_decode_kerne
     // -- the line of all rows, this CTA's piece [q_lo, q_hi) and the request it starts in.  A request counts
     // kOverhead rows more than it has, in front: what a CTA loses where one request ends and the next begins.
     auto length = [&](int b) { return min(max(a.seq_lens[b], 0), a.pool.capacity); };
-    const int per = (a.B + THREADS - 1) / THREADS;
-    const int b_lo = min(tid * per, a.B), b_hi = min(b_lo + per, a.B);
+    const bool few = a.B <= 32;  // every warp then looks at all requests by itself, a lane each: no barrier is needed
+    const int per = few ? 1 : (a.B + THREADS - 1) / THREADS;
+    const int b_lo = min((few ? lane : tid) * per, a.B), b_hi = min(b_lo + per, a.B);
     int mine8 = 0, mine16 = 0;  // in units of eight and of sixteen rows
+#pragma unroll 1
     for (int b = b_lo; b < b_hi; ++b) {
         const int n = length(b);
         mine8 += n > 0 ? (n + 7 + kOverhead) / 8 : 0;
@@ -296,15 +297,18 @@ __global__ void __launch_bounds__(Geom<T, TQ, D>::THREADS, 1) paged_decode_kerne
         const int x = __shfl_up_sync(0xffffffffu, upto8, o), y = __shfl_up_sync(0xffffffffu, upto16, o);
         if (lane >= o) upto8 += x, upto16 += y;
     }
-    if (lane == 31) sm.scan[0][warp] = upto8, sm.scan[1][warp] = upto16;
-    __syncthreads();
-    int total8 = 0, total16 = 0;
-#pragma unroll
-    for (int w = 0; w < W; ++w) {
-        const int x = sm.scan[0][w], y = sm.scan[1][w];
-        if (w < warp) upto8 += x, upto16 += y;
-        total8 += x;
-        total16 += y;
+    int total8 = __shfl_sync(0xffffffffu, upto8, 31), total16 = __shfl_sync(0xffffffffu, upto16, 31);
+    if (!few) {
+        if (lane == 31) sm.scan[0][warp] = upto8, sm.scan[1][warp] = upto16;
+        __syncthreads();
+        total8 = total16 = 0;
+#pragma unroll 1
+        for (int w = 0; w < W; ++w) {
+            const int x = sm.scan[0][w], y = sm.scan[1][w];
+            if (w < warp) upto8 += x, upto16 += y;
+            total8 += x;
+            total16 += y;
+        }
     }
     // Heads are dealt to several CTAs when a piece would be shorter than 32 rows, down to 4 heads a CTA.
     const int n_ctas = gridDim.x;
@@ -323,19 +327,32 @@ __global__ void __launch_bounds__(Geom<T, TQ, D>::THREADS, 1) paged_decode_kerne
     auto piece_start = [&](int i) { return i * each + small_div(i * rest, pieces); };  // (i and rest are at most kMaxCtas)
     const bool work = piece < pieces && total > 0;
     const int q_lo = work ? piece_start(piece) : 0, q_hi = work ? piece_start(piece + 1) : 0;
-    if (work && mine > 0 && q_lo >= upto - mine && q_lo < upto) {
-        int start = upto - mine, b = b_lo;
-        while (q_lo >= start + quanta(length(b))) start += quanta(length(b++));
-        sm.found_b = b;
-        sm.found_start = start;
+    int found_b = 0, found_start = 0;
+    {
+        const bool here = work && mine > 0 && q_lo >= upto - mine && q_lo < upto;
+        if (few) {
+            const unsigned who = __ballot_sync(0xffffffffu, here);
+            found_b = who ? __ffs(who) - 1 : 0;
+            found_start = __shfl_sync(0xffffffffu, upto - mine, found_b);
+        } else {
+            if (here) {
+                int start = upto - mine, b = b_lo;
+                while (q_lo >= start + quanta(length(b))) start += quanta(length(b++));
+                sm.found_b = b;
+                sm.found_start = start;
+            }
+            __syncthreads();
+            if (work) found_b = sm.found_b, found_start = sm.found_start;
+        }
     }
-    __syncthreads();
 
     // -- state of the division into segments and chunks, the same in every thread
-    int q_at = q_lo, b = work ? sm.found_b : 0, b_start = work ? sm.found_start : 0;
+    int q_at = q_lo, b = found_b, b_start = found_start;
     int seg_t = 0, seg_end = 0, seg_par = 1, seg_rows = 0, seg_heads = 0, seg_clusters = 0, seg_slot = 0, span_end = 0;
     bool seg_single = false, seg_first = false;
 
+    const bool by_request = a.n_desc == a.B;  // descriptions are kept per request, or (more requests than CTAs) per piece
+    bool opened_span = false;
     // Prepares the next chunk into buffer `par`; false if the piece is done.  Called by all threads together, which
     // meet at a barrier afterwards.
     auto prepare = [&](int par) -> bool {
@@ -372,6 +389,15 @@ __global__ void __launch_bounds__(Geom<T, TQ, D>::THREADS, 1) paged_decode_kerne
             seg_first = true;
             auto& sg = sm.seg[seg_par];
             const bool opens = from_start && group == 0;  // this CTA answers for the request's unknown heads
+            if (from_start && !seg_single) opened_span = true;
+            if (tid == THREADS - 1 && opens && (by_request || !seg_single)) {
+                int end = piece;  // the piece that the request ends in
+                if (!seg_single) {
+                    end = max(end, (span_end - 1) / (each + 1));  // (a piece has each or each + 1)
+                    while (piece_start(end + 1) < span_end) ++end;
+                }
+                a.ws.desc[by_request ? b : piece] = make_int4(seg_single ? -1 : b, seg_slot, end - piece + 1, 0);
+            }
             // heads ordered by cluster; unknown ones get zeros and are left out
             const int32_t* mem = a.membership + (size_t)b * a.H;
             const int32_t* reps = a.reps + (size_t)b * a.k;
@@ -453,7 +479,6 @@ __global__ void __launch_bounds__(Geom<T, TQ, D>::THREADS, 1) paged_decode_kerne
             c.single = seg_single;
             c.slot = seg_slot;
             c.seg = seg_par;
-            c.span_end = span_end;
         }
         seg_first = false;
         seg_t += rows;
@@ -612,12 +637,22 @@ __global__ void __launch_bounds__(Geom<T, TQ, D>::THREADS, 1) paged_decode_kerne
     };
 
     // -- chunk by chunk
-    const bool by_request = a.n_desc == a.B;  // descriptions are kept per request, or (more requests than CTAs) per piece
-    bool opened_span = false;
     int no = 0, par = 1;
     bool more = prepare(0);
     __syncthreads();
     if (more) ready_no = 1;
+
+    // -- requests without rows get zeros
+    if (!few || __any_sync(0xffffffffu, lane < a.B && mine == 0)) {
+#pragma unroll 1
+        for (int z = blockIdx.x; z < a.B; z += n_ctas) {
+            if (length(z) > 0) continue;
+            if (by_request && tid == 0) a.ws.desc[z] = make_int4(-1, 0, 0, 0);
+            uint4* o = reinterpret_cast<uint4*>(static_cast<TQ*>(a.out) + (size_t)z * a.H * D);
+#pragma unroll 1
+            for (int i = tid; i < a.H * D * (int)sizeof(TQ) / 16; i += THREADS) o[i] = make_uint4(0, 0, 0, 0);
+        }
+    }
 #pragma unroll 1
     while (more) {
         ++no;
@@ -997,17 +1032,8 @@ __global__ void __launch_bounds__(Geom<T, TQ, D>::THREADS, 1) paged_decode_kerne
             }
             emit(open);
         }
-        if (c.span_end > 0) opened_span = true;
         if (c.last && tid == 0) {
             if (!c.single && group == 0) a.ws.slot_bad[c.slot] = bad_so_far;
-            if (group == 0 && (c.span_end > 0 || (by_request && c.single))) {
-                int end = piece;  // the piece that the request ends in
-                if (c.span_end > 0) {
-                    end = max(end, (c.span_end - 1) / (each + 1));  // (a piece has each or each + 1)
-                    while (piece_start(end + 1) < c.span_end) ++end;
-                }
-                a.ws.desc[by_request ? c.b : piece] = make_int4(c.single ? -1 : c.b, c.slot, end - piece + 1, 0);
-            }
             if (bad_so_far && atomicCAS(&sm.err, CHAI_OK, CHAI_ERR_BAD_PAGE) == CHAI_OK) sm.err_b = c.b;
         }
     }
@@ -1020,15 +1046,6 @@ __global__ void __launch_bounds__(Geom<T, TQ, D>::THREADS, 1) paged_decode_kerne
             }
         }
 
-    // -- the rest: requests without rows get zeros, pieces that open no request that goes on say so
-#pragma unroll 1
-    for (int z = blockIdx.x; z < a.B; z += n_ctas) {
-        if (length(z) > 0) continue;
-        if (by_request && tid == 0) a.ws.desc[z] = make_int4(-1, 0, 0, 0);
-        uint4* o = reinterpret_cast<uint4*>(static_cast<TQ*>(a.out) + (size_t)z * a.H * D);
-#pragma unroll 1
-        for (int i = tid; i < a.H * D * (int)sizeof(TQ) / 16; i += THREADS) o[i] = make_uint4(0, 0, 0, 0);
-    }
     if (!by_request && tid == 0) {
         if ((int)blockIdx.x >= pieces && (int)blockIdx.x < a.n_desc) a.ws.desc[blockIdx.x] = make_int4(-1, 0, 0, 0);
         if (piece < pieces && group == 0 && !opened_span) a.ws.desc[piece] = make_int4(-1, 0, 0, 0);
