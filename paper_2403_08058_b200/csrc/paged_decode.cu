@@ -96,6 +96,9 @@ struct DecodeArgs {
 
 // ---- shared memory ----------------------------------------------------------------------------------------------
 
+// n / d for 0 <= n < 2^20, 0 < d: (n + 1/2) / d is 1/(2 d) or more away from an integer, its rounding at most n / d * 2^-22.
+__device__ __forceinline__ int small_div(int n, int d) { return (int)__fdividef((float)n + 0.5f, (float)d); }
+
 template <int HEADS>
 struct Segment {  // the rows of one request in this CTA's piece
     unsigned short head[HEADS];     // heads, ordered by cluster
@@ -111,6 +114,21 @@ struct Chunk {
     int seg;
 };
 __device__ __forceinline__ int uniform(int x) { return __shfl_sync(0xffffffffu, x, 0); }  // the same in every lane, and known to be
+struct Plan {  // how the line of all rows is divided; kept in shared memory, for registers are short
+    int pieces, each, rest;  // a piece has each or each + 1 units
+    int piece, group, groups;
+    int unit_log, overhead;  // rows of a unit (as a power of two), units that a request counts in front of its rows
+    int q_hi;                // where this CTA's piece ends
+    // place where piece i begins (i * total / pieces without 64-bit division; i and rest are at most kMaxCtas)
+    __device__ __forceinline__ int start(int i) const { return i * each + small_div(i * rest, pieces); }
+    __device__ __forceinline__ int quanta(int n) const { return n > 0 ? (n + (1 << unit_log) - 1 + kOverhead) >> unit_log : 0; }
+};
+struct Division {  // how far the CTA has divided its piece
+    int q_at, b, b_start;  // place on the line, request, its place
+    int t, end, rows;      // of the current segment: next row, last row, rows of a chunk
+    int par, heads, clusters, slot, span_end;
+    int single, first, opened_span;
+};
 template <int GROUPS>
 struct Rows {  // where each eight rows of a chunk lie: byte offsets in plane 0 of the pages, page and row
     size_t k[GROUPS], v[GROUPS];
@@ -133,6 +151,8 @@ struct Smem {
     alignas(16) Rows<G::CHUNK_ROWS / kQuantum> rows[2];
     alignas(8) unsigned long long full[G::W][G::STAGES];
     int scan[2][G::W];
+    Plan plan;
+    Division division[2];
     int found_b, found_start;
     int err, err_b, any_bad;
 };
@@ -219,8 +239,6 @@ __device__ __forceinline__ void mma16816(float* c, uint32_t a0, uint32_t a1, uin
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-// n / d for 0 <= n < 2^20, 0 < d: (n + 1/2) / d is 1/(2 d) or more away from an integer, its rounding at most n / d * 2^-22.
-__device__ __forceinline__ int small_div(int n, int d) { return (int)__fdividef((float)n + 0.5f, (float)d); }
 // A power of two f with |x| f in [1, 2) and its inverse; 1 where x is 0, tiny, infinite or NaN.
 __device__ __forceinline__ void normaliser(float x, float* f, float* inv) {
     const unsigned e = (__float_as_uint(x) >> 23) & 0xffu;
@@ -320,13 +338,18 @@ __global__ void __launch_bounds__(Geom<T, TQ, D>::THREADS, 1) paged_decode_kerne
     const bool coarse = total16 >= 12 * most_pieces;
     const int unit_log = coarse ? 4 : 3, total = coarse ? total16 : total8, overhead = kOverhead >> unit_log;
     const int upto = coarse ? upto16 : upto8, mine = coarse ? mine16 : mine8;
-    auto quanta = [&](int n) { return n > 0 ? (n + (1 << unit_log) - 1 + kOverhead) >> unit_log : 0; };
-    const int pieces = max(1, min(most_pieces, total));
-    const int piece = base_groups == 1 ? (int)blockIdx.x >> group_log : small_div(blockIdx.x, groups), group = blockIdx.x - piece * groups;
-    const int each = total / pieces, rest = total - each * pieces;  // (piece * total / pieces without 64-bit division)
-    auto piece_start = [&](int i) { return i * each + small_div(i * rest, pieces); };  // (i and rest are at most kMaxCtas)
-    const bool work = piece < pieces && total > 0;
-    const int q_lo = work ? piece_start(piece) : 0, q_hi = work ? piece_start(piece + 1) : 0;
+    Plan plan;
+    plan.unit_log = unit_log;
+    plan.overhead = overhead;
+    plan.pieces = max(1, min(most_pieces, total));
+    plan.groups = groups;
+    plan.piece = base_groups == 1 ? (int)blockIdx.x >> group_log : small_div(blockIdx.x, groups);
+    plan.group = blockIdx.x - plan.piece * groups;
+    plan.each = total / plan.pieces;
+    plan.rest = total - plan.each * plan.pieces;
+    const bool work = plan.piece < plan.pieces && total > 0;
+    const int q_lo = work ? plan.start(plan.piece) : 0;
+    plan.q_hi = work ? plan.start(plan.piece + 1) : 0;
     int found_b = 0, found_start = 0;
     {
         const bool here = work && mine > 0 && q_lo >= upto - mine && q_lo < upto;
@@ -337,7 +360,7 @@ __global__ void __launch_bounds__(Geom<T, TQ, D>::THREADS, 1) paged_decode_kerne
         } else {
             if (here) {
                 int start = upto - mine, b = b_lo;
-                while (q_lo >= start + quanta(length(b))) start += quanta(length(b++));
+                while (q_lo >= start + plan.quanta(length(b))) start += plan.quanta(length(b++));
                 sm.found_b = b;
                 sm.found_start = start;
             }
@@ -345,38 +368,47 @@ __global__ void __launch_bounds__(Geom<T, TQ, D>::THREADS, 1) paged_decode_kerne
             if (work) found_b = sm.found_b, found_start = sm.found_start;
         }
     }
-
-    // -- state of the division into segments and chunks, the same in every thread
-    int q_at = q_lo, b = found_b, b_start = found_start;
-    int seg_t = 0, seg_end = 0, seg_par = 1, seg_rows = 0, seg_heads = 0, seg_clusters = 0, seg_slot = 0, span_end = 0;
-    bool seg_single = false, seg_first = false;
-
     const bool by_request = a.n_desc == a.B;  // descriptions are kept per request, or (more requests than CTAs) per piece
-    bool opened_span = false;
+    const bool some_empty = !few || __any_sync(0xffffffffu, lane < a.B && mine == 0);
+    if (tid == 0) {
+        sm.plan = plan;
+        Division& d = sm.division[1];
+        d.q_at = q_lo;
+        d.b = found_b;
+        d.b_start = found_start;
+        d.t = d.end = 0;
+        d.par = 1;
+        d.opened_span = 0;
+    }
+    __syncthreads();
+
     // Prepares the next chunk into buffer `par`; false if the piece is done.  Called by all threads together, which
     // meet at a barrier afterwards.
     auto prepare = [&](int par) -> bool {
+        const Plan& plan = sm.plan;
+        Division d = sm.division[par ^ 1];
         bool fresh = false, from_start = false;
-        while (seg_t >= seg_end) {  // the next request that has rows here
-            if (q_at >= q_hi) return false;
-            int n = length(b);
-            while (q_at >= b_start + quanta(n)) {
-                b_start += quanta(n);
-                n = length(++b);
+        while (d.t >= d.end) {  // the next request that has rows here
+            if (d.q_at >= plan.q_hi) return false;
+            int n = length(d.b);
+            while (d.q_at >= d.b_start + plan.quanta(n)) {
+                d.b_start += plan.quanta(n);
+                n = length(++d.b);
             }
-            const int stop = b_start + quanta(n), rows_at = b_start + overhead, q_end = min(q_hi, stop);
-            from_start = q_at <= rows_at;
-            seg_t = max(q_at - rows_at, 0) << unit_log;
-            seg_end = q_end > rows_at ? min(n, (q_end - rows_at) << unit_log) : seg_t;
-            seg_single = from_start && q_end == stop;
-            span_end = from_start && !seg_single ? stop : 0;
-            seg_slot = piece + b;
-            q_at = q_end;
+            const int stop = d.b_start + plan.quanta(n), rows_at = d.b_start + plan.overhead, q_end = min(plan.q_hi, stop);
+            from_start = d.q_at <= rows_at;
+            d.t = max(d.q_at - rows_at, 0) << plan.unit_log;
+            d.end = q_end > rows_at ? min(n, (q_end - rows_at) << plan.unit_log) : d.t;
+            d.single = from_start && q_end == stop;
+            d.span_end = from_start && !d.single ? stop : 0;
+            d.slot = plan.piece + d.b;
+            d.q_at = q_end;
             fresh = true;
         }
+        const int b = d.b, seg_t = d.t, seg_end = d.end, group = plan.group, groups = plan.groups;
         // pages of the rows that the chunk may have (how many it has follows from the number of clusters)
         const int32_t* table = a.pool.block_table + (size_t)b * a.pool.max_pages;
-        const int reach = min(seg_end - seg_t, fresh ? G::CHUNK_ROWS : seg_rows);
+        const int reach = min(seg_end - seg_t, fresh ? G::CHUNK_ROWS : d.rows);
         int page = 0, row = 0;
         static_assert(G::CHUNK_ROWS / kQuantum <= THREADS, "one thread looks up eight rows");
         if (tid * kQuantum < reach) {
@@ -385,18 +417,18 @@ __global__ void __launch_bounds__(Geom<T, TQ, D>::THREADS, 1) paged_decode_kerne
             row = (int)(pos - pi * (unsigned)ps);
         }
         if (fresh) {
-            seg_par ^= 1;
-            seg_first = true;
-            auto& sg = sm.seg[seg_par];
+            d.par ^= 1;
+            d.first = 1;
+            auto& sg = sm.seg[d.par];
             const bool opens = from_start && group == 0;  // this CTA answers for the request's unknown heads
-            if (from_start && !seg_single) opened_span = true;
-            if (tid == THREADS - 1 && opens && (by_request || !seg_single)) {
-                int end = piece;  // the piece that the request ends in
-                if (!seg_single) {
-                    end = max(end, (span_end - 1) / (each + 1));  // (a piece has each or each + 1)
-                    while (piece_start(end + 1) < span_end) ++end;
+            if (d.span_end > 0) d.opened_span = 1;
+            if (tid == THREADS - 1 && opens && (by_request || !d.single)) {
+                int end = plan.piece;  // the piece that the request ends in
+                if (!d.single) {
+                    end = max(end, (d.span_end - 1) / (plan.each + 1));
+                    while (plan.start(end + 1) < d.span_end) ++end;
                 }
-                a.ws.desc[by_request ? b : piece] = make_int4(seg_single ? -1 : b, seg_slot, end - piece + 1, 0);
+                a.ws.desc[by_request ? b : plan.piece] = make_int4(d.single ? -1 : b, d.slot, end - plan.piece + 1, 0);
             }
             // heads ordered by cluster; unknown ones get zeros and are left out
             const int32_t* mem = a.membership + (size_t)b * a.H;
@@ -424,7 +456,7 @@ __global__ void __launch_bounds__(Geom<T, TQ, D>::THREADS, 1) paged_decode_kerne
                 if (h < a.H && !ok && opens) {
                     atomicCAS(&sm.err, CHAI_OK, CHAI_ERR_BAD_MEMBERSHIP);
                     sm.err_b = b;
-                    if (!seg_single) a.ws.ml[(size_t)seg_slot * a.H + h] = make_float2(0.f, -1.f);
+                    if (!d.single) a.ws.ml[(size_t)d.slot * a.H + h] = make_float2(0.f, -1.f);
                     TQ* o = static_cast<TQ*>(a.out) + ((size_t)b * a.H + h) * D;
                     for (int d = 0; d < D; ++d) o[d] = from_float<TQ>(0.f);
                 }
@@ -450,11 +482,11 @@ __global__ void __launch_bounds__(Geom<T, TQ, D>::THREADS, 1) paged_decode_kerne
                 }
             }
             __syncthreads();
-            seg_heads = hi - lo;
-            seg_clusters = seg_heads > 0 ? sg.last - sg.first + 1 : 0;
-            seg_rows = min(G::CHUNK_ROWS, small_div(G::SCORES, max(seg_clusters, 1)) / G::TR * G::TR);
+            d.heads = hi - lo;
+            d.clusters = d.heads > 0 ? sg.last - sg.first + 1 : 0;
+            d.rows = min(G::CHUNK_ROWS, small_div(G::SCORES, max(d.clusters, 1)) / G::TR * G::TR);
         }
-        const int rows = min(seg_rows, seg_end - seg_t);
+        const int rows = min(d.rows, seg_end - seg_t);
         if (tid * kQuantum < ((reach + 31) & ~31)) {  // (behind the rows: page 0, an address that is never read)
             if (page < 0 || page >= a.pool.n_pages) {
                 sm.any_bad = 1;  // of the segment so far
@@ -470,18 +502,19 @@ __global__ void __launch_bounds__(Geom<T, TQ, D>::THREADS, 1) paged_decode_kerne
             c.rows = rows;
             c.stride = (rows + G::TR - 1) / G::TR * G::TR;
             c.tiles = (rows + G::TR - 1) / G::TR;
-            c.heads = seg_heads;
-            c.clusters = seg_clusters;
+            c.heads = d.heads;
+            c.clusters = d.clusters;
             const int align = ps | seg_t;
             c.run = min(align & -align, G::TR);
-            c.first = seg_first;
+            c.first = d.first;
             c.last = seg_t + rows >= seg_end;
-            c.single = seg_single;
-            c.slot = seg_slot;
-            c.seg = seg_par;
+            c.single = d.single;
+            c.slot = d.slot;
+            c.seg = d.par;
+            d.first = 0;
+            d.t += rows;
+            sm.division[par] = d;
         }
-        seg_first = false;
-        seg_t += rows;
         return true;
     };
 
@@ -643,7 +676,7 @@ __global__ void __launch_bounds__(Geom<T, TQ, D>::THREADS, 1) paged_decode_kerne
     if (more) ready_no = 1;
 
     // -- requests without rows get zeros
-    if (!few || __any_sync(0xffffffffu, lane < a.B && mine == 0)) {
+    if (some_empty) {
 #pragma unroll 1
         for (int z = blockIdx.x; z < a.B; z += n_ctas) {
             if (length(z) > 0) continue;
@@ -1033,7 +1066,7 @@ __global__ void __launch_bounds__(Geom<T, TQ, D>::THREADS, 1) paged_decode_kerne
             emit(open);
         }
         if (c.last && tid == 0) {
-            if (!c.single && group == 0) a.ws.slot_bad[c.slot] = bad_so_far;
+            if (!c.single && sm.plan.group == 0) a.ws.slot_bad[c.slot] = bad_so_far;
             if (bad_so_far && atomicCAS(&sm.err, CHAI_OK, CHAI_ERR_BAD_PAGE) == CHAI_OK) sm.err_b = c.b;
         }
     }
@@ -1046,9 +1079,10 @@ __global__ void __launch_bounds__(Geom<T, TQ, D>::THREADS, 1) paged_decode_kerne
             }
         }
 
-    if (!by_request && tid == 0) {
-        if ((int)blockIdx.x >= pieces && (int)blockIdx.x < a.n_desc) a.ws.desc[blockIdx.x] = make_int4(-1, 0, 0, 0);
-        if (piece < pieces && group == 0 && !opened_span) a.ws.desc[piece] = make_int4(-1, 0, 0, 0);
+    if (!by_request && tid == 0) {  // pieces that open no request that goes on say so
+        const Plan& plan = sm.plan;
+        if ((int)blockIdx.x >= plan.pieces && (int)blockIdx.x < a.n_desc) a.ws.desc[blockIdx.x] = make_int4(-1, 0, 0, 0);
+        if (plan.piece < plan.pieces && plan.group == 0 && !sm.division[par].opened_span) a.ws.desc[plan.piece] = make_int4(-1, 0, 0, 0);
     }
     __syncthreads();
     if (tid == 0) {
