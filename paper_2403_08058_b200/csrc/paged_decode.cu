@@ -360,7 +360,7 @@ __global__ void __launch_bounds__(Geom<T, TQ, D>::THREADS, 1) paged_decode_kerne
         } else {
             if (here) {
                 int start = upto - mine, b = b_lo;
-                while (q_lo >= start + plan.quanta(length(b))) start += plan.quanta(length(b++));
+                while (b + 1 < b_hi && q_lo >= start + plan.quanta(length(b))) start += plan.quanta(length(b++));
                 sm.found_b = b;
                 sm.found_start = start;
             }
@@ -393,7 +393,8 @@ __global__ void __launch_bounds__(Geom<T, TQ, D>::THREADS, 1) paged_decode_kerne
             int n = length(d.b);
             while (d.q_at >= d.b_start + plan.quanta(n)) {
                 d.b_start += plan.quanta(n);
-                n = length(++d.b);
+                if (++d.b >= a.B) return false;  // (only if the lengths change under the call)
+                n = length(d.b);
             }
             const int stop = d.b_start + plan.quanta(n), rows_at = d.b_start + plan.overhead, q_end = min(plan.q_hi, stop);
             from_start = d.q_at <= rows_at;
@@ -1251,7 +1252,10 @@ int decode(const char* fn, bool fp8, const void* q, const void* k_pages, const v
     const size_t need = chai_decode_paged_workspace_bytes(B, H, D);
     CHAI_REQUIRE(workspace_bytes >= need, CHAI_ERR_WORKSPACE, "%s: workspace has %zu bytes, %zu needed", fn, workspace_bytes,
                  need);
-    decode_ws(static_cast<char*>(workspace), B, H, D, &a.ws);
+    CHAI_REQUIRE(decode_ws(static_cast<char*>(workspace), B, H, D, &a.ws) <= need, CHAI_ERR_WORKSPACE, "%s: workspace layout", fn);
+    const size_t rows = (size_t)B * H * D * elem_size(dtype);
+    CHAI_REQUIRE(static_cast<const char*>(q) + rows <= out || static_cast<const char*>(out) + rows <= q, CHAI_ERR_INVALID_ARG,
+                 "%s: q and out overlap (a head's query is read until the call ends)", fn);
     a.q = q;
     a.k_pages = k_pages;
     a.v_pages = v_pages;

@@ -293,6 +293,44 @@ def test_decode_repeats_bit_for_bit_on_other_streams_and_in_graphs(cache, io):
         assert chai.chai_device_status(ws) == chai.CHAI_OK
 
 
+def test_decode_into_its_own_queries_is_refused():
+    c = make("bf16", "bf16", 2, 4, 2, 64, 16, [31, 20], seed=27)
+    with pytest.raises(chai.ChaiError) as e:
+        decode(c, out=c["q"])
+    assert e.value.status == chai.CHAI_ERR_INVALID_ARG and "overlap" in str(e.value)
+
+
+def test_two_calls_at_once_on_streams_and_workspaces_of_their_own():
+    cases = [make("bf16", "bf16", 3, 16, 4, 128, 16, [3000, 500, 77], seed=71), make("e4m3", "bf16", 2, 24, 7, 128, 32, [900, 4000], seed=72)]
+    want = [decode(c).clone() for c in cases]
+    streams = [torch.cuda.Stream() for _ in cases]
+    outs = [torch.empty_like(c["q"]) for c in cases]
+    spaces = [chai.new_workspace(chai.chai_decode_paged_workspace_bytes(c["B"], c["H"], 128), DEV) for c in cases]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for c, s, o, ws in zip(cases, streams, outs, spaces):
+            with torch.cuda.stream(s):
+                decode(c, out=o, workspace=ws)
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, w) for o, w in zip(outs, want))
+
+
+@pytest.mark.parametrize("B", [33, 148, 149, 200])
+def test_decode_batches_around_the_grid(B):
+    """More requests than a warp has lanes, as many as the GPU has SMs, and more; some long enough for several pieces."""
+    rng = np.random.default_rng(B)
+    lens = [int(x) for x in rng.integers(0, 30, B)]
+    lens[B // 2], lens[-1], lens[0] = 700, 900, 0
+    c = make("bf16", "bf16", B, 5, 2, 64, 8, lens, seed=B)
+    ws = chai.new_workspace(chai.chai_decode_paged_workspace_bytes(B, 5, 64), DEV)
+    check(c, decode(c, workspace=ws), f"B {B}")
+    assert chai.chai_device_status(ws) == chai.CHAI_OK
+    c["table"][B // 2, 3] = -1
+    got = decode(c, workspace=ws)
+    assert chai.chai_device_status(ws) == chai.CHAI_ERR_BAD_PAGE and not got[B // 2].any()
+    check(dict(c, lens=[0 if b == B // 2 else n for b, n in enumerate(lens)]), got, "the others")
+
+
 def test_decode_lengths_are_clamped_to_the_table():
     c = make("bf16", "bf16", 2, 4, 2, 64, 16, [31, 20], seed=26)      # tables have one page to spare
     full = c["table_np"].shape[1] * 16
@@ -544,7 +582,7 @@ def test_a_request_from_prompt_to_answer(cache):
 
 # ---- waits that run out (bounded, nothing faults: see test_gpu_failure_paths.py) ---------------------------------
 
-@pytest.mark.parametrize("cache", ["bf16"])
+@pytest.mark.parametrize("cache", ["bf16", "e4m3"])
 def test_decode_wait_that_runs_out_is_reported_and_the_next_launch_is_clean(cache, guard):
     B, H, k, D, page, T = 2, 40, 8, 128, 16, 16000
     gen = torch.Generator(device=DEV).manual_seed(51)

@@ -77,6 +77,7 @@ def test_refusals(lib, name):
         need = chai.chai_decode_paged_workspace_bytes(2, 4, 128)
         assert call(lib, name, ws_bytes=need - 1) == chai.CHAI_ERR_WORKSPACE and str(need).encode() in lib.chai_last_error()
         assert call(lib, name, ws_bytes=0) == chai.CHAI_ERR_WORKSPACE
+        assert call(lib, name) == chai.CHAI_ERR_INVALID_ARG and b"overlap" in lib.chai_last_error()   # q and out are one address here
     else:
         assert call(lib, name, rows=0) == chai.CHAI_ERR_INVALID_ARG
         assert call(lib, name, rows=(1 << 30) // 4) == chai.CHAI_ERR_UNSUPPORTED
