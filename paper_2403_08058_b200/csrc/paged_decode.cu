@@ -26,7 +26,6 @@ namespace {
 
 constexpr int kMaxCtas = 160;     // the workspace bound is stated for this many; a B200 has 148 SMs
 constexpr int kQuantum = 8;       // rows; page sizes are multiples of it
-constexpr int kJoinThreads = 128;
 constexpr int kJoinBlocks = 37;   // blocks per head, at most
 constexpr int kOverhead = 32;     // rows; see below (a multiple of 16)
 constexpr float kProbScale = 16384.f;  // e4m3: probabilities are kept times 2^14 (see phase V)
@@ -37,7 +36,7 @@ struct Geom {
     static constexpr int W = 12, THREADS = W * 32;  // warps (more would have too few registers)
     static constexpr int ROW = D * (int)sizeof(T);
     static constexpr int TR = FP8 ? 32 : 4096 / ROW;    // rows of a tile
-    static constexpr int STAGES = FP8 && D == 64 ? 6 : 3;  // slots of a warp
+    static constexpr int STAGES = 2;                       // slots of a warp
     static constexpr int DATA = TR * ROW;
     static constexpr int QUERY = DATA + (FP8 ? TR * 4 : 0);  // e4m3: the rows' scales lie behind them ...
     static constexpr int QROW = D * (int)sizeof(TQ), SLOT = QUERY + QROW;  // ... and the query of a new cluster's keys
@@ -1096,9 +1095,9 @@ __global__ void __launch_bounds__(Geom<T, TQ, D>::THREADS, 1) paged_decode_kerne
 
 // grid (H, blocks): out[b][h] from the partial results of consecutive pieces.  Bound by the round trips to L2, one for the
 // description and one for everything else: the first rows are on their way before the weights are known.
-template <typename TQ, int D>
-__global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(const DecodeArgs a, int n_ctas) {
-    constexpr int WARPS = kJoinThreads / 32, E = D / 32, AHEAD = 4;
+template <typename TQ, int D, int THREADS>
+__global__ void __launch_bounds__(THREADS) paged_join_kernel(const DecodeArgs a, int n_ctas) {
+    constexpr int WARPS = THREADS / 32, E = D / 32, AHEAD = 4;
     __shared__ float s_w[kMaxCtas], s_top[WARPS], s_sum[WARPS], s_o[WARPS][D];
     dependent_grid_sync();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, h = blockIdx.x;
@@ -1146,7 +1145,7 @@ __global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(const DecodeAr
         float top = -INFINITY;
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            const int i = tid + u * kJoinThreads;
+            const int i = tid + u * THREADS;
             ml[u] = make_float2(-INFINITY, 0.f);
             if (i < n) {
                 ml[u] = a.ws.ml[(size_t)(first + i) * a.H + h];
@@ -1155,7 +1154,7 @@ __global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(const DecodeAr
             }
             top = fmaxf(top, ml[u].x);
         }
-        static_assert(2 * kJoinThreads >= kMaxCtas, "two slots a thread");
+        static_assert(2 * THREADS >= kMaxCtas, "two slots a thread");
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
         if (lane == 0) s_top[warp] = top;
@@ -1167,7 +1166,7 @@ __global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(const DecodeAr
         float sum = 0.f;
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            const int i = tid + u * kJoinThreads;
+            const int i = tid + u * THREADS;
             if (i < n) {
                 const float weight = exp2_approx(ml[u].x - ref);
                 s_w[i] = weight;
@@ -1226,8 +1225,14 @@ int launch_decode(const DecodeArgs& args, cudaStream_t s) {
     DecodeArgs a = args;
     a.n_desc = a.B < n_ctas ? a.B : n_ctas;
     CHAI_LAUNCH_DEPENDENT("paged_decode_kernel launch", (paged_decode_kernel<T, TQ, D>), dim3(n_ctas), dim3(G::THREADS), smem, s, a);
-    CHAI_LAUNCH_DEPENDENT("paged_join_kernel launch", (paged_join_kernel<TQ, D>), dim3(a.H, a.n_desc < kJoinBlocks ? a.n_desc : kJoinBlocks),
-                          dim3(kJoinThreads), 0, s, a, n_ctas);
+    // A few long requests have many pieces each: more warps to a head then (one request of 131072 tokens, 148 pieces:
+    // 212.5 us a call with 4 warps, 210.9 with 16).  Short ones are faster with 4: such blocks find room beside the main
+    // kernel's and wait for its end in place (one request of 256 tokens, 16 pieces: 9.9 us against 10.9).
+    const dim3 grid(a.H, a.n_desc < kJoinBlocks ? a.n_desc : kJoinBlocks);
+    if (a.n_desc <= 4 && a.pool.capacity > 16384)
+        CHAI_LAUNCH_DEPENDENT("paged_join_kernel launch", (paged_join_kernel<TQ, D, 512>), grid, dim3(512), 0, s, a, n_ctas);
+    else
+        CHAI_LAUNCH_DEPENDENT("paged_join_kernel launch", (paged_join_kernel<TQ, D, 128>), grid, dim3(128), 0, s, a, n_ctas);
     return CHAI_OK;
 }
 
