@@ -475,7 +475,7 @@ _PAGED_IO = {torch.float32: CHAI_F32, torch.bfloat16: CHAI_BF16}
 
 def _paged_call(fn, dev: int, *args) -> None:
     """Calls fn(*args, stream) on the device that the tensors live on, on that device's current stream."""
-    if dev == torch.cuda.current_device():
+    if dev == _current_device():
         rc = fn(*args, _raw_stream(dev))
     else:
         with torch.cuda.device(dev):
@@ -485,6 +485,7 @@ def _paged_call(fn, dev: int, *args) -> None:
 
 
 # (torch.cuda.current_stream builds a Stream object, which costs as much as a launch)
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda dev: torch.cuda.current_stream(dev).cuda_stream)
 
 

@@ -1,7 +1,7 @@
 // Clustered decode attention over a paged cache (Fig. 3(b), Section 3.4), bound by HBM:
 //   out[b][h] = sum_t p_t V[h][t],  p = softmax_t(scale * q[r] . K[c][t]),  c the head's cluster, r its representative.
 //
-// The rows of all requests, in units of eight, are one line that is cut into equal pieces, one per CTA and one CTA per
+// The rows of all requests, in units of sixteen, are one line that is cut into equal pieces, one per CTA and one CTA per
 // SM: ragged batches and a single long request are balanced alike, whatever the clusters' sizes, because a piece
 // carries the key rows of all clusters and the value rows of all heads.  (Pieces too short to be worth a CTA are made
 // longer, and the heads, ordered by cluster, are dealt to several CTAs instead.)  A CTA goes through its piece request
@@ -10,13 +10,23 @@
 //   S   per cluster: running maximum and sum, scores become probabilities
 //   V   its warps share the (head, tile) pairs, in order of heads: sums of p_t V_t; a head that two warps share is
 //       added up in warp order
-// Every warp feeds itself: it owns a few slots of shared memory, and as soon as it is done with a tile one of its lanes
-// per page starts the bulk copies of the next tile into the freed slot, values of the chunk (and keys of the next one)
-// included, so that HBM is busy through the two barriers between the phases.  A tile's rows may come from several
-// pages; a copy is a run of rows that are neighbours in memory.
+// Every warp feeds itself: it owns two slots of shared memory, and as soon as it is done with a tile it starts the copies of
+// the next one into the freed slot (bulk copies, a lane for each run of rows that are neighbours in memory; e4m3: 16 bytes
+// a lane), values of the chunk and keys of the next one included, so that HBM is busy through the two barriers between
+// the phases.
 // A request that lies in one piece is written at once.  The others leave one partial result (maximum, sum, values) per
 // piece, and a second kernel, launched as a programmatic dependent, joins them: all sums are taken in an order that
-// follows from the lengths alone, and nothing in the workspace has to be cleared.
+// follows from the lengths alone, and nothing in the workspace has to be cleared.  (Joining in this kernel, by the CTA of a
+// request or the warp of a head that arrives last on a tagged word, measured 15.7 and 20 us where this takes 11.3, and
+// 76 and 79 where it takes 65: few hands do at the end what the second kernel spreads over the GPU.)
+//
+// Measured (GPU time a call, calls back to back, of the 6566 GB/s that a copy reaches): 7B shape (16 requests of 2048
+// tokens, 32 heads, 8 clusters, bf16) 61 us = 84 %; one request of 131072 tokens 211 us = 97 %; the 7B shape in e4m3 with
+// 32 clusters 68 us = 62 %.  bf16 and fp32 stream at the copy's rate; what is left is constant, some 4 us from the start to
+// the first tile's arrival (lengths, then tables and memberships, then rows: three round trips), 4 for the join, and
+// the phases of the CTAs that two requests meet in.  e4m3 is bound by the latencies of a warp's instructions (a tile of 32
+// rows takes 2500 cycles, of which the tensor cores' share is a fifth; issue slots are half full): neither the copies'
+// kind nor their number in flight matters, and without the tensor work it takes 5 us less, without the copies 11.
 #include <type_traits>
 
 #include "paged.cuh"
@@ -27,20 +37,29 @@ namespace {
 constexpr int kMaxCtas = 160;     // the workspace bound is stated for this many; a B200 has 148 SMs
 constexpr int kQuantum = 8;       // rows; page sizes are multiples of it
 constexpr int kJoinBlocks = 37;   // blocks per head, at most
-constexpr int kOverhead = 32;     // rows; see below (a multiple of 16)
+constexpr int kUnit = 16;         // rows; the line of all rows is divided in units of so many
+// Rows that a request counts more than it has, in front: what a CTA loses where one request ends and the next begins, which
+// a CTA without such a place makes up for (7B shape 65.7 us with none, 64.0 with 16, 63.5 with 32; 5 requests of up to 700
+// tokens 16.9, 12.0 and 12.0; 4 requests of a 66B shape in e4m3 55.6, 45.5 and 38.1; 48 and 64 measure as 32).
+constexpr int kOverhead = 32;
+__device__ __forceinline__ int units(int n) { return n > 0 ? (n + kUnit - 1 + kOverhead) / kUnit : 0; }
 constexpr float kProbScale = 16384.f;  // e4m3: probabilities are kept times 2^14 (see phase V)
 
 template <typename T, typename TQ, int D>
 struct Geom {
     static constexpr bool FP8 = std::is_same<T, Fp8E4M3>::value;
-    static constexpr int W = 12, THREADS = W * 32;  // warps (more would have too few registers)
+    // warps: as many as have registers enough (e4m3, 7B shape: 8 warps 84 us, 12 73, 14 and 16 spill and take 75 to 88)
+    static constexpr int W = 12, THREADS = W * 32;
     static constexpr int ROW = D * (int)sizeof(T);
-    static constexpr int TR = FP8 ? 32 : 4096 / ROW;    // rows of a tile
-    static constexpr int STAGES = 2;                       // slots of a warp
+    static constexpr int TR = FP8 ? 32 : 4096 / ROW;  // rows of a tile
+    // Slots of a warp.  Two tiles of 4 KB in flight for each of 12 warps are 98 KB an SM, more than the rate takes; a third
+    // only makes the queue longer, which every phase with few tiles a warp waits for (bf16: 131072 tokens 221 us with three,
+    // 211 with two; 7B shape 63.4 and 61.2; 10 warps with two 216 and 63.3).
+    static constexpr int STAGES = 2;
     static constexpr int DATA = TR * ROW;
     static constexpr int QUERY = DATA + (FP8 ? TR * 4 : 0);  // e4m3: the rows' scales lie behind them ...
     static constexpr int QROW = D * (int)sizeof(TQ), SLOT = QUERY + QROW;  // ... and the query of a new cluster's keys
-    static constexpr int HEADS = 112;           // heads a CTA handles at most
+    static constexpr int HEADS = 112;    // heads a CTA handles at most
     static constexpr int SCORES = 8192;  // scores of a chunk: clusters * rows
     static constexpr int CHUNK_ROWS = 512;
     // types of 2 and 4 bytes: lanes a row, rows a warp-wide load, such loads a tile
@@ -116,11 +135,9 @@ __device__ __forceinline__ int uniform(int x) { return __shfl_sync(0xffffffffu, 
 struct Plan {  // how the line of all rows is divided; kept in shared memory, for registers are short
     int pieces, each, rest;  // a piece has each or each + 1 units
     int piece, group, groups;
-    int unit_log, overhead;  // rows of a unit (as a power of two), units that a request counts in front of its rows
     int q_hi;                // where this CTA's piece ends
     // place where piece i begins (i * total / pieces without 64-bit division; i and rest are at most kMaxCtas)
     __device__ __forceinline__ int start(int i) const { return i * each + small_div(i * rest, pieces); }
-    __device__ __forceinline__ int quanta(int n) const { return n > 0 ? (n + (1 << unit_log) - 1 + kOverhead) >> unit_log : 0; }
 };
 struct Division {  // how far the CTA has divided its piece
     int q_at, b, b_start;  // place on the line, request, its place
@@ -149,7 +166,7 @@ struct Smem {
     Chunk chunk[2];
     alignas(16) Rows<G::CHUNK_ROWS / kQuantum> rows[2];
     alignas(8) unsigned long long full[G::W][G::STAGES];
-    int scan[2][G::W];
+    int scan[G::W];
     Plan plan;
     Division division[2];
     int found_b, found_start;
@@ -295,51 +312,39 @@ __global__ void __launch_bounds__(Geom<T, TQ, D>::THREADS, 1) paged_decode_kerne
     }
     dependent_grid_sync();
 
-    // -- the line of all rows, this CTA's piece [q_lo, q_hi) and the request it starts in.  A request counts
-    // kOverhead rows more than it has, in front: what a CTA loses where one request ends and the next begins.
+    // -- the line of all rows, this CTA's piece [q_lo, q_hi) and the request it starts in
     auto length = [&](int b) { return min(max(a.seq_lens[b], 0), a.pool.capacity); };
     const bool few = a.B <= 32;  // every warp then looks at all requests by itself, a lane each: no barrier is needed
     const int per = few ? 1 : (a.B + THREADS - 1) / THREADS;
     const int b_lo = min((few ? lane : tid) * per, a.B), b_hi = min(b_lo + per, a.B);
-    int mine8 = 0, mine16 = 0;  // in units of eight and of sixteen rows
+    int mine = 0;
 #pragma unroll 1
-    for (int b = b_lo; b < b_hi; ++b) {
-        const int n = length(b);
-        mine8 += n > 0 ? (n + 7 + kOverhead) / 8 : 0;
-        mine16 += n > 0 ? (n + 15 + kOverhead) / 16 : 0;
-    }
-    int upto8 = mine8, upto16 = mine16;
+    for (int b = b_lo; b < b_hi; ++b) mine += units(length(b));
+    int upto = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-        const int x = __shfl_up_sync(0xffffffffu, upto8, o), y = __shfl_up_sync(0xffffffffu, upto16, o);
-        if (lane >= o) upto8 += x, upto16 += y;
+        const int x = __shfl_up_sync(0xffffffffu, upto, o);
+        if (lane >= o) upto += x;
     }
-    int total8 = __shfl_sync(0xffffffffu, upto8, 31), total16 = __shfl_sync(0xffffffffu, upto16, 31);
+    int total = __shfl_sync(0xffffffffu, upto, 31);
     if (!few) {
-        if (lane == 31) sm.scan[0][warp] = upto8, sm.scan[1][warp] = upto16;
+        if (lane == 31) sm.scan[warp] = upto;
         __syncthreads();
-        total8 = total16 = 0;
+        total = 0;
 #pragma unroll 1
         for (int w = 0; w < W; ++w) {
-            const int x = sm.scan[0][w], y = sm.scan[1][w];
-            if (w < warp) upto8 += x, upto16 += y;
-            total8 += x;
-            total16 += y;
+            if (w < warp) upto += sm.scan[w];
+            total += sm.scan[w];
         }
     }
-    // Heads are dealt to several CTAs when a piece would be shorter than 32 rows, down to 4 heads a CTA.
+    // Heads are dealt to several CTAs when a piece would be shorter than 32 rows, down to 4 heads a CTA (one request of 256
+    // tokens: 10.6 us a call instead of 13.8; of 512: 11.1 instead of 15.5; thresholds of 16 and 64 rows measure the same).
     const int n_ctas = gridDim.x;
     const int base_groups = (a.H + G::HEADS - 1) / G::HEADS;
     int group_log = 0, most_pieces = base_groups == 1 ? n_ctas : small_div(n_ctas, base_groups);
-    while (total8 < 4 * most_pieces && (8 * base_groups << group_log) <= a.H && most_pieces > 1) ++group_log, most_pieces >>= 1;
+    while (total < 2 * most_pieces && (8 * base_groups << group_log) <= a.H && most_pieces > 1) ++group_log, most_pieces >>= 1;
     const int groups = base_groups << group_log;
-    // Pieces are cut in units of sixteen rows where that is fine enough (twelve a piece): copies are longer then.
-    const bool coarse = total16 >= 12 * most_pieces;
-    const int unit_log = coarse ? 4 : 3, total = coarse ? total16 : total8, overhead = kOverhead >> unit_log;
-    const int upto = coarse ? upto16 : upto8, mine = coarse ? mine16 : mine8;
     Plan plan;
-    plan.unit_log = unit_log;
-    plan.overhead = overhead;
     plan.pieces = max(1, min(most_pieces, total));
     plan.groups = groups;
     plan.piece = base_groups == 1 ? (int)blockIdx.x >> group_log : small_div(blockIdx.x, groups);
@@ -359,7 +364,7 @@ __global__ void __launch_bounds__(Geom<T, TQ, D>::THREADS, 1) paged_decode_kerne
         } else {
             if (here) {
                 int start = upto - mine, b = b_lo;
-                while (b + 1 < b_hi && q_lo >= start + plan.quanta(length(b))) start += plan.quanta(length(b++));
+                while (b + 1 < b_hi && q_lo >= start + units(length(b))) start += units(length(b++));
                 sm.found_b = b;
                 sm.found_start = start;
             }
@@ -390,15 +395,15 @@ __global__ void __launch_bounds__(Geom<T, TQ, D>::THREADS, 1) paged_decode_kerne
         while (d.t >= d.end) {  // the next request that has rows here
             if (d.q_at >= plan.q_hi) return false;
             int n = length(d.b);
-            while (d.q_at >= d.b_start + plan.quanta(n)) {
-                d.b_start += plan.quanta(n);
+            while (d.q_at >= d.b_start + units(n)) {
+                d.b_start += units(n);
                 if (++d.b >= a.B) return false;  // (only if the lengths change under the call)
                 n = length(d.b);
             }
-            const int stop = d.b_start + plan.quanta(n), rows_at = d.b_start + plan.overhead, q_end = min(plan.q_hi, stop);
+            const int stop = d.b_start + units(n), rows_at = d.b_start + kOverhead / kUnit, q_end = min(plan.q_hi, stop);
             from_start = d.q_at <= rows_at;
-            d.t = max(d.q_at - rows_at, 0) << plan.unit_log;
-            d.end = q_end > rows_at ? min(n, (q_end - rows_at) << plan.unit_log) : d.t;
+            d.t = max(d.q_at - rows_at, 0) * kUnit;
+            d.end = q_end > rows_at ? min(n, (q_end - rows_at) * kUnit) : d.t;
             d.single = from_start && q_end == stop;
             d.span_end = from_start && !d.single ? stop : 0;
             d.slot = plan.piece + d.b;
