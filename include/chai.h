@@ -429,9 +429,11 @@ int chai_read_kv_paged_fp8(const void* k_pages, const void* v_pages, const float
  *   q, out [B,H,D] of type dtype, which is the pages' type too; _fp8: CHAI_F32 or CHAI_BF16, e4m3 pages.
  * A request of length 0 gets zero rows, and so does a request one of whose pages is bad (CHAI_ERR_BAD_PAGE) and a head
  * whose membership cannot be resolved (CHAI_ERR_BAD_MEMBERSHIP).  Rows at or beyond a request's length are never used,
- * whatever they hold.  Sums and softmax statistics are fp32, taken in an order that depends on the lengths alone:
- * results are bitwise repeatable.  The workspace (chai_decode_paged_workspace_bytes: 64 KiB and (160 + B) * H * (D + 8)
- * 32-bit words, whatever the lengths) needs no clearing; calls that share one must be ordered on one stream.
+ * whatever they hold.  q and out must not overlap.  Sums and softmax statistics are fp32, taken in an order that follows
+ * from the lengths and memberships: results are bitwise repeatable.  _fp8: probabilities times row scales are held to 2^-22
+ * of the head's largest row scale (a row of zeros has the scale 1).  The workspace (chai_decode_paged_workspace_bytes:
+ * 64 KiB and (160 + B) * H * (D + 8) 32-bit words, whatever the lengths) needs no clearing; calls that share one must be
+ * ordered on one stream.
  * H is at most 1024, B below 65536, B * max_pages * page_size below 2^33.
  */
 size_t chai_decode_paged_workspace_bytes(int B, int H, int D);

@@ -7,8 +7,8 @@
 // Both are copies, bound by HBM.  A block takes a run of tokens of one plane; a thread moves several 16-byte vectors of
 // the dense side, all loads issued before the first store.  (One sequence of vectors over planes and tokens alike, with
 // a division to find the plane of each, was bound by its instructions instead: append to e4m3 65 us where this takes
-// 31, read-back from e4m3 69 us and 52.)  A decode step's few rows go to one block per request that also advances
-// the request's length.
+// 31, read-back from e4m3 69 us and 49; of the 6566 GB/s that a copy reaches those are 88 % and 92 %.)  A decode step's
+// few rows go to one block per request that also advances the request's length.
 #include <type_traits>
 
 #include "paged.cuh"

@@ -3,8 +3,8 @@
 //
 // The rows of all requests, in units of sixteen, are one line that is cut into equal pieces, one per CTA and one CTA per
 // SM: ragged batches and a single long request are balanced alike, whatever the clusters' sizes, because a piece
-// carries the key rows of all clusters and the value rows of all heads.  (Pieces too short to be worth a CTA are made
-// longer, and the heads, ordered by cluster, are dealt to several CTAs instead.)  A CTA goes through its piece request
+// carries the key rows of all clusters and the value rows of all heads.  (Where pieces would be short or the layer has
+// many planes, pieces are made longer, and the heads, ordered by cluster, are dealt to several CTAs instead.)  A CTA goes through its piece request
 // by request in chunks that fit its score buffer:
 //   K   its warps share the (cluster, tile) pairs of the chunk: scores into shared memory
 //   S   per cluster: running maximum and sum, scores become probabilities
@@ -16,13 +16,13 @@
 // the phases.
 // A request that lies in one piece is written at once.  The others leave one partial result (maximum, sum, values) per
 // piece, and a second kernel, launched as a programmatic dependent, joins them: all sums are taken in an order that
-// follows from the lengths alone, and nothing in the workspace has to be cleared.  (Joining in this kernel, by the CTA of a
+// follows from the lengths and memberships alone, and nothing in the workspace has to be cleared.  (Joining in this kernel, by the CTA of a
 // request or the warp of a head that arrives last on a tagged word, measured 15.7 and 20 us where this takes 11.3, and
 // 76 and 79 where it takes 65: few hands do at the end what the second kernel spreads over the GPU.)
 //
 // Measured (GPU time a call, calls back to back, of the 6566 GB/s that a copy reaches): 7B shape (16 requests of 2048
-// tokens, 32 heads, 8 clusters, bf16) 61 us = 84 %; one request of 131072 tokens 211 us = 97 %; the 7B shape in e4m3 with
-// 32 clusters 68 us = 62 %.  bf16 and fp32 stream at the copy's rate; what is left is constant, some 4 us from the start to
+// tokens, 32 heads, 8 clusters, bf16) 61.6 us = 83 %; one request of 131072 tokens 209 us = 98 %; the 7B shape in e4m3 with
+// 32 clusters 65.7 us = 64 %.  bf16 and fp32 stream at the copy's rate; what is left is constant, some 4 us from the start to
 // the first tile's arrival (lengths, then tables and memberships, then rows: three round trips), 4 for the join, and
 // the phases of the CTAs that two requests meet in.  e4m3 is bound by the latencies of a warp's instructions (a tile of 32
 // rows takes 2500 cycles, of which the tensor cores' share is a fifth; issue slots are half full): neither the copies'
@@ -337,12 +337,19 @@ __global__ void __launch_bounds__(Geom<T, TQ, D>::THREADS, 1) paged_decode_kerne
             total += sm.scan[w];
         }
     }
-    // Heads are dealt to several CTAs when a piece would be shorter than 32 rows, down to 4 heads a CTA (one request of 256
-    // tokens: 10.6 us a call instead of 13.8; of 512: 11.1 instead of 15.5; thresholds of 16 and 64 rows measure the same).
+    // Heads are dealt to several CTAs when a piece would be shorter than two tiles of 16 rows (e4m3: of 32), down to 4 heads
+    // a CTA: one request of 256 tokens takes 10.6 us a call instead of 13.8; of 512, 11.1 instead of 15.5; thresholds of half
+    // and twice that measure the same or worse (e4m3, 66B shape of 1024 tokens: 24.5, and 25.6 with 128 rows).
+    // To two CTAs when a layer has many planes and the batch is small, for longer pieces are more even (in units) and leave
+    // fewer partial results: ragged 33B shape 63.2 -> 59.0 us, 66B shape in e4m3 35.6 -> 32.0, 131072 tokens 211 -> 209.4.
+    // A cluster that both have a part of has its keys read twice, which layers of few planes (12 heads, 5 clusters: 32.7 ->
+    // 34.5 us; 32 and 8 still 61.5 -> 61.7) and pieces of many requests (100: 110.4 -> 112) pay more for than they gain.
     const int n_ctas = gridDim.x;
     const int base_groups = (a.H + G::HEADS - 1) / G::HEADS;
     int group_log = 0, most_pieces = base_groups == 1 ? n_ctas : small_div(n_ctas, base_groups);
-    while (total < 2 * most_pieces && (8 * base_groups << group_log) <= a.H && most_pieces > 1) ++group_log, most_pieces >>= 1;
+    const bool two = a.H + a.k >= 40 && 4 * a.B <= n_ctas;
+    while (((two && group_log == 0) || total < (G::FP8 ? 4 : 2) * most_pieces) && (8 * base_groups << group_log) <= a.H && most_pieces > 1)
+        ++group_log, most_pieces >>= 1;
     const int groups = base_groups << group_log;
     Plan plan;
     plan.pieces = max(1, min(most_pieces, total));
@@ -444,7 +451,7 @@ __global__ void __launch_bounds__(Geom<T, TQ, D>::THREADS, 1) paged_decode_kerne
                 sm.all.mem[h] = c < (unsigned)a.k ? (unsigned short)c : 0xffff;
                 sm.all.rep[h] = r < (unsigned)a.H ? (unsigned short)r : 0xffff;
             }
-            if (tid == 0) sm.any_bad = 0;
+            if (tid == 0) sm.any_bad = 0, sg.last = -1;
             __syncthreads();
             int known = 0;
             for (int h0 = 0; h0 < padded; h0 += THREADS) {
@@ -466,28 +473,44 @@ __global__ void __launch_bounds__(Geom<T, TQ, D>::THREADS, 1) paged_decode_kerne
                     for (int d = 0; d < D; ++d) o[d] = from_float<TQ>(0.f);
                 }
             }
-            const int lo = groups == 1 ? 0 : small_div(known * group, groups), hi = groups == 1 ? known : small_div(known * (group + 1), groups);
-            for (int h = tid; h < a.H; h += THREADS) {
-                const unsigned own = sm.all.key[h], c = own / 2048;
-                if (own == 0xfffffffeu) continue;
-                int rank = 0, place = 0;  // heads before this one, clusters (their representatives) before its own
+            // the group's heads: of two groups half the planes (keys of the clusters and values, in order), else as many heads
+            // as any (half the heads instead of half the planes: 7B shape 62.8 us, 61.7 this way; many groups have short
+            // pieces, where the barrier that this takes costs more than it gains, 0.3 us)
+            const bool by_planes = groups == 2 && a.H <= G::HEADS;
+            int lo = groups == 1 ? 0 : small_div(known * group, groups), n_heads = groups == 1 ? known : small_div(known * (group + 1), groups) - lo;
+            int mine = -1;
+            for (int h0 = 0; h0 < a.H; h0 += THREADS) {
+                const int h = h0 + tid;
+                const unsigned own = h < a.H ? sm.all.key[h] : 0xfffffffeu, c = own / 2048;
+                const bool ok = own != 0xfffffffeu;
+                int rank = 0, place = 0, places = 0;  // heads before this one, clusters (their representatives) before its own, clusters
+                if (ok) {
 #pragma unroll 2
-                for (int x = 0; x < padded; x += 4) {
-                    const uint4 u = *reinterpret_cast<const uint4*>(&sm.all.key[x]);
-                    rank += (u.x < own) + (u.y < own) + (u.z < own) + (u.w < own);
-                    place += (u.x & (u.x < c * 2048)) + (u.y & (u.y < c * 2048)) + (u.z & (u.z < c * 2048)) + (u.w & (u.w < c * 2048));
+                    for (int x = 0; x < padded; x += 4) {
+                        const uint4 u = *reinterpret_cast<const uint4*>(&sm.all.key[x]);
+                        rank += (u.x < own) + (u.y < own) + (u.z < own) + (u.w < own);
+                        place += (u.x & (u.x < c * 2048)) + (u.y & (u.y < c * 2048)) + (u.z & (u.z < c * 2048)) + (u.w & (u.w < c * 2048));
+                        places += (u.x & 1) + (u.y & 1) + (u.z & 1) + (u.w & 1);
+                    }
                 }
-                if (rank >= lo && rank < hi) {
+                bool in = ok && rank >= lo && rank < lo + n_heads;
+                if (by_planes) {  // (one turn of the loop)
+                    mine = ok ? small_div((rank + place + 1) * groups, known + places) : -1;
+                    lo = __syncthreads_count(ok && mine < group);
+                    in = mine == group;
+                }
+                if (in) {
                     sg.head[rank - lo] = (unsigned short)h;
                     sg.cluster[rank - lo] = (unsigned short)place;
                     sg.id[place % G::HEADS] = (unsigned short)c;
                     sg.rep[place % G::HEADS] = sm.all.rep[c];
                     if (rank == lo) sg.first = place;
-                    if (rank == hi - 1) sg.last = place;
+                    atomicMax(&sg.last, place);
                 }
             }
-            __syncthreads();
-            d.heads = hi - lo;
+            if (by_planes) n_heads = __syncthreads_count(mine == group);
+            else __syncthreads();
+            d.heads = n_heads;
             d.clusters = d.heads > 0 ? sg.last - sg.first + 1 : 0;
             d.rows = min(G::CHUNK_ROWS, small_div(G::SCORES, max(d.clusters, 1)) / G::TR * G::TR);
         }

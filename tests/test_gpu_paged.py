@@ -92,6 +92,43 @@ def test_decode_heads_and_lengths(cache, io, B, H, k, page, lens):
     check(c, decode(c), f"{cache} {io} B {B} H {H} k {k} page {page} lens {lens}")
 
 
+@pytest.mark.parametrize("cache,io", KINDS)
+@pytest.mark.parametrize("H,k,lens", [(52, 13, [3000, 1]), (100, 1, [2500]), (112, 112, [600, 700]), (113, 40, [900, 50]), (39, 1, [4000])])
+def test_decode_heads_dealt_to_several_ctas(cache, io, H, k, lens):
+    """One cluster, clusters of one head, lists that just fit a CTA and that do not; some heads unknown."""
+    c = make(cache, io, len(lens), H, k, 64, 16, lens, seed=H)
+    ws = chai.new_workspace(chai.chai_decode_paged_workspace_bytes(len(lens), H, 64), DEV)
+    check(c, decode(c, workspace=ws), f"H {H} k {k}")
+    assert chai.chai_device_status(ws) == chai.CHAI_OK
+    lost = [h for h in range(H) if h not in c["reps"][0]][::3] or [int(c["reps"][0, 5])]
+    c["membership"][0, lost] = -1
+    got = decode(c, workspace=ws)
+    assert chai.chai_device_status(ws) == chai.CHAI_ERR_BAD_MEMBERSHIP
+    assert not got[0, lost].any()
+    # the others as before: known heads against the definition
+    kept = [h for h in range(H) if h not in lost]
+    want = got.clone()
+    c["membership"].copy_(torch.from_numpy(c["mem"]))
+    want[0, lost] = decode(c, workspace=ws)[0, lost]
+    check(c, want, f"H {H} k {k}, {len(kept)} known")
+
+
+@pytest.mark.parametrize("cache,io", KINDS)
+def test_decode_requests_that_share_pages(cache, io):
+    """A prefix in pages that three requests have in their lists, and one page twice in one list."""
+    lens, page = [150, 100, 64], 16
+    c = make(cache, io, 3, 6, 2, 128, page, lens, seed=91)
+    t = c["table"]
+    t[0, 3] = t[0, 1]
+    t[1, :4], t[2, :4] = t[0, :4], t[0, :4]
+    for name in ("k_rows", "v_rows"):
+        rows = c[name]
+        rows[0][:, 48:64] = rows[0][:, 16:32]
+        rows[1][:, :64] = rows[0][:, :64]
+        rows[2][:, :64] = rows[0][:, :64]
+    check(c, decode(c), f"{cache} {io}")
+
+
 @pytest.mark.parametrize("cache,io", KINDS[1:3])
 def test_decode_many_short_requests(cache, io):
     rng = np.random.default_rng(5)
