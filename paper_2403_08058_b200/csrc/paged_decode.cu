@@ -21,12 +21,11 @@
 // 76 and 79 where it takes 65: few hands do at the end what the second kernel spreads over the GPU.)
 //
 // Measured (GPU time a call, calls back to back, of the 6566 GB/s that a copy reaches): 7B shape (16 requests of 2048
-// tokens, 32 heads, 8 clusters, bf16) 61.6 us = 83 %; one request of 131072 tokens 209 us = 98 %; the 7B shape in e4m3 with
-// 32 clusters 65.7 us = 64 %.  bf16 and fp32 stream at the copy's rate; what is left is constant, some 4 us from the start to
-// the first tile's arrival (lengths, then tables and memberships, then rows: three round trips), 4 for the join, and
-// the phases of the CTAs that two requests meet in.  e4m3 is bound by the latencies of a warp's instructions (a tile of 32
-// rows takes 2500 cycles, of which the tensor cores' share is a fifth; issue slots are half full): neither the copies'
-// kind nor their number in flight matters, and without the tensor work it takes 5 us less, without the copies 11.
+// tokens, 32 heads, 8 clusters, bf16) 60.4 us = 85 %; one request of 131072 tokens 207 us = 99 %; the 7B shape in e4m3 with
+// 32 clusters 55 to 57 us = 74 to 77 %.  Rows stream at the copy's rate or near it; what is left is constant, some 4 us from
+// the start to the first tile's arrival (lengths, then tables and memberships, then rows: three round trips), 4 for the
+// join, and the phases of the CTAs that two requests meet in.  e4m3 is also bound by the latencies of a warp's instructions
+// (issue slots are half full, the tensor cores busy for a seventh of the time), which more warps hide: see Geom.
 #include <type_traits>
 
 #include "paged.cuh"
@@ -38,18 +37,23 @@ constexpr int kMaxCtas = 160;     // the workspace bound is stated for this many
 constexpr int kQuantum = 8;       // rows; page sizes are multiples of it
 constexpr int kJoinBlocks = 37;   // blocks per head, at most
 constexpr int kUnit = 16;         // rows; the line of all rows is divided in units of so many
-// Rows that a request counts more than it has, in front: what a CTA loses where one request ends and the next begins, which
-// a CTA without such a place makes up for (7B shape 65.7 us with none, 64.0 with 16, 63.5 with 32; 5 requests of up to 700
-// tokens 16.9, 12.0 and 12.0; 4 requests of a 66B shape in e4m3 55.6, 45.5 and 38.1; 48 and 64 measure as 32).
-constexpr int kOverhead = 32;
-__device__ __forceinline__ int units(int n) { return n > 0 ? (n + kUnit - 1 + kOverhead) / kUnit : 0; }
+// Units that a request counts more than it has, in front: what a CTA loses where one request ends and the next begins, which
+// a CTA without such a place makes up for.  In rows, e4m3, 7B shape: 32 59.9 us, 48 58.6, 64 57.4, 112 57.4; 16 requests of
+// 600 tokens 28.6, 27.7, 26.2, 26.4; bf16, 7B shape 61.1, 60.5, 60.3, 60.8; without any, before other changes, 65.7 against
+// 64.0 with 16 and 63.5 with 32.  Where all requests are short, CTAs meet several ends each, and more is lost to uneven
+// pieces: 100 requests of up to 700 tokens 82.0, 83.2, 84.0; 60 of up to 100 22.3, 23.3, 24.4 (16 of up to 200: 17.2 us
+// with 16 rows, 13.9 with 32).
+__device__ __forceinline__ int overhead(int n) { return min(4, max(2, n >> 7)); }
+__device__ __forceinline__ int units(int n) { return n > 0 ? (n + kUnit - 1) / kUnit + overhead(n) : 0; }
 constexpr float kProbScale = 16384.f;  // e4m3: probabilities are kept times 2^14 (see phase V)
 
 template <typename T, typename TQ, int D>
 struct Geom {
     static constexpr bool FP8 = std::is_same<T, Fp8E4M3>::value;
-    // warps: as many as have registers enough (e4m3, 7B shape: 8 warps 84 us, 12 73, 14 and 16 spill and take 75 to 88)
-    static constexpr int W = 12, THREADS = W * 32;
+    // warps: e4m3, bound by the latency of a warp's instructions, as many as have registers enough (7B shape: 12 62.2 us,
+    // 16 57.4; 18 spill, 78.8); the others as many as keep the copies going (bf16, 7B shape: 10 62.3 us, 12 60.6, 14 61.3, 16
+    // 60.7; fp32, one request of 256 tokens 9.8 with 12, 10.4 with 16)
+    static constexpr int W = FP8 ? 16 : 12, THREADS = W * 32;
     static constexpr int ROW = D * (int)sizeof(T);
     static constexpr int TR = FP8 ? 32 : 4096 / ROW;  // rows of a tile
     // Slots of a warp.  Two tiles of 4 KB in flight for each of 12 warps are 98 KB an SM, more than the rate takes; a third
@@ -337,9 +341,9 @@ __global__ void __launch_bounds__(Geom<T, TQ, D>::THREADS, 1) paged_decode_kerne
             total += sm.scan[w];
         }
     }
-    // Heads are dealt to several CTAs when a piece would be shorter than two tiles of 16 rows (e4m3: of 32), down to 4 heads
-    // a CTA: one request of 256 tokens takes 10.6 us a call instead of 13.8; of 512, 11.1 instead of 15.5; thresholds of half
-    // and twice that measure the same or worse (e4m3, 66B shape of 1024 tokens: 24.5, and 25.6 with 128 rows).
+    // Heads are dealt to several CTAs when a piece would be shorter than 32 rows, down to 4 heads a CTA: one request of 256
+    // tokens takes 10.6 us a call instead of 13.8; of 512, 11.1 instead of 15.5; thresholds of half and twice that measure the
+    // same or worse (e4m3, 66B shape of 400 tokens: 17.8 us, with 64 rows 21.4).
     // To two CTAs when a layer has many planes and the batch is small, for longer pieces are more even (in units) and leave
     // fewer partial results: ragged 33B shape 63.2 -> 59.0 us, 66B shape in e4m3 35.6 -> 32.0, 131072 tokens 211 -> 209.4.
     // A cluster that both have a part of has its keys read twice, which layers of few planes (12 heads, 5 clusters: 32.7 ->
@@ -348,7 +352,7 @@ __global__ void __launch_bounds__(Geom<T, TQ, D>::THREADS, 1) paged_decode_kerne
     const int base_groups = (a.H + G::HEADS - 1) / G::HEADS;
     int group_log = 0, most_pieces = base_groups == 1 ? n_ctas : small_div(n_ctas, base_groups);
     const bool two = a.H + a.k >= 40 && 4 * a.B <= n_ctas;
-    while (((two && group_log == 0) || total < (G::FP8 ? 4 : 2) * most_pieces) && (8 * base_groups << group_log) <= a.H && most_pieces > 1)
+    while (((two && group_log == 0) || total < 2 * most_pieces) && (8 * base_groups << group_log) <= a.H && most_pieces > 1)
         ++group_log, most_pieces >>= 1;
     const int groups = base_groups << group_log;
     Plan plan;
@@ -407,7 +411,7 @@ __global__ void __launch_bounds__(Geom<T, TQ, D>::THREADS, 1) paged_decode_kerne
                 if (++d.b >= a.B) return false;  // (only if the lengths change under the call)
                 n = length(d.b);
             }
-            const int stop = d.b_start + units(n), rows_at = d.b_start + kOverhead / kUnit, q_end = min(plan.q_hi, stop);
+            const int stop = d.b_start + units(n), rows_at = d.b_start + overhead(n), q_end = min(plan.q_hi, stop);
             from_start = d.q_at <= rows_at;
             d.t = max(d.q_at - rows_at, 0) * kUnit;
             d.end = q_end > rows_at ? min(n, (q_end - rows_at) * kUnit) : d.t;
@@ -547,153 +551,112 @@ __global__ void __launch_bounds__(Geom<T, TQ, D>::THREADS, 1) paged_decode_kerne
     };
 
     // -- the warp's own slots
-    int issued = 0, used = 0, in_slot = 0, out_slot = 0, out_phase = 0;  // tiles started / finished; next slot of each
+    int issued = 0, used = 0;                                            // tiles started / finished: the next slots follow from them
+    static_assert(G::STAGES == 2, "slots and phases are bits of the counts");
     bool dead = false;                                                   // a wait ran out: no more copies, no more waits
     Walk<W> ahead;                                                       // the next tile to start, of chunk number ahead_no
     int ahead_no = 0, ahead_par = 1, ready_no = 0;                       // chunks up to ready_no are prepared
-    int ahead_rows = 0, ahead_tiles = 1, ahead_run = 0;                  // of that chunk
     const char* ahead_plane = nullptr;                                   // the plane of the next tile, in page 0 ...
-    [[maybe_unused]] const float* ahead_scales = nullptr;                // ... its rows' scales ...
-    const char* ahead_query = nullptr;                                   // ... and, of keys, the query
+    [[maybe_unused]] const float* ahead_scales = nullptr;                // ... and its rows' scales
     ahead.left = 0;
     ahead.phase = 1;
     const size_t plane_bytes = (size_t)ps * D * sizeof(T);
     const uint32_t slots = smem_addr(sm.slot[warp][0]), bars = smem_addr(&sm.full[warp][0]);
-    // e4m3: a lane's place in a warp-wide copy of 512 bytes (see Geom), by row / 4 % 4 of the lane group's first row: four
-    // rows a copy for D = 128; eight for D = 64, where the lane's own row matters too
-    uint32_t copy_at[4] = {};
-    if constexpr (G::FP8) {
-        const int line = (lane >> 3) * 128;
-#pragma unroll
-        for (int q = 0; q < 4; ++q)
-            copy_at[q] = D == 128 ? line + 16 * ((lane & 7) ^ (4 * ((lane >> 3) & 1)) ^ (2 * q)) : line + 16 * ((lane & 7) ^ (2 * ((q + (lane >> 4)) & 3)));
-    }
+    // e4m3: a lane's place in a warp-wide copy of 512 bytes (see Geom) whose first row is one of the first four of sixteen:
+    // four rows a copy for D = 128; eight for D = 64, where the lane's own row matters too
+    [[maybe_unused]] const uint32_t copy_at = (lane >> 3) * 128 + 16 * ((lane & 7) ^ (D == 128 ? 4 * ((lane >> 3) & 1) : 2 * (lane >> 4)));
 
-    // The next tile to start, with its addresses worked out ahead of time: the shared-memory reads that they take pass
-    // behind the arithmetic of the tile before.
-    bool staged = false, next_query = false;
-    int next_rows = 0;
-    [[maybe_unused]] int next_run = 0;
-    constexpr int GROUPS = G::TR / kQuantum;
-    const char* next_src[G::FP8 ? GROUPS : 1] = {};
-    [[maybe_unused]] const float* next_scales = nullptr;
-    auto stage = [&]() __attribute__((always_inline)) {
-        while (ahead.left == 0) {
-            if (ahead.phase == 0) {
-                ahead.start(1, sm.chunk[ahead_par], warp);
-            } else {
-                if (ahead_no >= ready_no) return;
-                ++ahead_no;
-                ahead_par ^= 1;
-                const Chunk& c = sm.chunk[ahead_par];
-                ahead_rows = uniform(c.rows);
-                ahead_tiles = uniform(c.tiles);
-                ahead_run = uniform(c.run);
-                ahead.start(0, c, warp);
-            }
-        }
-        const bool key = ahead.phase == 0;
-        next_query = key && ahead.fresh;
-        if (ahead.fresh) {
-            ahead.fresh = false;
-            const auto& sg = sm.seg[sm.chunk[ahead_par].seg];
-            const int plane = key ? sg.id[(sg.first + ahead.p) % G::HEADS] : sg.head[ahead.p];
-            ahead_plane = static_cast<const char*>(key ? a.k_pages : a.v_pages) + plane * plane_bytes;
-            if constexpr (G::FP8) ahead_scales = (key ? a.k_scales : a.v_scales) + plane * (size_t)ps;
-            if (key)
-                ahead_query = static_cast<const char*>(a.q) +
-                              ((size_t)sm.chunk[ahead_par].b * a.H + sg.rep[(sg.first + ahead.p) % G::HEADS]) * G::QROW;
-        }
-        const int row0 = ahead.j * G::TR;
-        next_rows = min(G::TR, ahead_rows - row0);
-        const auto& rows = sm.rows[ahead_par];
-        const size_t* off = (key ? rows.k : rows.v) + row0 / kQuantum;
-        if constexpr (!G::FP8) {
-            next_src[0] = ahead_plane + off[min(lane * ahead_run, next_rows - 1) / kQuantum];
-            next_run = ahead_run;
-        } else {
-            static_assert(GROUPS == 4, "two loads");
-            const ulonglong2 x = reinterpret_cast<const ulonglong2*>(off)[0], y = reinterpret_cast<const ulonglong2*>(off)[1];
-            const char* mine = ahead_plane + lane * 16;
-            next_src[0] = mine + x.x;
-            next_src[1] = mine + x.y;
-            next_src[2] = mine + y.x;
-            next_src[3] = mine + y.y;
-            const int2 at = rows.at[row0 / kQuantum + (lane & 7) / 2];
-            next_scales = ahead_scales + (size_t)(unsigned)at.x * (unsigned)((key ? a.k : a.H) * ps) + (at.y + (lane & 1) * 4);
-        }
-        ahead.step(ahead_tiles);
-        staged = true;
-    };
-    // Starts copies until the warp's slots are in flight or nothing is known to copy.
+    // Starts copies until the warp's slots are in flight or nothing is known to copy.  (Addresses are worked out when a slot
+    // is free.  Held ready from a tile earlier they cost registers, which are worth more as warps: e4m3 with 16 warps, 7B
+    // shape 61.9 us that way and 56.5 this way, bf16 61.3 and 60.6.)
     auto fill = [&]() __attribute__((always_inline)) {
 #pragma unroll 1
-        while (!dead) {
-            if (staged) {
-                if (issued - used == G::STAGES) return;
-                const uint32_t slot = slots + in_slot * G::SLOT, bar = bars + in_slot * 8;
-                if constexpr (!G::FP8) {
-                    if (lane == 0)
-                        asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar),
-                                     "r"(next_rows * G::ROW + (next_query ? G::QROW : 0))
-                                     : "memory");
-                    __syncwarp();
-                    const int r0 = lane * next_run;
-                    if (r0 < next_rows) copy_rows(slot + r0 * G::ROW, next_src[0], min(next_run, next_rows - r0) * G::ROW, bar);
-                    if (next_query && lane == 31) copy_rows(slot + G::QUERY, ahead_query, G::QROW, bar);
+        while (!dead && issued - used < G::STAGES) {
+            while (ahead.left == 0) {
+                if (ahead.phase == 0) {
+                    ahead.start(1, sm.chunk[ahead_par], warp);
                 } else {
-                    // 16 bytes a lane, and as many of the scales.  Behind the last row the tile is filled with zeros, up to
-                    // the end of a step
-                    constexpr int UNITS = kQuantum * G::ROW / 512, EACH = 512 / G::ROW;  // warp-wide copies of eight rows, rows of one
-                    if (next_rows == G::TR) {
-#pragma unroll
-                        for (int g = 0; g < GROUPS; ++g)
-#pragma unroll
-                            for (int u = 0; u < UNITS; ++u) copy16(slot + copy_at[(2 * g + u) & (D == 128 ? 3 : 2)] + (g * kQuantum + u * EACH) * G::ROW, next_src[g] + u * 512);
-                        if (lane < 8) copy16(slot + G::DATA + lane * 16, next_scales);
-                    } else {
-                        const int left = next_rows - lane / (G::ROW / 16);
-#pragma unroll 1
-                        for (int s = 0; s * 16 < next_rows; ++s) {
-#pragma unroll
-                            for (int g = 0; g < 2; ++g)
-#pragma unroll
-                                for (int u = 0; u < UNITS; ++u)
-                                    copy16(slot + copy_at[(2 * g + u) & (D == 128 ? 3 : 2)] + (s * 16 + g * kQuantum + u * EACH) * G::ROW,
-                                           (s == 0 ? next_src[g] : next_src[g + 2]) + u * 512, left > s * 16 + g * kQuantum + u * EACH ? 16 : 0);
-                        }
-                        if (lane < 8) copy16(slot + G::DATA + lane * 16, next_scales, min(max(next_rows - lane * 4, 0), 4) * 4);
-                    }
-                    if (next_query && lane * 16 < G::QROW) copy16(slot + G::QUERY + lane * 16, ahead_query + lane * 16);
-                    asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
+                    if (ahead_no >= ready_no) return;
+                    ++ahead_no;
+                    ahead_par ^= 1;
+                    ahead.start(0, sm.chunk[ahead_par], warp);
                 }
-                in_slot = in_slot + 1 == G::STAGES ? 0 : in_slot + 1;
-                ++issued;
-                staged = false;
             }
-            stage();
-            if (!staged) return;
+            const Chunk& in = sm.chunk[ahead_par];
+            const bool key = ahead.phase == 0, query = key && ahead.fresh;
+            int query_row = 0;
+            if (ahead.fresh) {
+                ahead.fresh = false;
+                const auto& sg = sm.seg[in.seg];
+                const int plane = key ? sg.id[(sg.first + ahead.p) % G::HEADS] : sg.head[ahead.p];
+                ahead_plane = static_cast<const char*>(key ? a.k_pages : a.v_pages) + plane * plane_bytes;
+                if constexpr (G::FP8) ahead_scales = (key ? a.k_scales : a.v_scales) + plane * (size_t)ps;
+                if (key) query_row = in.b * a.H + sg.rep[(sg.first + ahead.p) % G::HEADS];
+            }
+            const uint32_t slot = slots + (issued & 1) * G::SLOT, bar = bars + (issued & 1) * 8;
+            const int row0 = ahead.j * G::TR, n = min(G::TR, in.rows - row0);
+            const auto& rows = sm.rows[ahead_par];
+            const size_t* off = (key ? rows.k : rows.v) + row0 / kQuantum;
+            const char* q = static_cast<const char*>(a.q) + (size_t)(unsigned)query_row * G::QROW;
+            ahead.step(in.tiles);
+            if constexpr (!G::FP8) {
+                const int run = in.run, r0 = lane * run;
+                if (lane == 0)
+                    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(n * G::ROW + (query ? G::QROW : 0))
+                                 : "memory");
+                __syncwarp();
+                if (r0 < n) copy_rows(slot + r0 * G::ROW, ahead_plane + off[r0 / kQuantum], min(run, n - r0) * G::ROW, bar);
+                if (query && lane == 31) copy_rows(slot + G::QUERY, q, G::QROW, bar);
+            } else {
+                // 16 bytes a lane, and as many of the scales.  Behind the last row the tile is filled with zeros, up to the
+                // end of a step
+                constexpr int UNITS = kQuantum * G::ROW / 512, EACH = 512 / G::ROW;  // warp-wide copies of eight rows, rows of one
+                constexpr int GROUPS = G::TR / kQuantum;
+                static_assert(GROUPS == 4 && G::SLOT % 128 == 0, "two loads of offsets; places within a line are found by xor");
+                auto place = [&](int g, int u) { return ((slot + copy_at) ^ (32 * ((2 * g + u) & (D == 128 ? 3 : 2)))) + (g * kQuantum + u * EACH) * G::ROW; };
+                const ulonglong2 x = reinterpret_cast<const ulonglong2*>(off)[0], y = reinterpret_cast<const ulonglong2*>(off)[1];
+                const char* mine = ahead_plane + lane * 16;
+                const char* src[GROUPS] = {mine + x.x, mine + x.y, mine + y.x, mine + y.y};
+                const int2 at = rows.at[row0 / kQuantum + (lane & 7) / 2];
+                const float* scales = ahead_scales + (size_t)(unsigned)at.x * (unsigned)((key ? a.k : a.H) * ps) + (at.y + (lane & 1) * 4);
+                if (n == G::TR) {
+#pragma unroll
+                    for (int g = 0; g < GROUPS; ++g)
+#pragma unroll
+                        for (int u = 0; u < UNITS; ++u) copy16(place(g, u), src[g] + u * 512);
+                    if (lane < 8) copy16(slot + G::DATA + lane * 16, scales);
+                } else {
+                    const int left = n - lane / (G::ROW / 16);
+#pragma unroll 1
+                    for (int s = 0; s * 16 < n; ++s)
+#pragma unroll
+                        for (int g = 0; g < 2; ++g)
+#pragma unroll
+                            for (int u = 0; u < UNITS; ++u)
+                                copy16(place(g, u) + s * 16 * G::ROW, (s == 0 ? src[g] : src[g + 2]) + u * 512, left > s * 16 + g * kQuantum + u * EACH ? 16 : 0);
+                    if (lane < 8) copy16(slot + G::DATA + lane * 16, scales, min(max(n - lane * 4, 0), 4) * 4);
+                }
+                if (query && lane * 16 < G::QROW) copy16(slot + G::QUERY + lane * 16, q + lane * 16);
+                asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
+            }
+            ++issued;
         }
     };
     // Waits for the warp's next tile; nothing if the wait ran out, now or earlier.
     auto take = [&]() -> const unsigned char* {
         if (dead) return nullptr;
-        const uint32_t bar = bars + out_slot * 8;
-        if (!__all_sync(0xffffffffu, bar_test(bar, out_phase))) {
-            dead = __any_sync(0xffffffffu, !bar_wait(bar, out_phase, a.wait_limit));
+        const uint32_t bar = bars + (used & 1) * 8, phase = (used >> 1) & 1;
+        if (!__all_sync(0xffffffffu, bar_test(bar, phase))) {
+            dead = __any_sync(0xffffffffu, !bar_wait(bar, phase, a.wait_limit));
             if (dead) {
                 if (lane == 0) sm.err = CHAI_ERR_TIMEOUT;
                 return nullptr;
             }
         }
-        return sm.slot[warp][out_slot];
+        return sm.slot[warp][used & 1];
     };
     auto release = [&]() {
         ++used;
-        if (++out_slot == G::STAGES) {
-            out_slot = 0;
-            out_phase ^= 1;
-        }
         __syncwarp();  // every lane has read the tile before a copy overwrites it
     };
 
@@ -941,7 +904,7 @@ __global__ void __launch_bounds__(Geom<T, TQ, D>::THREADS, 1) paged_decode_kerne
                     if (rows < G::TR) {  // rows behind the last hold anything: zeros instead
 #pragma unroll 1
                         for (int i = rows * G::LPR + lane; i < G::TR * G::LPR; i += 32)
-                            *reinterpret_cast<uint4*>(sm.slot[warp][out_slot] + i * 16) = make_uint4(0, 0, 0, 0);
+                            *reinterpret_cast<uint4*>(sm.slot[warp][used & 1] + i * 16) = make_uint4(0, 0, 0, 0);
                         __syncwarp();
                     }
                     const unsigned char* base = tile + first * G::ROW + (lane % G::LPR) * 16;
@@ -1099,13 +1062,7 @@ __global__ void __launch_bounds__(Geom<T, TQ, D>::THREADS, 1) paged_decode_kerne
         }
     }
     if (dead)  // copies in flight end before the shared memory goes
-        for (int i = used; i < issued; ++i) {
-            bar_wait(bars + out_slot * 8, out_phase, kDefaultWaitLimitCycles);
-            if (++out_slot == G::STAGES) {
-                out_slot = 0;
-                out_phase ^= 1;
-            }
-        }
+        for (int i = used; i < issued; ++i) bar_wait(bars + (i & 1) * 8, (i >> 1) & 1, kDefaultWaitLimitCycles);
 
     if (!by_request && tid == 0) {  // pieces that open no request that goes on say so
         const Plan& plan = sm.plan;
