@@ -4,8 +4,8 @@
 // The rows of all requests, in units of sixteen, are one line that is cut into equal pieces, one per CTA and one CTA per
 // SM: ragged batches and a single long request are balanced alike, whatever the clusters' sizes, because a piece
 // carries the key rows of all clusters and the value rows of all heads.  (Where pieces would be short or the layer has
-// many planes, pieces are made longer, and the heads, ordered by cluster, are dealt to several CTAs instead.)  A CTA goes through its piece request
-// by request in chunks that fit its score buffer:
+// many planes, pieces are made longer, and the heads, ordered by cluster, are dealt to several CTAs instead.)  A CTA goes
+// through its piece request by request in chunks that fit its score buffer:
 //   K   its warps share the (cluster, tile) pairs of the chunk: scores into shared memory
 //   S   per cluster: running maximum and sum, scores become probabilities
 //   V   its warps share the (head, tile) pairs, in order of heads: sums of p_t V_t; a head that two warps share is
@@ -16,9 +16,9 @@
 // the phases.
 // A request that lies in one piece is written at once.  The others leave one partial result (maximum, sum, values) per
 // piece, and a second kernel, launched as a programmatic dependent, joins them: all sums are taken in an order that
-// follows from the lengths and memberships alone, and nothing in the workspace has to be cleared.  (Joining in this kernel, by the CTA of a
-// request or the warp of a head that arrives last on a tagged word, measured 15.7 and 20 us where this takes 11.3, and
-// 76 and 79 where it takes 65: few hands do at the end what the second kernel spreads over the GPU.)
+// follows from the lengths and memberships alone, and nothing in the workspace has to be cleared.  (Joining in this
+// kernel, by the CTA of a request or the warp of a head that arrives last on a tagged word, measured 15.7 and 20 us where
+// this took 11.3, and 76 and 79 where it took 65: few hands do at the end what the second kernel spreads over the GPU.)
 //
 // Measured (GPU time a call, calls back to back, of the 6566 GB/s that a copy reaches): 7B shape (16 requests of 2048
 // tokens, 32 heads, 8 clusters, bf16) 60.4 us = 85 %; one request of 131072 tokens 207 us = 99 %; the 7B shape in e4m3 with
