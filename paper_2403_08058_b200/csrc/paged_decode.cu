@@ -441,8 +441,8 @@ __global__ void __launch_bounds__(Geom<T, TQ, D>::THREADS, 1) paged_decode_kerne
             if (tid == THREADS - 1 && opens && (by_request || !d.single)) {
                 int end = plan.piece;  // the piece that the request ends in
                 if (!d.single) {
-                    end = max(end, (d.span_end - 1) / (plan.each + 1));
-                    while (plan.start(end + 1) < d.span_end) ++end;
+                    end = max(end, min((d.span_end - 1) / (plan.each + 1), plan.pieces - 1));
+                    while (end + 1 < plan.pieces && plan.start(end + 1) < d.span_end) ++end;
                 }
                 a.ws.desc[by_request ? b : plan.piece] = make_int4(d.single ? -1 : b, d.slot, end - plan.piece + 1, 0);
             }
@@ -1117,8 +1117,10 @@ __global__ void __launch_bounds__(THREADS) paged_join_kernel(const DecodeArgs a,
 #pragma unroll 1
     for (int di = blockIdx.y; di < a.n_desc; di += gridDim.y) {
         const int4 d = a.ws.desc[di];
-        if (d.x < 0) continue;
         const int b = d.x, first = d.y, n = d.z;
+        // -1: nothing to join.  (The other bounds hold unless another stream changes lengths under the call, which leaves
+        // descriptions unwritten; results are anyone's guess then, addresses are not.)
+        if (b < 0 || b >= a.B || n < 1 || n > n_ctas || first < 0 || first > kMaxCtas + a.B - n) continue;
         const float* src = a.ws.o + ((size_t)first * a.H + h) * D + lane * E;
         const size_t apart = (size_t)a.H * D;
         Row ahead[AHEAD];
