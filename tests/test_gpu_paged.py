@@ -113,6 +113,38 @@ def test_decode_heads_dealt_to_several_ctas(cache, io, H, k, lens):
     check(c, want, f"H {H} k {k}, {len(kept)} known")
 
 
+def test_the_largest_batch_goes_through_all_three():
+    """65535 requests of no, one or two tokens: append, read-back and decode.  Rows of bf16, one head; the softmax of two
+    scores in 64 bits.  Scores are below 64 * 9 / 8 and good to 66 * 2^-24 * 72 < 2^-11, a probability to twice that."""
+    B, D, page = 65535, 64, 8
+    g = torch.Generator().manual_seed(65)
+    lens = torch.randint(0, 3, (B,), generator=g, dtype=torch.int32)
+    x = {n: torch.randn(B, 1, 2, D, generator=g).clamp_(-3, 3).bfloat16() for n in ("k", "v")}
+    q = torch.randn(B, 1, D, generator=g).clamp_(-3, 3).bfloat16()
+    table = torch.randperm(B, generator=g).to(torch.int32)[:, None].to(DEV)
+    kp, vp = (torch.full((B, 1, page, D), float("nan"), device=DEV, dtype=torch.bfloat16) for _ in range(2))
+    seq, zero = torch.zeros(B, dtype=torch.int32, device=DEV), torch.zeros(B, 1, dtype=torch.int32, device=DEV)
+    chai.chai_append_kv_paged(x["k"].to(DEV), x["v"].to(DEV), kp, vp, zero, table, seq, new_lens=lens.to(DEV))
+    assert torch.equal(seq.cpu(), lens)
+    held = (torch.arange(2)[None] < lens[:, None])[:, None, :, None]
+    for got, name in zip(chai.chai_read_kv_paged(kp, vp, table, seq, T_out=2), ("k", "v")):
+        assert torch.equal(got.cpu(), torch.where(held, x[name], torch.zeros(())))
+    ws = chai.new_workspace(chai.chai_decode_paged_workspace_bytes(B, 1, D), DEV)
+    out = chai.chai_decode_attention_paged(q.to(DEV), kp, vp, zero, zero, table, seq, 0.125, workspace=ws).double().cpu()
+    assert chai.chai_device_status(ws) == chai.CHAI_OK
+    s = 0.125 * (q.double()[:, :, None] * x["k"].double()).sum(-1, keepdim=True)
+    p = torch.where(held, (s - torch.where(held, s, -torch.inf).amax(2, keepdim=True)).exp(), torch.zeros((), dtype=torch.float64))
+    ref = (p * x["v"].double()).sum(2) / p.sum(2).clamp_min(1e-300)
+    assert ((out - ref).abs() <= 2.0 ** -8 * ref.abs() + 2.0 ** -9 * 3).all()
+    assert not out[lens == 0].any()
+
+
+@pytest.mark.parametrize("cache,io", KINDS[1:3])
+def test_decode_the_largest_page(cache, io):
+    c = make(cache, io, 2, 2, 1, 64, 65536, [66001, 40], seed=64)
+    check(c, decode(c), "page of 65536")
+
+
 @pytest.mark.parametrize("cache,io", KINDS)
 def test_decode_requests_that_share_pages(cache, io):
     """A prefix in pages that three requests have in their lists, and one page twice in one list."""
