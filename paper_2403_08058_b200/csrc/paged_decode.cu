@@ -953,7 +953,9 @@ __global__ void __launch_bounds__(Geom<T, TQ, D>::THREADS, 1) paged_decode_kerne
 #pragma unroll
                         for (int i = 0; i < PARTS; ++i) part[i][0] = part[i][1] = part[i][2] = part[i][3] = 0.f;
                     }
-                    if (__any_sync(0xffffffffu, top * factor > 2.f) || (begins && __all_sync(0xffffffffu, top < 1.f / 65536))) {
+                    const unsigned high = __ballot_sync(0xffffffffu, top * factor > 2.f);
+                    const unsigned low = __ballot_sync(0xffffffffu, begins && top < 1.f / 65536);
+                    if (high != 0 || low == 0xffffffffu) {
                         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
                         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
                         const float old = factor;
@@ -965,7 +967,7 @@ __global__ void __launch_bounds__(Geom<T, TQ, D>::THREADS, 1) paged_decode_kerne
 #pragma unroll
                             for (int e = 0; e < 4; ++e) part[i][e] *= change;
                     }
-                    if (__any_sync(0xffffffffu, factor != 1.f)) {
+                    if (factor != 1.f) {  // (the same in every lane, as the maximum is)
 #pragma unroll
                         for (int s = 0; s < G::STEPS; ++s) vs[s] = make_float4(vs[s].x * factor, vs[s].y * factor, vs[s].z * factor, vs[s].w * factor);
                     }
