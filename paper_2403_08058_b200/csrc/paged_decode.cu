@@ -22,7 +22,7 @@
 //
 // Measured (GPU time a call, calls back to back, of the 6566 GB/s that a copy reaches): 7B shape (16 requests of 2048
 // tokens, 32 heads, 8 clusters, bf16) 60.4 us = 85 %; one request of 131072 tokens 207 us = 99 %; the 7B shape in e4m3 with
-// 32 clusters 55 to 57 us = 74 to 77 %.  Rows stream at the copy's rate or near it; what is left is constant, some 4 us from
+// 32 clusters 54 to 57 us = 74 to 78 %.  Rows stream at the copy's rate or near it; what is left is constant, some 4 us from
 // the start to the first tile's arrival (lengths, then tables and memberships, then rows: three round trips), 4 for the
 // join, and the phases of the CTAs that two requests meet in.  e4m3 is also bound by the latencies of a warp's instructions
 // (issue slots are half full, the tensor cores busy for a seventh of the time), which more warps hide: see Geom.
