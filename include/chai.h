@@ -375,6 +375,9 @@ int chai_decode_attention_fp8(const void* q, const void* k_rep, const void* v, c
  * once; a row's scale is known when the row is written, so such a cache grows a token at a time.
  * Requests may share pages that are only read.  A block-table entry outside [0, n_pages) is never turned into an
  * address: it is reported as CHAI_ERR_BAD_PAGE in the status word of the workspace.
+ * seq_lens, new_lens, block_table, membership and reps are read on the device and must stay as they are while a call
+ * runs.  If another stream writes them meanwhile, what the call computes is undefined; it still ends, and touches only
+ * rows of the pool.
  */
 
 /*

@@ -144,7 +144,8 @@ struct Plan {  // how the line of all rows is divided; kept in shared memory, fo
     __device__ __forceinline__ int start(int i) const { return i * each + small_div(i * rest, pieces); }
 };
 struct Division {  // how far the CTA has divided its piece
-    int q_at, b, b_start;  // place on the line, request, its place
+    int q_at, b;                    // place on the line, request
+    int next_b, next_n, next_start; // the next request with rows (B: none), its length and place
     int t, end, rows;      // of the current segment: next row, last row, rows of a chunk
     int par, heads, clusters, slot, span_end;
     int single, first, opened_span;
@@ -173,7 +174,7 @@ struct Smem {
     int scan[G::W];
     Plan plan;
     Division division[2];
-    int found_b, found_start;
+    int found_b, found_n, found_start;
     int err, err_b, any_bad;
 };
 
@@ -321,9 +322,9 @@ __global__ void __launch_bounds__(Geom<T, TQ, D>::THREADS, 1) paged_decode_kerne
     const bool few = a.B <= 32;  // every warp then looks at all requests by itself, a lane each: no barrier is needed
     const int per = few ? 1 : (a.B + THREADS - 1) / THREADS;
     const int b_lo = min((few ? lane : tid) * per, a.B), b_hi = min(b_lo + per, a.B);
-    int mine = 0;
+    int mine = 0, n_last = 0;
 #pragma unroll 1
-    for (int b = b_lo; b < b_hi; ++b) mine += units(length(b));
+    for (int b = b_lo; b < b_hi; ++b) mine += units(n_last = length(b));
     int upto = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -365,22 +366,24 @@ __global__ void __launch_bounds__(Geom<T, TQ, D>::THREADS, 1) paged_decode_kerne
     const bool work = plan.piece < plan.pieces && total > 0;
     const int q_lo = work ? plan.start(plan.piece) : 0;
     plan.q_hi = work ? plan.start(plan.piece + 1) : 0;
-    int found_b = 0, found_start = 0;
+    int found_b = 0, found_n = 0, found_start = 0;
     {
         const bool here = work && mine > 0 && q_lo >= upto - mine && q_lo < upto;
         if (few) {
             const unsigned who = __ballot_sync(0xffffffffu, here);
             found_b = who ? __ffs(who) - 1 : 0;
+            found_n = __shfl_sync(0xffffffffu, n_last, found_b);
             found_start = __shfl_sync(0xffffffffu, upto - mine, found_b);
         } else {
             if (here) {
-                int start = upto - mine, b = b_lo;
-                while (b + 1 < b_hi && q_lo >= start + units(length(b))) start += units(length(b++));
+                int start = upto - mine, b = b_lo, n = length(b);
+                while (b + 1 < b_hi && q_lo >= start + units(n)) start += units(n), n = length(++b);
                 sm.found_b = b;
+                sm.found_n = n;
                 sm.found_start = start;
             }
             __syncthreads();
-            if (work) found_b = sm.found_b, found_start = sm.found_start;
+            if (work) found_b = sm.found_b, found_n = sm.found_n, found_start = sm.found_start;
         }
     }
     const bool by_request = a.n_desc == a.B;  // descriptions are kept per request, or (more requests than CTAs) per piece
@@ -389,8 +392,9 @@ __global__ void __launch_bounds__(Geom<T, TQ, D>::THREADS, 1) paged_decode_kerne
         sm.plan = plan;
         Division& d = sm.division[1];
         d.q_at = q_lo;
-        d.b = found_b;
-        d.b_start = found_start;
+        d.next_b = found_b;
+        d.next_n = found_n;
+        d.next_start = found_start;
         d.t = d.end = 0;
         d.par = 1;
         d.opened_span = 0;
@@ -398,30 +402,31 @@ __global__ void __launch_bounds__(Geom<T, TQ, D>::THREADS, 1) paged_decode_kerne
     __syncthreads();
 
     // Prepares the next chunk into buffer `par`; false if the piece is done.  Called by all threads together, which
-    // meet at a barrier afterwards.
+    // meet at a barrier afterwards.  Which way they take follows from the division in shared memory alone: one thread
+    // reads a request's length, once (threads that read it for themselves would go apart, and read rows that nobody looked
+    // up, if another stream wrote it meanwhile).
     auto prepare = [&](int par) -> bool {
         const Plan& plan = sm.plan;
         Division d = sm.division[par ^ 1];
         bool fresh = false, from_start = false;
-        while (d.t >= d.end) {  // the next request that has rows here
-            if (d.q_at >= plan.q_hi) return false;
-            int n = length(d.b);
-            while (d.q_at >= d.b_start + units(n)) {
-                d.b_start += units(n);
-                if (++d.b >= a.B) return false;  // (only if the lengths change under the call)
-                n = length(d.b);
-            }
-            const int stop = d.b_start + units(n), rows_at = d.b_start + overhead(n), q_end = min(plan.q_hi, stop);
+        if (d.t >= d.end) {  // the next request that has rows here
+            if (d.q_at >= plan.q_hi || d.next_b >= a.B) return false;
+            const int n = d.next_n, stop = d.next_start + units(n), rows_at = d.next_start + overhead(n), q_end = min(plan.q_hi, stop);
+            if (d.q_at >= stop || q_end <= rows_at) return false;  // (the piece ends before the request's first row)
+            d.b = d.next_b;
             from_start = d.q_at <= rows_at;
             d.t = max(d.q_at - rows_at, 0) * kUnit;
-            d.end = q_end > rows_at ? min(n, (q_end - rows_at) * kUnit) : d.t;
+            d.end = min(n, (q_end - rows_at) * kUnit);
             d.single = from_start && q_end == stop;
             d.span_end = from_start && !d.single ? stop : 0;
             d.slot = plan.piece + d.b;
-            d.q_at = q_end;
+            d.q_at = d.next_start = q_end;
+            d.next_b = d.b + 1;
             fresh = true;
         }
         const int b = d.b, seg_t = d.t, seg_end = d.end, group = plan.group, groups = plan.groups;
+        const bool look = tid == 0 && fresh && d.q_at < plan.q_hi && d.next_b < a.B;  // (its round trip passes beside those below)
+        int next_n = look ? length(d.next_b) : 0;
         // pages of the rows that the chunk may have (how many it has follows from the number of clusters)
         const int32_t* table = a.pool.block_table + (size_t)b * a.pool.max_pages;
         const int reach = min(seg_end - seg_t, fresh ? G::CHUNK_ROWS : d.rows);
@@ -545,6 +550,10 @@ __global__ void __launch_bounds__(Geom<T, TQ, D>::THREADS, 1) paged_decode_kerne
             c.seg = d.par;
             d.first = 0;
             d.t += rows;
+            if (look) {
+                while (next_n == 0 && ++d.next_b < a.B) next_n = length(d.next_b);
+                d.next_n = next_n;
+            }
             sm.division[par] = d;
         }
         return true;
