@@ -131,11 +131,21 @@ struct AppendArgs {
     bool wide;  // the dense arrays start on 32-byte boundaries
 };
 
-// Tokens of request b and whether they fit; the same in every thread of every block of the request.
-__device__ __forceinline__ bool tokens_fit(const AppendArgs& a, int b, int* pos0, int* n) {
-    *pos0 = a.seq_lens[b];
-    *n = a.new_lens != nullptr ? min(max(a.new_lens[b], 0), a.N) : a.N;
-    return *pos0 >= 0 && (*n == 0 || *pos0 <= a.pool.capacity - *n);
+// Tokens of request b and whether they fit.  The lengths are read once a warp, or once a block where its threads meet at
+// barriers later: what goes one way together follows from one reading, whatever another stream writes meanwhile.
+__device__ __forceinline__ bool fits(const AppendArgs& a, int pos0, int n) { return pos0 >= 0 && (n == 0 || pos0 <= a.pool.capacity - n); }
+__device__ __forceinline__ bool tokens_fit_warp(const AppendArgs& a, int b, int* pos0, int* n) {
+    *pos0 = __shfl_sync(0xffffffffu, a.seq_lens[b], 0);
+    *n = a.new_lens != nullptr ? __shfl_sync(0xffffffffu, min(max(a.new_lens[b], 0), a.N), 0) : a.N;
+    return fits(a, *pos0, *n);
+}
+__device__ __forceinline__ bool tokens_fit_block(const AppendArgs& a, int b, int* pos0, int* n) {
+    __shared__ int2 s;
+    if (threadIdx.x == 0) s = make_int2(a.seq_lens[b], a.new_lens != nullptr ? min(max(a.new_lens[b], 0), a.N) : a.N);
+    __syncthreads();
+    *pos0 = s.x;
+    *n = s.y;
+    return fits(a, *pos0, *n);
 }
 
 // Stores the vector x of a row at `row` of plane `pl` (of the keys or the values) of a page; page -1: nothing.  The lanes
@@ -173,9 +183,7 @@ __global__ void __launch_bounds__(kStepThreads) append_step_kernel(const AppendA
     constexpr int LPR = D * (int)sizeof(TS) / Dense<FP8>::BYTES, EPV = Dense<FP8>::BYTES / (int)sizeof(TS);
     const int b = blockIdx.y, tid = threadIdx.x;
     int pos0, n;
-    const bool fit = tokens_fit(a, b, &pos0, &n);
-    __syncthreads();  // every thread holds the position before thread 0 may advance it
-    if (!fit) {
+    if (!tokens_fit_block(a, b, &pos0, &n)) {
         if (tid == 0) flag_status(a.hdr, CHAI_ERR_CACHE_FULL, b);
         return;
     }
@@ -228,7 +236,7 @@ __global__ void __launch_bounds__(kRowThreads) append_rows_kernel(const AppendAr
     const int plane = blockIdx.y, b = blockIdx.z, x = threadIdx.x % LPR;
     const int t0 = blockIdx.x * (ROWS * kRowUnroll) + threadIdx.x / LPR;
     int pos0, n;
-    if (!tokens_fit(a, b, &pos0, &n)) {
+    if (!tokens_fit_warp(a, b, &pos0, &n)) {
         if (threadIdx.x == 0 && blockIdx.x == 0 && plane == 0) flag_status(a.hdr, CHAI_ERR_CACHE_FULL, b);
         return;
     }
@@ -274,7 +282,7 @@ __global__ void __launch_bounds__(128) advance_paged_kernel(const AppendArgs a) 
     dependent_grid_sync();
     const int b = blockIdx.x;
     int pos0, n;
-    if (!tokens_fit(a, b, &pos0, &n) || n == 0) return;
+    if (!tokens_fit_block(a, b, &pos0, &n) || n == 0) return;
     const int32_t* table = a.pool.block_table + (size_t)b * a.pool.max_pages;
     const unsigned last = a.pool.by_page.div((unsigned)(pos0 + n - 1));
     bool bad = false;

@@ -4,9 +4,9 @@ import numpy as np
 import pytest
 import torch
 
-from paged_cases import tables
+from paged_cases import partition, tables
 from paper_2403_08058_b200 import chai
-from test_gpu_paged import DEV, decode, make
+from test_gpu_paged import DEV, decode, make, random_pool
 
 pytestmark = pytest.mark.gpu
 
@@ -45,3 +45,46 @@ def test_decode_ends_and_stays_in_bounds_while_another_stream_writes_the_lengths
     for _ in range(2):
         assert torch.equal(decode(c, workspace=ws).view(torch.uint8), want.view(torch.uint8))
         assert chai.chai_device_status(ws) == chai.CHAI_OK
+
+
+@pytest.mark.parametrize("N", [1, 40])
+@pytest.mark.parametrize("fp8", [False, True])
+def test_append_ends_and_stays_in_bounds_while_another_stream_writes_the_lengths(fp8, N):
+    """Tokens may go to any row that the tables name, and to no other page; the next call is right."""
+    B, H, k, D, page = 40, 8, 3, 64, 8
+    rng = np.random.default_rng(N)
+    table_np, n_pages = tables([100] * B, page, N, extra_pages=30, room=N)
+    table, top = torch.from_numpy(table_np).to(DEV), table_np.shape[1] * page
+    _, reps = partition(B, H, k, N)
+    reps = torch.from_numpy(reps).to(DEV)
+    dt = torch.uint8 if fp8 else torch.bfloat16
+    k_new, v_new = (torch.randn(B, H, N, D, device=DEV).to(torch.bfloat16) for _ in range(2))
+    pages = [random_pool(n_pages, p, page, D, dt, p) for p in (k, H)]
+    pages += [torch.rand(n_pages, p, page, device=DEV) for p in (k, H)] if fp8 else []
+    before = [x.clone() for x in pages]
+    put = chai.chai_append_kv_paged_fp8 if fp8 else chai.chai_append_kv_paged
+    seq, count = torch.full((B,), 20, dtype=torch.int32, device=DEV), torch.full((B,), N, dtype=torch.int32, device=DEV)
+    other = [torch.from_numpy(rng.integers(-5, top + 3, B).astype(np.int32)).to(DEV) for _ in range(5)] + [torch.full_like(seq, 1 << 30)]
+    some = [torch.from_numpy(rng.integers(-3, N + 3, B).astype(np.int32)).to(DEV) for _ in range(5)]
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for i in range(100):
+        with torch.cuda.stream(side):
+            for j in range(3):
+                seq.copy_(other[(3 * i + j) % len(other)])
+                count.copy_(some[(3 * i + j) % len(some)])
+        put(k_new, v_new, *pages, reps, table, seq, new_lens=count)
+    torch.cuda.synchronize()
+    unnamed = torch.ones(n_pages, dtype=torch.bool)
+    unnamed[torch.from_numpy(table_np.ravel().astype(np.int64))] = False
+    assert unnamed.sum() == 30
+    for x, old in zip(pages, before):
+        assert torch.equal(x[unnamed.to(DEV)].view(torch.uint8), old[unnamed.to(DEV)].view(torch.uint8))
+    seq.fill_(20)
+    for x, old in zip(pages, before):
+        x.copy_(old)
+    put(k_new, v_new, *pages, reps, table, seq)
+    assert seq.tolist() == [20 + N] * B
+    if not fp8:
+        for b in (0, B - 1):
+            assert torch.equal(pages[1][table[b, 20 // page].long(), :, 20 % page], v_new[b, :, 0])
