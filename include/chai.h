@@ -431,7 +431,8 @@ int chai_read_kv_paged_fp8(const void* k_pages, const void* v_pages, const float
  * the rows t < seq_lens[b] (clamped to [0, max_pages*page_size]; they include the current token).
  *   q, out [B,H,D] of type dtype, which is the pages' type too; _fp8: CHAI_F32 or CHAI_BF16, e4m3 pages.
  * A request of length 0 gets zero rows, and so does a request one of whose pages is bad (CHAI_ERR_BAD_PAGE) and a head
- * whose membership cannot be resolved (CHAI_ERR_BAD_MEMBERSHIP).  Rows at or beyond a request's length are never used,
+ * whose membership cannot be resolved (CHAI_ERR_BAD_MEMBERSHIP).  A head whose scores are all -inf gets a zero row too, as
+ * in chai_decode_attention; a NaN among its scores makes it NaN.  Rows at or beyond a request's length are never used,
  * whatever they hold.  q and out must not overlap.  Sums and softmax statistics are fp32, taken in an order that follows
  * from the lengths and memberships: results are bitwise repeatable.  _fp8: probabilities times row scales are held to 2^-22
  * of the head's largest row scale (a row of zeros has the scale 1).  The workspace (chai_decode_paged_workspace_bytes:

@@ -884,9 +884,10 @@ __global__ void __launch_bounds__(Geom<T, TQ, D>::THREADS, 1) paged_decode_kerne
                 }
                 if (c.last && c.single) {
                     const float sum = sm.sum[cl];
+                    const bool zero = bad_so_far || sum == 0.f;  // (no score above -inf: nothing is left of the row)
                     TQ* dst = static_cast<TQ*>(a.out) + ((size_t)c.b * a.H + h) * D + G::col(lane);
 #pragma unroll
-                    for (int e = 0; e < G::VPL; ++e) dst[e] = from_float<TQ>(bad_so_far ? 0.f : acc[e] / sum);
+                    for (int e = 0; e < G::VPL; ++e) dst[e] = from_float<TQ>(zero ? 0.f : acc[e] / sum);
                 } else {
 #pragma unroll
                     for (int e = 0; e < G::VPL; e += 4)
@@ -1193,7 +1194,7 @@ __global__ void __launch_bounds__(THREADS) paged_join_kernel(const DecodeArgs a,
                 l += s_sum[w];
                 x += s_o[w][tid];
             }
-            static_cast<TQ*>(a.out)[((size_t)b * a.H + h) * D + tid] = from_float<TQ>(zero ? 0.f : x / l);
+            static_cast<TQ*>(a.out)[((size_t)b * a.H + h) * D + tid] = from_float<TQ>(zero || l == 0.f ? 0.f : x / l);
         }
         __syncthreads();  // s_* are free for the next description
     }

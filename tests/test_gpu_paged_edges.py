@@ -6,7 +6,7 @@ import torch
 
 from paged_cases import partition, tables
 from paper_2403_08058_b200 import chai
-from test_gpu_paged import DEV, decode, make, random_pool
+from test_gpu_paged import DEV, KINDS, decode, make, random_pool
 
 pytestmark = pytest.mark.gpu
 
@@ -88,3 +88,45 @@ def test_append_ends_and_stays_in_bounds_while_another_stream_writes_the_lengths
     if not fp8:
         for b in (0, B - 1):
             assert torch.equal(pages[1][table[b, 20 // page].long(), :, 20 % page], v_new[b, :, 0])
+
+
+# ---- softmax rows that nothing is left of ------------------------------------------------------------------------
+
+@pytest.mark.parametrize("cache,io", KINDS)
+@pytest.mark.parametrize("lens", [[1], [900, 1, 30], [2500], [7] * 200], ids=["one token", "joined and whole", "chunks", "many"])
+def test_decode_a_cluster_whose_scores_are_all_minus_infinity_is_zero(cache, io, lens):
+    """Keys of -inf along a positive query in every row of cluster 0 (e4m3: -1 with an infinite scale); one request in one
+    piece and requests that are joined.  The other clusters keep their results bit for bit."""
+    B, H, k, page = len(lens), 6, 2, 16
+    c = make(cache, io, B, H, k, 64, page, lens, seed=101)
+    c["q"].abs_().add_(0.125)
+    ws = status_workspace(c)
+    want = decode(c, workspace=ws).clone()
+    assert torch.isfinite(want).all()
+    if cache == "e4m3":
+        c["k_pages"][:, 0] = 0xB8                  # -1
+        c["k_scales"][:, 0] = float("inf")
+    else:
+        c["k_pages"][:, 0] = float("-inf")
+    got = decode(c, workspace=ws)
+    assert chai.chai_device_status(ws) == chai.CHAI_OK
+    mine = (c["membership"] == 0)
+    assert not got[mine].any() and not torch.isnan(got[mine]).any()
+    assert torch.equal(got[~mine], want[~mine])
+    # a row that is left counts alone; one that is NaN is not hidden
+    last = lens[0] - 1
+    at = (int(c["table_np"][0, last // page]), 0, last % page)
+    if cache == "e4m3":
+        c["k_pages"][at], c["k_scales"][at] = 0x30, 1.0
+    else:
+        c["k_pages"][at] = 0.5
+    row = c["v_rows"][0][:, last]
+    got = decode(c, workspace=ws)
+    first = [h for h in range(H) if c["mem"][0, h] == 0]
+    assert np.array_equal(got[0, first].double().cpu().numpy(), row[first])     # p = 1, values of the output's type
+    if cache == "e4m3":
+        c["k_scales"][at] = float("nan")
+    else:
+        c["k_pages"][at] = float("nan")
+    got = decode(c, workspace=ws)
+    assert torch.isnan(got[0, first]).all()
