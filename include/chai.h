@@ -434,10 +434,12 @@ int chai_read_kv_paged_fp8(const void* k_pages, const void* v_pages, const float
  * whose membership cannot be resolved (CHAI_ERR_BAD_MEMBERSHIP).  A head whose scores are all -inf gets a zero row too, as
  * in chai_decode_attention; a NaN among its scores makes it NaN.  Rows at or beyond a request's length are never used,
  * whatever they hold.  q and out must not overlap.  Sums and softmax statistics are fp32, taken in an order that follows
- * from the lengths and memberships: results are bitwise repeatable.  _fp8: probabilities times row scales are held to 2^-22
- * of the head's largest row scale (a row of zeros has the scale 1).  The workspace (chai_decode_paged_workspace_bytes:
- * 64 KiB and (160 + B) * H * (D + 8) 32-bit words, whatever the lengths) needs no clearing; calls that share one must be
- * ordered on one stream.
+ * from the lengths and memberships: results are bitwise repeatable.  _fp8: the tensor
+ * cores take the queries, and probabilities times row scales, as two fp16 numbers each: an element of a query is held to
+ * 2^-22 of itself or 2^-36 of the largest of its row, such a product to 2^-22 of itself or 2^-43 of the largest of its head,
+ * whichever is more (a row of zeros has the scale 1).  The workspace (chai_decode_paged_workspace_bytes: 64 KiB and
+ * (160 + B) * H * (D + 8) 32-bit words, whatever the lengths) needs no clearing; calls that share one must be ordered on one
+ * stream.
  * H is at most 1024, B below 65536, B * max_pages * page_size below 2^33.
  */
 size_t chai_decode_paged_workspace_bytes(int B, int H, int D);

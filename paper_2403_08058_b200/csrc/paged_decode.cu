@@ -45,7 +45,10 @@ constexpr int kUnit = 16;         // rows; the line of all rows is divided in un
 // with 16 rows, 13.9 with 32).
 __device__ __forceinline__ int overhead(int n) { return min(4, max(2, n >> 7)); }
 __device__ __forceinline__ int units(int n) { return n > 0 ? (n + kUnit - 1) / kUnit + overhead(n) : 0; }
-constexpr float kProbScale = 16384.f;  // e4m3: probabilities are kept times 2^14 (see phase V)
+// e4m3: x as two fp16 numbers, h = fp16(x) and fp16(2^11 (x - h)).  2^11 keeps the second as large as the first: where both
+// are normal numbers they hold x to 2^-22, and the error never exceeds 2^-36 (2^-25 if it were stored as it is).
+constexpr float kLow = 2048.f;
+constexpr float kProductFactor = 524288.f;  // brings products of 2^-12 ... 2^-4, as cached activations have, to 2^7 ... 2^15
 
 template <typename T, typename TQ, int D>
 struct Geom {
@@ -242,6 +245,11 @@ __device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
     asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
     return d;
 }
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+    uint64_t d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
 // four e4m3 numbers as two pairs of fp16 (exact): the low two bytes and the high two
 __device__ __forceinline__ void e4m3_halves(uint32_t w, uint32_t* lo, uint32_t* hi) {
     asm("{\n\t.reg .b16 x, y;\n\tmov.b32 {x, y}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, x;\n\tcvt.rn.f16x2.e4m3x2 %1, y;\n\t}"
@@ -260,12 +268,24 @@ __device__ __forceinline__ void mma16816(float* c, uint32_t a0, uint32_t a1, uin
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-// A power of two f with |x| f in [1, 2) and its inverse; 1 where x is 0, tiny, infinite or NaN.
+// The parts of two numbers times f, a power of two
+__device__ __forceinline__ void two_halves(uint64_t x, float f, uint32_t* hi, uint32_t* lo) {
+    const float2 y = unpack2(mul2(x, pack2(f, f)));
+    *hi = half_pair(y.x, y.y);
+    const float2 h = half_floats(*hi);
+    const float2 rest = unpack2(fma2(pack2(h.x, h.y), pack2(-kLow, -kLow), mul2(pack2(y.x, y.y), pack2(kLow, kLow))));  // (exact)
+    *lo = half_pair(rest.x, rest.y);
+}
+// A power of two f with |x| f in [1, 2) and its inverse; below 1 where x is subnormal or 0; 1 where x is infinite or NaN.
 __device__ __forceinline__ void normaliser(float x, float* f, float* inv) {
-    const unsigned e = (__float_as_uint(x) >> 23) & 0xffu;
-    const bool plain = e >= 1 && e <= 253;
-    *f = plain ? __uint_as_float((254u - e) << 23) : 1.f;
-    *inv = plain ? __uint_as_float(e << 23) : 1.f;
+    const unsigned e = max((__float_as_uint(x) >> 23) & 0xffu, 1u);
+    *f = e == 254u ? __uint_as_float(1u << 22) : __uint_as_float((e == 255u ? 127u : 254u - e) << 23);  // (2^-127 is subnormal)
+    *inv = __uint_as_float((e == 255u ? 127u : e) << 23);
+}
+// A power of two f with x f in [2^10, 2^11), for x of 2^-117 and more (below: f = 2^127); 1 where x is infinite.  1 / f is exact.
+__device__ __forceinline__ float product_factor(float x) {
+    const unsigned e = max((__float_as_uint(x) >> 23) & 0xffu, 10u);
+    return __uint_as_float((e == 255u ? 127u : 264u - e) << 23);
 }
 
 // ---- the main kernel --------------------------------------------------------------------------------------------
@@ -702,7 +722,7 @@ __global__ void __launch_bounds__(Geom<T, TQ, D>::THREADS, 1) paged_decode_kerne
             float factor = 1.f;
             constexpr int QN = G::FP8 ? 1 : 16 / (int)sizeof(T);
             [[maybe_unused]] uint64_t qf[QN / 2 + 1];
-            [[maybe_unused]] uint32_t qb[G::FP8 ? D / 8 : 1];  // e4m3: fp16 fragments, column 0 the leading and column 1 the trailing half
+            [[maybe_unused]] uint32_t qb[G::FP8 ? D / 8 : 1];  // e4m3: fp16 fragments, column 0 the leading and column 1 the trailing part
 #pragma unroll 1
             for (;; w.step(chunk_tiles)) {
                 fill();
@@ -736,10 +756,8 @@ __global__ void __launch_bounds__(Geom<T, TQ, D>::THREADS, 1) paged_decode_kerne
                         factor = a.scale_log2 * inv;
 #pragma unroll
                         for (int i = 0; i < 8 * J; ++i) {
-                            const float u = x[2 * i] * f, v = x[2 * i + 1] * f;
-                            const uint32_t hi = half_pair(u, v);
-                            const float2 h = half_floats(hi);
-                            const uint32_t lo = half_pair(u - h.x, v - h.y);
+                            uint32_t hi, lo;
+                            two_halves(pack2(x[2 * i], x[2 * i + 1]), f, &hi, &lo);
                             qb[i] = lane < 4 ? hi : (lane < 8 ? lo : 0u);
                         }
                     }
@@ -787,7 +805,7 @@ __global__ void __launch_bounds__(Geom<T, TQ, D>::THREADS, 1) paged_decode_kerne
                     for (int i = 0; i < LEFT; ++i)
                         if (lane % SAME == 0) score[row + i] = s[i];  // (rows behind the last get scores that nothing reads)
                 } else {
-                    // 16 keys are the rows of A, 16 columns of them a step; B holds the query (leading and trailing half)
+                    // 16 keys are the rows of A, 16 columns of them a step; B holds the query (leading and trailing part)
                     const int g = lane >> 2, t = lane & 3;
                     const float* scales = reinterpret_cast<const float*>(tile + G::DATA) + g;
                     // rows 16 m + g and 16 m + g + 8, pieces t + 4 j (see Geom; the lane's share taken out)
@@ -812,8 +830,8 @@ __global__ void __launch_bounds__(Geom<T, TQ, D>::THREADS, 1) paged_decode_kerne
                         // (rows behind the last get scores that nothing reads)
                         const float ks = scales[16 * m], ks8 = scales[16 * m + 8];
                         if (t == 0) {
-                            score[16 * m + g] = (acc[0] + acc[1]) * (ks * factor);
-                            score[16 * m + g + 8] = (acc[2] + acc[3]) * (ks8 * factor);
+                            score[16 * m + g] = fmaf(acc[1], 1.f / kLow, acc[0]) * (ks * factor);
+                            score[16 * m + g + 8] = fmaf(acc[3], 1.f / kLow, acc[2]) * (ks8 * factor);
                         }
                     }
                 }
@@ -836,7 +854,7 @@ __global__ void __launch_bounds__(Geom<T, TQ, D>::THREADS, 1) paged_decode_kerne
 #pragma unroll 4
             for (int r = lane; r < chunk_rows; r += 32) {
                 const float p = exp2_approx(score[r] - ref);
-                score[r] = G::FP8 ? p * kProbScale : p;
+                score[r] = p;
                 sum += p;
             }
             const int r0 = chunk_rows + lane;
@@ -862,7 +880,7 @@ __global__ void __launch_bounds__(Geom<T, TQ, D>::THREADS, 1) paged_decode_kerne
         float acc[G::VPL];
 #pragma unroll
         for (int e = 0; e < G::VPL; ++e) acc[e] = 0.f;
-        // e4m3: sums on the tensor cores, of products that are kProbScale * factor too large
+        // e4m3: sums on the tensor cores, of products that are `factor` too large
         constexpr int PARTS = G::FP8 ? D / 16 : 1;
         [[maybe_unused]] float part[PARTS][4];
         [[maybe_unused]] float factor = 1.f;
@@ -943,54 +961,53 @@ __global__ void __launch_bounds__(Geom<T, TQ, D>::THREADS, 1) paged_decode_kerne
                         acc[2 * e + 1] = x.y;
                     }
                 } else {
-                    // 16 columns are the rows of A, 16 cache rows a step; B holds the probabilities
-                    // times the rows' scales, as two fp16 numbers each, the leading and the trailing half.  They are good
-                    // to 2^-25 then: with probabilities kept times 2^14 and the largest scale of a head's first rows
-                    // between 2^-16 and 2 that is at most 2^-22 of the largest product.  Other scales, and larger ones
-                    // later, are brought there by a power of two.
+                    // 16 columns are the rows of A, 16 cache rows a step; B holds the probabilities times the rows' scales, as
+                    // two fp16 numbers each, times a power of two that brings the largest product of a head's first tile to
+                    // 2^7 ... 2^15.  Where a later one passes 2^15 the sums so far are brought to a new one.  So every
+                    // product is held to 2^-22 of itself or 2^-43 of the head's largest, whichever is more.  (By the largest
+                    // scale instead of the largest product, and with the second number stored as it is, rows whose scale is
+                    // large and whose probability is not took the others' bits.  This way costs 0.3 to 0.6 %: 7B shape 54.1
+                    // -> 54.3 us, 66B shape 28.8 -> 29.0; with a power found anew for every head, 54.4 and 29.5.)
                     const int g = lane >> 2, t = lane & 3;
                     const float4* scales = reinterpret_cast<const float4*>(tile + G::DATA + 16 * t);
                     const bool both = chunk_rows - row0 > 16;  // the tile has rows for both steps
-                    float4 vs[G::STEPS];
+                    uint64_t x[G::STEPS][2];
                     float top = 0.f;
 #pragma unroll
                     for (int s = 0; s < G::STEPS; ++s) {
-                        vs[s] = s == 0 || both ? scales[4 * s] : make_float4(0.f, 0.f, 0.f, 0.f);
-                        top = fmaxf(top, fmaxf(fmaxf(fabsf(vs[s].x), fabsf(vs[s].y)), fmaxf(fabsf(vs[s].z), fabsf(vs[s].w))));
+                        const float4 vs = s == 0 || both ? scales[4 * s] : make_float4(0.f, 0.f, 0.f, 0.f);
+                        const float4 pr = *reinterpret_cast<const float4*>(prob + 16 * s + 4 * t);  // (zeros behind the last row)
+                        x[s][0] = mul2(pack2(pr.x, pr.y), pack2(vs.x, vs.y));
+                        x[s][1] = mul2(pack2(pr.z, pr.w), pack2(vs.z, vs.w));
+                        const float2 u = unpack2(x[s][0]), v = unpack2(x[s][1]);
+                        top = fmaxf(top, fmaxf(fmaxf(fabsf(u.x), fabsf(u.y)), fmaxf(fabsf(v.x), fabsf(v.y))));
                     }
                     if (begins) {
-                        factor = 1.f;
+                        factor = kProductFactor;
 #pragma unroll
                         for (int i = 0; i < PARTS; ++i) part[i][0] = part[i][1] = part[i][2] = part[i][3] = 0.f;
                     }
-                    const unsigned high = __ballot_sync(0xffffffffu, top * factor > 2.f);
-                    const unsigned low = __ballot_sync(0xffffffffu, begins && top < 1.f / 65536);
+                    const unsigned high = __ballot_sync(0xffffffffu, top * factor > 32768.f);
+                    const unsigned low = __ballot_sync(0xffffffffu, begins && top * factor < 128.f);
                     if (high != 0 || low == 0xffffffffu) {
                         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
                         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
                         const float old = factor;
-                        float inverse;
-                        normaliser(top, &factor, &inverse);
+                        factor = product_factor(top);
                         const float change = factor / old;
 #pragma unroll
                         for (int i = 0; i < PARTS; ++i)
 #pragma unroll
                             for (int e = 0; e < 4; ++e) part[i][e] *= change;
                     }
-                    if (factor != 1.f) {  // (the same in every lane, as the maximum is)
-#pragma unroll
-                        for (int s = 0; s < G::STEPS; ++s) vs[s] = make_float4(vs[s].x * factor, vs[s].y * factor, vs[s].z * factor, vs[s].w * factor);
-                    }
                     constexpr int WORDS = D / 32;  // 32-bit words a lane holds of a row
                     const int lane_at = 4 * t * G::ROW + (D == 128 ? 16 * (g ^ (2 * t)) : (16 * ((g >> 1) ^ (2 * t)) + 8 * (g & 1)));
 #pragma unroll
                     for (int s = 0; s < G::STEPS; ++s) {
                         if (s == 1 && !both) break;
-                        const float4 pr = *reinterpret_cast<const float4*>(prob + 16 * s + 4 * t);
-                        const float x0 = pr.x * vs[s].x, x1 = pr.y * vs[s].y, x2 = pr.z * vs[s].z, x3 = pr.w * vs[s].w;
-                        const uint32_t h0 = half_pair(x0, x1), h1 = half_pair(x2, x3);
-                        const float2 y0 = half_floats(h0), y1 = half_floats(h1);
-                        const uint32_t l0 = half_pair(x0 - y0.x, x1 - y0.y), l1 = half_pair(x2 - y1.x, x3 - y1.y);
+                        uint32_t h0, h1, l0, l1;
+                        two_halves(x[s][0], factor, &h0, &l0);
+                        two_halves(x[s][1], factor, &h1, &l1);
                         const uint32_t b0 = g == 0 ? h0 : (g == 1 ? l0 : 0u), b1 = g == 0 ? h1 : (g == 1 ? l1 : 0u);
                         uint32_t v[4][WORDS];
 #pragma unroll
@@ -1026,11 +1043,11 @@ __global__ void __launch_bounds__(Geom<T, TQ, D>::THREADS, 1) paged_decode_kerne
                 begins = ends;
                 if (!ends && w.left > 0) continue;
                 if constexpr (G::FP8) {
-                    const float f = (1.f / kProbScale) / factor;
+                    const float f = 1.f / factor;
 #pragma unroll
                     for (int i = 0; i < PARTS; ++i) {
-                        acc[2 * i] = (part[i][0] + part[i][1]) * f;
-                        acc[2 * i + 1] = (part[i][2] + part[i][3]) * f;
+                        acc[2 * i] = fmaf(part[i][1], 1.f / kLow, part[i][0]) * f;
+                        acc[2 * i + 1] = fmaf(part[i][3], 1.f / kLow, part[i][2]) * f;
                     }
                 } else {
 #pragma unroll

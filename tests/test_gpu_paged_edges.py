@@ -4,7 +4,8 @@ import numpy as np
 import pytest
 import torch
 
-from paged_cases import partition, tables
+from oracle import chai_oracle as orc
+from paged_cases import bits, partition, tables
 from paper_2403_08058_b200 import chai
 from test_gpu_paged import DEV, KINDS, decode, make, random_pool
 
@@ -130,3 +131,157 @@ def test_decode_a_cluster_whose_scores_are_all_minus_infinity_is_zero(cache, io,
         c["k_pages"][at] = float("nan")
     got = decode(c, workspace=ws)
     assert torch.isnan(got[0, first]).all()
+
+
+# ---- e4m3 rows with scales of every size -------------------------------------------------------------------------
+
+U = 2.0 ** -24
+
+
+def scaled_case(io, D, n, seed, scales, H=4, k=2, B=1, values=None, spread=1.0):
+    """Requests of n tokens whose value rows have the given scales (scales(rng, n) -> [n] exponents) and full mantissas."""
+    c = make("e4m3", io, B, H, k, D, 16, [n] * B, seed=seed, peaked=spread)
+    rng = np.random.default_rng(seed)
+    for b in range(B):
+        s8 = np.exp2(np.asarray(scales(rng, n), dtype=np.float64))
+        codes = rng.integers(1, 0x7F, (H, n, D)) | (rng.integers(0, 2, (H, n, D)) << 7)
+        if values is not None:
+            codes, s8 = values(rng, codes, s8)
+        at = (torch.from_numpy(c["table_np"][b, np.arange(n) // 16].astype(np.int64)), torch.arange(n) % 16)
+        c["v_pages"][at[0], :, at[1]] = torch.from_numpy(codes.astype(np.uint8)).transpose(0, 1).to(DEV)
+        c["v_scales"][at[0], :, at[1]] = torch.from_numpy(s8.astype(np.float32))[:, None].expand(-1, H).to(DEV)
+        c["v_rows"][b] = orc.e4m3_values()[codes] * s8[:, None]
+        c.setdefault("v_codes", {})[b] = orc.e4m3_values()[codes]
+        c.setdefault("v_size", {})[b] = s8
+    return c
+
+
+def check_tightly(c, what):
+    """Bounds for n rows that leave no room for a floor set by the largest scale.
+
+    Scores: fp32 sums of D products on the tensor cores, 4 u a term (u = 2^-24) of S = scale * sum|q k|; a query element is
+    held to 2^-22 of itself or 2^-36 of the largest of its row.  Probabilities: twice the score's error (numerator
+    and sum), and 2 |s| + 8 units u for an exponential and its argument, of which a row meets three (its own, from chunk
+    to chunk, from piece to piece).  Probability times row scale: 2^-22 of
+    itself, or 2^-43 of the largest such product of the head; sums over n rows 4 u a term.  The result is rounded once."""
+    got = decode(c).double().cpu().numpy()
+    D, scale = c["D"], c["scale"]
+    for b, n in enumerate(c["lens"]):
+        q, kr, vr = c["q_np"][b][c["reps"][b]], c["k_rows"][b], c["v_rows"][b]
+        s = scale * np.einsum("cd,ctd->ct", q, kr)
+        top = s.max(1, keepdims=True)
+        p = np.exp(s - top)
+        total = p.sum(1)
+        size = scale * np.einsum("cd,ctd->ct", np.abs(q), np.abs(kr)).max(1)
+        low = scale * np.abs(q).max(1) * np.abs(kr).sum(2).max(1)
+        ds = (4 * (D + 4) * U + 2.0 ** -22) * size + 2.0 ** -36 * low
+        rel = 2 * (ds + (6 * np.abs(s).max(1) + 24) * U) + (2 * n + 16) * 4 * U + 2.0 ** -22
+        for h in range(c["H"]):
+            cl = c["mem"][b, h]
+            w = p[cl] / total[cl]
+            ref = w @ vr[h]
+            product = (w * c["v_size"][b]).max()
+            allowed = rel[cl] * (w @ np.abs(vr[h])) + 2.0 ** -43 * product * np.abs(c["v_codes"][b][h]).sum(0) + n * 2.0 ** -140
+            allowed = allowed + {"f32": 2.0 ** -24, "bf16": 2.0 ** -8}[c["io"]] * (np.abs(ref) + allowed)
+            err = np.abs(got[b, h] - ref)
+            assert (err <= allowed).all(), f"{what}: head {h}: {(err / allowed).max():.3g} of what is allowed"
+
+
+SCALES = {
+    "all tiny": lambda r, n: r.integers(-30, -17, n),
+    "all large": lambda r, n: r.integers(2, 30, n),
+    "rising through the head": lambda r, n: np.linspace(-28, 9, n).astype(int),
+    "falling through the head": lambda r, n: np.linspace(9, -28, n).astype(int),
+    "one much larger row late": lambda r, n: np.where(np.arange(n) == n - 3, 24, r.integers(-8, -4, n)),
+    "smallest scales": lambda r, n: r.integers(-112, -108, n),
+    "largest scales": lambda r, n: r.integers(100, 110, n),
+    "smallest, then largest": lambda r, n: np.where(np.arange(n) < n // 2, -120, 100),
+    "ends of the range in turn": lambda r, n: np.where(np.arange(n) % 37 < 20, -100, 60),
+}
+
+
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("kind", list(SCALES))
+@pytest.mark.parametrize("n,B", [(1, 1), (31, 1), (190, 1), (75, 160)], ids=["a token", "a tile", "pieces", "many requests"])
+def test_decode_row_scales_of_every_size(io, D, kind, n, B):
+    """Scales that start below 2^-16, pass 2 in the middle of a head, fall, and lie at the ends of the range; heads shared
+    by warps (n = 75 in one piece of many requests), pieces that are joined, several chunks (below)."""
+    check_tightly(scaled_case(io, D, n, 7 + n, SCALES[kind], B=B), f"{kind}, n {n}")
+
+
+@pytest.mark.parametrize("kind", list(SCALES))
+def test_decode_row_scales_in_several_chunks(kind):
+    """150 requests of 600 tokens: a piece holds more than a chunk of 512, and sums go on from chunk to chunk."""
+    check_tightly(scaled_case("f32", 64, 600, 3, SCALES[kind], B=150, H=2, k=1), kind)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("size", [-22, -25, -28])
+def test_decode_a_row_of_zeros_among_small_ones(D, size):
+    """Such a row's scale is 1, whatever the others' (values of about 1e-4, 1e-5 and 1e-6 here)."""
+    def values(rng, codes, s8):
+        codes[:, 5] = 0
+        s8[5] = 1.0
+        return codes, s8
+    check_tightly(scaled_case("f32", D, 45, 12, lambda r, n: np.full(n, size), values=values, spread=2.0 ** -6), f"2^{size}")
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_decode_a_large_row_that_the_softmax_leaves_out(D):
+    """A row 2^30 larger than the others whose probability is below 2^-45 of theirs."""
+    c = scaled_case("f32", D, 45, 13, lambda r, n: np.where(np.arange(n) == 9, 30, -4))
+    key = -np.sign(c["q_np"][0][c["reps"][0]])                       # [k, D]: far below every other score
+    q8, s8 = orc.quantize_rows_fp8(key)
+    strength = 2.0 ** np.ceil(np.log2(40.0 / (c["scale"] * np.abs(c["q_np"][0][c["reps"][0]]).sum(1).min())))
+    page, row = int(c["table_np"][0, 0]), 9
+    c["k_pages"][page, :, row] = torch.from_numpy(q8).to(DEV)
+    c["k_scales"][page, :, row] = torch.from_numpy((s8 * strength).astype(np.float32)).to(DEV)
+    c["k_rows"][0][:, 9] = key * strength
+    s = c["scale"] * np.einsum("cd,ctd->ct", c["q_np"][0][c["reps"][0]], c["k_rows"][0])
+    assert (s[:, 9] < s.max(1) - 32).all()
+    check_tightly(c, "a large row left out")
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_decode_a_token_above_the_others_with_small_values(D):
+    """A first token whose score lies 12 above the others' and whose values are near zero."""
+    c = scaled_case("f32", D, 45, 14, lambda r, n: np.where(np.arange(n) == 0, -30, -15), spread=0.1)
+    q = c["q_np"][0][c["reps"][0]]
+    key = np.sign(q) * 2.0 ** np.round(np.log2(12.0 / (c["scale"] * np.abs(q).sum(1))))[:, None]
+    q8, s8 = orc.quantize_rows_fp8(key)
+    page = int(c["table_np"][0, 0])
+    c["k_pages"][page, :, 0] = torch.from_numpy(q8).to(DEV)
+    c["k_scales"][page, :, 0] = torch.from_numpy(s8.astype(np.float32)).to(DEV)
+    c["k_rows"][0][:, 0] = key
+    check_tightly(c, "a token above the others")
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("exponent", [128, -130, -140])
+def test_decode_queries_at_the_ends_of_the_range(D, exponent):
+    """Queries near 2^128 and subnormal ones, with a scale that makes their scores ordinary."""
+    c = scaled_case("f32", D, 45, 15, lambda r, n: np.full(n, -4))
+    rng = np.random.default_rng(15)
+    # whole numbers of nine bits: exact at every exponent here
+    q = rng.integers(-511, 512, c["q_np"].shape) * 2.0 ** -9 * 2.0 ** (exponent if exponent > 0 else exponent + 9)
+    c["q_np"] = q.astype(np.float32).astype(np.float64)
+    c["q"] = torch.from_numpy(q.astype(np.float32)).to(DEV)
+    c["scale"] = 2.0 ** -126 if exponent > 0 else 2.0 ** (-exponent - 14)
+    if exponent > 0:                                   # (the least scale that is a normal number)
+        c["k_scales"] *= 2.0 ** -8
+        c["k_rows"][0] = c["k_rows"][0] * 2.0 ** -8
+    check_tightly(c, f"2^{exponent}")
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_decode_a_query_with_one_large_element(D):
+    """Keys are zero where the query is large: the scores come from elements 2^-20 of its size."""
+    c = scaled_case("f32", D, 45, 16, lambda r, n: np.full(n, -4))
+    c["q_np"] = (c["q_np"] * 2.0 ** -20).astype(np.float32).astype(np.float64)
+    c["q_np"][..., 3] = 1.0
+    c["q"] = torch.from_numpy(c["q_np"].astype(np.float32)).to(DEV)
+    c["k_pages"][..., 3] = 0
+    c["k_rows"][0][..., 3] = 0.0
+    c["scale"] = 2.0 ** 19 / np.sqrt(D)
+    check_tightly(c, "one large element")
