@@ -397,7 +397,9 @@ int chai_decode_attention_fp8(const void* q, const void* k_rep, const void* v, c
  * _fp8: k_new / v_new of type dtype become e4m3 rows: scale = 2^e with the smallest e >= -126 for which the row's
  *   largest finite magnitude is at most 448 * 2^e (1 if that magnitude is 0), byte = x / scale rounded to the nearest
  *   e4m3 value, ties to even; an infinity saturates to +-448, a NaN stays one.  Since the scale is a power of two the
- *   division is exact, and so is reading back to bf16: writing what was read back gives the same numbers again.
+ *   division is exact, and so is reading back: writing what was read back gives the same numbers again.  Two exceptions, at
+ *   the ends of the range: magnitudes of 248 * 2^120 and more become 256 * 2^120 = 2^128, which reads back as infinity; and
+ *   with the scales 2^-126 and 2^-125 numbers may lie below the smallest of bf16, 2^-133, and are rounded when read as such.
  * k*N and H*N (rows of one request) must stay below 2^30 each, B below 65536, H at most 1024.
  */
 int chai_append_kv_paged(const void* k_new, const void* v_new, void* k_pages, void* v_pages, const int32_t* reps,

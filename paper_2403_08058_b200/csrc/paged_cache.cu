@@ -367,6 +367,13 @@ __device__ __forceinline__ uint4 pack16<__nv_bfloat16>(const float* f) {
     return r;
 }
 
+// x * scale for a type of fewer bits than fp32: rounded to odd (the last bit says that something was cut off), so that the
+// rounding to that type is the only one.
+__device__ __forceinline__ float product_to_odd(float x, float scale) {
+    const float p = __fmul_rz(x, scale);
+    return __uint_as_float(__float_as_uint(p) | (isfinite(p) && (double)p != (double)x * scale ? 1u : 0u));  // (28 bits: exact in fp64)
+}
+
 // grid (runs of tokens, planes that are wanted, B).
 template <typename TO, int D, bool FP8>
 __global__ void __launch_bounds__(kRowThreads) read_paged_kernel(const ReadArgs a) {
@@ -417,8 +424,17 @@ __global__ void __launch_bounds__(kRowThreads) read_paged_kernel(const ReadArgs 
             for (int e = 0; e < EPV / 2; ++e) {
                 const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)((w[e / 2] >> (16 * (e & 1))) & 0xffffu), __NV_E4M3);
                 const float2 p = __half22float2(*reinterpret_cast<const __half2*>(&h));
-                f[2 * e] = p.x * scale[u];
-                f[2 * e + 1] = p.y * scale[u];
+                f[2 * e] = p.x;
+                f[2 * e + 1] = p.y;
+            }
+            // A power of two, as append writes it, multiplies without rounding.  Other scales do not: fp32, then bf16, would
+            // round twice
+            if (sizeof(TO) < 4 && (__float_as_uint(scale[u]) & 0x7fffffu) != 0) {
+#pragma unroll
+                for (int e = 0; e < EPV; ++e) f[e] = product_to_odd(f[e], scale[u]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < EPV; ++e) f[e] *= scale[u];
             }
             v.a = pack16<TO>(f);
             v.b = pack16<TO>(f + EPV / 2);

@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from oracle import chai_oracle as orc
-from paged_cases import bits, partition, tables
+from paged_cases import TORCH, bits, partition, tables
 from paper_2403_08058_b200 import chai
 from test_gpu_paged import DEV, KINDS, decode, make, random_pool
 
@@ -285,3 +285,65 @@ def test_decode_a_query_with_one_large_element(D):
     c["k_rows"][0][..., 3] = 0.0
     c["scale"] = 2.0 ** 19 / np.sqrt(D)
     check_tightly(c, "one large element")
+
+
+# ---- read-back ---------------------------------------------------------------------------------------------------
+
+def nearest_bf16(x):
+    """float64 -> the nearest bf16 number, ties to even, as float64 (normal range)."""
+    m, e = np.frexp(x)
+    return np.ldexp(np.rint(m * 256.0), e - 8)      # (rint: ties to even)
+
+
+def test_read_back_is_rounded_once_with_any_scale():
+    """Scales that are no powers of two: the 28-bit product goes to bf16 (or fp32) in one rounding.  Half the rows have a
+    scale near (a tie of bf16) / (one of their numbers): fp32 rounds such products to the tie."""
+    B, H, k, D, page, T = 1, 8, 8, 128, 16, 512
+    rng = np.random.default_rng(77)
+    c = make("e4m3", "bf16", B, H, k, D, page, [T], seed=77)
+    codes = rng.integers(0, 0x7F, (H, T, D)) | (rng.integers(0, 2, (H, T, D)) << 7)
+    numbers = orc.e4m3_values()[codes]
+    # scales whose product with some code of the row is just beside a tie: (odd multiple of 2^-8 + 2^-25) / code
+    s8 = (1 + rng.integers(0, 2 ** 23, (H, T)) * 2.0 ** -23).astype(np.float32)
+    tie = (1 + (2 * rng.integers(0, 128, (H, T // 2)) + 1) * 2.0 ** -8)
+    code = 1 + rng.integers(1, 8, (H, T // 2)) / 8.0
+    near = (tie / code).astype(np.float32)
+    near = np.where(near < 1, near * 2, near).astype(np.float32)
+    s8[:, : T // 2] = near
+    codes[:, : T // 2, :8] = 0x38 + np.arange(8)     # 1, 1.125 ... 1.875
+    numbers = orc.e4m3_values()[codes]
+    for dt in ("bf16", "f32"):
+        exact = numbers * s8[..., None].astype(np.float64)
+        want = nearest_bf16(exact) if dt == "bf16" else exact.astype(np.float32).astype(np.float64)
+        if dt == "bf16":    # the oracle's second rounding would show
+            assert (nearest_bf16(exact.astype(np.float32).astype(np.float64)) != want).sum() > 20
+        at = (torch.from_numpy(c["table_np"][0, np.arange(T) // page].astype(np.int64)), torch.arange(T) % page)
+        c["v_pages"][at[0], :, at[1]] = torch.from_numpy(codes.astype(np.uint8)).transpose(0, 1).to(DEV)
+        c["v_scales"][at[0], :, at[1]] = torch.from_numpy(s8).T.contiguous().to(DEV)
+        _, v = chai.chai_read_kv_paged_fp8(c["k_pages"], c["v_pages"], c["k_scales"], c["v_scales"], c["table"], c["seq"], T_out=T,
+                                           dtype=TORCH[dt])
+        assert np.array_equal(v[0].double().cpu().numpy(), want), dt
+
+
+def test_the_largest_and_the_smallest_rows_go_through_pages():
+    """What the header says of the ends of the range: 2^128 reads back as infinity, 2^-135 as a bf16 number of 2^-133 steps."""
+    B, H, k, D, page = 1, 4, 1, 64, 16
+    x = torch.zeros(B, H, 3, D)
+    x[0, 0, :, 0] = torch.tensor([247.0, 248.0, 255.0]) * 2.0 ** 120
+    x[0, 0, :, 1] = -(2.0 ** 118)
+    x[0, 1, :, 0] = torch.tensor([2.0 ** -126 * 300, 2.0 ** -133, 5 * 2.0 ** -135])
+    x[0, 1, :, 1] = torch.tensor([2.0 ** -135, 3 * 2.0 ** -135, 2.0 ** -149])
+    kp, vp = (torch.zeros(1, p, page, D, device=DEV, dtype=torch.uint8) for p in (k, H))
+    ks, vs = (torch.zeros(1, p, page, device=DEV) for p in (k, H))
+    table, seq = torch.zeros(1, 1, dtype=torch.int32, device=DEV), torch.zeros(1, dtype=torch.int32, device=DEV)
+    chai.chai_append_kv_paged_fp8(x.to(DEV), x.to(DEV), kp, vp, ks, vs, torch.zeros(1, 1, dtype=torch.int32, device=DEV), table, seq)
+    codes, scales = orc.quantize_rows_fp8(x.double().numpy())
+    assert np.array_equal(vp[0, :, :3].cpu().numpy(), codes[0]) and np.array_equal(vs[0, :, :3].cpu().numpy(), scales[0].astype(np.float32))
+    exact = orc.e4m3_values()[codes] * scales[..., None]
+    assert exact.max() == 2.0 ** 128 and (scales[0, 1] == 2.0 ** -126).all()
+    for dt, step in ((torch.float32, 2.0 ** -149), (torch.bfloat16, 2.0 ** -133)):
+        _, v = chai.chai_read_kv_paged_fp8(kp, vp, ks, vs, table, seq, T_out=3, dtype=dt)
+        want = np.where(np.abs(exact) >= 2.0 ** 128, np.inf, exact)
+        small = np.abs(exact) < 2.0 ** -126
+        want = np.where(small, np.rint(exact / step) * step, want)
+        assert np.array_equal(v.double().cpu().numpy(), want)
