@@ -35,7 +35,11 @@ namespace {
 
 constexpr int kMaxCtas = 160;     // the workspace bound is stated for this many; a B200 has 148 SMs
 constexpr int kQuantum = 8;       // rows; page sizes are multiples of it
-constexpr int kJoinBlocks = 37;   // blocks per head, at most
+constexpr int kJoinThreads = 128, kJoinBlocks = 37;  // blocks per head, at most
+// Up to so many requests, their columns are dealt to D / 32 blocks a head: few requests have many pieces each and few blocks
+// to join them.  One request of 2000 tokens 14.5 -> 12.6 us, of 20000 44.0 -> 41.4, of 131072 209.5 -> 206.8; two of 2048 19.1
+// -> 17.4; four of 300 and less 11.6 -> 11.9, four of 2048 and less, e4m3, 28.8 -> 29.3.
+constexpr int kJoinFew = 2;
 constexpr int kUnit = 16;         // rows; the line of all rows is divided in units of so many
 // Units that a request counts more than it has, in front: what a CTA loses where one request ends and the next begins, which
 // a CTA without such a place makes up for.  In rows, e4m3, 7B shape: 32 59.9 us, 48 58.6, 64 57.4, 112 57.4; 16 requests of
@@ -1107,15 +1111,17 @@ __global__ void __launch_bounds__(Geom<T, TQ, D>::THREADS, 1) paged_decode_kerne
 
 // ---- joining the pieces of a request ----------------------------------------------------------------------------
 
-// grid (H, blocks): out[b][h] from the partial results of consecutive pieces.  Bound by the round trips to L2, one for the
-// description and one for everything else: the first rows are on their way before the weights are known.
-template <typename TQ, int D, int THREADS>
-__global__ void __launch_bounds__(THREADS) paged_join_kernel(const DecodeArgs a, int n_ctas) {
-    constexpr int WARPS = THREADS / 32, E = D / 32, AHEAD = 4;
-    __shared__ float s_w[kMaxCtas], s_top[WARPS], s_sum[WARPS], s_o[WARPS][D];
+// grid (H, blocks, SPLIT): out[b][h] from the partial results of consecutive pieces, a SPLIT-th of its columns.  Bound by the
+// round trips to L2, one for the description and one for everything else: the first rows are on their way before the
+// weights are known.  The order of the sums is the same for every SPLIT, and does not depend on the width of the tables.
+template <typename TQ, int D, int SPLIT>
+__global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(const DecodeArgs a, int n_ctas) {
+    constexpr int THREADS = kJoinThreads, WARPS = THREADS / 32, COLS = D / SPLIT, E = COLS / 32;
+    constexpr int AHEAD = SPLIT == 1 ? 4 : 16, THEN = SPLIT == 1 ? 8 : 24;  // rows a warp has on their way, at first and later
+    __shared__ float s_w[kMaxCtas], s_top[WARPS], s_sum[WARPS], s_o[WARPS][COLS];
     dependent_grid_sync();
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, h = blockIdx.x;
-    if (blockIdx.x == 0 && blockIdx.y == 0 && warp == 0) {  // the call's status
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, h = blockIdx.x, col = blockIdx.z * COLS;
+    if (blockIdx.x == 0 && blockIdx.y == 0 && blockIdx.z == 0 && warp == 0) {  // the call's status
         int code = CHAI_OK, at = -1;
         for (int i = lane; i < n_ctas; i += 32) {
             const int e = a.ws.err[i];
@@ -1134,14 +1140,12 @@ __global__ void __launch_bounds__(THREADS) paged_join_kernel(const DecodeArgs a,
             a.hdr->bad_b = at;
         }
     }
-    using Row = typename std::conditional<E == 4, float4, float2>::type;
-    auto add = [&](float* o, float w, const Row& x) {
-        o[0] = fmaf(w, x.x, o[0]);
-        o[1] = fmaf(w, x.y, o[1]);
-        if constexpr (E == 4) {
-            o[2] = fmaf(w, x.z, o[2]);
-            o[3] = fmaf(w, x.w, o[3]);
-        }
+    struct alignas(4 * E) Row {
+        float x[E];
+    };
+    auto add = [&](float* o, float w, const Row& r) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[e] = fmaf(w, r.x[e], o[e]);
     };
 #pragma unroll 1
     for (int di = blockIdx.y; di < a.n_desc; di += gridDim.y) {
@@ -1150,7 +1154,7 @@ __global__ void __launch_bounds__(THREADS) paged_join_kernel(const DecodeArgs a,
         // -1: nothing to join.  (The other bounds hold unless another stream changes lengths under the call, which leaves
         // descriptions unwritten; results are anyone's guess then, addresses are not.)
         if (b < 0 || b >= a.B || n < 1 || n > n_ctas || first < 0 || first > kMaxCtas + a.B - n) continue;
-        const float* src = a.ws.o + ((size_t)first * a.H + h) * D + lane * E;
+        const float* src = a.ws.o + ((size_t)first * a.H + h) * D + col + lane * E;
         const size_t apart = (size_t)a.H * D;
         Row ahead[AHEAD];
 #pragma unroll
@@ -1199,19 +1203,19 @@ __global__ void __launch_bounds__(THREADS) paged_join_kernel(const DecodeArgs a,
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u)
             if (warp + u * WARPS < n) add(o, s_w[warp + u * WARPS], ahead[u]);
-#pragma unroll 8
+#pragma unroll THEN
         for (int i = warp + AHEAD * WARPS; i < n; i += WARPS) add(o, s_w[i], *reinterpret_cast<const Row*>(src + i * apart));
 #pragma unroll
         for (int e = 0; e < E; ++e) s_o[warp][lane * E + e] = o[e];
         __syncthreads();
-        if (tid < D) {
+        if (tid < COLS) {
             float l = 0.f, x = 0.f;
 #pragma unroll
             for (int w = 0; w < WARPS; ++w) {
                 l += s_sum[w];
                 x += s_o[w][tid];
             }
-            static_cast<TQ*>(a.out)[((size_t)b * a.H + h) * D + tid] = from_float<TQ>(zero || l == 0.f ? 0.f : x / l);
+            static_cast<TQ*>(a.out)[((size_t)b * a.H + h) * D + col + tid] = from_float<TQ>(zero || l == 0.f ? 0.f : x / l);
         }
         __syncthreads();  // s_* are free for the next description
     }
@@ -1241,14 +1245,13 @@ int launch_decode(const DecodeArgs& args, cudaStream_t s) {
     DecodeArgs a = args;
     a.n_desc = a.B < n_ctas ? a.B : n_ctas;
     CHAI_LAUNCH_DEPENDENT("paged_decode_kernel launch", (paged_decode_kernel<T, TQ, D>), dim3(n_ctas), dim3(G::THREADS), smem, s, a);
-    // A few long requests have many pieces each: more warps to a head then (one request of 131072 tokens, 148 pieces:
-    // 212.5 us a call with 4 warps, 210.9 with 16).  Short ones are faster with 4: such blocks find room beside the main
-    // kernel's and wait for its end in place (one request of 256 tokens, 16 pieces: 9.9 us against 10.9).
-    const dim3 grid(a.H, a.n_desc < kJoinBlocks ? a.n_desc : kJoinBlocks);
-    if (a.n_desc <= 4 && a.pool.capacity > 16384)
-        CHAI_LAUNCH_DEPENDENT("paged_join_kernel launch", (paged_join_kernel<TQ, D, 512>), grid, dim3(512), 0, s, a, n_ctas);
+    const int blocks = a.n_desc < kJoinBlocks ? a.n_desc : kJoinBlocks;
+    if (a.n_desc <= kJoinFew)
+        CHAI_LAUNCH_DEPENDENT("paged_join_kernel launch", (paged_join_kernel<TQ, D, D / 32>), dim3(a.H, blocks, D / 32),
+                              dim3(kJoinThreads), 0, s, a, n_ctas);
     else
-        CHAI_LAUNCH_DEPENDENT("paged_join_kernel launch", (paged_join_kernel<TQ, D, 128>), grid, dim3(128), 0, s, a, n_ctas);
+        CHAI_LAUNCH_DEPENDENT("paged_join_kernel launch", (paged_join_kernel<TQ, D, 1>), dim3(a.H, blocks), dim3(kJoinThreads), 0,
+                              s, a, n_ctas);
     return CHAI_OK;
 }
 

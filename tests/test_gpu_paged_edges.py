@@ -7,7 +7,7 @@ import torch
 from oracle import chai_oracle as orc
 from paged_cases import TORCH, bits, partition, tables
 from paper_2403_08058_b200 import chai
-from test_gpu_paged import DEV, KINDS, decode, make, random_pool
+from test_gpu_paged import DEV, KINDS, check, decode, make, random_pool
 
 pytestmark = pytest.mark.gpu
 
@@ -347,3 +347,20 @@ def test_the_largest_and_the_smallest_rows_go_through_pages():
         small = np.abs(exact) < 2.0 ** -126
         want = np.where(small, np.rint(exact / step) * step, want)
         assert np.array_equal(v.double().cpu().numpy(), want)
+
+
+# ---- tables wider than the requests ------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("cache,io", [("f32", "f32"), ("bf16", "bf16"), ("e4m3", "f32")])
+@pytest.mark.parametrize("lens", [[300], [5000, 700, 3000]])
+def test_decode_does_not_depend_on_the_width_of_the_table(cache, io, lens):
+    """Sums are taken in an order that follows from lengths and memberships: tables for 16 and for 40000 positions more give
+    the same bits."""
+    c = make(cache, io, len(lens), 12, 3, 128, 16, lens, seed=55)
+    want = decode(c).clone()
+    check(c, want)
+    for more in (1, 2500):
+        wide = torch.full((len(lens), c["table"].shape[1] + more), -1, dtype=torch.int32, device=DEV)
+        wide[:, : c["table"].shape[1]] = c["table"]
+        got = decode(dict(c, table=wide))
+        assert torch.equal(got.view(torch.uint8), want.view(torch.uint8)), more
