@@ -369,14 +369,17 @@ __global__ void __launch_bounds__(Geom<T, TQ, D>::THREADS, 1) paged_decode_kerne
     // Heads are dealt to several CTAs when a piece would be shorter than 32 rows, down to 4 heads a CTA: one request of 256
     // tokens takes 10.6 us a call instead of 13.8; of 512, 11.1 instead of 15.5; thresholds of half and twice that measure the
     // same or worse (e4m3, 66B shape of 400 tokens: 17.8 us, with 64 rows 21.4).
-    // To two CTAs when a layer has many planes and the batch is small, for longer pieces are more even (in units) and leave
-    // fewer partial results: ragged 33B shape 63.2 -> 59.0 us, 66B shape in e4m3 35.6 -> 32.0, 131072 tokens 211 -> 209.4.
-    // A cluster that both have a part of has its keys read twice, which layers of few planes (12 heads, 5 clusters: 32.7 ->
-    // 34.5 us; 32 and 8 still 61.5 -> 61.7) and pieces of many requests (100: 110.4 -> 112) pay more for than they gain.
+    // To two CTAs, in layers of 40 planes and more, when that makes pieces longer at little cost: more even (in units), and
+    // fewer partial results.  A cluster that both have a part of has its keys read twice, and a CTA meets twice the requests.
+    // Worth it for few requests whatever the rows (32 heads, 8 clusters, e4m3: one of 16384 tokens 33.5 -> 28.5 us, five ragged
+    // to 2000 21.4 -> 18.4, to 8000 37.9 -> 39.5); else where the planes' rows are 8 KB and more (bf16, 32 and 8: 8 requests 29.6
+    // -> 28.7, 16 62.0 -> 60.8; 72 and 24, e4m3: 8 requests 42.9 -> 36.5) or more than 16 clusters shorten the chunks (32 and
+    // 32, e4m3, D = 64: 16 requests 44.9 -> 42.2).  Not otherwise (32 and 8, e4m3: 8 requests ragged to 8000 54.2 -> 59.8, 16 of
+    // 2048 41.3 -> 43.8), nor for many requests (64: 52.6 -> 60.5, bf16 76.7 -> 78.2).
     const int n_ctas = gridDim.x;
     const int base_groups = (a.H + G::HEADS - 1) / G::HEADS;
     int group_log = 0, most_pieces = base_groups == 1 ? n_ctas : small_div(n_ctas, base_groups);
-    const bool two = a.H + a.k >= 40 && 4 * a.B <= n_ctas;
+    const bool two = a.H + a.k >= 40 && 4 * a.B <= n_ctas && (a.B < 8 || (a.H + a.k) * G::ROW >= 8192 || a.k > 16);
     while (((two && group_log == 0) || total < 2 * most_pieces) && (8 * base_groups << group_log) <= a.H && most_pieces > 1)
         ++group_log, most_pieces >>= 1;
     const int groups = base_groups << group_log;
