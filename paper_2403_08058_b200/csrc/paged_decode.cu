@@ -334,11 +334,6 @@ __global__ void __launch_bounds__(Geom<T, TQ, D>::THREADS, 1) paged_decode_kerne
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
     if (tid == 0) sm.err = CHAI_OK, sm.err_b = -1;
-    if (tid < 5) {  // warms the address translation while the kernel before this one drains; what is there is read later
-        const void* p = tid == 0 ? (const void*)a.seq_lens : tid == 1 ? (const void*)a.membership : tid == 2 ? (const void*)a.reps
-                        : tid == 3 ? (const void*)a.pool.block_table : a.q;
-        asm volatile("prefetch.global.L2 [%0];" ::"l"(p));
-    }
     dependent_grid_sync();
 
     // -- the line of all rows, this CTA's piece [q_lo, q_hi) and the request it starts in
