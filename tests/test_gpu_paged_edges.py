@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from oracle import chai_oracle as orc
-from paged_cases import TORCH, bits, partition, tables
+from paged_cases import TORCH, bits, decode_bounds, partition, tables
 from paper_2403_08058_b200 import chai
 from test_gpu_paged import DEV, KINDS, check, decode, make, random_pool
 
@@ -364,3 +364,88 @@ def test_decode_does_not_depend_on_the_width_of_the_table(cache, io, lens):
         wide[:, : c["table"].shape[1]] = c["table"]
         got = decode(dict(c, table=wide))
         assert torch.equal(got.view(torch.uint8), want.view(torch.uint8)), more
+
+
+# ---- appends of one launch and of several ------------------------------------------------------------------------
+
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("advance", [True, False])
+@pytest.mark.parametrize("H,k,N", [(32, 8, 1), (72, 24, 1), (96, 32, 1), (97, 32, 1), (20, 5, 2), (16, 5, 3), (16, 16, 4),
+                                   (32, 32, 4), (33, 32, 4), (128, 128, 1), (130, 128, 1), (128, 128, 2), (500, 12, 1)])
+def test_append_around_the_passes_of_a_step(io, fp8, advance, H, k, N):
+    """Below, at and above one pass (1024 vectors) and two of the one-block form, N of one to four with requests that have
+    fewer tokens; pages that are bad for the last vectors only."""
+    B, D, page = 4, 128, 8
+    g = torch.Generator().manual_seed(H * 8 + N)
+    lens = [0, page - 1, 2 * page - N + 1 if N > 1 else page, 3]
+    new = [N, N, max(0, N - 2), N - 1] if N > 1 else [1, 1, 1, 0]
+    table, n_pages = tables(lens, page, H, room=N)
+    table = table.copy()
+    _, reps = partition(B, H, k, H)
+    reps = reps.copy()
+    reps[2, k - 1] = -1
+    k_new, v_new = ((torch.randn(B, H, N, D, generator=g) * 3).to(TORCH[io]) for _ in range(2))
+    before = [random_pool(n_pages, p, page, D, torch.uint8 if fp8 else TORCH[io], 7 + p) for p in (k, H)]
+    before += [torch.rand(n_pages, p, page, generator=g).to(DEV) for p in (k, H)]
+    for spoil in (False, True):
+        if spoil:        # request 1's last token lies on its second page
+            table[1, 1 if N > 1 else 0] = n_pages + 5
+        kp, vp, ks, vs = (x.clone() for x in before)
+        host = [x.cpu() for x in before]
+        seq = torch.tensor(lens, dtype=torch.int32, device=DEV)
+        ws = chai.new_workspace(256, DEV)
+        call = (chai.chai_append_kv_paged_fp8, (kp, vp, ks, vs)) if fp8 else (chai.chai_append_kv_paged, (kp, vp))
+        call[0](k_new.to(DEV), v_new.to(DEV), *call[1], torch.from_numpy(reps).to(DEV), torch.from_numpy(table).to(DEV), seq,
+                new_lens=torch.tensor(new, dtype=torch.int32, device=DEV), advance=advance, workspace=ws)
+        assert chai.chai_device_status(ws) == (chai.CHAI_ERR_BAD_PAGE if spoil else chai.CHAI_OK)
+        if fp8:
+            (k8, ksc), (v8, vsc) = (orc.quantize_rows_fp8(x.double().numpy()) for x in (k_new, v_new))
+            wk, wv, wl = orc.append_kv_paged(k8, v8, host[0].numpy(), host[1].numpy(), reps, table, lens, new)
+            wks, wvs, _ = orc.append_kv_paged(ksc.astype(np.float32), vsc.astype(np.float32), host[2].numpy(), host[3].numpy(),
+                                              reps, table, lens, new)
+            assert np.array_equal(kp.cpu().numpy(), wk) and np.array_equal(vp.cpu().numpy(), wv)
+            assert np.array_equal(ks.cpu().numpy(), wks) and np.array_equal(vs.cpu().numpy(), wvs)
+        else:
+            wk, wv, wl = orc.append_kv_paged(bits(k_new), bits(v_new), bits(host[0]), bits(host[1]), reps, table, lens, new)
+            assert np.array_equal(bits(kp), wk) and np.array_equal(bits(vp), wv)
+        assert seq.cpu().tolist() == (wl.tolist() if advance else lens)
+
+
+# ---- decode against the definition on the pages themselves -------------------------------------------------------
+
+@pytest.mark.parametrize("cache", ["f32", "e4m3"])
+@pytest.mark.parametrize("page", [8, 24, 64])
+def test_decode_of_random_pages_follows_the_block_table(cache, page):
+    """Every row of the pool is random, tables name pages in any order and more than once; the oracle goes through them row
+    by row."""
+    B, H, k, D, n_pages, scale = 5, 7, 3, 64, 20, 0.125
+    lens = [page * 5 + 3, 0, 1, page * 9, 2 * page - 1]
+    rng = np.random.default_rng(page)
+    table = rng.integers(0, n_pages, (B, 10)).astype(np.int32)
+    mem, reps = partition(B, H, k, page)
+    q = torch.randn(B, H, D, generator=torch.Generator().manual_seed(page))
+    stored, scales, exact = [], [], []
+    for planes in (k, H):
+        shape = (n_pages, planes, page, D)
+        if cache == "e4m3":
+            codes = (rng.integers(0, 0x7F, shape) | (rng.integers(0, 2, shape) << 7)).astype(np.uint8)
+            size = np.exp2(rng.integers(-10, -6, shape[:3]))
+            stored.append(torch.from_numpy(codes).to(DEV))
+            scales.append(torch.from_numpy(size.astype(np.float32)).to(DEV))
+            exact.append(orc.e4m3_values()[codes] * size[..., None])
+        else:
+            x = rng.standard_normal(shape).astype(np.float32)
+            stored.append(torch.from_numpy(x).to(DEV))
+            exact.append(x.astype(np.float64))
+    fn = chai.chai_decode_attention_paged_fp8 if cache == "e4m3" else chai.chai_decode_attention_paged
+    got = fn(q.to(DEV), *stored, *scales, *(torch.from_numpy(x).to(DEV) for x in (mem, reps, table, np.array(lens, np.int32))), scale)
+    got, q = got.double().cpu().numpy(), q.double().numpy()
+    ref = orc.decode_attention_paged(q, *exact, mem, reps, table, lens, scale)
+    for b, n in enumerate(lens):
+        if n == 0:
+            assert not got[b].any()
+            continue
+        kr, vr = (orc.paged_rows(x, table[b], n) for x in exact)
+        allowed = decode_bounds(q[b], kr, vr, mem[b], reps[b], scale, "f32", cache == "e4m3") + 2.0 ** -24 * np.abs(ref[b])
+        assert (np.abs(got[b] - ref[b]) <= allowed).all(), f"request {b}"
