@@ -412,6 +412,46 @@ def test_append_around_the_passes_of_a_step(io, fp8, advance, H, k, N):
         assert seq.cpu().tolist() == (wl.tolist() if advance else lens)
 
 
+@pytest.mark.parametrize("cache,io", [("bf16", "bf16"), ("e4m3", "bf16"), ("f32", "f32")])
+def test_arrays_much_longer_than_the_requests(cache, io):
+    """Dense arrays for 5000 tokens and 500 planes: blocks go on from run to run; rows behind the lengths stay as they were."""
+    B, H, k, D, page, N = 5, 80, 20, 128 if cache == "e4m3" else 64, 16, 5000      # 79 runs of 64 tokens (fp32: 157 of 32)
+    lens = [5000, 0, 1, 4097, 37]
+    g = torch.Generator(device=DEV).manual_seed(5)
+    table_np, n_pages = tables(lens, page, 9)
+    table = torch.from_numpy(table_np).to(DEV)
+    _, reps = partition(B, H, k, 9)
+    reps = torch.from_numpy(reps).to(DEV)
+    k_new, v_new = (torch.randn(B, H, N, D, device=DEV, generator=g).to(TORCH[io]) for _ in range(2))
+    fp8 = cache == "e4m3"
+    pages = [torch.zeros(n_pages, p, page, D, device=DEV, dtype=torch.uint8 if fp8 else TORCH[cache]) for p in (k, H)]
+    pages += [torch.zeros(n_pages, p, page, device=DEV) for p in (k, H)] if fp8 else []
+    seq, count = torch.zeros(B, dtype=torch.int32, device=DEV), torch.tensor(lens, dtype=torch.int32, device=DEV)
+    ws = chai.new_workspace(256, DEV)
+    put, get = (chai.chai_append_kv_paged_fp8, chai.chai_read_kv_paged_fp8) if fp8 else (chai.chai_append_kv_paged, chai.chai_read_kv_paged)
+    put(k_new, v_new, *pages, reps, table, seq, new_lens=count, workspace=ws)
+    assert chai.chai_device_status(ws) == chai.CHAI_OK and seq.tolist() == lens
+    k_out, v_out = (torch.full((B, p, N, D), 9.0, device=DEV, dtype=TORCH[io]) for p in (k, H))
+    get(*pages, table, seq, k_out=k_out, v_out=v_out, workspace=ws)
+    assert chai.chai_device_status(ws) == chai.CHAI_OK
+    for b, n in enumerate(lens):
+        keys = k_new[b, reps[b].long(), :n]
+        for out, x in ((k_out[b], keys), (v_out[b], v_new[b, :, :n])):
+            assert (out[:, n:] == 9.0).all()
+            if fp8:      # half a step of three mantissa bits, or of the row's smallest numbers
+                top = x.float().abs().amax(-1, keepdim=True) if n else x.float()
+                assert ((out[:, :n].float() - x.float()).abs() <= torch.maximum(x.float().abs() * 2.0 ** -4, top * 2.0 ** -17)).all()
+            else:
+                assert torch.equal(out[:, :n], x)
+    table[3, 4090 // page] = -1          # a page that a block's last run meets
+    get(*pages, table, seq, k_out=k_out, v_out=v_out, workspace=ws)
+    assert chai.chai_device_status(ws) == chai.CHAI_ERR_BAD_PAGE
+    assert not v_out[3, :, 4080:4096].any()
+    seq.zero_()
+    put(k_new, v_new, *pages, reps, table, seq, new_lens=count, workspace=ws)
+    assert chai.chai_device_status(ws) == chai.CHAI_ERR_BAD_PAGE and seq.tolist() == [5000, 0, 1, 0, 37]
+
+
 # ---- decode against the definition on the pages themselves -------------------------------------------------------
 
 @pytest.mark.parametrize("cache", ["f32", "e4m3"])
