@@ -6,7 +6,8 @@
 namespace chai {
 
 // n / d for 0 <= n < 2^31 by a multiplication: with s = ceil(log2 d) and m = floor(2^32 (2^s - d) / d) + 1 the
-// quotient is (hi32(m n) + n) >> s.  (A division by a kernel argument costs about twenty instructions; the copy kernels
+// quotient is (hi32(m n) + n) >> s (Granlund and Montgomery, "Division by invariant integers using multiplication", 1994).
+// (A division by a kernel argument costs about twenty instructions; the copy kernels
 // would need one for every 16 bytes.)
 struct FastDiv {
     unsigned d, m, s;

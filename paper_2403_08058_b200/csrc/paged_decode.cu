@@ -17,12 +17,13 @@
 // A request that lies in one piece is written at once.  The others leave one partial result (maximum, sum, values) per
 // piece, and a second kernel, launched as a programmatic dependent, joins them: all sums are taken in an order that
 // follows from the lengths and memberships alone, and nothing in the workspace has to be cleared.  (Joining in this
-// kernel, by the CTA of a request or the warp of a head that arrives last on a tagged word, measured 15.7 and 20 us where
-// this took 11.3, and 76 and 79 where it took 65: few hands do at the end what the second kernel spreads over the GPU.)
+// kernel, by the CTA of a request or the warp of a head that arrives last on a tagged word, was tried on an earlier form that
+// took 11.3 us for one request of 256 tokens and 65 for the 7B shape below: 15.7 and 20, 76 and 79.  Few hands then do at
+// the end what the second kernel spreads over the GPU.)
 //
 // Measured (GPU time a call, calls back to back, of the 6566 GB/s that a copy reaches): 7B shape (16 requests of 2048
-// tokens, 32 heads, 8 clusters, bf16) 60.4 us = 85 %; one request of 131072 tokens 207 us = 99 %; the 7B shape in e4m3 with
-// 32 clusters 54 to 57 us = 74 to 78 %.  Rows stream at the copy's rate or near it; what is left is constant, some 4 us from
+// tokens, 32 heads, 8 clusters, bf16) 60.0 us = 85 %; one request of 131072 tokens 207 us = 99 %; the 7B shape in e4m3 with
+// 32 clusters 54.5 us = 77 %.  Rows stream at the copy's rate or near it; what is left is constant, some 4 us from
 // the start to the first tile's arrival (lengths, then tables and memberships, then rows: three round trips), 4 for the
 // join, and the phases of the CTAs that two requests meet in.  e4m3 is also bound by the latencies of a warp's instructions
 // (issue slots are half full, the tensor cores busy for a seventh of the time), which more warps hide: see Geom.
@@ -42,11 +43,11 @@ constexpr int kJoinThreads = 128, kJoinBlocks = 37;  // blocks per head, at most
 constexpr int kJoinFew = 2;
 constexpr int kUnit = 16;         // rows; the line of all rows is divided in units of so many
 // Units that a request counts more than it has, in front: what a CTA loses where one request ends and the next begins, which
-// a CTA without such a place makes up for.  In rows, e4m3, 7B shape: 32 59.9 us, 48 58.6, 64 57.4, 112 57.4; 16 requests of
-// 600 tokens 28.6, 27.7, 26.2, 26.4; bf16, 7B shape 61.1, 60.5, 60.3, 60.8; without any, before other changes, 65.7 against
-// 64.0 with 16 and 63.5 with 32.  Where all requests are short, CTAs meet several ends each, and more is lost to uneven
-// pieces: 100 requests of up to 700 tokens 82.0, 83.2, 84.0; 60 of up to 100 22.3, 23.3, 24.4 (16 of up to 200: 17.2 us
-// with 16 rows, 13.9 with 32).
+// a CTA without such a place makes up for.  In rows, 0 / 16 / 32 / 48 / 64 / 112: e4m3, 7B shape 58.4 / 56.7 / 56.9 / 55.9 /
+// 54.5 / 54.8 us; 16 requests of 600 tokens 31.6 / 30.7 / 28.8 / 27.9 / 26.3 / 26.5; bf16, 7B shape 62.5 / 61.0 / 60.9 / 60.1 /
+// 60.2 / 60.5.  Where all requests are short, CTAs meet several ends each, and more is lost to uneven pieces: 60 of up to 100
+// tokens 32.5 / 30.7 / 27.1 / 27.0 / 28.2 / 30.3, 16 of up to 200 21.1 / 20.3 / 15.6 / 15.7 / 15.7 / 16.4.  So by the length, 32
+// to 64.
 __device__ __forceinline__ int overhead(int n) { return min(4, max(2, n >> 7)); }
 __device__ __forceinline__ int units(int n) { return n > 0 ? (n + kUnit - 1) / kUnit + overhead(n) : 0; }
 // e4m3: x as two fp16 numbers, h = fp16(x) and fp16(2^11 (x - h)).  2^11 keeps the second as large as the first: where both
@@ -57,15 +58,15 @@ constexpr float kProductFactor = 524288.f;  // brings products of 2^-12 ... 2^-4
 template <typename T, typename TQ, int D>
 struct Geom {
     static constexpr bool FP8 = std::is_same<T, Fp8E4M3>::value;
-    // warps: e4m3, bound by the latency of a warp's instructions, as many as have registers enough (7B shape: 12 62.2 us,
-    // 16 57.4; 18 spill, 78.8); the others as many as keep the copies going (bf16, 7B shape: 10 62.3 us, 12 60.6, 14 61.3, 16
-    // 60.7; fp32, one request of 256 tokens 9.8 with 12, 10.4 with 16)
+    // warps: e4m3, bound by the latency of a warp's instructions, as many as have registers enough (7B shape: 12 59.4 us,
+    // 14 60.4, 16 54.5; 18 spill); the others as many as keep the copies going (bf16, 7B shape: 10 62.7 us, 12 60.0, 14 59.9, 16
+    // 59.1, ragged 33B shape 60.3, 58.4, 58.3, 59.1; fp32, one request of 256 tokens 10.2, 10.1, 10.5, 10.7)
     static constexpr int W = FP8 ? 16 : 12, THREADS = W * 32;
     static constexpr int ROW = D * (int)sizeof(T);
     static constexpr int TR = FP8 ? 32 : 4096 / ROW;  // rows of a tile
     // Slots of a warp.  Two tiles of 4 KB in flight for each of 12 warps are 98 KB an SM, more than the rate takes; a third
-    // only makes the queue longer, which every phase with few tiles a warp waits for (bf16: 131072 tokens 221 us with three,
-    // 211 with two; 7B shape 63.4 and 61.2; 10 warps with two 216 and 63.3).
+    // only makes the queue longer, which every phase with few tiles a warp waits for (an earlier form, bf16: 131072 tokens 221
+    // us with three, 211 with two; 7B shape 63.4 and 61.2).
     static constexpr int STAGES = 2;
     static constexpr int DATA = TR * ROW;
     static constexpr int QUERY = DATA + (FP8 ? TR * 4 : 0);  // e4m3: the rows' scales lie behind them ...
@@ -362,8 +363,9 @@ __global__ void __launch_bounds__(Geom<T, TQ, D>::THREADS, 1) paged_decode_kerne
         }
     }
     // Heads are dealt to several CTAs when a piece would be shorter than 32 rows, down to 4 heads a CTA: one request of 256
-    // tokens takes 10.6 us a call instead of 13.8; of 512, 11.1 instead of 15.5; thresholds of half and twice that measure the
-    // same or worse (e4m3, 66B shape of 400 tokens: 17.8 us, with 64 rows 21.4).
+    // tokens takes 10.1 us a call instead of 11.4; of 512, 10.6 instead of 12.0.  With thresholds of 16 and 64 rows: one of 2000
+    // 13.7 and 13.5 us, 13.0 with 32; four ragged to 500 12.8 and 12.0, 11.4; but e4m3, 66B shape, ragged to 400: 15.0 and 21.2,
+    // 19.5.
     // To two CTAs, in layers of 40 planes and more, when that makes pieces longer at little cost: more even (in units), and
     // fewer partial results.  A cluster that both have a part of has its keys read twice, and a CTA meets twice the requests.
     // Worth it for few requests whatever the rows (32 heads, 8 clusters, e4m3: one of 16384 tokens 33.5 -> 28.5 us, five ragged
@@ -505,8 +507,8 @@ __global__ void __launch_bounds__(Geom<T, TQ, D>::THREADS, 1) paged_decode_kerne
                 }
             }
             // the group's heads: of two groups half the planes (keys of the clusters and values, in order), else as many heads
-            // as any (half the heads instead of half the planes: 7B shape 62.8 us, 61.7 this way; many groups have short
-            // pieces, where the barrier that this takes costs more than it gains, 0.3 us)
+            // as any (half the heads instead of half the planes: 7B shape 61.6 us, 60.0 this way, 66B shape in e4m3 30.4 and 29.2;
+            // many groups have short pieces, where the barrier that this takes costs more than it gains, 0.3 us)
             const bool by_planes = groups == 2 && a.H <= G::HEADS;
             int lo = groups == 1 ? 0 : small_div(known * group, groups), n_heads = groups == 1 ? known : small_div(known * (group + 1), groups) - lo;
             int mine = -1;
@@ -598,8 +600,8 @@ __global__ void __launch_bounds__(Geom<T, TQ, D>::THREADS, 1) paged_decode_kerne
     [[maybe_unused]] const uint32_t copy_at = (lane >> 3) * 128 + 16 * ((lane & 7) ^ (D == 128 ? 4 * ((lane >> 3) & 1) : 2 * (lane >> 4)));
 
     // Starts copies until the warp's slots are in flight or nothing is known to copy.  (Addresses are worked out when a slot
-    // is free.  Held ready from a tile earlier they cost registers, which are worth more as warps: e4m3 with 16 warps, 7B
-    // shape 61.9 us that way and 56.5 this way, bf16 61.3 and 60.6.)
+    // is free.  Held ready from a tile earlier they cost registers, which are worth more as warps: in an earlier form
+    // e4m3 with 16 warps, 7B shape, 61.9 us that way and 56.5 this way, bf16 61.3 and 60.6.)
     auto fill = [&]() __attribute__((always_inline)) {
 #pragma unroll 1
         while (!dead && issued - used < G::STAGES) {
