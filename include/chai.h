@@ -457,6 +457,139 @@ int chai_decode_attention_paged_fp8(const void* q, const void* k_pages, const vo
                                     size_t v_page_stride, float scale, int dtype, void* workspace, size_t workspace_bytes,
                                     void* stream);
 
+/*
+ * A serving step of many tokens.  The new tokens of all requests are packed: rows token_start[b] .. token_start[b+1]-1 of
+ * [n_tokens, ...] arrays belong to request b; rows behind token_start[B] are padding that no call reads or writes, so that a
+ * step of fewer tokens can replay a captured one.  Three calls make the step's attention, each of its own use:
+ *   chai_plan_paged               pages for the tokens; where every token goes
+ *   chai_append_rope_paged        q and k rotated, keys and values into the pages
+ *   chai_prefill_attention_paged  attention of the tokens over the pages
+ * (a step of one token a request may decode with chai_decode_attention_paged, whose seq_lens are kv_lens here).
+ */
+
+/*
+ * Pages for a step's tokens, from a stack of free pages on the device.
+ *   seq_lens [B] int32       cached positions of each request
+ *   new_lens [B] int32       tokens that each request gets; below 0: the request ends
+ *   block_table [B,max_pages] int32, in and out: entries behind a request's pages are written as it grows
+ *   free_pages [n_pages] int32, in and out; free_count [1] int32: the stack's entries 0 .. free_count-1 are the free
+ *                            pages, the top one last; free_count_out [1] its new height (may be free_count itself)
+ *   kv_lens [B] int32 out    cached positions with the new tokens (may be seq_lens itself); 0 for a request that ends
+ *   token_start [B+1] int32 out
+ *   token_request, positions [n_tokens] int32 out, slots [n_tokens] int64 out: a token's request, its position, and
+ *                            page * page_size + row of where it is cached; -1, 0 and -1 behind the last token
+ * First the pages of requests that end are pushed, request by request in the order of their lists (a list with an entry outside
+ * [0, n_pages) is not given back; pages must not be in the list of a request that goes on).  Then, in the order of the
+ * requests: one that needs p more pages (ceil((s+n)/page_size) - ceil(s/page_size)) takes the top p.  A request that
+ * does not fit gets no tokens: its length is outside [0, max_pages*page_size - n], or it needs pages and its needs and those of
+ * all requests before it (that fit their lists) exceed the stack, or its tokens and those of all before it exceed n_tokens.  So
+ * requests are served first come, first served, except that tokens in a page that is there already need no page.
+ * The status word of the workspace (chai_plan_paged_workspace_bytes: 512 + 4 B) says CHAI_ERR_BAD_PAGE (an entry of a
+ * list or of the stack that is no page: such a token's slot is -1; free_count outside [0, n_pages]; more pages given back
+ * than there are), else CHAI_ERR_CACHE_FULL if some request did not fit, else CHAI_OK.
+ * page_size as for the paged calls above; B below 65536, n_tokens at most 2^30.  token_request, positions, slots and the
+ * workspace must be 16-byte aligned, the other arrays 4-byte.
+ */
+size_t chai_plan_paged_workspace_bytes(int B);
+int chai_plan_paged(const int32_t* seq_lens, const int32_t* new_lens, int32_t* block_table, int32_t* free_pages,
+                    const int32_t* free_count, int32_t* free_count_out, int32_t* kv_lens, int32_t* token_start,
+                    int32_t* token_request, int32_t* positions, int64_t* slots, int B, int n_tokens, int n_pages, int page_size,
+                    int max_pages, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Rotary positions (Section 2 of the paper: attention of decoder models; the models that it measures rotate queries and
+ * keys by their positions before their product).  The first `rot` elements of a row (a multiple of 16, 0: none) are pairs,
+ * i and i + rot/2, or 2i and 2i+1 with `interleaved`; at position p pair i is turned by the angle a = 2 pi p turns[i]:
+ *   y1 = magnitude (x1 cos a - x2 sin a),  y2 = magnitude (x2 cos a + x1 sin a)
+ * and the other elements are copied.  p turns[i] is reduced in fp64, the rest is fp32; results are rounded once.  Positions
+ * may be any int32: negative ones turn back, which is also the operator's gradient and what moves a cached key
+ * by a difference of positions.
+ *
+ * chai_rope_frequencies fills a HOST array of rot/2 frequencies in turns a position, f_i = base^(-2i/rot) / (2 pi), and
+ * the magnitude that goes with them, from the HOST array parameters[5] = base, factor, context, low, high:
+ *   CHAI_ROPE_PLAIN   f_i
+ *   CHAI_ROPE_LINEAR  f_i / factor
+ *   CHAI_ROPE_BASE    base * factor^(rot/(rot-2)) in place of base
+ *   CHAI_ROPE_RAMP    f_i (1-g) + f_i / factor g, g rising from 0 to 1 between the pairs that turn `high` and `low` times
+ *                     over `context` positions: indexes floor and ceil of rot ln(context / (2 pi times)) / (2 ln base),
+ *                     cut to [0, rot-1]; the magnitude is 0.1 ln(factor) + 1 (customary: low 1, high 32)
+ *   CHAI_ROPE_BANDS   f_i s + f_i / factor (1-s), s = (context f_i - low) / (high - low) cut to [0, 1]  (low 1, high 4)
+ * factor >= 1; context, low < high only matter to the last two.
+ */
+typedef enum { CHAI_ROPE_PLAIN = 0, CHAI_ROPE_LINEAR = 1, CHAI_ROPE_BASE = 2, CHAI_ROPE_RAMP = 3, CHAI_ROPE_BANDS = 4 } chai_rope_scaling_t;
+int chai_rope_frequencies(double* turns_host, double* magnitude_host, int rot, int scaling, const double* parameters_host);
+
+/*
+ * Whole prompts, before chai_prefix_features and chai_prefill_attention: q [B,Hq,N,D] and k [B,Hk,N,D] (Hk may be 0).
+ *   positions [B,N] int32, device, or NULL: 0 .. N-1;  turns [rot/2] fp64, device;  magnitude_host: HOST, or NULL for 1
+ *   strides  HOST array of 12, elements: batch, head, token of q, of q_out, of k, of k_out; NULL: all contiguous.  Multiples of
+ *            16 bytes; the D elements of a row are contiguous
+ * q_out may be q itself (same strides) and k_out k; other overlaps are not allowed.
+ */
+int chai_rope(const void* q, const void* k, void* q_out, void* k_out, const int32_t* positions, const double* turns, int B,
+              int Hq, int Hk, int N, int D, int rot, int interleaved, const double* magnitude_host, const int64_t* strides, int dtype,
+              void* stream);
+
+/*
+ * A packed batch enters the cache: for every token t with slots[t] >= 0, b = token_request[t], each cluster c of b with
+ * r = reps[b][c] >= 0 and each head h, with page and row from the slot and R the rotation above at positions[t]:
+ *   k_pages[page][c][row] = R k[t][r],   v_pages[page][h][row] = v[t][h],   q_out[t][r] = R q[t][r]
+ * Only representatives' queries are looked at by the attention calls; the other rows of q_out stay as they were, and so do
+ * tokens with slot -1.
+ *   q, k, v [n_tokens,H,D], q_out [n_tokens,H,D] contiguous, not overlapping q
+ *   *_token_stride           elements between tokens of q, k and v: 0 for H*D; more where they are parts of one
+ *                            projection's output.  Multiples of 16 bytes
+ *   k_pages, v_pages, their strides, page_size, reps as for the paged calls above; no two tokens share a slot
+ *   workspace                NULL, or >= 256 bytes for the status word: CHAI_OK, or CHAI_ERR_BAD_PAGE if a slot is at or beyond
+ *                            n_pages*page_size or its token_request is outside [0, B) (that token is skipped)
+ * _fp8: rows become e4m3 as chai_append_kv_paged_fp8 makes them, of the rotated fp32 numbers (one rounding).  n_tokens at
+ * most 2^30.
+ */
+int chai_append_rope_paged(const void* q, const void* k, const void* v, void* q_out, void* k_pages, void* v_pages,
+                           const int32_t* reps, const int32_t* token_request, const int32_t* positions, const int64_t* slots,
+                           const double* turns, int rot, int interleaved, const double* magnitude_host, int B, int H, int k_planes,
+                           int n_tokens, int n_pages, int page_size, int D, size_t q_token_stride, size_t k_token_stride,
+                           size_t v_token_stride, size_t k_page_stride, size_t v_page_stride, int dtype, void* workspace,
+                           void* stream);
+int chai_append_rope_paged_fp8(const void* q, const void* k, const void* v, void* q_out, void* k_pages, void* v_pages,
+                               float* k_scales, float* v_scales, const int32_t* reps, const int32_t* token_request,
+                               const int32_t* positions, const int64_t* slots, const double* turns, int rot, int interleaved,
+                               const double* magnitude_host, int B, int H, int k_planes, int n_tokens, int n_pages, int page_size, int D,
+                               size_t q_token_stride, size_t k_token_stride, size_t v_token_stride, size_t k_page_stride,
+                               size_t v_page_stride, int dtype, void* workspace, void* stream);
+
+/*
+ * Clustered attention of a packed batch over a paged cache (chai_prefill_attention's operator): token i of the n =
+ * token_start[b+1] - token_start[b] of request b, in row t = token_start[b] + i, gets
+ *   out[t][h] = sum_s softmax_s(scale * q[t][r] . K[c][s]) * V[h][s],   c = membership[b][h], r = reps[b][c]
+ * over the request's cached positions s < kv_lens[b], with causal != 0 only s <= kv_lens[b] - n + i: the tokens are the last
+ * n of the cached positions (chunks of a prompt, guessed tokens, single tokens: any mix).  causal == 0: every token sees
+ * every position, whatever their numbers (states of another length).  A row that sees nothing gets zeros.
+ *   q [n_tokens,H,D] with q_token_stride as above, out [n_tokens,H,D] contiguous, not overlapping q
+ *   kv_lens [B], token_start [B+1] int32, device (clamped to [0, max_pages*page_size] and [0, n_tokens])
+ * Types, refusals and what inconsistent memberships and bad pages lead to are as for chai_decode_attention_paged; scale must be
+ * positive and finite.  CHAI_BF16 runs on the tensor cores, with probabilities rounded to bf16 and e4m3 rows as the bf16
+ * numbers that they stand for; CHAI_F32 on the CUDA cores.  Sums and statistics are fp32.  Rows at or beyond kv_lens[b] are never
+ * used, whatever they hold.  An infinity or NaN among the cached values below kv_lens[b] may also reach tokens of its
+ * request that do not see it (as zero times infinity); among keys it reaches only those that see it.
+ * The workspace (chai_prefill_paged_workspace_bytes: 2^20 + 64 B + 36 H (B + n_tokens/128 + 1) + 640000 min(n_tokens, 128), whatever
+ * the lengths) needs no clearing; calls that share one must be ordered on one stream.
+ * H at most 1024, B below 65536, (n_tokens/16 + B + 1) * H below 2^26, and the planner's limit on H and k that
+ * chai_prefill_attention states.
+ */
+size_t chai_prefill_paged_workspace_bytes(int B, int H, int n_tokens);
+int chai_prefill_attention_paged(const void* q, const void* k_pages, const void* v_pages, const int32_t* membership,
+                                 const int32_t* reps, const int32_t* block_table, const int32_t* kv_lens, const int32_t* token_start,
+                                 void* out, int B, int H, int k, int n_tokens, int n_pages, int page_size, int max_pages, int D,
+                                 size_t q_token_stride, size_t k_page_stride, size_t v_page_stride, float scale, int causal,
+                                 int dtype, void* workspace, size_t workspace_bytes, void* stream);
+int chai_prefill_attention_paged_fp8(const void* q, const void* k_pages, const void* v_pages, const float* k_scales,
+                                     const float* v_scales, const int32_t* membership, const int32_t* reps,
+                                     const int32_t* block_table, const int32_t* kv_lens, const int32_t* token_start, void* out, int B,
+                                     int H, int k, int n_tokens, int n_pages, int page_size, int max_pages, int D,
+                                     size_t q_token_stride, size_t k_page_stride, size_t v_page_stride, float scale, int causal,
+                                     int dtype, void* workspace, size_t workspace_bytes, void* stream);
+
 /* Blocking read of the status a decode/prefill call left in `workspace`
  * (synchronises `stream`).  *status_out receives a chai_status_t. */
 int chai_device_status(const void* workspace, int* status_out, void* stream);

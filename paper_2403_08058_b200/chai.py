@@ -33,6 +33,9 @@ EXPORTS = [
     "chai_set_decode_wait_limit_cycles",
     "chai_append_kv_paged", "chai_append_kv_paged_fp8", "chai_read_kv_paged", "chai_read_kv_paged_fp8",
     "chai_decode_paged_workspace_bytes", "chai_decode_attention_paged", "chai_decode_attention_paged_fp8",
+    "chai_plan_paged", "chai_plan_paged_workspace_bytes", "chai_rope_frequencies", "chai_rope", "chai_append_rope_paged",
+    "chai_append_rope_paged_fp8", "chai_prefill_paged_workspace_bytes", "chai_prefill_attention_paged",
+    "chai_prefill_attention_paged_fp8",
 ]
 DECODE_STATIC_SCRATCH_BYTES = 8 << 20   # CHAI_DECODE_STATIC_SCRATCH_BYTES
 
@@ -95,6 +98,17 @@ def load() -> ctypes.CDLL:
     lib.chai_decode_paged_workspace_bytes.restype = sz
     lib.chai_decode_attention_paged.argtypes = [vp] * 8 + [ci] * 7 + [sz, sz, cf, ci, vp, sz, vp]
     lib.chai_decode_attention_paged_fp8.argtypes = [vp] * 10 + [ci] * 7 + [sz, sz, cf, ci, vp, sz, vp]
+    lib.chai_plan_paged_workspace_bytes.argtypes = [ci]
+    lib.chai_plan_paged_workspace_bytes.restype = sz
+    lib.chai_plan_paged.argtypes = [vp] * 11 + [ci] * 5 + [vp, sz, vp]
+    lib.chai_rope_frequencies.argtypes = [vp, vp, ci, ci, vp]
+    lib.chai_rope.argtypes = [vp] * 6 + [ci] * 7 + [vp, vp, ci, vp]
+    lib.chai_append_rope_paged.argtypes = [vp] * 11 + [ci, ci, vp] + [ci] * 7 + [sz] * 5 + [ci, vp, vp]
+    lib.chai_append_rope_paged_fp8.argtypes = [vp] * 13 + [ci, ci, vp] + [ci] * 7 + [sz] * 5 + [ci, vp, vp]
+    lib.chai_prefill_paged_workspace_bytes.argtypes = [ci, ci, ci]
+    lib.chai_prefill_paged_workspace_bytes.restype = sz
+    lib.chai_prefill_attention_paged.argtypes = [vp] * 9 + [ci] * 8 + [sz] * 3 + [cf, ci, ci, vp, sz, vp]
+    lib.chai_prefill_attention_paged_fp8.argtypes = [vp] * 11 + [ci] * 8 + [sz] * 3 + [cf, ci, ci, vp, sz, vp]
     lib.chai_status_string.argtypes = [ci]
     lib.chai_status_string.restype = ctypes.c_char_p
     lib.chai_last_error.restype = ctypes.c_char_p
@@ -502,8 +516,8 @@ def _want(t, name, shape, dtype, dev) -> None:
 _E4M3 = (torch.uint8, torch.float8_e4m3fn)
 
 
-def _pages(k_pages, v_pages, k_scales, v_scales, block_table, seq_lens):
-    """Checks a pool and its tables; returns (n_pages, k, H, page_size, D, page strides, B, max_pages, device index)."""
+def _pool_shapes(k_pages, v_pages, k_scales, v_scales):
+    """Checks a pool; returns (n_pages, k, H, page_size, D, page strides, device index)."""
     if k_pages.dim() != 4 or v_pages.dim() != 4:
         raise ValueError("k_pages must be [n_pages,k,page_size,D] and v_pages [n_pages,H,page_size,D]")
     n, k, ps, D = k_pages.shape
@@ -530,6 +544,12 @@ def _pages(k_pages, v_pages, k_scales, v_scales, block_table, seq_lens):
             raise TypeError(f"e4m3 pages must be uint8 or float8_e4m3fn, got {k_pages.dtype} and {v_pages.dtype}")
         _want(k_scales, "k_scales", (n, k, ps), torch.float32, dev)
         _want(v_scales, "v_scales", (n, H, ps), torch.float32, dev)
+    return n, k, H, ps, D, k_stride, v_stride, dev
+
+
+def _pages(k_pages, v_pages, k_scales, v_scales, block_table, seq_lens):
+    """Checks a pool and its tables; returns (n_pages, k, H, page_size, D, page strides, B, max_pages, device index)."""
+    n, k, H, ps, D, k_stride, v_stride, dev = _pool_shapes(k_pages, v_pages, k_scales, v_scales)
     if block_table.dim() != 2:
         raise ValueError("block_table must be [B,max_pages]")
     B, max_pages = block_table.shape
@@ -676,6 +696,246 @@ def chai_decode_attention_paged_fp8(q, k_pages, v_pages, k_scales, v_scales, mem
     """The same over e4m3 pages with one scale per row, as chai_append_kv_paged_fp8 writes them; q float32 or bfloat16."""
     return _decode_paged("chai_decode_attention_paged_fp8", q, k_pages, v_pages, k_scales, v_scales, membership, reps,
                          block_table, seq_lens, scale, out, workspace)
+
+
+# ---- a serving step of many tokens ------------------------------------------------------------------------------
+
+def chai_plan_paged(seq_lens, new_lens, block_table, free_pages, free_count, n_tokens: int, page_size: int, kv_lens=None,
+                    free_count_out=None, token_start=None, token_request=None, positions=None, slots=None, workspace=None):
+    """Pages for a step's tokens, from a stack of free pages: seq_lens [B] (cached positions), new_lens [B] (tokens that each
+    request gets; below 0: it ends and its pages go back), block_table [B,max_pages] and free_pages [n_pages] (both written),
+    free_count [1], all int32 -> (kv_lens [B], token_start [B+1], token_request [n_tokens], positions [n_tokens], slots
+    [n_tokens] int64).  kv_lens may be seq_lens; free_count is updated in place unless free_count_out is given."""
+    if block_table.dim() != 2 or free_pages.dim() != 1:
+        raise ValueError("block_table must be [B,max_pages] and free_pages [n_pages]")
+    (B, max_pages), n_pages, dev = block_table.shape, free_pages.shape[0], block_table.get_device()
+    if dev < 0:
+        raise ValueError("tensors must be contiguous CUDA tensors")
+    i32 = torch.int32
+    _want(block_table, "block_table", (B, max_pages), i32, dev)
+    _want(free_pages, "free_pages", (n_pages,), i32, dev)
+    _want(free_count, "free_count", (1,), i32, dev)
+    _want(seq_lens, "seq_lens", (B,), i32, dev)
+    _want(new_lens, "new_lens", (B,), i32, dev)
+    if free_count_out is None:
+        free_count_out = free_count
+    else:
+        _want(free_count_out, "free_count_out", (1,), i32, dev)
+    like = block_table.device
+    if kv_lens is None:
+        kv_lens = torch.empty((B,), device=like, dtype=i32)
+    else:
+        _want(kv_lens, "kv_lens", (B,), i32, dev)
+    if token_start is None:
+        token_start = torch.empty((B + 1,), device=like, dtype=i32)
+    else:
+        _want(token_start, "token_start", (B + 1,), i32, dev)
+    if token_request is None:
+        token_request = torch.empty((n_tokens,), device=like, dtype=i32)
+    else:
+        _want(token_request, "token_request", (n_tokens,), i32, dev)
+    if positions is None:
+        positions = torch.empty((n_tokens,), device=like, dtype=i32)
+    else:
+        _want(positions, "positions", (n_tokens,), i32, dev)
+    if slots is None:
+        slots = torch.empty((n_tokens,), device=like, dtype=torch.int64)
+    else:
+        _want(slots, "slots", (n_tokens,), torch.int64, dev)
+    if workspace is None:
+        workspace = new_workspace(512 + 4 * B, like)
+    ws, ws_bytes = _paged_workspace(workspace, dev)
+    _paged_call(load().chai_plan_paged, dev, seq_lens.data_ptr(), new_lens.data_ptr(), block_table.data_ptr(),
+                free_pages.data_ptr(), free_count.data_ptr(), free_count_out.data_ptr(), kv_lens.data_ptr(),
+                token_start.data_ptr(), token_request.data_ptr(), positions.data_ptr(), slots.data_ptr(), B, n_tokens, n_pages,
+                page_size, max_pages, ws, ws_bytes)
+    return kv_lens, token_start, token_request, positions, slots
+
+
+ROPE_SCALINGS = {"plain": 0, "linear": 1, "base": 2, "ramp": 3, "bands": 4}   # CHAI_ROPE_*
+
+
+def chai_rope_frequencies(rot: int, base: float = 10000.0, scaling: str = "plain", factor: float = 1.0, context: float = 0.0,
+                          low: float = 1.0, high: float | None = None, device=None):
+    """Frequencies of rotary positions: (turns [rot/2] float64 on `device`, the magnitude that goes with them).  scaling:
+    "plain", "linear", "base", "ramp" (high 32 unless given) or "bands" (high 4 unless given); see the header."""
+    if scaling not in ROPE_SCALINGS:
+        raise ValueError(f"scaling must be one of {sorted(ROPE_SCALINGS)}")
+    if high is None:
+        high = 32.0 if scaling == "ramp" else 4.0
+    turns = torch.empty((max(int(rot) // 2, 1),), dtype=torch.float64)
+    magnitude = ctypes.c_double(1.0)
+    _check(load().chai_rope_frequencies(turns.data_ptr(), ctypes.addressof(magnitude), rot, ROPE_SCALINGS[scaling],
+                                        (ctypes.c_double * 5)(base, factor, context, low, high)))
+    return (turns if device is None else turns.to(device)), magnitude.value
+
+
+def _double(x: float):
+    return ctypes.byref(ctypes.c_double(x))
+
+
+def _turns(turns, dev):
+    """(pointer, rot) of the frequencies, which may be None."""
+    if turns is None:
+        return None, 0
+    _want(turns, "turns", (turns.numel(),), torch.float64, dev)
+    return turns.data_ptr(), 2 * turns.numel()
+
+
+def chai_rope(q, k=None, positions=None, turns=None, magnitude: float = 1.0, interleaved: bool = False, q_out=None, k_out=None):
+    """q [B,Hq,N,D] and k [B,Hk,N,D] (or None) rotated by positions [B,N] int32 (None: 0 .. N-1) -> (q_out, k_out), new arrays
+    of the same strides unless given (they may be q and k themselves).  Any strides with contiguous rows, e.g.
+    x.transpose(1, 2) of [B,N,H,D]."""
+    if q.dim() != 4:
+        raise ValueError("q must be [B,Hq,N,D]")
+    B, Hq, N, D = q.shape
+    dev = q.get_device()
+    if dev < 0:
+        raise ValueError("q must be a CUDA tensor")
+    dtype = q.dtype
+    io = _PAGED_IO.get(dtype)
+    if io is None:
+        raise TypeError(f"unsupported dtype {dtype}")
+    Hk = 0
+    if k is not None:
+        if k.dim() != 4 or k.shape[0] != B or k.shape[2] != N or k.shape[3] != D:
+            raise ValueError(f"k must have shape ({B}, Hk, {N}, {D}), got {tuple(k.shape)}")
+        Hk = k.shape[1]
+    if q_out is None:
+        q_out = torch.empty_strided(q.shape, q.stride(), device=q.device, dtype=dtype)
+    if k_out is None and k is not None:
+        k_out = torch.empty_strided(k.shape, k.stride(), device=k.device, dtype=dtype)
+    strides = []
+    for x, out, name in ((q, q_out, "q"), (k, k_out, "k")):
+        if x is None:
+            strides += [0] * 6
+            continue
+        if x.dtype is not dtype or out.dtype is not dtype:
+            raise TypeError(f"{name} and its output must be {dtype}")
+        if out.shape != x.shape or x.get_device() != dev or out.get_device() != dev or x.stride(3) != 1 or out.stride(3) != 1:
+            raise ValueError(f"{name} and its output must have one shape, rows without gaps, and be on cuda:{dev}")
+        strides += x.stride()[:3] + out.stride()[:3]
+    if positions is not None:
+        _want(positions, "positions", (B, N), torch.int32, dev)
+    if turns is None:
+        raise ValueError("give the frequencies (chai_rope_frequencies)")
+    at, rot = _turns(turns, dev)
+    _paged_call(load().chai_rope, dev, q.data_ptr(), _ptr(k), q_out.data_ptr(), _ptr(k_out), _ptr(positions), at, B, Hq, Hk, N,
+                D, rot, 1 if interleaved else 0, _double(magnitude), (ctypes.c_int64 * 12)(*strides), io)
+    return q_out, k_out
+
+
+def _tokens(t, name, shape, dtype, dev) -> int:
+    """Checks a packed [n_tokens,H,D] array whose tokens may lie further apart; returns the distance in elements."""
+    if t.dtype is not dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.shape != shape:
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    apart, heads, one = t.stride()
+    if t.get_device() != dev or one != 1 or (heads != shape[2] and shape[1] > 1):
+        raise ValueError(f"{name} must be on cuda:{dev}, the heads of a token side by side")
+    return apart if shape[0] > 1 else 0
+
+
+def _append_rope(fn_name, q, k, v, k_pages, v_pages, k_scales, v_scales, reps, token_request, positions, slots, turns,
+                 magnitude, interleaved, q_out, workspace):
+    n, kp, H, ps, D, k_stride, v_stride, dev = _pool_shapes(k_pages, v_pages, k_scales, v_scales)
+    io = _PAGED_IO.get(q.dtype)
+    if io is None or (k_scales is None and q.dtype is not k_pages.dtype):
+        raise TypeError(f"tokens of type {q.dtype} do not go into pages of type {k_pages.dtype}")
+    n_tokens = q.shape[0]
+    shape = (n_tokens, H, D)
+    apart = [_tokens(t, name, shape, q.dtype, dev) for t, name in ((q, "q"), (k, "k"), (v, "v"))]
+    if q_out is None:
+        q_out = torch.zeros(shape, device=q.device, dtype=q.dtype)
+    else:
+        _want(q_out, "q_out", shape, q.dtype, dev)
+    if reps.dim() != 2:
+        raise ValueError("reps must be [B,k]")
+    _want(reps, "reps", (reps.shape[0], kp), torch.int32, dev)
+    _want(token_request, "token_request", (n_tokens,), torch.int32, dev)
+    _want(positions, "positions", (n_tokens,), torch.int32, dev)
+    _want(slots, "slots", (n_tokens,), torch.int64, dev)
+    at, rot = _turns(turns, dev)
+    ws, ws_bytes = _paged_workspace(workspace, dev)
+    if workspace is not None and ws_bytes < 256:
+        raise ValueError("workspace must hold at least 256 bytes")
+    scales = () if k_scales is None else (k_scales.data_ptr(), v_scales.data_ptr())
+    _paged_call(getattr(load(), fn_name), dev, q.data_ptr(), k.data_ptr(), v.data_ptr(), q_out.data_ptr(), k_pages.data_ptr(),
+                v_pages.data_ptr(), *scales, reps.data_ptr(), token_request.data_ptr(), positions.data_ptr(), slots.data_ptr(),
+                at, rot, 1 if interleaved else 0, _double(magnitude), reps.shape[0], H, kp, n_tokens, n, ps, D, *apart, k_stride,
+                v_stride, io, ws)
+    return q_out
+
+
+def chai_append_rope_paged(q, k, v, k_pages, v_pages, reps, token_request, positions, slots, turns, magnitude: float = 1.0,
+                           interleaved: bool = False, q_out=None, workspace=None):
+    """A packed batch enters a paged cache: q, k, v [n_tokens,H,D] (they may be parts of one projection's output), where
+    each token goes as chai_plan_paged says, turns from chai_rope_frequencies (None: no rotation).  Writes the rotated keys of
+    representatives and all values, and returns q_out [n_tokens,H,D] with the representatives' queries rotated (other rows: as
+    they were, zeros in an array made here)."""
+    return _append_rope("chai_append_rope_paged", q, k, v, k_pages, v_pages, None, None, reps, token_request, positions, slots,
+                        turns, magnitude, interleaved, q_out, workspace)
+
+
+def chai_append_rope_paged_fp8(q, k, v, k_pages, v_pages, k_scales, v_scales, reps, token_request, positions, slots, turns,
+                               magnitude: float = 1.0, interleaved: bool = False, q_out=None, workspace=None):
+    """The same into e4m3 pages with one power-of-two scale per row (see chai_append_kv_paged_fp8)."""
+    return _append_rope("chai_append_rope_paged_fp8", q, k, v, k_pages, v_pages, k_scales, v_scales, reps, token_request,
+                        positions, slots, turns, magnitude, interleaved, q_out, workspace)
+
+
+def chai_prefill_paged_workspace_bytes(B, H, n_tokens) -> int:
+    return int(load().chai_prefill_paged_workspace_bytes(B, H, n_tokens))
+
+
+def _prefill_paged(fn_name, q, k_pages, v_pages, k_scales, v_scales, membership, reps, block_table, kv_lens, token_start, scale,
+                   causal, out, workspace):
+    n, k, H, ps, D, k_stride, v_stride, dev = _pool_shapes(k_pages, v_pages, k_scales, v_scales)
+    io = _PAGED_IO.get(q.dtype)
+    if io is None or (k_scales is None and q.dtype is not k_pages.dtype):
+        raise TypeError(f"queries of type {q.dtype} do not go with pages of type {k_pages.dtype}")
+    if block_table.dim() != 2:
+        raise ValueError("block_table must be [B,max_pages]")
+    B, max_pages = block_table.shape
+    i32 = torch.int32
+    _want(block_table, "block_table", (B, max_pages), i32, dev)
+    _want(kv_lens, "kv_lens", (B,), i32, dev)
+    _want(token_start, "token_start", (B + 1,), i32, dev)
+    _want(membership, "membership", (B, H), i32, dev)
+    _want(reps, "reps", (B, k), i32, dev)
+    n_tokens = q.shape[0]
+    shape = (n_tokens, H, D)
+    apart = _tokens(q, "q", shape, q.dtype, dev)
+    if out is None:
+        out = torch.zeros(shape, device=q.device, dtype=q.dtype)
+    else:
+        _want(out, "out", shape, q.dtype, dev)
+    if workspace is None:
+        workspace = new_workspace(chai_prefill_paged_workspace_bytes(B, H, n_tokens), q.device)
+    ws, ws_bytes = _paged_workspace(workspace, dev)
+    scales = () if k_scales is None else (k_scales.data_ptr(), v_scales.data_ptr())
+    _paged_call(getattr(load(), fn_name), dev, q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), *scales,
+                membership.data_ptr(), reps.data_ptr(), block_table.data_ptr(), kv_lens.data_ptr(), token_start.data_ptr(),
+                out.data_ptr(), B, H, k, n_tokens, n, ps, max_pages, D, apart, k_stride, v_stride, scale, 1 if causal else 0, io,
+                ws, ws_bytes)
+    return out
+
+
+def chai_prefill_attention_paged(q, k_pages, v_pages, membership, reps, block_table, kv_lens, token_start, scale: float,
+                                 causal: bool = True, out=None, workspace=None):
+    """Clustered attention of a packed batch over a paged cache: q [n_tokens,H,D], rows token_start[b] .. token_start[b+1]-1
+    of request b, whose cached positions are kv_lens[b] with the new tokens last (causal), or all seen by every token
+    -> out [n_tokens,H,D].  Rows behind token_start[B] are left as they were (zeros in an array made here)."""
+    return _prefill_paged("chai_prefill_attention_paged", q, k_pages, v_pages, None, None, membership, reps, block_table, kv_lens,
+                          token_start, scale, causal, out, workspace)
+
+
+def chai_prefill_attention_paged_fp8(q, k_pages, v_pages, k_scales, v_scales, membership, reps, block_table, kv_lens,
+                                     token_start, scale: float, causal: bool = True, out=None, workspace=None):
+    """The same over e4m3 pages with one scale per row; q float32 or bfloat16."""
+    return _prefill_paged("chai_prefill_attention_paged_fp8", q, k_pages, v_pages, k_scales, v_scales, membership, reps,
+                          block_table, kv_lens, token_start, scale, causal, out, workspace)
 
 
 def chai_set_decode_wait_limit_cycles(cycles: int) -> None:

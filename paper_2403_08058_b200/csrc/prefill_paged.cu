@@ -1,0 +1,835 @@
+// Clustered attention of packed tokens over a paged cache: a prompt's chunk behind what is cached of it, guessed tokens that are
+// verified at once, a batch that mixes chunks and single tokens, or queries over states of another length without a mask.
+// The entry points, and the kernel on the 5th-generation tensor cores (tcgen05 + TMEM + TMA) for bf16; 32-bit queries run on
+// the CUDA cores (prefill_paged_simt.cu).
+//
+// The arithmetic is prefill_tc.cu's: S = Q K^T of a tile of 128 query rows and 128 keys into tensor memory, the softmax against
+// a reference that moves only when a row's maximum leaves a window of 2^32 around it, P as bf16 in tensor memory, O_g += P V_g
+// for the members of a cluster, two at a time (head_dim 64: four).  P is rounded to bf16, at most 2^-8 of each
+// probability, because that is the tensor core's type beside bf16 values; row sums are of the unrounded ones, in fp32.
+// What differs:
+//   - keys and values come from pages.  A page's rows are whole 8-row groups of the swizzled tile (page sizes are multiples of 8), so a
+//     tile is filled by boxes of as many rows as divide both the page size and 128; the lanes of the loading warp look up
+//     and issue one box each.  Tables are looked up a tile ahead.
+//   - rows behind a request's length are never used, whatever they hold: their scores are masked, and their values, which
+//     would meet probabilities of zero, are zeroed in shared memory before the last tile is multiplied.
+//   - a request may have few tokens: rows that it does not have cost tensor work but no softmax, and there may be too few
+//     tiles for the GPU: key tiles are divided into pieces (prefill_paged.cuh), whose accumulators leave unnormalised and are joined
+//     by the warp that finishes a row's last piece, in order of the pieces.
+// Bound by the cache's bytes for few tokens a request, by the softmax chain of a tile (as in prefill_tc.cu) for many.
+#include <cuda.h>
+#include <math.h>
+
+#include <atomic>
+
+#include "prefill_paged.cuh"
+#include "tc_ptx.cuh"
+
+namespace chai {
+
+int prefill_paged_simt_rows(int B, int n_tokens);
+int prefill_paged_simt(const PagedCall& a, int D, bool fp8, cudaStream_t s);
+
+namespace pp {
+
+using namespace tcx;
+
+constexpr int BM = 128, BN = 128;
+constexpr int GMAX = 4;
+constexpr int KST = 2;                       // key tile stages: tile kt uses stage kt & 1
+constexpr int TILE_BYTES = BN * 128 * 2;     // a tile slot (head_dim 64: two members' value tiles share one)
+constexpr int HALF_BYTES = TILE_BYTES / 2;   // 128 rows x 64 columns, 128-byte swizzled rows
+constexpr int SOFTMAX_WARPS = 8, EPILOGUE_WARPS = 4;
+constexpr int PV_WARP = 2 + SOFTMAX_WARPS + EPILOGUE_WARPS;
+constexpr int THREADS = 96 + (SOFTMAX_WARPS + EPILOGUE_WARPS) * 32;
+constexpr float REF_WINDOW = 32.f;
+constexpr uint32_t TMEM_COLS = 512;
+constexpr uint32_t S_COL0 = 0, P_COL0 = 128, O_COL0 = 256;
+
+// shared memory map (offsets from a 1024-byte aligned base)
+constexpr int OFF_Q = 0;
+constexpr int OFF_K = OFF_Q + TILE_BYTES;
+constexpr int OFF_V = OFF_K + KST * TILE_BYTES;
+constexpr int OFF_BAR = OFF_V + 4 * TILE_BYTES;
+constexpr int NUM_BARS = 23;
+constexpr int OFF_XCH = OFF_BAR + 8 * NUM_BARS + 16;
+constexpr int OFF_LSUM = OFF_XCH + 2 * BM * 4;       // [half][row] sums
+constexpr int OFF_REF = OFF_LSUM + 2 * BM * 4;       // [row] reference of the exponentials
+constexpr int OFF_ITEM = OFF_REF + BM * 4;
+constexpr int ITEM_BYTES = 64;
+constexpr int SMEM_BYTES = OFF_ITEM + 3 * ITEM_BYTES;
+static_assert(SMEM_BYTES <= 232448, "shared memory budget");
+
+struct Bars {
+    uint32_t base;
+    __device__ __forceinline__ uint32_t q_full() const { return base; }
+    __device__ __forceinline__ uint32_t q_empty() const { return base + 8; }
+    __device__ __forceinline__ uint32_t o_free(int g) const { return g == 0 ? base + 16 : base + 8 * (18 + g); }
+    __device__ __forceinline__ uint32_t p_full(int i) const { return i == 0 ? base + 24 : base + 8 * 22; }
+    __device__ __forceinline__ uint32_t item_full(int i) const { return base + 8 * (4 + i); }
+    __device__ __forceinline__ uint32_t item_empty(int i) const { return base + 8 * (6 + i); }
+    __device__ __forceinline__ uint32_t k_full(int i) const { return base + 8 * (8 + i); }
+    __device__ __forceinline__ uint32_t v_full(int i) const { return base + 8 * (10 + i); }
+    __device__ __forceinline__ uint32_t qk_done(int i) const { return base + 8 * (12 + i); }
+    __device__ __forceinline__ uint32_t pv_done(int i) const { return base + 8 * (14 + i); }
+    __device__ __forceinline__ uint32_t epi_full() const { return base + 8 * 16; }
+    __device__ __forceinline__ uint32_t epi_empty() const { return base + 8 * 17; }
+    __device__ __forceinline__ uint32_t s_free() const { return base + 8 * 18; }
+};
+static_assert(NUM_BARS == 23, "barrier count");
+
+// One unit of work, published by the loading warp to the other roles through shared memory.
+struct Item {
+    int n_kv;       // key tiles to walk; 0: zero rows (no keys, unresolved heads); -1: no more work
+    int n_members;
+    int row0;       // first row of the packed arrays
+    int rows;       // rows of the tile that exist
+    int col0;       // first position of the first tile
+    int sees;       // positions that row 0 sees; row r: r more, at most kv (unmasked: kv)
+    int kv;
+    int pieces, piece, slot, counter;
+    int heads[GMAX];
+    int pad;
+};
+static_assert(sizeof(Item) == ITEM_BYTES, "item descriptor");
+
+struct Tma {
+    CUtensorMap q, k, v;
+};
+
+template <int HD>
+__global__ void __launch_bounds__(THREADS, 1)
+prefill_paged_kernel(const __grid_constant__ Tma maps, const PagedCall a, const int box_rows, const float scale_log2) {
+    constexpr int GM = HD == 128 ? 2 : 4, HALVES = HD / 64, ROW_BYTES = HD * 2;
+    constexpr int V_TILE = BN * ROW_BYTES;   // distance between the members' value tiles
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    extern __shared__ uint8_t smem[];
+    const uint32_t sbase = smem_u32(smem);
+    if ((sbase & 1023u) != 0) {  // swizzled tiles need it; a kernel without static shared memory has it
+        asm volatile("griddepcontrol.wait;" ::: "memory");
+        if (tid == 0) atomicExch(&a.hdr->status, CHAI_ERR_TIMEOUT);
+        return;
+    }
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + OFF_BAR + 8 * NUM_BARS);
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+    Item* items = reinterpret_cast<Item*>(smem + OFF_ITEM);  // [2] to the issuers and softmax warps, [2] = to the epilogue
+    const Bars bar{sbase + OFF_BAR};
+
+    if (tid == 0) {
+        mbar_init(bar.q_full(), 1);
+        mbar_init(bar.q_empty(), 1);
+        for (int g = 0; g < GMAX; ++g) mbar_init(bar.o_free(g), EPILOGUE_WARPS);
+        mbar_init(bar.epi_full(), SOFTMAX_WARPS);
+        mbar_init(bar.epi_empty(), EPILOGUE_WARPS);
+        mbar_init(bar.s_free(), SOFTMAX_WARPS);
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(bar.p_full(i), SOFTMAX_WARPS);
+            mbar_init(bar.item_full(i), 1);
+            mbar_init(bar.item_empty(i), 2 + SOFTMAX_WARPS);
+            mbar_init(bar.k_full(i), 1);
+            mbar_init(bar.v_full(i), 1);
+            mbar_init(bar.qk_done(i), 1);
+            mbar_init(bar.pv_done(i), 1);
+        }
+        *abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        fence_async_proxy();
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(TMEM_COLS) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem_base = *tmem_slot;
+
+    if (warp == 0) {
+        // ---------------- work distribution and loads, by all lanes ----------------
+        auto wait_all = [&](uint32_t b, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait(b, parity, abort_flag)); };
+        const int n_items = __ldcg(&a.hdr->pad[kPagedItems]);
+        const int blocks = BN / box_rows;                    // boxes of a tile, per 64 columns
+        auto claim = [&]() { return __shfl_sync(0xffffffffu, lane == 0 ? atomicAdd(&a.hdr->pad[kPagedCounter], 1) : 0, 0); };
+        bool ok = true;
+        int it = 0, qi = 0, kt = 0;                          // items published, items with loads, key tiles issued
+        int id = claim();
+        GroupEntry e, e_next;
+        PagedItem cur = {}, nxt = {};
+        if (id < n_items) cur = paged_item(a, id, &e);
+        while (ok) {
+            const int next_id = claim();                     // (looked at when this item's loads are on their way)
+            if (id < n_items && cur.n_kv < 0) {              // nothing to do
+                id = next_id;
+                if (id < n_items) cur = paged_item(a, id, &e);
+                continue;
+            }
+            const int is = it & 1;
+            ok = wait_all(bar.item_empty(is), ((it >> 1) & 1) ^ 1);
+            if (!ok) break;
+            if (id >= n_items) {
+                if (lane == 0) {
+                    items[is].n_kv = -1;
+                    mbar_arrive(bar.item_full(is));
+                }
+                break;
+            }
+            const int n_kv = cur.n_kv, n_members = min(e.n, GM), col0 = cur.first_tile * BN, kv = cur.kv, b = cur.b;
+            if (lane == 0) {
+                Item& item = items[is];
+                item.n_kv = n_kv;
+                item.n_members = n_members;
+                item.row0 = cur.q0;
+                item.rows = cur.rows;
+                item.col0 = col0;
+                item.kv = kv;
+                item.sees = a.causal ? kv - cur.n + (cur.q0 - __ldcg(&a.req[b].start)) + 1 : kv;
+                item.pieces = cur.pieces;
+                item.piece = cur.piece;
+                item.slot = cur.slot;
+                item.counter = cur.counter;
+                for (int g = 0; g < GMAX; ++g) item.heads[g] = e.heads[g < n_members ? g : 0];
+                mbar_arrive(bar.item_full(is));
+            }
+            __syncwarp();
+            ++it;
+            if (n_kv == 0) {
+                id = next_id;
+                if (id < n_items) cur = paged_item(a, id, &e);
+                continue;
+            }
+            // queries: wait until the previous item's last S = Q K^T has been computed
+            ok = wait_all(bar.q_empty(), (qi & 1) ^ 1);
+            if (!ok) break;
+            if (lane == 0) {
+                mbar_expect_tx(bar.q_full(), BM * ROW_BYTES);
+#pragma unroll
+                for (int h = 0; h < HALVES; ++h)
+                    tma_load_3d(sbase + OFF_Q + h * HALF_BYTES, &maps.q, h * 64, e.rep, cur.q0, bar.q_full());
+            }
+            __syncwarp();
+            // Lane l knows the place of box l of a tile: page and first row in it.
+            const int32_t* table = a.pool.block_table + (size_t)b * a.pool.max_pages;
+            auto boxes = [&](int j) { return (min(BN, kv - (col0 + j * BN)) + box_rows - 1) / box_rows; };  // that hold rows
+            auto look_up = [&](int j, int& page, int& row) {
+                const int pos = col0 + j * BN + lane * box_rows;
+                page = -1;
+                row = 0;
+                if (j < n_kv && lane < blocks && pos < kv) {
+                    const int pi = (int)a.pool.by_page.div((unsigned)pos);
+                    row = pos - pi * a.pool.page_size;
+                    page = table[pi];  // (an entry that is no page: outside the map, zeros arrive)
+                }
+            };
+            // `count` boxes x HALVES of plane `plane` to dst
+            auto issue = [&](const CUtensorMap* map, int plane, uint32_t dst, uint32_t full, int count, int page, int row) {
+#pragma unroll 1
+                for (int base = 0; base < count * HALVES; base += 32) {
+                    const int i = base + lane, blk = i / HALVES, h = i % HALVES;
+                    const int p = __shfl_sync(0xffffffffu, page, blk & 31), r = __shfl_sync(0xffffffffu, row, blk & 31);
+                    if (i < count * HALVES)
+                        tma_load_page(dst + h * HALF_BYTES + blk * box_rows * 128, map, h * 64, r, plane, p, full);
+                }
+            };
+            int page_v, row_v, page_k, row_k, page_n, row_n;
+            look_up(0, page_v, row_v);
+            look_up(1, page_k, row_k);
+            auto load_k = [&](int j, int page, int row) -> bool {
+                const int n = kt + j, ts = n & 1, count = boxes(j);
+                if (!wait_all(bar.qk_done(ts), ((n >> 1) & 1) ^ 1)) return false;  // stage free
+                if (lane == 0) mbar_expect_tx(bar.k_full(ts), count * box_rows * ROW_BYTES);
+                __syncwarp();
+                issue(&maps.k, e.cluster, sbase + OFF_K + ts * TILE_BYTES, bar.k_full(ts), count, page, row);
+                return true;
+            };
+            // order of need: K(0), K(1), V(0), K(2), V(1), ...
+            ok = load_k(0, page_v, row_v);
+            for (int j = 0; j < n_kv && ok; ++j) {
+                look_up(j + 2, page_n, row_n);
+                if (j + 1 < n_kv) ok = load_k(j + 1, page_k, row_k);
+                if (!ok) break;
+                const int n = kt + j, ts = n & 1, count = boxes(j);
+                ok = wait_all(bar.pv_done(ts), ((n >> 1) & 1) ^ 1);  // the tile's value slots are free
+                if (!ok) break;
+                if (lane == 0) mbar_expect_tx(bar.v_full(ts), n_members * count * box_rows * ROW_BYTES);
+                __syncwarp();
+#pragma unroll
+                for (int g = 0; g < GM; ++g)
+                    if (g < n_members)
+                        issue(&maps.v, e.heads[g], sbase + OFF_V + ts * 2 * TILE_BYTES + g * V_TILE, bar.v_full(ts), count, page_v, row_v);
+                if (j == 0 && next_id < n_items) nxt = paged_item(a, next_id, &e_next);
+                page_v = page_k, row_v = row_k;
+                page_k = page_n, row_k = row_n;
+            }
+            kt += n_kv;
+            ++qi;
+            cur = nxt;
+            e = e_next;
+            id = next_id;
+        }
+    } else if (warp == 1 || warp == PV_WARP) {
+        // ---------------- MMA issuers ----------------
+        constexpr uint32_t IDESC_QK = make_idesc(false);
+        auto desc = [](uint32_t hi, uint32_t lo) { return ((uint64_t)hi << 32) | lo; };
+        auto wait_all = [&](uint32_t b, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait_polling(b, parity, abort_flag)); };
+        const bool qk_role = warp == 1;
+        const uint64_t dq = make_desc(sbase + OFF_Q, 16, 1024);
+        const uint64_t dk = make_desc(sbase + OFF_K, 16, 1024);
+        const uint64_t dv = make_desc(sbase + OFF_V, HALF_BYTES, 1024);
+        const uint32_t hi_k = (uint32_t)(dq >> 32), hi_v = (uint32_t)(dv >> 32);
+        const uint32_t q_lo = (uint32_t)dq, k_lo = (uint32_t)dk, v_lo = (uint32_t)dv;
+        bool ok = true;
+        int it = 0, qi = 0, kt = 0;
+        while (ok) {
+            const int is = it & 1;
+            ok = wait_all(bar.item_full(is), (it >> 1) & 1);
+            if (!ok) break;
+            const int n_kv = items[is].n_kv, n_members = items[is].n_members, left = items[is].kv - items[is].col0;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar.item_empty(is));
+            if (n_kv < 0) break;
+            ++it;
+            if (n_kv == 0) continue;
+            if (qk_role) {
+                ok = wait_all(bar.q_full(), qi & 1);
+                for (int j = 0; j < n_kv && ok; ++j, ++kt) {
+                    const int ts = kt & 1;
+                    ok = wait_all(bar.k_full(ts), (kt >> 1) & 1) && (kt == 0 || wait_all(bar.s_free(), (kt - 1) & 1));
+                    if (!ok) break;
+                    tc_fence_after();
+                    const uint32_t d = tmem_base + S_COL0;
+                    const uint32_t kb = k_lo + ts * (TILE_BYTES >> 4);
+                    if (elect_one()) {
+#pragma unroll
+                        for (int s = 0; s < HD / 16; ++s) {
+                            const uint32_t off = ((s >> 2) * HALF_BYTES + (s & 3) * 32) >> 4;
+                            tc_mma(d, desc(hi_k, q_lo + off), desc(hi_k, kb + off), IDESC_QK, s > 0);
+                        }
+                        tc_commit(bar.qk_done(ts));
+                        if (j + 1 == n_kv) tc_commit(bar.q_empty());
+                    }
+                    __syncwarp();
+                }
+            } else {
+                for (int j = 0; j < n_kv && ok; ++j, ++kt) {
+                    const int ts = kt & 1;
+                    ok = wait_all(bar.v_full(ts), (kt >> 1) & 1);
+                    if (!ok) break;
+                    const int valid = left - j * BN;
+                    if (valid < BN) {  // rows behind the request's length: zeros, whatever is there
+                        const int per = (BN - valid) * 8, total = n_members * HALVES * per;
+                        for (int i = lane; i < total; i += 32) {
+                            const int m = i / per, r = i - m * per;
+                            const uint32_t at = sbase + OFF_V + ts * 2 * TILE_BYTES + (m / HALVES) * V_TILE + (m % HALVES) * HALF_BYTES + valid * 128 + r * 16;
+                            asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(at), "r"(0) : "memory");
+                        }
+                        fence_async_proxy();
+                        __syncwarp();
+                    }
+                    ok = wait_all(bar.p_full(ts), (kt >> 1) & 1);
+                    if (!ok) break;
+                    const uint32_t p_addr = tmem_base + P_COL0 + ts * 64;
+                    if (j == 0 && qi > 0)  // the accumulators still hold the previous item's output
+                        for (int g = 0; g < n_members && ok; ++g) ok = wait_all(bar.o_free(g), (qi - 1) & 1);
+                    if (!ok) break;
+                    tc_fence_after();
+                    if (elect_one()) {
+                        const uint32_t d = tmem_base + O_COL0;
+                        const uint32_t vb = v_lo + (ts * 2) * (TILE_BYTES >> 4);
+                        const uint32_t idesc_all = make_idesc_n(true, (unsigned)(HD * n_members));
+#pragma unroll
+                        for (int s = 0; s < BN / 16; ++s)
+                            tc_mma_ts(d, p_addr + s * 8, desc(hi_v, vb + s * (2048 >> 4)), idesc_all, (j > 0 || s > 0) ? 1u : 0u);
+                        tc_commit(bar.pv_done(ts));
+                    }
+                    __syncwarp();
+                }
+            }
+            ++qi;
+        }
+    } else if (warp < 2 + SOFTMAX_WARPS) {
+        // ---------------- softmax / correction: two threads per query row ----------------
+        const int quad = warp & 3, half = (warp - 2) >> 2;
+        const int row = quad * 32 + lane, cbase = half * 64;
+        const uint32_t lane_addr = tmem_base + ((uint32_t)(quad * 32) << 16);
+        __nv_bfloat16* xch = reinterpret_cast<__nv_bfloat16*>(smem + OFF_XCH);  // [tile parity][half][row]
+        float* lsum = reinterpret_cast<float*>(smem + OFF_LSUM);
+        float* refs = reinterpret_cast<float*>(smem + OFF_REF);
+        bool ok = true;
+        int it = 0, ei = 0, kt = 0;
+        uint32_t r[64];
+        while (true) {
+            const int is = it & 1;
+            ok = ok && mbar_wait(bar.item_full(is), (it >> 1) & 1, abort_flag);
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) break;
+            const int n_kv = items[is].n_kv, n_members = items[is].n_members, rows = items[is].rows;
+            const int item_col0 = items[is].col0, kv = items[is].kv, sees0 = items[is].sees;
+            // (the warp that hands the item on to the epilogue keeps it until then)
+            const bool keeps = warp == 2 && n_kv > 0;
+            if (n_kv == 0 && row < rows)
+#pragma unroll
+                for (int g = 0; g < GM; ++g) {
+                    if (g >= n_members) break;
+                    uint4* o = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(a.out) + ((size_t)(items[is].row0 + row) * a.H + items[is].heads[g]) * HD + half * (HD / 2));
+#pragma unroll
+                    for (int u = 0; u < HD / 16; ++u) o[u] = make_uint4(0, 0, 0, 0);
+                }
+            __syncwarp();
+            if (lane == 0 && !keeps) mbar_arrive(bar.item_empty(is));
+            if (n_kv < 0) break;
+            ++it;
+            if (n_kv == 0) continue;
+            const bool idle = quad * 32 >= rows;  // none of the warp's rows exists: it only keeps step
+            // positions that the row sees (a row that does not exist: none, so that it cannot move a reference)
+            const int sees = row < rows ? min(kv, a.causal ? sees0 + row : kv) : 0;
+            float m_used = 0.f, l_run = 0.f;
+            for (int j = 0; j < n_kv && ok; ++j, ++kt) {
+                const int sb = kt & 1;
+                ok = __all_sync(0xffffffffu, mbar_wait(bar.qk_done(sb), (kt >> 1) & 1, abort_flag));
+                if (!ok) break;
+                if (idle) {
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(bar.s_free());
+                    if (kt >= 2) ok = __all_sync(0xffffffffu, mbar_wait(bar.pv_done(sb), ((kt >> 1) & 1) ^ 1, abort_flag));
+                    if (!ok) break;
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(bar.p_full(sb));
+                    continue;
+                }
+                tc_fence_after();
+                const uint32_t s_addr = lane_addr + S_COL0;
+                const uint32_t p_st = lane_addr + P_COL0 + sb * 64 + half * 32;
+                const int col0 = item_col0 + j * BN;
+                const int vis = max(0, min(sees - col0 - cbase, 64));
+                const bool full_tile = col0 + BN <= min(kv, sees0) && quad * 32 + 32 <= rows;
+                tc_ld64_wait(s_addr + cbase, r);
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar.s_free());
+                if (!full_tile) {
+#pragma unroll
+                    for (int i = 0; i < 64; ++i)
+                        if (i >= vis) r[i] = 0xff800000u;
+                }
+                float mxa[8];
+#pragma unroll
+                for (int c = 0; c < 8; ++c) mxa[c] = -INFINITY;
+                __nv_bfloat16 mx_up;
+                __nv_bfloat16* xs = xch + (kt & 1) * 2 * BM;
+                auto publish = [&]() {
+                    mx_up = __float2bfloat16_ru(max3(max3(mxa[0], mxa[1], mxa[2]), max3(mxa[3], mxa[4], mxa[5]), fmaxf(mxa[6], mxa[7])));
+                    xs[half * BM + row] = mx_up;
+                };
+                float m_new = m_used, corr = 1.f;
+                auto meet = [&]() -> bool {
+                    // (the two warps of a quadrant; whoever gives up arrives once on its way out)
+                    asm volatile("bar.sync %0, 64;" ::"r"(quad + 1) : "memory");
+                    if (*abort_flag) return false;
+                    const float mx = fmaxf(__bfloat162float(mx_up), __bfloat162float(xs[(half ^ 1) * BM + row]));
+                    const float m_tile = mx * scale_log2;
+                    if (m_tile > m_used + REF_WINDOW || (j == 0 && m_tile < m_used - REF_WINDOW)) {
+                        m_new = m_tile;
+                        corr = j == 0 ? 1.f : fast_exp2(m_used - m_new);
+                    }
+                    return true;
+                };
+                auto emit = [&](float m, auto with_max) -> float {
+                    const float m_ref = m == -INFINITY ? 0.f : m;
+                    const uint64_t sc2 = pack2(scale_log2, scale_log2), nm2 = pack2(-m_ref, -m_ref);
+                    uint64_t acc01 = 0ull, acc23 = 0ull;
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        uint32_t packed[8];
+#pragma unroll
+                        for (int u = 0; u < 16; u += 4) {
+                            const int i = c * 16 + u;
+                            float x0, x1, x2, x3;
+                            unpack2(fma2(pack2(__uint_as_float(r[i]), __uint_as_float(r[i + 1])), sc2, nm2), x0, x1);
+                            unpack2(fma2(pack2(__uint_as_float(r[i + 2]), __uint_as_float(r[i + 3])), sc2, nm2), x2, x3);
+                            const float p0 = fast_exp2(x0), p1 = fast_exp2(x1), p2 = fast_exp2(x2), p3 = fast_exp2(x3);
+                            if constexpr (decltype(with_max)::value) {
+                                mxa[(i >> 1) & 7] = max3(mxa[(i >> 1) & 7], __uint_as_float(r[i]), __uint_as_float(r[i + 1]));
+                                mxa[((i >> 1) + 1) & 7] = max3(mxa[((i >> 1) + 1) & 7], __uint_as_float(r[i + 2]), __uint_as_float(r[i + 3]));
+                            }
+                            acc01 = add2(acc01, pack2(p0, p1));
+                            acc23 = add2(acc23, pack2(p2, p3));
+                            __nv_bfloat162 pa = __floats2bfloat162_rn(p0, p1), pb = __floats2bfloat162_rn(p2, p3);
+                            packed[u >> 1] = *reinterpret_cast<uint32_t*>(&pa);
+                            packed[(u >> 1) + 1] = *reinterpret_cast<uint32_t*>(&pb);
+                        }
+                        tc_st8(p_st + c * 8, packed);
+                    }
+                    float s0, s1;
+                    unpack2(add2(acc01, acc23), s0, s1);
+                    return s0 + s1;
+                };
+                if (kt >= 2) {  // P buffer kt & 1 was last read by the P V of tile kt - 2
+                    ok = __all_sync(0xffffffffu, mbar_wait(bar.pv_done(sb), ((kt >> 1) & 1) ^ 1, abort_flag));
+                    if (!ok) break;
+                    tc_fence_after();
+                }
+                float ls = emit(m_used, std::true_type{});
+                publish();
+                ok = meet();
+                if (!ok) break;
+                const bool moved = __any_sync(0xffffffffu, m_new != m_used);
+                if (moved) ls = emit(m_new, std::false_type{});
+                l_run = l_run * corr + ls;
+                m_used = m_new;
+                if (j > 0 && moved) {
+                    ok = __all_sync(0xffffffffu, mbar_wait(bar.pv_done((kt - 1) & 1), ((kt - 1) >> 1) & 1, abort_flag));
+                    if (!ok) break;
+                    tc_fence_after();
+                    for (int g = 0; g < n_members; ++g) {
+                        const uint32_t o_addr = lane_addr + O_COL0 + g * HD + half * (HD / 2);
+                        if constexpr (HD == 128) tc_ld64_wait(o_addr, r);
+                        else tc_ld32_wait(o_addr, r);
+#pragma unroll
+                        for (int i = 0; i < HD / 2; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * corr);
+                        tc_st32(o_addr, r);
+                        if constexpr (HD == 128) tc_st32(o_addr + 32, r + 32);
+                    }
+                }
+                tc_wait_st();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar.p_full(sb));
+            }
+            ok = __all_sync(0xffffffffu, ok && mbar_wait(bar.epi_empty(), (ei & 1) ^ 1, abort_flag));
+            if (!ok) break;
+            lsum[half * BM + row] = l_run;
+            if (half == 0) refs[row] = m_used;
+            if (tid == 64) {
+                items[2] = items[is];
+                items[2].n_kv = kt - 1;  // number of the item's last key tile (its P V is awaited)
+                mbar_arrive(bar.item_empty(is));
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar.epi_full());
+            ++ei;
+        }
+        if (__all_sync(0xffffffffu, mbar_wait(bar.epi_empty(), (ei & 1) ^ 1, abort_flag))) {
+            if (tid == 64) items[2].n_members = -1;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar.epi_full());
+        }
+        if (!ok) asm volatile("bar.arrive %0, 64;" ::"r"(quad + 1) : "memory");
+    } else {
+        // ---------------- epilogue: one thread per query row ----------------
+        const int quad = warp & 3, row = quad * 32 + lane;
+        const uint32_t lane_addr = tmem_base + ((uint32_t)(quad * 32) << 16);
+        const float* lsum = reinterpret_cast<const float*>(smem + OFF_LSUM);
+        const float* refs = reinterpret_cast<const float*>(smem + OFF_REF);
+        __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.out);
+        const bool wide = (reinterpret_cast<uintptr_t>(out) & 31u) == 0;
+        const size_t slot_bytes = (size_t)a.slot_rows * kSlotRowBytes, stats = (size_t)a.slot_rows * 1024;
+        for (int ei = 0;; ++ei) {
+            bool ok = __all_sync(0xffffffffu, mbar_wait(bar.epi_full(), ei & 1, abort_flag));
+            if (!ok) break;
+            const Item ep = items[2];
+            const float l = lsum[row] + lsum[BM + row], ref = refs[row];
+            if (ep.n_members < 0) break;
+            const int last = ep.n_kv;
+            ok = __all_sync(0xffffffffu, mbar_wait(bar.pv_done(last & 1), (last >> 1) & 1, abort_flag));
+            if (!ok) break;
+            tc_fence_after();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar.epi_empty());
+            const bool live = row < ep.rows, split = ep.pieces > 1;
+            const float inv = split ? 1.f : l == 0.f ? 0.f : 1.f / l;  // (a NaN stays one)
+            const uint64_t inv2 = pack2(inv, inv);
+            char* slots = a.slots + (size_t)ep.slot * slot_bytes;
+            float* part = reinterpret_cast<float*>(slots + (size_t)ep.piece * slot_bytes);
+            constexpr int NSUB = HD / 32;
+            const int n_sub = ep.n_members * NSUB;
+            uint32_t ra[32], rb[32];
+            tc_ld32(lane_addr + O_COL0, ra);
+            tc_wait_ld32(ra);
+#pragma unroll
+            for (int c = 0; c < GM * NSUB; ++c) {
+                if (c >= n_sub) break;
+                uint32_t* cur = (c & 1) ? rb : ra;
+                uint32_t* nxt = (c & 1) ? ra : rb;
+                const int g = c / NSUB, sc = c % NSUB;
+                if (c + 1 < n_sub) tc_ld32(lane_addr + O_COL0 + (c + 1) * 32, nxt);
+                if (sc == NSUB - 1) {
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) {
+                        mbar_arrive(bar.o_free(g));
+                        if (g == ep.n_members - 1)
+                            for (int x = ep.n_members; x < GM; ++x) mbar_arrive(bar.o_free(x));
+                    }
+                }
+                if (live && !split) {
+                    int h = ep.heads[0];
+#pragma unroll
+                    for (int x = 1; x < GM; ++x)
+                        if (g == x) h = ep.heads[x];
+                    __nv_bfloat16* orow = out + ((size_t)(ep.row0 + row) * a.H + h) * HD + sc * 32;
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) {
+                        uint32_t w[8];
+#pragma unroll
+                        for (int x = 0; x < 8; ++x) {
+                            float y0, y1;
+                            unpack2(mul2(pack2(__uint_as_float(cur[16 * u + 2 * x]), __uint_as_float(cur[16 * u + 2 * x + 1])), inv2), y0, y1);
+                            if (inv == 0.f) y0 = y1 = 0.f;
+                            __nv_bfloat162 pk = __floats2bfloat162_rn(y0, y1);
+                            w[x] = *reinterpret_cast<uint32_t*>(&pk);
+                        }
+                        st_global_row32(orow + u * 16, w, wide);
+                    }
+                } else if (live) {
+                    float* prow = part + ((size_t)g * a.slot_rows + row) * HD + sc * 32;
+#pragma unroll
+                    for (int u = 0; u < 8; ++u)
+                        reinterpret_cast<uint4*>(prow)[u] = make_uint4(cur[4 * u], cur[4 * u + 1], cur[4 * u + 2], cur[4 * u + 3]);
+                }
+                if (c + 1 < n_sub) tc_wait_ld32(nxt);
+            }
+            if (!split || quad * 32 >= ep.rows) continue;
+            // A piece: its rows' references and sums; the warp that finishes its rows' last piece joins them, in order of the
+            // pieces.  (A byte of the counter per warp.)
+            if (live) reinterpret_cast<float2*>(reinterpret_cast<char*>(part) + stats)[row] = make_float2(ref, l);
+            __threadfence();
+            __syncwarp();
+            unsigned before = 0;
+            if (lane == 0) {
+                before = (unsigned)atomicAdd(&a.counters[ep.counter], 1 << (8 * quad)) >> (8 * quad) & 255u;
+                __threadfence();
+            }
+            before = __shfl_sync(0xffffffffu, before, 0);
+            if ((int)before != ep.pieces - 1) continue;
+            const int n_rows = min(32, ep.rows - quad * 32);
+#pragma unroll 1
+            for (int rr = 0; rr < n_rows; ++rr) {  // the warp takes a row at a time, a lane 8 columns of its members
+                const int rw = quad * 32 + rr;
+                const float2 mine = lane < ep.pieces ? __ldcg(reinterpret_cast<const float2*>(slots + (size_t)lane * slot_bytes + stats) + rw) : make_float2(0.f, 0.f);
+                float m = mine.y != 0.f ? mine.x : -INFINITY;  // (pieces are at most 32)
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+                // (a reference of -inf or a NaN comes with a sum of 0 or NaN)
+                const float w_mine = mine.y != 0.f ? fast_exp2(mine.x - (m == -INFINITY ? 0.f : m)) : 0.f;
+                float sum = 0.f;
+                float o8[8] = {};
+                const int g = lane / (HD / 8), x = lane % (HD / 8);
+                for (int p = 0; p < ep.pieces; ++p) {
+                    const float w = __shfl_sync(0xffffffffu, w_mine, p), lp = __shfl_sync(0xffffffffu, mine.y, p);
+                    if (lp == 0.f) continue;
+                    sum += w * lp;
+                    if (g < ep.n_members) {
+                        const float4* src = reinterpret_cast<const float4*>(slots + (size_t)p * slot_bytes) + (((size_t)g * a.slot_rows + rw) * HD + x * 8) / 4;
+                        const float4 u = __ldcg(src), v = __ldcg(src + 1);
+                        o8[0] += w * u.x, o8[1] += w * u.y, o8[2] += w * u.z, o8[3] += w * u.w;
+                        o8[4] += w * v.x, o8[5] += w * v.y, o8[6] += w * v.z, o8[7] += w * v.w;
+                    }
+                }
+                const float f = sum == 0.f ? 0.f : 1.f / sum;
+                if (g < ep.n_members) {
+                    uint4 w;
+                    uint32_t* words = &w.x;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        __nv_bfloat162 pk = __floats2bfloat162_rn(o8[2 * i] * f, o8[2 * i + 1] * f);
+                        words[i] = *reinterpret_cast<uint32_t*>(&pk);
+                    }
+                    int h = ep.heads[0];
+#pragma unroll
+                    for (int i = 1; i < GM; ++i)
+                        if (g == i) h = ep.heads[i];
+                    reinterpret_cast<uint4*>(out + ((size_t)(ep.row0 + rw) * a.H + h) * HD)[x] = w;
+                }
+            }
+        }
+    }
+
+    // teardown: every tcgen05 operation of this CTA has completed or been abandoned after a timeout
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 1) {
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(TMEM_COLS) : "memory");
+    }
+    if (tid == 0 && *abort_flag) atomicExch(&a.hdr->status, CHAI_ERR_TIMEOUT);
+}
+
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                  const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+static EncodeTiledFn encode_tiled_fn() {
+    static const EncodeTiledFn fn = [] {
+        void* p = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        const bool ok = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) == cudaSuccess &&
+                        q == cudaDriverEntryPointSuccess;
+        return ok ? reinterpret_cast<EncodeTiledFn>(p) : nullptr;
+    }();
+    return fn;
+}
+
+static bool make_map(CUtensorMap* map, const void* base, int rank, const cuuint64_t* dims, const cuuint64_t* strides, const cuuint32_t* box) {
+    const EncodeTiledFn fn = encode_tiled_fn();
+    if (fn == nullptr) return false;
+    const cuuint32_t estr[4] = {1, 1, 1, 1};
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, rank, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+// pages: (64 columns of D, rows of a page, planes, pages)
+static bool make_page_map(CUtensorMap* map, const void* base, int D, const PagePool& p, int planes, size_t page_stride, int box_rows) {
+    const cuuint64_t dims[4] = {(cuuint64_t)D, (cuuint64_t)p.page_size, (cuuint64_t)planes, (cuuint64_t)p.n_pages};
+    const cuuint64_t strides[3] = {(cuuint64_t)D * 2, (cuuint64_t)p.page_size * D * 2, (cuuint64_t)page_stride * 2};
+    const cuuint32_t box[4] = {64, (cuuint32_t)box_rows, 1, 1};
+    return make_map(map, base, 4, dims, strides, box);
+}
+
+}  // namespace pp
+
+static int prefill_paged(const char* fn, bool fp8, PagedCall a, int n_pages, int page_size, int max_pages, int D,
+                         const int32_t* block_table, size_t k_page_stride, size_t v_page_stride, int dtype, void* workspace,
+                         size_t workspace_bytes, cudaStream_t s) {
+    CHAI_REQUIRE(a.q && a.k_pages && a.v_pages && a.membership && a.reps && block_table && a.kv_lens && a.token_start && a.out && workspace,
+                 CHAI_ERR_INVALID_ARG, "%s: null pointer", fn);
+    CHAI_REQUIRE(!fp8 || (a.k_scales && a.v_scales), CHAI_ERR_INVALID_ARG, "%s: null pointer", fn);
+    const void* all[] = {a.q, a.k_pages, a.v_pages, a.membership, a.reps, block_table, a.kv_lens, a.token_start, a.out, workspace, a.k_scales, a.v_scales};
+    for (const void* p : all) CHAI_REQUIRE(aligned16(p), CHAI_ERR_INVALID_ARG, "%s: pointers must be 16-byte aligned", fn);
+    CHAI_REQUIRE(dtype == CHAI_F32 || dtype == CHAI_BF16, CHAI_ERR_UNSUPPORTED, "%s: unknown dtype %d", fn, dtype);
+    const int rc = make_pool(fn, block_table, a.B, a.H, a.k, n_pages, page_size, max_pages, D, k_page_stride, v_page_stride,
+                             fp8 ? 1 : elem_size(dtype), &a.pool);
+    if (rc != CHAI_OK) return rc;
+    CHAI_REQUIRE(a.n_tokens > 0, CHAI_ERR_INVALID_ARG, "%s: need n_tokens > 0", fn);
+    CHAI_REQUIRE(isfinite(a.scale) && a.scale > 0.f, CHAI_ERR_INVALID_ARG, "%s: scale must be positive and finite", fn);
+    CHAI_REQUIRE(((long long)a.n_tokens / 16 + a.B + 1) * a.H < (1ll << 26), CHAI_ERR_UNSUPPORTED,
+                 "%s: (n_tokens / 16 + B + 1) * H must be below 2^26", fn);
+    CHAI_REQUIRE(prefill_plan_smem(a.H, a.k) <= 48 * 1024, CHAI_ERR_UNSUPPORTED,
+                 "%s: too many heads and clusters for the planner (H=%d, k=%d need %zu bytes of shared memory, limit 49152)", fn, a.H,
+                 a.k, prefill_plan_smem(a.H, a.k));
+    const long long dense = (long long)a.H * D, es = (long long)elem_size(dtype);
+    if (a.q_stride == 0) a.q_stride = dense;
+    CHAI_REQUIRE(a.q_stride >= dense && a.q_stride * es % 16 == 0 && a.q_stride * es < (1ll << 40), CHAI_ERR_INVALID_ARG,
+                 "%s: the token stride of q must be at least H*D=%lld elements and a multiple of 16 bytes", fn, dense);
+    CHAI_REQUIRE(a.pool.k_page_stride * 2 < (1ull << 40) && a.pool.v_page_stride * 2 < (1ull << 40), CHAI_ERR_UNSUPPORTED,
+                 "%s: page strides must be below 2^39 elements", fn);
+    const char *q_at = static_cast<const char*>(a.q), *o_at = static_cast<const char*>(a.out);
+    CHAI_REQUIRE(q_at + ((a.n_tokens - 1) * a.q_stride + dense) * es <= o_at || o_at + a.n_tokens * dense * es <= q_at,
+                 CHAI_ERR_INVALID_ARG, "%s: q and out must not overlap", fn);
+    const size_t need = chai_prefill_paged_workspace_bytes(a.B, a.H, a.n_tokens);
+    CHAI_REQUIRE(workspace_bytes >= need, CHAI_ERR_WORKSPACE, "%s: workspace has %zu bytes, %zu needed", fn, workspace_bytes, need);
+
+    static PerDeviceOnce once;
+    static int sms_of_device[kMaxDevices] = {};
+    int dev = 0;
+    cudaError_t de = cudaGetDevice(&dev);
+    if (de != cudaSuccess) return cuda_fail(de, "prefill_paged_kernel set-up");
+    CHAI_REQUIRE(dev >= 0 && dev < kMaxDevices, CHAI_ERR_UNSUPPORTED, "%s: device index %d out of range", fn, dev);
+    const int set_up = once.run(dev, [&]() -> int {
+        int count = 0;
+        cudaError_t e = cudaDeviceGetAttribute(&count, cudaDevAttrMultiProcessorCount, dev);
+        if (e == cudaSuccess) e = cudaFuncSetAttribute(pp::prefill_paged_kernel<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, pp::SMEM_BYTES);
+        if (e == cudaSuccess) e = cudaFuncSetAttribute(pp::prefill_paged_kernel<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, pp::SMEM_BYTES);
+        if (e != cudaSuccess) return cuda_fail(e, "prefill_paged_kernel set-up");
+        sms_of_device[dev] = count;
+        return CHAI_OK;
+    });
+    if (set_up != CHAI_OK) return set_up;
+
+    const bool tensor = dtype == CHAI_BF16;
+    const PagedLayout L = paged_layout(a.B, a.H, a.n_tokens);
+    char* ws = static_cast<char*>(workspace);
+    a.hdr = reinterpret_cast<WsHeader*>(ws);
+    a.req = reinterpret_cast<PagedRequest*>(ws + L.off_req);
+    a.groups = reinterpret_cast<GroupEntry*>(ws + L.off_groups);
+    a.counters = reinterpret_cast<int*>(ws + L.off_counters);
+    a.slots = ws + L.off_slots;
+    a.gmax = 256 / D;
+    a.bq = tensor ? pp::BM : prefill_paged_simt_rows(a.B, a.n_tokens);
+    a.bk = tensor ? pp::BN : 64;
+    a.ctas = sms_of_device[dev];
+    a.slot_rows = ((a.bq < a.n_tokens ? a.bq : a.n_tokens) + 1) & ~1;  // (even: slots are multiples of 16 bytes)
+    a.max_slots = (int)((L.total - L.off_slots) / ((size_t)a.slot_rows * kSlotRowBytes));
+    static std::atomic<unsigned> launches{0};
+    a.token = 0x80000000u | launches.fetch_add(1, std::memory_order_relaxed);  // (never 0)
+    CHAI_LOG_CALL("%s: B=%d H=%d k=%d n_tokens=%d D=%d dtype=%d page_size=%d causal=%d, query tiles of %d rows", fn, a.B, a.H, a.k,
+                  a.n_tokens, D, dtype, page_size, a.causal, a.bq);
+    CHAI_LAUNCH_DEPENDENT("prefill_paged_plan_kernel launch", prefill_paged_plan_kernel, dim3(a.B), dim3(128), prefill_plan_smem(a.H, a.k), s, a);
+    if (!tensor) return prefill_paged_simt(a, D, fp8, s);
+    CHAI_REQUIRE(!fp8, CHAI_ERR_UNSUPPORTED, "%s: not yet", fn);
+    pp::Tma maps;
+    int box_rows = 128;
+    while (page_size % box_rows != 0) box_rows >>= 1;
+    const cuuint64_t q_dims[3] = {(cuuint64_t)D, (cuuint64_t)a.H, (cuuint64_t)a.n_tokens};
+    const cuuint64_t q_strides[2] = {(cuuint64_t)D * 2, (cuuint64_t)a.q_stride * 2};
+    const cuuint32_t q_box[3] = {64, 1, pp::BM};
+    CHAI_REQUIRE(pp::make_map(&maps.q, a.q, 3, q_dims, q_strides, q_box) &&
+                     pp::make_page_map(&maps.k, a.k_pages, D, a.pool, a.k, a.pool.k_page_stride, box_rows) &&
+                     pp::make_page_map(&maps.v, a.v_pages, D, a.pool, a.H, a.pool.v_page_stride, box_rows),
+                 CHAI_ERR_CUDA, "%s: cuTensorMapEncodeTiled failed", fn);
+    const float scale_log2 = a.scale * 1.4426950408889634f;
+    if (D == 128) CHAI_LAUNCH_DEPENDENT("prefill_paged_kernel launch", pp::prefill_paged_kernel<128>, dim3(a.ctas), dim3(pp::THREADS), pp::SMEM_BYTES, s, maps, a, box_rows, scale_log2);
+    else CHAI_LAUNCH_DEPENDENT("prefill_paged_kernel launch", pp::prefill_paged_kernel<64>, dim3(a.ctas), dim3(pp::THREADS), pp::SMEM_BYTES, s, maps, a, box_rows, scale_log2);
+    return CHAI_OK;
+}
+
+static PagedCall paged_call(const void* q, const void* k_pages, const void* v_pages, const float* k_scales, const float* v_scales,
+                            const int32_t* membership, const int32_t* reps, const int32_t* kv_lens, const int32_t* token_start,
+                            void* out, int B, int H, int k, int n_tokens, size_t q_token_stride, float scale, int causal) {
+    PagedCall a = {};
+    a.q = q;
+    a.k_pages = k_pages;
+    a.v_pages = v_pages;
+    a.k_scales = k_scales;
+    a.v_scales = v_scales;
+    a.membership = membership;
+    a.reps = reps;
+    a.kv_lens = kv_lens;
+    a.token_start = token_start;
+    a.out = out;
+    a.B = B;
+    a.H = H;
+    a.k = k;
+    a.n_tokens = n_tokens;
+    a.q_stride = (long long)q_token_stride;
+    a.scale = scale;
+    a.causal = causal != 0;
+    return a;
+}
+
+}  // namespace chai
+
+extern "C" {
+
+size_t chai_prefill_paged_workspace_bytes(int B, int H, int n_tokens) {
+    if (B <= 0 || H <= 0 || n_tokens <= 0) return 0;
+    return ((size_t)1 << 20) + 64 * (size_t)B + 36 * (size_t)H * ((size_t)B + n_tokens / 128 + 1) +
+           chai::kSlotBytesPerToken * (size_t)(n_tokens < 128 ? n_tokens : 128);
+}
+
+int chai_prefill_attention_paged(const void* q, const void* k_pages, const void* v_pages, const int32_t* membership,
+                                 const int32_t* reps, const int32_t* block_table, const int32_t* kv_lens, const int32_t* token_start,
+                                 void* out, int B, int H, int k, int n_tokens, int n_pages, int page_size, int max_pages, int D,
+                                 size_t q_token_stride, size_t k_page_stride, size_t v_page_stride, float scale, int causal,
+                                 int dtype, void* workspace, size_t workspace_bytes, void* stream) {
+    return chai::prefill_paged("chai_prefill_attention_paged", false,
+                               chai::paged_call(q, k_pages, v_pages, nullptr, nullptr, membership, reps, kv_lens, token_start, out, B,
+                                                H, k, n_tokens, q_token_stride, scale, causal),
+                               n_pages, page_size, max_pages, D, block_table, k_page_stride, v_page_stride, dtype, workspace,
+                               workspace_bytes, static_cast<cudaStream_t>(stream));
+}
+
+int chai_prefill_attention_paged_fp8(const void* q, const void* k_pages, const void* v_pages, const float* k_scales,
+                                     const float* v_scales, const int32_t* membership, const int32_t* reps,
+                                     const int32_t* block_table, const int32_t* kv_lens, const int32_t* token_start, void* out, int B,
+                                     int H, int k, int n_tokens, int n_pages, int page_size, int max_pages, int D,
+                                     size_t q_token_stride, size_t k_page_stride, size_t v_page_stride, float scale, int causal,
+                                     int dtype, void* workspace, size_t workspace_bytes, void* stream) {
+    return chai::prefill_paged("chai_prefill_attention_paged_fp8", true,
+                               chai::paged_call(q, k_pages, v_pages, k_scales, v_scales, membership, reps, kv_lens, token_start, out,
+                                                B, H, k, n_tokens, q_token_stride, scale, causal),
+                               n_pages, page_size, max_pages, D, block_table, k_page_stride, v_page_stride, dtype, workspace,
+                               workspace_bytes, static_cast<cudaStream_t>(stream));
+}
+
+}  // extern "C"

@@ -1,0 +1,579 @@
+// Rotary positions: queries and keys are rotated by their positions before their products are taken.
+//
+//   chai_rope                     q and k of whole prompts, any strides
+//   chai_append_rope_paged, _fp8  a packed batch on its way into the pages: the representatives' q and k rotated, k and v
+//                                 written to the tokens' slots (Section 3.5: only representatives' keys are cached, so only
+//                                 they, and the queries that meet them, are read at all)
+//   chai_rope_frequencies         the frequencies, on the host
+//
+// Pair i of a row, (x_i, x_{i + rot/2}) or (x_2i, x_2i+1), at position p turns by the angle a = 2 pi p f_i:
+//   y1 = m (x1 cos a - x2 sin a),   y2 = m (x2 cos a + x1 sin a).
+// f_i is held in turns a position and fp64, so that p f_i minus the nearest whole number is good to 2^-53 p f_i turns at any
+// position; that remainder, rounded to fp32 (at most 2^-26 of a turn), goes to sincospi.  An angle in fp32 would be off by
+// 0.008 at position 131072.
+//
+// Bound by HBM.  A block takes kTokens tokens; their cosines and sines are worked out once, into shared memory; a thread owns one
+// token and one 16-byte vector of its rows, keeps that vector's factors in registers and goes from head to head, so that an
+// angle costs nothing per head.  The other number of a pair comes from a neighbouring lane (half layout) or is the thread's
+// own.  Few tokens are spread over more blocks by heads.
+#include <math.h>
+
+#include "paged.cuh"
+
+namespace chai {
+namespace {
+
+constexpr int kThreads = 256, kTokens = 8, kUnroll = 4;
+constexpr int kMaxPairs = 64;
+
+struct Rotation {
+    const double* turns;  // [rot / 2], device
+    int rot;              // rotated elements of a row, a multiple of 16; 0: none
+    int interleaved;
+    double magnitude;
+};
+
+// cos and sin (times the magnitude) of a token's pair.
+__device__ __forceinline__ float2 factors(const Rotation& r, int pos, int i) {
+    const double t = __dmul_rn((double)pos, r.turns[i]);  // (rounded: the remainder is of this product)
+    float s, c;
+    sincospif(2.f * (float)(t - rint(t)), &s, &c);
+    return make_float2(c * (float)r.magnitude, s * (float)r.magnitude);
+}
+
+// What a thread needs to rotate its vector of EPV elements: per element the factor of itself and of its partner.
+template <int EPV>
+struct Factors {
+    float own[EPV], other[EPV];
+};
+// cs: the token's factors, [rot / 2].  x: the vector's index in the row.
+template <int EPV>
+__device__ __forceinline__ void gather(const Rotation& r, const float2* cs, int x, Factors<EPV>& f) {
+    const int half = r.rot >> 1;
+#pragma unroll
+    for (int e = 0; e < EPV; ++e) {
+        const int at = x * EPV + e;
+        f.own[e] = 1.f;
+        f.other[e] = 0.f;
+        if (at < r.rot) {
+            const bool second = r.interleaved ? (at & 1) : at >= half;
+            const float2 v = cs[r.interleaved ? at >> 1 : second ? at - half : at];
+            f.own[e] = v.x;
+            f.other[e] = second ? v.y : -v.y;
+        }
+    }
+}
+// The lane that holds the partners of vector x (half layout); itself outside the rotated part.
+template <int EPV>
+__device__ __forceinline__ int partner_vector(const Rotation& r, int x) {
+    if (r.interleaved || x * EPV >= r.rot) return x;
+    const int half = r.rot / (2 * EPV);
+    return x < half ? x + half : x - half;
+}
+// y = rotated x in fp32.  src_lane: the lane of the partner vector.  All lanes of the warp call this.
+template <typename T, int EPV>
+__device__ __forceinline__ void rotate(const uint4& raw, bool interleaved, bool rotated, int src_lane, const Factors<EPV>& f, float* y) {
+    float a[EPV], b[EPV];
+    Vec16<T>::unpack(raw, a);
+    if (interleaved) {
+#pragma unroll
+        for (int e = 0; e < EPV; ++e) b[e] = a[e ^ 1];
+    } else {
+        uint4 o;
+        o.x = __shfl_sync(0xffffffffu, raw.x, src_lane);
+        o.y = __shfl_sync(0xffffffffu, raw.y, src_lane);
+        o.z = __shfl_sync(0xffffffffu, raw.z, src_lane);
+        o.w = __shfl_sync(0xffffffffu, raw.w, src_lane);
+        Vec16<T>::unpack(o, b);
+    }
+#pragma unroll
+    for (int e = 0; e < EPV; ++e) y[e] = rotated ? fmaf(a[e], f.own[e], b[e] * f.other[e]) : a[e];  // (outside the rotated part a bit copy)
+}
+template <typename T>
+__device__ __forceinline__ uint4 pack(const float* f);
+template <>
+__device__ __forceinline__ uint4 pack<float>(const float* f) {
+    return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+}
+template <>
+__device__ __forceinline__ uint4 pack<__nv_bfloat16>(const float* f) {
+    uint4 r;
+    unsigned* w = &r.x;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const __nv_bfloat162 p = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
+        w[i] = *reinterpret_cast<const unsigned*>(&p);
+    }
+    return r;
+}
+
+// ---- whole prompts ----------------------------------------------------------------------------------------------
+
+struct Strided {
+    const void* in;
+    void* out;
+    long long b, h, n, ob, oh, on;  // strides in elements, input and output
+    int heads;
+};
+struct RopeArgs {
+    Strided x[2];  // q, k
+    const int32_t* positions;  // [B, N] or null: 0, 1, ...
+    Rotation rot;
+    int B, N, heads_per_block;
+    FastDiv by_n;
+};
+
+// grid (token groups, parts of the heads)
+template <typename T, int D>
+__global__ void __launch_bounds__(kThreads) rope_kernel(const RopeArgs a) {
+    constexpr int EPV = 16 / (int)sizeof(T), LPR = D / EPV, ROWS = kThreads / LPR, STEP = ROWS / kTokens;
+    static_assert(ROWS % kTokens == 0, "a thread keeps its token");
+    __shared__ float2 cs[kTokens][kMaxPairs + 1];
+    const int tid = threadIdx.x, x = tid % LPR, local = (tid / LPR) % kTokens, h_off = tid / LPR / kTokens;
+    const long long total = (long long)a.B * a.N, first = (long long)blockIdx.x * kTokens;
+    const int pairs = a.rot.rot >> 1;
+    for (int i = tid; i < kTokens * pairs; i += kThreads) {
+        const int t = i / pairs, p = i - t * pairs;
+        if (first + t >= total) break;
+        const int pos = a.positions != nullptr ? a.positions[first + t] : (int)((first + t) % a.N);
+        cs[t][p] = factors(a.rot, pos, p);
+    }
+    __syncthreads();
+    const bool live = first + local < total;
+    const long long token = live ? first + local : total - 1;
+    const int b = (int)(token / a.N), n = (int)(token - (long long)b * a.N);
+    Factors<EPV> f;
+    gather<EPV>(a.rot, cs[live ? local : 0], x, f);
+    const int lane = tid & 31, src_lane = lane - x % 32 + partner_vector<EPV>(a.rot, x);
+    const bool rotated = x * EPV < a.rot.rot;
+    const int all = a.x[0].heads + a.x[1].heads;
+    const int h_end = min(all, (int)(blockIdx.y + 1) * a.heads_per_block);
+    for (int h0 = (int)blockIdx.y * a.heads_per_block; h0 < h_end; h0 += STEP * kUnroll) {
+        uint4 raw[kUnroll];
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+            const int hh = h0 + u * STEP + h_off;
+            raw[u] = make_uint4(0, 0, 0, 0);
+            if (hh < h_end && live) {
+                const bool key = hh >= a.x[0].heads;
+                const Strided& s = a.x[key ? 1 : 0];
+                // (an ordinary load: input and output may be one array)
+                raw[u] = __ldcs(reinterpret_cast<const uint4*>(static_cast<const T*>(s.in) + b * s.b + (hh - (key ? a.x[0].heads : 0)) * s.h + n * s.n) + x);
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+            const int hh = h0 + u * STEP + h_off;
+            float y[EPV];
+            rotate<T, EPV>(raw[u], a.rot.interleaved != 0, rotated, src_lane, f, y);
+            if (hh < h_end && live) {
+                const bool key = hh >= a.x[0].heads;
+                const Strided& s = a.x[key ? 1 : 0];
+                __stcs(reinterpret_cast<uint4*>(static_cast<T*>(s.out) + b * s.ob + (hh - (key ? a.x[0].heads : 0)) * s.oh + n * s.on) + x, rotated ? pack<T>(y) : raw[u]);
+            }
+        }
+    }
+}
+
+template <typename T, int D>
+int launch_rope(RopeArgs a, cudaStream_t s) {
+    constexpr int LPR = D * (int)sizeof(T) / 16, STEP = kThreads / LPR / kTokens;
+    const int heads = a.x[0].heads + a.x[1].heads;
+    const long long groups = ((long long)a.B * a.N + kTokens - 1) / kTokens;
+    // Few tokens: the heads go to several blocks, so that there are four for every SM while each has a load for every slot
+    const long long want = (148 * 4 + groups - 1) / groups, most = (heads + STEP * kUnroll - 1) / (STEP * kUnroll);
+    const int parts = (int)(want < most ? want : most);
+    a.heads_per_block = ((heads + parts - 1) / parts + STEP - 1) / STEP * STEP;
+    const int grid_y = (heads + a.heads_per_block - 1) / a.heads_per_block;
+    rope_kernel<T, D><<<dim3((unsigned)groups, grid_y), kThreads, 0, s>>>(a);
+    CHAI_LAUNCH_CHECK("rope_kernel launch");
+    return CHAI_OK;
+}
+
+int check_rotation(const char* fn, const Rotation& r, int D) {
+    CHAI_REQUIRE(r.rot >= 0 && r.rot <= D && r.rot % 16 == 0, CHAI_ERR_UNSUPPORTED,
+                 "%s: rot %d (a multiple of 16 up to the head dimension supported)", fn, r.rot);
+    CHAI_REQUIRE(r.rot == 0 || r.turns != nullptr, CHAI_ERR_INVALID_ARG, "%s: null pointer to the frequencies", fn);
+    CHAI_REQUIRE((reinterpret_cast<uintptr_t>(r.turns) & 7u) == 0, CHAI_ERR_INVALID_ARG, "%s: frequencies must be 8-byte aligned", fn);
+    CHAI_REQUIRE(isfinite(r.magnitude), CHAI_ERR_INVALID_ARG, "%s: magnitude must be finite", fn);
+    return CHAI_OK;
+}
+
+// ---- into the pages ---------------------------------------------------------------------------------------------
+
+struct EnterArgs {
+    const void *q, *k, *v;
+    void* q_out;
+    void *k_pages, *v_pages;
+    float *k_scales, *v_scales;
+    const int32_t *reps, *token_request, *positions;
+    const int64_t* slots;
+    WsHeader* hdr;
+    Rotation rot;
+    long long q_stride, k_stride, v_stride;  // elements between tokens
+    size_t k_page_stride, v_page_stride;
+    FastDiv by_page;
+    long long n_slots;
+    int B, H, k_planes, n_tokens, page_size, rows_per_block;
+};
+
+__device__ __forceinline__ unsigned finite_bits(float x) {
+    const unsigned m = __float_as_uint(x) & 0x7fffffffu;
+    return m < 0x7f800000u ? m : 0u;
+}
+// The smallest e >= -126 with amax <= 448 * 2^e: 448 = 1.75 * 2^8, and adding 0x1fffff carries into the exponent exactly
+// when the mantissa is above 1.75.
+__device__ __forceinline__ int scale_exponent(unsigned amax_bits) { return max((int)((amax_bits + 0x1fffffu) >> 23) - 135, -126); }
+__device__ __forceinline__ float pow2(int e) { return __uint_as_float((unsigned)(e + 127) << 23); }
+
+// A rotated row's largest magnitude decides its scale, and lies within fp32's rounding of 1.75 * 2^i about once in 10^6 rows;
+// there the scale could be off by a factor of two for want of a last bit.  Rows that near to the border are decided in
+// fp64.  A rotated number is off by at most 6 u (|x1| + |x2|) m, u = 2^-24 (4 u for a factor, 2 for product and sum), and
+// the row's largest is at least m max|x| / sqrt 2: the error is less than 17 u of it, 15 units of its mantissa.
+constexpr unsigned kBorder = 0x600000u, kNear = 32u;
+__device__ __forceinline__ bool near_border(unsigned amax_bits) { return (amax_bits & 0x7fffffu) - (kBorder - kNear) <= 2 * kNear; }
+
+// Whether any |y| of this thread's vector is above `border`, computed in fp64.
+template <typename T, int EPV>
+__device__ __noinline__ bool above_border(const Rotation& r, int pos, int x, uint4 raw, uint4 partner, double border) {
+    float a[EPV], o[EPV];
+    Vec16<T>::unpack(raw, a);
+    Vec16<T>::unpack(partner, o);
+    bool above = false;
+    for (int e = 0; e < EPV; ++e) {
+        const int at = x * EPV + e, half = r.rot >> 1;
+        double y = a[e];
+        if (at < r.rot) {
+            const bool second = r.interleaved ? (at & 1) : at >= half;
+            const double t = __dmul_rn((double)pos, r.turns[r.interleaved ? at >> 1 : second ? at - half : at]);
+            double s, c;
+            sincospi(2.0 * (t - rint(t)), &s, &c);
+            const double b = r.interleaved ? a[e ^ 1] : o[e];
+            y = (a[e] * c + (second ? b : -b) * s) * r.magnitude;
+        }
+        above |= isfinite(y) && fabs(y) > border;
+    }
+    return above;
+}
+
+// grid (token groups, parts of the rows).  Rows of a token: k_planes keys, k_planes queries, H values.
+template <typename T, int D, bool FP8>
+__global__ void __launch_bounds__(kThreads) append_rope_kernel(const EnterArgs a) {
+    constexpr int EPV = 16 / (int)sizeof(T), LPR = D / EPV, ROWS = kThreads / LPR, STEP = ROWS / kTokens;
+    __shared__ float2 cs[kTokens][kMaxPairs + 1];
+    dependent_grid_sync();
+    const int tid = threadIdx.x, x = tid % LPR, local = (tid / LPR) % kTokens, r_off = tid / LPR / kTokens;
+    const int first = (int)blockIdx.x * kTokens, token = first + local;
+    const int r_begin = (int)blockIdx.y * a.rows_per_block, rows = 2 * a.k_planes + a.H;
+    const int r_end = min(rows, r_begin + a.rows_per_block);
+    const int pairs = a.rot.rot >> 1;
+    // where the token goes
+    long long slot = -1;
+    int b = 0, pos = 0;
+    bool bad = false;
+    if (token < a.n_tokens) {
+        slot = a.slots[token];
+        b = a.token_request[token];
+        pos = a.positions[token];
+        if (slot >= 0 && (slot >= a.n_slots || b < 0 || b >= a.B)) bad = true, slot = -1;
+    }
+    const bool live = slot >= 0;
+    if (r_begin < 2 * a.k_planes) {  // (block-uniform)
+        for (int i = tid; i < kTokens * pairs; i += kThreads) {
+            const int t = i / pairs, p = i - t * pairs;
+            if (first + t < a.n_tokens) cs[t][p] = factors(a.rot, a.positions[first + t], p);
+        }
+        __syncthreads();
+    }
+    const unsigned page = slot < 0x7fffffffll ? a.by_page.div((unsigned)max(slot, 0ll)) : (unsigned)(slot / a.page_size);
+    const int row = live ? (int)(slot - (long long)page * a.page_size) : 0;
+    Factors<EPV> f = {};
+    if (r_begin < 2 * a.k_planes) gather<EPV>(a.rot, cs[token < a.n_tokens ? local : 0], x, f);
+    const int lane = tid & 31, src_lane = lane - x % 32 + partner_vector<EPV>(a.rot, x);
+    const bool in_rot = x * EPV < a.rot.rot;
+    const int32_t* reps = a.reps + (size_t)b * a.k_planes;
+#pragma unroll 1
+    for (int r0 = r_begin; r0 < r_end; r0 += STEP * kUnroll) {
+        uint4 raw[kUnroll];
+        int head[kUnroll];  // -1: nothing to do
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+            const int r = r0 + u * STEP + r_off;
+            raw[u] = make_uint4(0, 0, 0, 0);
+            head[u] = -1;
+            if (r >= r_end || !live) continue;
+            const int kind = r < a.k_planes ? 0 : r < 2 * a.k_planes ? 1 : 2;
+            head[u] = r - 2 * a.k_planes;
+            if (kind < 2) {
+                head[u] = reps[kind == 0 ? r : r - a.k_planes];
+                if (head[u] < 0 || head[u] >= a.H) {  // unused cluster slot
+                    head[u] = -1;
+                    continue;
+                }
+            }
+            const T* src = static_cast<const T*>(kind == 0 ? a.k : kind == 1 ? a.q : a.v);
+            const long long stride = kind == 0 ? a.k_stride : kind == 1 ? a.q_stride : a.v_stride;
+            raw[u] = __ldcs(reinterpret_cast<const uint4*>(src + token * stride + (long long)head[u] * D) + x);
+        }
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+            const int r = r0 + u * STEP + r_off;
+            // (the rows of a warp are the same row of neighbouring tokens, or of neighbouring rows: `turn` may differ in a warp)
+            const bool turn = r < 2 * a.k_planes, key = r < a.k_planes;
+            float y[EPV];
+            uint4 out = raw[u];
+            if (__any_sync(0xffffffffu, turn)) {
+                rotate<T, EPV>(raw[u], a.rot.interleaved != 0, in_rot && turn, src_lane, f, y);
+                if (turn && in_rot) out = pack<T>(y);
+            } else {
+                Vec16<T>::unpack(raw[u], y);
+            }
+            const bool query = turn && !key;
+            if (query && head[u] >= 0)
+                reinterpret_cast<uint4*>(static_cast<T*>(a.q_out) + ((long long)token * a.H + head[u]) * D)[x] = out;
+            const int pl = key ? r : r - 2 * a.k_planes;
+            const bool store = head[u] >= 0 && !query;
+            const size_t at = store ? (size_t)page * (key ? a.k_page_stride : a.v_page_stride) + ((size_t)pl * a.page_size + row) * D + x * EPV : 0;
+            if constexpr (!FP8) {
+                if (store) *reinterpret_cast<uint4*>(static_cast<T*>(key ? a.k_pages : a.v_pages) + at) = out;
+            } else {
+                unsigned m = 0;
+#pragma unroll
+                for (int e = 0; e < EPV; ++e) m = max(m, finite_bits(y[e]));
+#pragma unroll
+                for (int o = LPR / 2; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
+                int e2 = m == 0 ? 0 : scale_exponent(m);
+                const bool close = key && store && a.rot.rot > 0 && near_border(m) && m >= 0x08000000u;
+                if (__any_sync(0xffffffffu, close)) {
+                    uint4 o;
+                    o.x = __shfl_sync(0xffffffffu, raw[u].x, src_lane);
+                    o.y = __shfl_sync(0xffffffffu, raw[u].y, src_lane);
+                    o.z = __shfl_sync(0xffffffffu, raw[u].z, src_lane);
+                    o.w = __shfl_sync(0xffffffffu, raw[u].w, src_lane);
+                    const unsigned border = (m & 0x7f800000u) | kBorder;
+                    unsigned above = close && above_border<T, EPV>(a.rot, pos, x, raw[u], o, (double)__uint_as_float(border)) ? 1u : 0u;
+#pragma unroll
+                    for (int s = LPR / 2; s > 0; s >>= 1) above |= __shfl_xor_sync(0xffffffffu, above, s);
+                    if (close) e2 = scale_exponent(border) + (int)above;
+                }
+                const float inv = pow2(-e2);
+                unsigned w[EPV / 4];
+#pragma unroll
+                for (int i = 0; i < EPV / 4; ++i) {
+                    const unsigned lo = __nv_cvt_float2_to_fp8x2(make_float2(y[4 * i] * inv, y[4 * i + 1] * inv), __NV_SATFINITE, __NV_E4M3);
+                    const unsigned hi = __nv_cvt_float2_to_fp8x2(make_float2(y[4 * i + 2] * inv, y[4 * i + 3] * inv), __NV_SATFINITE, __NV_E4M3);
+                    w[i] = lo | (hi << 16);
+                }
+                if (store) {
+                    unsigned char* dst = static_cast<unsigned char*>(key ? a.k_pages : a.v_pages) + at;
+                    if constexpr (EPV == 8) *reinterpret_cast<uint2*>(dst) = make_uint2(w[0], w[1]);
+                    else *reinterpret_cast<unsigned*>(dst) = w[0];
+                    if (x == 0) (key ? a.k_scales : a.v_scales)[((size_t)page * (key ? a.k_planes : a.H) + pl) * a.page_size + row] = pow2(e2);
+                }
+            }
+        }
+    }
+    if (bad) flag_status(a.hdr, CHAI_ERR_BAD_PAGE, b);
+}
+
+__global__ void enter_reset_status_kernel(WsHeader* hdr) {
+    dependent_grid_sync();
+    reset_status(hdr);
+}
+
+template <typename T, int D, bool FP8>
+int launch_enter(EnterArgs a, cudaStream_t s) {
+    constexpr int LPR = D * (int)sizeof(T) / 16, STEP = kThreads / LPR / kTokens;
+    const int rows = 2 * a.k_planes + a.H;
+    const long long groups = ((long long)a.n_tokens + kTokens - 1) / kTokens;
+    const long long want = (148 * 4 + groups - 1) / groups, most = (rows + STEP * kUnroll - 1) / (STEP * kUnroll);
+    const int parts = (int)(want < most ? want : most);
+    a.rows_per_block = ((rows + parts - 1) / parts + STEP - 1) / STEP * STEP;
+    CHAI_LAUNCH_DEPENDENT("append_rope_kernel launch", (append_rope_kernel<T, D, FP8>),
+                          dim3((unsigned)groups, (rows + a.rows_per_block - 1) / a.rows_per_block), dim3(kThreads), 0, s, a);
+    return CHAI_OK;
+}
+
+int enter(const char* fn, bool fp8, EnterArgs a, int n_pages, int D, size_t k_page_stride, size_t v_page_stride, int dtype,
+          cudaStream_t s) {
+    CHAI_REQUIRE(a.q && a.k && a.v && a.q_out && a.k_pages && a.v_pages && a.reps && a.token_request && a.positions && a.slots,
+                 CHAI_ERR_INVALID_ARG, "%s: null pointer", fn);
+    CHAI_REQUIRE(!fp8 || (a.k_scales && a.v_scales), CHAI_ERR_INVALID_ARG, "%s: null pointer", fn);
+    CHAI_REQUIRE(aligned16(a.q) && aligned16(a.k) && aligned16(a.v) && aligned16(a.q_out) && aligned16(a.k_pages) &&
+                     aligned16(a.v_pages) && aligned16(a.hdr) && aligned16(a.k_scales) && aligned16(a.v_scales) &&
+                     aligned16(a.reps) && aligned16(a.token_request) && aligned16(a.positions) && aligned16(a.slots),
+                 CHAI_ERR_INVALID_ARG, "%s: pointers must be 16-byte aligned", fn);
+    CHAI_REQUIRE(dtype == CHAI_F32 || dtype == CHAI_BF16, CHAI_ERR_UNSUPPORTED, "%s: unknown dtype %d", fn, dtype);
+    CHAI_REQUIRE(a.n_tokens > 0, CHAI_ERR_INVALID_ARG, "%s: need n_tokens > 0", fn);
+    CHAI_REQUIRE(a.n_tokens <= (1 << 30), CHAI_ERR_UNSUPPORTED, "%s: n_tokens must be <= 2^30", fn);
+    PagePool pool = {};
+    int rc = make_pool(fn, nullptr, a.B, a.H, a.k_planes, n_pages, a.page_size, 1, D, k_page_stride, v_page_stride,
+                       fp8 ? 1 : elem_size(dtype), &pool);
+    if (rc != CHAI_OK) return rc;
+    rc = check_rotation(fn, a.rot, D);
+    if (rc != CHAI_OK) return rc;
+    const long long dense = (long long)a.H * D, es = (long long)elem_size(dtype);
+    for (long long* st : {&a.q_stride, &a.k_stride, &a.v_stride}) {
+        if (*st == 0) *st = dense;
+        CHAI_REQUIRE(*st >= dense && *st * es % 16 == 0 && *st <= (1ll << 40), CHAI_ERR_INVALID_ARG,
+                     "%s: token strides must be at least H*D=%lld elements and multiples of 16 bytes", fn, dense);
+    }
+    const char *q_in = static_cast<const char*>(a.q), *q_to = static_cast<const char*>(a.q_out);
+    CHAI_REQUIRE(q_in + ((a.n_tokens - 1) * a.q_stride + dense) * es <= q_to || q_to + a.n_tokens * dense * es <= q_in,
+                 CHAI_ERR_INVALID_ARG, "%s: q and q_out must not overlap", fn);
+    a.k_page_stride = pool.k_page_stride;
+    a.v_page_stride = pool.v_page_stride;
+    a.by_page = pool.by_page;
+    a.n_slots = (long long)n_pages * a.page_size;
+    CHAI_LOG_CALL("%s: n_tokens=%d B=%d H=%d k=%d D=%d rot=%d dtype=%d page_size=%d", fn, a.n_tokens, a.B, a.H, a.k_planes, D,
+                  a.rot.rot, dtype, a.page_size);
+    if (a.hdr != nullptr)
+        CHAI_LAUNCH_DEPENDENT("status reset", enter_reset_status_kernel, dim3(1), dim3(1), 0, s, a.hdr);
+    using bf16 = __nv_bfloat16;
+    if (dtype == CHAI_BF16) {
+        if (D == 128) return fp8 ? launch_enter<bf16, 128, true>(a, s) : launch_enter<bf16, 128, false>(a, s);
+        return fp8 ? launch_enter<bf16, 64, true>(a, s) : launch_enter<bf16, 64, false>(a, s);
+    }
+    if (D == 128) return fp8 ? launch_enter<float, 128, true>(a, s) : launch_enter<float, 128, false>(a, s);
+    return fp8 ? launch_enter<float, 64, true>(a, s) : launch_enter<float, 64, false>(a, s);
+}
+
+EnterArgs enter_args(const void* q, const void* k, const void* v, void* q_out, void* k_pages, void* v_pages, float* k_scales,
+                     float* v_scales, const int32_t* reps, const int32_t* token_request, const int32_t* positions,
+                     const int64_t* slots, const double* turns, int rot, int interleaved, const double* magnitude_host, int B, int H,
+                     int k_planes, int n_tokens, int page_size, size_t q_stride, size_t k_stride, size_t v_stride, void* workspace) {
+    EnterArgs a = {};
+    a.q = q;
+    a.k = k;
+    a.v = v;
+    a.q_out = q_out;
+    a.k_pages = k_pages;
+    a.v_pages = v_pages;
+    a.k_scales = k_scales;
+    a.v_scales = v_scales;
+    a.reps = reps;
+    a.token_request = token_request;
+    a.positions = positions;
+    a.slots = slots;
+    a.rot = {turns, rot, interleaved, magnitude_host != nullptr ? *magnitude_host : 1.0};
+    a.B = B;
+    a.H = H;
+    a.k_planes = k_planes;
+    a.n_tokens = n_tokens;
+    a.page_size = page_size;
+    a.q_stride = (long long)q_stride;
+    a.k_stride = (long long)k_stride;
+    a.v_stride = (long long)v_stride;
+    a.hdr = static_cast<WsHeader*>(workspace);
+    return a;
+}
+
+}  // namespace
+}  // namespace chai
+
+extern "C" {
+
+int chai_rope(const void* q, const void* k, void* q_out, void* k_out, const int32_t* positions, const double* turns, int B,
+              int Hq, int Hk, int N, int D, int rot, int interleaved, const double* magnitude_host, const int64_t* strides, int dtype,
+              void* stream) {
+    using namespace chai;
+    const char* fn = "chai_rope";
+    CHAI_REQUIRE(q && q_out && (Hk == 0 || (k && k_out)), CHAI_ERR_INVALID_ARG, "%s: null pointer", fn);
+    CHAI_REQUIRE(aligned16(q) && aligned16(q_out) && aligned16(k) && aligned16(k_out) && (reinterpret_cast<uintptr_t>(positions) & 3u) == 0,
+                 CHAI_ERR_INVALID_ARG, "%s: pointers must be 16-byte aligned", fn);
+    CHAI_REQUIRE(B > 0 && Hq > 0 && Hk >= 0 && N > 0, CHAI_ERR_INVALID_ARG, "%s: need B, Hq, N > 0 and Hk >= 0", fn);
+    CHAI_REQUIRE(dtype == CHAI_F32 || dtype == CHAI_BF16, CHAI_ERR_UNSUPPORTED, "%s: unknown dtype %d", fn, dtype);
+    CHAI_REQUIRE(D == 64 || D == 128, CHAI_ERR_UNSUPPORTED, "%s: head_dim %d (64 or 128 supported)", fn, D);
+    CHAI_REQUIRE(Hq <= 65535 && Hk <= 65535 && (long long)B * N < (1ll << 31) * kTokens, CHAI_ERR_UNSUPPORTED,
+                 "%s: heads must be <= 65535 and B * N below 2^34", fn);
+    RopeArgs a = {};
+    a.positions = positions;
+    a.rot = {turns, rot, interleaved, magnitude_host != nullptr ? *magnitude_host : 1.0};
+    int rc = check_rotation(fn, a.rot, D);
+    if (rc != CHAI_OK) return rc;
+    a.B = B;
+    a.N = N;
+    const int heads[2] = {Hq, Hk};
+    const void* in[2] = {q, k};
+    void* out[2] = {q_out, k_out};
+    const long long es = (long long)elem_size(dtype);
+    for (int i = 0; i < 2; ++i) {
+        Strided& x = a.x[i];
+        x.in = in[i];
+        x.out = out[i];
+        x.heads = heads[i];
+        long long* to[6] = {&x.b, &x.h, &x.n, &x.ob, &x.oh, &x.on};
+        for (int j = 0; j < 6; ++j) {
+            const long long dense[3] = {(long long)heads[i] * N * D, (long long)N * D, (long long)D};
+            *to[j] = strides != nullptr ? strides[6 * i + j] : dense[j % 3];
+            CHAI_REQUIRE(heads[i] == 0 || (*to[j] >= 0 && *to[j] * es % 16 == 0 && *to[j] <= (1ll << 40)), CHAI_ERR_INVALID_ARG,
+                         "%s: strides must be multiples of 16 bytes, from 0 to 2^40 elements", fn);
+        }
+    }
+    CHAI_LOG_CALL("%s: B=%d Hq=%d Hk=%d N=%d D=%d rot=%d interleaved=%d dtype=%d", fn, B, Hq, Hk, N, D, rot, interleaved, dtype);
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (dtype == CHAI_BF16) return D == 128 ? launch_rope<__nv_bfloat16, 128>(a, s) : launch_rope<__nv_bfloat16, 64>(a, s);
+    return D == 128 ? launch_rope<float, 128>(a, s) : launch_rope<float, 64>(a, s);
+}
+
+int chai_append_rope_paged(const void* q, const void* k, const void* v, void* q_out, void* k_pages, void* v_pages,
+                           const int32_t* reps, const int32_t* token_request, const int32_t* positions, const int64_t* slots,
+                           const double* turns, int rot, int interleaved, const double* magnitude_host, int B, int H, int k_planes,
+                           int n_tokens, int n_pages, int page_size, int D, size_t q_token_stride, size_t k_token_stride,
+                           size_t v_token_stride, size_t k_page_stride, size_t v_page_stride, int dtype, void* workspace,
+                           void* stream) {
+    return chai::enter("chai_append_rope_paged", false,
+                       chai::enter_args(q, k, v, q_out, k_pages, v_pages, nullptr, nullptr, reps, token_request, positions, slots,
+                                        turns, rot, interleaved, magnitude_host, B, H, k_planes, n_tokens, page_size, q_token_stride,
+                                        k_token_stride, v_token_stride, workspace),
+                       n_pages, D, k_page_stride, v_page_stride, dtype, static_cast<cudaStream_t>(stream));
+}
+
+int chai_append_rope_paged_fp8(const void* q, const void* k, const void* v, void* q_out, void* k_pages, void* v_pages,
+                               float* k_scales, float* v_scales, const int32_t* reps, const int32_t* token_request,
+                               const int32_t* positions, const int64_t* slots, const double* turns, int rot, int interleaved,
+                               const double* magnitude_host, int B, int H, int k_planes, int n_tokens, int n_pages, int page_size, int D,
+                               size_t q_token_stride, size_t k_token_stride, size_t v_token_stride, size_t k_page_stride,
+                               size_t v_page_stride, int dtype, void* workspace, void* stream) {
+    return chai::enter("chai_append_rope_paged_fp8", true,
+                       chai::enter_args(q, k, v, q_out, k_pages, v_pages, k_scales, v_scales, reps, token_request, positions,
+                                        slots, turns, rot, interleaved, magnitude_host, B, H, k_planes, n_tokens, page_size,
+                                        q_token_stride, k_token_stride, v_token_stride, workspace),
+                       n_pages, D, k_page_stride, v_page_stride, dtype, static_cast<cudaStream_t>(stream));
+}
+
+int chai_rope_frequencies(double* turns_host, double* magnitude_host, int rot, int scaling, const double* parameters_host) {
+    using namespace chai;
+    const char* fn = "chai_rope_frequencies";
+    CHAI_REQUIRE(turns_host != nullptr && magnitude_host != nullptr && parameters_host != nullptr, CHAI_ERR_INVALID_ARG, "%s: null pointer", fn);
+    const double base = parameters_host[0], factor = parameters_host[1], context = parameters_host[2], low = parameters_host[3], high = parameters_host[4];
+    CHAI_REQUIRE(rot > 0 && rot % 2 == 0 && rot <= 1024, CHAI_ERR_INVALID_ARG, "%s: rot must be even, from 2 to 1024", fn);
+    CHAI_REQUIRE(isfinite(base) && base > 1.0, CHAI_ERR_INVALID_ARG, "%s: base must be above 1", fn);
+    CHAI_REQUIRE(scaling >= CHAI_ROPE_PLAIN && scaling <= CHAI_ROPE_BANDS, CHAI_ERR_UNSUPPORTED, "%s: unknown scaling %d", fn, scaling);
+    CHAI_REQUIRE(scaling == CHAI_ROPE_PLAIN || (isfinite(factor) && factor >= 1.0), CHAI_ERR_INVALID_ARG, "%s: factor must be at least 1", fn);
+    CHAI_REQUIRE(scaling != CHAI_ROPE_BASE || rot > 2, CHAI_ERR_INVALID_ARG, "%s: a scaled base needs rot > 2", fn);
+    CHAI_REQUIRE(scaling < CHAI_ROPE_RAMP || (isfinite(context) && context > 0.0 && isfinite(low) && low > 0.0 && isfinite(high) && high > low),
+                 CHAI_ERR_INVALID_ARG, "%s: need context > 0 and 0 < low < high", fn);
+    const double pi = 3.14159265358979323846;
+    const double used = scaling == CHAI_ROPE_BASE ? base * pow(factor, (double)rot / (rot - 2)) : base;
+    *magnitude_host = 1.0;
+    double first = 0, last = 0;
+    if (scaling == CHAI_ROPE_RAMP) {
+        // the pairs that turn `high` and `low` times over the context, as fractional indexes
+        first = fmax(floor(rot * log(context / (high * 2 * pi)) / (2 * log(base))), 0.0);
+        last = fmin(ceil(rot * log(context / (low * 2 * pi)) / (2 * log(base))), (double)(rot - 1));
+        *magnitude_host = 0.1 * log(factor) + 1.0;
+    }
+    for (int i = 0; i < rot / 2; ++i) {
+        const double f = pow(used, -2.0 * i / rot) / (2 * pi);
+        double keep = 1.0;  // the share of the unscaled frequency
+        if (scaling == CHAI_ROPE_LINEAR) keep = 0.0;
+        if (scaling == CHAI_ROPE_RAMP) keep = 1.0 - fmin(fmax((i - first) / fmax(last - first, 0.001), 0.0), 1.0);
+        if (scaling == CHAI_ROPE_BANDS) keep = fmin(fmax((context * f - low) / (high - low), 0.0), 1.0);
+        turns_host[i] = f * keep + f / factor * (1.0 - keep);
+        if (scaling == CHAI_ROPE_PLAIN || scaling == CHAI_ROPE_BASE) turns_host[i] = f;
+    }
+    return CHAI_OK;
+}
+
+}  // extern "C"

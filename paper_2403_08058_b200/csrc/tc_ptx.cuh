@@ -82,6 +82,19 @@ __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map
         ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(0), "r"(row), "r"(0), "r"(plane), "r"(bar)
         : "memory");
 }
+// a box of a packed array (64 columns, 1 head, rows) or of a page (64 columns, rows, 1 plane, 1 page)
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map, int col, int head, int row, uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+        ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(col), "r"(head), "r"(row), "r"(bar)
+        : "memory");
+}
+__device__ __forceinline__ void tma_load_page(uint32_t dst, const CUtensorMap* map, int col, int row, int plane, int page, uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
+        ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(col), "r"(row), "r"(plane), "r"(page), "r"(bar)
+        : "memory");
+}
 // the same tile, fetched into L2 only (no shared memory, no barrier): takes the HBM latency off a later load
 __device__ __forceinline__ void tma_prefetch_4d(const CUtensorMap* map, int row, int plane) {
     asm volatile("cp.async.bulk.prefetch.tensor.4d.L2.global.tile [%0, {%1, %2, %3, %4}];"
@@ -131,6 +144,15 @@ __device__ __forceinline__ void st_global_32B(void* p, const uint32_t* w) {
     asm volatile("st.global.L1::no_allocate.L2::cache_hint.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8}, %9;"
                  ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]), "l"(pol)
                  : "memory");
+}
+// 32 bytes of a row that may start on a 16-byte boundary (wide: on a 32-byte one)
+__device__ __forceinline__ void st_global_row32(void* p, const uint32_t* w, bool wide) {
+    if (wide) {
+        st_global_32B(p, w);
+        return;
+    }
+    static_cast<uint4*>(p)[0] = make_uint4(w[0], w[1], w[2], w[3]);
+    static_cast<uint4*>(p)[1] = make_uint4(w[4], w[5], w[6], w[7]);
 }
 __device__ __forceinline__ void tc_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
