@@ -8,19 +8,19 @@
 // for the members of a cluster, two at a time (head_dim 64: four).  P is rounded to bf16, at most 2^-8 of each
 // probability, because that is the tensor core's type beside bf16 values; row sums are of the unrounded ones, in fp32.
 // What differs:
-//   - keys and values come from pages.  A page's rows are whole 8-row groups of the swizzled tile (page sizes are multiples of 8), so a
-//     tile is filled by boxes of as many rows as divide both the page size and 128; the lanes of the loading warp look up
-//     and issue one box each.  Tables are looked up a tile ahead.
+//   - keys and values come from pages, in boxes of as many rows as divide both the page size and 128, whole rows each: a box
+//     costs about 90 cycles of the copy engine whatever it holds.  A box lands as one piece of shared memory, so tiles are
+//     laid out by boxes: keys as 8-row groups of both column halves (one distance between groups), values as boxes of
+//     all members side by side (one distance between 64-column blocks).  The lanes of the loading warp look up and issue
+//     one box each, tables a tile ahead.
 //   - rows behind a request's length are never used, whatever they hold: their scores are masked, and their values, which
 //     would meet probabilities of zero, are zeroed in shared memory before the last tile is multiplied.
-//   - a request may have few tokens: rows that it does not have cost tensor work but no softmax, and there may be too few
-//     tiles for the GPU: key tiles are divided into pieces (prefill_paged.cuh), whose accumulators leave unnormalised and are joined
-//     by the warp that finishes a row's last piece, in order of the pieces.
+//   - a request may have few tokens: rows that it does not have cost tensor work but no softmax, and all tiles are one line that
+//     is cut into equal shares (prefill_paged.cuh); a query tile on both sides of a cut leaves unnormalised accumulators, joined
+//     by the warp that finishes its rows' last piece, in order of the pieces.
 // Bound by the cache's bytes for few tokens a request, by the softmax chain of a tile (as in prefill_tc.cu) for many.
 #include <cuda.h>
 #include <math.h>
-
-#include <atomic>
 
 #include "prefill_paged.cuh"
 #include "tc_ptx.cuh"
@@ -80,18 +80,21 @@ static_assert(NUM_BARS == 23, "barrier count");
 
 // One unit of work, published by the loading warp to the other roles through shared memory.
 struct Item {
-    int n_kv;       // key tiles to walk; 0: zero rows (no keys, unresolved heads); -1: no more work
+    int n_kv;         // key tiles to walk; 0: zero rows (no keys, unresolved heads); -1: no more work
     int n_members;
-    int row0;       // first row of the packed arrays
-    int rows;       // rows of the tile that exist
-    int col0;       // first position of the first tile
-    int sees;       // positions that row 0 sees; row r: r more, at most kv (unmasked: kv)
+    int row0;         // first row of the packed arrays
+    int rows;         // rows of the tile that exist
+    int first, tiles; // the walk begins at key tile `first` and wraps around at `tiles`
+    int sees;         // positions that row 0 sees; row r: r more, at most kv (unmasked: kv)
     int kv;
-    int pieces, piece, slot, counter;
+    int pieces, piece, owner;
     int heads[GMAX];
     int pad;
 };
 static_assert(sizeof(Item) == ITEM_BYTES, "item descriptor");
+
+// First position of the j-th tile of a walk.
+__device__ __forceinline__ int tile_col(int first, int tiles, int j) { return (first + j < tiles ? first + j : first + j - tiles) * BN; }
 
 struct Tma {
     CUtensorMap q, k, v;
@@ -101,7 +104,8 @@ template <int HD>
 __global__ void __launch_bounds__(THREADS, 1)
 prefill_paged_kernel(const __grid_constant__ Tma maps, const PagedCall a, const int box_rows, const float scale_log2) {
     constexpr int GM = HD == 128 ? 2 : 4, HALVES = HD / 64, ROW_BYTES = HD * 2;
-    constexpr int V_TILE = BN * ROW_BYTES;   // distance between the members' value tiles
+    // Bytes between two 64-column blocks of a value box, and between two boxes of a value tile (those of all members).
+    const int v_block = box_rows * 128, v_box = GM * HALVES * v_block;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     extern __shared__ uint8_t smem[];
     const uint32_t sbase = smem_u32(smem);
@@ -149,56 +153,66 @@ prefill_paged_kernel(const __grid_constant__ Tma maps, const PagedCall a, const 
     if (warp == 0) {
         // ---------------- work distribution and loads, by all lanes ----------------
         auto wait_all = [&](uint32_t b, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait(b, parity, abort_flag)); };
-        const int n_items = __ldcg(&a.hdr->pad[kPagedItems]);
-        const int blocks = BN / box_rows;                    // boxes of a tile, per 64 columns
-        auto claim = [&]() { return __shfl_sync(0xffffffffu, lane == 0 ? atomicAdd(&a.hdr->pad[kPagedCounter], 1) : 0, 0); };
+        const int blocks = BN / box_rows;                    // boxes of a tile
         bool ok = true;
         int it = 0, qi = 0, kt = 0;                          // items published, items with loads, key tiles issued
-        int id = claim();
-        GroupEntry e, e_next;
+        PagedGroup e, e_next;
         PagedItem cur = {}, nxt = {};
-        if (id < n_items) cur = paged_item(a, id, &e);
+        PagedWalk walk;
+        walk.begin(a, lane);
+        bool more = walk.next(a, cur, e);
         while (ok) {
-            const int next_id = claim();                     // (looked at when this item's loads are on their way)
-            if (id < n_items && cur.n_kv < 0) {              // nothing to do
-                id = next_id;
-                if (id < n_items) cur = paged_item(a, id, &e);
-                continue;
-            }
             const int is = it & 1;
             ok = wait_all(bar.item_empty(is), ((it >> 1) & 1) ^ 1);
             if (!ok) break;
-            if (id >= n_items) {
+            if (!more) {
                 if (lane == 0) {
                     items[is].n_kv = -1;
                     mbar_arrive(bar.item_full(is));
                 }
                 break;
             }
-            const int n_kv = cur.n_kv, n_members = min(e.n, GM), col0 = cur.first_tile * BN, kv = cur.kv, b = cur.b;
+            const int n_kv = cur.count, n_members = min(e.n, GM), kv = cur.kv;
             if (lane == 0) {
                 Item& item = items[is];
                 item.n_kv = n_kv;
                 item.n_members = n_members;
                 item.row0 = cur.q0;
                 item.rows = cur.rows;
-                item.col0 = col0;
+                item.first = cur.first;
+                item.tiles = cur.tiles;
                 item.kv = kv;
-                item.sees = a.causal ? kv - cur.n + (cur.q0 - __ldcg(&a.req[b].start)) + 1 : kv;
+                item.sees = a.causal ? kv - cur.n + cur.t0 + 1 : kv;
                 item.pieces = cur.pieces;
                 item.piece = cur.piece;
-                item.slot = cur.slot;
-                item.counter = cur.counter;
-                for (int g = 0; g < GMAX; ++g) item.heads[g] = e.heads[g < n_members ? g : 0];
+                item.owner = cur.owner;
+#pragma unroll
+                for (int g = 0; g < GMAX; ++g) item.heads[g] = g < n_members ? e.heads[g] : e.heads[0];
                 mbar_arrive(bar.item_full(is));
             }
             __syncwarp();
             ++it;
             if (n_kv == 0) {
-                id = next_id;
-                if (id < n_items) cur = paged_item(a, id, &e);
+                more = walk.next(a, cur, e);
                 continue;
             }
+            // Lane l knows the place of box l of a tile: page and first row in it.
+            const int32_t* table = a.pool.block_table + (size_t)cur.b * a.pool.max_pages;
+            auto col = [&](int j) { return tile_col(cur.first, cur.tiles, j); };
+            auto boxes = [&](int j) { return (min(BN, kv - col(j)) + box_rows - 1) / box_rows; };  // that hold rows
+            auto look_up = [&](int j, int& page, int& row) {
+                page = -1;
+                row = 0;
+                if (j >= n_kv || lane >= blocks) return;
+                const int pos = col(j) + lane * box_rows;
+                if (pos >= kv) return;
+                const int pi = (int)a.pool.by_page.div((unsigned)pos);
+                row = pos - pi * a.pool.page_size;
+                page = table[pi];  // (an entry that is no page: outside the map, zeros arrive)
+            };
+            int page_v, row_v, page_k, row_k, page_n, row_n;
+            look_up(0, page_v, row_v);
+            look_up(1, page_k, row_k);
             // queries: wait until the previous item's last S = Q K^T has been computed
             ok = wait_all(bar.q_empty(), (qi & 1) ^ 1);
             if (!ok) break;
@@ -209,38 +223,17 @@ prefill_paged_kernel(const __grid_constant__ Tma maps, const PagedCall a, const 
                     tma_load_3d(sbase + OFF_Q + h * HALF_BYTES, &maps.q, h * 64, e.rep, cur.q0, bar.q_full());
             }
             __syncwarp();
-            // Lane l knows the place of box l of a tile: page and first row in it.
-            const int32_t* table = a.pool.block_table + (size_t)b * a.pool.max_pages;
-            auto boxes = [&](int j) { return (min(BN, kv - (col0 + j * BN)) + box_rows - 1) / box_rows; };  // that hold rows
-            auto look_up = [&](int j, int& page, int& row) {
-                const int pos = col0 + j * BN + lane * box_rows;
-                page = -1;
-                row = 0;
-                if (j < n_kv && lane < blocks && pos < kv) {
-                    const int pi = (int)a.pool.by_page.div((unsigned)pos);
-                    row = pos - pi * a.pool.page_size;
-                    page = table[pi];  // (an entry that is no page: outside the map, zeros arrive)
-                }
-            };
-            // `count` boxes x HALVES of plane `plane` to dst
-            auto issue = [&](const CUtensorMap* map, int plane, uint32_t dst, uint32_t full, int count, int page, int row) {
-#pragma unroll 1
-                for (int base = 0; base < count * HALVES; base += 32) {
-                    const int i = base + lane, blk = i / HALVES, h = i % HALVES;
-                    const int p = __shfl_sync(0xffffffffu, page, blk & 31), r = __shfl_sync(0xffffffffu, row, blk & 31);
-                    if (i < count * HALVES)
-                        tma_load_page(dst + h * HALF_BYTES + blk * box_rows * 128, map, h * 64, r, plane, p, full);
-                }
-            };
-            int page_v, row_v, page_k, row_k, page_n, row_n;
-            look_up(0, page_v, row_v);
-            look_up(1, page_k, row_k);
             auto load_k = [&](int j, int page, int row) -> bool {
                 const int n = kt + j, ts = n & 1, count = boxes(j);
                 if (!wait_all(bar.qk_done(ts), ((n >> 1) & 1) ^ 1)) return false;  // stage free
                 if (lane == 0) mbar_expect_tx(bar.k_full(ts), count * box_rows * ROW_BYTES);
                 __syncwarp();
-                issue(&maps.k, e.cluster, sbase + OFF_K + ts * TILE_BYTES, bar.k_full(ts), count, page, row);
+                if (lane < count) {
+                    const uint32_t dst = sbase + OFF_K + ts * TILE_BYTES + lane * box_rows * ROW_BYTES;
+                    const int at = e.cluster * a.pool.page_size + row;
+                    if constexpr (HD == 128) tma_load_5d(dst, &maps.k, 0, 0, 0, at >> 3, page, bar.k_full(ts));
+                    else tma_load_3d(dst, &maps.k, 0, at, page, bar.k_full(ts));
+                }
                 return true;
             };
             // order of need: K(0), K(1), V(0), K(2), V(1), ...
@@ -254,11 +247,17 @@ prefill_paged_kernel(const __grid_constant__ Tma maps, const PagedCall a, const 
                 if (!ok) break;
                 if (lane == 0) mbar_expect_tx(bar.v_full(ts), n_members * count * box_rows * ROW_BYTES);
                 __syncwarp();
+                if (lane < count) {
+                    const uint32_t dst = sbase + OFF_V + ts * 2 * TILE_BYTES + lane * v_box;
 #pragma unroll
-                for (int g = 0; g < GM; ++g)
-                    if (g < n_members)
-                        issue(&maps.v, e.heads[g], sbase + OFF_V + ts * 2 * TILE_BYTES + g * V_TILE, bar.v_full(ts), count, page_v, row_v);
-                if (j == 0 && next_id < n_items) nxt = paged_item(a, next_id, &e_next);
+                    for (int g = 0; g < GM; ++g) {
+                        if (g >= n_members) break;
+                        const int at = e.heads[g] * a.pool.page_size + row_v;
+                        if constexpr (HD == 128) tma_load_page(dst + g * HALVES * v_block, &maps.v, 0, at, 0, page_v, bar.v_full(ts));
+                        else tma_load_3d(dst + g * v_block, &maps.v, 0, at, page_v, bar.v_full(ts));
+                    }
+                }
+                if (j == 0) more = walk.next(a, nxt, e_next);
                 page_v = page_k, row_v = row_k;
                 page_k = page_n, row_k = row_n;
             }
@@ -266,7 +265,6 @@ prefill_paged_kernel(const __grid_constant__ Tma maps, const PagedCall a, const 
             ++qi;
             cur = nxt;
             e = e_next;
-            id = next_id;
         }
     } else if (warp == 1 || warp == PV_WARP) {
         // ---------------- MMA issuers ----------------
@@ -275,17 +273,21 @@ prefill_paged_kernel(const __grid_constant__ Tma maps, const PagedCall a, const 
         auto wait_all = [&](uint32_t b, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait_polling(b, parity, abort_flag)); };
         const bool qk_role = warp == 1;
         const uint64_t dq = make_desc(sbase + OFF_Q, 16, 1024);
-        const uint64_t dk = make_desc(sbase + OFF_K, 16, 1024);
-        const uint64_t dv = make_desc(sbase + OFF_V, HALF_BYTES, 1024);
-        const uint32_t hi_k = (uint32_t)(dq >> 32), hi_v = (uint32_t)(dv >> 32);
+        // keys: 8-row groups of HALVES blocks of 1 KB; values: 8-row groups of a block 1 KB apart, or (boxes of 8 rows) a box apart
+        const uint64_t dk = make_desc(sbase + OFF_K, 16, HALVES * 1024);
+        const uint64_t dv = make_desc(sbase + OFF_V, v_block, box_rows == 8 ? v_box : 1024);
+        const uint32_t hi_q = (uint32_t)(dq >> 32), hi_k = (uint32_t)(dk >> 32), hi_v = (uint32_t)(dv >> 32);
         const uint32_t q_lo = (uint32_t)dq, k_lo = (uint32_t)dk, v_lo = (uint32_t)dv;
+        // 16 keys further in a value tile: within a box of 128 rows or less, or in another box
+        const int box_shift = __ffs(box_rows) - 1;
+        const int steps_of_box = box_rows >= 16 ? box_rows / 16 : 1, box_step = box_rows >= 16 ? v_box : 2 * v_box, step_shift = __ffs(steps_of_box) - 1;
         bool ok = true;
         int it = 0, qi = 0, kt = 0;
         while (ok) {
             const int is = it & 1;
             ok = wait_all(bar.item_full(is), (it >> 1) & 1);
             if (!ok) break;
-            const int n_kv = items[is].n_kv, n_members = items[is].n_members, left = items[is].kv - items[is].col0;
+            const int n_kv = items[is].n_kv, n_members = items[is].n_members, first = items[is].first, tiles = items[is].tiles, kv = items[is].kv;
             __syncwarp();
             if (lane == 0) mbar_arrive(bar.item_empty(is));
             if (n_kv < 0) break;
@@ -303,8 +305,8 @@ prefill_paged_kernel(const __grid_constant__ Tma maps, const PagedCall a, const 
                     if (elect_one()) {
 #pragma unroll
                         for (int s = 0; s < HD / 16; ++s) {
-                            const uint32_t off = ((s >> 2) * HALF_BYTES + (s & 3) * 32) >> 4;
-                            tc_mma(d, desc(hi_k, q_lo + off), desc(hi_k, kb + off), IDESC_QK, s > 0);
+                            const uint32_t q_off = ((s >> 2) * HALF_BYTES + (s & 3) * 32) >> 4, k_off = ((s >> 2) * 1024 + (s & 3) * 32) >> 4;
+                            tc_mma(d, desc(hi_q, q_lo + q_off), desc(hi_k, kb + k_off), IDESC_QK, s > 0);
                         }
                         tc_commit(bar.qk_done(ts));
                         if (j + 1 == n_kv) tc_commit(bar.q_empty());
@@ -316,14 +318,14 @@ prefill_paged_kernel(const __grid_constant__ Tma maps, const PagedCall a, const 
                     const int ts = kt & 1;
                     ok = wait_all(bar.v_full(ts), (kt >> 1) & 1);
                     if (!ok) break;
-                    const int valid = left - j * BN;
+                    const int valid = kv - tile_col(first, tiles, j);
                     if (valid < BN) {  // rows behind the request's length: zeros, whatever is there
-                        const int per = (BN - valid) * 8, total = n_members * HALVES * per;
-                        for (int i = lane; i < total; i += 32) {
-                            const int m = i / per, r = i - m * per;
-                            const uint32_t at = sbase + OFF_V + ts * 2 * TILE_BYTES + (m / HALVES) * V_TILE + (m % HALVES) * HALF_BYTES + valid * 128 + r * 16;
-                            asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(at), "r"(0) : "memory");
-                        }
+                        const int strip = lane >> 3;  // a 64-column block of a member: 4 in all
+                        if (strip < n_members * HALVES)
+                            for (int r = valid; r < BN; ++r) {
+                                const uint32_t at = sbase + OFF_V + ts * 2 * TILE_BYTES + (r >> box_shift) * v_box + strip * v_block + (r & (box_rows - 1)) * 128 + (lane & 7) * 16;
+                                asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(at), "r"(0) : "memory");
+                            }
                         fence_async_proxy();
                         __syncwarp();
                     }
@@ -340,7 +342,7 @@ prefill_paged_kernel(const __grid_constant__ Tma maps, const PagedCall a, const 
                         const uint32_t idesc_all = make_idesc_n(true, (unsigned)(HD * n_members));
 #pragma unroll
                         for (int s = 0; s < BN / 16; ++s)
-                            tc_mma_ts(d, p_addr + s * 8, desc(hi_v, vb + s * (2048 >> 4)), idesc_all, (j > 0 || s > 0) ? 1u : 0u);
+                            tc_mma_ts(d, p_addr + s * 8, desc(hi_v, vb + (uint32_t)(((s >> step_shift) * box_step + (s & (steps_of_box - 1)) * 2048) >> 4)), idesc_all, (j > 0 || s > 0) ? 1u : 0u);
                         tc_commit(bar.pv_done(ts));
                     }
                     __syncwarp();
@@ -365,7 +367,7 @@ prefill_paged_kernel(const __grid_constant__ Tma maps, const PagedCall a, const 
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) break;
             const int n_kv = items[is].n_kv, n_members = items[is].n_members, rows = items[is].rows;
-            const int item_col0 = items[is].col0, kv = items[is].kv, sees0 = items[is].sees;
+            const int first = items[is].first, tiles = items[is].tiles, kv = items[is].kv, sees0 = items[is].sees;
             // (the warp that hands the item on to the epilogue keeps it until then)
             const bool keeps = warp == 2 && n_kv > 0;
             if (n_kv == 0 && row < rows)
@@ -384,7 +386,10 @@ prefill_paged_kernel(const __grid_constant__ Tma maps, const PagedCall a, const 
             const bool idle = quad * 32 >= rows;  // none of the warp's rows exists: it only keeps step
             // positions that the row sees (a row that does not exist: none, so that it cannot move a reference)
             const int sees = row < rows ? min(kv, a.causal ? sees0 + row : kv) : 0;
+            // The reference starts at 0, may be lowered by the first tile that the row sees something of, and grows when a
+            // tile's maximum leaves the window around it.
             float m_used = 0.f, l_run = 0.f;
+            bool fresh = true;  // the row has seen nothing so far
             for (int j = 0; j < n_kv && ok; ++j, ++kt) {
                 const int sb = kt & 1;
                 ok = __all_sync(0xffffffffu, mbar_wait(bar.qk_done(sb), (kt >> 1) & 1, abort_flag));
@@ -401,7 +406,7 @@ prefill_paged_kernel(const __grid_constant__ Tma maps, const PagedCall a, const 
                 tc_fence_after();
                 const uint32_t s_addr = lane_addr + S_COL0;
                 const uint32_t p_st = lane_addr + P_COL0 + sb * 64 + half * 32;
-                const int col0 = item_col0 + j * BN;
+                const int col0 = tile_col(first, tiles, j);
                 const int vis = max(0, min(sees - col0 - cbase, 64));
                 const bool full_tile = col0 + BN <= min(kv, sees0) && quad * 32 + 32 <= rows;
                 tc_ld64_wait(s_addr + cbase, r);
@@ -429,15 +434,17 @@ prefill_paged_kernel(const __grid_constant__ Tma maps, const PagedCall a, const 
                     if (*abort_flag) return false;
                     const float mx = fmaxf(__bfloat162float(mx_up), __bfloat162float(xs[(half ^ 1) * BM + row]));
                     const float m_tile = mx * scale_log2;
-                    if (m_tile > m_used + REF_WINDOW || (j == 0 && m_tile < m_used - REF_WINDOW)) {
-                        m_new = m_tile;
-                        corr = j == 0 ? 1.f : fast_exp2(m_used - m_new);
+                    if (m_tile > -INFINITY) {
+                        if (m_tile > m_used + REF_WINDOW || (fresh && m_tile < m_used - REF_WINDOW)) {
+                            m_new = m_tile;
+                            corr = fresh ? 1.f : fast_exp2(m_used - m_new);  // (nothing has been accumulated yet)
+                        }
+                        fresh = false;
                     }
                     return true;
                 };
                 auto emit = [&](float m, auto with_max) -> float {
-                    const float m_ref = m == -INFINITY ? 0.f : m;
-                    const uint64_t sc2 = pack2(scale_log2, scale_log2), nm2 = pack2(-m_ref, -m_ref);
+                    const uint64_t sc2 = pack2(scale_log2, scale_log2), nm2 = pack2(-m, -m);
                     uint64_t acc01 = 0ull, acc23 = 0ull;
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
@@ -540,8 +547,8 @@ prefill_paged_kernel(const __grid_constant__ Tma maps, const PagedCall a, const 
             const bool live = row < ep.rows, split = ep.pieces > 1;
             const float inv = split ? 1.f : l == 0.f ? 0.f : 1.f / l;  // (a NaN stays one)
             const uint64_t inv2 = pack2(inv, inv);
-            char* slots = a.slots + (size_t)ep.slot * slot_bytes;
-            float* part = reinterpret_cast<float*>(slots + (size_t)ep.piece * slot_bytes);
+            auto slot = [&](int piece) { return a.slots + (size_t)piece_slot(ep.owner, piece) * slot_bytes; };
+            float* part = reinterpret_cast<float*>(slot(ep.piece));
             constexpr int NSUB = HD / 32;
             const int n_sub = ep.n_members * NSUB;
             uint32_t ra[32], rb[32];
@@ -598,49 +605,69 @@ prefill_paged_kernel(const __grid_constant__ Tma maps, const PagedCall a, const 
             __syncwarp();
             unsigned before = 0;
             if (lane == 0) {
-                before = (unsigned)atomicAdd(&a.counters[ep.counter], 1 << (8 * quad)) >> (8 * quad) & 255u;
+                before = (unsigned)atomicAdd(&a.done[ep.owner], 1 << (8 * quad)) >> (8 * quad) & 255u;
                 __threadfence();
             }
             before = __shfl_sync(0xffffffffu, before, 0);
             if ((int)before != ep.pieces - 1) continue;
             const int n_rows = min(32, ep.rows - quad * 32);
-#pragma unroll 1
-            for (int rr = 0; rr < n_rows; ++rr) {  // the warp takes a row at a time, a lane 8 columns of its members
-                const int rw = quad * 32 + rr;
-                const float2 mine = lane < ep.pieces ? __ldcg(reinterpret_cast<const float2*>(slots + (size_t)lane * slot_bytes + stats) + rw) : make_float2(0.f, 0.f);
-                float m = mine.y != 0.f ? mine.x : -INFINITY;  // (pieces are at most 32)
+            // Lane l holds the statistics of piece l; the warp takes JOIN rows at a time, a lane 8 columns of one member, and
+            // has the loads of a piece for all of them under way at once.
+            constexpr int JOIN = 4;
+            const int g = lane / (HD / 8), x = lane % (HD / 8);
+            int h = ep.heads[0];
 #pragma unroll
-                for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-                // (a reference of -inf or a NaN comes with a sum of 0 or NaN)
-                const float w_mine = mine.y != 0.f ? fast_exp2(mine.x - (m == -INFINITY ? 0.f : m)) : 0.f;
-                float sum = 0.f;
-                float o8[8] = {};
-                const int g = lane / (HD / 8), x = lane % (HD / 8);
+            for (int i = 1; i < GM; ++i)
+                if (g == i) h = ep.heads[i];
+#pragma unroll 1
+            for (int r0 = 0; r0 < n_rows; r0 += JOIN) {
+                const int first_row = quad * 32 + r0;
+                float2 mine[JOIN];
+                float o8[JOIN][8], sum[JOIN], w_mine[JOIN];
+#pragma unroll
+                for (int u = 0; u < JOIN; ++u)
+                    mine[u] = lane < ep.pieces && r0 + u < n_rows ? __ldcg(reinterpret_cast<const float2*>(slot(lane) + stats) + first_row + u) : make_float2(0.f, 0.f);
+#pragma unroll
+                for (int u = 0; u < JOIN; ++u) {
+                    float m = mine[u].y != 0.f ? mine[u].x : -INFINITY;  // (a piece that the row sees nothing of has the sum 0)
+#pragma unroll
+                    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+                    w_mine[u] = mine[u].y != 0.f ? fast_exp2(mine[u].x - m) : 0.f;
+                    sum[u] = 0.f;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) o8[u][i] = 0.f;
+                }
+#pragma unroll 2
                 for (int p = 0; p < ep.pieces; ++p) {
-                    const float w = __shfl_sync(0xffffffffu, w_mine, p), lp = __shfl_sync(0xffffffffu, mine.y, p);
-                    if (lp == 0.f) continue;
-                    sum += w * lp;
-                    if (g < ep.n_members) {
-                        const float4* src = reinterpret_cast<const float4*>(slots + (size_t)p * slot_bytes) + (((size_t)g * a.slot_rows + rw) * HD + x * 8) / 4;
-                        const float4 u = __ldcg(src), v = __ldcg(src + 1);
-                        o8[0] += w * u.x, o8[1] += w * u.y, o8[2] += w * u.z, o8[3] += w * u.w;
-                        o8[4] += w * v.x, o8[5] += w * v.y, o8[6] += w * v.z, o8[7] += w * v.w;
+                    const float* src = reinterpret_cast<const float*>(slot(p)) + ((size_t)g * a.slot_rows + first_row) * HD + x * 8;
+                    float4 v[JOIN][2];
+#pragma unroll
+                    for (int u = 0; u < JOIN; ++u)
+                        if (g < ep.n_members && r0 + u < n_rows) {
+                            v[u][0] = __ldcg(reinterpret_cast<const float4*>(src + u * HD));
+                            v[u][1] = __ldcg(reinterpret_cast<const float4*>(src + u * HD) + 1);
+                        }
+#pragma unroll
+                    for (int u = 0; u < JOIN; ++u) {
+                        const float w = __shfl_sync(0xffffffffu, w_mine[u], p), l = __shfl_sync(0xffffffffu, mine[u].y, p);
+                        if (l == 0.f) continue;
+                        sum[u] += w * l;
+                        o8[u][0] += w * v[u][0].x, o8[u][1] += w * v[u][0].y, o8[u][2] += w * v[u][0].z, o8[u][3] += w * v[u][0].w;
+                        o8[u][4] += w * v[u][1].x, o8[u][5] += w * v[u][1].y, o8[u][6] += w * v[u][1].z, o8[u][7] += w * v[u][1].w;
                     }
                 }
-                const float f = sum == 0.f ? 0.f : 1.f / sum;
-                if (g < ep.n_members) {
+#pragma unroll
+                for (int u = 0; u < JOIN; ++u) {
+                    if (g >= ep.n_members || r0 + u >= n_rows) continue;
+                    const float f = sum[u] == 0.f ? 0.f : 1.f / sum[u];
                     uint4 w;
                     uint32_t* words = &w.x;
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        __nv_bfloat162 pk = __floats2bfloat162_rn(o8[2 * i] * f, o8[2 * i + 1] * f);
+                        __nv_bfloat162 pk = __floats2bfloat162_rn(o8[u][2 * i] * f, o8[u][2 * i + 1] * f);
                         words[i] = *reinterpret_cast<uint32_t*>(&pk);
                     }
-                    int h = ep.heads[0];
-#pragma unroll
-                    for (int i = 1; i < GM; ++i)
-                        if (g == i) h = ep.heads[i];
-                    reinterpret_cast<uint4*>(out + ((size_t)(ep.row0 + rw) * a.H + h) * HD)[x] = w;
+                    reinterpret_cast<uint4*>(out + ((size_t)(ep.row0 + first_row + u) * a.H + h) * HD)[x] = w;
                 }
             }
         }
@@ -674,16 +701,29 @@ static EncodeTiledFn encode_tiled_fn() {
 static bool make_map(CUtensorMap* map, const void* base, int rank, const cuuint64_t* dims, const cuuint64_t* strides, const cuuint32_t* box) {
     const EncodeTiledFn fn = encode_tiled_fn();
     if (fn == nullptr) return false;
-    const cuuint32_t estr[4] = {1, 1, 1, 1};
+    const cuuint32_t estr[5] = {1, 1, 1, 1, 1};
     return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, rank, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
-// pages: (64 columns of D, rows of a page, planes, pages)
-static bool make_page_map(CUtensorMap* map, const void* base, int D, const PagePool& p, int planes, size_t page_stride, int box_rows) {
-    const cuuint64_t dims[4] = {(cuuint64_t)D, (cuuint64_t)p.page_size, (cuuint64_t)planes, (cuuint64_t)p.n_pages};
-    const cuuint64_t strides[3] = {(cuuint64_t)D * 2, (cuuint64_t)p.page_size * D * 2, (cuuint64_t)page_stride * 2};
-    const cuuint32_t box[4] = {64, (cuuint32_t)box_rows, 1, 1};
-    return make_map(map, base, 4, dims, strides, box);
+// Keys, D = 128: (64 columns, 8 rows, 2 column halves, row groups of all planes, pages); a box of box_rows whole rows lands as
+// 8-row groups of both halves.  Values: (64 columns, rows of all planes, 2 halves, pages); a box lands as one half behind the
+// other.  D = 64 needs no halves: (64 columns, rows of all planes, pages).
+static bool make_page_map(CUtensorMap* map, const void* base, int D, const PagePool& p, int planes, size_t page_stride, int box_rows, bool keys) {
+    const cuuint64_t rows = (cuuint64_t)planes * p.page_size, pages = (cuuint64_t)p.n_pages, apart = (cuuint64_t)page_stride * 2;
+    const cuuint32_t box = (cuuint32_t)box_rows;
+    if (D == 64) {
+        const cuuint64_t dims[3] = {64, rows, pages}, strides[2] = {128, apart};
+        const cuuint32_t b[3] = {64, box, 1};
+        return make_map(map, base, 3, dims, strides, b);
+    }
+    if (keys) {
+        const cuuint64_t dims[5] = {64, 8, 2, rows / 8, pages}, strides[4] = {256, 128, 2048, apart};
+        const cuuint32_t b[5] = {64, 8, 2, box / 8, 1};
+        return make_map(map, base, 5, dims, strides, b);
+    }
+    const cuuint64_t dims[4] = {64, rows, 2, pages}, strides[3] = {256, 128, apart};
+    const cuuint32_t b[4] = {64, box, 2, 1};
+    return make_map(map, base, 4, dims, strides, b);
 }
 
 }  // namespace pp
@@ -702,11 +742,10 @@ static int prefill_paged(const char* fn, bool fp8, PagedCall a, int n_pages, int
     if (rc != CHAI_OK) return rc;
     CHAI_REQUIRE(a.n_tokens > 0, CHAI_ERR_INVALID_ARG, "%s: need n_tokens > 0", fn);
     CHAI_REQUIRE(isfinite(a.scale) && a.scale > 0.f, CHAI_ERR_INVALID_ARG, "%s: scale must be positive and finite", fn);
-    CHAI_REQUIRE(((long long)a.n_tokens / 16 + a.B + 1) * a.H < (1ll << 26), CHAI_ERR_UNSUPPORTED,
-                 "%s: (n_tokens / 16 + B + 1) * H must be below 2^26", fn);
-    CHAI_REQUIRE(prefill_plan_smem(a.H, a.k) <= 48 * 1024, CHAI_ERR_UNSUPPORTED,
+    CHAI_REQUIRE(a.n_tokens <= (1 << 26), CHAI_ERR_UNSUPPORTED, "%s: n_tokens must be <= 2^26", fn);
+    CHAI_REQUIRE(prefill_paged_plan_smem(a.H, a.k) <= 48 * 1024, CHAI_ERR_UNSUPPORTED,
                  "%s: too many heads and clusters for the planner (H=%d, k=%d need %zu bytes of shared memory, limit 49152)", fn, a.H,
-                 a.k, prefill_plan_smem(a.H, a.k));
+                 a.k, prefill_paged_plan_smem(a.H, a.k));
     const long long dense = (long long)a.H * D, es = (long long)elem_size(dtype);
     if (a.q_stride == 0) a.q_stride = dense;
     CHAI_REQUIRE(a.q_stride >= dense && a.q_stride * es % 16 == 0 && a.q_stride * es < (1ll << 40), CHAI_ERR_INVALID_ARG,
@@ -716,6 +755,10 @@ static int prefill_paged(const char* fn, bool fp8, PagedCall a, int n_pages, int
     const char *q_at = static_cast<const char*>(a.q), *o_at = static_cast<const char*>(a.out);
     CHAI_REQUIRE(q_at + ((a.n_tokens - 1) * a.q_stride + dense) * es <= o_at || o_at + a.n_tokens * dense * es <= q_at,
                  CHAI_ERR_INVALID_ARG, "%s: q and out must not overlap", fn);
+    // (the work's line is counted in 32 bits a group and query tile, and 2^36 in all)
+    const long long row_tiles = (long long)a.n_tokens / 16 + 1, keys = a.pool.capacity / 64 + 2;
+    CHAI_REQUIRE(row_tiles * keys < (1ll << 31) && (row_tiles + a.B) * keys * a.H < (1ll << 36), CHAI_ERR_UNSUPPORTED,
+                 "%s: tokens x table too large: n_tokens/16 * max_pages*page_size/64 must be below 2^31, with B more rows and H heads below 2^36", fn);
     const size_t need = chai_prefill_paged_workspace_bytes(a.B, a.H, a.n_tokens);
     CHAI_REQUIRE(workspace_bytes >= need, CHAI_ERR_WORKSPACE, "%s: workspace has %zu bytes, %zu needed", fn, workspace_bytes, need);
 
@@ -740,21 +783,18 @@ static int prefill_paged(const char* fn, bool fp8, PagedCall a, int n_pages, int
     const PagedLayout L = paged_layout(a.B, a.H, a.n_tokens);
     char* ws = static_cast<char*>(workspace);
     a.hdr = reinterpret_cast<WsHeader*>(ws);
+    a.done = reinterpret_cast<int*>(ws + L.off_done);
     a.req = reinterpret_cast<PagedRequest*>(ws + L.off_req);
-    a.groups = reinterpret_cast<GroupEntry*>(ws + L.off_groups);
-    a.counters = reinterpret_cast<int*>(ws + L.off_counters);
+    a.groups = reinterpret_cast<PagedGroup*>(ws + L.off_groups);
     a.slots = ws + L.off_slots;
     a.gmax = 256 / D;
     a.bq = tensor ? pp::BM : prefill_paged_simt_rows(a.B, a.n_tokens);
     a.bk = tensor ? pp::BN : 64;
-    a.ctas = sms_of_device[dev];
+    a.ctas = sms_of_device[dev] < kPagedMaxCtas ? sms_of_device[dev] : kPagedMaxCtas;
     a.slot_rows = ((a.bq < a.n_tokens ? a.bq : a.n_tokens) + 1) & ~1;  // (even: slots are multiples of 16 bytes)
-    a.max_slots = (int)((L.total - L.off_slots) / ((size_t)a.slot_rows * kSlotRowBytes));
-    static std::atomic<unsigned> launches{0};
-    a.token = 0x80000000u | launches.fetch_add(1, std::memory_order_relaxed);  // (never 0)
     CHAI_LOG_CALL("%s: B=%d H=%d k=%d n_tokens=%d D=%d dtype=%d page_size=%d causal=%d, query tiles of %d rows", fn, a.B, a.H, a.k,
                   a.n_tokens, D, dtype, page_size, a.causal, a.bq);
-    CHAI_LAUNCH_DEPENDENT("prefill_paged_plan_kernel launch", prefill_paged_plan_kernel, dim3(a.B), dim3(128), prefill_plan_smem(a.H, a.k), s, a);
+    CHAI_LAUNCH_DEPENDENT("prefill_paged_plan_kernel launch", prefill_paged_plan_kernel, dim3(a.B), dim3(128), prefill_paged_plan_smem(a.H, a.k), s, a);
     if (!tensor) return prefill_paged_simt(a, D, fp8, s);
     CHAI_REQUIRE(!fp8, CHAI_ERR_UNSUPPORTED, "%s: not yet", fn);
     pp::Tma maps;
@@ -764,8 +804,8 @@ static int prefill_paged(const char* fn, bool fp8, PagedCall a, int n_pages, int
     const cuuint64_t q_strides[2] = {(cuuint64_t)D * 2, (cuuint64_t)a.q_stride * 2};
     const cuuint32_t q_box[3] = {64, 1, pp::BM};
     CHAI_REQUIRE(pp::make_map(&maps.q, a.q, 3, q_dims, q_strides, q_box) &&
-                     pp::make_page_map(&maps.k, a.k_pages, D, a.pool, a.k, a.pool.k_page_stride, box_rows) &&
-                     pp::make_page_map(&maps.v, a.v_pages, D, a.pool, a.H, a.pool.v_page_stride, box_rows),
+                     pp::make_page_map(&maps.k, a.k_pages, D, a.pool, a.k, a.pool.k_page_stride, box_rows, true) &&
+                     pp::make_page_map(&maps.v, a.v_pages, D, a.pool, a.H, a.pool.v_page_stride, box_rows, false),
                  CHAI_ERR_CUDA, "%s: cuTensorMapEncodeTiled failed", fn);
     const float scale_log2 = a.scale * 1.4426950408889634f;
     if (D == 128) CHAI_LAUNCH_DEPENDENT("prefill_paged_kernel launch", pp::prefill_paged_kernel<128>, dim3(a.ctas), dim3(pp::THREADS), pp::SMEM_BYTES, s, maps, a, box_rows, scale_log2);

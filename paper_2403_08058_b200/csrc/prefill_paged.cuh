@@ -1,45 +1,62 @@
 // Work division of clustered attention of packed tokens over a paged cache, shared by its kernels.
 //
-// A unit of work is (request, member group of a cluster, tile of bq query rows, piece of the key tiles).  Requests differ in new
-// tokens and cached positions, and the host knows neither, so a planning kernel divides: its blocks (one a request) build the member
-// groups and look the pages over; the last one to finish chooses how many key tiles a piece has and numbers the items.
-// Pieces of one (group, query tile) leave unnormalised partial results, which whoever finishes last joins.
+// The work is one line: requests, their member groups, the groups' query tiles, the key tiles of each.  Every key tile counts 1
+// and every (group, query tile) kPagedItemCost more.  The line is cut into equal shares, one per CTA, wherever the cuts fall:
+// neither ragged lengths nor uneven clusters nor a batch with few tiles unbalance it.  A planning kernel (a block a request,
+// since the host knows no lengths) builds the member groups, looks the pages over and counts a request's tiles; one warp of
+// each CTA then finds its share.  What lies on both sides of a cut leaves unnormalised partial results, at most two a
+// CTA, which whoever finishes last joins in order: results follow from the lengths and memberships alone.
+// (Tiles of one member and of two count alike: the softmax, which they share, takes most of a tile's time, and where
+// copies do, a CTA that is done early leaves its bandwidth to the others.)
+// CTAs that walk the same keys for different query tiles should meet them at the same time, while they are in L2: a CTA
+// that has done t tiles begins a whole query tile at key tile t modulo its count and wraps around, and of a divided one the
+// share that begins it, late in that CTA's time, takes the last key tiles.
+// All of this stands in front of the first tile, mostly as code that runs once and has to be fetched: it is kept short
+// (one warp, no block-wide barriers, 32-bit distances from the share's beginning).
 #pragma once
 
 #include "paged.cuh"
-#include "prefill_plan.cuh"
 
 namespace chai {
+
+// Up to 256 / head_dim heads of one cluster.
+struct PagedGroup {
+    int cluster;  // -1: heads of no usable cluster
+    int rep;      // representative head
+    int n;
+    int pad;
+    int heads[4];
+};
+static_assert(sizeof(PagedGroup) == 32, "PagedGroup is 32 bytes");
 
 struct PagedRequest {
     int start, n, kv;      // first row, rows, cached positions (0 where a page is bad)
     int n_groups;
-    int item_base;         // number of the request's first item
-    int pieces;            // pieces of its longest query tile
-    int slot_base;         // first partial result of a request whose tiles are divided
+    int cost;              // of a group: its key tiles over all query tiles, and kPagedItemCost for each query tile
+    int longest;           // key tiles of the last query tile
     int code;              // chai_status_t
+    int pad;
 };
 static_assert(sizeof(PagedRequest) == 32, "PagedRequest is 32 bytes");
 
-// words of the workspace header
-constexpr int kPagedCounter = 0, kPagedArrival = 1, kPagedItems = 3, kPagedPiece = 4;
-static_assert((12 + 4 * kPagedArrival) % 8 == 0, "the arrival word is 8-byte aligned");
-
+constexpr int kPagedItemCost = 1;
 constexpr int kSlotRowBytes = 256 * 4 + 8;     // members x head_dim = 256 numbers and (reference, sum), per row
 static_assert(2 * kSlotRowBytes % 16 == 0, "slots have an even number of rows");
 constexpr size_t kSlotBytesPerToken = 640000;  // see chai_prefill_paged_workspace_bytes
+constexpr int kPagedMaxCtas = 300;             // (two partial results each)
+static_assert(2 * kPagedMaxCtas * kSlotRowBytes <= kSlotBytesPerToken, "partial results fit");
+constexpr int kPagedMaxPieces = 32;
 
 struct PagedLayout {
-    size_t off_req, off_groups, off_counters, off_slots, total;
+    size_t off_done, off_req, off_groups, off_slots, total;
 };
-// The counters are laid out for query tiles of 16 rows, the smallest.
 inline PagedLayout paged_layout(int B, int H, int n_tokens) {
     PagedLayout L;
-    L.off_req = sizeof(WsHeader);
+    L.off_done = sizeof(WsHeader);
+    L.off_req = round_up(L.off_done + sizeof(int) * kPagedMaxCtas, 256);
     L.off_groups = round_up(L.off_req + sizeof(PagedRequest) * (size_t)B, 256);
-    L.off_counters = round_up(L.off_groups + sizeof(GroupEntry) * (size_t)B * H, 256);
-    L.off_slots = round_up(L.off_counters + sizeof(int) * (size_t)H * ((size_t)B + n_tokens / 16 + 1), 256);
-    L.total = L.off_slots + kSlotBytesPerToken * (n_tokens < 128 ? n_tokens : 128);
+    L.off_slots = round_up(L.off_groups + sizeof(PagedGroup) * (size_t)B * H, 256);
+    L.total = L.off_slots + 2 * (size_t)kPagedMaxCtas * kSlotRowBytes * ((n_tokens < 128 ? n_tokens + 1 : 128) & ~1);
     return L;
 }
 
@@ -51,17 +68,16 @@ struct PagedCall {
     void* out;
     PagePool pool;
     WsHeader* hdr;
+    int* done;              // [ctas] pieces that are finished of the query tile that a CTA's share ends in
     PagedRequest* req;
-    GroupEntry* groups;
-    int* counters;  // pieces that are done, per (query tile, group)
-    char* slots;
+    PagedGroup* groups;
+    char* slots;            // [2 ctas] partial results
     long long q_stride;
     float scale;
     int B, H, k, n_tokens, causal;
     int gmax, bq, bk;       // members per group, rows and keys per tile
-    int slot_rows, max_slots;
-    int ctas;               // that will work on the items
-    unsigned token;         // of this launch
+    int slot_rows;
+    int ctas;               // that share the work
 };
 
 // Key tiles that query tile qt needs.
@@ -70,213 +86,284 @@ __device__ __forceinline__ int key_tiles(const PagedCall& a, int n, int kv, int 
     return (end + a.bk - 1) / a.bk;
 }
 
-// An item, resolved.  n_kv < 0: nothing to do; 0: rows of zeros.
-struct PagedItem {
-    int b, q0, rows, first_tile, n_kv, kv, n;
-    int pieces, piece, slot, counter;
-};
-__device__ __forceinline__ PagedItem paged_item(const PagedCall& a, int id, GroupEntry* e) {
-    int lo = 0, hi = a.B;  // the last request whose items begin at or before id
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (__ldcg(&a.req[mid].item_base) <= id) lo = mid; else hi = mid;
-    }
-    const int4 r0 = __ldcg(reinterpret_cast<const int4*>(a.req + lo)), r1 = __ldcg(reinterpret_cast<const int4*>(a.req + lo) + 1);
-    PagedItem it;
-    it.b = lo;
-    const int start = r0.x, n = r0.y, kv = r0.z, pieces = r1.y, local = id - r1.x;
-    const int n_qt = (n + a.bq - 1) / a.bq, per = n_qt * pieces;
-    const int g = local / per, rem = local - g * per, qt = n_qt - 1 - rem / pieces;
-    it.piece = rem % pieces;
-    const int4* src = reinterpret_cast<const int4*>(a.groups + (size_t)lo * a.H + g);
-    reinterpret_cast<int4*>(e)[0] = __ldcg(src);
-    reinterpret_cast<int4*>(e)[1] = __ldcg(src + 1);
-    const int C = __ldcg(&a.hdr->pad[kPagedPiece]);
-    const int tiles = e->cluster < 0 ? 0 : key_tiles(a, n, kv, qt);
-    it.pieces = tiles <= C ? 1 : (tiles + C - 1) / C;
-    it.q0 = qt * a.bq;
-    it.rows = min(a.bq, n - it.q0);
-    it.n = n;
-    it.kv = kv;
-    it.first_tile = it.piece * C;
-    it.n_kv = it.piece >= it.pieces ? -1 : min(tiles - it.first_tile, C);
-    it.slot = r1.z + local - it.piece;  // of piece 0
-    it.counter = (start / a.bq + lo + qt) * a.H + g;
-    it.q0 += start;                     // (a row of the packed arrays from here on)
-    return it;
-}
+// Shared memory of the planner: membership, representatives, member masks and first groups of the clusters.
+inline size_t prefill_paged_plan_smem(int H, int k) { return sizeof(int) * ((size_t)H + 2 * (size_t)k + (size_t)k * ((H + 31) / 32)); }
 
-// Grid B, 128 threads.
+// Grid B, 128 threads: the first warp builds the groups, the others look the pages over.
 static __global__ void __launch_bounds__(128) prefill_paged_plan_kernel(const PagedCall a) {
     extern __shared__ __align__(16) int s_plan[];
-    __shared__ int s_in[3], s_last;
-    __shared__ float s_items[4][32], s_slots[4][32];
-    __shared__ float s_work[4];
-    __shared__ int s_most[4], s_scan[4][2], s_code[4];
-    __shared__ int2 s_req[128];  // 128 requests at a time: (groups x query tiles, key tiles of the longest)
+    __shared__ int s_in[3];
     dependent_grid_sync();
-    const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    if (tid == 0) {
-        const int start = min(max(a.token_start[b], 0), a.n_tokens);
-        s_in[0] = start;
-        s_in[1] = max(min(max(a.token_start[b + 1], 0), a.n_tokens) - start, 0);
-        s_in[2] = min(max(a.kv_lens[b], 0), a.pool.capacity);
-    }
+    const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 31, H = a.H, k = a.k, W = (H + 31) >> 5;
+    int* mem = s_plan;
+    int* rep = mem + H;
+    int* slot = rep + k;
+    unsigned* mask = reinterpret_cast<unsigned*>(slot + k);
+    int x = 0;
+    if (tid >= 32 && tid < 35) x = tid == 34 ? a.kv_lens[b] : a.token_start[b + tid - 32];
+    for (int h = tid; h < H; h += 128) mem[h] = a.membership[(size_t)b * H + h];
+    for (int c = tid; c < k; c += 128) rep[c] = a.reps[(size_t)b * k + c];
+    for (int i = tid; i < k * W; i += 128) mask[i] = 0u;
+    if (b == 0)
+        for (int i = tid; i < a.ctas; i += 128) a.done[i] = 0;
+    if (tid >= 32 && tid < 35) s_in[tid - 32] = min(max(x, 0), tid == 34 ? a.pool.capacity : a.n_tokens);
     __syncthreads();
-    const int start = s_in[0], n = s_in[1];
-    int kv = s_in[2], n_groups = 0, code = CHAI_OK;
-    if (n > 0) {
-        int first_bad = a.H;
-        plan_groups(a.membership + (size_t)b * a.H, a.reps + (size_t)b * a.k, a.groups + (size_t)b * a.H, s_plan, a.H, a.k, a.gmax,
-                    &n_groups, &first_bad);
+    const int start = s_in[0], n = max(s_in[1] - start, 0);
+    int kv = s_in[2], n_groups = 0;
+    bool bad_page = false, bad_head = false;
+    if (tid >= 32) {
         const int32_t* table = a.pool.block_table + (size_t)b * a.pool.max_pages;
-        const int pages = (kv + a.pool.page_size - 1) / a.pool.page_size;
-        bool bad = false;
-        for (int p = tid; p < pages; p += blockDim.x) bad |= table[p] < 0 || table[p] >= a.pool.n_pages;
-        int* done = a.counters + (size_t)(start / a.bq + b) * a.H;
-        const int n_done = (n + a.bq - 1) / a.bq * a.H;
-        for (int i = tid; i < n_done; i += blockDim.x) done[i] = 0;
-        if (__syncthreads_or(bad)) {
-            code = CHAI_ERR_BAD_PAGE;
-            kv = 0;
-        } else if (first_bad < a.H) {  // (thread 0 knows)
-            code = CHAI_ERR_BAD_MEMBERSHIP;
+        const int pages = n > 0 ? (kv + a.pool.page_size - 1) / a.pool.page_size : 0;
+#pragma unroll 4
+        for (int p = tid - 32; p < pages; p += 96) bad_page |= (unsigned)table[p] >= (unsigned)a.pool.n_pages;
+    } else if (n > 0) {
+        // a cluster is usable if its representative is one of its heads
+        auto usable = [&](int c) {
+            if (c < 0 || c >= k) return false;
+            const int r = rep[c];
+            return r >= 0 && r < H && mem[r] == c;
+        };
+        int n_bad = 0;
+        for (int w = 0; w < W; ++w) {
+            const int h = w * 32 + lane, c = h < H ? mem[h] : -2;
+            const bool good = h < H && usable(c);
+            const unsigned peers = __match_any_sync(0xffffffffu, good ? c : -1);
+            if (good && lane == __ffs(peers) - 1) mask[c * W + w] = peers;
+            n_bad += __popc(__ballot_sync(0xffffffffu, h < H && !good));
         }
+        __syncwarp();
+        for (int c0 = 0; c0 < k; c0 += 32) {  // first group of each cluster
+            int members = 0;
+            if (c0 + lane < k)
+                for (int w = 0; w < W; ++w) members += __popc(mask[(c0 + lane) * W + w]);
+            const int groups = (members + a.gmax - 1) / a.gmax;
+            int incl = groups;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int y = __shfl_up_sync(0xffffffffu, incl, o);
+                if (lane >= o) incl += y;
+            }
+            if (c0 + lane < k) slot[c0 + lane] = n_groups + incl - groups;
+            n_groups += __shfl_sync(0xffffffffu, incl, 31);
+        }
+        __syncwarp();
+        int bad_before = 0;
+        for (int w = 0; w < W; ++w) {  // every head finds its group: sizes as even as possible, the larger ones first
+            const int h = w * 32 + lane, c = h < H ? mem[h] : -2;
+            const bool good = h < H && usable(c);
+            const unsigned bads = __ballot_sync(0xffffffffu, h < H && !good), below = (1u << lane) - 1u;
+            if (h < H) {
+                int rank, members, at, groups;
+                if (good) {
+                    rank = members = 0;
+                    for (int v = 0; v < W; ++v) {
+                        const unsigned m = mask[c * W + v];
+                        members += __popc(m);
+                        rank += v < w ? __popc(m) : v == w ? __popc(m & below) : 0;
+                    }
+                    at = slot[c];
+                } else {
+                    rank = bad_before + __popc(bads & below);
+                    members = n_bad;
+                    at = n_groups;
+                }
+                groups = (members + a.gmax - 1) / a.gmax;
+                const int size = members / groups, larger = members - size * groups, cut = larger * (size + 1);
+                const int g = rank < cut ? rank / (size + 1) : larger + (rank - cut) / size;
+                const int first = g <= larger ? g * (size + 1) : cut + (g - larger) * size;
+                PagedGroup* e = a.groups + (size_t)b * H + at + g;
+                e->heads[rank - first] = h;
+                if (rank == first) *reinterpret_cast<int4*>(e) = make_int4(good ? c : -1, good ? rep[c] : -1, g < larger ? size + 1 : size, 0);
+            }
+            bad_before += __popc(bads);
+        }
+        n_groups += (n_bad + a.gmax - 1) / a.gmax;
+        bad_head = n_bad > 0;
     }
-    __threadfence();
-    __syncthreads();
-    if (tid == 0) {
+    bad_page = __syncthreads_or(bad_page);
+    if (tid >= 32) return;
+    if (bad_page) kv = 0;
+    const int n_qt = (n + a.bq - 1) / a.bq;
+    int cost = 0;
+    for (int qt = lane; qt < n_qt; qt += 32) cost += key_tiles(a, n, kv, qt) + kPagedItemCost;
+    cost = __reduce_add_sync(0xffffffffu, cost);
+    if (lane == 0) {
         int4* r = reinterpret_cast<int4*>(a.req + b);
         r[0] = make_int4(start, n, kv, n_groups);
-        r[1] = make_int4(0, 1, 0, code);
-        __threadfence();
-        // Arrivals are counted under this launch's token, whatever the word held before; the last one clears it, so that a
-        // replayed launch begins at none again.
-        unsigned long long* word = reinterpret_cast<unsigned long long*>(&a.hdr->pad[kPagedArrival]);
-        unsigned long long old = *reinterpret_cast<volatile unsigned long long*>(word), seen;
-        unsigned count;
-        do {
-            seen = old;
-            count = (unsigned)(seen >> 32) == a.token ? (unsigned)seen : 0u;
-            const unsigned long long next = count + 1 == gridDim.x ? 0ull : ((unsigned long long)a.token << 32) | (count + 1);
-            old = atomicCAS(word, seen, next);
-        } while (old != seen);
-        s_last = count + 1 == gridDim.x;
-        __threadfence();
-    }
-    __syncthreads();
-    if (!s_last) return;
-
-    // The last block: how long a piece is.  Work is counted in key tiles of a group.
-    float work = 0.f;
-    int most = 1;
-    auto measure = [&](int i) {
-        const int4 r = __ldcg(reinterpret_cast<const int4*>(a.req + i));
-        const int n_qt = (r.y + a.bq - 1) / a.bq;
-        return make_int2(r.w * n_qt, r.w > 0 ? key_tiles(a, r.y, r.z, n_qt - 1) : 0);
-    };
-    for (int i = tid; i < a.B; i += 128) {
-        const int4 r = __ldcg(reinterpret_cast<const int4*>(a.req + i));
-        const int2 m = measure(i);
-        s_req[tid] = m;  // (with at most 128 requests: all of them)
-        if (m.x == 0) continue;
-        work += (float)m.x * 0.5f * (max(m.y, 1) + max(key_tiles(a, r.y, r.z, 0), 1));
-        most = max(most, m.y);
-    }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        work += __shfl_xor_sync(0xffffffffu, work, o);
-        most = max(most, __shfl_xor_sync(0xffffffffu, most, o));
-    }
-    if (lane == 0) s_work[warp] = work, s_most[warp] = most;
-    __syncthreads();
-    work = s_work[0] + s_work[1] + s_work[2] + s_work[3];
-    most = max(max(s_most[0], s_most[1]), max(s_most[2], s_most[3]));
-    // Lane l tries pieces of ceil(most / (l + 1)) tiles.
-    int piece = (most + lane) / (lane + 1);
-    float items = 0.f, slots = 0.f;
-    for (int base = 0; base < a.B; base += 128) {
-        if (a.B > 128) {  // (else they lie there already)
-            __syncthreads();
-            s_req[tid] = base + tid < a.B ? measure(base + tid) : make_int2(0, 0);
-            __syncthreads();
-        }
-        for (int i = warp; i < min(128, a.B - base); i += 4) {
-            const int2 r = s_req[i];
-            const int p = max((r.y + piece - 1) / piece, 1);
-            items += (float)r.x * p;
-            if (p > 1) slots += (float)r.x * p;
-        }
-    }
-    s_items[warp][lane] = items;
-    s_slots[warp][lane] = slots;
-    __syncthreads();
-    items = s_items[0][lane] + s_items[1][lane] + s_items[2][lane] + s_items[3][lane];
-    slots = s_slots[0][lane] + s_slots[1][lane] + s_slots[2][lane] + s_slots[3][lane];
-    // Time in tiles: whole rounds of average items, or the work with half an item left over at the end, or one item.  An item
-    // costs about a tile more than its tiles, a piece's partial result as much again.
-    const float own = lane == 0 ? 1.f : 2.f;
-    float time = INFINITY;
-    if (slots <= (float)a.max_slots) {
-        const float avg = work / fmaxf(items, 1.f) + own;
-        time = fmaxf(fmaxf(ceilf(items / a.ctas) * avg, items * avg / a.ctas + 0.5f * piece), piece + own);
-    }
-    int best = lane;
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        const float t = __shfl_xor_sync(0xffffffffu, time, o);
-        const int l = __shfl_xor_sync(0xffffffffu, best, o);
-        if (t < time || (t == time && l < best)) time = t, best = l;
-    }
-    piece = __shfl_sync(0xffffffffu, piece, best);
-
-    // Numbers of the requests' items and slots: running sums, 128 requests at a time.
-    int item_run = 0, slot_run = 0;
-    for (int base = 0; base < a.B; base += 128) {
-        const int i = base + tid;
-        int count = 0, split = 0, p = 1;
-        if (i < a.B) {
-            const int2 r = a.B <= 128 ? s_req[tid] : measure(i);
-            p = max((r.y + piece - 1) / piece, 1);
-            count = r.x * p;
-            split = p > 1 ? count : 0;
-        }
-        int c = count, s = split;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int x = __shfl_up_sync(0xffffffffu, c, o), y = __shfl_up_sync(0xffffffffu, s, o);
-            if (lane >= o) c += x, s += y;
-        }
-        __syncthreads();
-        if (lane == 31) s_scan[warp][0] = c, s_scan[warp][1] = s;
-        __syncthreads();
-        for (int w = 0; w < warp; ++w) c += s_scan[w][0], s += s_scan[w][1];
-        if (i < a.B) {
-            a.req[i].item_base = item_run + c - count;
-            a.req[i].pieces = p;
-            a.req[i].slot_base = slot_run + s - split;
-        }
-        for (int w = 0; w < 4; ++w) item_run += s_scan[w][0], slot_run += s_scan[w][1];
-    }
-    // The first request with something to report.
-    int who = 0x7fffffff;
-    for (int i = tid; i < a.B; i += 128)
-        if (__ldcg(&a.req[i].code) != CHAI_OK) who = min(who, i);
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) who = min(who, __shfl_xor_sync(0xffffffffu, who, o));
-    if (lane == 0) s_code[warp] = who;
-    __syncthreads();
-    if (tid == 0) {
-        who = min(min(s_code[0], s_code[1]), min(s_code[2], s_code[3]));
-        reset_status(a.hdr);
-        if (who < a.B) {
-            a.hdr->status = __ldcg(&a.req[who].code);
-            a.hdr->bad_b = who;
-        }
-        a.hdr->pad[kPagedCounter] = 0;
-        a.hdr->pad[kPagedItems] = item_run;
-        a.hdr->pad[kPagedPiece] = piece;
+        r[1] = make_int4(cost, n > 0 ? key_tiles(a, n, kv, n_qt - 1) : 0, n > 0 && bad_page ? CHAI_ERR_BAD_PAGE : bad_head ? CHAI_ERR_BAD_MEMBERSHIP : CHAI_OK, 0);
     }
 }
+
+// What a CTA does of one (group, query tile).  count 0: rows of zeros.
+struct PagedItem {
+    int b, q0, rows, t0;            // request; first row of the packed arrays, rows, their first among the request's tokens
+    int kv, n;                      // of the request
+    int tiles, first, count;        // key tiles first, first + 1, ... (modulo tiles), count of them
+    int pieces, piece;              // of the query tile, and which one this is
+    int owner;                      // CTA whose share it begins in: pieces lie in the slots 2 owner + 1, 2 (owner + 1), 2 (owner + 2), ...
+};
+__device__ __forceinline__ int piece_slot(int owner, int piece) { return piece == 0 ? 2 * owner + 1 : 2 * (owner + piece); }
+
+// A CTA's walk along its share, by one warp (or the same in several).  Every field is the same in all lanes.
+struct PagedWalk {
+    int at, length, share;          // where the current (group, query tile) begins, from the share's beginning; the share
+    int b, g, qt;
+    int start, n, kv, n_groups, n_qt;
+    int done_tiles;
+    PagedGroup e;
+
+    __device__ __forceinline__ void set_request(const PagedCall& a, const int4& r) {
+        start = r.x;
+        n = r.y;
+        kv = r.z;
+        n_groups = r.w;
+        n_qt = (n + a.bq - 1) / a.bq;
+    }
+    __device__ __forceinline__ void load_group(const PagedCall& a) {
+        const int4* src = reinterpret_cast<const int4*>(a.groups + (size_t)b * a.H + g);
+        reinterpret_cast<int4*>(&e)[0] = __ldcg(src);
+        reinterpret_cast<int4*>(&e)[1] = __ldcg(src + 1);
+    }
+    // Tiles of the query tile that begins at `at` which begin before `end`: tile 0 at `at`, tile i at at + kPagedItemCost + i.
+    __device__ __forceinline__ int tiles_before(int end, int tiles) const {
+        return end <= at ? 0 : max(min(end - at - kPagedItemCost, tiles), min(tiles, 1));
+    }
+
+    // Finds the share.
+    __device__ __forceinline__ void begin(const PagedCall& a, int lane) {
+        const int per = (a.B + 31) >> 5, first = min(a.B, lane * per), last = min(a.B, first + per);
+        int4 r0 = make_int4(0, 0, 0, 0);
+        int longest = 0, bad = 0x7fffffff, cost = 0;
+        long long mine = 0;
+        auto read = [&](int i) {
+            r0 = __ldcg(reinterpret_cast<const int4*>(a.req + i));
+            const int4 r1 = __ldcg(reinterpret_cast<const int4*>(a.req + i) + 1);
+            cost = r1.x;
+            if (r1.z != CHAI_OK) bad = min(bad, i);
+            longest = max(longest, r1.y);
+            return (long long)r0.w * r1.x;
+        };
+        for (int i = first; i < last; ++i) mine += read(i);
+        long long incl = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const long long x = __shfl_up_sync(0xffffffffu, incl, o);
+            if (lane >= o) incl += x;
+        }
+        const long long total = __shfl_sync(0xffffffffu, incl, 31);
+        longest = (int)__reduce_max_sync(0xffffffffu, (unsigned)longest);
+        if (blockIdx.x == 0) {
+            bad = (int)__reduce_min_sync(0xffffffffu, (unsigned)bad);
+            if (lane == 0) {
+                reset_status(a.hdr);
+                if (bad < a.B) {
+                    a.hdr->status = __ldcg(&a.req[bad].code);
+                    a.hdr->bad_b = bad;
+                }
+            }
+        }
+        // A share holds the beginning of a tile wherever it lies, and no query tile is cut into more than kPagedMaxPieces.
+        const int even = total >> 32 == 0 ? (int)(((unsigned)total + a.ctas - 1) / a.ctas) : (int)((total + a.ctas - 1) / a.ctas);
+        share = max(max(even, kPagedItemCost + 1), (longest + kPagedItemCost) / (kPagedMaxPieces - 1) + 1);
+        const long long lo = (long long)share * (int)blockIdx.x;
+        done_tiles = 0;
+        at = length = 0;
+        if (lo >= total) return;
+        length = (int)min((long long)share, total - lo);
+        long long before = incl - mine;
+        const bool here = before <= lo && lo < incl;
+        int i = last - 1;
+        if (here && per > 1)
+            for (i = first;; ++i) {
+                const long long c = read(i);
+                if (lo < before + c) break;
+                before += c;
+            }
+        const int src = __ffs(__ballot_sync(0xffffffffu, here)) - 1;
+        b = __shfl_sync(0xffffffffu, i, src);
+        cost = __shfl_sync(0xffffffffu, cost, src);
+        r0.x = __shfl_sync(0xffffffffu, r0.x, src);
+        r0.y = __shfl_sync(0xffffffffu, r0.y, src);
+        r0.z = __shfl_sync(0xffffffffu, r0.z, src);
+        r0.w = __shfl_sync(0xffffffffu, r0.w, src);
+        const long long x = lo - __shfl_sync(0xffffffffu, before, src);
+        set_request(a, r0);
+        g = x >> 32 == 0 ? (int)((unsigned)x / (unsigned)cost) : (int)(x / cost);
+        load_group(a);
+        at = -(int)(x - (long long)g * cost);  // (of the group)
+        for (qt = n_qt - 1; qt > 0; qt -= 32) {  // query tiles from the last to the first, 32 at a time
+            const int q = qt - lane, c = q >= 0 ? kPagedItemCost + key_tiles(a, n, kv, q) : 0;
+            int sum = c;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int y = __shfl_up_sync(0xffffffffu, sum, o);
+                if (lane >= o) sum += y;
+            }
+            const unsigned behind = __ballot_sync(0xffffffffu, at + sum > 0);
+            const int w = behind != 0 ? __ffs(behind) - 1 : 31;
+            const int upto = __shfl_sync(0xffffffffu, sum, w);
+            if (behind != 0) {
+                at += upto - __shfl_sync(0xffffffffu, c, w);
+                qt -= w;
+                break;
+            }
+            at += upto;
+        }
+    }
+    // The next thing to do and its group; false: the share is done.
+    __device__ __forceinline__ bool next(const PagedCall& a, PagedItem& it, PagedGroup& entry) {
+        while (at < length) {
+            const int tiles = key_tiles(a, n, kv, qt), end = at + kPagedItemCost + tiles;
+            bool mine = at >= 0;
+            it.tiles = it.first = it.count = 0;
+            it.pieces = 1;
+            it.piece = 0;
+            it.owner = blockIdx.x;
+            if (tiles > 0 && e.cluster >= 0) {
+                it.tiles = tiles;
+                if (at >= 0 && end <= length) {
+                    it.count = tiles;
+                    it.first = done_tiles % tiles;
+                } else {
+                    const int i0 = tiles_before(0, tiles), i1 = tiles_before(length, tiles), cta = blockIdx.x;
+                    it.count = i1 - i0;
+                    mine = i1 > i0;
+                    if (it.count < tiles) {
+                        if (at < 0) it.owner = cta - (share - 1 - at) / share;
+                        const int last = tiles == 1 ? at : end - 1;  // where the last tile begins
+                        it.pieces = (last < length ? cta : cta + last / share) - it.owner + 1;
+                        it.piece = cta - it.owner;
+                        const int x = tiles_before((it.owner + 1 - cta) * share, tiles);  // tiles of the first share
+                        it.first = i0 < x ? i0 + tiles - x : i0 - x;
+                    }
+                }
+            }
+            it.b = b;
+            it.t0 = qt * a.bq;
+            it.q0 = start + it.t0;
+            it.rows = min(a.bq, n - it.t0);
+            it.n = n;
+            it.kv = kv;
+            entry = e;
+            at = end;
+            if (--qt < 0 && at < length) {
+                if (++g == n_groups) {
+                    g = 0;
+                    int4 r;
+                    do r = __ldcg(reinterpret_cast<const int4*>(a.req + ++b));
+                    while (r.w == 0);  // (there is a request behind, for the share goes on)
+                    set_request(a, r);
+                }
+                qt = n_qt - 1;
+                load_group(a);
+            }
+            if (mine) {
+                done_tiles += it.count;
+                return true;
+            }
+        }
+        return false;
+    }
+};
 
 }  // namespace chai

@@ -25,7 +25,7 @@ struct Smem {
     static constexpr int BQ = 16 * RPT, STRIDE = D + 4;
     static constexpr int Q = 0, K = Q + BQ * STRIDE, V = K + BK * STRIDE, P = V + 2 * BK * STRIDE, M = P + BQ * PSTRIDE,
                          L = M + BQ, C = L + BQ, FLOATS = C + BQ;
-    static constexpr int BYTES = FLOATS * 4 + 64 + (int)sizeof(GroupEntry);
+    static constexpr int BYTES = FLOATS * 4 + 16;
 };
 
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there) {
@@ -82,19 +82,15 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_paged_simt_kernel(const P
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int rg = (warp & 3) * 4 + (lane >> 3), cg = (warp >> 2) * 8 + (lane & 7);  // rows i * 16 + rg, keys j * 16 + cg
     dependent_grid_sync();
-    const int n_items = a.hdr->pad[kPagedItems];
-    while (true) {
-        __syncthreads();
-        if (tid == 0) *s_id = atomicAdd(&a.hdr->pad[kPagedCounter], 1);
-        __syncthreads();
-        const int id = *s_id;
-        if (id >= n_items) break;
-        GroupEntry e;
-        const PagedItem it = paged_item(a, id, &e);
-        if (it.n_kv < 0) continue;
+    PagedWalk walk;
+    walk.begin(a, lane);  // (every warp does)
+    PagedItem it;
+    PagedGroup e;
+    while (walk.next(a, it, e)) {
+        __syncthreads();  // (the shared arrays are still read by the item before)
         const int members = min(e.n, GM);
         float* out = static_cast<float*>(a.out);
-        if (it.n_kv == 0) {
+        if (it.count == 0) {
             for (int i = tid; i < it.rows * D * members; i += kThreads) {
                 const int g = i / (it.rows * D), r = i / D % it.rows;
                 int h = e.heads[0];
@@ -105,9 +101,9 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_paged_simt_kernel(const P
             }
             continue;
         }
-        const int t_first = it.q0 - __ldcg(&a.req[it.b].start);  // the tile's first row among the request's tokens
         // row t of the request sees positions below kv - n + t + 1 (causal)
-        auto sees = [&](int r) { return a.causal ? min(it.kv, it.kv - it.n + t_first + r + 1) : it.kv; };
+        auto sees = [&](int r) { return a.causal ? min(it.kv, it.kv - it.n + it.t0 + r + 1) : it.kv; };
+        auto pos0 = [&](int j) { return (it.first + j < it.tiles ? it.first + j : it.first + j - it.tiles) * BK; };
         const float* q = static_cast<const float*>(a.q) + (long long)it.q0 * a.q_stride + (long long)e.rep * D;
         for (int i = tid; i < BQ * (D / 4); i += kThreads) {
             const int r = i / (D / 4), x = i % (D / 4);
@@ -115,16 +111,16 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_paged_simt_kernel(const P
         }
         if (tid < BQ) Ms[tid] = -INFINITY, Ls[tid] = 0.f;
         auto load_k = [&](int j) {
-            if (j < it.n_kv) load_tile<TC, D>(a, true, it.b, e.cluster, (it.first_tile + j) * BK, it.kv, Ks);
+            if (j < it.count) load_tile<TC, D>(a, true, it.b, e.cluster, pos0(j), it.kv, Ks);
             asm volatile("cp.async.commit_group;" ::: "memory");
         };
         auto load_v = [&](int j, int g) {  // (buffers alternate over the members of all tiles)
-            if (j < it.n_kv) {
+            if (j < it.count) {
                 int h = e.heads[0];
 #pragma unroll
                 for (int x = 1; x < GM; ++x)
                     if (g == x) h = e.heads[x];
-                load_tile<TC, D>(a, false, it.b, h, (it.first_tile + j) * BK, it.kv, Vs + ((j * members + g) & 1) * BK * STRIDE);
+                load_tile<TC, D>(a, false, it.b, h, pos0(j), it.kv, Vs + ((j * members + g) & 1) * BK * STRIDE);
             }
             asm volatile("cp.async.commit_group;" ::: "memory");
         };
@@ -139,7 +135,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_paged_simt_kernel(const P
 #pragma unroll
                 for (int c = 0; c < CPT; ++c) acc[g][i][c] = 0.f;
 
-        for (int j = 0; j < it.n_kv; ++j) {
+        for (int j = 0; j < it.count; ++j) {
             // the latest copy is a later value tile's: everything but that has arrived
             asm volatile("cp.async.wait_group 1;" ::: "memory");
             __syncthreads();
@@ -161,7 +157,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_paged_simt_kernel(const P
                         for (int c = 0; c < 4; ++c) s2[i][c] = fma2(qq.y, kk[c].y, fma2(qq.x, kk[c].x, s2[i][c]));
                     }
                 }
-                const int col0 = (it.first_tile + j) * BK;
+                const int col0 = pos0(j);
 #pragma unroll
                 for (int i = 0; i < RPT; ++i) {
                     const int r = i * 16 + rg, end = sees(r);
@@ -268,10 +264,10 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_paged_simt_kernel(const P
         }
         // A piece: [member][row][D], then (reference, sum) of every row.
         const size_t slot_bytes = (size_t)a.slot_rows * kSlotRowBytes;
-        char* slots = a.slots + (size_t)it.slot * slot_bytes;
+        auto slot = [&](int piece) { return a.slots + (size_t)piece_slot(it.owner, piece) * slot_bytes; };
         const size_t stats = (size_t)a.slot_rows * 1024;
         {
-            float* o = reinterpret_cast<float*>(slots + (size_t)it.piece * slot_bytes);
+            float* o = reinterpret_cast<float*>(slot(it.piece));
 #pragma unroll
             for (int i = 0; i < RPT; ++i) {
                 const int r = i * 16 + rg;
@@ -286,12 +282,12 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_paged_simt_kernel(const P
                 }
             }
             if (tid < it.rows && tid < BQ)
-                reinterpret_cast<float2*>(slots + (size_t)it.piece * slot_bytes + stats)[tid] = make_float2(Ms[tid], Ls[tid]);
+                reinterpret_cast<float2*>(slot(it.piece) + stats)[tid] = make_float2(Ms[tid], Ls[tid]);
         }
         __threadfence();
         __syncthreads();
         if (tid == 0) {
-            *s_id = atomicAdd(&a.counters[it.counter], 1);
+            *s_id = atomicAdd(&a.done[it.owner], 1);
             __threadfence();
         }
         __syncthreads();
@@ -301,17 +297,17 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_paged_simt_kernel(const P
             const int x = i % (D / 4), r = i / (D / 4) % it.rows, g = i / (D / 4) / it.rows;
             float m = -INFINITY;
             for (int p = 0; p < it.pieces; ++p) {
-                const float2 ml = __ldcg(reinterpret_cast<const float2*>(slots + p * slot_bytes + stats) + r);
+                const float2 ml = __ldcg(reinterpret_cast<const float2*>(slot(p) + stats) + r);
                 if (ml.y != 0.f) m = fmaxf(m, ml.x);
             }
             const float ref = m == -INFINITY ? 0.f : m;
             float l = 0.f;
             float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
             for (int p = 0; p < it.pieces; ++p) {
-                const float2 ml = __ldcg(reinterpret_cast<const float2*>(slots + p * slot_bytes + stats) + r);
+                const float2 ml = __ldcg(reinterpret_cast<const float2*>(slot(p) + stats) + r);
                 if (ml.y == 0.f) continue;  // (nothing that the row may see)
                 const float w = expf(ml.x - ref);
-                const float4 v = __ldcg(reinterpret_cast<const float4*>(slots + p * slot_bytes + (((size_t)g * a.slot_rows + r) * D + x * 4) * 4));
+                const float4 v = __ldcg(reinterpret_cast<const float4*>(slot(p) + (((size_t)g * a.slot_rows + r) * D + x * 4) * 4));
                 l += w * ml.y;
                 o.x += w * v.x;
                 o.y += w * v.y;

@@ -52,11 +52,11 @@ inline size_t prefill_plan_smem(int H, int k) {
     return sizeof(int) * ((size_t)H + 3 * (size_t)k + (size_t)k * ((H + 31) / 32));
 }
 
-// The groups of one request, by all threads of a block: entries to out[0..], their number and the first head that could not be
-// resolved (H: none) to *n_groups and *first_bad, written by thread 0.
-__device__ __forceinline__ void plan_groups(const int32_t* __restrict__ membership, const int32_t* __restrict__ reps,
-                                            GroupEntry* __restrict__ out, int* s_plan, int H, int k, int gmax, int* n_groups,
-                                            int* first_bad) {
+static __global__ void __launch_bounds__(128)
+prefill_plan_kernel(const int32_t* __restrict__ membership, const int32_t* __restrict__ reps, WsHeader* __restrict__ hdr,
+                    int* __restrict__ n_groups, int* __restrict__ bad_out, GroupEntry* __restrict__ groups, int H, int k,
+                    int gmax) {
+    extern __shared__ __align__(16) int s_plan[];
     const int W = (H + 31) >> 5;             // 32-head words per mask
     int* mem = s_plan;                       // [H] membership of this request
     int* rep = mem + H;                      // [k] representative of each cluster, -1 if the cluster is unusable
@@ -64,9 +64,17 @@ __device__ __forceinline__ void plan_groups(const int32_t* __restrict__ membersh
     int* slot = ngrp + k;                    // [k] first group slot of the cluster
     unsigned* mask = reinterpret_cast<unsigned*>(slot + k);  // [k][W] members of each usable cluster
     __shared__ int s_total, s_first_bad, s_nbad;
-    const int tid = threadIdx.x, nt = blockDim.x, lane = tid & 31;
-    for (int h = tid; h < H; h += nt) mem[h] = membership[h];
-    for (int c = tid; c < k; c += nt) rep[c] = reps[c];
+    const int b = blockIdx.x, tid = threadIdx.x, nt = blockDim.x, lane = tid & 31;
+    // a kernel launched as a programmatic dependent may start its own set-up now; it still waits for this
+    // grid to finish (griddepcontrol.wait) before it reads anything written here
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    // launched as a programmatic dependent itself, the planner may be here while its predecessor still runs
+    // (and still uses the workspace): wait for it before the first access to global memory
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    if (b == 0)
+        for (int i = tid; i < 60; i += nt) hdr->pad[i] = 0;
+    for (int h = tid; h < H; h += nt) mem[h] = membership[(size_t)b * H + h];
+    for (int c = tid; c < k; c += nt) rep[c] = reps[(size_t)b * k + c];
     for (int i = tid; i < k * W; i += nt) mask[i] = 0u;
     if (tid == 0) {
         s_first_bad = H;
@@ -119,6 +127,7 @@ __device__ __forceinline__ void plan_groups(const int32_t* __restrict__ membersh
         if (lane == 0) s_total = carry;
     }
     __syncthreads();
+    GroupEntry* out = groups + (size_t)b * H;
     // every usable cluster writes its own groups, members in ascending head order
     for (int c = tid; c < k; c += nt) {
         const int ng = ngrp[c];
@@ -175,30 +184,8 @@ __device__ __forceinline__ void plan_groups(const int32_t* __restrict__ membersh
                 }
             }
         }
-        *n_groups = total + (nbad + gmax - 1) / gmax;
-        *first_bad = s_first_bad;
-    }
-}
-
-static __global__ void __launch_bounds__(128)
-prefill_plan_kernel(const int32_t* __restrict__ membership, const int32_t* __restrict__ reps, WsHeader* __restrict__ hdr,
-                    int* __restrict__ n_groups, int* __restrict__ bad_out, GroupEntry* __restrict__ groups, int H, int k,
-                    int gmax) {
-    extern __shared__ __align__(16) int s_plan[];
-    int total = 0, first_bad = 0;
-    const int b = blockIdx.x, tid = threadIdx.x;
-    // a kernel launched as a programmatic dependent may start its own set-up now; it still waits for this
-    // grid to finish (griddepcontrol.wait) before it reads anything written here
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    // launched as a programmatic dependent itself, the planner may be here while its predecessor still runs
-    // (and still uses the workspace): wait for it before the first access to global memory
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    if (b == 0)
-        for (int i = tid; i < 60; i += blockDim.x) hdr->pad[i] = 0;
-    plan_groups(membership + (size_t)b * H, reps + (size_t)b * k, groups + (size_t)b * H, s_plan, H, k, gmax, &total, &first_bad);
-    if (tid == 0) {
-        n_groups[b] = total;
-        bad_out[b] = first_bad < H ? first_bad + 1 : 0;
+        n_groups[b] = total + (nbad + gmax - 1) / gmax;
+        bad_out[b] = nbad > 0 ? s_first_bad + 1 : 0;
     }
 }
 
