@@ -40,8 +40,20 @@ constexpr int KST = 2;                       // key tile stages: tile kt uses st
 constexpr int TILE_BYTES = BN * 128 * 2;     // a tile slot (head_dim 64: two members' value tiles share one)
 constexpr int HALF_BYTES = TILE_BYTES / 2;   // 128 rows x 64 columns, 128-byte swizzled rows
 constexpr int SOFTMAX_WARPS = 8, EPILOGUE_WARPS = 4;
-constexpr int PV_WARP = 2 + SOFTMAX_WARPS + EPILOGUE_WARPS;
-constexpr int THREADS = 96 + (SOFTMAX_WARPS + EPILOGUE_WARPS) * 32;
+// Warps of the roles.  With e4m3 pages eight warps convert, four of which are the epilogue's too, one brings row scales, and roles are
+// whole warpgroups, which trade registers.  (Spills cost more than they look: beside this much shared memory there is hardly any L1.)
+template <bool FP8>
+struct Roles {
+    static constexpr int QK = 1, SCALES = FP8 ? 3 : -1, SOFTMAX = FP8 ? 4 : 2, EPILOGUE = SOFTMAX + SOFTMAX_WARPS, CONVERT_WARPS = FP8 ? 8 : 0;
+    static constexpr int PV = FP8 ? 2 : EPILOGUE + EPILOGUE_WARPS;
+    static constexpr int THREADS = FP8 ? 640 : 480;
+};
+constexpr int LAUNCH_REGS = 96, WORKER_REGS = 80, CONVERT_REGS = 72, SOFTMAX_REGS = 128;  // e4m3, a thread
+static_assert(128 * WORKER_REGS + 256 * CONVERT_REGS + 256 * SOFTMAX_REGS <= 640 * LAUNCH_REGS, "registers are only moved");
+template <int N>
+__device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N>
+__device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
 constexpr float REF_WINDOW = 32.f;
 constexpr uint32_t TMEM_COLS = 512;
 constexpr uint32_t S_COL0 = 0, P_COL0 = 128, O_COL0 = 256;
@@ -51,14 +63,23 @@ constexpr int OFF_Q = 0;
 constexpr int OFF_K = OFF_Q + TILE_BYTES;
 constexpr int OFF_V = OFF_K + KST * TILE_BYTES;
 constexpr int OFF_BAR = OFF_V + 4 * TILE_BYTES;
-constexpr int NUM_BARS = 23;
-constexpr int OFF_XCH = OFF_BAR + 8 * NUM_BARS + 16;
+constexpr int NUM_BARS = 35;
+// e4m3: keys and values have one stage each; in the others' places lie units (128 rows of one plane) as they come from the
+// pages, and their scales.
+template <int HD>
+struct Units {
+    static constexpr int SLOTS = HD == 128 ? 4 : 6;
+};
+constexpr int RAW_SLOTS = 6, OFF_RAW = OFF_V + 2 * TILE_BYTES, OFF_SCALES = OFF_K + TILE_BYTES;
+static_assert(OFF_RAW + Units<128>::SLOTS * BN * 128 <= OFF_BAR && OFF_RAW + Units<64>::SLOTS * BN * 64 <= OFF_BAR && OFF_SCALES + RAW_SLOTS * BN * 4 <= OFF_V,
+              "units and scales fit");
+constexpr int OFF_XCH = OFF_BAR + 8 * NUM_BARS + 24;  // (the barriers, the tensor-memory address, the abort flag)
 constexpr int OFF_LSUM = OFF_XCH + 2 * BM * 4;       // [half][row] sums
 constexpr int OFF_REF = OFF_LSUM + 2 * BM * 4;       // [row] reference of the exponentials
 constexpr int OFF_ITEM = OFF_REF + BM * 4;
 constexpr int ITEM_BYTES = 64;
 constexpr int SMEM_BYTES = OFF_ITEM + 3 * ITEM_BYTES;
-static_assert(SMEM_BYTES <= 232448, "shared memory budget");
+static_assert(OFF_ITEM % 16 == 0 && SMEM_BYTES <= 232448, "shared memory budget");
 
 struct Bars {
     uint32_t base;
@@ -75,8 +96,10 @@ struct Bars {
     __device__ __forceinline__ uint32_t epi_full() const { return base + 8 * 16; }
     __device__ __forceinline__ uint32_t epi_empty() const { return base + 8 * 17; }
     __device__ __forceinline__ uint32_t s_free() const { return base + 8 * 18; }
+    __device__ __forceinline__ uint32_t raw_full(int i) const { return base + 8 * (23 + i); }
+    __device__ __forceinline__ uint32_t raw_free(int i) const { return base + 8 * (29 + i); }
 };
-static_assert(NUM_BARS == 23, "barrier count");
+static_assert(NUM_BARS == 29 + RAW_SLOTS, "barrier count");
 
 // One unit of work, published by the loading warp to the other roles through shared memory.
 struct Item {
@@ -87,9 +110,10 @@ struct Item {
     int first, tiles; // the walk begins at key tile `first` and wraps around at `tiles`
     int sees;         // positions that row 0 sees; row r: r more, at most kv (unmasked: kv)
     int kv;
-    int pieces, piece, owner;
+    int pieces, owner;
+    short piece, cluster;
     int heads[GMAX];
-    int pad;
+    int b;
 };
 static_assert(sizeof(Item) == ITEM_BYTES, "item descriptor");
 
@@ -100,12 +124,212 @@ struct Tma {
     CUtensorMap q, k, v;
 };
 
+// e4m3: the slot of the next unit, and the parity of its filling.
 template <int HD>
-__global__ void __launch_bounds__(THREADS, 1)
-prefill_paged_kernel(const __grid_constant__ Tma maps, const PagedCall a, const int box_rows, const float scale_log2) {
+struct Unit {
+    int slot = 0, phase = 0;
+    __device__ __forceinline__ void next() {
+        if (++slot == Units<HD>::SLOTS) slot = 0, phase ^= 1;
+    }
+};
+
+// Four e4m3 numbers times a scale, as bf16 (rounded once where the scale is a power of two, twice otherwise).
+__device__ __forceinline__ void e4m3x4_to_bf16(uint32_t w, float scale, uint32_t* o) {
+    const __half2_raw lo = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w & 0xffffu), __NV_E4M3);
+    const __half2_raw hi = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w >> 16), __NV_E4M3);
+    const float2 u = __half22float2(*reinterpret_cast<const __half2*>(&lo)), v = __half22float2(*reinterpret_cast<const __half2*>(&hi));
+    const __nv_bfloat162 p = __floats2bfloat162_rn(u.x * scale, u.y * scale), q = __floats2bfloat162_rn(v.x * scale, v.y * scale);
+    o[0] = *reinterpret_cast<const uint32_t*>(&p);
+    o[1] = *reinterpret_cast<const uint32_t*>(&q);
+}
+// The same by moving bits, for a scale 2^e with -126 <= e <= 7: the byte s eeee mmm is, as the bf16 number s 0000eeee mmm0000, its
+// value times 2^-120 (the exponents' biases are 7 and 127; e4m3's subnormal numbers become bf16's), and the product with 2^(120 + e)
+// is exact.  The result has the highest bit of a byte set where that number is a NaN, which this does not know: 1111 111 would
+// be 480.  (The conversion instructions run on a pipe that takes them some thirty cycles a warp.)
+__device__ __forceinline__ uint32_t e4m3_factor(float scale) {  // (two bf16 numbers: the upper halves of fp32's)
+    const uint32_t f = __float_as_uint(scale * 0x1p120f);
+    return __byte_perm(f, f, 0x3232);
+}
+__device__ __forceinline__ uint32_t e4m3x4_to_bf16_bits(uint32_t w, uint32_t factor, uint32_t* o) {
+    const uint32_t high = (w & 0x80808080u) | ((w >> 4) & 0x07070707u), low = (w << 4) & 0xf0f0f0f0u;
+    uint32_t p[2] = {__byte_perm(low, high, 0x5140), __byte_perm(low, high, 0x7362)};
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const __nv_bfloat162 v = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&p[i]), *reinterpret_cast<const __nv_bfloat162*>(&factor));
+        o[i] = *reinterpret_cast<const uint32_t*>(&v);
+    }
+    return (w & 0x7f7f7f7fu) + 0x01010101u;
+}
+
+// Writes out the ei-th finished item, by the four epilogue warps, one thread per query row; false: there is none any more, or a wait ran
+// out.
+template <int HD, int JOIN>
+__device__ __forceinline__ bool finish_item(const PagedCall& a, uint8_t* smem, uint32_t tmem_base, volatile int* abort_flag, int ei) {
+    constexpr int GM = HD == 128 ? 2 : 4;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const Item* items = reinterpret_cast<const Item*>(smem + OFF_ITEM);
+    const Bars bar{smem_u32(smem) + OFF_BAR};
+    const int quad = warp & 3, row = quad * 32 + lane;
+    const uint32_t lane_addr = tmem_base + ((uint32_t)(quad * 32) << 16);
+    const float* lsum = reinterpret_cast<const float*>(smem + OFF_LSUM);
+    const float* refs = reinterpret_cast<const float*>(smem + OFF_REF);
+    __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.out);
+    const bool wide = (reinterpret_cast<uintptr_t>(out) & 31u) == 0;
+    const size_t slot_bytes = (size_t)a.slot_rows * kSlotRowBytes, stats = (size_t)a.slot_rows * 1024;
+    bool ok = __all_sync(0xffffffffu, mbar_wait(bar.epi_full(), ei & 1, abort_flag));
+    if (!ok) return false;
+    const Item ep = items[2];
+    const float l = lsum[row] + lsum[BM + row], ref = refs[row];
+    if (ep.n_members < 0) return false;
+    const int last = ep.n_kv;
+    ok = __all_sync(0xffffffffu, mbar_wait(bar.pv_done(last & 1), (last >> 1) & 1, abort_flag));
+    if (!ok) return false;
+    tc_fence_after();
+    __syncwarp();
+    if (lane == 0) mbar_arrive(bar.epi_empty());
+    const bool live = row < ep.rows, split = ep.pieces > 1;
+    const float inv = split ? 1.f : l == 0.f ? 0.f : 1.f / l;  // (a NaN stays one)
+    const uint64_t inv2 = pack2(inv, inv);
+    auto slot = [&](int piece) { return a.slots + (size_t)piece_slot(ep.owner, piece) * slot_bytes; };
+    float* part = reinterpret_cast<float*>(slot(ep.piece));
+    constexpr int NSUB = HD / 32;
+    const int n_sub = ep.n_members * NSUB;
+    uint32_t cur[32];
+#pragma unroll
+    for (int c = 0; c < GM * NSUB; ++c) {
+        if (c >= n_sub) break;
+        __syncwarp();  // (the stores below are for some lanes only, the load is for the warp as a whole)
+        tc_ld32_wait(lane_addr + O_COL0 + c * 32, cur);  // (members' accumulators are contiguous)
+        const int g = c / NSUB, sc = c % NSUB;
+        if (sc == NSUB - 1) {
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) {
+                mbar_arrive(bar.o_free(g));
+                if (g == ep.n_members - 1)
+                    for (int x = ep.n_members; x < GM; ++x) mbar_arrive(bar.o_free(x));
+            }
+        }
+        if (live && !split) {
+            int h = ep.heads[0];
+#pragma unroll
+            for (int x = 1; x < GM; ++x)
+                if (g == x) h = ep.heads[x];
+            __nv_bfloat16* orow = out + ((size_t)(ep.row0 + row) * a.H + h) * HD + sc * 32;
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                uint32_t w[8];
+#pragma unroll
+                for (int x = 0; x < 8; ++x) {
+                    float y0, y1;
+                    unpack2(mul2(pack2(__uint_as_float(cur[16 * u + 2 * x]), __uint_as_float(cur[16 * u + 2 * x + 1])), inv2), y0, y1);
+                    if (inv == 0.f) y0 = y1 = 0.f;
+                    __nv_bfloat162 pk = __floats2bfloat162_rn(y0, y1);
+                    w[x] = *reinterpret_cast<uint32_t*>(&pk);
+                }
+                st_global_row32(orow + u * 16, w, wide);
+            }
+        } else if (live) {
+            float* prow = part + ((size_t)g * a.slot_rows + row) * HD + sc * 32;
+#pragma unroll
+            for (int u = 0; u < 8; ++u)
+                reinterpret_cast<uint4*>(prow)[u] = make_uint4(cur[4 * u], cur[4 * u + 1], cur[4 * u + 2], cur[4 * u + 3]);
+        }
+    }
+    if (!split || quad * 32 >= ep.rows) return true;
+    // A piece: its rows' references and sums; the warp that finishes its rows' last piece joins them, in order of the
+    // pieces.  (A byte of the counter per warp.)
+    if (live) reinterpret_cast<float2*>(reinterpret_cast<char*>(part) + stats)[row] = make_float2(ref, l);
+    __threadfence();
+    __syncwarp();
+    unsigned before = 0;
+    if (lane == 0) {
+        before = (unsigned)atomicAdd(&a.done[ep.owner], 1 << (8 * quad)) >> (8 * quad) & 255u;
+        __threadfence();
+    }
+    before = __shfl_sync(0xffffffffu, before, 0);
+    if ((int)before != ep.pieces - 1) return true;
+    const int n_rows = min(32, ep.rows - quad * 32), pieces = ep.pieces;
+    // First a lane a row: the reference of all pieces, and what the sum is divided by.
+    float m_all = -INFINITY, sum = 0.f;
+#pragma unroll 4
+    for (int p = 0; p < pieces; ++p) {
+        const float2 s = live ? __ldcg(reinterpret_cast<const float2*>(slot(p) + stats) + row) : make_float2(0.f, 0.f);
+        if (s.y == 0.f) continue;  // (a piece that the row sees nothing of)
+        const float m = fmaxf(m_all, s.x);
+        sum = sum * (sum == 0.f ? 0.f : fast_exp2(m_all - m)) + s.y * fast_exp2(s.x - m);
+        m_all = m;
+    }
+    const float over = sum == 0.f ? 0.f : 1.f / sum;
+    // Then the warp goes through the rows, piece by piece, a lane 8 columns of one member; JOIN (row, piece) at a time, whose
+    // loads are under way at once.
+    const int g = lane / (HD / 8), x = lane % (HD / 8);
+    const bool mine = g < ep.n_members;
+    int h = ep.heads[0];
+#pragma unroll
+    for (int i = 1; i < GM; ++i)
+        if (g == i) h = ep.heads[i];
+    const size_t column = (size_t)g * a.slot_rows * HD + x * 8;
+    __nv_bfloat16* to = out + ((size_t)(ep.row0 + quad * 32) * a.H + h) * HD + x * 8;
+    int r_load = 0, p_load = 0, r_use = 0, p_use = 0;
+    float o8[8] = {};
+#pragma unroll 1
+    for (int left = n_rows * pieces; left > 0; left -= JOIN) {
+        float4 v[JOIN][2];
+        float2 s[JOIN];
+#pragma unroll
+        for (int u = 0; u < JOIN; ++u) {
+            v[u][0] = v[u][1] = make_float4(0.f, 0.f, 0.f, 0.f);
+            s[u] = make_float2(0.f, 0.f);
+            if (u < left) {
+                const char* base = slot(p_load);
+                const int rw = quad * 32 + r_load;
+                s[u] = __ldcg(reinterpret_cast<const float2*>(base + stats) + rw);
+                if (mine) {
+                    const float4* src = reinterpret_cast<const float4*>(reinterpret_cast<const float*>(base) + column + (size_t)rw * HD);
+                    v[u][0] = __ldcg(src);
+                    v[u][1] = __ldcg(src + 1);
+                }
+            }
+            if (++p_load == pieces) p_load = 0, ++r_load;
+        }
+#pragma unroll
+        for (int u = 0; u < JOIN; ++u) {
+            const float m = __shfl_sync(0xffffffffu, m_all, r_use & 31), f = __shfl_sync(0xffffffffu, over, r_use & 31);
+            if (s[u].y != 0.f) {
+                const float w = fast_exp2(s[u].x - m);
+                o8[0] += w * v[u][0].x, o8[1] += w * v[u][0].y, o8[2] += w * v[u][0].z, o8[3] += w * v[u][0].w;
+                o8[4] += w * v[u][1].x, o8[5] += w * v[u][1].y, o8[6] += w * v[u][1].z, o8[7] += w * v[u][1].w;
+            }
+            if (++p_use == pieces) {
+                if (mine && u < left) {
+                    uint4 w;
+                    uint32_t* words = &w.x;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const __nv_bfloat162 pk = __floats2bfloat162_rn(o8[2 * i] * f, o8[2 * i + 1] * f);
+                        words[i] = *reinterpret_cast<const uint32_t*>(&pk);
+                    }
+                    *reinterpret_cast<uint4*>(to + (size_t)r_use * a.H * HD) = w;
+                }
+#pragma unroll
+                for (int i = 0; i < 8; ++i) o8[i] = 0.f;
+                p_use = 0;
+                ++r_use;
+            }
+        }
+    }
+    return true;
+}
+
+template <int HD, bool FP8>
+__global__ void __launch_bounds__(Roles<FP8>::THREADS, 1)
+prefill_paged_kernel(const __grid_constant__ Tma maps, const __grid_constant__ PagedCall a, const int box_rows, const float scale_log2) {
+    using R = Roles<FP8>;
     constexpr int GM = HD == 128 ? 2 : 4, HALVES = HD / 64, ROW_BYTES = HD * 2;
-    // Bytes between two 64-column blocks of a value box, and between two boxes of a value tile (those of all members).
-    const int v_block = box_rows * 128, v_box = GM * HALVES * v_block;
+    // Bytes between two 64-column blocks of a value box, and between two boxes of a value tile (those of all members).  (e4m3: the
+    // converting warps write a tile as one box.)
+    const int tile_rows = FP8 ? BN : box_rows, v_block = tile_rows * 128, v_box = GM * HALVES * v_block;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     extern __shared__ uint8_t smem[];
     const uint32_t sbase = smem_u32(smem);
@@ -129,11 +353,15 @@ prefill_paged_kernel(const __grid_constant__ Tma maps, const PagedCall a, const 
         for (int i = 0; i < 2; ++i) {
             mbar_init(bar.p_full(i), SOFTMAX_WARPS);
             mbar_init(bar.item_full(i), 1);
-            mbar_init(bar.item_empty(i), 2 + SOFTMAX_WARPS);
-            mbar_init(bar.k_full(i), 1);
-            mbar_init(bar.v_full(i), 1);
+            mbar_init(bar.item_empty(i), 2 + SOFTMAX_WARPS + R::CONVERT_WARPS + (FP8 ? 1 : 0));
+            mbar_init(bar.k_full(i), FP8 ? R::CONVERT_WARPS : 1);
+            mbar_init(bar.v_full(i), FP8 ? R::CONVERT_WARPS : 1);
             mbar_init(bar.qk_done(i), 1);
             mbar_init(bar.pv_done(i), 1);
+        }
+        for (int i = 0; i < RAW_SLOTS; ++i) {
+            mbar_init(bar.raw_full(i), 2);  // the copies, and the scales
+            mbar_init(bar.raw_free(i), 8);  // (e4m3: R::CONVERT_WARPS)
         }
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -152,12 +380,14 @@ prefill_paged_kernel(const __grid_constant__ Tma maps, const PagedCall a, const 
 
     if (warp == 0) {
         // ---------------- work distribution and loads, by all lanes ----------------
+        if constexpr (FP8) fewer_registers<WORKER_REGS>();
         auto wait_all = [&](uint32_t b, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait(b, parity, abort_flag)); };
         const int blocks = BN / box_rows;                    // boxes of a tile
         bool ok = true;
         int it = 0, qi = 0, kt = 0;                          // items published, items with loads, key tiles issued
         PagedGroup e, e_next;
         PagedItem cur = {}, nxt = {};
+        [[maybe_unused]] Unit<HD> unit;
         PagedWalk walk;
         walk.begin(a, lane);
         bool more = walk.next(a, cur, e);
@@ -184,7 +414,9 @@ prefill_paged_kernel(const __grid_constant__ Tma maps, const PagedCall a, const 
                 item.kv = kv;
                 item.sees = a.causal ? kv - cur.n + cur.t0 + 1 : kv;
                 item.pieces = cur.pieces;
-                item.piece = cur.piece;
+                item.piece = (short)cur.piece;
+                item.cluster = (short)e.cluster;
+                item.b = cur.b;
                 item.owner = cur.owner;
 #pragma unroll
                 for (int g = 0; g < GMAX; ++g) item.heads[g] = g < n_members ? e.heads[g] : e.heads[0];
@@ -223,6 +455,34 @@ prefill_paged_kernel(const __grid_constant__ Tma maps, const PagedCall a, const 
                     tma_load_3d(sbase + OFF_Q + h * HALF_BYTES, &maps.q, h * 64, e.rep, cur.q0, bar.q_full());
             }
             __syncwarp();
+            if constexpr (FP8) {  // units in order: K(0), K(1), V(0) of every member, K(2), V(1), ...
+                auto load_unit = [&](bool key, int plane, int j, int page, int row) -> bool {
+                    const int count = boxes(j);
+                    if (!wait_all(bar.raw_free(unit.slot), unit.phase ^ 1)) return false;
+                    if (lane == 0) mbar_expect_tx(bar.raw_full(unit.slot), count * box_rows * HD);
+                    __syncwarp();
+                    if (lane < count)
+                        tma_load_3d(sbase + OFF_RAW + (unit.slot * BN + lane * box_rows) * HD, key ? &maps.k : &maps.v, 0, plane * a.pool.page_size + row, page, bar.raw_full(unit.slot));
+                    unit.next();
+                    return true;
+                };
+                ok = load_unit(true, e.cluster, 0, page_v, row_v);
+                for (int j = 0; j < n_kv && ok; ++j) {
+                    look_up(j + 2, page_n, row_n);
+                    if (j + 1 < n_kv) ok = load_unit(true, e.cluster, j + 1, page_k, row_k);
+#pragma unroll
+                    for (int g = 0; g < GM; ++g)
+                        if (g < n_members && ok) ok = load_unit(false, e.heads[g], j, page_v, row_v);
+                    if (j == 0) more = walk.next(a, nxt, e_next);
+                    page_v = page_k, row_v = row_k;
+                    page_k = page_n, row_k = row_n;
+                }
+                kt += n_kv;
+                ++qi;
+                cur = nxt;
+                e = e_next;
+                continue;
+            }
             auto load_k = [&](int j, int page, int row) -> bool {
                 const int n = kt + j, ts = n & 1, count = boxes(j);
                 if (!wait_all(bar.qk_done(ts), ((n >> 1) & 1) ^ 1)) return false;  // stage free
@@ -266,21 +526,23 @@ prefill_paged_kernel(const __grid_constant__ Tma maps, const PagedCall a, const 
             cur = nxt;
             e = e_next;
         }
-    } else if (warp == 1 || warp == PV_WARP) {
+    } else if (warp == R::QK || warp == R::PV) {
         // ---------------- MMA issuers ----------------
+        if constexpr (FP8) fewer_registers<WORKER_REGS>();
         constexpr uint32_t IDESC_QK = make_idesc(false);
         auto desc = [](uint32_t hi, uint32_t lo) { return ((uint64_t)hi << 32) | lo; };
-        auto wait_all = [&](uint32_t b, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait_polling(b, parity, abort_flag)); };
-        const bool qk_role = warp == 1;
+        // (e4m3: polling takes issue slots from the converting warps, 2 % of the kernel's time)
+        auto wait_all = [&](uint32_t b, uint32_t parity) { return __all_sync(0xffffffffu, (FP8 ? mbar_wait(b, parity, abort_flag) : mbar_wait_polling(b, parity, abort_flag))); };
+        const bool qk_role = warp == R::QK;
         const uint64_t dq = make_desc(sbase + OFF_Q, 16, 1024);
         // keys: 8-row groups of HALVES blocks of 1 KB; values: 8-row groups of a block 1 KB apart, or (boxes of 8 rows) a box apart
         const uint64_t dk = make_desc(sbase + OFF_K, 16, HALVES * 1024);
-        const uint64_t dv = make_desc(sbase + OFF_V, v_block, box_rows == 8 ? v_box : 1024);
+        const uint64_t dv = make_desc(sbase + OFF_V, v_block, tile_rows == 8 ? v_box : 1024);
         const uint32_t hi_q = (uint32_t)(dq >> 32), hi_k = (uint32_t)(dk >> 32), hi_v = (uint32_t)(dv >> 32);
         const uint32_t q_lo = (uint32_t)dq, k_lo = (uint32_t)dk, v_lo = (uint32_t)dv;
         // 16 keys further in a value tile: within a box of 128 rows or less, or in another box
-        const int box_shift = __ffs(box_rows) - 1;
-        const int steps_of_box = box_rows >= 16 ? box_rows / 16 : 1, box_step = box_rows >= 16 ? v_box : 2 * v_box, step_shift = __ffs(steps_of_box) - 1;
+        const int box_shift = __ffs(tile_rows) - 1;
+        const int steps_of_box = tile_rows >= 16 ? tile_rows / 16 : 1, box_step = tile_rows >= 16 ? v_box : 2 * v_box, step_shift = __ffs(steps_of_box) - 1;
         bool ok = true;
         int it = 0, qi = 0, kt = 0;
         while (ok) {
@@ -301,7 +563,7 @@ prefill_paged_kernel(const __grid_constant__ Tma maps, const PagedCall a, const 
                     if (!ok) break;
                     tc_fence_after();
                     const uint32_t d = tmem_base + S_COL0;
-                    const uint32_t kb = k_lo + ts * (TILE_BYTES >> 4);
+                    const uint32_t kb = k_lo + (FP8 ? 0 : ts) * (TILE_BYTES >> 4);
                     if (elect_one()) {
 #pragma unroll
                         for (int s = 0; s < HD / 16; ++s) {
@@ -319,7 +581,7 @@ prefill_paged_kernel(const __grid_constant__ Tma maps, const PagedCall a, const 
                     ok = wait_all(bar.v_full(ts), (kt >> 1) & 1);
                     if (!ok) break;
                     const int valid = kv - tile_col(first, tiles, j);
-                    if (valid < BN) {  // rows behind the request's length: zeros, whatever is there
+                    if (!FP8 && valid < BN) {  // rows behind the request's length: zeros, whatever is there
                         const int strip = lane >> 3;  // a 64-column block of a member: 4 in all
                         if (strip < n_members * HALVES)
                             for (int r = valid; r < BN; ++r) {
@@ -338,7 +600,7 @@ prefill_paged_kernel(const __grid_constant__ Tma maps, const PagedCall a, const 
                     tc_fence_after();
                     if (elect_one()) {
                         const uint32_t d = tmem_base + O_COL0;
-                        const uint32_t vb = v_lo + (ts * 2) * (TILE_BYTES >> 4);
+                        const uint32_t vb = v_lo + (FP8 ? 0 : ts * 2) * (TILE_BYTES >> 4);
                         const uint32_t idesc_all = make_idesc_n(true, (unsigned)(HD * n_members));
 #pragma unroll
                         for (int s = 0; s < BN / 16; ++s)
@@ -350,9 +612,10 @@ prefill_paged_kernel(const __grid_constant__ Tma maps, const PagedCall a, const 
             }
             ++qi;
         }
-    } else if (warp < 2 + SOFTMAX_WARPS) {
+    } else if (warp >= R::SOFTMAX && warp < R::EPILOGUE) {
         // ---------------- softmax / correction: two threads per query row ----------------
-        const int quad = warp & 3, half = (warp - 2) >> 2;
+        if constexpr (FP8) more_registers<SOFTMAX_REGS>();
+        const int quad = warp & 3, half = (warp - R::SOFTMAX) >> 2;
         const int row = quad * 32 + lane, cbase = half * 64;
         const uint32_t lane_addr = tmem_base + ((uint32_t)(quad * 32) << 16);
         __nv_bfloat16* xch = reinterpret_cast<__nv_bfloat16*>(smem + OFF_XCH);  // [tile parity][half][row]
@@ -369,7 +632,7 @@ prefill_paged_kernel(const __grid_constant__ Tma maps, const PagedCall a, const 
             const int n_kv = items[is].n_kv, n_members = items[is].n_members, rows = items[is].rows;
             const int first = items[is].first, tiles = items[is].tiles, kv = items[is].kv, sees0 = items[is].sees;
             // (the warp that hands the item on to the epilogue keeps it until then)
-            const bool keeps = warp == 2 && n_kv > 0;
+            const bool keeps = warp == R::SOFTMAX && n_kv > 0;
             if (n_kv == 0 && row < rows)
 #pragma unroll
                 for (int g = 0; g < GM; ++g) {
@@ -508,7 +771,7 @@ prefill_paged_kernel(const __grid_constant__ Tma maps, const PagedCall a, const 
             if (!ok) break;
             lsum[half * BM + row] = l_run;
             if (half == 0) refs[row] = m_used;
-            if (tid == 64) {
+            if (tid == 32 * R::SOFTMAX) {
                 items[2] = items[is];
                 items[2].n_kv = kt - 1;  // number of the item's last key tile (its P V is awaited)
                 mbar_arrive(bar.item_empty(is));
@@ -518,157 +781,183 @@ prefill_paged_kernel(const __grid_constant__ Tma maps, const PagedCall a, const 
             ++ei;
         }
         if (__all_sync(0xffffffffu, mbar_wait(bar.epi_empty(), (ei & 1) ^ 1, abort_flag))) {
-            if (tid == 64) items[2].n_members = -1;
+            if (tid == 32 * R::SOFTMAX) items[2].n_members = -1;
             __syncwarp();
             if (lane == 0) mbar_arrive(bar.epi_full());
         }
         if (!ok) asm volatile("bar.arrive %0, 64;" ::"r"(quad + 1) : "memory");
-    } else {
+    } else if (warp >= R::EPILOGUE) {
         // ---------------- epilogue: one thread per query row ----------------
-        const int quad = warp & 3, row = quad * 32 + lane;
-        const uint32_t lane_addr = tmem_base + ((uint32_t)(quad * 32) << 16);
-        const float* lsum = reinterpret_cast<const float*>(smem + OFF_LSUM);
-        const float* refs = reinterpret_cast<const float*>(smem + OFF_REF);
-        __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.out);
-        const bool wide = (reinterpret_cast<uintptr_t>(out) & 31u) == 0;
-        const size_t slot_bytes = (size_t)a.slot_rows * kSlotRowBytes, stats = (size_t)a.slot_rows * 1024;
-        for (int ei = 0;; ++ei) {
-            bool ok = __all_sync(0xffffffffu, mbar_wait(bar.epi_full(), ei & 1, abort_flag));
-            if (!ok) break;
-            const Item ep = items[2];
-            const float l = lsum[row] + lsum[BM + row], ref = refs[row];
-            if (ep.n_members < 0) break;
-            const int last = ep.n_kv;
-            ok = __all_sync(0xffffffffu, mbar_wait(bar.pv_done(last & 1), (last >> 1) & 1, abort_flag));
-            if (!ok) break;
-            tc_fence_after();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(bar.epi_empty());
-            const bool live = row < ep.rows, split = ep.pieces > 1;
-            const float inv = split ? 1.f : l == 0.f ? 0.f : 1.f / l;  // (a NaN stays one)
-            const uint64_t inv2 = pack2(inv, inv);
-            auto slot = [&](int piece) { return a.slots + (size_t)piece_slot(ep.owner, piece) * slot_bytes; };
-            float* part = reinterpret_cast<float*>(slot(ep.piece));
-            constexpr int NSUB = HD / 32;
-            const int n_sub = ep.n_members * NSUB;
-            uint32_t ra[32], rb[32];
-            tc_ld32(lane_addr + O_COL0, ra);
-            tc_wait_ld32(ra);
-#pragma unroll
-            for (int c = 0; c < GM * NSUB; ++c) {
-                if (c >= n_sub) break;
-                uint32_t* cur = (c & 1) ? rb : ra;
-                uint32_t* nxt = (c & 1) ? ra : rb;
-                const int g = c / NSUB, sc = c % NSUB;
-                if (c + 1 < n_sub) tc_ld32(lane_addr + O_COL0 + (c + 1) * 32, nxt);
-                if (sc == NSUB - 1) {
-                    tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) {
-                        mbar_arrive(bar.o_free(g));
-                        if (g == ep.n_members - 1)
-                            for (int x = ep.n_members; x < GM; ++x) mbar_arrive(bar.o_free(x));
-                    }
-                }
-                if (live && !split) {
-                    int h = ep.heads[0];
-#pragma unroll
-                    for (int x = 1; x < GM; ++x)
-                        if (g == x) h = ep.heads[x];
-                    __nv_bfloat16* orow = out + ((size_t)(ep.row0 + row) * a.H + h) * HD + sc * 32;
-#pragma unroll
-                    for (int u = 0; u < 2; ++u) {
-                        uint32_t w[8];
-#pragma unroll
-                        for (int x = 0; x < 8; ++x) {
-                            float y0, y1;
-                            unpack2(mul2(pack2(__uint_as_float(cur[16 * u + 2 * x]), __uint_as_float(cur[16 * u + 2 * x + 1])), inv2), y0, y1);
-                            if (inv == 0.f) y0 = y1 = 0.f;
-                            __nv_bfloat162 pk = __floats2bfloat162_rn(y0, y1);
-                            w[x] = *reinterpret_cast<uint32_t*>(&pk);
-                        }
-                        st_global_row32(orow + u * 16, w, wide);
-                    }
-                } else if (live) {
-                    float* prow = part + ((size_t)g * a.slot_rows + row) * HD + sc * 32;
-#pragma unroll
-                    for (int u = 0; u < 8; ++u)
-                        reinterpret_cast<uint4*>(prow)[u] = make_uint4(cur[4 * u], cur[4 * u + 1], cur[4 * u + 2], cur[4 * u + 3]);
-                }
-                if (c + 1 < n_sub) tc_wait_ld32(nxt);
-            }
-            if (!split || quad * 32 >= ep.rows) continue;
-            // A piece: its rows' references and sums; the warp that finishes its rows' last piece joins them, in order of the
-            // pieces.  (A byte of the counter per warp.)
-            if (live) reinterpret_cast<float2*>(reinterpret_cast<char*>(part) + stats)[row] = make_float2(ref, l);
-            __threadfence();
-            __syncwarp();
-            unsigned before = 0;
-            if (lane == 0) {
-                before = (unsigned)atomicAdd(&a.done[ep.owner], 1 << (8 * quad)) >> (8 * quad) & 255u;
-                __threadfence();
-            }
-            before = __shfl_sync(0xffffffffu, before, 0);
-            if ((int)before != ep.pieces - 1) continue;
-            const int n_rows = min(32, ep.rows - quad * 32);
-            // Lane l holds the statistics of piece l; the warp takes JOIN rows at a time, a lane 8 columns of one member, and
-            // has the loads of a piece for all of them under way at once.
-            constexpr int JOIN = 4;
-            const int g = lane / (HD / 8), x = lane % (HD / 8);
-            int h = ep.heads[0];
-#pragma unroll
-            for (int i = 1; i < GM; ++i)
-                if (g == i) h = ep.heads[i];
+        if constexpr (!FP8) {
+            for (int ei = 0; finish_item<HD, 8>(a, smem, tmem_base, abort_flag, ei); ++ei) {}
+        } else {
+            // e4m3: units become bf16 tiles, by eight warps; a thread takes 16 numbers of NV rows, a row at a time: there are no
+            // registers for more, and what is spilled comes back from L2.  The first four warps write the item before
+            // out ahead of V(0), whose product waits for its accumulators.  (Two teams that take turns would hide more of the
+            // waits, but a team that does not wait for every tile's products in order can mistake a barrier's phase for another.)
+            fewer_registers<CONVERT_REGS>();
+            constexpr int CHUNKS = HD / 16, STEP = 32 * R::CONVERT_WARPS / CHUNKS, NV = BN / STEP;
+            const int ct = tid - 32 * R::EPILOGUE, x = ct % CHUNKS, row = ct / CHUNKS;  // row + i * STEP
+            const bool writes_out = warp < R::EPILOGUE + EPILOGUE_WARPS;
+            // 16 numbers are two 16-byte vectors of the bf16 row, in its 64-column block x / 4; vectors are swizzled within 128 bytes
+            const uint32_t swizzled = (((x & 3) * 2) ^ (row & 7)) << 4;  // (STEP is a multiple of 8; the other vector: ^ 16)
+            const uint32_t k_row = sbase + OFF_K + (row >> 3) * (HALVES * 1024) + (row & 7) * 128 + (x >> 2) * 1024 + swizzled;
+            const uint32_t v_row = sbase + OFF_V + row * 128 + (x >> 2) * HALF_BYTES + swizzled;
+            auto wait_all = [&](uint32_t b, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait(b, parity, abort_flag)); };
+            Unit<HD> unit;
+            bool ok = true, pending = false;
+            int it = 0, kt = 0, ei = 0;  // items seen, key tiles, items written out
+            // The next unit to dst, rows STEP apart `apart` bytes; rows from `valid` on become zeros.
+            auto convert = [&](uint32_t dst, uint32_t apart, int valid) -> bool {
+                if (!wait_all(bar.raw_full(unit.slot), unit.phase)) return false;
+                valid -= row;
+                const uint8_t* raw = smem + OFF_RAW + (unit.slot * BN + row) * HD + x * 16;
+                const float* scales = reinterpret_cast<const float*>(smem + OFF_SCALES) + unit.slot * BN + row;
+                // Two rows at a time, for one chain of dependent instructions leaves most of the issue slots empty; not unrolled, for
+                // what does not fit the instruction caches beside the other roles' loops waits for them.
 #pragma unroll 1
-            for (int r0 = 0; r0 < n_rows; r0 += JOIN) {
-                const int first_row = quad * 32 + r0;
-                float2 mine[JOIN];
-                float o8[JOIN][8], sum[JOIN], w_mine[JOIN];
+                for (int i0 = 0; i0 < NV; i0 += 2) {
+                    uint4 v[2];
+                    float scale[2];
+                    uint32_t o[2][8];
+                    bool other = false;  // a NaN, or a scale that is no power of two or above 2^7
 #pragma unroll
-                for (int u = 0; u < JOIN; ++u)
-                    mine[u] = lane < ep.pieces && r0 + u < n_rows ? __ldcg(reinterpret_cast<const float2*>(slot(lane) + stats) + first_row + u) : make_float2(0.f, 0.f);
-#pragma unroll
-                for (int u = 0; u < JOIN; ++u) {
-                    float m = mine[u].y != 0.f ? mine[u].x : -INFINITY;  // (a piece that the row sees nothing of has the sum 0)
-#pragma unroll
-                    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-                    w_mine[u] = mine[u].y != 0.f ? fast_exp2(mine[u].x - m) : 0.f;
-                    sum[u] = 0.f;
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) o8[u][i] = 0.f;
-                }
-#pragma unroll 2
-                for (int p = 0; p < ep.pieces; ++p) {
-                    const float* src = reinterpret_cast<const float*>(slot(p)) + ((size_t)g * a.slot_rows + first_row) * HD + x * 8;
-                    float4 v[JOIN][2];
-#pragma unroll
-                    for (int u = 0; u < JOIN; ++u)
-                        if (g < ep.n_members && r0 + u < n_rows) {
-                            v[u][0] = __ldcg(reinterpret_cast<const float4*>(src + u * HD));
-                            v[u][1] = __ldcg(reinterpret_cast<const float4*>(src + u * HD) + 1);
-                        }
-#pragma unroll
-                    for (int u = 0; u < JOIN; ++u) {
-                        const float w = __shfl_sync(0xffffffffu, w_mine[u], p), l = __shfl_sync(0xffffffffu, mine[u].y, p);
-                        if (l == 0.f) continue;
-                        sum[u] += w * l;
-                        o8[u][0] += w * v[u][0].x, o8[u][1] += w * v[u][0].y, o8[u][2] += w * v[u][0].z, o8[u][3] += w * v[u][0].w;
-                        o8[u][4] += w * v[u][1].x, o8[u][5] += w * v[u][1].y, o8[u][6] += w * v[u][1].z, o8[u][7] += w * v[u][1].w;
+                    for (int i = 0; i < 2; ++i) {
+                        v[i] = *reinterpret_cast<const uint4*>(raw + i * STEP * HD);
+                        scale[i] = scales[i * STEP];
+                        if (i * STEP >= valid) v[i] = make_uint4(0, 0, 0, 0), scale[i] = 1.f;
                     }
-                }
 #pragma unroll
-                for (int u = 0; u < JOIN; ++u) {
-                    if (g >= ep.n_members || r0 + u >= n_rows) continue;
-                    const float f = sum[u] == 0.f ? 0.f : 1.f / sum[u];
-                    uint4 w;
-                    uint32_t* words = &w.x;
+                    for (int i = 0; i < 2; ++i) {
+                        const uint32_t words[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+                        const uint32_t f = e4m3_factor(scale[i]);
+                        uint32_t nan = 0;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        __nv_bfloat162 pk = __floats2bfloat162_rn(o8[u][2 * i] * f, o8[u][2 * i + 1] * f);
-                        words[i] = *reinterpret_cast<uint32_t*>(&pk);
+                        for (int w = 0; w < 4; ++w) nan |= e4m3x4_to_bf16_bits(words[w], f, o[i] + 2 * w);
+                        other |= (nan & 0x80808080u) != 0 || (__float_as_uint(scale[i]) & 0x007fffffu) != 0 || __float_as_uint(scale[i]) - 0x00800000u > 0x42800000u;
                     }
-                    reinterpret_cast<uint4*>(out + ((size_t)(ep.row0 + first_row + u) * a.H + h) * HD)[x] = w;
+                    if (__any_sync(0xffffffffu, other))
+#pragma unroll
+                        for (int w = 0; w < 8; ++w)
+                            e4m3x4_to_bf16(w % 4 == 0 ? v[w / 4].x : w % 4 == 1 ? v[w / 4].y : w % 4 == 2 ? v[w / 4].z : v[w / 4].w, scale[w / 4], o[w / 4] + 2 * (w % 4));
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        st_shared16(dst + i * apart, o[i]);
+                        st_shared16((dst + i * apart) ^ 16, o[i] + 4);
+                    }
+                    raw += 2 * STEP * HD;
+                    scales += 2 * STEP;
+                    dst += 2 * apart;
+                    valid -= 2 * STEP;
                 }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar.raw_free(unit.slot));
+                unit.next();
+                return true;
+            };
+            while (ok) {
+                const int is = it & 1;
+                ok = wait_all(bar.item_full(is), (it >> 1) & 1);
+                if (!ok) break;
+                const int n_kv = items[is].n_kv, n_members = items[is].n_members, first = items[is].first, tiles = items[is].tiles, kv = items[is].kv;
+                if (n_kv < 0) break;
+                ++it;
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar.item_empty(is));
+                if (n_kv == 0) continue;
+                auto done = [&](uint32_t b0, uint32_t b1, int n) { return n < 0 || wait_all((n & 1) ? b1 : b0, (n >> 1) & 1); };
+                auto put_k = [&](int j) -> bool {  // once the products of the tile before have read theirs
+                    const int n = kt + j;
+                    if (!done(bar.qk_done(0), bar.qk_done(1), n - 1) || !convert(k_row, STEP / 8 * (HALVES * 1024), kv - tile_col(first, tiles, j))) return false;
+                    fence_async_proxy();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(bar.k_full(n & 1));
+                    return true;
+                };
+                ok = put_k(0);
+                for (int j = 0; j < n_kv && ok; ++j) {
+                    if (j + 1 < n_kv) ok = put_k(j + 1);
+                    if (!ok) break;
+                    if (j == 0 && pending && writes_out) {
+                        ok = finish_item<HD, 4>(a, smem, tmem_base, abort_flag, ei++);
+                        if (!ok) break;
+                    }
+                    const int n = kt + j;
+                    ok = done(bar.pv_done(0), bar.pv_done(1), n - 1);
+                    for (int g = 0; g < n_members && ok; ++g) ok = convert(v_row + g * HALVES * HALF_BYTES, STEP * 128, kv - tile_col(first, tiles, j));
+                    if (!ok) break;
+                    fence_async_proxy();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(bar.v_full(n & 1));
+                }
+                kt += n_kv;
+                pending = true;
+            }
+            if (ok && pending && writes_out) finish_item<HD, 4>(a, smem, tmem_base, abort_flag, ei);
+        }
+    } else if constexpr (FP8) {
+        // ---------------- row scales of the units, four rows a lane (of one page: page sizes are multiples of 8) ----------------
+        fewer_registers<WORKER_REGS>();
+        auto wait_all = [&](uint32_t b, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait(b, parity, abort_flag)); };
+        Unit<HD> unit;
+        bool ok = true;
+        for (int it = 0; ok; ++it) {
+            const int is = it & 1;
+            ok = wait_all(bar.item_full(is), (it >> 1) & 1);
+            if (!ok) break;
+            const int n_kv = items[is].n_kv, n_members = items[is].n_members, first = items[is].first, tiles = items[is].tiles, kv = items[is].kv;
+            const int b = items[is].b, cluster = items[is].cluster;
+            int heads[GM];
+#pragma unroll
+            for (int g = 0; g < GM; ++g) heads[g] = items[is].heads[g];
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar.item_empty(is));
+            if (n_kv < 0) break;
+            if (n_kv == 0) continue;
+            const int32_t* table = a.pool.block_table + (size_t)b * a.pool.max_pages;
+            auto look_up = [&](int j, int& page, int& row) {
+                page = -1;
+                row = 0;
+                if (j >= n_kv) return;
+                const int pos = tile_col(first, tiles, j) + lane * 4;
+                if (pos >= kv) return;
+                const int pi = (int)a.pool.by_page.div((unsigned)pos);
+                row = pos - pi * a.pool.page_size;
+                page = table[pi];
+            };
+            auto load = [&](bool key, int plane, int page, int row) {
+                if ((unsigned)page >= (unsigned)a.pool.n_pages) return make_float4(0.f, 0.f, 0.f, 0.f);
+                return __ldg(reinterpret_cast<const float4*>((key ? a.k_scales : a.v_scales) + ((size_t)page * (key ? a.k : a.H) + plane) * a.pool.page_size + row));
+            };
+            auto put = [&](const float4& v) -> bool {
+                if (!wait_all(bar.raw_free(unit.slot), unit.phase ^ 1)) return false;
+                *reinterpret_cast<float4*>(smem + OFF_SCALES + (unit.slot * BN + lane * 4) * 4) = v;
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar.raw_full(unit.slot));
+                unit.next();
+                return true;
+            };
+            // the scales of tile j's values and of key tile j + 1 are loaded while the ones before wait for their slots
+            int page_v, row_v, page_k, row_k, page_n, row_n;
+            look_up(0, page_v, row_v);
+            look_up(1, page_k, row_k);
+            look_up(2, page_n, row_n);
+            ok = put(load(true, cluster, page_v, row_v));
+            float4 k_next = load(true, cluster, page_k, row_k), v_now[GM];
+#pragma unroll
+            for (int g = 0; g < GM; ++g) v_now[g] = load(false, heads[g], g < n_members ? page_v : -1, row_v);
+            for (int j = 0; j < n_kv && ok; ++j) {
+                page_v = page_k, row_v = row_k;
+                page_k = page_n, row_k = row_n;
+                look_up(j + 3, page_n, row_n);
+                if (j + 1 < n_kv) ok = put(k_next);
+                k_next = load(true, cluster, page_k, row_k);
+#pragma unroll
+                for (int g = 0; g < GM; ++g)
+                    if (g < n_members && ok) {
+                        ok = put(v_now[g]);
+                        v_now[g] = load(false, heads[g], page_v, row_v);
+                    }
             }
         }
     }
@@ -698,19 +987,24 @@ static EncodeTiledFn encode_tiled_fn() {
     return fn;
 }
 
-static bool make_map(CUtensorMap* map, const void* base, int rank, const cuuint64_t* dims, const cuuint64_t* strides, const cuuint32_t* box) {
+static bool make_map(CUtensorMap* map, const void* base, int rank, const cuuint64_t* dims, const cuuint64_t* strides, const cuuint32_t* box, bool bytes = false) {
     const EncodeTiledFn fn = encode_tiled_fn();
     if (fn == nullptr) return false;
     const cuuint32_t estr[5] = {1, 1, 1, 1, 1};
-    return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, rank, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    return fn(map, bytes ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, rank, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              bytes ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 // Keys, D = 128: (64 columns, 8 rows, 2 column halves, row groups of all planes, pages); a box of box_rows whole rows lands as
 // 8-row groups of both halves.  Values: (64 columns, rows of all planes, 2 halves, pages); a box lands as one half behind the
-// other.  D = 64 needs no halves: (64 columns, rows of all planes, pages).
-static bool make_page_map(CUtensorMap* map, const void* base, int D, const PagePool& p, int planes, size_t page_stride, int box_rows, bool keys) {
-    const cuuint64_t rows = (cuuint64_t)planes * p.page_size, pages = (cuuint64_t)p.n_pages, apart = (cuuint64_t)page_stride * 2;
+// other.  D = 64 needs no halves: (64 columns, rows of all planes, pages).  e4m3: (D bytes, rows of all planes, pages), not swizzled.
+static bool make_page_map(CUtensorMap* map, const void* base, int D, const PagePool& p, int planes, size_t page_stride, int box_rows, bool keys, bool fp8) {
+    const cuuint64_t rows = (cuuint64_t)planes * p.page_size, pages = (cuuint64_t)p.n_pages, apart = (cuuint64_t)page_stride * (fp8 ? 1 : 2);
     const cuuint32_t box = (cuuint32_t)box_rows;
+    if (fp8) {
+        const cuuint64_t dims[3] = {(cuuint64_t)D, rows, pages}, strides[2] = {(cuuint64_t)D, apart};
+        const cuuint32_t b[3] = {(cuuint32_t)D, box, 1};
+        return make_map(map, base, 3, dims, strides, b, true);
+    }
     if (D == 64) {
         const cuuint64_t dims[3] = {64, rows, pages}, strides[2] = {128, apart};
         const cuuint32_t b[3] = {64, box, 1};
@@ -755,10 +1049,6 @@ static int prefill_paged(const char* fn, bool fp8, PagedCall a, int n_pages, int
     const char *q_at = static_cast<const char*>(a.q), *o_at = static_cast<const char*>(a.out);
     CHAI_REQUIRE(q_at + ((a.n_tokens - 1) * a.q_stride + dense) * es <= o_at || o_at + a.n_tokens * dense * es <= q_at,
                  CHAI_ERR_INVALID_ARG, "%s: q and out must not overlap", fn);
-    // (the work's line is counted in 32 bits a group and query tile, and 2^36 in all)
-    const long long row_tiles = (long long)a.n_tokens / 16 + 1, keys = a.pool.capacity / 64 + 2;
-    CHAI_REQUIRE(row_tiles * keys < (1ll << 31) && (row_tiles + a.B) * keys * a.H < (1ll << 36), CHAI_ERR_UNSUPPORTED,
-                 "%s: tokens x table too large: n_tokens/16 * max_pages*page_size/64 must be below 2^31, with B more rows and H heads below 2^36", fn);
     const size_t need = chai_prefill_paged_workspace_bytes(a.B, a.H, a.n_tokens);
     CHAI_REQUIRE(workspace_bytes >= need, CHAI_ERR_WORKSPACE, "%s: workspace has %zu bytes, %zu needed", fn, workspace_bytes, need);
 
@@ -771,8 +1061,17 @@ static int prefill_paged(const char* fn, bool fp8, PagedCall a, int n_pages, int
     const int set_up = once.run(dev, [&]() -> int {
         int count = 0;
         cudaError_t e = cudaDeviceGetAttribute(&count, cudaDevAttrMultiProcessorCount, dev);
-        if (e == cudaSuccess) e = cudaFuncSetAttribute(pp::prefill_paged_kernel<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, pp::SMEM_BYTES);
-        if (e == cudaSuccess) e = cudaFuncSetAttribute(pp::prefill_paged_kernel<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, pp::SMEM_BYTES);
+        if (e == cudaSuccess) e = cudaFuncSetAttribute(pp::prefill_paged_kernel<128, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, pp::SMEM_BYTES);
+        if (e == cudaSuccess) e = cudaFuncSetAttribute(pp::prefill_paged_kernel<64, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, pp::SMEM_BYTES);
+        if (e == cudaSuccess) e = cudaFuncSetAttribute(pp::prefill_paged_kernel<128, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, pp::SMEM_BYTES);
+        if (e == cudaSuccess) e = cudaFuncSetAttribute(pp::prefill_paged_kernel<64, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, pp::SMEM_BYTES);
+        // the e4m3 kernels move registers between their warpgroups: no more than they were launched with
+        for (const void* f : {(const void*)pp::prefill_paged_kernel<128, true>, (const void*)pp::prefill_paged_kernel<64, true>}) {
+            cudaFuncAttributes attr = {};
+            if (e == cudaSuccess) e = cudaFuncGetAttributes(&attr, f);
+            CHAI_REQUIRE(e != cudaSuccess || attr.numRegs == pp::LAUNCH_REGS, CHAI_ERR_CUDA,
+                         "prefill_paged_kernel was compiled for %d registers a thread, %d expected", attr.numRegs, pp::LAUNCH_REGS);
+        }
         if (e != cudaSuccess) return cuda_fail(e, "prefill_paged_kernel set-up");
         sms_of_device[dev] = count;
         return CHAI_OK;
@@ -792,11 +1091,15 @@ static int prefill_paged(const char* fn, bool fp8, PagedCall a, int n_pages, int
     a.bk = tensor ? pp::BN : 64;
     a.ctas = sms_of_device[dev] < kPagedMaxCtas ? sms_of_device[dev] : kPagedMaxCtas;
     a.slot_rows = ((a.bq < a.n_tokens ? a.bq : a.n_tokens) + 1) & ~1;  // (even: slots are multiples of 16 bytes)
+    // (the work's line is counted in 32 bits for a group, and shares of all of it are)
+    const long long row_tiles = (long long)a.n_tokens / a.bq + 1, keys = a.pool.capacity / a.bk + 2;
+    CHAI_REQUIRE(row_tiles * keys < (1ll << 27) && (row_tiles + a.B) * keys * a.H < (1ll << 32), CHAI_ERR_UNSUPPORTED,
+                 "%s: tokens x table too large: with query tiles of %d rows and key tiles of %d, (tiles + B) * key tiles * H must be below "
+                 "2^32, and tiles * key tiles below 2^27", fn, a.bq, a.bk);
     CHAI_LOG_CALL("%s: B=%d H=%d k=%d n_tokens=%d D=%d dtype=%d page_size=%d causal=%d, query tiles of %d rows", fn, a.B, a.H, a.k,
                   a.n_tokens, D, dtype, page_size, a.causal, a.bq);
     CHAI_LAUNCH_DEPENDENT("prefill_paged_plan_kernel launch", prefill_paged_plan_kernel, dim3(a.B), dim3(128), prefill_paged_plan_smem(a.H, a.k), s, a);
     if (!tensor) return prefill_paged_simt(a, D, fp8, s);
-    CHAI_REQUIRE(!fp8, CHAI_ERR_UNSUPPORTED, "%s: not yet", fn);
     pp::Tma maps;
     int box_rows = 128;
     while (page_size % box_rows != 0) box_rows >>= 1;
@@ -804,12 +1107,13 @@ static int prefill_paged(const char* fn, bool fp8, PagedCall a, int n_pages, int
     const cuuint64_t q_strides[2] = {(cuuint64_t)D * 2, (cuuint64_t)a.q_stride * 2};
     const cuuint32_t q_box[3] = {64, 1, pp::BM};
     CHAI_REQUIRE(pp::make_map(&maps.q, a.q, 3, q_dims, q_strides, q_box) &&
-                     pp::make_page_map(&maps.k, a.k_pages, D, a.pool, a.k, a.pool.k_page_stride, box_rows, true) &&
-                     pp::make_page_map(&maps.v, a.v_pages, D, a.pool, a.H, a.pool.v_page_stride, box_rows, false),
+                     pp::make_page_map(&maps.k, a.k_pages, D, a.pool, a.k, a.pool.k_page_stride, box_rows, true, fp8) &&
+                     pp::make_page_map(&maps.v, a.v_pages, D, a.pool, a.H, a.pool.v_page_stride, box_rows, false, fp8),
                  CHAI_ERR_CUDA, "%s: cuTensorMapEncodeTiled failed", fn);
     const float scale_log2 = a.scale * 1.4426950408889634f;
-    if (D == 128) CHAI_LAUNCH_DEPENDENT("prefill_paged_kernel launch", pp::prefill_paged_kernel<128>, dim3(a.ctas), dim3(pp::THREADS), pp::SMEM_BYTES, s, maps, a, box_rows, scale_log2);
-    else CHAI_LAUNCH_DEPENDENT("prefill_paged_kernel launch", pp::prefill_paged_kernel<64>, dim3(a.ctas), dim3(pp::THREADS), pp::SMEM_BYTES, s, maps, a, box_rows, scale_log2);
+    auto kernel = D == 128 ? (fp8 ? pp::prefill_paged_kernel<128, true> : pp::prefill_paged_kernel<128, false>)
+                           : (fp8 ? pp::prefill_paged_kernel<64, true> : pp::prefill_paged_kernel<64, false>);
+    CHAI_LAUNCH_DEPENDENT("prefill_paged_kernel launch", kernel, dim3(a.ctas), dim3(fp8 ? pp::Roles<true>::THREADS : pp::Roles<false>::THREADS), pp::SMEM_BYTES, s, maps, a, box_rows, scale_log2);
     return CHAI_OK;
 }
 

@@ -73,7 +73,7 @@ __device__ __forceinline__ void load_tile(const PagedCall& a, bool key, int b, i
 }
 
 template <typename TC, int D, int RPT>
-__global__ void __launch_bounds__(kThreads, 1) prefill_paged_simt_kernel(const PagedCall a) {
+__global__ void __launch_bounds__(kThreads, 1) prefill_paged_simt_kernel(const __grid_constant__ PagedCall a) {
     using S = Smem<D, RPT>;
     constexpr int BQ = S::BQ, STRIDE = S::STRIDE, GM = 256 / D, CPT = D / 16;
     extern __shared__ __align__(16) float smem[];

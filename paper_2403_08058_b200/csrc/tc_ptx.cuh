@@ -107,6 +107,10 @@ __device__ __forceinline__ void tma_prefetch_4d(const CUtensorMap* map, int row,
                  ::"l"(reinterpret_cast<uint64_t>(map)), "r"(0), "r"(row), "r"(0), "r"(plane)
                  : "memory");
 }
+// (no memory clobber: loads of other places may move across it; the fence that follows stays behind it)
+__device__ __forceinline__ void st_shared16(uint32_t at, const uint32_t* w) {
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]));
+}
 // true in exactly one lane of a converged warp
 __device__ __forceinline__ bool elect_one() {
     uint32_t is_leader;
