@@ -12,8 +12,8 @@
 // position; that remainder, rounded to fp32 (at most 2^-26 of a turn), goes to sincospi.  An angle in fp32 would be off by
 // 0.008 at position 131072.
 //
-// Bound by HBM.  A block takes kTokens tokens; their cosines and sines are worked out once, into shared memory; a thread owns one
-// token and one 16-byte vector of its rows, keeps that vector's factors in registers and goes from head to head, so that an
+// Bound by HBM.  A block takes some tokens; their cosines and sines are worked out once, into shared memory; a thread owns one
+// token and 16 (to e4m3: 32) bytes of its rows, keeps the factors of these in registers and goes from head to head, so that an
 // angle costs nothing per head.  The other number of a pair comes from a neighbouring lane (half layout) or is the thread's
 // own.  Few tokens are spread over more blocks by heads.
 #include <math.h>
@@ -23,7 +23,8 @@
 namespace chai {
 namespace {
 
-constexpr int kThreads = 256, kTokens = 8, kUnroll = 4;
+constexpr int kThreads = 256, kUnroll = 4;
+constexpr int kEnterTokens = 4;  // of a block: few, so that most of a token's rows are in flight at once behind its angles (8: 3.2 -> 3.4 us for 16)
 constexpr int kMaxPairs = 64;
 
 struct Rotation {
@@ -123,16 +124,21 @@ struct RopeArgs {
     FastDiv by_n;
 };
 
-// grid (token groups, parts of the heads)
+// grid (token groups, parts of the heads).  The rows of a pass are neighbouring tokens of one head: as much of an array that has
+// tokens behind one another is read in one piece as the block is wide (with 8 tokens, two heads a pass, 8192 x 64 rows
+// took 61 us, now 47: 268 MB at 5.7 TB/s).
 template <typename T, int D>
-__global__ void __launch_bounds__(kThreads) rope_kernel(const RopeArgs a) {
-    constexpr int EPV = 16 / (int)sizeof(T), LPR = D / EPV, ROWS = kThreads / LPR, STEP = ROWS / kTokens;
-    static_assert(ROWS % kTokens == 0, "a thread keeps its token");
-    __shared__ float2 cs[kTokens][kMaxPairs + 1];
-    const int tid = threadIdx.x, x = tid % LPR, local = (tid / LPR) % kTokens, h_off = tid / LPR / kTokens;
-    const long long total = (long long)a.B * a.N, first = (long long)blockIdx.x * kTokens;
+struct RopeShape {
+    static constexpr int EPV = 16 / (int)sizeof(T), LPR = D / EPV, TOKENS = kThreads / LPR;
+};
+template <typename T, int D>
+__global__ void __launch_bounds__(kThreads) rope_kernel(const __grid_constant__ RopeArgs a) {
+    constexpr int EPV = RopeShape<T, D>::EPV, LPR = RopeShape<T, D>::LPR, TOKENS = RopeShape<T, D>::TOKENS;
+    __shared__ float2 cs[TOKENS][D / 2 + 1];
+    const int tid = threadIdx.x, x = tid % LPR, local = tid / LPR;
+    const long long total = (long long)a.B * a.N, first = (long long)blockIdx.x * TOKENS;
     const int pairs = a.rot.rot >> 1;
-    for (int i = tid; i < kTokens * pairs; i += kThreads) {
+    for (int i = tid; i < TOKENS * pairs; i += kThreads) {
         const int t = i / pairs, p = i - t * pairs;
         if (first + t >= total) break;
         const int pos = a.positions != nullptr ? a.positions[first + t] : (int)((first + t) % a.N);
@@ -144,32 +150,28 @@ __global__ void __launch_bounds__(kThreads) rope_kernel(const RopeArgs a) {
     const int b = (int)(token / a.N), n = (int)(token - (long long)b * a.N);
     Factors<EPV> f;
     gather<EPV>(a.rot, cs[live ? local : 0], x, f);
-    const int lane = tid & 31, src_lane = lane - x % 32 + partner_vector<EPV>(a.rot, x);
+    const int lane = tid & 31, src_lane = lane - x + partner_vector<EPV>(a.rot, x);
     const bool rotated = x * EPV < a.rot.rot;
-    const int all = a.x[0].heads + a.x[1].heads;
-    const int h_end = min(all, (int)(blockIdx.y + 1) * a.heads_per_block);
-    for (int h0 = (int)blockIdx.y * a.heads_per_block; h0 < h_end; h0 += STEP * kUnroll) {
-        uint4 raw[kUnroll];
+#pragma unroll 1
+    for (int which = 0; which < 2; ++which) {  // q, then k
+        const Strided& s = a.x[which];
+        const int from = which == 0 ? 0 : a.x[0].heads;
+        const int h0 = max((int)blockIdx.y * a.heads_per_block - from, 0), h1 = min(((int)blockIdx.y + 1) * a.heads_per_block - from, s.heads);
+        const T* in = static_cast<const T*>(s.in) + b * s.b + n * s.n + h0 * s.h + x * EPV;
+        T* out = static_cast<T*>(s.out) + b * s.ob + n * s.on + h0 * s.oh + x * EPV;
+#pragma unroll 1
+        for (int h = h0; h < h1; h += kUnroll, in += kUnroll * s.h, out += kUnroll * s.oh) {
+            uint4 raw[kUnroll];
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u) {
-            const int hh = h0 + u * STEP + h_off;
-            raw[u] = make_uint4(0, 0, 0, 0);
-            if (hh < h_end && live) {
-                const bool key = hh >= a.x[0].heads;
-                const Strided& s = a.x[key ? 1 : 0];
-                // (an ordinary load: input and output may be one array)
-                raw[u] = __ldcs(reinterpret_cast<const uint4*>(static_cast<const T*>(s.in) + b * s.b + (hh - (key ? a.x[0].heads : 0)) * s.h + n * s.n) + x);
+            for (int u = 0; u < kUnroll; ++u) {
+                raw[u] = make_uint4(0, 0, 0, 0);
+                if (h + u < h1 && live) raw[u] = __ldcs(reinterpret_cast<const uint4*>(in + u * s.h));  // (input and output may be one array)
             }
-        }
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u) {
-            const int hh = h0 + u * STEP + h_off;
-            float y[EPV];
-            rotate<T, EPV>(raw[u], a.rot.interleaved != 0, rotated, src_lane, f, y);
-            if (hh < h_end && live) {
-                const bool key = hh >= a.x[0].heads;
-                const Strided& s = a.x[key ? 1 : 0];
-                __stcs(reinterpret_cast<uint4*>(static_cast<T*>(s.out) + b * s.ob + (hh - (key ? a.x[0].heads : 0)) * s.oh + n * s.on) + x, rotated ? pack<T>(y) : raw[u]);
+            for (int u = 0; u < kUnroll; ++u) {
+                float y[EPV];
+                rotate<T, EPV>(raw[u], a.rot.interleaved != 0, rotated, src_lane, f, y);
+                if (h + u < h1 && live) __stcs(reinterpret_cast<uint4*>(out + u * s.oh), rotated ? pack<T>(y) : raw[u]);
             }
         }
     }
@@ -177,15 +179,13 @@ __global__ void __launch_bounds__(kThreads) rope_kernel(const RopeArgs a) {
 
 template <typename T, int D>
 int launch_rope(RopeArgs a, cudaStream_t s) {
-    constexpr int LPR = D * (int)sizeof(T) / 16, STEP = kThreads / LPR / kTokens;
     const int heads = a.x[0].heads + a.x[1].heads;
-    const long long groups = ((long long)a.B * a.N + kTokens - 1) / kTokens;
+    const long long groups = ((long long)a.B * a.N + RopeShape<T, D>::TOKENS - 1) / RopeShape<T, D>::TOKENS;
     // Few tokens: the heads go to several blocks, so that there are four for every SM while each has a load for every slot
-    const long long want = (148 * 4 + groups - 1) / groups, most = (heads + STEP * kUnroll - 1) / (STEP * kUnroll);
+    const long long want = (148 * 4 + groups - 1) / groups, most = (heads + kUnroll - 1) / kUnroll;
     const int parts = (int)(want < most ? want : most);
-    a.heads_per_block = ((heads + parts - 1) / parts + STEP - 1) / STEP * STEP;
-    const int grid_y = (heads + a.heads_per_block - 1) / a.heads_per_block;
-    rope_kernel<T, D><<<dim3((unsigned)groups, grid_y), kThreads, 0, s>>>(a);
+    a.heads_per_block = (heads + parts - 1) / parts;
+    rope_kernel<T, D><<<dim3((unsigned)groups, (heads + a.heads_per_block - 1) / a.heads_per_block), kThreads, 0, s>>>(a);
     CHAI_LAUNCH_CHECK("rope_kernel launch");
     return CHAI_OK;
 }
@@ -215,16 +215,8 @@ struct EnterArgs {
     FastDiv by_page;
     long long n_slots;
     int B, H, k_planes, n_tokens, page_size, rows_per_block;
+    bool wide;  // q, k and v have tokens on 32-byte boundaries
 };
-
-__device__ __forceinline__ unsigned finite_bits(float x) {
-    const unsigned m = __float_as_uint(x) & 0x7fffffffu;
-    return m < 0x7f800000u ? m : 0u;
-}
-// The smallest e >= -126 with amax <= 448 * 2^e: 448 = 1.75 * 2^8, and adding 0x1fffff carries into the exponent exactly
-// when the mantissa is above 1.75.
-__device__ __forceinline__ int scale_exponent(unsigned amax_bits) { return max((int)((amax_bits + 0x1fffffu) >> 23) - 135, -126); }
-__device__ __forceinline__ float pow2(int e) { return __uint_as_float((unsigned)(e + 127) << 23); }
 
 // A rotated row's largest magnitude decides its scale, and lies within fp32's rounding of 1.75 * 2^i about once in 10^6 rows;
 // there the scale could be off by a factor of two for want of a last bit.  Rows that near to the border are decided in
@@ -256,16 +248,44 @@ __device__ __noinline__ bool above_border(const Rotation& r, int pos, int x, uin
     return above;
 }
 
-// grid (token groups, parts of the rows).  Rows of a token: k_planes keys, k_planes queries, H values.
+// Stores what a thread has of a row (raw, or of a rotated one the numbers y) at `row` of plane `pl` of a page; store: whether at
+// all.  The lanes of a row call this together.
 template <typename T, int D, bool FP8>
-__global__ void __launch_bounds__(kThreads) append_rope_kernel(const EnterArgs a) {
-    constexpr int EPV = 16 / (int)sizeof(T), LPR = D / EPV, ROWS = kThreads / LPR, STEP = ROWS / kTokens;
-    __shared__ float2 cs[kTokens][kMaxPairs + 1];
+__device__ __forceinline__ void put_row(const EnterArgs& a, bool key, int pl, unsigned page, int row, int x, bool store, const Dense<FP8>& raw) {
+    constexpr int EPL = Dense<FP8>::BYTES / (int)sizeof(T);
+    const size_t at = (size_t)page * (key ? a.k_page_stride : a.v_page_stride) + ((size_t)pl * a.page_size + row) * D + x * EPL;
+    if (store) *reinterpret_cast<uint4*>(static_cast<T*>(key ? a.k_pages : a.v_pages) + at) = raw.a;
+}
+template <typename T, int D>
+__device__ __forceinline__ void put_row_fp8(const EnterArgs& a, bool key, int pl, unsigned page, int row, int x, bool store, const float* y, int e2) {
+    constexpr int EPL = 32 / (int)sizeof(T);
+    unsigned w[EPL / 4];
+    quantize<EPL>(y, pow2(-e2), w);
+    if (!store) return;
+    const size_t in_page = (size_t)pl * a.page_size + row;
+    unsigned char* dst = static_cast<unsigned char*>(key ? a.k_pages : a.v_pages) + (size_t)page * (key ? a.k_page_stride : a.v_page_stride) + in_page * D + x * EPL;
+    if constexpr (EPL == 16) *reinterpret_cast<uint4*>(dst) = make_uint4(w[0], w[1], w[2], w[3]);
+    else *reinterpret_cast<uint2*>(dst) = make_uint2(w[0], w[1]);
+    if (x == 0) (key ? a.k_scales : a.v_scales)[(size_t)page * (key ? a.k_planes : a.H) * a.page_size + in_page] = pow2(e2);
+}
+
+// grid (token groups, parts of the rows).  Rows of a token: k_planes keys, k_planes queries, then H values, which are not rotated and
+// go through a loop of their own.  Blocks to an SM: what the registers of a rotated e4m3 row (its border check among them) allow is
+// two; rows stored as they are gain from a third (bf16, 8172 tokens of 32 heads, 128 wide: 57 -> 50 us), and a fourth, 47 us there,
+// spills what 800 tokens wait for (6.8 -> 7.6 us).
+// To e4m3 the 8172 tokens take 58 us, 178 MB at 3.1 TB/s: bound by the instructions of the rotation, the row's largest magnitude
+// and the conversion, 16 warps to an SM.
+template <typename T, int D, bool FP8>
+__global__ void __launch_bounds__(kThreads, FP8 ? 2 : 3) append_rope_kernel(const __grid_constant__ EnterArgs a) {
+    constexpr int BYTES = Dense<FP8>::BYTES, VPL = BYTES / 16, EPV = 16 / (int)sizeof(T), EPL = EPV * VPL, LPR = D / EPL;
+    constexpr int ROWS = kThreads / LPR, STEP = ROWS / kEnterTokens, UNROLL = kUnroll / VPL;
+    static_assert(ROWS % kEnterTokens == 0, "a thread keeps its token");
+    __shared__ float2 cs[kEnterTokens][kMaxPairs + 1];
     dependent_grid_sync();
-    const int tid = threadIdx.x, x = tid % LPR, local = (tid / LPR) % kTokens, r_off = tid / LPR / kTokens;
-    const int first = (int)blockIdx.x * kTokens, token = first + local;
-    const int r_begin = (int)blockIdx.y * a.rows_per_block, rows = 2 * a.k_planes + a.H;
-    const int r_end = min(rows, r_begin + a.rows_per_block);
+    const int tid = threadIdx.x, x = tid % LPR, local = (tid / LPR) % kEnterTokens, r_off = tid / LPR / kEnterTokens;
+    const int first = (int)blockIdx.x * kEnterTokens, token = first + local;
+    const int turned = 2 * a.k_planes, r_begin = (int)blockIdx.y * a.rows_per_block;
+    const int r_end = min(turned + a.H, r_begin + a.rows_per_block);
     const int pairs = a.rot.rot >> 1;
     // where the token goes
     long long slot = -1;
@@ -278,98 +298,131 @@ __global__ void __launch_bounds__(kThreads) append_rope_kernel(const EnterArgs a
         if (slot >= 0 && (slot >= a.n_slots || b < 0 || b >= a.B)) bad = true, slot = -1;
     }
     const bool live = slot >= 0;
-    if (r_begin < 2 * a.k_planes) {  // (block-uniform)
-        for (int i = tid; i < kTokens * pairs; i += kThreads) {
+    const unsigned page = slot < 0x7fffffffll ? a.by_page.div((unsigned)max(slot, 0ll)) : (unsigned)(slot / a.page_size);
+    const int row = live ? (int)(slot - (long long)page * a.page_size) : 0;
+    if (r_begin < turned) {  // (block-uniform)
+        const int32_t* reps = a.reps + (size_t)b * a.k_planes;
+        const int t_end = min(r_end, turned);
+        Dense<FP8> raw[UNROLL];
+        int head[UNROLL];  // -1: nothing to do
+        auto load = [&](int r0) {
+#pragma unroll
+            for (int u = 0; u < UNROLL; ++u) {
+                const int r = r0 + u * STEP + r_off;
+                head[u] = r < t_end && live ? reps[r < a.k_planes ? r : r - a.k_planes] : -1;
+            }
+#pragma unroll
+            for (int u = 0; u < UNROLL; ++u) {
+                const bool key = r0 + u * STEP + r_off < a.k_planes;
+                raw[u].zero();
+                if (head[u] < 0 || head[u] >= a.H) head[u] = -1;  // (-1: unused cluster slot)
+                else raw[u].load(static_cast<const T*>(key ? a.k : a.q) + token * (key ? a.k_stride : a.q_stride) + (long long)head[u] * D + x * EPL, a.wide);
+            }
+        };
+        load(r_begin);  // (on its way while the angles are worked out)
+        for (int i = tid; i < kEnterTokens * pairs; i += kThreads) {
             const int t = i / pairs, p = i - t * pairs;
             if (first + t < a.n_tokens) cs[t][p] = factors(a.rot, a.positions[first + t], p);
         }
         __syncthreads();
-    }
-    const unsigned page = slot < 0x7fffffffll ? a.by_page.div((unsigned)max(slot, 0ll)) : (unsigned)(slot / a.page_size);
-    const int row = live ? (int)(slot - (long long)page * a.page_size) : 0;
-    Factors<EPV> f = {};
-    if (r_begin < 2 * a.k_planes) gather<EPV>(a.rot, cs[token < a.n_tokens ? local : 0], x, f);
-    const int lane = tid & 31, src_lane = lane - x % 32 + partner_vector<EPV>(a.rot, x);
-    const bool in_rot = x * EPV < a.rot.rot;
-    const int32_t* reps = a.reps + (size_t)b * a.k_planes;
-#pragma unroll 1
-    for (int r0 = r_begin; r0 < r_end; r0 += STEP * kUnroll) {
-        uint4 raw[kUnroll];
-        int head[kUnroll];  // -1: nothing to do
+        Factors<EPL> f;
+        gather<EPL>(a.rot, cs[token < a.n_tokens ? local : 0], x, f);
+        // (half layout) the lane that holds the partners of each of the thread's vectors, and which of that lane's they are
+        const int lane = tid & 31, half_vectors = a.rot.rot / (2 * EPV), odd = VPL == 2 ? half_vectors & 1 : 0;
+        int src_lane[VPL];
+        bool in_rot[VPL];
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u) {
-            const int r = r0 + u * STEP + r_off;
-            raw[u] = make_uint4(0, 0, 0, 0);
-            head[u] = -1;
-            if (r >= r_end || !live) continue;
-            const int kind = r < a.k_planes ? 0 : r < 2 * a.k_planes ? 1 : 2;
-            head[u] = r - 2 * a.k_planes;
-            if (kind < 2) {
-                head[u] = reps[kind == 0 ? r : r - a.k_planes];
-                if (head[u] < 0 || head[u] >= a.H) {  // unused cluster slot
-                    head[u] = -1;
-                    continue;
+        for (int i = 0; i < VPL; ++i) {
+            src_lane[i] = lane - x + partner_vector<EPV>(a.rot, x * VPL + i) / VPL;
+            in_rot[i] = (x * VPL + i) * EPV < a.rot.rot;
+        }
+#pragma unroll 1
+        for (int r0 = r_begin; r0 < t_end; r0 += STEP * UNROLL) {
+            if (r0 != r_begin) load(r0);
+#pragma unroll
+            for (int u = 0; u < UNROLL; ++u) {
+                const int r = r0 + u * STEP + r_off;
+                const bool key = r < a.k_planes, there = head[u] >= 0;
+                float y[EPL];
+                uint4 mine[VPL], other[VPL];
+                mine[0] = raw[u].a;
+                if constexpr (VPL == 2) mine[1] = raw[u].b;
+#pragma unroll
+                for (int i = 0; i < VPL; ++i) {
+                    const uint4 give = VPL == 2 && odd != 0 ? mine[(i ^ 1) % VPL] : mine[i];
+                    other[i] = give;
+                    if (!a.rot.interleaved) {
+                        other[i].x = __shfl_sync(0xffffffffu, give.x, src_lane[i]);
+                        other[i].y = __shfl_sync(0xffffffffu, give.y, src_lane[i]);
+                        other[i].z = __shfl_sync(0xffffffffu, give.z, src_lane[i]);
+                        other[i].w = __shfl_sync(0xffffffffu, give.w, src_lane[i]);
+                    }
+                    float m[EPV], o[EPV];
+                    Vec16<T>::unpack(mine[i], m);
+                    Vec16<T>::unpack(other[i], o);
+#pragma unroll
+                    for (int e = 0; e < EPV; ++e) {
+                        const float partner = a.rot.interleaved ? m[e ^ 1] : o[e];
+                        y[i * EPV + e] = in_rot[i] ? fmaf(m[e], f.own[i * EPV + e], partner * f.other[i * EPV + e]) : m[e];
+                    }
+                }
+                if (there && !key) {
+                    uint4* to = reinterpret_cast<uint4*>(static_cast<T*>(a.q_out) + ((long long)token * a.H + head[u]) * D + x * EPL);
+#pragma unroll
+                    for (int i = 0; i < VPL; ++i) to[i] = in_rot[i] ? pack<T>(y + i * EPV) : mine[i];
+                }
+                if constexpr (!FP8) {
+                    Dense<FP8> out;
+                    out.a = in_rot[0] ? pack<T>(y) : mine[0];
+                    put_row<T, D, FP8>(a, true, r, page, row, x, there && key, out);
+                } else {
+                    if (!__any_sync(0xffffffffu, there && key)) continue;
+                    unsigned m = 0;
+#pragma unroll
+                    for (int e = 0; e < EPL; ++e) m = max(m, finite_magnitude(y[e]));
+#pragma unroll
+                    for (int o = LPR / 2; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
+                    int e2 = m == 0 ? 0 : scale_exponent(m);
+                    const bool close = key && there && a.rot.rot > 0 && near_border(m) && m >= 0x08000000u;
+                    if (__any_sync(0xffffffffu, close)) {
+                        const unsigned border = (m & 0x7f800000u) | kBorder;
+                        unsigned above = 0;
+#pragma unroll
+                        for (int i = 0; i < VPL; ++i)
+                            if (close && above_border<T, EPV>(a.rot, pos, x * VPL + i, mine[i], other[i], (double)__uint_as_float(border))) above = 1;
+#pragma unroll
+                        for (int s = LPR / 2; s > 0; s >>= 1) above |= __shfl_xor_sync(0xffffffffu, above, s);
+                        if (close) e2 = scale_exponent(border) + (int)above;
+                    }
+                    put_row_fp8<T, D>(a, true, r, page, row, x, there && key, y, e2);
                 }
             }
-            const T* src = static_cast<const T*>(kind == 0 ? a.k : kind == 1 ? a.q : a.v);
-            const long long stride = kind == 0 ? a.k_stride : kind == 1 ? a.q_stride : a.v_stride;
-            raw[u] = __ldcs(reinterpret_cast<const uint4*>(src + token * stride + (long long)head[u] * D) + x);
+        }
+    }
+    const T* v = static_cast<const T*>(a.v) + (live ? token * a.v_stride : 0) + x * EPL;
+    const int h_end = r_end - turned;
+#pragma unroll 1
+    for (int h0 = max(r_begin - turned, 0); h0 < h_end; h0 += STEP * UNROLL) {
+        Dense<FP8> raw[UNROLL];
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u) {
+            const int h = h0 + u * STEP + r_off;
+            raw[u].zero();
+            if (h < h_end && live) raw[u].load(v + (long long)h * D, a.wide);
         }
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u) {
-            const int r = r0 + u * STEP + r_off;
-            // (the rows of a warp are the same row of neighbouring tokens, or of neighbouring rows: `turn` may differ in a warp)
-            const bool turn = r < 2 * a.k_planes, key = r < a.k_planes;
-            float y[EPV];
-            uint4 out = raw[u];
-            if (__any_sync(0xffffffffu, turn)) {
-                rotate<T, EPV>(raw[u], a.rot.interleaved != 0, in_rot && turn, src_lane, f, y);
-                if (turn && in_rot) out = pack<T>(y);
-            } else {
-                Vec16<T>::unpack(raw[u], y);
-            }
-            const bool query = turn && !key;
-            if (query && head[u] >= 0)
-                reinterpret_cast<uint4*>(static_cast<T*>(a.q_out) + ((long long)token * a.H + head[u]) * D)[x] = out;
-            const int pl = key ? r : r - 2 * a.k_planes;
-            const bool store = head[u] >= 0 && !query;
-            const size_t at = store ? (size_t)page * (key ? a.k_page_stride : a.v_page_stride) + ((size_t)pl * a.page_size + row) * D + x * EPV : 0;
+        for (int u = 0; u < UNROLL; ++u) {
+            const int h = h0 + u * STEP + r_off;
+            const bool store = h < h_end && live;
             if constexpr (!FP8) {
-                if (store) *reinterpret_cast<uint4*>(static_cast<T*>(key ? a.k_pages : a.v_pages) + at) = out;
+                put_row<T, D, FP8>(a, false, h, page, row, x, store, raw[u]);
             } else {
-                unsigned m = 0;
-#pragma unroll
-                for (int e = 0; e < EPV; ++e) m = max(m, finite_bits(y[e]));
-#pragma unroll
-                for (int o = LPR / 2; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
-                int e2 = m == 0 ? 0 : scale_exponent(m);
-                const bool close = key && store && a.rot.rot > 0 && near_border(m) && m >= 0x08000000u;
-                if (__any_sync(0xffffffffu, close)) {
-                    uint4 o;
-                    o.x = __shfl_sync(0xffffffffu, raw[u].x, src_lane);
-                    o.y = __shfl_sync(0xffffffffu, raw[u].y, src_lane);
-                    o.z = __shfl_sync(0xffffffffu, raw[u].z, src_lane);
-                    o.w = __shfl_sync(0xffffffffu, raw[u].w, src_lane);
-                    const unsigned border = (m & 0x7f800000u) | kBorder;
-                    unsigned above = close && above_border<T, EPV>(a.rot, pos, x, raw[u], o, (double)__uint_as_float(border)) ? 1u : 0u;
-#pragma unroll
-                    for (int s = LPR / 2; s > 0; s >>= 1) above |= __shfl_xor_sync(0xffffffffu, above, s);
-                    if (close) e2 = scale_exponent(border) + (int)above;
-                }
-                const float inv = pow2(-e2);
-                unsigned w[EPV / 4];
-#pragma unroll
-                for (int i = 0; i < EPV / 4; ++i) {
-                    const unsigned lo = __nv_cvt_float2_to_fp8x2(make_float2(y[4 * i] * inv, y[4 * i + 1] * inv), __NV_SATFINITE, __NV_E4M3);
-                    const unsigned hi = __nv_cvt_float2_to_fp8x2(make_float2(y[4 * i + 2] * inv, y[4 * i + 3] * inv), __NV_SATFINITE, __NV_E4M3);
-                    w[i] = lo | (hi << 16);
-                }
-                if (store) {
-                    unsigned char* dst = static_cast<unsigned char*>(key ? a.k_pages : a.v_pages) + at;
-                    if constexpr (EPV == 8) *reinterpret_cast<uint2*>(dst) = make_uint2(w[0], w[1]);
-                    else *reinterpret_cast<unsigned*>(dst) = w[0];
-                    if (x == 0) (key ? a.k_scales : a.v_scales)[((size_t)page * (key ? a.k_planes : a.H) + pl) * a.page_size + row] = pow2(e2);
-                }
+                float y[EPL];
+                Vec16<T>::unpack(raw[u].a, y);
+                Vec16<T>::unpack(raw[u].b, y + EPV);
+                const unsigned bits[8] = {raw[u].a.x, raw[u].a.y, raw[u].a.z, raw[u].a.w, raw[u].b.x, raw[u].b.y, raw[u].b.z, raw[u].b.w};
+                const unsigned m = row_max<T, LPR>(bits, y);
+                put_row_fp8<T, D>(a, false, h, page, row, x, store, y, m == 0 ? 0 : scale_exponent(m));
             }
         }
     }
@@ -383,10 +436,10 @@ __global__ void enter_reset_status_kernel(WsHeader* hdr) {
 
 template <typename T, int D, bool FP8>
 int launch_enter(EnterArgs a, cudaStream_t s) {
-    constexpr int LPR = D * (int)sizeof(T) / 16, STEP = kThreads / LPR / kTokens;
+    constexpr int LPR = D * (int)sizeof(T) / Dense<FP8>::BYTES, STEP = kThreads / LPR / kEnterTokens, UNROLL = kUnroll * 16 / Dense<FP8>::BYTES;
     const int rows = 2 * a.k_planes + a.H;
-    const long long groups = ((long long)a.n_tokens + kTokens - 1) / kTokens;
-    const long long want = (148 * 4 + groups - 1) / groups, most = (rows + STEP * kUnroll - 1) / (STEP * kUnroll);
+    const long long groups = ((long long)a.n_tokens + kEnterTokens - 1) / kEnterTokens;
+    const long long want = (148 * 4 + groups - 1) / groups, most = (rows + STEP * UNROLL - 1) / (STEP * UNROLL);
     const int parts = (int)(want < most ? want : most);
     a.rows_per_block = ((rows + parts - 1) / parts + STEP - 1) / STEP * STEP;
     CHAI_LAUNCH_DEPENDENT("append_rope_kernel launch", (append_rope_kernel<T, D, FP8>),
@@ -425,6 +478,7 @@ int enter(const char* fn, bool fp8, EnterArgs a, int n_pages, int D, size_t k_pa
     a.v_page_stride = pool.v_page_stride;
     a.by_page = pool.by_page;
     a.n_slots = (long long)n_pages * a.page_size;
+    a.wide = aligned32(a.q) && aligned32(a.k) && aligned32(a.v) && a.q_stride * es % 32 == 0 && a.k_stride * es % 32 == 0 && a.v_stride * es % 32 == 0;
     CHAI_LOG_CALL("%s: n_tokens=%d B=%d H=%d k=%d D=%d rot=%d dtype=%d page_size=%d", fn, a.n_tokens, a.B, a.H, a.k_planes, D,
                   a.rot.rot, dtype, a.page_size);
     if (a.hdr != nullptr)
@@ -484,7 +538,7 @@ int chai_rope(const void* q, const void* k, void* q_out, void* k_out, const int3
     CHAI_REQUIRE(B > 0 && Hq > 0 && Hk >= 0 && N > 0, CHAI_ERR_INVALID_ARG, "%s: need B, Hq, N > 0 and Hk >= 0", fn);
     CHAI_REQUIRE(dtype == CHAI_F32 || dtype == CHAI_BF16, CHAI_ERR_UNSUPPORTED, "%s: unknown dtype %d", fn, dtype);
     CHAI_REQUIRE(D == 64 || D == 128, CHAI_ERR_UNSUPPORTED, "%s: head_dim %d (64 or 128 supported)", fn, D);
-    CHAI_REQUIRE(Hq <= 65535 && Hk <= 65535 && (long long)B * N < (1ll << 31) * kTokens, CHAI_ERR_UNSUPPORTED,
+    CHAI_REQUIRE(Hq <= 65535 && Hk <= 65535 && (long long)B * N < (1ll << 34), CHAI_ERR_UNSUPPORTED,
                  "%s: heads must be <= 65535 and B * N below 2^34", fn);
     RopeArgs a = {};
     a.positions = positions;
