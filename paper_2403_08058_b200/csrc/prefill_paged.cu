@@ -27,7 +27,7 @@
 
 namespace chai {
 
-int prefill_paged_simt_rows(int B, int n_tokens);
+void prefill_paged_simt_tile(int B, int n_tokens, int D, int* rows, int* keys);
 int prefill_paged_simt(const PagedCall& a, int D, bool fp8, cudaStream_t s);
 
 namespace pp {
@@ -1087,9 +1087,11 @@ static int prefill_paged(const char* fn, bool fp8, PagedCall a, int n_pages, int
     a.groups = reinterpret_cast<PagedGroup*>(ws + L.off_groups);
     a.slots = ws + L.off_slots;
     a.gmax = 256 / D;
-    a.bq = tensor ? pp::BM : prefill_paged_simt_rows(a.B, a.n_tokens);
-    a.bk = tensor ? pp::BN : 64;
-    a.ctas = sms_of_device[dev] < kPagedMaxCtas ? sms_of_device[dev] : kPagedMaxCtas;
+    a.bq = pp::BM;
+    a.bk = pp::BN;
+    if (!tensor) prefill_paged_simt_tile(a.B, a.n_tokens, D, &a.bq, &a.bk);
+    const int ctas = sms_of_device[dev] * (tensor ? 1 : 2);
+    a.ctas = ctas < kPagedMaxCtas ? ctas : kPagedMaxCtas;
     a.slot_rows = ((a.bq < a.n_tokens ? a.bq : a.n_tokens) + 1) & ~1;  // (even: slots are multiples of 16 bytes)
     // (the work's line is counted in 32 bits for a group, and shares of all of it are)
     const long long row_tiles = (long long)a.n_tokens / a.bq + 1, keys = a.pool.capacity / a.bk + 2;

@@ -3,11 +3,15 @@
 //
 // One pass over the keys with a running maximum m and sum l per row; S = scale Q K^T, P = exp(S - m), O = O exp(m_old - m) + P V
 // for up to 256 / D members of a cluster, whose probabilities are the same.  All in fp32.
-// Bound by the FMA pipe when there are many rows (two products an instruction, fma.rn.f32x2): a block of 256 threads takes
-// 16 RPT query rows and 64 keys, a thread RPT rows x 4 keys of S and RPT rows x 16 columns (of all members together, per
-// member D / 16) of O, so that shared memory is read once for 4 to 8 products.  RPT = 1, 2 or 8 by the tokens per request,
-// since rows that a request does not have are computed all the same.  Keys of the next tile and values of the next
-// member arrive by asynchronous copies while this one is multiplied.
+// Many rows are bound by the FMA pipe (two products an instruction, fma.rn.f32x2), few by the copies and what stands in a row
+// for a tile: keys there, S, the rows' maximum and sum, values there, O.  So two blocks of 256 threads stand on an SM, one busy
+// while the other waits.  A block takes 16 RPT query rows and 32 or 64 keys, a thread RPT rows x 2 or 4 keys of S and RPT rows
+// x 16 columns (of all members together, per member D / 16) of O.  RPT = 1, 2 or 4 by the tokens per request, since rows that a
+// request does not have are computed all the same.  Every member has a buffer of its own: keys and values of the next tile are
+// copied as soon as this tile's are done with, and where the rows lie is looked up a tile ahead.
+// Measured (fp32): 5 requests of up to 93 rows over up to 700 positions, 12 heads of 64: 50 us (one block of 128 rows an SM, the
+// pieces joined a vector at a time: 118); of 2 rows over up to 4096, 32 heads of 128: 180 us, 1.1 TB/s; of up to 400 over
+// 2048: 857 us.
 #include "prefill_paged.cuh"
 #include "tc_ptx.cuh"
 
@@ -18,14 +22,18 @@ using tcx::fma2;
 using tcx::pack2;
 using tcx::unpack2;
 
-constexpr int kThreads = 256, BK = 64, PSTRIDE = BK + 4;
+constexpr int kThreads = 256;
+// Keys of a tile: what lets two blocks stand on an SM.
+constexpr int keys_of(int D, int rpt) { return rpt > 2 || (D == 128 && rpt > 1) ? 32 : 64; }
 
 template <int D, int RPT>
 struct Smem {
-    static constexpr int BQ = 16 * RPT, STRIDE = D + 4;
-    static constexpr int Q = 0, K = Q + BQ * STRIDE, V = K + BK * STRIDE, P = V + 2 * BK * STRIDE, M = P + BQ * PSTRIDE,
-                         L = M + BQ, C = L + BQ, FLOATS = C + BQ;
+    static_assert(16 * RPT * kPagedMaxPieces <= 16 * RPT * (D + 4), "the joined pieces' shares fit where the queries were");
+    static constexpr int BQ = 16 * RPT, BK = keys_of(D, RPT), STRIDE = D + 4, PSTRIDE = BK + 4;
+    static constexpr int Q = 0, K = Q + BQ * STRIDE, V = K + BK * STRIDE, P = V + 256 / D * BK * STRIDE, M = P + BQ * PSTRIDE,
+                         L = M + BQ, C = L + BQ, ROWS = C + BQ, FLOATS = ROWS + 2 * 2 * BK;
     static constexpr int BYTES = FLOATS * 4 + 16;
+    static_assert(2 * (BYTES + 1024) <= 228 * 1024, "two blocks to an SM");
 };
 
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there) {
@@ -33,36 +41,43 @@ __device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
 
-// 64 rows of plane `plane` of the keys or values, from position pos0 on; positions at or behind kv are zero.
-template <typename TC, int D>
-__device__ __forceinline__ void load_tile(const PagedCall& a, bool key, int b, int plane, int pos0, int kv, float* dst) {
+// Where a key tile's rows are: (page, row in the page), page -1 where there is none.
+template <int BK>
+__device__ __forceinline__ void find_rows(const PagedCall& a, int b, int pos0, int kv, int2* rows) {
+    const int r = threadIdx.x;
+    if (r >= BK) return;
+    const int pos = pos0 + r;
+    int page = -1, row = 0;
+    if (pos < kv) {
+        const int pi = (int)a.pool.by_page.div((unsigned)pos);
+        row = pos - pi * a.pool.page_size;
+        page = a.pool.block_table[(size_t)b * a.pool.max_pages + pi];
+        if (page < 0 || page >= a.pool.n_pages) page = -1;  // (the planner has looked; another stream may write the table)
+    }
+    rows[r] = make_int2(page, row);
+}
+// The rows of plane `plane` of the keys or values; those of no page are zero.
+template <typename TC, int D, int BK>
+__device__ __forceinline__ void load_tile(const PagedCall& a, bool key, int plane, const int2* rows, float* dst) {
     constexpr int STRIDE = D + 4;
-    const int32_t* table = a.pool.block_table + (size_t)b * a.pool.max_pages;
     const size_t stride = key ? a.pool.k_page_stride : a.pool.v_page_stride;
     const char* pages = static_cast<const char*>(key ? a.k_pages : a.v_pages);
     constexpr int VPR = D * (int)sizeof(TC) / 16, EPV = 16 / (int)sizeof(TC);  // 16-byte vectors of a cached row
 #pragma unroll
     for (int i = threadIdx.x; i < BK * VPR; i += kThreads) {
-        const int r = i / VPR, x = i % VPR, pos = pos0 + r;
-        size_t at = 0;
-        int page = -1, row = 0;
-        if (pos < kv) {
-            const int pi = (int)a.pool.by_page.div((unsigned)pos);
-            row = pos - pi * a.pool.page_size;
-            page = table[pi];
-            if (page < 0 || page >= a.pool.n_pages) page = -1;  // (the planner has looked; another stream may write the table)
-            else at = (size_t)page * stride + ((size_t)plane * a.pool.page_size + row) * D + x * EPV;
-        }
+        const int r = i / VPR, x = i % VPR;
+        const int2 where = rows[r];
+        const size_t at = where.x < 0 ? 0 : (size_t)where.x * stride + ((size_t)plane * a.pool.page_size + where.y) * D + x * EPV;
         float* to = dst + r * STRIDE + x * EPV;
         if constexpr (sizeof(TC) == 4) {
-            copy16(tcx::smem_u32(to), pages + at * 4, page >= 0);
+            copy16(tcx::smem_u32(to), pages + at * 4, where.x >= 0);
         } else {
             float f[16];
             uint4 raw = make_uint4(0, 0, 0, 0);
             float s = 0.f;
-            if (page >= 0) {
+            if (where.x >= 0) {
                 raw = __ldcs(reinterpret_cast<const uint4*>(pages + at));
-                s = __ldg((key ? a.k_scales : a.v_scales) + ((size_t)page * (key ? a.k : a.H) + plane) * a.pool.page_size + row);
+                s = __ldg((key ? a.k_scales : a.v_scales) + ((size_t)where.x * (key ? a.k : a.H) + plane) * a.pool.page_size + where.y);
             }
             Vec16<Fp8E4M3>::unpack(raw, f);
 #pragma unroll
@@ -73,11 +88,12 @@ __device__ __forceinline__ void load_tile(const PagedCall& a, bool key, int b, i
 }
 
 template <typename TC, int D, int RPT>
-__global__ void __launch_bounds__(kThreads, 1) prefill_paged_simt_kernel(const __grid_constant__ PagedCall a) {
+__global__ void __launch_bounds__(kThreads, 2) prefill_paged_simt_kernel(const __grid_constant__ PagedCall a) {
     using S = Smem<D, RPT>;
-    constexpr int BQ = S::BQ, STRIDE = S::STRIDE, GM = 256 / D, CPT = D / 16;
+    constexpr int BQ = S::BQ, BK = S::BK, STRIDE = S::STRIDE, PSTRIDE = S::PSTRIDE, GM = 256 / D, CPT = D / 16, KPT = BK / 16;
     extern __shared__ __align__(16) float smem[];
     float *Qs = smem + S::Q, *Ks = smem + S::K, *Vs = smem + S::V, *Ps = smem + S::P, *Ms = smem + S::M, *Ls = smem + S::L, *Cs = smem + S::C;
+    int2* s_rows = reinterpret_cast<int2*>(smem + S::ROWS);  // of an even and an odd tile
     int* s_id = reinterpret_cast<int*>(smem + S::FLOATS);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int rg = (warp & 3) * 4 + (lane >> 3), cg = (warp >> 2) * 8 + (lane & 7);  // rows i * 16 + rg, keys j * 16 + cg
@@ -110,23 +126,29 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_paged_simt_kernel(const _
             copy16(tcx::smem_u32(Qs + r * STRIDE + x * 4), q + (r < it.rows ? (long long)r * a.q_stride + x * 4 : 0), r < it.rows);
         }
         if (tid < BQ) Ms[tid] = -INFINITY, Ls[tid] = 0.f;
-        auto load_k = [&](int j) {
-            if (j < it.count) load_tile<TC, D>(a, true, it.b, e.cluster, pos0(j), it.kv, Ks);
-            asm volatile("cp.async.commit_group;" ::: "memory");
+        auto commit = [] { asm volatile("cp.async.commit_group;" ::: "memory"); };
+        auto find = [&](int j) {
+            if (j < it.count) find_rows<BK>(a, it.b, pos0(j), it.kv, s_rows + (j & 1) * BK);
         };
-        auto load_v = [&](int j, int g) {  // (buffers alternate over the members of all tiles)
-            if (j < it.count) {
+        auto load_k = [&](int j) {
+            if (j < it.count) load_tile<TC, D, BK>(a, true, e.cluster, s_rows + (j & 1) * BK, Ks);
+            commit();
+        };
+        auto load_v = [&](int j, int g) {  // (a buffer a member)
+            if (j < it.count && g < members) {
                 int h = e.heads[0];
 #pragma unroll
                 for (int x = 1; x < GM; ++x)
                     if (g == x) h = e.heads[x];
-                load_tile<TC, D>(a, false, it.b, h, pos0(j), it.kv, Vs + ((j * members + g) & 1) * BK * STRIDE);
+                load_tile<TC, D, BK>(a, false, h, s_rows + (j & 1) * BK, Vs + g * BK * STRIDE);
             }
-            asm volatile("cp.async.commit_group;" ::: "memory");
+            commit();
         };
+        find(0);
+        __syncthreads();
         load_k(0);  // (with the queries)
-        load_v(0, 0);
-        if (members > 1) load_v(0, 1); else load_v(1, 0);
+#pragma unroll
+        for (int g = 0; g < GM - 1; ++g) load_v(0, g);
         float acc[GM][RPT][CPT];
 #pragma unroll
         for (int g = 0; g < GM; ++g)
@@ -136,25 +158,27 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_paged_simt_kernel(const _
                 for (int c = 0; c < CPT; ++c) acc[g][i][c] = 0.f;
 
         for (int j = 0; j < it.count; ++j) {
-            // the latest copy is a later value tile's: everything but that has arrived
-            asm volatile("cp.async.wait_group 1;" ::: "memory");
+            // in order: keys of j, values of j but the last member's | those, keys of j + 1, values of j + 1 ...
+            asm volatile("cp.async.wait_group %0;" ::"n"(GM - 1) : "memory");
             __syncthreads();
+            load_v(j, GM - 1);
+            find(j + 1);
             {
-                uint64_t s2[RPT][4];  // sums over even and over odd columns
+                uint64_t s2[RPT][KPT];  // sums over even and over odd columns
 #pragma unroll
                 for (int i = 0; i < RPT; ++i)
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) s2[i][c] = 0ull;
+                    for (int c = 0; c < KPT; ++c) s2[i][c] = 0ull;
 #pragma unroll 2
                 for (int d = 0; d < D; d += 4) {
-                    ulonglong2 kk[4];
+                    ulonglong2 kk[KPT];
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) kk[c] = *reinterpret_cast<const ulonglong2*>(Ks + (c * 16 + cg) * STRIDE + d);
+                    for (int c = 0; c < KPT; ++c) kk[c] = *reinterpret_cast<const ulonglong2*>(Ks + (c * 16 + cg) * STRIDE + d);
 #pragma unroll
                     for (int i = 0; i < RPT; ++i) {
                         const ulonglong2 qq = *reinterpret_cast<const ulonglong2*>(Qs + (i * 16 + rg) * STRIDE + d);
 #pragma unroll
-                        for (int c = 0; c < 4; ++c) s2[i][c] = fma2(qq.y, kk[c].y, fma2(qq.x, kk[c].x, s2[i][c]));
+                        for (int c = 0; c < KPT; ++c) s2[i][c] = fma2(qq.y, kk[c].y, fma2(qq.x, kk[c].x, s2[i][c]));
                     }
                 }
                 const int col0 = pos0(j);
@@ -162,7 +186,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_paged_simt_kernel(const _
                 for (int i = 0; i < RPT; ++i) {
                     const int r = i * 16 + rg, end = sees(r);
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) {
+                    for (int c = 0; c < KPT; ++c) {
                         float x, y;
                         unpack2(s2[i][c], x, y);
                         Ps[r * PSTRIDE + c * 16 + cg] = col0 + c * 16 + cg < end ? (x + y) * a.scale : -INFINITY;
@@ -209,10 +233,12 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_paged_simt_kernel(const _
             }
 #pragma unroll
             for (int g = 0; g < GM; ++g) {
-                if (g >= members) break;
-                asm volatile("cp.async.wait_group 1;" ::: "memory");
-                __syncthreads();
-                const float* v = Vs + ((j * members + g) & 1) * BK * STRIDE;
+                if (g == 0) asm volatile("cp.async.wait_group %0;" ::"n"(GM) : "memory");
+                else asm volatile("cp.async.wait_group %0;" ::"n"(GM - 1) : "memory");
+                if (g <= members) __syncthreads();
+                if (g > 0) load_v(j + 1, g - 1);  // (the member before is done with its buffer)
+                if (g >= members) continue;
+                const float* v = Vs + g * BK * STRIDE;
 #pragma unroll 1
                 for (int t = 0; t < BK; t += 4) {
                     float4 p[RPT];
@@ -234,11 +260,6 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_paged_simt_kernel(const _
                         }
                     }
                 }
-                __syncthreads();
-                // this buffer is free: the value tile after the next
-                int g2 = g + 2, j2 = j;
-                while (g2 >= members) g2 -= members, ++j2;
-                load_v(j2, g2);
             }
         }
         asm volatile("cp.async.wait_group 0;" ::: "memory");
@@ -292,34 +313,63 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_paged_simt_kernel(const _
         }
         __syncthreads();
         if (*s_id != it.pieces - 1) continue;
-        // The last one joins them, in order of the pieces.
-        for (int i = tid; i < it.rows * members * (D / 4); i += kThreads) {
-            const int x = i % (D / 4), r = i / (D / 4) % it.rows, g = i / (D / 4) / it.rows;
-            float m = -INFINITY;
+        // The last one joins them, in order of the pieces: first every piece's share of every row, then four vectors at a time, whose
+        // loads are on their way together.
+        float* share = smem + S::Q;  // [row][piece]
+        for (int r = tid; r < it.rows; r += kThreads) {
+            float m = -INFINITY, l = 0.f;
             for (int p = 0; p < it.pieces; ++p) {
                 const float2 ml = __ldcg(reinterpret_cast<const float2*>(slot(p) + stats) + r);
+                share[r * kPagedMaxPieces + p] = ml.y == 0.f ? -INFINITY : ml.x;  // (nothing that the row may see)
                 if (ml.y != 0.f) m = fmaxf(m, ml.x);
             }
             const float ref = m == -INFINITY ? 0.f : m;
-            float l = 0.f;
-            float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
             for (int p = 0; p < it.pieces; ++p) {
-                const float2 ml = __ldcg(reinterpret_cast<const float2*>(slot(p) + stats) + r);
-                if (ml.y == 0.f) continue;  // (nothing that the row may see)
-                const float w = expf(ml.x - ref);
-                const float4 v = __ldcg(reinterpret_cast<const float4*>(slot(p) + (((size_t)g * a.slot_rows + r) * D + x * 4) * 4));
-                l += w * ml.y;
-                o.x += w * v.x;
-                o.y += w * v.y;
-                o.z += w * v.z;
-                o.w += w * v.w;
+                const float w = expf(share[r * kPagedMaxPieces + p] - ref);
+                share[r * kPagedMaxPieces + p] = w;
+                l += w * __ldcg(reinterpret_cast<const float2*>(slot(p) + stats) + r).y;
             }
             const float inv = l == 0.f ? 0.f : 1.f / l;
-            int h = e.heads[0];
+            for (int p = 0; p < it.pieces; ++p) share[r * kPagedMaxPieces + p] *= inv;
+        }
+        __syncthreads();
+        const int vectors = it.rows * members * (D / 4);
+        constexpr int U = 4;
+        for (int i0 = tid; i0 < vectors; i0 += U * kThreads) {
+            size_t at[U];
+            int row[U], to[U];
+            float4 o[U];
 #pragma unroll
-            for (int y = 1; y < GM; ++y)
-                if (g == y) h = e.heads[y];
-            *reinterpret_cast<float4*>(out + ((size_t)(it.q0 + r) * a.H + h) * D + x * 4) = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
+            for (int u = 0; u < U; ++u) {
+                const int i = min(i0 + u * kThreads, vectors - 1), x = i % (D / 4), r = i / (D / 4) % it.rows, g = i / (D / 4) / it.rows;
+                int h = e.heads[0];
+#pragma unroll
+                for (int y = 1; y < GM; ++y)
+                    if (g == y) h = e.heads[y];
+                at[u] = (((size_t)g * a.slot_rows + r) * D + x * 4) * 4;
+                row[u] = r * kPagedMaxPieces;
+                to[u] = h * D + x * 4;
+                o[u] = make_float4(0.f, 0.f, 0.f, 0.f);
+            }
+#pragma unroll 4
+            for (int p = 0; p < it.pieces; ++p) {
+                const char* from = slot(p);
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    const float w = share[row[u] + p];
+                    const float4 v = __ldcg(reinterpret_cast<const float4*>(from + at[u]));
+                    if (w != 0.f) {
+                        o[u].x += w * v.x;
+                        o[u].y += w * v.y;
+                        o[u].z += w * v.z;
+                        o[u].w += w * v.w;
+                    }
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (i0 + u * kThreads < vectors)
+                    *reinterpret_cast<float4*>(out + ((size_t)it.q0 + row[u] / kPagedMaxPieces) * a.H * D + to[u]) = o[u];
         }
     }
 }
@@ -343,21 +393,23 @@ int launch(const PagedCall& a, cudaStream_t s) {
 
 }  // namespace
 
-// Rows of a query tile: requests of few tokens take the smaller ones.
-int prefill_paged_simt_rows(int B, int n_tokens) {
+// Rows and keys of a tile: requests of few tokens take fewer rows.
+void prefill_paged_simt_tile(int B, int n_tokens, int D, int* rows, int* keys) {
     const long long per = ((long long)n_tokens + B - 1) / B;
-    return per <= 16 ? 16 : per <= 48 ? 32 : 128;
+    const int rpt = per <= 16 ? 1 : per <= 48 ? 2 : 4;
+    *rows = 16 * rpt;
+    *keys = keys_of(D, rpt);
 }
 
 int prefill_paged_simt(const PagedCall& a, int D, bool fp8, cudaStream_t s) {
     if (D == 128) {
         if (a.bq == 16) return fp8 ? launch<Fp8E4M3, 128, 1>(a, s) : launch<float, 128, 1>(a, s);
         if (a.bq == 32) return fp8 ? launch<Fp8E4M3, 128, 2>(a, s) : launch<float, 128, 2>(a, s);
-        return fp8 ? launch<Fp8E4M3, 128, 8>(a, s) : launch<float, 128, 8>(a, s);
+        return fp8 ? launch<Fp8E4M3, 128, 4>(a, s) : launch<float, 128, 4>(a, s);
     }
     if (a.bq == 16) return fp8 ? launch<Fp8E4M3, 64, 1>(a, s) : launch<float, 64, 1>(a, s);
     if (a.bq == 32) return fp8 ? launch<Fp8E4M3, 64, 2>(a, s) : launch<float, 64, 2>(a, s);
-    return fp8 ? launch<Fp8E4M3, 64, 8>(a, s) : launch<float, 64, 8>(a, s);
+    return fp8 ? launch<Fp8E4M3, 64, 4>(a, s) : launch<float, 64, 4>(a, s);
 }
 
 }  // namespace chai
