@@ -575,8 +575,8 @@ int chai_append_rope_paged_fp8(const void* q, const void* k, const void* v, void
  * The workspace (chai_prefill_paged_workspace_bytes: 2^20 + 64 B + 36 H (B + n_tokens/128 + 1) + 640000 min(n_tokens, 128), whatever
  * the lengths) needs no clearing; calls that share one must be ordered on one stream.
  * H at most 1024, B below 65536, n_tokens at most 2^26, 4 (H + 2 k + k ceil(H/32)) at most 48 KB (the planner's shared
- * memory), and with r query tiles of 128 rows, t key tiles of 128 in a row of the table (CHAI_F32: tiles of 16, 32 or 128
- * rows and 64 keys): r t below 2^27, (r + B) t H below 2^32.
+ * memory), and with r query tiles of 128 rows, t key tiles of 128 in a row of the table (CHAI_F32: tiles of 16, 32 or 64
+ * rows and 32 or 64 keys): r t below 2^27, (r + B) t H below 2^32.
  */
 size_t chai_prefill_paged_workspace_bytes(int B, int H, int n_tokens);
 int chai_prefill_attention_paged(const void* q, const void* k_pages, const void* v_pages, const int32_t* membership,

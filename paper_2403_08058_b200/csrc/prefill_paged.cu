@@ -1042,13 +1042,23 @@ static int prefill_paged(const char* fn, bool fp8, PagedCall a, int n_pages, int
                  a.k, prefill_paged_plan_smem(a.H, a.k));
     const long long dense = (long long)a.H * D, es = (long long)elem_size(dtype);
     if (a.q_stride == 0) a.q_stride = dense;
-    CHAI_REQUIRE(a.q_stride >= dense && a.q_stride * es % 16 == 0 && a.q_stride * es < (1ll << 40), CHAI_ERR_INVALID_ARG,
-                 "%s: the token stride of q must be at least H*D=%lld elements and a multiple of 16 bytes", fn, dense);
+    CHAI_REQUIRE(a.q_stride >= dense && a.q_stride < (1ll << 40) / es && a.q_stride <= (1ll << 56) / a.n_tokens && a.q_stride * es % 16 == 0,
+                 CHAI_ERR_INVALID_ARG,
+                 "%s: the token stride of q must be at least H*D=%lld elements, a multiple of 16 bytes and below 2^40 bytes", fn, dense);
     CHAI_REQUIRE(a.pool.k_page_stride * 2 < (1ull << 40) && a.pool.v_page_stride * 2 < (1ull << 40), CHAI_ERR_UNSUPPORTED,
                  "%s: page strides must be below 2^39 elements", fn);
     const char *q_at = static_cast<const char*>(a.q), *o_at = static_cast<const char*>(a.out);
     CHAI_REQUIRE(q_at + ((a.n_tokens - 1) * a.q_stride + dense) * es <= o_at || o_at + a.n_tokens * dense * es <= q_at,
                  CHAI_ERR_INVALID_ARG, "%s: q and out must not overlap", fn);
+    const bool tensor = dtype == CHAI_BF16;
+    a.bq = pp::BM;
+    a.bk = pp::BN;
+    if (!tensor) prefill_paged_simt_tile(a.B, a.n_tokens, D, &a.bq, &a.bk);
+    // (the work's line is counted in 32 bits for a group, and shares of all of it are)
+    const long long row_tiles = (long long)a.n_tokens / a.bq + 1, keys = a.pool.capacity / a.bk + 2;
+    CHAI_REQUIRE(row_tiles * keys < (1ll << 27) && (row_tiles + a.B) * keys * a.H < (1ll << 32), CHAI_ERR_UNSUPPORTED,
+                 "%s: tokens x table too large: with query tiles of %d rows and key tiles of %d, (tiles + B) * key tiles * H must be below "
+                 "2^32, and tiles * key tiles below 2^27", fn, a.bq, a.bk);
     const size_t need = chai_prefill_paged_workspace_bytes(a.B, a.H, a.n_tokens);
     CHAI_REQUIRE(workspace_bytes >= need, CHAI_ERR_WORKSPACE, "%s: workspace has %zu bytes, %zu needed", fn, workspace_bytes, need);
 
@@ -1078,7 +1088,6 @@ static int prefill_paged(const char* fn, bool fp8, PagedCall a, int n_pages, int
     });
     if (set_up != CHAI_OK) return set_up;
 
-    const bool tensor = dtype == CHAI_BF16;
     const PagedLayout L = paged_layout(a.B, a.H, a.n_tokens);
     char* ws = static_cast<char*>(workspace);
     a.hdr = reinterpret_cast<WsHeader*>(ws);
@@ -1087,17 +1096,9 @@ static int prefill_paged(const char* fn, bool fp8, PagedCall a, int n_pages, int
     a.groups = reinterpret_cast<PagedGroup*>(ws + L.off_groups);
     a.slots = ws + L.off_slots;
     a.gmax = 256 / D;
-    a.bq = pp::BM;
-    a.bk = pp::BN;
-    if (!tensor) prefill_paged_simt_tile(a.B, a.n_tokens, D, &a.bq, &a.bk);
     const int ctas = sms_of_device[dev] * (tensor ? 1 : 2);
     a.ctas = ctas < kPagedMaxCtas ? ctas : kPagedMaxCtas;
     a.slot_rows = ((a.bq < a.n_tokens ? a.bq : a.n_tokens) + 1) & ~1;  // (even: slots are multiples of 16 bytes)
-    // (the work's line is counted in 32 bits for a group, and shares of all of it are)
-    const long long row_tiles = (long long)a.n_tokens / a.bq + 1, keys = a.pool.capacity / a.bk + 2;
-    CHAI_REQUIRE(row_tiles * keys < (1ll << 27) && (row_tiles + a.B) * keys * a.H < (1ll << 32), CHAI_ERR_UNSUPPORTED,
-                 "%s: tokens x table too large: with query tiles of %d rows and key tiles of %d, (tiles + B) * key tiles * H must be below "
-                 "2^32, and tiles * key tiles below 2^27", fn, a.bq, a.bk);
     CHAI_LOG_CALL("%s: B=%d H=%d k=%d n_tokens=%d D=%d dtype=%d page_size=%d causal=%d, query tiles of %d rows", fn, a.B, a.H, a.k,
                   a.n_tokens, D, dtype, page_size, a.causal, a.bq);
     CHAI_LAUNCH_DEPENDENT("prefill_paged_plan_kernel launch", prefill_paged_plan_kernel, dim3(a.B), dim3(128), prefill_paged_plan_smem(a.H, a.k), s, a);

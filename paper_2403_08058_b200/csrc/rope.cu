@@ -468,8 +468,8 @@ int enter(const char* fn, bool fp8, EnterArgs a, int n_pages, int D, size_t k_pa
     const long long dense = (long long)a.H * D, es = (long long)elem_size(dtype);
     for (long long* st : {&a.q_stride, &a.k_stride, &a.v_stride}) {
         if (*st == 0) *st = dense;
-        CHAI_REQUIRE(*st >= dense && *st * es % 16 == 0 && *st <= (1ll << 40), CHAI_ERR_INVALID_ARG,
-                     "%s: token strides must be at least H*D=%lld elements and multiples of 16 bytes", fn, dense);
+        CHAI_REQUIRE(*st >= dense && *st <= (1ll << 56) / a.n_tokens && *st * es % 16 == 0, CHAI_ERR_INVALID_ARG,
+                     "%s: token strides must be at least H*D=%lld elements, multiples of 16 bytes and below 2^56 / n_tokens", fn, dense);
     }
     const char *q_in = static_cast<const char*>(a.q), *q_to = static_cast<const char*>(a.q_out);
     CHAI_REQUIRE(q_in + ((a.n_tokens - 1) * a.q_stride + dense) * es <= q_to || q_to + a.n_tokens * dense * es <= q_in,
