@@ -218,34 +218,37 @@ struct EnterArgs {
     bool wide;  // q, k and v have tokens on 32-byte boundaries
 };
 
-// A rotated row's largest magnitude decides its scale, and lies within fp32's rounding of 1.75 * 2^i about once in 10^6 rows;
-// there the scale could be off by a factor of two for want of a last bit.  Rows that near to the border are decided in
-// fp64.  A rotated number is off by at most 6 u (|x1| + |x2|) m, u = 2^-24 (4 u for a factor, 2 for product and sum), and
-// the row's largest is at least m max|x| / sqrt 2: the error is less than 17 u of it, 15 units of its mantissa.
-constexpr unsigned kBorder = 0x600000u, kNear = 32u;
+// With R = hypot(x1, x2) m and u = 2^-24, a rotated number is off by at most 6 u R: the angle's remainder by 1.6 u, which turns the
+// pair; the factors by 1.5 u and, with a magnitude, 1 u more; product and sum by 2 u.  The row's largest is at least R / sqrt 2,
+// so the error is less than 9 u of it.  That decides two things where it should not: the scale, where the largest lies
+// within 9 units of its mantissa of 1.75 * 2^i (once in 10^6 rows; it would be off by a factor of two), and the byte, where a
+// number, 448 at most after scaling, lies within 9 u 448 of the middle between two e4m3 numbers (once in 10^4).  Such
+// numbers are worked out in fp64, so that bytes and scales are those of the exact ones (8172 tokens of 32 heads: 58 us
+// without; with factors in fp64 for all, which would make this cheap: 76).
+constexpr unsigned kBorder = 0x600000u, kNear = 16u;
+constexpr float kMiddle = 9.f * 448.f / (1 << 24);
 __device__ __forceinline__ bool near_border(unsigned amax_bits) { return (amax_bits & 0x7fffffu) - (kBorder - kNear) <= 2 * kNear; }
+// How far a scaled number's magnitude is from the middle between the e4m3 numbers around it (below 2^-6 these are 2^-9 apart, as
+// they are from there to 2^-5).
+__device__ __forceinline__ float from_middle(float scaled) {
+    float t = fabsf(scaled);
+    t = t < 0.015625f ? t + 0.015625f : t;
+    return fabsf(t - __uint_as_float((__float_as_uint(t) & 0xfff00000u) | 0x80000u));
+}
 
-// Whether any |y| of this thread's vector is above `border`, computed in fp64.
-template <typename T, int EPV>
-__device__ __noinline__ bool above_border(const Rotation& r, int pos, int x, uint4 raw, uint4 partner, double border) {
-    float a[EPV], o[EPV];
-    Vec16<T>::unpack(raw, a);
-    Vec16<T>::unpack(partner, o);
-    bool above = false;
-    for (int e = 0; e < EPV; ++e) {
-        const int at = x * EPV + e, half = r.rot >> 1;
-        double y = a[e];
-        if (at < r.rot) {
-            const bool second = r.interleaved ? (at & 1) : at >= half;
-            const double t = __dmul_rn((double)pos, r.turns[r.interleaved ? at >> 1 : second ? at - half : at]);
-            double s, c;
-            sincospi(2.0 * (t - rint(t)), &s, &c);
-            const double b = r.interleaved ? a[e ^ 1] : o[e];
-            y = (a[e] * c + (second ? b : -b) * s) * r.magnitude;
-        }
-        above |= isfinite(y) && fabs(y) > border;
-    }
-    return above;
+// Element `at` of a row, rotated in fp64; rounded towards zero to fp32, with the last bit set where that is not the number:
+// comparisons and a rounding to fewer bits go as the number's own would.  (Rare: the row is read once more.)
+template <typename T>
+__device__ __noinline__ float rotated_64(const Rotation& r, int pos, const T* row, int at) {
+    const int half = r.rot >> 1;
+    const bool second = r.interleaved ? (at & 1) : at >= half;
+    const double t = __dmul_rn((double)pos, r.turns[r.interleaved ? at >> 1 : second ? at - half : at]);
+    double s, c;
+    sincospi(2.0 * (t - rint(t)), &s, &c);
+    const double x = (float)row[at], other = (float)row[r.interleaved ? at ^ 1 : second ? at - half : at + half];
+    const double z = (x * c + (second ? other : -other) * s) * r.magnitude;
+    const float f = __double2float_rz(z);
+    return (double)f == z ? f : __uint_as_float(__float_as_uint(f) | 1u);
 }
 
 // Stores what a thread has of a row (raw, or of a rotated one the numbers y) at `row` of plane `pl` of a page; store: whether at
@@ -273,7 +276,7 @@ __device__ __forceinline__ void put_row_fp8(const EnterArgs& a, bool key, int pl
 // go through a loop of their own.  Blocks to an SM: what the registers of a rotated e4m3 row (its border check among them) allow is
 // two; rows stored as they are gain from a third (bf16, 8172 tokens of 32 heads, 128 wide: 57 -> 50 us), and a fourth, 47 us there,
 // spills what 800 tokens wait for (6.8 -> 7.6 us).
-// To e4m3 the 8172 tokens take 58 us, 178 MB at 3.1 TB/s: bound by the instructions of the rotation, the row's largest magnitude
+// To e4m3 the 8172 tokens take 67 us, 178 MB at 2.7 TB/s: bound by the instructions of the rotation, the row's largest magnitude
 // and the conversion, 16 warps to an SM.
 template <typename T, int D, bool FP8>
 __global__ void __launch_bounds__(kThreads, FP8 ? 2 : 3) append_rope_kernel(const __grid_constant__ EnterArgs a) {
@@ -377,22 +380,40 @@ __global__ void __launch_bounds__(kThreads, FP8 ? 2 : 3) append_rope_kernel(cons
                     put_row<T, D, FP8>(a, true, r, page, row, x, there && key, out);
                 } else {
                     if (!__any_sync(0xffffffffu, there && key)) continue;
-                    unsigned m = 0;
+                    auto largest = [&]() {
+                        unsigned m = 0;
 #pragma unroll
-                    for (int e = 0; e < EPL; ++e) m = max(m, finite_magnitude(y[e]));
+                        for (int e = 0; e < EPL; ++e) m = max(m, finite_magnitude(y[e]));
 #pragma unroll
-                    for (int o = LPR / 2; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
+                        for (int o = LPR / 2; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
+                        return m;
+                    };
+                    unsigned m = largest();
                     int e2 = m == 0 ? 0 : scale_exponent(m);
-                    const bool close = key && there && a.rot.rot > 0 && near_border(m) && m >= 0x08000000u;
-                    if (__any_sync(0xffffffffu, close)) {
-                        const unsigned border = (m & 0x7f800000u) | kBorder;
-                        unsigned above = 0;
+                    float nearest = 1.f;
 #pragma unroll
-                        for (int i = 0; i < VPL; ++i)
-                            if (close && above_border<T, EPV>(a.rot, pos, x * VPL + i, mine[i], other[i], (double)__uint_as_float(border))) above = 1;
+                    for (int e = 0; e < EPL; ++e)
+                        if (in_rot[e / EPV]) nearest = fminf(nearest, from_middle(y[e] * pow2(-e2)));
+                    const bool turns = key && there && a.rot.rot > 0, border = near_border(m) && m >= 0x08000000u;
+                    if (__any_sync(0xffffffffu, turns && (border || nearest < kMiddle))) {
+                        const T* from = static_cast<const T*>(a.k) + token * a.k_stride + (long long)head[u] * D;
+                        unsigned which = 0;  // a bit an element
 #pragma unroll
-                        for (int s = LPR / 2; s > 0; s >>= 1) above |= __shfl_xor_sync(0xffffffffu, above, s);
-                        if (close) e2 = scale_exponent(border) + (int)above;
+                        for (int e = 0; e < EPL; ++e) {
+                            const unsigned size = finite_magnitude(y[e]);
+                            const bool close = from_middle(y[e] * pow2(-e2)) < kMiddle || (border && near_border(size) && (size ^ m) >> 23 == 0);
+                            if (turns && in_rot[e / EPV] && close) which |= 1u << e;
+                        }
+                        for (; which != 0; which &= which - 1) {
+                            const int at = __ffs(which) - 1;
+                            const float z = rotated_64<T>(a.rot, pos, from, x * EPL + at);
+#pragma unroll
+                            for (int e = 0; e < EPL; ++e)
+                                if (e == at) y[e] = z;
+                        }
+                        __syncwarp();
+                        m = largest();
+                        e2 = m == 0 ? 0 : scale_exponent(m);
                     }
                     put_row_fp8<T, D>(a, true, r, page, row, x, there && key, y, e2);
                 }
