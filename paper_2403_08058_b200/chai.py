@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 
 import torch
 
@@ -782,6 +783,9 @@ def _turns(turns, dev):
     return turns.data_ptr(), 2 * turns.numel()
 
 
+_STRIDES = struct.Struct("12q")   # (an array of ctypes takes four times as long to fill)
+
+
 def chai_rope(q, k=None, positions=None, turns=None, magnitude: float = 1.0, interleaved: bool = False, q_out=None, k_out=None):
     """q [B,Hq,N,D] and k [B,Hk,N,D] (or None) rotated by positions [B,N] int32 (None: 0 .. N-1) -> (q_out, k_out), new arrays
     of the same strides unless given (they may be q and k themselves).  Any strides with contiguous rows, e.g.
@@ -821,7 +825,7 @@ def chai_rope(q, k=None, positions=None, turns=None, magnitude: float = 1.0, int
         raise ValueError("give the frequencies (chai_rope_frequencies)")
     at, rot = _turns(turns, dev)
     _paged_call(load().chai_rope, dev, q.data_ptr(), _ptr(k), q_out.data_ptr(), _ptr(k_out), _ptr(positions), at, B, Hq, Hk, N,
-                D, rot, 1 if interleaved else 0, _double(magnitude), (ctypes.c_int64 * 12)(*strides), io)
+                D, rot, 1 if interleaved else 0, _double(magnitude), _STRIDES.pack(*strides), io)
     return q_out, k_out
 
 

@@ -29,6 +29,7 @@ struct PlanArgs {
     WsHeader* hdr;
     int32_t *top, *page_start;  // workspace: depth of the stack before pages are taken, and [B] pages taken before each request
     int B, n_tokens, n_pages, page_size, max_pages, capacity;
+    int step, n_starts;         // of the requests' beginnings, every step-th (n_starts and the end) goes to shared memory
     FastDiv by_page;
 };
 
@@ -47,28 +48,53 @@ __device__ __forceinline__ Two block_scan(Two v, Two* s_warp, Two* total) {
         const long long x = __shfl_up_sync(0xffffffffu, v.x, o), y = __shfl_up_sync(0xffffffffu, v.y, o);
         if (lane >= o) v.x += x, v.y += y;
     }
+    if (n_warps == 1) {
+        *total = {__shfl_sync(0xffffffffu, v.x, 31), __shfl_sync(0xffffffffu, v.y, 31)};
+        return v;
+    }
     __syncthreads();  // (the array may still be read by the scan before)
     if (lane == 31) s_warp[warp] = v;
     __syncthreads();
-    Two before = {0, 0}, all = {0, 0};
-    for (int w = 0; w < n_warps; ++w) {
-        const Two t = s_warp[w];
-        if (w < warp) before.x += t.x, before.y += t.y;
-        all.x += t.x, all.y += t.y;
+    Two all = lane < n_warps ? s_warp[lane] : Two{0, 0}, own = all;  // (every warp scans the warps' sums)
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const long long x = __shfl_up_sync(0xffffffffu, all.x, o), y = __shfl_up_sync(0xffffffffu, all.y, o);
+        if (lane >= o) all.x += x, all.y += y;
     }
-    *total = all;
-    return {v.x + before.x, v.y + before.y};
+    v.x += __shfl_sync(0xffffffffu, all.x - own.x, warp);
+    v.y += __shfl_sync(0xffffffffu, all.y - own.y, warp);
+    *total = {__shfl_sync(0xffffffffu, all.x, 31), __shfl_sync(0xffffffffu, all.y, 31)};
+    return v;
+}
+
+// Where requests' tokens begin, in shared memory: all beginnings, or of many requests every step-th.
+constexpr int kStarts = 1024;
+__device__ __forceinline__ void load_starts(const PlanArgs& a, int* s_start) {
+    const int step = a.step;
+    for (int i = threadIdx.x; i * step <= a.B; i += blockDim.x) s_start[i] = a.token_start[i * step];
+    __syncthreads();
 }
 
 // Tokens t0 .. t0 + kTokensPerThread - 1 of the packed arrays.
-__device__ __forceinline__ void plan_tokens(const PlanArgs& a, int t0, int top) {
+__device__ __forceinline__ void plan_tokens(const PlanArgs& a, const int* s_start, int t0, int top) {
     if (t0 >= a.n_tokens) return;
-    int lo = 0, hi = a.B;  // the largest request with token_start <= t0 (requests without tokens: the last of equals)
+    // the largest request with token_start <= t0 (requests without tokens: the last of equals)
+    const int step = a.step;
+    int lo = 0, hi = a.n_starts;
     while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
-        if (a.token_start[mid] <= t0) lo = mid; else hi = mid;
+        if (s_start[mid] <= t0) lo = mid; else hi = mid;
     }
-    int b = lo, start = a.token_start[b], end = a.token_start[b + 1], cur = -1, held = 0, seq = 0, first = 0;
+    if (step > 1) {
+        hi = min((lo + 1) * step, a.B);
+        lo *= step;
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (a.token_start[mid] <= t0) lo = mid; else hi = mid;
+        }
+    }
+    auto begins = [&](int i) { return step == 1 ? s_start[i] : a.token_start[i]; };
+    int b = lo, start = begins(b), end = begins(b + 1), cur = -1, held = 0, seq = 0, first = 0;
     int request[kTokensPerThread], position[kTokensPerThread];
     long long slot[kTokensPerThread];
     bool bad = false;
@@ -78,7 +104,7 @@ __device__ __forceinline__ void plan_tokens(const PlanArgs& a, int t0, int top) 
         while (t >= end && b + 1 < a.B) {
             ++b;
             start = end;
-            end = a.token_start[b + 1];
+            end = begins(b + 1);
         }
         request[i] = -1;
         position[i] = 0;
@@ -129,6 +155,7 @@ __global__ void __launch_bounds__(kPlanThreads) plan_requests_kernel(const PlanA
     __shared__ Two s_warp[32];
     __shared__ int s_held[kPlanThreads];
     __shared__ long long s_off[kPlanThreads];
+    __shared__ int s_list[kPlanThreads], s_n, s_start[kStarts + 1];
     dependent_grid_sync();
     const int tid = threadIdx.x, nt = blockDim.x, lane = tid & 31, warp = tid >> 5, n_warps = nt >> 5;
     const int count = *a.free_count;
@@ -145,12 +172,14 @@ __global__ void __launch_bounds__(kPlanThreads) plan_requests_kernel(const PlanA
             if (s < 0 || s > a.capacity) full = true;  // (not a length of this list: nothing is given back)
             else held = pages_for(a, s);
         }
+        if (tid == 0) s_n = 0;
         if (!__syncthreads_or(held > 0)) continue;
         s_held[tid] = held;
+        if (held > 0) s_list[atomicAdd(&s_n, 1)] = tid;  // (in any order: where a list goes is a sum over the requests before)
         __syncthreads();
-        for (int i = warp; i < nt; i += n_warps) {  // a list with an entry that is no page is not given back
-            const int h = s_held[i];
-            if (h == 0) continue;
+        const int n_ended = s_n;
+        for (int e = warp; e < n_ended; e += n_warps) {  // a list with an entry that is no page is not given back
+            const int i = s_list[e], h = s_held[i];
             const int32_t* list = a.block_table + (size_t)(base + i) * a.max_pages;
             bool odd = false;
             for (int j = lane; j < h; j += 32) odd |= list[j] < 0 || list[j] >= a.n_pages;
@@ -163,8 +192,8 @@ __global__ void __launch_bounds__(kPlanThreads) plan_requests_kernel(const PlanA
         held = s_held[tid];
         s_off[tid] = block_scan({held, 0}, s_warp, &total).x - held;
         __syncthreads();
-        for (int i = warp; i < nt; i += n_warps) {
-            const int h = s_held[i];
+        for (int e = warp; e < n_ended; e += n_warps) {
+            const int i = s_list[e], h = s_held[i];
             const int32_t* list = a.block_table + (size_t)(base + i) * a.max_pages;
             for (int j = lane; j < h; j += 32) {
                 const long long at = (long long)top + s_off[i] + j;
@@ -214,13 +243,16 @@ __global__ void __launch_bounds__(kPlanThreads) plan_requests_kernel(const PlanA
     }
     if constexpr (TOKENS) {
         __syncthreads();
-        for (int t0 = tid * kTokensPerThread; t0 < a.n_tokens; t0 += nt * kTokensPerThread) plan_tokens(a, t0, top);
+        load_starts(a, s_start);
+        for (int t0 = tid * kTokensPerThread; t0 < a.n_tokens; t0 += nt * kTokensPerThread) plan_tokens(a, s_start, t0, top);
     }
 }
 
 __global__ void __launch_bounds__(kTokenThreads) plan_tokens_kernel(const PlanArgs a) {
+    __shared__ int s_start[kStarts + 1];
     dependent_grid_sync();
-    plan_tokens(a, (int)(blockIdx.x * kTokenThreads + threadIdx.x) * kTokensPerThread, *a.top);
+    load_starts(a, s_start);
+    plan_tokens(a, s_start, (int)(blockIdx.x * kTokenThreads + threadIdx.x) * kTokensPerThread, *a.top);
 }
 
 int plan(PlanArgs a, cudaStream_t s) {
@@ -241,6 +273,8 @@ int plan(PlanArgs a, cudaStream_t s) {
                  "%s: max_pages * page_size must be below 2^30", fn);
     a.capacity = a.max_pages * a.page_size;
     a.by_page = FastDiv((unsigned)a.page_size);
+    a.step = (a.B + kStarts - 1) / kStarts;
+    a.n_starts = (a.B + a.step - 1) / a.step;
     const bool one = a.n_tokens <= kOneBlockTokens;
     const int want = max(a.B, one ? (a.n_tokens + kTokensPerThread - 1) / kTokensPerThread : 1);
     const int threads = want >= kPlanThreads ? kPlanThreads : (want + 31) / 32 * 32;
