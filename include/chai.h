@@ -523,7 +523,7 @@ int chai_rope_frequencies(double* turns_host, double* magnitude_host, int rot, i
  * Whole prompts, before chai_prefix_features and chai_prefill_attention: q [B,Hq,N,D] and k [B,Hk,N,D] (Hk may be 0).
  *   positions [B,N] int32, device, or NULL: 0 .. N-1;  turns [rot/2] fp64, device;  magnitude_host: HOST, or NULL for 1
  *   strides  HOST array of 12, elements: batch, head, token of q, of q_out, of k, of k_out; NULL: all contiguous.  Multiples of
- *            16 bytes; the D elements of a row are contiguous
+ *            16 bytes, of inputs 0 too (one row for many); the D elements of a row are contiguous
  * q_out may be q itself (same strides) and k_out k; other overlaps are not allowed.
  */
 int chai_rope(const void* q, const void* k, void* q_out, void* k_out, const int32_t* positions, const double* turns, int B,
@@ -536,7 +536,7 @@ int chai_rope(const void* q, const void* k, void* q_out, void* k_out, const int3
  *   k_pages[page][c][row] = R k[t][r],   v_pages[page][h][row] = v[t][h],   q_out[t][r] = R q[t][r]
  * Only representatives' queries are looked at by the attention calls; the other rows of q_out stay as they were, and so do
  * tokens with slot -1.
- *   q, k, v [n_tokens,H,D], q_out [n_tokens,H,D] contiguous, not overlapping q
+ *   q, k, v [n_tokens,H,D], q_out [n_tokens,H,D] contiguous, overlapping none of them
  *   *_token_stride           elements between tokens of q, k and v: 0 for H*D; more where they are parts of one
  *                            projection's output.  Multiples of 16 bytes
  *   k_pages, v_pages, their strides, page_size, reps as for the paged calls above; no two tokens share a slot
@@ -574,7 +574,7 @@ int chai_append_rope_paged_fp8(const void* q, const void* k, const void* v, void
  * request that do not see it (as zero times infinity); among keys it reaches only those that see it.
  * The workspace (chai_prefill_paged_workspace_bytes: 2^20 + 64 B + 36 H (B + n_tokens/128 + 1) + 640000 min(n_tokens, 128), whatever
  * the lengths) needs no clearing; calls that share one must be ordered on one stream.
- * H at most 1024, B below 65536, n_tokens at most 2^26, 4 (H + 2 k + k ceil(H/32)) at most 48 KB (the planner's shared
+ * H at most 1024, B below 65536, n_tokens at most 2^26, 4 (H + (k + 1) (3 + ceil(H/32))) at most 48 KB (the planner's shared
  * memory), and with r query tiles of 128 rows, t key tiles of 128 in a row of the table (CHAI_F32: tiles of 16, 32 or 64
  * rows and 32 or 64 keys): r t below 2^27, (r + B) t H below 2^32.
  */

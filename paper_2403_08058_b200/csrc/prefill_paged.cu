@@ -1101,7 +1101,7 @@ static int prefill_paged(const char* fn, bool fp8, PagedCall a, int n_pages, int
     a.slot_rows = ((a.bq < a.n_tokens ? a.bq : a.n_tokens) + 1) & ~1;  // (even: slots are multiples of 16 bytes)
     CHAI_LOG_CALL("%s: B=%d H=%d k=%d n_tokens=%d D=%d dtype=%d page_size=%d causal=%d, query tiles of %d rows", fn, a.B, a.H, a.k,
                   a.n_tokens, D, dtype, page_size, a.causal, a.bq);
-    CHAI_LAUNCH_DEPENDENT("prefill_paged_plan_kernel launch", prefill_paged_plan_kernel, dim3(a.B), dim3(128), prefill_paged_plan_smem(a.H, a.k), s, a);
+    CHAI_LAUNCH_DEPENDENT("prefill_paged_plan_kernel launch", prefill_paged_plan_kernel, dim3(a.B), dim3(kPagedPlanThreads), prefill_paged_plan_smem(a.H, a.k), s, a);
     if (!tensor) return prefill_paged_simt(a, D, fp8, s);
     pp::Tma maps;
     int box_rows = 128;

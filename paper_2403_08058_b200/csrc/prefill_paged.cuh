@@ -86,100 +86,84 @@ __device__ __forceinline__ int key_tiles(const PagedCall& a, int n, int kv, int 
     return (end + a.bk - 1) / a.bk;
 }
 
-// Shared memory of the planner: membership, representatives, member masks and first groups of the clusters.
-inline size_t prefill_paged_plan_smem(int H, int k) { return sizeof(int) * ((size_t)H + 2 * (size_t)k + (size_t)k * ((H + 31) / 32)); }
+// Shared memory of the planner: membership, and of every cluster and the heads of none the representative, members, first group and
+// member mask.
+inline size_t prefill_paged_plan_smem(int H, int k) { return sizeof(int) * ((size_t)H + ((size_t)k + 1) * (3 + (H + 31) / 32)); }
 
-// Grid B, 128 threads: the first warp builds the groups, the others look the pages over.
-static __global__ void __launch_bounds__(128) prefill_paged_plan_kernel(const PagedCall a) {
+// Grid B.  A head a thread, but for the clusters' sums, which the first warp makes while the others look the pages over.
+// (One warp for all of it took 3 us for 32 heads, 10 for 72.)
+constexpr int kPagedPlanThreads = 256;
+static __global__ void __launch_bounds__(kPagedPlanThreads) prefill_paged_plan_kernel(const PagedCall a) {
     extern __shared__ __align__(16) int s_plan[];
     __shared__ int s_in[3];
     dependent_grid_sync();
     const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 31, H = a.H, k = a.k, W = (H + 31) >> 5;
     int* mem = s_plan;
-    int* rep = mem + H;
-    int* slot = rep + k;
-    unsigned* mask = reinterpret_cast<unsigned*>(slot + k);
+    int* rep = mem + H;           // (k: the heads of no usable cluster)
+    int* members = rep + k + 1;
+    int* slot = members + k + 1;
+    unsigned* mask = reinterpret_cast<unsigned*>(slot + k + 1);
     int x = 0;
-    if (tid >= 32 && tid < 35) x = tid == 34 ? a.kv_lens[b] : a.token_start[b + tid - 32];
-    for (int h = tid; h < H; h += 128) mem[h] = a.membership[(size_t)b * H + h];
-    for (int c = tid; c < k; c += 128) rep[c] = a.reps[(size_t)b * k + c];
-    for (int i = tid; i < k * W; i += 128) mask[i] = 0u;
+    if (tid < 3) x = tid == 2 ? a.kv_lens[b] : a.token_start[b + tid];
+    for (int h = tid; h < H; h += kPagedPlanThreads) mem[h] = a.membership[(size_t)b * H + h];
+    for (int c = tid; c <= k; c += kPagedPlanThreads) rep[c] = c < k ? a.reps[(size_t)b * k + c] : -1;
+    for (int i = tid; i < (k + 1) * W; i += kPagedPlanThreads) mask[i] = 0u;
     if (b == 0)
-        for (int i = tid; i < a.ctas; i += 128) a.done[i] = 0;
-    if (tid >= 32 && tid < 35) s_in[tid - 32] = min(max(x, 0), tid == 34 ? a.pool.capacity : a.n_tokens);
+        for (int i = tid; i < a.ctas; i += kPagedPlanThreads) a.done[i] = 0;
+    if (tid < 3) s_in[tid] = min(max(x, 0), tid == 2 ? a.pool.capacity : a.n_tokens);
     __syncthreads();
     const int start = s_in[0], n = max(s_in[1] - start, 0);
     int kv = s_in[2], n_groups = 0;
-    bool bad_page = false, bad_head = false;
-    if (tid >= 32) {
-        const int32_t* table = a.pool.block_table + (size_t)b * a.pool.max_pages;
-        const int pages = n > 0 ? (kv + a.pool.page_size - 1) / a.pool.page_size : 0;
-#pragma unroll 4
-        for (int p = tid - 32; p < pages; p += 96) bad_page |= (unsigned)table[p] >= (unsigned)a.pool.n_pages;
-    } else if (n > 0) {
+    bool bad_page = false;
+    if (n > 0) {
         // a cluster is usable if its representative is one of its heads
-        auto usable = [&](int c) {
-            if (c < 0 || c >= k) return false;
+        auto row_of = [&](int h) {
+            const int c = mem[h];
+            if (c < 0 || c >= k) return k;
             const int r = rep[c];
-            return r >= 0 && r < H && mem[r] == c;
+            return r >= 0 && r < H && mem[r] == c ? c : k;
         };
-        int n_bad = 0;
-        for (int w = 0; w < W; ++w) {
-            const int h = w * 32 + lane, c = h < H ? mem[h] : -2;
-            const bool good = h < H && usable(c);
-            const unsigned peers = __match_any_sync(0xffffffffu, good ? c : -1);
-            if (good && lane == __ffs(peers) - 1) mask[c * W + w] = peers;
-            n_bad += __popc(__ballot_sync(0xffffffffu, h < H && !good));
-        }
-        __syncwarp();
-        for (int c0 = 0; c0 < k; c0 += 32) {  // first group of each cluster
-            int members = 0;
-            if (c0 + lane < k)
-                for (int w = 0; w < W; ++w) members += __popc(mask[(c0 + lane) * W + w]);
-            const int groups = (members + a.gmax - 1) / a.gmax;
-            int incl = groups;
+        for (int h = tid; h < H; h += kPagedPlanThreads) atomicOr(&mask[row_of(h) * W + (h >> 5)], 1u << (h & 31));
+        __syncthreads();
+        if (tid < 32) {  // first group of each cluster
+            for (int c0 = 0; c0 <= k; c0 += 32) {
+                const int c = c0 + lane;
+                int count = 0;
+                if (c <= k)
+                    for (int w = 0; w < W; ++w) count += __popc(mask[c * W + w]);
+                const int groups = (count + a.gmax - 1) / a.gmax;
+                int incl = groups;
 #pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const int y = __shfl_up_sync(0xffffffffu, incl, o);
-                if (lane >= o) incl += y;
-            }
-            if (c0 + lane < k) slot[c0 + lane] = n_groups + incl - groups;
-            n_groups += __shfl_sync(0xffffffffu, incl, 31);
-        }
-        __syncwarp();
-        int bad_before = 0;
-        for (int w = 0; w < W; ++w) {  // every head finds its group: sizes as even as possible, the larger ones first
-            const int h = w * 32 + lane, c = h < H ? mem[h] : -2;
-            const bool good = h < H && usable(c);
-            const unsigned bads = __ballot_sync(0xffffffffu, h < H && !good), below = (1u << lane) - 1u;
-            if (h < H) {
-                int rank, members, at, groups;
-                if (good) {
-                    rank = members = 0;
-                    for (int v = 0; v < W; ++v) {
-                        const unsigned m = mask[c * W + v];
-                        members += __popc(m);
-                        rank += v < w ? __popc(m) : v == w ? __popc(m & below) : 0;
-                    }
-                    at = slot[c];
-                } else {
-                    rank = bad_before + __popc(bads & below);
-                    members = n_bad;
-                    at = n_groups;
+                for (int o = 1; o < 32; o <<= 1) {
+                    const int y = __shfl_up_sync(0xffffffffu, incl, o);
+                    if (lane >= o) incl += y;
                 }
-                groups = (members + a.gmax - 1) / a.gmax;
-                const int size = members / groups, larger = members - size * groups, cut = larger * (size + 1);
-                const int g = rank < cut ? rank / (size + 1) : larger + (rank - cut) / size;
-                const int first = g <= larger ? g * (size + 1) : cut + (g - larger) * size;
-                PagedGroup* e = a.groups + (size_t)b * H + at + g;
-                e->heads[rank - first] = h;
-                if (rank == first) *reinterpret_cast<int4*>(e) = make_int4(good ? c : -1, good ? rep[c] : -1, g < larger ? size + 1 : size, 0);
+                if (c <= k) {
+                    members[c] = count;
+                    slot[c] = n_groups + incl - groups;
+                }
+                n_groups += __shfl_sync(0xffffffffu, incl, 31);
             }
-            bad_before += __popc(bads);
+        } else {
+            const int32_t* table = a.pool.block_table + (size_t)b * a.pool.max_pages;
+            const int pages = (kv + a.pool.page_size - 1) / a.pool.page_size;
+#pragma unroll 4
+            for (int p = tid - 32; p < pages; p += kPagedPlanThreads - 32) bad_page |= (unsigned)table[p] >= (unsigned)a.pool.n_pages;
         }
-        n_groups += (n_bad + a.gmax - 1) / a.gmax;
-        bad_head = n_bad > 0;
+        __syncthreads();
+        for (int h = tid; h < H; h += kPagedPlanThreads) {  // every head finds its group: sizes as even as possible, the larger ones first
+            const int c = row_of(h), w = h >> 5, all = members[c];
+            int rank = __popc(mask[c * W + w] & ((1u << (h & 31)) - 1u));
+            for (int v = 0; v < w; ++v) rank += __popc(mask[c * W + v]);
+            const int groups = (all + a.gmax - 1) / a.gmax, size = all / groups, larger = all - size * groups, cut = larger * (size + 1);
+            const int g = rank < cut ? rank / (size + 1) : larger + (rank - cut) / size;
+            const int first = g <= larger ? g * (size + 1) : cut + (g - larger) * size;
+            PagedGroup* e = a.groups + (size_t)b * H + slot[c] + g;
+            e->heads[rank - first] = h;
+            if (rank == first) *reinterpret_cast<int4*>(e) = make_int4(c < k ? c : -1, rep[c], g < larger ? size + 1 : size, 0);
+        }
     }
+    const bool bad_head = n > 0 && members[k] > 0;  // (the first warp's own writing)
     bad_page = __syncthreads_or(bad_page);
     if (tid >= 32) return;
     if (bad_page) kv = 0;

@@ -492,9 +492,14 @@ int enter(const char* fn, bool fp8, EnterArgs a, int n_pages, int D, size_t k_pa
         CHAI_REQUIRE(*st >= dense && *st <= (1ll << 56) / a.n_tokens && *st * es % 16 == 0, CHAI_ERR_INVALID_ARG,
                      "%s: token strides must be at least H*D=%lld elements, multiples of 16 bytes and below 2^56 / n_tokens", fn, dense);
     }
-    const char *q_in = static_cast<const char*>(a.q), *q_to = static_cast<const char*>(a.q_out);
-    CHAI_REQUIRE(q_in + ((a.n_tokens - 1) * a.q_stride + dense) * es <= q_to || q_to + a.n_tokens * dense * es <= q_in,
-                 CHAI_ERR_INVALID_ARG, "%s: q and q_out must not overlap", fn);
+    const char* q_to = static_cast<const char*>(a.q_out);
+    const long long apart[3] = {a.q_stride, a.k_stride, a.v_stride};
+    const void* in[3] = {a.q, a.k, a.v};
+    for (int i = 0; i < 3; ++i) {
+        const char* from = static_cast<const char*>(in[i]);
+        CHAI_REQUIRE(from + ((a.n_tokens - 1) * apart[i] + dense) * es <= q_to || q_to + a.n_tokens * dense * es <= from,
+                     CHAI_ERR_INVALID_ARG, "%s: q_out must not overlap q, k or v", fn);
+    }
     a.k_page_stride = pool.k_page_stride;
     a.v_page_stride = pool.v_page_stride;
     a.by_page = pool.by_page;
@@ -583,6 +588,8 @@ int chai_rope(const void* q, const void* k, void* q_out, void* k_out, const int3
             *to[j] = strides != nullptr ? strides[6 * i + j] : dense[j % 3];
             CHAI_REQUIRE(heads[i] == 0 || (*to[j] >= 0 && *to[j] * es % 16 == 0 && *to[j] <= (1ll << 40)), CHAI_ERR_INVALID_ARG,
                          "%s: strides must be multiples of 16 bytes, from 0 to 2^40 elements", fn);
+            const long long sizes[3] = {B, heads[i], N};
+            CHAI_REQUIRE(heads[i] == 0 || j < 3 || *to[j] > 0 || sizes[j % 3] <= 1, CHAI_ERR_INVALID_ARG, "%s: strides of an output must not be 0", fn);
         }
     }
     CHAI_LOG_CALL("%s: B=%d Hq=%d Hk=%d N=%d D=%d rot=%d interleaved=%d dtype=%d", fn, B, Hq, Hk, N, D, rot, interleaved, dtype);

@@ -94,6 +94,9 @@ def test_rope_refusals(lib):
             strides = list(dense)
             strides[i] = bad
             assert rope(lib, strides=strides) == INVALID and b"strides" in lib.chai_last_error(), (i, bad)
+        if i % 6 >= 3:                                           # rows of an output on top of one another
+            strides[i] = 0
+            assert rope(lib, strides=strides) == INVALID and b"output" in lib.chai_last_error(), i
 
 
 @pytest.mark.parametrize("fp8", [False, True])
@@ -117,6 +120,10 @@ def test_append_rope_refusals(lib, fp8):
     for at in (AT, AT + 16, AT + 5 * 4 * 128 * 2 - 16):          # the queries' output inside, before its end, on its last row
         p = [AT, AT, AT, at] + [AT] * (n - 4)
         assert enter(lib, fp8, p) == INVALID and b"overlap" in lib.chai_last_error()
+    for i in (0, 1, 2):                                          # any of the three behind it, but for its last row's end
+        p = [AT - 65536] * 3 + [AT] * (n - 3)
+        p[i] = AT + 4 * 512 * 2
+        assert enter(lib, fp8, p) == INVALID and b"overlap" in lib.chai_last_error(), i
     p = [AT + 4 * 512 * 2, AT, AT, AT] + [AT] * (n - 4)
     assert enter(lib, fp8, p) == INVALID and b"overlap" in lib.chai_last_error()
     p = [AT, AT, AT, AT + 5 * 4 * 128 * 2] + [AT] * (n - 4)      # (the rows of a wider array reach further)
