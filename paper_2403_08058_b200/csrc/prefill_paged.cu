@@ -56,6 +56,7 @@ template <int N>
 __device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
 template <int N>
 __device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
+constexpr int JOIN_BARRIER = 5;  // (1 - 4: the quadrants' pairs of softmax warps)
 constexpr float REF_WINDOW = 32.f;
 constexpr uint32_t TMEM_COLS = 512;
 constexpr uint32_t S_COL0 = 0, P_COL0 = 128, O_COL0 = 256;
@@ -80,8 +81,9 @@ constexpr int OFF_LSUM = OFF_XCH + 2 * BM * 4;       // [half][row] sums
 constexpr int OFF_REF = OFF_LSUM + 2 * BM * 4;       // [row] reference of the exponentials
 constexpr int OFF_ITEM = OFF_REF + BM * 4;
 constexpr int ITEM_BYTES = 64;
-constexpr int SMEM_BYTES = OFF_ITEM + 3 * ITEM_BYTES;
-static_assert(OFF_ITEM % 16 == 0 && SMEM_BYTES <= 232448, "shared memory budget");
+constexpr int OFF_JOINS = OFF_ITEM + 3 * ITEM_BYTES;  // bits: which query tiles' (begun before the share, in it) quadrants to join
+constexpr int SMEM_BYTES = OFF_JOINS + 16;
+static_assert(ITEM_BYTES == kPagedJoinBytes && OFF_ITEM % 16 == 0 && SMEM_BYTES <= 232448, "shared memory budget");
 
 struct Bars {
     uint32_t base;
@@ -165,7 +167,7 @@ __device__ __forceinline__ uint32_t e4m3x4_to_bf16_bits(uint32_t w, uint32_t fac
 
 // Writes out the ei-th finished item, by the four epilogue warps, one thread per query row; false: there is none any more, or a wait ran
 // out.
-template <int HD, int JOIN>
+template <int HD>
 __device__ __forceinline__ bool finish_item(const PagedCall& a, uint8_t* smem, uint32_t tmem_base, volatile int* abort_flag, int ei) {
     constexpr int GM = HD == 128 ? 2 : 4;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -239,7 +241,7 @@ __device__ __forceinline__ bool finish_item(const PagedCall& a, uint8_t* smem, u
         }
     }
     if (!split || quad * 32 >= ep.rows) return true;
-    // A piece: its rows' references and sums; the warp that finishes its rows' last piece joins them, in order of the
+    // A piece: its rows' references and sums; the CTA whose warp finishes its rows' last piece joins them, in order of the
     // pieces.  (A byte of the counter per warp.)
     if (live) reinterpret_cast<float2*>(reinterpret_cast<char*>(part) + stats)[row] = make_float2(ref, l);
     __threadfence();
@@ -251,77 +253,91 @@ __device__ __forceinline__ bool finish_item(const PagedCall& a, uint8_t* smem, u
     }
     before = __shfl_sync(0xffffffffu, before, 0);
     if ((int)before != ep.pieces - 1) return true;
-    const int n_rows = min(32, ep.rows - quad * 32), pieces = ep.pieces;
-    // First a lane a row: the reference of all pieces, and what the sum is divided by.
-    float m_all = -INFINITY, sum = 0.f;
-#pragma unroll 4
-    for (int p = 0; p < pieces; ++p) {
-        const float2 s = live ? __ldcg(reinterpret_cast<const float2*>(slot(p) + stats) + row) : make_float2(0.f, 0.f);
-        if (s.y == 0.f) continue;  // (a piece that the row sees nothing of)
-        const float m = fmaxf(m_all, s.x);
-        sum = sum * (sum == 0.f ? 0.f : fast_exp2(m_all - m)) + s.y * fast_exp2(s.x - m);
-        m_all = m;
-    }
-    const float over = sum == 0.f ? 0.f : 1.f / sum;
-    // Then the warp goes through the rows, piece by piece, a lane 8 columns of one member; JOIN (row, piece) at a time, whose
-    // loads are under way at once.
-    const int g = lane / (HD / 8), x = lane % (HD / 8);
-    const bool mine = g < ep.n_members;
-    int h = ep.heads[0];
-#pragma unroll
-    for (int i = 1; i < GM; ++i)
-        if (g == i) h = ep.heads[i];
-    const size_t column = (size_t)g * a.slot_rows * HD + x * 8;
-    __nv_bfloat16* to = out + ((size_t)(ep.row0 + quad * 32) * a.H + h) * HD + x * 8;
-    int r_load = 0, p_load = 0, r_use = 0, p_use = 0;
-    float o8[8] = {};
-#pragma unroll 1
-    for (int left = n_rows * pieces; left > 0; left -= JOIN) {
-        float4 v[JOIN][2];
-        float2 s[JOIN];
-#pragma unroll
-        for (int u = 0; u < JOIN; ++u) {
-            v[u][0] = v[u][1] = make_float4(0.f, 0.f, 0.f, 0.f);
-            s[u] = make_float2(0.f, 0.f);
-            if (u < left) {
-                const char* base = slot(p_load);
-                const int rw = quad * 32 + r_load;
-                s[u] = __ldcg(reinterpret_cast<const float2*>(base + stats) + rw);
-                if (mine) {
-                    const float4* src = reinterpret_cast<const float4*>(reinterpret_cast<const float*>(base) + column + (size_t)rw * HD);
-                    v[u][0] = __ldcg(src);
-                    v[u][1] = __ldcg(src + 1);
-                }
-            }
-            if (++p_load == pieces) p_load = 0, ++r_load;
-        }
-#pragma unroll
-        for (int u = 0; u < JOIN; ++u) {
-            const float m = __shfl_sync(0xffffffffu, m_all, r_use & 31), f = __shfl_sync(0xffffffffu, over, r_use & 31);
-            if (s[u].y != 0.f) {
-                const float w = fast_exp2(s[u].x - m);
-                o8[0] += w * v[u][0].x, o8[1] += w * v[u][0].y, o8[2] += w * v[u][0].z, o8[3] += w * v[u][0].w;
-                o8[4] += w * v[u][1].x, o8[5] += w * v[u][1].y, o8[6] += w * v[u][1].z, o8[7] += w * v[u][1].w;
-            }
-            if (++p_use == pieces) {
-                if (mine && u < left) {
-                    uint4 w;
-                    uint32_t* words = &w.x;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const __nv_bfloat162 pk = __floats2bfloat162_rn(o8[2 * i] * f, o8[2 * i + 1] * f);
-                        words[i] = *reinterpret_cast<const uint32_t*>(&pk);
-                    }
-                    *reinterpret_cast<uint4*>(to + (size_t)r_use * a.H * HD) = w;
-                }
-#pragma unroll
-                for (int i = 0; i < 8; ++i) o8[i] = 0.f;
-                p_use = 0;
-                ++r_use;
-            }
-        }
+    if (lane == 0) {  // (at the end of the CTA's work, by warps that have nothing else to do then)
+        const int which = ep.piece > 0 ? 0 : 1;
+        reinterpret_cast<Item*>(a.joins)[blockIdx.x * 2 + which] = ep;
+        atomicOr(reinterpret_cast<unsigned*>(smem + OFF_JOINS), 1u << (which * 4 + quad));
+        __threadfence_block();
     }
     return true;
+}
+
+// Joins the pieces that the CTA finished last, by the softmax warps: a warp takes ROWS rows of a quadrant at a time, a lane 8 columns
+// of one member (a row of both or all members is 1 KB), whose loads of one piece are under way at once.
+template <int HD>
+__device__ __forceinline__ void join_pieces(const PagedCall& a, const uint8_t* smem, int warp) {
+    constexpr int GM = HD == 128 ? 2 : 4, ROWS = 4;
+    const int lane = threadIdx.x & 31;
+    const unsigned todo = *reinterpret_cast<const volatile unsigned*>(smem + OFF_JOINS);
+    const size_t slot_bytes = (size_t)a.slot_rows * kSlotRowBytes, stats = (size_t)a.slot_rows * 1024;
+    const int g = lane / (HD / 8), x = lane % (HD / 8);
+#pragma unroll 1
+    for (int i = warp; i < 8 * (32 / ROWS); i += SOFTMAX_WARPS) {
+        const int bit = i / (32 / ROWS), row0 = (bit & 3) * 32 + i % (32 / ROWS) * ROWS;
+        if (!(todo >> bit & 1u)) continue;
+        const Item* ep = reinterpret_cast<const Item*>(a.joins) + blockIdx.x * 2 + (bit >> 2);
+        const int rows = ep->rows, pieces = ep->pieces, owner = ep->owner;
+        if (row0 >= rows) continue;
+        auto slot = [&](int piece) { return a.slots + (size_t)piece_slot(owner, piece) * slot_bytes; };
+        // A lane a piece: its share of every row, relative to the reference of all.
+        float share[ROWS];
+        float2 st[ROWS];
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) {
+            st[r] = make_float2(0.f, 0.f);
+            if (lane < pieces && row0 + r < rows) st[r] = __ldcg(reinterpret_cast<const float2*>(slot(lane) + stats) + row0 + r);
+        }
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) {
+            const bool sees = st[r].y != 0.f;  // (a piece that the row sees nothing of)
+            float m = sees ? st[r].x : -INFINITY;
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+            const float w = sees ? fast_exp2(st[r].x - m) : 0.f;
+            float sum = w * st[r].y;
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+            share[r] = sees ? w / sum : 0.f;
+        }
+        const bool mine = g < ep->n_members;
+        const float* from = reinterpret_cast<const float*>(slot(0)) + ((size_t)(mine ? g : 0) * a.slot_rows + row0) * HD + x * 8;
+        float o8[ROWS][8];
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r)
+#pragma unroll
+            for (int y = 0; y < 8; ++y) o8[r][y] = 0.f;
+#pragma unroll 2
+        for (int p = 0; p < pieces; ++p) {
+            const float* src = reinterpret_cast<const float*>(reinterpret_cast<const char*>(from) + (slot(p) - slot(0)));
+            float4 v[ROWS][2];
+#pragma unroll
+            for (int r = 0; r < ROWS; ++r) {
+                const int at = row0 + r < rows ? r : 0;
+                v[r][0] = __ldcg(reinterpret_cast<const float4*>(src + at * HD));
+                v[r][1] = __ldcg(reinterpret_cast<const float4*>(src + at * HD) + 1);
+            }
+#pragma unroll
+            for (int r = 0; r < ROWS; ++r) {
+                const float w = __shfl_sync(0xffffffffu, share[r], p);
+                if (w == 0.f) continue;  // (what such a piece holds is not a number it may be)
+                o8[r][0] += w * v[r][0].x, o8[r][1] += w * v[r][0].y, o8[r][2] += w * v[r][0].z, o8[r][3] += w * v[r][0].w;
+                o8[r][4] += w * v[r][1].x, o8[r][5] += w * v[r][1].y, o8[r][6] += w * v[r][1].z, o8[r][7] += w * v[r][1].w;
+            }
+        }
+        if (!mine) continue;
+        __nv_bfloat16* to = static_cast<__nv_bfloat16*>(a.out) + ((size_t)(ep->row0 + row0) * a.H + ep->heads[g]) * HD + x * 8;
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) {
+            uint4 w;
+            uint32_t* words = &w.x;
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+                const __nv_bfloat162 pk = __floats2bfloat162_rn(o8[r][2 * y], o8[r][2 * y + 1]);
+                words[y] = *reinterpret_cast<const uint32_t*>(&pk);
+            }
+            if (row0 + r < rows) *reinterpret_cast<uint4*>(to + (size_t)r * a.H * HD) = w;
+        }
+    }
 }
 
 template <int HD, bool FP8>
@@ -366,6 +382,7 @@ prefill_paged_kernel(const __grid_constant__ Tma maps, const __grid_constant__ P
             mbar_init(bar.raw_free(i), 8);  // (e4m3: R::CONVERT_WARPS)
         }
         *abort_flag = 0;
+        *reinterpret_cast<unsigned*>(smem + OFF_JOINS) = 0u;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         fence_async_proxy();
     }
@@ -786,10 +803,13 @@ prefill_paged_kernel(const __grid_constant__ Tma maps, const __grid_constant__ P
             if (lane == 0) mbar_arrive(bar.epi_full());
         }
         if (!ok) asm volatile("bar.arrive %0, 64;" ::"r"(quad + 1) : "memory");
+        asm volatile("bar.sync %0, %1;" ::"n"(JOIN_BARRIER), "n"(32 * (SOFTMAX_WARPS + EPILOGUE_WARPS)) : "memory");
+        if (!*abort_flag) join_pieces<HD>(a, smem, warp - R::SOFTMAX);
     } else if (warp >= R::EPILOGUE) {
         // ---------------- epilogue: one thread per query row ----------------
         if constexpr (!FP8) {
-            for (int ei = 0; finish_item<HD, 8>(a, smem, tmem_base, abort_flag, ei); ++ei) {}
+            for (int ei = 0; finish_item<HD>(a, smem, tmem_base, abort_flag, ei); ++ei) {}
+            asm volatile("bar.arrive %0, %1;" ::"n"(JOIN_BARRIER), "n"(32 * (SOFTMAX_WARPS + EPILOGUE_WARPS)) : "memory");
         } else {
             // e4m3: units become bf16 tiles, by eight warps; a thread takes 16 numbers of NV rows, a row at a time: there are no
             // registers for more, and what is spilled comes back from L2.  The first four warps write the item before
@@ -879,7 +899,7 @@ prefill_paged_kernel(const __grid_constant__ Tma maps, const __grid_constant__ P
                     if (j + 1 < n_kv) ok = put_k(j + 1);
                     if (!ok) break;
                     if (j == 0 && pending && writes_out) {
-                        ok = finish_item<HD, 4>(a, smem, tmem_base, abort_flag, ei++);
+                        ok = finish_item<HD>(a, smem, tmem_base, abort_flag, ei++);
                         if (!ok) break;
                     }
                     const int n = kt + j;
@@ -893,7 +913,8 @@ prefill_paged_kernel(const __grid_constant__ Tma maps, const __grid_constant__ P
                 kt += n_kv;
                 pending = true;
             }
-            if (ok && pending && writes_out) finish_item<HD, 4>(a, smem, tmem_base, abort_flag, ei);
+            if (ok && pending && writes_out) finish_item<HD>(a, smem, tmem_base, abort_flag, ei);
+            if (writes_out) asm volatile("bar.arrive %0, %1;" ::"n"(JOIN_BARRIER), "n"(32 * (SOFTMAX_WARPS + EPILOGUE_WARPS)) : "memory");
         }
     } else if constexpr (FP8) {
         // ---------------- row scales of the units, four rows a lane (of one page: page sizes are multiples of 8) ----------------
@@ -1092,6 +1113,7 @@ static int prefill_paged(const char* fn, bool fp8, PagedCall a, int n_pages, int
     char* ws = static_cast<char*>(workspace);
     a.hdr = reinterpret_cast<WsHeader*>(ws);
     a.done = reinterpret_cast<int*>(ws + L.off_done);
+    a.joins = ws + L.off_joins;
     a.req = reinterpret_cast<PagedRequest*>(ws + L.off_req);
     a.groups = reinterpret_cast<PagedGroup*>(ws + L.off_groups);
     a.slots = ws + L.off_slots;

@@ -46,14 +46,16 @@ constexpr size_t kSlotBytesPerToken = 640000;  // see chai_prefill_paged_workspa
 constexpr int kPagedMaxCtas = 300;             // (two partial results each)
 static_assert(2 * kPagedMaxCtas * kSlotRowBytes <= kSlotBytesPerToken, "partial results fit");
 constexpr int kPagedMaxPieces = 32;
+constexpr int kPagedJoinBytes = 64;            // what a CTA has to know of a query tile whose pieces it joins
 
 struct PagedLayout {
-    size_t off_done, off_req, off_groups, off_slots, total;
+    size_t off_done, off_joins, off_req, off_groups, off_slots, total;
 };
 inline PagedLayout paged_layout(int B, int H, int n_tokens) {
     PagedLayout L;
     L.off_done = sizeof(WsHeader);
-    L.off_req = round_up(L.off_done + sizeof(int) * kPagedMaxCtas, 256);
+    L.off_joins = round_up(L.off_done + sizeof(int) * kPagedMaxCtas, 256);
+    L.off_req = round_up(L.off_joins + 2 * kPagedJoinBytes * (size_t)kPagedMaxCtas, 256);
     L.off_groups = round_up(L.off_req + sizeof(PagedRequest) * (size_t)B, 256);
     L.off_slots = round_up(L.off_groups + sizeof(PagedGroup) * (size_t)B * H, 256);
     L.total = L.off_slots + 2 * (size_t)kPagedMaxCtas * kSlotRowBytes * ((n_tokens < 128 ? n_tokens + 1 : 128) & ~1);
@@ -69,6 +71,7 @@ struct PagedCall {
     PagePool pool;
     WsHeader* hdr;
     int* done;              // [ctas] pieces that are finished of the query tile that a CTA's share ends in
+    char* joins;            // [ctas][2] query tiles whose last piece the CTA finished (tensor cores)
     PagedRequest* req;
     PagedGroup* groups;
     char* slots;            // [2 ctas] partial results
