@@ -263,7 +263,7 @@ __device__ __forceinline__ bool finish_item(const PagedCall& a, uint8_t* smem, u
 }
 
 // Joins the pieces that the CTA finished last, by the softmax warps: a warp takes ROWS rows of a quadrant at a time, a lane 8 columns
-// of one member (a row of both or all members is 1 KB), whose loads of one piece are under way at once.
+// of one member (a row of both or all members is 1 KB), whose loads of the next piece are under way meanwhile.
 template <int HD>
 __device__ __forceinline__ void join_pieces(const PagedCall& a, const uint8_t* smem, int warp) {
     constexpr int GM = HD == 128 ? 2 : 4, ROWS = 4;
@@ -279,6 +279,18 @@ __device__ __forceinline__ void join_pieces(const PagedCall& a, const uint8_t* s
         const int rows = ep->rows, pieces = ep->pieces, owner = ep->owner;
         if (row0 >= rows) continue;
         auto slot = [&](int piece) { return a.slots + (size_t)piece_slot(owner, piece) * slot_bytes; };
+        const bool mine = g < ep->n_members;
+        const size_t offset = (((size_t)(mine ? g : 0) * a.slot_rows + row0) * HD + x * 8) * 4;
+        float4 v[ROWS][2];
+        auto load = [&](int p) {
+            const float* src = reinterpret_cast<const float*>(slot(p) + offset);
+#pragma unroll
+            for (int r = 0; r < ROWS; ++r) {
+                const int at = row0 + r < rows ? r : 0;
+                v[r][0] = __ldcg(reinterpret_cast<const float4*>(src + at * HD));
+                v[r][1] = __ldcg(reinterpret_cast<const float4*>(src + at * HD) + 1);
+            }
+        };
         // A lane a piece: its share of every row, relative to the reference of all.
         float share[ROWS];
         float2 st[ROWS];
@@ -287,6 +299,7 @@ __device__ __forceinline__ void join_pieces(const PagedCall& a, const uint8_t* s
             st[r] = make_float2(0.f, 0.f);
             if (lane < pieces && row0 + r < rows) st[r] = __ldcg(reinterpret_cast<const float2*>(slot(lane) + stats) + row0 + r);
         }
+        load(0);  // (on its way meanwhile)
 #pragma unroll
         for (int r = 0; r < ROWS; ++r) {
             const bool sees = st[r].y != 0.f;  // (a piece that the row sees nothing of)
@@ -299,29 +312,23 @@ __device__ __forceinline__ void join_pieces(const PagedCall& a, const uint8_t* s
             for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
             share[r] = sees ? w / sum : 0.f;
         }
-        const bool mine = g < ep->n_members;
-        const float* from = reinterpret_cast<const float*>(slot(0)) + ((size_t)(mine ? g : 0) * a.slot_rows + row0) * HD + x * 8;
         float o8[ROWS][8];
 #pragma unroll
         for (int r = 0; r < ROWS; ++r)
 #pragma unroll
             for (int y = 0; y < 8; ++y) o8[r][y] = 0.f;
-#pragma unroll 2
+#pragma unroll 1
         for (int p = 0; p < pieces; ++p) {
-            const float* src = reinterpret_cast<const float*>(reinterpret_cast<const char*>(from) + (slot(p) - slot(0)));
-            float4 v[ROWS][2];
+            float4 u[ROWS][2];
 #pragma unroll
-            for (int r = 0; r < ROWS; ++r) {
-                const int at = row0 + r < rows ? r : 0;
-                v[r][0] = __ldcg(reinterpret_cast<const float4*>(src + at * HD));
-                v[r][1] = __ldcg(reinterpret_cast<const float4*>(src + at * HD) + 1);
-            }
+            for (int r = 0; r < ROWS; ++r) u[r][0] = v[r][0], u[r][1] = v[r][1];
+            if (p + 1 < pieces) load(p + 1);
 #pragma unroll
             for (int r = 0; r < ROWS; ++r) {
                 const float w = __shfl_sync(0xffffffffu, share[r], p);
                 if (w == 0.f) continue;  // (what such a piece holds is not a number it may be)
-                o8[r][0] += w * v[r][0].x, o8[r][1] += w * v[r][0].y, o8[r][2] += w * v[r][0].z, o8[r][3] += w * v[r][0].w;
-                o8[r][4] += w * v[r][1].x, o8[r][5] += w * v[r][1].y, o8[r][6] += w * v[r][1].z, o8[r][7] += w * v[r][1].w;
+                o8[r][0] += w * u[r][0].x, o8[r][1] += w * u[r][0].y, o8[r][2] += w * u[r][0].z, o8[r][3] += w * u[r][0].w;
+                o8[r][4] += w * u[r][1].x, o8[r][5] += w * u[r][1].y, o8[r][6] += w * u[r][1].z, o8[r][7] += w * u[r][1].w;
             }
         }
         if (!mine) continue;
