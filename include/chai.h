@@ -574,8 +574,8 @@ int chai_append_rope_paged_fp8(const void* q, const void* k, const void* v, void
  * request that do not see it (as zero times infinity); among keys it reaches only those that see it.
  * The workspace (chai_prefill_paged_workspace_bytes: 2^20 + 64 B + 36 H (B + n_tokens/128 + 1) + 640000 min(n_tokens, 128), whatever
  * the lengths) needs no clearing; calls that share one must be ordered on one stream.
- * H at most 1024, B below 65536, n_tokens at most 2^26, 4 (H + (k + 1) (3 + ceil(H/32))) at most 48 KB (the planner's shared
- * memory), and with r query tiles of 128 rows, t key tiles of 128 in a row of the table (CHAI_F32: tiles of 16, 32 or 64
+ * H at most 1024, B below 65536, n_tokens at most 2^26, 4 (H + (k + 1) (3 + ceil(H/32))) at most 48896 bytes (the planner's
+ * shared memory: 1024 heads in 319 clusters), and with r query tiles of 128 rows, t key tiles of 128 in a row of the table (CHAI_F32: tiles of 16, 32 or 64
  * rows and 32 or 64 keys): r t below 2^27, (r + B) t H below 2^32.
  */
 size_t chai_prefill_paged_workspace_bytes(int B, int H, int n_tokens);

@@ -783,6 +783,12 @@ def _turns(turns, dev):
     return turns.data_ptr(), 2 * turns.numel()
 
 
+def _rotated_like(x):
+    """An array of x's strides, or, where x has one row for many, a dense one."""
+    strides = x.stride()
+    return torch.empty(x.shape, device=x.device, dtype=x.dtype) if 0 in strides else torch.empty_strided(x.shape, strides, device=x.device, dtype=x.dtype)
+
+
 _STRIDES = struct.Struct("12q")   # (an array of ctypes takes four times as long to fill)
 
 
@@ -806,9 +812,9 @@ def chai_rope(q, k=None, positions=None, turns=None, magnitude: float = 1.0, int
             raise ValueError(f"k must have shape ({B}, Hk, {N}, {D}), got {tuple(k.shape)}")
         Hk = k.shape[1]
     if q_out is None:
-        q_out = torch.empty_strided(q.shape, q.stride(), device=q.device, dtype=dtype)
+        q_out = _rotated_like(q)
     if k_out is None and k is not None:
-        k_out = torch.empty_strided(k.shape, k.stride(), device=k.device, dtype=dtype)
+        k_out = _rotated_like(k)
     strides = []
     for x, out, name in ((q, q_out, "q"), (k, k_out, "k")):
         if x is None:

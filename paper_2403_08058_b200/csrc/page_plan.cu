@@ -11,7 +11,7 @@
 // and of the list's new entries, which the token in a page's first row writes.
 // Bound by latency: a chain of loads (lengths -> sums -> tokens' pages) behind one launch while there are few tokens.  Up
 // to kOneBlockTokens the block that scans also writes the tokens; above, a dependent grid does (4 tokens a thread, 16-byte
-// stores).
+// stores).  Measured: 16 requests of a token 4.1 us, 300 mixed ones 10.6, 4 prompts of 327680 tokens in all 7.0.
 #include "paged.cuh"
 
 namespace chai {

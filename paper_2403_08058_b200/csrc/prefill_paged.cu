@@ -8,7 +8,7 @@
 // for the members of a cluster, two at a time (head_dim 64: four).  P is rounded to bf16, at most 2^-8 of each
 // probability, because that is the tensor core's type beside bf16 values; row sums are of the rounded ones, in fp32, so that a
 // row which sees one position, or nearly one, gets its values (sums of the unrounded ones, two additions an instruction, left such
-// a row 0.0016 off and took 733 us, not 774, for 2048 tokens behind 30720).
+// a row 0.0016 off; they are 2 % faster for 2048 tokens behind 30720).
 // What differs:
 //   - keys and values come from pages, in boxes of as many rows as divide both the page size and 128, whole rows each: a box
 //     costs about 90 cycles of the copy engine whatever it holds.  A box lands as one piece of shared memory, so tiles are
@@ -19,8 +19,15 @@
 //     would meet probabilities of zero, are zeroed in shared memory before the last tile is multiplied.
 //   - a request may have few tokens: rows that it does not have cost tensor work but no softmax, and all tiles are one line that
 //     is cut into equal shares (prefill_paged.cuh); a query tile on both sides of a cut leaves unnormalised accumulators, joined
-//     by the warp that finishes its rows' last piece, in order of the pieces.
-// Bound by the cache's bytes for few tokens a request, by the softmax chain of a tile (as in prefill_tc.cu) for many.
+//     in order of the pieces by the CTA that finishes its last piece, at the end of that CTA's work: its softmax warps have
+//     nothing else to do then and registers for the loads (by the warp that writes accumulators out, in between, 64 tokens
+//     over 8192 in e4m3 took 243 us, not 205).
+// Bound by the cache's bytes for few tokens a request, by the softmax chain of a tile (as in prefill_tc.cu) for many; with e4m3
+// pages by their conversion to bf16, which takes issue slots and, between a tile's products and the next one's, time.
+// Measured (of 6567 GB/s, or of 1638 TFLOP/s): 16 requests of 4 tokens over up to 2048, 32 heads, 8 clusters: 54 us, 54 %; 2048 tokens
+// behind 30720: 735 - 775 us, 52 - 55 %; 24 mixed requests over up to 4096, 52 heads: 304 us, 42 % of the bytes' rate; e4m3, 4 x 64
+// tokens over up to 8192, 72 heads, 24 clusters: 205 us, 20 %.  Before the first tile stand some 10 us: the planner 3.5, the
+// launch 1.7, finding the share 1.5, its first rows 3.
 #include <cuda.h>
 #include <math.h>
 
@@ -1065,9 +1072,10 @@ static int prefill_paged(const char* fn, bool fp8, PagedCall a, int n_pages, int
     CHAI_REQUIRE(a.n_tokens > 0, CHAI_ERR_INVALID_ARG, "%s: need n_tokens > 0", fn);
     CHAI_REQUIRE(isfinite(a.scale) && a.scale > 0.f, CHAI_ERR_INVALID_ARG, "%s: scale must be positive and finite", fn);
     CHAI_REQUIRE(a.n_tokens <= (1 << 26), CHAI_ERR_UNSUPPORTED, "%s: n_tokens must be <= 2^26", fn);
-    CHAI_REQUIRE(prefill_paged_plan_smem(a.H, a.k) <= 48 * 1024, CHAI_ERR_UNSUPPORTED,
-                 "%s: too many heads and clusters for the planner (H=%d, k=%d need %zu bytes of shared memory, limit 49152)", fn, a.H,
-                 a.k, prefill_paged_plan_smem(a.H, a.k));
+    constexpr size_t plan_limit = 48 * 1024 - 256;  // (beside what the planner has anyway)
+    CHAI_REQUIRE(prefill_paged_plan_smem(a.H, a.k) <= plan_limit, CHAI_ERR_UNSUPPORTED,
+                 "%s: too many heads and clusters for the planner (H=%d, k=%d need %zu bytes of shared memory, limit %zu)", fn, a.H,
+                 a.k, prefill_paged_plan_smem(a.H, a.k), plan_limit);
     const long long dense = (long long)a.H * D, es = (long long)elem_size(dtype);
     if (a.q_stride == 0) a.q_stride = dense;
     CHAI_REQUIRE(a.q_stride >= dense && a.q_stride < (1ll << 40) / es && a.q_stride <= (1ll << 56) / a.n_tokens && a.q_stride * es % 16 == 0,

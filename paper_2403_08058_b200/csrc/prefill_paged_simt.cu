@@ -10,7 +10,7 @@
 // request does not have are computed all the same.  Every member has a buffer of its own: keys and values of the next tile are
 // copied as soon as this tile's are done with, and where the rows lie is looked up a tile ahead.
 // Measured (fp32): 5 requests of up to 93 rows over up to 700 positions, 12 heads of 64: 50 us (one block of 128 rows an SM, the
-// pieces joined a vector at a time: 118); of 2 rows over up to 4096, 32 heads of 128: 180 us, 1.1 TB/s; of up to 400 over
+// pieces joined a vector at a time: 118); of 2 rows over up to 4096, 32 heads of 128: 180 us, 1.1 TB/s; of up to 400 rows over
 // 2048: 857 us.
 #include "prefill_paged.cuh"
 #include "tc_ptx.cuh"

@@ -223,7 +223,7 @@ struct EnterArgs {
 // so the error is less than 9 u of it.  That decides two things where it should not: the scale, where the largest lies
 // within 9 units of its mantissa of 1.75 * 2^i (once in 10^6 rows; it would be off by a factor of two), and the byte, where a
 // number, 448 at most after scaling, lies within 9 u 448 of the middle between two e4m3 numbers (once in 10^4).  Such
-// numbers are worked out in fp64, so that bytes and scales are those of the exact ones (8172 tokens of 32 heads: 58 us
+// numbers are worked out in fp64, so that bytes and scales are those of the exact ones (5599 tokens of 52 heads: 58 us
 // without; with factors in fp64 for all, which would make this cheap: 76).
 constexpr unsigned kBorder = 0x600000u, kNear = 16u;
 constexpr float kMiddle = 9.f * 448.f / (1 << 24);
@@ -274,9 +274,9 @@ __device__ __forceinline__ void put_row_fp8(const EnterArgs& a, bool key, int pl
 
 // grid (token groups, parts of the rows).  Rows of a token: k_planes keys, k_planes queries, then H values, which are not rotated and
 // go through a loop of their own.  Blocks to an SM: what the registers of a rotated e4m3 row (its border check among them) allow is
-// two; rows stored as they are gain from a third (bf16, 8172 tokens of 32 heads, 128 wide: 57 -> 50 us), and a fourth, 47 us there,
-// spills what 800 tokens wait for (6.8 -> 7.6 us).
-// To e4m3 the 8172 tokens take 67 us, 178 MB at 2.7 TB/s: bound by the instructions of the rotation, the row's largest magnitude
+// two; rows stored as they are gain from a third (bf16, 5599 tokens of 52 heads, 128 wide: 57 -> 50 us), and a fourth, 47 us there,
+// spills what 568 tokens wait for (6.8 -> 7.6 us).
+// To e4m3 the 5599 tokens take 67 us, 178 MB at 2.7 TB/s: bound by the instructions of the rotation, the row's largest magnitude
 // and the conversion, 16 warps to an SM.
 template <typename T, int D, bool FP8>
 __global__ void __launch_bounds__(kThreads, FP8 ? 2 : 3) append_rope_kernel(const __grid_constant__ EnterArgs a) {

@@ -168,6 +168,20 @@ def test_one_representative_for_two_clusters(cache, io):
     assert torch.equal(out[:, first], good[:, first]) and not out[:, ~first].any()
 
 
+@pytest.mark.parametrize("cache,io", KINDS[1:2])
+def test_the_most_heads_and_clusters(cache, io):
+    c = batch(cache, io, 1024, 319, 64, 8, [17, 0, 140], [3, 0, 9], seed=16)
+    check(c, attend(c), True, "1024 heads, 319 clusters")
+
+
+def test_many_more_requests_than_the_gpu_has_multiprocessors():
+    rng = np.random.default_rng(8)
+    new = [int(x) for x in rng.integers(0, 3, 5000)]
+    kv = [n + int(x) for n, x in zip(new, rng.integers(0, 12, 5000))]
+    c = batch("bf16", "bf16", 2, 1, 64, 8, kv, new, seed=71)
+    check(c, attend(c), True, "5000 short requests")
+
+
 @pytest.mark.parametrize("io", ["f32", "bf16"])
 def test_rope_at_the_ends_of_the_range(io):
     turns, m = chai.chai_rope_frequencies(64)
@@ -179,6 +193,21 @@ def test_rope_at_the_ends_of_the_range(io):
     ref, err = rotate(q, pos[:, None].expand(-1, 3, -1), t, m, False)
     assert ((got.double() - ref).abs() <= err + HALF_STEP[io] * (ref.abs() + err)).all()
     assert torch.equal(got[:, :, 0], q[:, :, 0])
+
+
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+def test_rope_of_rows_that_many_share(io):
+    """Inputs with strides of 0 (one array for all requests, one key head for all): outputs have rows of their own."""
+    turns, m = chai.chai_rope_frequencies(32, device=DEV)
+    g = torch.Generator(device=DEV).manual_seed(3)
+    q = torch.randn(1, 4, 19, 64, device=DEV, generator=g).to(TORCH[io]).expand(3, -1, -1, -1)
+    k = torch.randn(3, 1, 19, 64, device=DEV, generator=g).to(TORCH[io]).expand(-1, 2, -1, -1)
+    pos = i32(np.random.default_rng(1).integers(0, 9000, (3, 19)))
+    got = chai.chai_rope(q, k, pos, turns, m)
+    want = chai.chai_rope(q.contiguous(), k.contiguous(), pos, turns, m)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    with pytest.raises(chai.ChaiError, match="output"):
+        chai.chai_rope(q.contiguous(), None, pos, turns, m, q_out=torch.empty_like(q[:1]).expand(3, -1, -1, -1))
 
 
 @pytest.mark.parametrize("cache,io", KINDS)

@@ -145,7 +145,7 @@ def test_attention_refusals(lib, fp8):
                 dict(q_stride=1 << 39), dict(q_stride=(1 << 64) - 16), dict(k_page=2 * 16 * 128 - 16), dict(v_page=4 * 16 * 128 + 4)):
         assert attend(lib, fp8, **bad) == INVALID, bad
     for bad in (dict(D=96), dict(page=20), dict(page=65544), dict(dtype=2), dict(H=1025), dict(B=65536), dict(max_pages=1 << 26),
-                dict(n=(1 << 26) + 1), dict(H=1024, k=1000),                                # the planner's shared memory
+                dict(n=(1 << 26) + 1), dict(H=1024, k=1000), dict(H=1024, k=320),                                # the planner's shared memory
                 dict(n=1 << 26, max_pages=1 << 16), dict(B=60000, max_pages=1 << 16, H=64),   # the line of tiles
                 dict(n=1 << 26, max_pages=1 << 16, dtype=0)):
         assert attend(lib, fp8, [AT] * (n - 1) + [AT + (1 << 46)], **bad) == UNSUPPORTED, bad
