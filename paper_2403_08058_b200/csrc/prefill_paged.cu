@@ -25,8 +25,9 @@
 // Bound by the cache's bytes for few tokens a request, by the softmax chain of a tile (as in prefill_tc.cu) for many; with e4m3
 // pages by their conversion to bf16, which takes issue slots and, between a tile's products and the next one's, time.
 // Measured (of 6567 GB/s, or of 1638 TFLOP/s): 16 requests of 4 tokens over up to 2048, 32 heads, 8 clusters: 54 us, 54 %; 2048 tokens
-// behind 30720: 735 - 775 us, 52 - 55 %; 24 mixed requests over up to 4096, 52 heads: 304 us, 42 % of the bytes' rate; e4m3, 4 x 64
-// tokens over up to 8192, 72 heads, 24 clusters: 205 us, 20 %.  Before the first tile stand some 10 us: the planner 3.5, the
+// behind 30720: 735 - 800 us, 51 - 55 %; 24 mixed requests over up to 4096, 52 heads: 300 us, 43 % (the chunks' query tiles read their rows
+// again, after they have left L2: 1.7 GB at 5.9 TB/s, where 0.80 would do); e4m3, 4 x 64 tokens over up to 8192, 72 heads, 24
+// clusters: 205 us, 20 %.  Before the first tile stand some 10 us: the planner 3.5, the
 // launch 1.7, finding the share 1.5, its first rows 3.
 #include <cuda.h>
 #include <math.h>
@@ -273,7 +274,7 @@ __device__ __forceinline__ bool finish_item(const PagedCall& a, uint8_t* smem, u
 // of one member (a row of both or all members is 1 KB), whose loads of the next piece are under way meanwhile.
 template <int HD>
 __device__ __forceinline__ void join_pieces(const PagedCall& a, const uint8_t* smem, int warp) {
-    constexpr int GM = HD == 128 ? 2 : 4, ROWS = 4;
+    constexpr int ROWS = 4;
     const int lane = threadIdx.x & 31;
     const unsigned todo = *reinterpret_cast<const volatile unsigned*>(smem + OFF_JOINS);
     const size_t slot_bytes = (size_t)a.slot_rows * kSlotRowBytes, stats = (size_t)a.slot_rows * 1024;
