@@ -11,8 +11,8 @@
 // CTAs that walk the same keys for different query tiles should meet them at the same time, while they are in L2: a CTA
 // that has done t tiles begins a whole query tile at key tile t modulo its count and wraps around, and of a divided one the
 // share that begins it, late in that CTA's time, takes the last key tiles.
-// All of this stands in front of the first tile, mostly as code that runs once and has to be fetched: it is kept short
-// (one warp, no block-wide barriers, 32-bit distances from the share's beginning).
+// All of this stands in front of the first tile, mostly as code that runs once and has to be fetched: it is kept short (a share is
+// found by one warp, without block-wide barriers, in 32-bit distances from its beginning).
 #pragma once
 
 #include "paged.cuh"
