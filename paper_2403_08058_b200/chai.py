@@ -844,7 +844,11 @@ def _tokens(t, name, shape, dtype, dev) -> int:
     apart, heads, one = t.stride()
     if t.get_device() != dev or one != 1 or (heads != shape[2] and shape[1] > 1):
         raise ValueError(f"{name} must be on cuda:{dev}, the heads of a token side by side")
-    return apart if shape[0] > 1 else 0
+    if shape[0] <= 1:
+        return 0
+    if apart < shape[1] * shape[2]:   # (0, one row for many tokens, would be taken for "side by side")
+        raise ValueError(f"{name} must have rows of its own for every token, got a token stride of {apart}")
+    return apart
 
 
 def _append_rope(fn_name, q, k, v, k_pages, v_pages, k_scales, v_scales, reps, token_request, positions, slots, turns,
