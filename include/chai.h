@@ -569,8 +569,9 @@ int chai_append_rope_paged_fp8(const void* q, const void* k, const void* v, void
  *   kv_lens [B], token_start [B+1] int32, device (clamped to [0, max_pages*page_size] and [0, n_tokens])
  * Types, refusals and what inconsistent memberships and bad pages lead to are as for chai_decode_attention_paged; scale must be
  * positive and finite.  CHAI_BF16 runs on the tensor cores, with probabilities rounded to bf16 and e4m3 rows as the bf16
- * numbers that they stand for; CHAI_F32 on the CUDA cores.  Sums and statistics are fp32.  Rows at or beyond kv_lens[b] are never
- * used, whatever they hold.  An infinity or NaN among the cached values below kv_lens[b] may also reach tokens of its
+ * numbers that they stand for, for scores (scale q . K) below 2^26 and values below 2^60 in magnitude (the exponentials'
+ * reference lies up to 2^32 below a row's largest; larger numbers may leave fp32's range); CHAI_F32 on the CUDA cores.  Sums and
+ * statistics are fp32.  Rows at or beyond kv_lens[b] are never used, whatever they hold.  An infinity or NaN among the cached values below kv_lens[b] may also reach tokens of its
  * request that do not see it (as zero times infinity); among keys it reaches only those that see it.
  * The workspace (chai_prefill_paged_workspace_bytes: 2^20 + 64 B + 36 H (B + n_tokens/128 + 1) + 640000 min(n_tokens, 128), whatever
  * the lengths) needs no clearing; calls that share one must be ordered on one stream.

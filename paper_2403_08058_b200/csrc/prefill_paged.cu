@@ -652,7 +652,8 @@ prefill_paged_kernel(const __grid_constant__ Tma maps, const __grid_constant__ P
         const int quad = warp & 3, half = (warp - R::SOFTMAX) >> 2;
         const int row = quad * 32 + lane, cbase = half * 64;
         const uint32_t lane_addr = tmem_base + ((uint32_t)(quad * 32) << 16);
-        __nv_bfloat16* xch = reinterpret_cast<__nv_bfloat16*>(smem + OFF_XCH);  // [tile parity][half][row]
+        // row maxima: bf16 [half][row][tile parity], or fp32 [half][row]
+        const uint32_t xch = sbase + OFF_XCH + (half * BM + row) * 4, xch_other = sbase + OFF_XCH + ((half ^ 1) * BM + row) * 4;
         float* lsum = reinterpret_cast<float*>(smem + OFF_LSUM);
         float* refs = reinterpret_cast<float*>(smem + OFF_REF);
         bool ok = true;
@@ -718,28 +719,15 @@ prefill_paged_kernel(const __grid_constant__ Tma maps, const __grid_constant__ P
                 float mxa[8];
 #pragma unroll
                 for (int c = 0; c < 8; ++c) mxa[c] = -INFINITY;
-                __nv_bfloat16 mx_up;
-                __nv_bfloat16* xs = xch + (kt & 1) * 2 * BM;
                 auto publish = [&]() {
-                    mx_up = __float2bfloat16_ru(max3(max3(mxa[0], mxa[1], mxa[2]), max3(mxa[3], mxa[4], mxa[5]), fmaxf(mxa[6], mxa[7])));
-                    xs[half * BM + row] = mx_up;
+                    st_shared_bf16(xch + (kt & 1) * 2, __float2bfloat16_ru(max3(max3(mxa[0], mxa[1], mxa[2]), max3(mxa[3], mxa[4], mxa[5]), fmaxf(mxa[6], mxa[7]))));
                 };
-                float m_new = m_used, corr = 1.f;
-                auto meet = [&]() -> bool {
+                auto together = [&]() -> bool {
                     // (the two warps of a quadrant; whoever gives up arrives once on its way out)
                     asm volatile("bar.sync %0, 64;" ::"r"(quad + 1) : "memory");
-                    if (*abort_flag) return false;
-                    const float mx = fmaxf(__bfloat162float(mx_up), __bfloat162float(xs[(half ^ 1) * BM + row]));
-                    const float m_tile = mx * scale_log2;
-                    if (m_tile > -INFINITY) {
-                        if (m_tile > m_used + REF_WINDOW || (fresh && m_tile < m_used - REF_WINDOW)) {
-                            m_new = m_tile;
-                            corr = fresh ? 1.f : fast_exp2(m_used - m_new);  // (nothing has been accumulated yet)
-                        }
-                        fresh = false;
-                    }
-                    return true;
+                    return !*abort_flag;
                 };
+                auto leaves = [&](float m) { return m > m_used + REF_WINDOW || (fresh && m > -INFINITY && m < m_used - REF_WINDOW); };
                 auto emit = [&](float m, auto with_max) -> float {
                     const uint64_t sc2 = pack2(scale_log2, scale_log2), nm2 = pack2(-m, -m);
                     float l0 = 0.f, l1 = 0.f, l2 = 0.f, l3 = 0.f;  // of the rounded probabilities
@@ -774,12 +762,36 @@ prefill_paged_kernel(const __grid_constant__ Tma maps, const __grid_constant__ P
                 }
                 float ls = emit(m_used, std::true_type{});
                 publish();
-                ok = meet();
+                ok = together();
                 if (!ok) break;
-                const bool moved = __any_sync(0xffffffffu, m_new != m_used);
-                if (moved) ls = emit(m_new, std::false_type{});
+                // The maximum rounded up to bf16 says whether a reference may move, the one in fp32 where to: scores of thousands
+                // would otherwise lie further below a reference that is 2^-7 too large than exponentials reach.  (Both warps
+                // see the same numbers and decide alike.  The fp32 maximum is taken again, for nothing is free to hold it.)
+                float m_tile = fmaxf(__bfloat162float(ld_shared_bf16(xch + (kt & 1) * 2)), __bfloat162float(ld_shared_bf16(xch_other + (kt & 1) * 2))) * scale_log2;
+                float corr = 1.f;
+                bool moved = __any_sync(0xffffffffu, leaves(m_tile));
+                if (moved) {
+                    ok = together();  // (both have read)
+                    if (!ok) break;
+                    float mx = -INFINITY;
+#pragma unroll
+                    for (int i = 0; i < 64; ++i) mx = fmaxf(mx, __uint_as_float(r[i]));
+                    st_shared_f32(xch, mx);
+                    ok = together();
+                    if (!ok) break;
+                    m_tile = fmaxf(mx, ld_shared_f32(xch_other)) * scale_log2;
+                    ok = together();  // (the next tile writes there)
+                    if (!ok) break;
+                    const float m_old = m_used;
+                    if (leaves(m_tile)) {
+                        corr = fresh ? 1.f : fast_exp2(m_used - m_tile);  // (nothing has been accumulated yet)
+                        m_used = m_tile;
+                    }
+                    moved = __any_sync(0xffffffffu, m_used != m_old);
+                    if (moved) ls = emit(m_used, std::false_type{});
+                }
+                if (m_tile > -INFINITY) fresh = false;
                 l_run = l_run * corr + ls;
-                m_used = m_new;
                 if (j > 0 && moved) {
                     ok = __all_sync(0xffffffffu, mbar_wait(bar.pv_done((kt - 1) & 1), ((kt - 1) >> 1) & 1, abort_flag));
                     if (!ok) break;
