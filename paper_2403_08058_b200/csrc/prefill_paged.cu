@@ -65,7 +65,7 @@ __device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.
 template <int N>
 __device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
 constexpr int JOIN_BARRIER = 5;  // (1 - 4: the quadrants' pairs of softmax warps)
-constexpr float REF_WINDOW = 32.f;
+constexpr float REF_WINDOW = 32.f, EXACT_FROM = 2048.f;  // log2
 constexpr uint32_t TMEM_COLS = 512;
 constexpr uint32_t S_COL0 = 0, P_COL0 = 128, O_COL0 = 256;
 
@@ -653,7 +653,8 @@ prefill_paged_kernel(const __grid_constant__ Tma maps, const __grid_constant__ P
         const int row = quad * 32 + lane, cbase = half * 64;
         const uint32_t lane_addr = tmem_base + ((uint32_t)(quad * 32) << 16);
         // row maxima: bf16 [half][row][tile parity], or fp32 [half][row]
-        const uint32_t xch = sbase + OFF_XCH + (half * BM + row) * 4, xch_other = sbase + OFF_XCH + ((half ^ 1) * BM + row) * 4;
+        uint8_t* const xch = smem + OFF_XCH + (half * BM + row) * 4;
+        const uint8_t* const xch_other = smem + OFF_XCH + ((half ^ 1) * BM + row) * 4;
         float* lsum = reinterpret_cast<float*>(smem + OFF_LSUM);
         float* refs = reinterpret_cast<float*>(smem + OFF_REF);
         bool ok = true;
@@ -720,7 +721,7 @@ prefill_paged_kernel(const __grid_constant__ Tma maps, const __grid_constant__ P
 #pragma unroll
                 for (int c = 0; c < 8; ++c) mxa[c] = -INFINITY;
                 auto publish = [&]() {
-                    st_shared_bf16(xch + (kt & 1) * 2, __float2bfloat16_ru(max3(max3(mxa[0], mxa[1], mxa[2]), max3(mxa[3], mxa[4], mxa[5]), fmaxf(mxa[6], mxa[7]))));
+                    *reinterpret_cast<__nv_bfloat16*>(xch + (kt & 1) * 2) = __float2bfloat16_ru(max3(max3(mxa[0], mxa[1], mxa[2]), max3(mxa[3], mxa[4], mxa[5]), fmaxf(mxa[6], mxa[7])));
                 };
                 auto together = [&]() -> bool {
                     // (the two warps of a quadrant; whoever gives up arrives once on its way out)
@@ -764,24 +765,27 @@ prefill_paged_kernel(const __grid_constant__ Tma maps, const __grid_constant__ P
                 publish();
                 ok = together();
                 if (!ok) break;
-                // The maximum rounded up to bf16 says whether a reference may move, the one in fp32 where to: scores of thousands
-                // would otherwise lie further below a reference that is 2^-7 too large than exponentials reach.  (Both warps
-                // see the same numbers and decide alike.  The fp32 maximum is taken again, for nothing is free to hold it.)
-                float m_tile = fmaxf(__bfloat162float(ld_shared_bf16(xch + (kt & 1) * 2)), __bfloat162float(ld_shared_bf16(xch_other + (kt & 1) * 2))) * scale_log2;
+                // The maximum rounded up to bf16 says whether a reference may move.  It is less than 2^-7 of itself too large: up
+                // to EXACT_FROM that is less than 16 binary orders, and as good a reference; beyond, rows would lie further below
+                // it than exponentials reach, and the two warps exchange the maximum in fp32.  (They see the same numbers and
+                // decide alike.  The fp32 maximum is taken again, for nothing is free to hold it.)
+                float m_tile = fmaxf(__bfloat162float(*reinterpret_cast<const __nv_bfloat16*>(xch + (kt & 1) * 2)), __bfloat162float(*reinterpret_cast<const __nv_bfloat16*>(xch_other + (kt & 1) * 2))) * scale_log2;
                 float corr = 1.f;
                 bool moved = __any_sync(0xffffffffu, leaves(m_tile));
                 if (moved) {
-                    ok = together();  // (both have read)
-                    if (!ok) break;
-                    float mx = -INFINITY;
+                    if (__any_sync(0xffffffffu, fabsf(m_tile) > EXACT_FROM)) {
+                        ok = together();  // (both have read)
+                        if (!ok) break;
+                        float mx = -INFINITY;
 #pragma unroll
-                    for (int i = 0; i < 64; ++i) mx = fmaxf(mx, __uint_as_float(r[i]));
-                    st_shared_f32(xch, mx);
-                    ok = together();
-                    if (!ok) break;
-                    m_tile = fmaxf(mx, ld_shared_f32(xch_other)) * scale_log2;
-                    ok = together();  // (the next tile writes there)
-                    if (!ok) break;
+                        for (int i = 0; i < 64; ++i) mx = fmaxf(mx, __uint_as_float(r[i]));
+                        *reinterpret_cast<float*>(xch) = mx;
+                        ok = together();
+                        if (!ok) break;
+                        if (fabsf(m_tile) > EXACT_FROM) m_tile = fmaxf(mx, *reinterpret_cast<const float*>(xch_other)) * scale_log2;  // (a row's reference follows from its own scores)
+                        ok = together();  // (the next tile writes there)
+                        if (!ok) break;
+                    }
                     const float m_old = m_used;
                     if (leaves(m_tile)) {
                         corr = fresh ? 1.f : fast_exp2(m_used - m_tile);  // (nothing has been accumulated yet)

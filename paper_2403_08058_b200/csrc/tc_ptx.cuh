@@ -111,21 +111,6 @@ __device__ __forceinline__ void tma_prefetch_4d(const CUtensorMap* map, int row,
 __device__ __forceinline__ void st_shared16(uint32_t at, const uint32_t* w) {
     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]));
 }
-// single numbers at a shared address (32 bits of it, where a generic pointer takes two registers)
-__device__ __forceinline__ void st_shared_bf16(uint32_t at, __nv_bfloat16 x) {
-    asm volatile("st.shared.b16 [%0], %1;" ::"r"(at), "h"(__bfloat16_as_ushort(x)) : "memory");
-}
-__device__ __forceinline__ __nv_bfloat16 ld_shared_bf16(uint32_t at) {
-    unsigned short x;
-    asm volatile("ld.shared.b16 %0, [%1];" : "=h"(x) : "r"(at) : "memory");
-    return __ushort_as_bfloat16(x);
-}
-__device__ __forceinline__ void st_shared_f32(uint32_t at, float x) { asm volatile("st.shared.f32 [%0], %1;" ::"r"(at), "f"(x) : "memory"); }
-__device__ __forceinline__ float ld_shared_f32(uint32_t at) {
-    float x;
-    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(x) : "r"(at) : "memory");
-    return x;
-}
 // true in exactly one lane of a converged warp
 __device__ __forceinline__ bool elect_one() {
     uint32_t is_leader;
