@@ -272,7 +272,8 @@ int chai_decode_attention_static(const void* q, const void* k_rep, const void* v
  * bf16 (D = 128 or 64) with a positive, finite scale runs on the tcgen05 tensor-core
  * kernel; fp32 (and any other scale) on the CUDA-core kernel, a correct but far slower
  * path (milliseconds where the tensor-core kernel needs a tenth of one), which
- * chai_prefill_attention_simt selects for any dtype.
+ * chai_prefill_attention_simt selects for any dtype.  The tensor-core kernel takes scores (scale q . K) below 2^26
+ * and values below 2^60 in magnitude (the exponentials' reference lies up to 2^32 below a row's largest).
  * Errors: CHAI_ERR_INVALID_ARG / CHAI_ERR_WORKSPACE as for decode; CHAI_ERR_UNSUPPORTED for another head_dim or
  * dtype, for H or B above 65535, and when the work list of one request does not fit the planning kernel's
  * 48 KB of shared memory (4 * (H + 3 k + k * ceil(H / 32)) bytes: e.g. H = k = 512 still fits).  Inconsistent
@@ -571,8 +572,9 @@ int chai_append_rope_paged_fp8(const void* q, const void* k, const void* v, void
  * positive and finite.  CHAI_BF16 runs on the tensor cores, with probabilities rounded to bf16 and e4m3 rows as the bf16
  * numbers that they stand for, for scores (scale q . K) below 2^26 and values below 2^60 in magnitude (the exponentials'
  * reference lies up to 2^32 below a row's largest; larger numbers may leave fp32's range); CHAI_F32 on the CUDA cores.  Sums and
- * statistics are fp32.  Rows at or beyond kv_lens[b] are never used, whatever they hold.  An infinity or NaN among the cached values below kv_lens[b] may also reach tokens of its
- * request that do not see it (as zero times infinity); among keys it reaches only those that see it.
+ * statistics are fp32.  Rows at or beyond kv_lens[b] are never used, whatever they hold.  An infinity or NaN among the cached
+ * values below kv_lens[b] may also reach tokens of its request that do not see it (as zero times infinity); among keys it
+ * reaches only those that see it.
  * The workspace (chai_prefill_paged_workspace_bytes: 2^20 + 64 B + 36 H (B + n_tokens/128 + 1) + 640000 min(n_tokens, 128), whatever
  * the lengths) needs no clearing; calls that share one must be ordered on one stream.
  * H at most 1024, B below 65536, n_tokens at most 2^26, 4 (H + (k + 1) (3 + ceil(H/32))) at most 48896 bytes (the planner's

@@ -57,6 +57,7 @@ constexpr int EPILOGUE_WARPS = 4;   // one thread per query row: O / l -> bf16 -
 constexpr int PV_WARP = 2 + SOFTMAX_WARPS + EPILOGUE_WARPS;  // the warp that issues the P V batches
 constexpr int THREADS = 96 + (SOFTMAX_WARPS + EPILOGUE_WARPS) * 32;
 constexpr float REF_WINDOW = 32.f;   // log2 of how far a row's maximum may be from the softmax reference
+constexpr float EXACT_FROM = 2048.f; // log2 from where on a maximum rounded to bf16 is no reference
 constexpr uint32_t TMEM_COLS = 512;
 constexpr uint32_t S_COL0 = 0, P_COL0 = 128, O_COL0 = 256;  // S at 0..127, P buffers at 128 + 64 i, O_g at 256 + 128 g
 
@@ -391,7 +392,9 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
         const int row = quad * 32 + lane;        // row of the tile
         const int cbase = half * 64;
         const uint32_t lane_addr = tmem_base + ((uint32_t)(quad * 32) << 16);
-        __nv_bfloat16* xch = reinterpret_cast<__nv_bfloat16*>(smem + OFF_XCH);  // [tile parity][half][row]
+        // row maxima: bf16 [half][row][tile parity], or fp32 [half][row]
+        uint8_t* const xch = smem + OFF_XCH + (half * BM + row) * 4;
+        const uint8_t* const xch_other = smem + OFF_XCH + ((half ^ 1) * BM + row) * 4;
         float* lsum = reinterpret_cast<float*>(smem + OFF_LSUM);  // [half][row]
         bool ok = true;
         int it = 0, ei = 0, kt = 0;  // items seen, items handed to the epilogue, key tiles processed so far
@@ -460,32 +463,24 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
 #pragma unroll
                 for (int c = 0; c < 8; ++c) mxa[c] = -INFINITY;
                 // The two threads of a row must agree on one reference.  Each rounds its half-row maximum up to
-                // bf16 and publishes it (slots alternate with the tile's parity); both take the larger of the two
-                // rounded values, a reference slightly above the true maximum being as good.
-                __nv_bfloat16 mx_up;
-                __nv_bfloat16* xs = xch + (kt & 1) * 2 * BM;
+                // bf16 and publishes it (slots alternate with the tile's parity); the larger of the two rounded values
+                // says whether the reference may have to move.
+                float mx_own;
                 auto publish = [&]() {
-                    mx_up = __float2bfloat16_ru(max3(max3(mxa[0], mxa[1], mxa[2]), max3(mxa[3], mxa[4], mxa[5]), fmaxf(mxa[6], mxa[7])));
-                    xs[half * BM + row] = mx_up;
+                    mx_own = max3(max3(mxa[0], mxa[1], mxa[2]), max3(mxa[3], mxa[4], mxa[5]), fmaxf(mxa[6], mxa[7]));
+                    *reinterpret_cast<__nv_bfloat16*>(xch + (kt & 1) * 2) = __float2bfloat16_ru(mx_own);
                 };
-                float m_new = m_used, corr = 1.f;
-                // Meet the partner: reference of this tile, by the lazy-rescale rule above.
-                auto meet = [&]() -> bool {
-                    // The two warps of a quadrant meet at a named barrier (hardware barrier 1 + quad, 64 threads):
-                    // a fraction of the latency of an mbarrier round trip, once per tile on the path that bounds
-                    // the kernel.  It has no time limit of its own, so a warp that gives up (a bounded wait
-                    // elsewhere ran out: the abort flag is set) arrives here once on its way out, and everyone
-                    // looks at the flag right after the barrier: nobody can be left waiting for a warp that is gone.
+                // Meet the partner.  The two warps of a quadrant meet at a named barrier (hardware barrier 1 + quad, 64
+                // threads): a fraction of the latency of an mbarrier round trip, once per tile on the path that bounds
+                // the kernel.  It has no time limit of its own, so a warp that gives up (a bounded wait elsewhere ran
+                // out: the abort flag is set) arrives here once on its way out, and everyone looks at the flag right
+                // after the barrier: nobody can be left waiting for a warp that is gone.
+                auto together = [&]() -> bool {
                     asm volatile("bar.sync %0, 64;" ::"r"(quad + 1) : "memory");
-                    if (*abort_flag) return false;
-                    const float mx = fmaxf(__bfloat162float(mx_up), __bfloat162float(xs[(half ^ 1) * BM + row]));
-                    const float m_tile = mx * scale_log2;
-                    if (m_tile > m_used + REF_WINDOW || (j == 0 && m_tile < m_used - REF_WINDOW)) {
-                        m_new = m_tile;
-                        corr = j == 0 ? 1.f : fast_exp2(m_used - m_new);  // (nothing has been accumulated before the first tile)
-                    }
-                    return true;
+                    return !*abort_flag;
                 };
+                // The lazy-rescale rule above.
+                auto leaves = [&](float m) { return m > m_used + REF_WINDOW || (j == 0 && m < m_used - REF_WINDOW); };
                 // probabilities against reference m, rounded to bf16, two per 32-bit column: the layout of an A
                 // operand in tensor memory (score columns 64 h + c map to column 32 h + c / 2 of the tile's P
                 // buffer); they leave in chunks of 16 as they are ready.  Returns the row's partial sum.
@@ -530,12 +525,34 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                 // row's reference did move is the tile computed and stored again.
                 float ls = emit(m_used, std::true_type{});
                 publish();
-                ok = meet();
+                ok = together();
                 if (!ok) break;
-                const bool moved = __any_sync(0xffffffffu, m_new != m_used);  // some row of this warp changed its reference
-                if (moved) ls = emit(m_new, std::false_type{});
+                float m_tile = fmaxf(__bfloat162float(__float2bfloat16_ru(mx_own)), __bfloat162float(*reinterpret_cast<const __nv_bfloat16*>(xch_other + (kt & 1) * 2))) * scale_log2;
+                float corr = 1.f;
+                // Both warps see the same numbers and decide alike.  A rounded maximum is less than 2^-7 of itself too
+                // large: up to EXACT_FROM that is less than 16 binary orders, and as good a reference; beyond, rows
+                // would lie further below it than exponentials reach, and the maximum is exchanged in fp32.
+                bool moved = __any_sync(0xffffffffu, leaves(m_tile));
+                if (moved) {
+                    if (__any_sync(0xffffffffu, fabsf(m_tile) > EXACT_FROM)) {
+                        ok = together();  // (both have read)
+                        if (!ok) break;
+                        *reinterpret_cast<float*>(xch) = mx_own;
+                        ok = together();
+                        if (!ok) break;
+                        if (fabsf(m_tile) > EXACT_FROM) m_tile = fmaxf(mx_own, *reinterpret_cast<const float*>(xch_other)) * scale_log2;  // (a row's reference follows from its own scores)
+                        ok = together();  // (the next tile writes there)
+                        if (!ok) break;
+                    }
+                    const float m_old = m_used;
+                    if (leaves(m_tile)) {
+                        corr = j == 0 ? 1.f : fast_exp2(m_used - m_tile);  // (nothing has been accumulated before the first tile)
+                        m_used = m_tile;
+                    }
+                    moved = __any_sync(0xffffffffu, m_used != m_old);
+                    if (moved) ls = emit(m_used, std::false_type{});
+                }
                 l_run = l_run * corr + ls;
-                m_used = m_new;
                 // Rescaling touches the O accumulators, so the previous tile's P V must be complete first; a warp
                 // whose rows all keep their reference (the usual case after the first tiles) has nothing to wait
                 // for.  Skipping the wait cannot confuse the barrier's phase parity: the P V of tile kt - 3 (same
