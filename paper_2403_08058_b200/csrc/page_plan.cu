@@ -146,7 +146,7 @@ __device__ __forceinline__ void plan_tokens(const PlanArgs& a, const int* s_star
             a.slots[t0 + i] = slot[i];
         }
     }
-    if (bad) flag_status(a.hdr, CHAI_ERR_BAD_PAGE, b);
+    if (bad) atomicExch(&a.hdr->status, CHAI_ERR_BAD_PAGE);  // (whatever the requests' sums said: it comes first)
 }
 
 // One block.  TOKENS: writes the tokens too.
