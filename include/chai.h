@@ -544,7 +544,7 @@ int chai_rope(const void* q, const void* k, void* q_out, void* k_out, const int3
  *   workspace                NULL, or >= 256 bytes for the status word: CHAI_OK, or CHAI_ERR_BAD_PAGE if a slot is at or beyond
  *                            n_pages*page_size or its token_request is outside [0, B) (that token is skipped)
  * _fp8: rows become e4m3 as chai_append_kv_paged_fp8 makes them, of the rotated numbers, rounded once (what fp32 leaves in doubt
- * is worked out in fp64).  n_tokens at most 2^30.
+ * is worked out in fp64, but for the sign of what rounds to zero).  n_tokens at most 2^30.
  */
 int chai_append_rope_paged(const void* q, const void* k, const void* v, void* q_out, void* k_pages, void* v_pages,
                            const int32_t* reps, const int32_t* token_request, const int32_t* positions, const int64_t* slots,

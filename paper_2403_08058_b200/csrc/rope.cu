@@ -397,23 +397,29 @@ __global__ void __launch_bounds__(kThreads, FP8 ? 2 : 3) append_rope_kernel(cons
                     const bool turns = key && there && a.rot.rot > 0, border = near_border(m) && m >= 0x08000000u;
                     if (__any_sync(0xffffffffu, turns && (border || nearest < kMiddle))) {
                         const T* from = static_cast<const T*>(a.k) + token * a.k_stride + (long long)head[u] * D;
-                        unsigned which = 0;  // a bit an element
+                        bool again = true;  // twice at most: where the scale moves, the smallest numbers have other middles
+#pragma unroll 1
+                        for (int look = 0; look < 2 && again; ++look) {
+                            unsigned which = 0;  // a bit an element
 #pragma unroll
-                        for (int e = 0; e < EPL; ++e) {
-                            const unsigned size = finite_magnitude(y[e]);
-                            const bool close = from_middle(y[e] * pow2(-e2)) < kMiddle || (border && near_border(size) && (size ^ m) >> 23 == 0);
-                            if (turns && in_rot[e / EPV] && close) which |= 1u << e;
-                        }
-                        for (; which != 0; which &= which - 1) {
-                            const int at = __ffs(which) - 1;
-                            const float z = rotated_64<T>(a.rot, pos, from, x * EPL + at);
+                            for (int e = 0; e < EPL; ++e) {
+                                const unsigned size = finite_magnitude(y[e]);
+                                const bool close = from_middle(y[e] * pow2(-e2)) < kMiddle || (border && near_border(size) && (size ^ m) >> 23 == 0);
+                                if (turns && in_rot[e / EPV] && close) which |= 1u << e;
+                            }
+                            for (; which != 0; which &= which - 1) {
+                                const int at = __ffs(which) - 1;
+                                const float z = rotated_64<T>(a.rot, pos, from, x * EPL + at);
 #pragma unroll
-                            for (int e = 0; e < EPL; ++e)
-                                if (e == at) y[e] = z;
+                                for (int e = 0; e < EPL; ++e)
+                                    if (e == at) y[e] = z;
+                            }
+                            __syncwarp();
+                            m = largest();
+                            const int e_now = m == 0 ? 0 : scale_exponent(m);
+                            again = __any_sync(0xffffffffu, e_now != e2);
+                            e2 = e_now;
                         }
-                        __syncwarp();
-                        m = largest();
-                        e2 = m == 0 ? 0 : scale_exponent(m);
                     }
                     put_row_fp8<T, D>(a, true, r, page, row, x, there && key, y, e2);
                 }
