@@ -394,7 +394,7 @@ __global__ void __launch_bounds__(kThreads, FP8 ? 2 : 3) append_rope_kernel(cons
 #pragma unroll
                     for (int e = 0; e < EPL; ++e)
                         if (in_rot[e / EPV]) nearest = fminf(nearest, from_middle(y[e] * pow2(-e2)));
-                    const bool turns = key && there && a.rot.rot > 0, border = near_border(m) && m >= 0x08000000u;
+                    const bool turns = key && there && a.rot.rot > 0, border = near_border(m);
                     if (__any_sync(0xffffffffu, turns && (border || nearest < kMiddle))) {
                         const T* from = static_cast<const T*>(a.k) + token * a.k_stride + (long long)head[u] * D;
                         bool again = true;  // twice at most: where the scale moves, the smallest numbers have other middles

@@ -97,3 +97,16 @@ def test_bytes_where_the_scale_is_next_to_a_border(interleaved, io_bits):
     ref, _ = rotate(x, pos[:, None], turns, m, interleaved)
     assert len(set(orc.quantize_rows_fp8(ref.cpu().numpy())[1].flatten().tolist())) == 2            # both sides occur
     check(x, pos, turns, m, interleaved, decides=True)
+
+
+@pytest.mark.parametrize("bits", [-111, -113, -117, -118, -119, -121])
+def test_scales_of_tiny_rows_next_to_a_border(bits):
+    """Down to 2^-118, below which every row has the smallest scale there is."""
+    n, D = 4096, 64
+    g = torch.Generator(device=DEV).manual_seed(-bits)
+    turns, m = chai.chai_rope_frequencies(D, device=DEV)
+    pos = torch.randint(1, 3000, (n,), generator=g, device=DEV).to(torch.int32)
+    x = torch.randn(n, 1, D, generator=g, device=DEV)
+    ref, _ = rotate(x, pos[:, None], turns, m, False)
+    x = (x.double() * (1.75 / ref.abs().amax(-1, keepdim=True))).float() * 2.0 ** bits
+    check(x, pos, turns, m, False, decides=bits >= -118)
