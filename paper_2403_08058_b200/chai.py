@@ -784,18 +784,29 @@ def _turns(turns, dev):
 
 
 def _rotated_like(x):
-    """An array of x's strides, or, where x has one row for many, a dense one."""
-    strides = x.stride()
-    return torch.empty(x.shape, device=x.device, dtype=x.dtype) if 0 in strides else torch.empty_strided(x.shape, strides, device=x.device, dtype=x.dtype)
+    """A dense array with x's rows in their order in memory; in that of the indexes where one row stands for many."""
+    if x.is_contiguous():
+        return torch.empty_like(x)
+    shape, strides = x.shape, x.stride()
+    _, H, N, D = shape
+    if 0 in strides:
+        return torch.empty(shape, device=x.device, dtype=x.dtype)
+    if strides != (N * H * D, D, H * D, 1):   # (tokens before heads: as it is)
+        dense, apart = [0, 0, 0, 1], D
+        for i in sorted((0, 1, 2), key=lambda i: (strides[i], shape[i])):
+            dense[i] = apart
+            apart *= shape[i]
+        strides = dense
+    return torch.empty_strided(shape, strides, device=x.device, dtype=x.dtype)
 
 
 _STRIDES = struct.Struct("12q")   # (an array of ctypes takes four times as long to fill)
 
 
 def chai_rope(q, k=None, positions=None, turns=None, magnitude: float = 1.0, interleaved: bool = False, q_out=None, k_out=None):
-    """q [B,Hq,N,D] and k [B,Hk,N,D] (or None) rotated by positions [B,N] int32 (None: 0 .. N-1) -> (q_out, k_out), new arrays
-    of the same strides unless given (they may be q and k themselves).  Any strides with contiguous rows, e.g.
-    x.transpose(1, 2) of [B,N,H,D]."""
+    """q [B,Hq,N,D] and k [B,Hk,N,D] (or None) rotated by positions [B,N] int32 (None: 0 .. N-1) -> (q_out, k_out), new dense
+    arrays with rows in the order of the input's unless given (they may be q and k themselves).  Any strides with contiguous
+    rows, e.g. x.transpose(1, 2) of [B,N,H,D], or of a part of one projection's output."""
     if q.dim() != 4:
         raise ValueError("q must be [B,Hq,N,D]")
     B, Hq, N, D = q.shape
