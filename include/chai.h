@@ -525,7 +525,8 @@ int chai_rope_frequencies(double* turns_host, double* magnitude_host, int rot, i
  *   positions [B,N] int32, device, or NULL: 0 .. N-1;  turns [rot/2] fp64, device;  magnitude_host: HOST, or NULL for 1
  *   strides  HOST array of 12, elements: batch, head, token of q, of q_out, of k, of k_out; NULL: all contiguous.  Multiples of
  *            16 bytes, of inputs 0 too (one row for many); the D elements of a row are contiguous
- * q_out may be q itself (same strides) and k_out k; other overlaps are not allowed.
+ * q_out may be q itself (same strides) and k_out k; other overlaps are refused, as are an output's strides that are not, in
+ * ascending order, each at least what the smaller ones span.  Arrays may lie between one another's rows if they have the same strides.
  */
 int chai_rope(const void* q, const void* k, void* q_out, void* k_out, const int32_t* positions, const double* turns, int B,
               int Hq, int Hk, int N, int D, int rot, int interleaved, const double* magnitude_host, const int64_t* strides, int dtype,

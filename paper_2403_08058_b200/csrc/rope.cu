@@ -177,6 +177,71 @@ __global__ void __launch_bounds__(kThreads) rope_kernel(const __grid_constant__ 
     }
 }
 
+// Rows of an array: D elements each, `stride` elements apart along every index; a single index has no stride.
+struct Rows {
+    const char* base;
+    long long stride[3], size[3];
+};
+Rows rows_of(const Strided& x, bool out, int B, int N) {
+    Rows r = {static_cast<const char*>(out ? x.out : x.in), {out ? x.ob : x.b, out ? x.oh : x.h, out ? x.on : x.n}, {B, x.heads, N}};
+    for (int i = 0; i < 3; ++i)
+        if (r.size[i] == 1 || r.stride[i] == 0) r.size[i] = 1, r.stride[i] = 0;  // (one row for many is one row)
+    return r;
+}
+// Whether strides in ascending order are each at least what the smaller ones span: then no two rows overlap.
+bool nested(const Rows& r, int D) {
+    __int128 span = D;
+    bool done[3] = {};
+    for (int n = 0; n < 3; ++n) {
+        int at = -1;
+        for (int i = 0; i < 3; ++i)
+            if (!done[i] && (at < 0 || r.stride[i] < r.stride[at])) at = i;
+        done[at] = true;
+        if (r.size[at] == 1) continue;
+        if (r.stride[at] < span) return false;
+        span += (__int128)(r.size[at] - 1) * r.stride[at];
+    }
+    return true;
+}
+// Whether a row of x may overlap a row of y.  Exact where they have the same strides and are nested (parts of one array, say):
+// a distance of two rows is e0 s0 + e1 s1 + e2 s2, and of the largest stride only the two multiples around what is
+// to be bridged can do it.  Where strides differ, arrays are taken for the ranges that they span.
+bool rows_meet(const Rows& x, const Rows& y, int D, int es) {
+    __int128 x_span = D, y_span = D, to = ((__int128)(reinterpret_cast<intptr_t>(y.base)) - (__int128)(reinterpret_cast<intptr_t>(x.base))) / es;
+    Rows both = x;
+    bool same = true;
+    for (int i = 0; i < 3; ++i) {
+        x_span += (__int128)(x.size[i] - 1) * x.stride[i];
+        y_span += (__int128)(y.size[i] - 1) * y.stride[i];
+        if (x.size[i] > 1 && y.size[i] > 1 && x.stride[i] != y.stride[i]) same = false;
+        both.stride[i] = x.size[i] > 1 ? x.stride[i] : y.stride[i];
+        both.size[i] = x.size[i] > y.size[i] ? x.size[i] : y.size[i];
+    }
+    if (to >= x_span || -to >= y_span) return false;
+    if (!same || !nested(both, D)) return true;
+    int order[3] = {0, 1, 2};  // largest stride first
+    for (int i = 0; i < 2; ++i)
+        for (int j = 0; j < 2 - i; ++j)
+            if (both.stride[order[j]] < both.stride[order[j + 1]]) {
+                const int swap = order[j];
+                order[j] = order[j + 1];
+                order[j + 1] = swap;
+            }
+    for (int pick = 0; pick < 8; ++pick) {  // of the two multiples of every stride
+        __int128 rest = to;
+        bool there = true;
+        for (int i = 0; i < 3 && there; ++i) {
+            const int at = order[i];
+            if (both.size[at] == 1) continue;
+            const __int128 s = both.stride[at], below = -rest >= 0 ? -rest / s : -((rest + s - 1) / s), e = below + (pick >> i & 1);
+            there = e >= -(__int128)(x.size[at] - 1) && e <= y.size[at] - 1;
+            rest += e * s;
+        }
+        if (there && rest < D && -rest < D) return true;
+    }
+    return false;
+}
+
 template <typename T, int D>
 int launch_rope(RopeArgs a, cudaStream_t s) {
     const int heads = a.x[0].heads + a.x[1].heads;
@@ -598,6 +663,22 @@ int chai_rope(const void* q, const void* k, void* q_out, void* k_out, const int3
             CHAI_REQUIRE(heads[i] == 0 || j < 3 || *to[j] > 0 || sizes[j % 3] <= 1, CHAI_ERR_INVALID_ARG, "%s: strides of an output must not be 0", fn);
         }
     }
+    Rows from[2], to[2];
+    const int arrays = Hk > 0 ? 2 : 1;
+    for (int i = 0; i < arrays; ++i) {
+        from[i] = rows_of(a.x[i], false, B, N);
+        to[i] = rows_of(a.x[i], true, B, N);
+        CHAI_REQUIRE(nested(to[i], D), CHAI_ERR_INVALID_ARG,
+                     "%s: rows of an output must not overlap one another (strides, in ascending order, each at least what the smaller ones span)", fn);
+    }
+    for (int i = 0; i < arrays; ++i)
+        for (int j = 0; j < arrays; ++j) {
+            bool in_place = i == j && from[i].base == to[i].base;
+            for (int d = 0; d < 3; ++d) in_place &= from[i].stride[d] == to[j].stride[d];
+            CHAI_REQUIRE(in_place || !rows_meet(from[i], to[j], D, (int)es), CHAI_ERR_INVALID_ARG,
+                         "%s: an output may be its own input, with the same strides, but not overlap an input otherwise", fn);
+        }
+    CHAI_REQUIRE(arrays < 2 || !rows_meet(to[0], to[1], D, (int)es), CHAI_ERR_INVALID_ARG, "%s: outputs must not overlap", fn);
     CHAI_LOG_CALL("%s: B=%d Hq=%d Hk=%d N=%d D=%d rot=%d interleaved=%d dtype=%d", fn, B, Hq, Hk, N, D, rot, interleaved, dtype);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     if (dtype == CHAI_BF16) return D == 128 ? launch_rope<__nv_bfloat16, 128>(a, s) : launch_rope<__nv_bfloat16, 64>(a, s);
