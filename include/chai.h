@@ -480,8 +480,10 @@ int chai_decode_attention_paged_fp8(const void* q, const void* k_pages, const vo
  *   token_request, positions [n_tokens] int32 out, slots [n_tokens] int64 out: a token's request, its position, and
  *                            page * page_size + row of where it is cached; -1, 0 and -1 behind the last token
  * First the pages of requests that end are pushed, request by request in the order of their lists (a list with an entry outside
- * [0, n_pages) is not given back; pages must not be in the list of a request that goes on).  Then, in the order of the
- * requests: one that needs p more pages (ceil((s+n)/page_size) - ceil(s/page_size)) takes the top p.  A request that
+ * [0, n_pages) is not given back).  Nothing counts who has a page: one that is in the list of a request that goes on, in two
+ * lists that end, or twice in one must not be given back here, for it would go to several requests later (a request that ends
+ * with seq_lens 0 gives nothing back; whoever shares pages pushes them when the last one has let go).  Then, in the order of
+ * the requests: one that needs p more pages (ceil((s+n)/page_size) - ceil(s/page_size)) takes the top p.  A request that
  * does not fit gets no tokens: its length is outside [0, max_pages*page_size - n], or it needs pages and its needs and those of
  * all requests before it (that fit their lists) exceed the stack, or its tokens and those of all before it exceed n_tokens.  So
  * requests are served first come, first served, except that tokens in a page that is there already need no page.

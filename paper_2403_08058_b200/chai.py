@@ -706,7 +706,8 @@ def chai_plan_paged(seq_lens, new_lens, block_table, free_pages, free_count, n_t
     """Pages for a step's tokens, from a stack of free pages: seq_lens [B] (cached positions), new_lens [B] (tokens that each
     request gets; below 0: it ends and its pages go back), block_table [B,max_pages] and free_pages [n_pages] (both written),
     free_count [1], all int32 -> (kv_lens [B], token_start [B+1], token_request [n_tokens], positions [n_tokens], slots
-    [n_tokens] int64).  kv_lens may be seq_lens; free_count is updated in place unless free_count_out is given."""
+    [n_tokens] int64).  kv_lens may be seq_lens; free_count is updated in place unless free_count_out is given.  Pages that an
+    ending request shares with any other must not be given back here: nothing counts who has a page."""
     if block_table.dim() != 2 or free_pages.dim() != 1:
         raise ValueError("block_table must be [B,max_pages] and free_pages [n_pages]")
     (B, max_pages), n_pages, dev = block_table.shape, free_pages.shape[0], block_table.get_device()
