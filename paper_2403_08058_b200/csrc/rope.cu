@@ -24,6 +24,7 @@ namespace chai {
 namespace {
 
 constexpr int kThreads = 256, kUnroll = 4;
+constexpr int kFill = 148 * 4;   // blocks that fill the GPU: four for each of its multiprocessors
 constexpr int kEnterTokens = 4;  // of a block: few, so that most of a token's rows are in flight at once behind its angles (8: 3.2 -> 3.4 us for 16)
 constexpr int kMaxPairs = 64;
 
@@ -121,7 +122,6 @@ struct RopeArgs {
     const int32_t* positions;  // [B, N] or null: 0, 1, ...
     Rotation rot;
     int B, N, heads_per_block;
-    FastDiv by_n;
 };
 
 // grid (token groups, parts of the heads).  The rows of a pass are neighbouring tokens of one head: as much of an array that has
@@ -247,7 +247,7 @@ int launch_rope(RopeArgs a, cudaStream_t s) {
     const int heads = a.x[0].heads + a.x[1].heads;
     const long long groups = ((long long)a.B * a.N + RopeShape<T, D>::TOKENS - 1) / RopeShape<T, D>::TOKENS;
     // Few tokens: the heads go to several blocks, so that there are four for every SM while each has a load for every slot
-    const long long want = (148 * 4 + groups - 1) / groups, most = (heads + kUnroll - 1) / kUnroll;
+    const long long want = (kFill + groups - 1) / groups, most = (heads + kUnroll - 1) / kUnroll;
     const int parts = (int)(want < most ? want : most);
     a.heads_per_block = (heads + parts - 1) / parts;
     rope_kernel<T, D><<<dim3((unsigned)groups, (heads + a.heads_per_block - 1) / a.heads_per_block), kThreads, 0, s>>>(a);
@@ -318,11 +318,10 @@ __device__ __noinline__ float rotated_64(const Rotation& r, int pos, const T* ro
 
 // Stores what a thread has of a row (raw, or of a rotated one the numbers y) at `row` of plane `pl` of a page; store: whether at
 // all.  The lanes of a row call this together.
-template <typename T, int D, bool FP8>
-__device__ __forceinline__ void put_row(const EnterArgs& a, bool key, int pl, unsigned page, int row, int x, bool store, const Dense<FP8>& raw) {
-    constexpr int EPL = Dense<FP8>::BYTES / (int)sizeof(T);
-    const size_t at = (size_t)page * (key ? a.k_page_stride : a.v_page_stride) + ((size_t)pl * a.page_size + row) * D + x * EPL;
-    if (store) *reinterpret_cast<uint4*>(static_cast<T*>(key ? a.k_pages : a.v_pages) + at) = raw.a;
+template <typename T, int D>
+__device__ __forceinline__ void put_row(const EnterArgs& a, bool key, int pl, unsigned page, int row, int x, bool store, const uint4& raw) {
+    const size_t at = (size_t)page * (key ? a.k_page_stride : a.v_page_stride) + ((size_t)pl * a.page_size + row) * D + x * (16 / (int)sizeof(T));
+    if (store) *reinterpret_cast<uint4*>(static_cast<T*>(key ? a.k_pages : a.v_pages) + at) = raw;
 }
 template <typename T, int D>
 __device__ __forceinline__ void put_row_fp8(const EnterArgs& a, bool key, int pl, unsigned page, int row, int x, bool store, const float* y, int e2) {
@@ -440,9 +439,7 @@ __global__ void __launch_bounds__(kThreads, FP8 ? 2 : 3) append_rope_kernel(cons
                     for (int i = 0; i < VPL; ++i) to[i] = in_rot[i] ? pack<T>(y + i * EPV) : mine[i];
                 }
                 if constexpr (!FP8) {
-                    Dense<FP8> out;
-                    out.a = in_rot[0] ? pack<T>(y) : mine[0];
-                    put_row<T, D, FP8>(a, true, r, page, row, x, there && key, out);
+                    put_row<T, D>(a, true, r, page, row, x, there && key, in_rot[0] ? pack<T>(y) : mine[0]);
                 } else {
                     if (!__any_sync(0xffffffffu, there && key)) continue;
                     auto largest = [&]() {
@@ -507,7 +504,7 @@ __global__ void __launch_bounds__(kThreads, FP8 ? 2 : 3) append_rope_kernel(cons
             const int h = h0 + u * STEP + r_off;
             const bool store = h < h_end && live;
             if constexpr (!FP8) {
-                put_row<T, D, FP8>(a, false, h, page, row, x, store, raw[u]);
+                put_row<T, D>(a, false, h, page, row, x, store, raw[u].a);
             } else {
                 float y[EPL];
                 Vec16<T>::unpack(raw[u].a, y);
@@ -531,7 +528,7 @@ int launch_enter(EnterArgs a, cudaStream_t s) {
     constexpr int LPR = D * (int)sizeof(T) / Dense<FP8>::BYTES, STEP = kThreads / LPR / kEnterTokens, UNROLL = kUnroll * 16 / Dense<FP8>::BYTES;
     const int rows = 2 * a.k_planes + a.H;
     const long long groups = ((long long)a.n_tokens + kEnterTokens - 1) / kEnterTokens;
-    const long long want = (148 * 4 + groups - 1) / groups, most = (rows + STEP * UNROLL - 1) / (STEP * UNROLL);
+    const long long want = (kFill + groups - 1) / groups, most = (rows + STEP * UNROLL - 1) / (STEP * UNROLL);
     const int parts = (int)(want < most ? want : most);
     a.rows_per_block = ((rows + parts - 1) / parts + STEP - 1) / STEP * STEP;
     CHAI_LAUNCH_DEPENDENT("append_rope_kernel launch", (append_rope_kernel<T, D, FP8>),
