@@ -500,8 +500,8 @@ int chai_plan_paged(const int32_t* seq_lens, const int32_t* new_lens, int32_t* b
                     int max_pages, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
- * Rotary positions (Section 2 of the paper: attention of decoder models; the models that it measures rotate queries and
- * keys by their positions before their product).  The first `rot` elements of a row (a multiple of 16, 0: none) are pairs,
+ * Rotary positions (Section 2 of the paper: attention of decoder models; of those that it measures, the LLaMA models rotate
+ * queries and keys by their positions before their product, while OPT learns its positions).  The first `rot` elements of a row (a multiple of 16, 0: none) are pairs,
  * i and i + rot/2, or 2i and 2i+1 with `interleaved`; at position p pair i is turned by the angle a = 2 pi p turns[i]:
  *   y1 = magnitude (x1 cos a - x2 sin a),  y2 = magnitude (x2 cos a + x1 sin a)
  * and the other elements are copied.  p turns[i] is reduced in fp64, the rest is fp32; results are rounded once.  Positions

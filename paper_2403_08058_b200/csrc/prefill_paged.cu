@@ -23,11 +23,13 @@
 //     nothing else to do then and registers for the loads (by the warp that writes accumulators out, in between, 64 tokens
 //     over 8192 in e4m3 took 243 us, not 205).
 // Bound by the cache's bytes for few tokens a request, by the softmax chain of a tile (as in prefill_tc.cu) for many; with e4m3
-// pages by their conversion to bf16, which takes issue slots and, between a tile's products and the next one's, time.
-// Measured (of 6567 GB/s, or of 1638 TFLOP/s): 16 requests of 4 tokens over up to 2048, 32 heads, 8 clusters: 54 us, 54 %; 2048 tokens
-// behind 30720: 735 - 800 us, 51 - 55 %; 24 mixed requests over up to 4096, 52 heads: 300 us, 43 % (the chunks' query tiles read their rows
-// again, after they have left L2: 1.7 GB at 5.9 TB/s, where 0.80 would do); e4m3, 4 x 64 tokens over up to 8192, 72 heads, 24
-// clusters: 205 us, 20 %.  Before the first tile stand some 10 us: the planner 3.5, the
+// pages by their conversion to bf16, which stands in the chain between a tile's products and the next one's (instructions issue in
+// 45 % of the cycles, the tensor pipe is busy in 22 %).
+// Measured (of 6567 GB/s, or of 1638 TFLOP/s), in bursts of some ten ms at 1965 MHz: 16 requests of 4 tokens over up to 2048, 32 heads,
+// 8 clusters: 54 us, 54 %; 2048 tokens behind 30720: 760 - 800 us, 51 - 53 %; 24 mixed requests over up to 4096, 52 heads: 305 us, 42 %
+// (the chunks' query tiles read their rows again, after they have left L2: 1.7 GB at 5.7 TB/s, where 0.80 would do); e4m3, 4 x 64 tokens
+// over up to 8192, 72 heads, 24 clusters: 199 us, 21 %.  Without a pause the chunk and the mixed batch draw 1000 W, the clock falls
+// to 1570 and 1450 MHz, and they take 840 - 890 and 340 - 360 us.  Before the first tile stand some 10 us: the planner 3.5, the
 // launch 1.7, finding the share 1.5, its first rows 3.
 #include <cuda.h>
 #include <math.h>
